@@ -90,6 +90,13 @@ def _log(rng, lo, hi):
 
 
 def draw(rng):
+    c = _draw(rng)
+    while work(c)["bytes"] > 1_600_000_000:            # no more than the largest listed case
+        c["L" if c.get("L", 1) > 1 else "n_copy" if "n_copy" in c else "P"] //= 2
+    return c
+
+
+def _draw(rng):
     kind = rng.choice(["attn", "attn", "attn", "commit", "import", "fork", "compact", "copy", "sample", "sample"])
     ps = rng.choice([16, 32, 64, 128])
     d = rng.choice([128, 128, 128, 64])
