@@ -370,7 +370,7 @@ def _handle(ctx, c):
     from paper_2502_06282_b200 import binding
     names = ("k_pages", "v_pages", "k_scale", "v_scale", "k_open", "v_open", "kv_len", "page_table", "refcount",
              "free_list", "n_free")
-    return binding.KV8Cache.from_tensors(ctx, {n: c[n] for n in names})
+    return binding.PagedCache.from_tensors(ctx, {n: c[n] for n in names})
 
 
 # --------------------------------------------------------------------------------------------------
@@ -404,7 +404,7 @@ def _run_attn(s):
     B, M, Hq, Hkv, d, ps = (case[k] for k in ("B", "M", "Hq", "Hkv", "d", "ps"))
     scale = 1.0 / math.sqrt(d)
     if own:
-        s["ctx"].tree_verify_attn_kv8(s["handle"], 0, B, M, s["q"], s["k_tree"], s["v_tree"], s["parent"], scale,
+        s["ctx"].tree_verify_attn_paged(s["handle"], 0, B, M, s["q"], s["k_tree"], s["v_tree"], s["parent"], scale,
                                       s["out"])
         return s["out"]
     G = Hq // Hkv
@@ -457,7 +457,7 @@ def _run_commit(s):
     case, c = s["case"], s["cache"]
     B, M, ps, L = case["B"], case["M"], case["ps"], case["L"]
     if own:
-        s["ctx"].kv8_commit(s["handle"], B, M, s["k_ptrs"], s["v_ptrs"], s["k_tree"][0].stride(0),
+        s["ctx"].paged_commit(s["handle"], B, M, s["k_ptrs"], s["v_ptrs"], s["k_tree"][0].stride(0),
                             s["k_tree"][0].stride(1), s["n_acc"], s["acc_idx"])
         return _cache_values(c)
     n = c["kv_len"][:B]
@@ -484,7 +484,7 @@ def _run_import(s):
     B, P, ps, L = case["B"], case["P"], case["ps"], case["L"]
     if own:
         src = s["k_src"][0]
-        s["ctx"].kv8_import(s["handle"], B, s["n_tokens"], 0, L, s["k_ptrs"], s["v_ptrs"], src.stride(0),
+        s["ctx"].paged_import(s["handle"], B, s["n_tokens"], 0, L, s["k_ptrs"], s["v_ptrs"], src.stride(0),
                             src.stride(1), P)
         return _cache_values(c)
     n = s["n_tokens"]
@@ -521,9 +521,9 @@ def _run_fork(s):
     case, c = s["case"], s["cache"]
     ps = case["ps"]
     if own:
-        s["ctx"].kv8_fork(s["handle"], s["src"], s["dst"])
+        s["ctx"].paged_fork(s["handle"], s["src"], s["dst"])
         forked = c["page_table"].clone(), c["kv_len"].clone()
-        s["ctx"].kv8_free(s["handle"], s["gone"])
+        s["ctx"].paged_free(s["handle"], s["gone"])
     else:
         src, dst = s["src"].long(), s["dst"].long()
         c["page_table"][dst] = c["page_table"][src]
@@ -545,8 +545,8 @@ def _run_compact(s):
     case, c = s["case"], s["cache"]
     c["book"].copy_(s["book"])
     if own:
-        s["ctx"].kv8_free(s["handle"], s["gone"])
-        s["ctx"].kv8_compact(s["handle"], s["n_moved"])
+        s["ctx"].paged_free(s["handle"], s["gone"])
+        s["ctx"].paged_compact(s["handle"], s["n_moved"])
         return {"n_moved": s["n_moved"], "cache": _cache_values(c), "free_list": _live(c)}
     _free(c, s["gone"])
     n_pages = c["refcount"].numel()
@@ -578,7 +578,7 @@ def _live(c):
 def _run_copy(s):
     c, to = s["cache"], s["to"]
     if own:
-        s["ctx"].kv8_copy_pages(s["handle"], s["to_handle"], s["src"], s["dst"])
+        s["ctx"].paged_copy(s["handle"], s["to_handle"], s["src"], s["dst"])
     else:
         src, dst = s["src"].long(), s["dst"].long()
         for x in ("k_pages", "v_pages", "k_scale", "v_scale"):
