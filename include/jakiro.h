@@ -388,6 +388,156 @@ int jk_accept_and_compact(jk_ctx* ctx, void* stream, int32_t batch, int32_t tree
                           int32_t* kv_len, int32_t* n_acc, int32_t* acc_idx, int32_t* acc_tok,
                           int32_t* bonus_tok);
 
+/* ------------------------------------------------------------------------------------------
+ * Paged 8-bit KV cache.  (The paper has no counterpart: it keeps one 16-bit cache per sequence.
+ * These calls are for servers that verify many or long sequences: the same step over a cache of
+ * half the bytes, in pages that sequences can share.)
+ *
+ * A page holds page_size consecutive tokens of one sequence, for all kv heads of a layer, as
+ * 8-bit floats (e4m3: 4 significant bits) with one scale per (page, kv head) for K and one for
+ * V.  The scale is a power of two, the smallest s >= 2^-32 with max|x| <= 448 s over the block's
+ * finite values, so that x / s and s * code are exact and a value is rounded once, to code =
+ * e4m3(x / s), ties to even; values under 2^-42 become 0, infinities the largest code, NaN stays
+ * NaN.  Page ids are the same in all layers.  Only full pages are 8-bit, and a full page is
+ * never written again: forked sequences share pages by reference count and nothing is copied on
+ * write.  The last kv_len % page_size tokens of a sequence, its open page, stay in T; token
+ * position c is row c mod (2 page_size) of the sequence's open rows, so that a call that
+ * completes a page never overwrites what the page is made from.  The step's tree tokens stay
+ * outside the cache, in T, until jk_paged_commit takes the accepted ones in.
+ *
+ * All arrays are the caller's.  Pages are taken from the end of free_list
+ * (free_list[n_free - 1] first) in the order (sequence, page), so results repeat bit for bit.
+ * The calls that change a cache check everything first and then change all or nothing: on an
+ * index out of range, a row that does not fit or a page that others share they set JK_ERR_BOUNDS
+ * in the status word of the context, and JK_ERR_CAPACITY when the free pages do not suffice; the
+ * cache is then as it was and the call can be repeated.  Calls on one cache must not overlap on
+ * the device unless all of them are jk_tree_verify_attn_paged.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+  int32_t n_layers;         /* L                                                             */
+  int32_t n_pages;          /* pages in the pool (per layer)                                 */
+  int32_t page_size;        /* tokens per page: 16, 32, 64 or 128                            */
+  int32_t max_seqs;         /* sequences (rows of page_table), <= 1024                       */
+  int32_t max_pages;        /* pages a sequence can hold (columns of page_table)             */
+  void* k_pages;            /* e4m3 [L, n_pages, Hkv, page_size, d]                          */
+  void* v_pages;
+  float* k_scale;           /* f32 [L, n_pages, Hkv]                                         */
+  float* v_scale;
+  void* k_open;             /* T [L, max_seqs, Hkv, 2 page_size, d]                          */
+  void* v_open;
+  int32_t* kv_len;          /* i32 [max_seqs] committed tokens                               */
+  int32_t* page_table;      /* i32 [max_seqs, max_pages], -1 = none                          */
+  int32_t* refcount;        /* i32 [n_pages] sequences that hold the page                    */
+  int32_t* free_list;       /* i32 [n_pages], the first n_free entries count                 */
+  int32_t* n_free;          /* i32 [1]                                                       */
+  int32_t* scratch;         /* i32 [jk_paged_scratch_ints(n_pages)]                            */
+} jk_paged;
+
+/* int32 entries of jk_paged.scratch (0 for n_pages outside 1 .. 2^24). */
+int64_t jk_paged_scratch_ints(int32_t n_pages);
+
+/* An empty cache: no sequence has tokens or pages, the free list hands out pages 0, 1, 2, ... */
+int jk_paged_init(jk_ctx* ctx, void* stream, const jk_paged* host_cache);
+
+/*
+ * Take prompts into the cache: for i < batch, tokens 0 .. n_tokens[i]-1 of source sequence i become
+ * sequence seqs[i] (seqs = NULL: i) of the layers first_layer .. first_layer + n_layers - 1; full
+ * pages are quantised, the rest goes to the open rows, kv_len is set.  Pages are taken once: a row
+ * that holds unshared pages (an earlier layer's call) keeps them.  A row that holds shared pages,
+ * or more pages than the prompt fills, and a sequence named twice set JK_ERR_BOUNDS.
+ *   n_tokens i32 [batch], 0 <= n_tokens <= src_rows
+ *   k_src, v_src  device arrays of n_layers device pointers to T [batch, Hkv, src_rows, d] with the
+ *                 strides given (elements)
+ */
+int jk_paged_import(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t batch,
+                  const int32_t* seqs, const int32_t* n_tokens, int32_t first_layer,
+                  int32_t n_layers, void* const* k_src, void* const* v_src, int64_t src_stride_b,
+                  int64_t src_stride_h, int32_t src_rows);
+
+/*
+ * Tree-masked attention of one target layer over the paged cache: jk_tree_verify_attn with, for
+ * sequence b, columns c < kv_len[b] read from its pages and open rows and column kv_len[b] + i from
+ * row i of the tree arrays.  tree_size = 1 with parent = -1 is ordinary decoding of one token.
+ *   q, out   T [B, M, Hq, d];  parent i32 [B, M], parent[i] < i, -1 for the root
+ *   k_tree, v_tree  T [B, Hkv, >= M, d] with the strides given (elements): this layer's keys and
+ *            values of the tree tokens; they have to be finite
+ * kv_len[b] < 0 or past max_pages * page_size, and a page id outside the pool, set JK_ERR_BOUNDS.
+ * With bf16 and the tensor path, softmax weights are carried with 8 significant bits, sums in
+ * fp32; otherwise everything in fp32.
+ */
+int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t layer,
+                            int32_t batch, int32_t tree_size, const void* q, const void* k_tree,
+                            const void* v_tree, int64_t tree_stride_b, int64_t tree_stride_h,
+                            const int32_t* parent, float softmax_scale, void* out);
+
+/*
+ * jk_verify_qkv for a paged cache: the rotated K and V of node i go to row i of k_tree, v_tree
+ * (T [B, Hkv, >= M, d]); positions are kv_len[b] + depth[i] with kv_len as given (jk_paged.kv_len).
+ */
+int jk_verify_qkv_tree(jk_ctx* ctx, void* stream, const void* w_qkv, int32_t batch,
+                       int32_t tree_size, const void* x, const int32_t* depth, void* q_out,
+                       void* k_tree, void* v_tree, int64_t tree_stride_b, int64_t tree_stride_h,
+                       const int32_t* kv_len, float rope_theta);
+
+/*
+ * After jk_accept_and_compact (called with n_layers = 0, kv_len = jk_paged.kv_len and cache_rows =
+ * max_pages * page_size): the root and the accepted nodes of every sequence b < batch join the
+ * cache, all layers.  kv_len[b] already counts them (1 + n_acc[b]); n_acc[b] < 0 skips a sequence.
+ * Pages this completes are taken from the free list, unless the row holds an unshared page there
+ * already, and quantised.  Repeating the call changes nothing.
+ *   k_tree, v_tree  device arrays of L device pointers to T [B, Hkv, >= M, d], strides in elements
+ *   n_acc i32 [B], acc_idx i32 [B, max_depth] as written by jk_accept_and_compact
+ */
+int jk_paged_commit(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t batch,
+                  int32_t tree_size, void* const* k_tree, void* const* v_tree,
+                  int64_t tree_stride_b, int64_t tree_stride_h, const int32_t* n_acc,
+                  const int32_t* acc_idx);
+
+/* Fork: sequence dst[i] becomes a copy of sequence src[i], i < n: it shares the full pages and
+ * gets its own open rows.  Each dst[i] has to be empty, named once and no src. */
+int jk_paged_fork(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t n, const int32_t* src,
+                const int32_t* dst);
+/* Free the sequences seqs[i], i < n, each named once (an empty one is allowed): kv_len 0, no
+ * pages.  Pages that no sequence holds any more are appended to the free list in ascending order. */
+int jk_paged_free(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t n, const int32_t* seqs);
+/* Pack the pool: with n_live pages in use, the i-th unused id below n_live takes over the i-th
+ * used page at or above it (data of all layers, reference count, table entries); afterwards the
+ * free list hands out n_live, n_live + 1, ...  n_moved i32 [1] (opt) receives the pages moved. */
+int jk_paged_compact(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t* n_moved);
+/* Copy page src_ids[i] of host_src to page dst_ids[i] of host_dst, i < n, codes and scales of all
+ * layers; the two pools agree in L, page_size, Hkv and d and may be the same.  No bookkeeping is
+ * touched.  A dst id named twice, or (same pool) also named as a source, sets JK_ERR_BOUNDS and
+ * nothing is copied. */
+int jk_paged_copy(jk_ctx* ctx, void* stream, const jk_paged* host_src, const jk_paged* host_dst,
+                      int32_t n, const int32_t* src_ids, const int32_t* dst_ids);
+
+/*
+ * Sampling with temperature, top-k, top-p and min-p from given random numbers, per row of logits:
+ * the draw of a next token, and the filtered target rows that jk_accept_and_compact (mode 1,
+ * temperature 1) takes as target_logits.
+ *   Tokens are ordered by (logit descending, index ascending).  Weights w = exp((z - z_max) / T) are
+ *   formed and summed in 64 bits (a vocabulary of 1e5 has cumulative sums 1e-5 apart, where
+ *   fp32 sums are off by 1e-6).  The kept set is the shortest of three prefixes of the order,
+ *   never empty:
+ *     top_k > 0:    the first top_k tokens
+ *     top_p < 1:    the tokens before which less than top_p of the weight of the first top_k lies
+ *     min_p > 0:    the tokens with z - z_max >= T ln(min_p), i.e. w >= min_p
+ *   The token drawn is the first kept one, in index order, whose cumulative weight exceeds u times
+ *   the kept weight.  T not above 0 keeps the first token alone (greedy).
+ *   NaN counts as -inf, +inf as the largest float.  A row of nothing but -inf gives token -1.
+ *   logits       f32 or bf16 (logits_dtype) [rows, V], row_stride elements between rows (>= V);
+ *                aligned to its element (16-byte alignment of pointer and rows is faster)
+ *   temperature, top_p, min_p  f32 [rows], top_k i32 [rows]; each may be NULL (1, 1, 0, 0 = off)
+ *   u            f32 [rows] in [0, 1); may be NULL when out_tok is
+ *   out_tok      i32 [rows] (opt)
+ *   out_logits   f32 [rows, V], dense (opt): z / T for kept tokens (0 for a greedy row's), -inf for
+ *                the others.  At least one of the two outputs has to be given.
+ */
+int jk_sample(jk_ctx* ctx, void* stream, int32_t rows, const void* logits, int32_t logits_dtype,
+              int64_t row_stride, const float* temperature, const int32_t* top_k,
+              const float* top_p, const float* min_p, const float* u, int32_t* out_tok,
+              float* out_logits);
+
 #ifdef __cplusplus
 }
 #endif

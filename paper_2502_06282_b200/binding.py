@@ -27,7 +27,9 @@ EXPORTS = ["jk_create", "jk_destroy", "jk_workspace_bytes", "jk_set_workspace", 
            "jk_profile_enable", "jk_profile_collect", "jk_profile_stage_count",
            "jk_profile_stage_name", "jk_tree_verify_attn_static", "jk_tensor_path_active",
            "jk_set_attn_kernel", "jk_profile_read", "jk_draft_pre",
-           "jk_verify_qkv", "jk_gather_accepted"]
+           "jk_verify_qkv", "jk_gather_accepted", "jk_paged_scratch_ints", "jk_paged_init",
+           "jk_paged_import", "jk_tree_verify_attn_paged", "jk_verify_qkv_tree", "jk_paged_commit",
+           "jk_paged_fork", "jk_paged_free", "jk_paged_compact", "jk_paged_copy", "jk_sample"]
 
 
 class JkConfig(C.Structure):
@@ -55,6 +57,14 @@ class JkPreWeights(C.Structure):
 class JkPreState(C.Structure):
     _fields_ = [("q", C.c_void_p), ("slot_parent", C.c_void_p), ("slot_depth", C.c_void_p),
                 ("stride_b", C.c_int64)]
+
+
+class JkPaged(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_pages", "page_size", "max_seqs",
+                                         "max_pages")] + [
+        (n, C.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale", "k_open", "v_open",
+                                  "kv_len", "page_table", "refcount", "free_list", "n_free",
+                                  "scratch")]
 
 
 _lib = None
@@ -99,6 +109,19 @@ def lib() -> C.CDLL:
                                    i64, i32, vp, f32, f32, vp]
         L.jk_verify_qkv.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, i64, i64, i32, vp, f32]
         L.jk_gather_accepted.argtypes = [vp, vp, i32, i32, vp, vp, vp, i32, vp]
+        kv = C.POINTER(JkPaged)
+        L.jk_paged_scratch_ints.argtypes = [i32]
+        L.jk_paged_init.argtypes = [vp, vp, kv]
+        L.jk_paged_import.argtypes = [vp, vp, kv, i32, vp, vp, i32, i32, vp, vp, i64, i64, i32]
+        L.jk_tree_verify_attn_paged.argtypes = [vp, vp, kv, i32, i32, i32, vp, vp, vp, i64, i64, vp,
+                                              f32, vp]
+        L.jk_verify_qkv_tree.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, i64, i64, vp, f32]
+        L.jk_paged_commit.argtypes = [vp, vp, kv, i32, i32, vp, vp, i64, i64, vp, vp]
+        L.jk_paged_fork.argtypes = [vp, vp, kv, i32, vp, vp]
+        L.jk_paged_free.argtypes = [vp, vp, kv, i32, vp]
+        L.jk_paged_compact.argtypes = [vp, vp, kv, vp]
+        L.jk_paged_copy.argtypes = [vp, vp, kv, kv, i32, vp, vp]
+        L.jk_sample.argtypes = [vp, vp, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp]
         L.jk_profile_enable.argtypes = [vp, i32]
         L.jk_profile_collect.argtypes = [vp, vp, C.POINTER(f32), C.POINTER(i32)]
         L.jk_profile_read.argtypes = [vp, vp, C.POINTER(f32), C.POINTER(i32)]
@@ -107,8 +130,9 @@ def lib() -> C.CDLL:
         L.jk_profile_stage_name.restype = C.c_char_p
         for name in EXPORTS:
             if name not in ("jk_workspace_bytes", "jk_strerror", "jk_last_cuda_error",
-                            "jk_profile_stage_name"):
+                            "jk_profile_stage_name", "jk_paged_scratch_ints"):
                 getattr(L, name).restype = C.c_int
+        L.jk_paged_scratch_ints.restype = i64
         _lib = L
     return _lib
 
@@ -287,6 +311,77 @@ class Context:
                                       _ptr(n_acc), _ptr(acc_idx), rows_out, _ptr(out))
         self._check(rc, "jk_gather_accepted")
 
+    def verify_qkv_tree(self, w_qkv, batch, tree_size, x, depth, q_out, k_tree, v_tree, kv_len,
+                        rope_theta):
+        """jk_verify_qkv_tree: as verify_qkv, K and V of node i at row i of k_tree / v_tree."""
+        rc = lib().jk_verify_qkv_tree(self._h, _stream(), _ptr(w_qkv), batch, tree_size, _ptr(x),
+                                      _ptr(depth), _ptr(q_out), _ptr(k_tree), _ptr(v_tree),
+                                      k_tree.stride(0), k_tree.stride(1), _ptr(kv_len),
+                                      float(rope_theta))
+        self._check(rc, "jk_verify_qkv_tree")
+
+    def tree_verify_attn_paged(self, cache: "PagedCache", layer, batch, tree_size, q, k_tree, v_tree,
+                             parent, scale, out):
+        rc = lib().jk_tree_verify_attn_paged(
+            self._h, _stream(), cache.ref, layer, batch, tree_size, q.data_ptr(),
+            k_tree.data_ptr(), v_tree.data_ptr(), k_tree.stride(0), k_tree.stride(1),
+            parent.data_ptr(), scale, out.data_ptr())
+        if rc:
+            self._check(rc, "jk_tree_verify_attn_paged")
+
+    def paged_init(self, cache: "PagedCache"):
+        self._check(lib().jk_paged_init(self._h, _stream(), cache.ref), "jk_paged_init")
+
+    def paged_import(self, cache: "PagedCache", batch, n_tokens, first_layer, n_layers, k_ptrs, v_ptrs,
+                   stride_b, stride_h, src_rows, seqs=None):
+        """k_ptrs, v_ptrs: int64 device tensors of n_layers pointers to T [batch, Hkv, src_rows, d]."""
+        rc = lib().jk_paged_import(self._h, _stream(), cache.ref, batch, _ptr(seqs), _ptr(n_tokens),
+                                 first_layer, n_layers, _ptr(k_ptrs), _ptr(v_ptrs), stride_b,
+                                 stride_h, src_rows)
+        self._check(rc, "jk_paged_import")
+
+    def paged_commit(self, cache: "PagedCache", batch, tree_size, k_ptrs, v_ptrs, stride_b, stride_h,
+                   n_acc, acc_idx):
+        """k_ptrs, v_ptrs: int64 device tensors of n_layers pointers to the layers' tree arrays."""
+        rc = lib().jk_paged_commit(self._h, _stream(), cache.ref, batch, tree_size, _ptr(k_ptrs),
+                                 _ptr(v_ptrs), stride_b, stride_h, _ptr(n_acc), _ptr(acc_idx))
+        self._check(rc, "jk_paged_commit")
+
+    def paged_fork(self, cache: "PagedCache", src, dst):
+        if src.numel() != dst.numel():
+            raise ValueError("src and dst name different numbers of sequences")
+        rc = lib().jk_paged_fork(self._h, _stream(), cache.ref, src.numel(), _ptr(src), _ptr(dst))
+        self._check(rc, "jk_paged_fork")
+
+    def paged_free(self, cache: "PagedCache", seqs):
+        rc = lib().jk_paged_free(self._h, _stream(), cache.ref, seqs.numel(), _ptr(seqs))
+        self._check(rc, "jk_paged_free")
+
+    def paged_compact(self, cache: "PagedCache", n_moved=None):
+        self._check(lib().jk_paged_compact(self._h, _stream(), cache.ref, _ptr(n_moved)),
+                    "jk_paged_compact")
+
+    def paged_copy(self, src: "PagedCache", dst: "PagedCache", src_ids, dst_ids):
+        if src_ids.numel() != dst_ids.numel():
+            raise ValueError("src_ids and dst_ids name different numbers of pages")
+        rc = lib().jk_paged_copy(self._h, _stream(), src.ref, dst.ref, src_ids.numel(),
+                                     _ptr(src_ids), _ptr(dst_ids))
+        self._check(rc, "jk_paged_copy")
+
+    def sample(self, logits, temperature=None, top_k=None, top_p=None, min_p=None, u=None,
+               out_tok=None, out_logits=None):
+        """jk_sample on logits [rows, V] (f32 or bf16; rows may be strided).  The per-row arrays
+        and the outputs are device tensors or None."""
+        if logits.dim() != 2 or logits.shape[1] != self.cfg.vocab or (
+                logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise ValueError("logits must be [rows, vocab] with contiguous rows")
+        dt = {torch.bfloat16: JK_BF16, torch.float32: JK_F32}.get(logits.dtype, -1)
+        stride = logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
+        rc = lib().jk_sample(self._h, _stream(), logits.shape[0], _ptr(logits), dt, stride,
+                             _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u),
+                             _ptr(out_tok), _ptr(out_logits))
+        self._check(rc, "jk_sample")
+
     def tree_finalize(self, batch, pool, pool_n, root_tok, tree_size, tok, parent, depth, branch,
                       qslot, anc, static_keep=None):
         ps = pool if isinstance(pool, JkPool) else self.pool_struct(pool)
@@ -334,6 +429,68 @@ class Context:
             cache_stride_h, cache_rows, _ptr(kv_len), _ptr(n_acc), _ptr(acc_idx), _ptr(acc_tok),
             _ptr(bonus_tok))
         self._check(rc, "jk_accept_and_compact")
+
+
+class PagedCache:
+    """A paged 8-bit KV cache (jk_paged): the device tensors, as attributes, and the descriptor that
+    the calls take.  `PagedCache(ctx, ...)` allocates an empty one; `from_tensors` wraps tensors the
+    caller already has."""
+
+    _NAMES = ("k_pages", "v_pages", "k_scale", "v_scale", "k_open", "v_open", "kv_len",
+              "page_table", "refcount", "free_list", "n_free")
+
+    def __init__(self, ctx: Context, *, n_layers, n_pages, page_size, max_seqs, max_pages,
+                 device="cuda"):
+        Hkv, d = ctx.cfg.n_kv_heads, ctx.cfg.head_dim
+        u8 = dict(dtype=torch.uint8, device=device)
+        f32 = dict(dtype=torch.float32, device=device)
+        i32 = dict(dtype=torch.int32, device=device)
+        T = dict(dtype=ctx.tdtype, device=device)
+        blocks = (n_layers, n_pages, Hkv)
+        opened = (n_layers, max_seqs, Hkv, 2 * page_size, d)
+        self._wrap(ctx, {
+            "k_pages": torch.empty(*blocks, page_size, d, **u8),
+            "v_pages": torch.empty(*blocks, page_size, d, **u8),
+            "k_scale": torch.empty(*blocks, **f32), "v_scale": torch.empty(*blocks, **f32),
+            "k_open": torch.empty(*opened, **T), "v_open": torch.empty(*opened, **T),
+            "kv_len": torch.empty(max_seqs, **i32),
+            "page_table": torch.empty(max_seqs, max_pages, **i32),
+            "refcount": torch.empty(n_pages, **i32), "free_list": torch.empty(n_pages, **i32),
+            "n_free": torch.empty(1, **i32)})
+        ctx.paged_init(self)
+
+    @classmethod
+    def from_tensors(cls, ctx: Context, tensors: Dict[str, torch.Tensor]) -> "PagedCache":
+        """The tensors of a cache under the names of jk_paged (without scratch), already filled."""
+        self = cls.__new__(cls)
+        self._wrap(ctx, tensors)
+        return self
+
+    def _wrap(self, ctx, t):
+        L, n_pages, Hkv, ps, d = t["k_pages"].shape
+        max_seqs, max_pages = t["page_table"].shape
+        want = {"k_pages": ((L, n_pages, Hkv, ps, d), None), "v_pages": ((L, n_pages, Hkv, ps, d), None),
+                "k_scale": ((L, n_pages, Hkv), torch.float32), "v_scale": ((L, n_pages, Hkv), torch.float32),
+                "k_open": ((L, max_seqs, Hkv, 2 * ps, d), ctx.tdtype),
+                "v_open": ((L, max_seqs, Hkv, 2 * ps, d), ctx.tdtype),
+                "kv_len": ((max_seqs,), torch.int32), "page_table": ((max_seqs, max_pages), torch.int32),
+                "refcount": ((n_pages,), torch.int32), "free_list": ((n_pages,), torch.int32),
+                "n_free": ((1,), torch.int32)}
+        if (Hkv, d) != (ctx.cfg.n_kv_heads, ctx.cfg.head_dim):
+            raise ValueError("the pages' kv heads or head size are not the context's")
+        for n in self._NAMES:
+            shape, dtype = want[n]
+            ok = t[n].element_size() == 1 if dtype is None else t[n].dtype == dtype
+            if not ok or tuple(t[n].shape) != shape or not t[n].is_contiguous():
+                raise ValueError(f"{n}: expected a contiguous {shape} tensor of its type")
+            setattr(self, n, t[n])
+        self.page_size, self.n_pages, self.n_layers = ps, n_pages, L
+        self.max_seqs, self.max_pages = max_seqs, max_pages
+        ints = lib().jk_paged_scratch_ints(n_pages)
+        self.scratch = torch.empty(max(1, ints), dtype=torch.int32, device=t["k_pages"].device)
+        self.struct = JkPaged(L, n_pages, ps, max_seqs, max_pages,
+                            *[t[n].data_ptr() for n in self._NAMES], self.scratch.data_ptr())
+        self.ref = C.byref(self.struct)
 
 
 class StepBuffers:

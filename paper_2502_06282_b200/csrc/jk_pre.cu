@@ -115,7 +115,8 @@ __global__ void __launch_bounds__(256) k_linear(
 
 // Rotary positions (LLaMA convention: pair (i, i + d/2) turns by pos / theta^(2i/d), pos = prefix
 // length + depth of the node), the rotated query kept per slot, K and V appended to the draft
-// layer's cache at row prefix length + slot.  One block per node; the angle is formed and reduced
+// layer's cache at row prefix length + slot (with slot_rows: at row slot of arrays that hold the
+// tree's nodes alone).  One block per node; the angle is formed and reduced
 // in double precision (a position of several thousand times a frequency near one loses the
 // tolerance in fp32).
 template <typename T>
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(256) k_pre_rope_scatter(
     const float* __restrict__ qkv, int F, int Hq, int Hkv, int D, float theta,
     const int32_t* __restrict__ kv_len, const int32_t* __restrict__ slot_depth, int slot_base,
     long long slot_stride, T* __restrict__ q_slots, T* __restrict__ k_cache, T* __restrict__ v_cache,
-    long long cache_sb, long long cache_sh, int cache_rows, int32_t* status) {
+    long long cache_sb, long long cache_sh, int cache_rows, int slot_rows, int32_t* status) {
   // The frequencies theta^(-2j/d) in double precision, once per block and ahead of the
   // dependency wait (they depend on nothing); per pair the angle is then one double product,
   // reduced to [-pi, pi] in double, and only the sine and cosine of the small remainder are
@@ -137,7 +138,8 @@ __global__ void __launch_bounds__(256) k_pre_rope_scatter(
   const int r = blockIdx.x, b = r / F, f = r % F;
   const int slot = slot_base + f;
   const int P = kv_len[b];
-  if (P < 0 || P + slot >= cache_rows) {
+  const int crow = slot_rows ? slot : P + slot;      // row of this node's K and V
+  if (P < 0 || crow >= cache_rows) {
     if (threadIdx.x == 0) jk_set_status(status, JK_ERR_BOUNDS);
     return;
   }
@@ -162,7 +164,7 @@ __global__ void __launch_bounds__(256) k_pre_rope_scatter(
       dst[j] = jk_from_float<T>(o1);
       dst[half + j] = jk_from_float<T>(o2);
     } else {
-      T* dst = k_cache + (size_t)b * cache_sb + (size_t)(head - Hq) * cache_sh + (size_t)(P + slot) * D;
+      T* dst = k_cache + (size_t)b * cache_sb + (size_t)(head - Hq) * cache_sh + (size_t)crow * D;
       dst[j] = jk_from_float<T>(o1);
       dst[half + j] = jk_from_float<T>(o2);
     }
@@ -170,7 +172,7 @@ __global__ void __launch_bounds__(256) k_pre_rope_scatter(
   const float* vrow = row + (size_t)(Hq + Hkv) * D;
   for (int i = threadIdx.x; i < Hkv * D; i += blockDim.x) {
     const int head = i / D, j = i % D;
-    v_cache[(size_t)b * cache_sb + (size_t)head * cache_sh + (size_t)(P + slot) * D + j] =
+    v_cache[(size_t)b * cache_sb + (size_t)head * cache_sh + (size_t)crow * D + j] =
         jk_from_float<T>(vrow[i]);
   }
 }
@@ -262,7 +264,7 @@ static int pre_impl(jk_ctx* ctx, cudaStream_t st, const jk_pre_weights* w, const
   JK_PROF(ctx, st, JK_ST_PRE_ROPE);
   jk_launch_pdl(k_pre_rope_scatter<T>, dim3(R), dim3(256), 0, st, (const float*)qkv, F, Hq, Hkv, D,
                 theta, kv_len, (const int32_t*)s->slot_depth, slot_base, (long long)s->stride_b,
-                (T*)s->q, (T*)k_cache, (T*)v_cache, (long long)sb, (long long)sh, cache_rows, status);
+                (T*)s->q, (T*)k_cache, (T*)v_cache, (long long)sb, (long long)sh, cache_rows, 0, status);
   JK_LAUNCH_CHECK(ctx);
   // With one sequence the slots of the nodes expanded so far already are a dense [M, Hq, d]
   // array (and their parents a dense list): the attention call reads them where they are.
@@ -343,11 +345,11 @@ extern "C" int jk_draft_pre(jk_ctx* ctx, void* stream, const jk_pre_weights* w,
 // ------------------------------------------------------------------------------------------
 // Verification-side steps around the tree attention of one target layer (Sec. 2.1 step 2)
 // ------------------------------------------------------------------------------------------
-extern "C" int jk_verify_qkv(jk_ctx* ctx, void* stream, const void* w_qkv, int32_t batch,
-                             int32_t tree_size, const void* x, const int32_t* depth, void* q_out,
-                             void* k_cache, void* v_cache, int64_t cache_stride_b,
-                             int64_t cache_stride_h, int32_t cache_rows, const int32_t* kv_len,
-                             float rope_theta) {
+static int verify_qkv(jk_ctx* ctx, void* stream, const void* w_qkv, int32_t batch,
+                      int32_t tree_size, const void* x, const int32_t* depth, void* q_out,
+                      void* k_cache, void* v_cache, int64_t cache_stride_b,
+                      int64_t cache_stride_h, int32_t cache_rows, const int32_t* kv_len,
+                      float rope_theta, int slot_rows) {
   if (!ctx || !w_qkv || !x || !depth || !q_out || !k_cache || !v_cache || !kv_len) return JK_ERR_NULL;
   const jk_config& c = ctx->cfg;
   if (batch < 1 || tree_size < 1 || cache_rows < tree_size || !(rope_theta > 0.f)) return JK_ERR_SHAPE;
@@ -386,14 +388,32 @@ extern "C" int jk_verify_qkv(jk_ctx* ctx, void* stream, const void* w_qkv, int32
     jk_launch_pdl(k_pre_rope_scatter<__nv_bfloat16>, dim3(R), dim3(256), 0, st, (const float*)qkv,
                   tree_size, Hq, Hkv, D, rope_theta, kv_len, depth, 0, (long long)tree_size,
                   (__nv_bfloat16*)q_out, (__nv_bfloat16*)k_cache, (__nv_bfloat16*)v_cache,
-                  (long long)cache_stride_b, (long long)cache_stride_h, cache_rows, status);
+                  (long long)cache_stride_b, (long long)cache_stride_h, cache_rows, slot_rows, status);
   else
     jk_launch_pdl(k_pre_rope_scatter<float>, dim3(R), dim3(256), 0, st, (const float*)qkv, tree_size,
                   Hq, Hkv, D, rope_theta, kv_len, depth, 0, (long long)tree_size, (float*)q_out,
                   (float*)k_cache, (float*)v_cache, (long long)cache_stride_b,
-                  (long long)cache_stride_h, cache_rows, status);
+                  (long long)cache_stride_h, cache_rows, slot_rows, status);
   JK_LAUNCH_CHECK(ctx);
   return JK_OK;
+}
+
+extern "C" int jk_verify_qkv(jk_ctx* ctx, void* stream, const void* w_qkv, int32_t batch,
+                             int32_t tree_size, const void* x, const int32_t* depth, void* q_out,
+                             void* k_cache, void* v_cache, int64_t cache_stride_b,
+                             int64_t cache_stride_h, int32_t cache_rows, const int32_t* kv_len,
+                             float rope_theta) {
+  return verify_qkv(ctx, stream, w_qkv, batch, tree_size, x, depth, q_out, k_cache, v_cache,
+                    cache_stride_b, cache_stride_h, cache_rows, kv_len, rope_theta, 0);
+}
+
+// The same for a paged cache: K and V go to arrays that hold the tree's nodes alone.
+extern "C" int jk_verify_qkv_tree(jk_ctx* ctx, void* stream, const void* w_qkv, int32_t batch,
+                                  int32_t tree_size, const void* x, const int32_t* depth, void* q_out,
+                                  void* k_tree, void* v_tree, int64_t tree_stride_b,
+                                  int64_t tree_stride_h, const int32_t* kv_len, float rope_theta) {
+  return verify_qkv(ctx, stream, w_qkv, batch, tree_size, x, depth, q_out, k_tree, v_tree,
+                    tree_stride_b, tree_stride_h, tree_size, kv_len, rope_theta, 1);
 }
 
 // out[b, 0] = hidden[b, 0]; out[b, 1 + j] = hidden[b, acc_idx[b, j]] for j < n_acc[b]; zero after.

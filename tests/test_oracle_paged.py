@@ -1,0 +1,189 @@
+"""Pins of the plain model of the paged 8-bit cache and of filtered sampling, and the refusals of the C entry
+points that need no GPU."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as pg
+from paper_2502_06282_b200 import binding as jk
+
+
+def test_e4m3_table_is_torchs():
+    codes = torch.arange(256, dtype=torch.uint8)
+    want = codes.view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(pg.E4M3, want, equal_nan=True)
+
+
+def test_e4m3_rounding_is_to_nearest_even():
+    x = np.concatenate([np.linspace(-448, 448, 20001), np.geomspace(2.0 ** -12, 448, 4001),
+                        (pg.E4M3[:126] + pg.E4M3[1:127]) / 2])                       # the ties
+    want = torch.from_numpy(x.astype(np.float32)).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    got = pg.e4m3_encode(x.astype(np.float32).astype(np.float64))
+    assert np.array_equal(got, want)
+    assert pg.e4m3_encode(np.array([1e9, -1e9, np.inf, np.nan])).tolist() == [0x7E, 0xFE, 0x7E, 0x7F]
+
+
+@pytest.mark.parametrize("amax", [448.0, 448.0000305, 1.75, 1.7500001, 3.0, 2.0 ** -24, 1e-12, 0.0, 3e38])
+def test_block_scale_is_the_smallest_power_of_two(amax):
+    s = pg.block_scale(np.array([amax, -amax / 3]))
+    assert math.frexp(s)[0] == 0.5 and s >= 2.0 ** -32
+    assert amax <= 448 * s and (s == 2.0 ** -32 or amax > 448 * s / 2)
+
+
+def test_attention_without_pages_is_tree_attention():
+    from oracle import jakiro_oracle as orc
+    rng = np.random.default_rng(0)
+    c = pg.Cache(1, 2, 16, 1, 2, 2, 8)
+    n, M = 11, 5
+    src = rng.standard_normal((2, 1, 1, 2, n, 8))
+    c.import_([0], [n], 0, src[0], src[1])
+    q, kt, vt = rng.standard_normal((1, M, 4, 8)), rng.standard_normal((1, 2, M, 8)), rng.standard_normal((1, 2, M, 8))
+    parent = np.array([[-1, 0, 0, 1, 2]])
+    got, _ = pg.tree_attention(c, 0, q, kt, vt, parent, 0.3)
+    want = orc.tree_verify_attn(q, np.concatenate([src[0][0], kt], 2), np.concatenate([src[1][0], vt], 2),
+                                np.array([n]), parent, 0.3)
+    assert np.allclose(got, want, rtol=1e-12, atol=1e-12)
+
+
+def test_commit_and_import_agree():
+    """Tokens that arrive one by one end up as the same pages as a whole prompt."""
+    rng = np.random.default_rng(1)
+    L, Hkv, d, ps, n = 2, 1, 4, 16, 53
+    src = rng.standard_normal((2, L, 1, Hkv, n, d))
+    a, b = (pg.Cache(L, 8, ps, 1, 4, Hkv, d) for _ in range(2))
+    a.import_([0], [n], 0, src[0], src[1])
+    for c in range(n):
+        b.kv_len[0] = c + 1
+        b.commit(src[0][:, :, :, c:c + 1], src[1][:, :, :, c:c + 1], [0], [[]], 1)
+    assert a.table == b.table and a.free == b.free
+    assert np.array_equal(a.pages, b.pages) and np.array_equal(a.scale, b.scale)
+    r = slice(n // ps % 2 * ps, n // ps % 2 * ps + n % ps)
+    assert np.array_equal(a.open[..., r, :], b.open[..., r, :])
+
+
+def test_fork_free_compact_bookkeeping():
+    rng = np.random.default_rng(2)
+    c = pg.Cache(1, 12, 16, 5, 4, 1, 2)
+    src = rng.standard_normal((2, 1, 3, 1, 60, 2))
+    c.import_([0, 1, 2], [60, 33, 17], 0, src[0], src[1])
+    c.fork([0, 0], [3, 4])
+    assert [c.refcount[e] for e in c.table[0][:3]] == [3, 3, 3]
+    before = c.columns(0, 0, 3, 0, [])
+    c.release([0, 1])
+    assert c.free[-2:] == [3, 4] and c.refcount[c.table[3][0]] == 2
+    assert c.compact() == 1 and sorted(set(sum((r[:3] for r in c.table), []))) == [-1, 0, 1, 2, 3]
+    assert np.array_equal(before, c.columns(0, 0, 3, 0, []))
+    with pytest.raises(pg.Refused):
+        c.fork([3], [4])
+
+
+def test_sampling_rule_by_hand():
+    z = np.log([0.4, 0.1, 0.1, 0.25, 0.15])
+    tok, kept = pg.sample_row(z, top_k=3)
+    assert kept.tolist() == [True, False, False, True, True] and tok == 0
+    assert pg.sample_row(z, top_k=4)[1].tolist() == [True, True, False, True, True]      # tie: lower index
+    assert pg.sample_row(z, top_p=0.6)[1].tolist() == [True, False, False, True, False]
+    assert pg.sample_row(z, top_p=0.0)[1].tolist() == [True, False, False, False, False]
+    assert pg.sample_row(z, min_p=0.3)[1].tolist() == [True, False, False, True, True]
+    # cumulative sums in index order over the kept: 0.4, 0.65, 0.8 of 0.8
+    assert [pg.sample_row(z, top_k=3, u=u)[0] for u in (0.0, 0.49, 0.51, 0.8, 0.82, 0.999)] == [0, 0, 3, 3, 4, 4]
+    assert pg.sample_row(z, temperature=0.0, u=0.9)[0] == 0
+    assert pg.sample_row([-np.inf, np.nan])[0] == -1
+    assert pg.sample_row([np.nan, 1.0, np.inf, np.inf], u=0.7)[0] == 3
+
+
+# ------------------------------------------------------------------------------------------
+# refusals that come back before anything is launched
+# ------------------------------------------------------------------------------------------
+ALIGNED = 1 << 20
+
+
+def _context(dtype="bf16", **kw):
+    cfg = dict(hidden=64, n_experts=2, top_k=1, inter=64, vocab=64, n_q_heads=4, n_kv_heads=2, head_dim=64,
+               max_batch=2, max_tree=8, max_depth=4, max_frontier=2, k_per_expert=2, dtype=dtype, allocate=False)
+    ctx = jk.Context(**{**cfg, **kw})
+    # a workspace nobody touches: the call itself may fail where there is no device, the pointer is kept
+    jk.lib().jk_set_workspace(ctx._h, None, ALIGNED, ctx.workspace_bytes)
+    return ctx
+
+
+def _cache(**kw):
+    f = dict(n_layers=2, n_pages=8, page_size=16, max_seqs=4, max_pages=4)
+    p = {n: ALIGNED for n, _ in jk.JkPaged._fields_[5:]}
+    return jk.JkPaged(**{**f, **p, **kw})
+
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="a made-up workspace is only given without a device")
+
+
+@no_gpu
+@pytest.mark.parametrize("change,code", [
+    (dict(page_size=48), "SHAPE"), (dict(page_size=0), "SHAPE"), (dict(n_pages=0), "SHAPE"),
+    (dict(n_pages=(1 << 24) + 1), "SHAPE"), (dict(max_seqs=1025), "SHAPE"), (dict(max_pages=0), "SHAPE"),
+    (dict(max_pages=1 << 30), "SHAPE"), (dict(n_layers=0), "SHAPE"), (dict(k_pages=None), "NULL"),
+    (dict(scratch=None), "NULL"), (dict(v_open=ALIGNED + 8), "ALIGN"), (dict(k_scale=ALIGNED + 4), "ALIGN"),
+    (dict(kv_len=ALIGNED + 2), "ALIGN")])
+def test_descriptor_refusals(change, code):
+    ctx, c = _context(), _cache(**change)
+    L, want = jk.lib(), jk.ERR[code]
+    r = C.byref(c)
+    assert L.jk_paged_init(ctx._h, None, r) == want
+    assert L.jk_paged_import(ctx._h, None, r, 1, None, ALIGNED, 0, 1, ALIGNED, ALIGNED, 2048, 1024, 16) == want
+    assert L.jk_tree_verify_attn_paged(ctx._h, None, r, 0, 1, 1, ALIGNED, ALIGNED, ALIGNED, 128, 64, ALIGNED, 1.0,
+                                     ALIGNED) == want
+    assert L.jk_paged_commit(ctx._h, None, r, 1, 1, ALIGNED, ALIGNED, 128, 64, ALIGNED, ALIGNED) == want
+    assert L.jk_paged_fork(ctx._h, None, r, 1, ALIGNED, ALIGNED) == want
+    assert L.jk_paged_free(ctx._h, None, r, 1, ALIGNED) == want
+    assert L.jk_paged_compact(ctx._h, None, r, None) == want
+    assert L.jk_paged_copy(ctx._h, None, C.byref(_cache()), r, 1, ALIGNED, ALIGNED) == want
+
+
+@no_gpu
+def test_argument_refusals():
+    ctx, c = _context(), _cache()
+    L, E, A, r = jk.lib(), jk.ERR, ALIGNED, C.byref(c)
+    attn = lambda layer=0, B=1, M=1, q=A, kt=A, sb=128, sh=64, par=A, scale=1.0, out=A: \
+        L.jk_tree_verify_attn_paged(ctx._h, None, r, layer, B, M, q, kt, A, sb, sh, par, scale, out)
+    assert attn(layer=2) == E["SHAPE"] and attn(layer=-1) == E["SHAPE"]
+    assert attn(B=0) == E["SHAPE"] and attn(M=0) == E["SHAPE"] and attn(scale=0.0) == E["SHAPE"]
+    assert attn(scale=math.nan) == E["SHAPE"]
+    assert attn(B=3) == E["CAPACITY"] and attn(M=9, sh=1024) == E["CAPACITY"]
+    assert attn(M=4) == E["SHAPE"]                               # a head's tree rows would overlap the next head's
+    assert attn(q=None) == E["NULL"] and attn(par=None) == E["NULL"]
+    assert attn(q=A + 8) == E["ALIGN"] and attn(out=A + 2) == E["ALIGN"] and attn(sh=68) == E["ALIGN"]
+    imp = lambda B=1, n=A, l0=0, nl=2, k=A, sb=2048, sh=1024, rows=16: \
+        L.jk_paged_import(ctx._h, None, r, B, None, n, l0, nl, k, A, sb, sh, rows)
+    assert imp(B=5) == E["CAPACITY"] and imp(B=0) == E["SHAPE"] and imp(l0=1) == E["SHAPE"]
+    assert imp(l0=-1) == E["SHAPE"] and imp(nl=0) == E["SHAPE"] and imp(n=None) == E["NULL"]
+    assert imp(rows=17) == E["SHAPE"] and imp(sb=2044) == E["ALIGN"] and imp(sb=-8) == E["SHAPE"]
+    com = lambda B=1, M=1, sh=64, n=A: L.jk_paged_commit(ctx._h, None, r, B, M, A, A, 128, sh, n, A)
+    assert com(B=3) == E["CAPACITY"] and com(M=9, sh=640) == E["CAPACITY"] and com(M=2) == E["SHAPE"]
+    assert com(n=None) == E["NULL"]
+    assert L.jk_paged_fork(ctx._h, None, r, 5, A, A) == E["CAPACITY"]
+    assert L.jk_paged_fork(ctx._h, None, r, 0, A, A) == E["SHAPE"]
+    assert L.jk_paged_free(ctx._h, None, r, 5, A) == E["CAPACITY"]
+    assert L.jk_paged_compact(ctx._h, None, r, A + 1) == E["ALIGN"]
+    copy = lambda d, n=1: L.jk_paged_copy(ctx._h, None, r, C.byref(d), n, A, A)
+    assert copy(_cache(page_size=32)) == E["SHAPE"] and copy(_cache(n_layers=1)) == E["SHAPE"]
+    assert copy(_cache(), n=9) == E["CAPACITY"] and copy(_cache(n_pages=4)) == E["SHAPE"]     # the same arrays
+    assert copy(_cache(v_pages=A + 4096)) == E["SHAPE"]
+    assert L.jk_paged_init(None, None, r) == E["NULL"] and L.jk_paged_init(ctx._h, None, None) == E["NULL"]
+    bare = jk.Context(hidden=64, n_experts=2, top_k=1, inter=64, vocab=64, n_q_heads=4, n_kv_heads=2, head_dim=64,
+                      max_batch=2, max_tree=8, max_depth=4, max_frontier=2, k_per_expert=2, dtype="bf16",
+                      allocate=False)
+    assert L.jk_paged_init(bare._h, None, r) == E["WORKSPACE"]
+    assert [L.jk_paged_scratch_ints(n) for n in (0, -1, (1 << 24) + 1, 1)] == [0, 0, 0, 67]
+
+
+@no_gpu
+def test_sample_refusals():
+    ctx = _context()
+    L, E, A = jk.lib(), jk.ERR, ALIGNED
+    s = lambda rows=1, z=A, dt=0, stride=64, T=None, u=A, tok=A, out=None: \
+        L.jk_sample(ctx._h, None, rows, z, dt, stride, T, None, None, None, u, tok, out)
+    assert s(rows=0) == E["SHAPE"] and s(stride=63) == E["SHAPE"] and s(dt=2) == E["DTYPE"]
+    assert s(z=None) == E["NULL"] and s(u=None) == E["NULL"] and s(tok=None) == E["NULL"]
+    assert s(z=A + 2) == E["ALIGN"] and s(T=A + 1) == E["ALIGN"] and s(tok=A + 2) == E["ALIGN"]
