@@ -6,6 +6,7 @@
 
 size_t jk_tc_partial_bytes(const jk_config& c);   // jk_gemm_tc.cu
 void jk_tc_destroy(jk_ctx* ctx);                  // jk_gemm_tc.cu
+size_t jk_paged_part_floats(const jk_config& c, int with_ml);   // jk_paged_tc.cu
 static void prof_free(jk_ctx* ctx);
 void jk_attn_tc_destroy(jk_ctx* ctx);             // jk_attn_tc.cu
 void jk_attn_cl_destroy(jk_ctx* ctx);             // jk_attn_cl.cu
@@ -94,6 +95,8 @@ static void build_layout(const jk_config& c, jk_ws_layout* L) {
   L->pre_par = take((size_t)c.max_batch * S * 4);
   L->pre_att = take((size_t)c.max_batch * S * qd * es);
   L->pre_ao = take(Rp * qd * es);
+  L->paged_o = take(jk_paged_part_floats(c, 0) * 4);
+  L->paged_ml = take(jk_paged_part_floats(c, 1) * 4);
   L->total = off;
 }
 

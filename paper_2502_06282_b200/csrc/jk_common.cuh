@@ -51,6 +51,8 @@ struct jk_ws_layout {
   size_t pre_par;       // i32 [B * S]       their parent slots, dense
   size_t pre_att;       // T   [B * S, Hq d] attention outputs of those nodes
   size_t pre_ao;        // T   [Rp, Hq d]    attention outputs of this pass's nodes (O-proj input)
+  size_t paged_o;       // f32 partials of the paged attention's CTAs, two slots each
+  size_t paged_ml;
   size_t total;
   int attn_max_split;
   size_t gemm_cnt;       // four item counters of the streaming GEMM (zero between launches)

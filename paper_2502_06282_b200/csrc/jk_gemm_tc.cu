@@ -870,21 +870,36 @@ int jk_tc_linear(jk_ctx* ctx, cudaStream_t st, const void* W, int Mrows, int Kdi
 
 // General bf16 tensor map with the 128-byte swizzle (used by the attention kernel): `rank` dims,
 // innermost first; strides in bytes for dims 1..rank-1; box extents per dim.
-int jk_tma_encode_bf16(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank,
-                       const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box) {
+static int tma_encode(jk_ctx* ctx, CUtensorMap* out, CUtensorMapDataType type, CUtensorMapSwizzle swizzle,
+                      const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                      const uint32_t* box) {
   tc_state* s = tc_get_state(ctx);
   if (!s || s->failed) return JK_ERR_CUDA;
   cuuint64_t gdim[5], gstr[4];
   cuuint32_t bx[5], es[5];
   for (int i = 0; i < rank; ++i) { gdim[i] = dims[i]; bx[i] = box[i]; es[i] = 1; }
   for (int i = 0; i + 1 < rank; ++i) gstr[i] = strides_bytes[i];
-  CUresult r = s->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
+  CUresult r = s->encode(out, type, (cuuint32_t)rank,
                          const_cast<void*>(ptr), gdim, gstr, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     snprintf(ctx->cuda_err, sizeof(ctx->cuda_err), "cuTensorMapEncodeTiled failed (%d)", (int)r);
     return JK_ERR_CUDA;
   }
   return JK_OK;
+}
+
+int jk_tma_encode_bf16(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank,
+                       const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box) {
+  return tma_encode(ctx, out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, ptr, rank, dims,
+                    strides_bytes, box);
+}
+
+// 8-bit elements; the swizzle spans a box row (64 or 128 bytes).
+int jk_tma_encode_u8(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, const uint64_t* dims,
+                     const uint64_t* strides_bytes, const uint32_t* box) {
+  return tma_encode(ctx, out, CU_TENSOR_MAP_DATA_TYPE_UINT8,
+                    box[0] == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, ptr, rank, dims,
+                    strides_bytes, box);
 }

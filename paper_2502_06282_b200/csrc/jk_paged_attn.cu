@@ -195,6 +195,11 @@ static int ka_launch(jk_ctx* ctx, cudaStream_t st, const jk_paged* c, int layer,
   return rc;
 }
 
+// jk_paged_tc.cu
+int jk_paged_attn_tc(jk_ctx* ctx, cudaStream_t st, const jk_paged* c, int layer, int B, int M, const void* q,
+                     const void* kt, const void* vt, int64_t sb, int64_t sh, const int32_t* parent, float scale,
+                     void* out);
+
 extern "C" int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_paged* c, int32_t layer,
                                        int32_t batch, int32_t tree_size, const void* q,
                                        const void* k_tree, const void* v_tree, int64_t tree_stride_b,
@@ -207,7 +212,9 @@ extern "C" int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_pag
   if (layer < 0 || layer >= c->n_layers || batch < 1 || tree_size < 1 || !(softmax_scale > 0.f))
     return JK_ERR_SHAPE;
   if (batch > g.max_batch || batch > c->max_seqs || tree_size > g.max_tree) return JK_ERR_CAPACITY;
-  if (tree_stride_b < 0 || tree_stride_h < (int64_t)tree_size * g.head_dim) return JK_ERR_SHAPE;
+  if (tree_stride_h < (int64_t)tree_size * g.head_dim ||
+      (batch > 1 && tree_stride_b < (int64_t)tree_size * g.head_dim))
+    return JK_ERR_SHAPE;
   const void* ptrs[] = {q, k_tree, v_tree, out};
   for (const void* p : ptrs)
     if (!jk_aligned16(p)) return JK_ERR_ALIGN;
@@ -215,6 +222,9 @@ extern "C" int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_pag
   if ((tree_stride_b * es) % 16 || (tree_stride_h * es) % 16) return JK_ERR_ALIGN;
   if ((rc = jk_ensure_device_info(ctx)) != JK_OK) return rc;
   cudaStream_t st = (cudaStream_t)stream;
+  if (g.dtype == JK_BF16 && ctx->tensor_path)
+    return jk_paged_attn_tc(ctx, st, c, layer, batch, tree_size, q, k_tree, v_tree, tree_stride_b, tree_stride_h,
+                            parent, softmax_scale, out);
 #define KA_CASE(T, D)                                                                              \
   return ka_launch<T, D>(ctx, st, c, layer, batch, tree_size, q, k_tree, v_tree, tree_stride_b,    \
                          tree_stride_h, parent, softmax_scale, out)

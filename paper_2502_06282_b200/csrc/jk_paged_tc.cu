@@ -1,0 +1,974 @@
+// Tensor-core (tcgen05) kernel of jk_tree_verify_attn_paged for bf16 contexts.
+//
+// For a block of query rows (pairs of a q head of the group and a tree node) and tiles of 128 keys:
+//   S^T = K Q^T   (keys on the 128 lanes, query rows on the columns), then
+//   O^T = V^T P^T (head dims on the lanes, query rows on the columns).
+// Keys on the lanes because a call has few query rows (1 .. 128 per kv head): with rows on the lanes a
+// block of 60 would leave half of the SM's sub-partitions idle in the softmax, and a single token
+// 127 of 128 lanes.  A thread owns one key: its page's scales are two constants of the thread.
+//
+// Full pages stay 8-bit up to the tensor core.  A bf16 query has 8 significant bits, an e4m3 number 4, so
+// q 2^a = hi + lo with hi = e4m3(q 2^a) and lo = e4m3(q 2^a - hi) is exact down to 2^-17 of the block's
+// largest q, and S is two e4m3 products into one fp32 accumulator.  The softmax weights go the same
+// way: p = hi + lo keeps 8 significant bits, as bf16 would.  Two e4m3 products cost what one bf16
+// product costs, and no code is ever widened.  V's scale (a power of two) is added to the logit, so
+// that p already carries it: x = s scale_k + log2(scale_v), p = 2^(x - ref), and the row sum takes
+// 2^(x - ref) / scale_v.
+//
+// ref is the (rounded up) maximum of this row in this tile, not the running one: e4m3 reaches down to
+// 2^-18 of the tile's largest weight, so what is lost of a tile is below 2^-11 of its own weight,
+// however small that is against another tile (with a running reference a long prefix behind one
+// dominant key would vanish).  So every tile has its own product O_t, and the running output is
+// kept in registers: acc = alpha acc + beta O_t with powers of two alpha, beta.
+//
+// The open page and the tree tokens are bf16 tiles at the end of the sequence (16-row boxes of either
+// array, dead rows cleared in V): the same pipeline with kind::f16 products.
+//
+// One CTA per SM; all tiles of the call are dealt out evenly in order (sequence, kv head, row block,
+// tile), so a unit (sequence, kv head, row block) spans CTAs where it has to; such a CTA leaves an
+// unnormalised partial, which k_paged_merge adds up, and a unit inside one CTA is written directly.
+// Warps: TMA producer, MMA issuer, two idle, two softmax groups of four.  Up to 64 rows the groups take
+// the two tiles of a stage (256 keys); with 128 rows each takes 64 rows of every tile.
+#include <math.h>
+
+#include "jk_paged.cuh"
+#include "jk_tcgen05.cuh"
+
+#define PT_KEYS 128
+#define PT_THREADS 384
+#define PT_MAX_CTAS 160
+#define PT_INFO 8                    // ring of stage descriptions
+#define PT_PSHIFT 8.f                // weights are scaled by 2^8: the largest lie in (2^7, 2^8]
+
+// ------------------------------------------------------------------------------------------ PTX
+__device__ __forceinline__ void pt_mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ float pt_warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <int ID, int N> __device__ __forceinline__ void pt_bar() {
+  asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(N) : "memory");
+}
+// Shared-memory matrix descriptor; layout 2 / 4 / 6 / 0 = 128 / 64 / 32-byte swizzle / none.
+__device__ __forceinline__ uint64_t pt_desc(uint32_t addr, uint32_t lbo, uint32_t sbo, uint32_t layout) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(lbo >> 4) << 16;
+  d |= (uint64_t)(sbo >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)layout << 61;
+  return d;
+}
+// Layout code of rows of `bytes` bytes (one row = one swizzle span).
+__host__ __device__ constexpr uint32_t pt_layout(int bytes) {
+  return bytes == 128 ? 2u : bytes == 64 ? 4u : bytes == 32 ? 6u : 0u;
+}
+// Byte offset of 16-byte piece c of row r in such an array.
+template <int BYTES> __device__ __forceinline__ uint32_t pt_piece(int r, int c) {
+  const int x = BYTES == 128 ? (r & 7) : BYTES == 64 ? ((r >> 1) & 3) : BYTES == 32 ? ((r >> 2) & 1) : 0;
+  return (uint32_t)(r * BYTES + ((c ^ x) << 4));
+}
+// Instruction descriptor, fp32 accumulate, M = 128; fmt 1 = bf16 (kind::f16), 0 = e4m3 (kind::f8f6f4).
+__device__ __forceinline__ uint32_t pt_idesc(uint32_t fmt, int n, int a_mn, int b_mn) {
+  return (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+         ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+// ------------------------------------------------------------------------------------------ layout
+template <int D, int NR> struct pt_cfg {
+  static constexpr bool ROWS2 = NR == 128;             // the softmax groups split the rows, not the keys
+  static constexpr int RW = ROWS2 ? 64 : NR;           // rows of a softmax group
+  static constexpr int WK = ROWS2 ? 64 : 128;          // keys of a bf16 tile
+  static constexpr int SLOT = WK * D * 2;              // a bf16 tile; two 8-bit tiles (one with ROWS2)
+  static constexpr int KST = ROWS2 || NR == 16 ? 3 : 2;
+  static constexpr int VST = ROWS2 ? 4 : NR <= 32 ? 3 : 2;
+  static constexpr int Q8 = NR * D;                    // one of the two e4m3 parts of the queries
+  static constexpr int Q16 = NR * D * 2;
+  static constexpr int PB = PT_KEYS * RW * 2;          // a group's weights: two e4m3 parts, or bf16
+  static constexpr int OFF_Q16 = 2 * Q8;
+  static constexpr int OFF_P = OFF_Q16 + Q16;
+  static constexpr int OFF_K = OFF_P + 2 * PB;
+  static constexpr int OFF_V = OFF_K + KST * SLOT;
+  static constexpr int OFF_X = OFF_V + VST * SLOT + 1024;   // (a head size of 64 reads one row group further)
+  static constexpr uint32_t COLS = 8 * RW < 32 ? 32 : 8 * RW;
+};
+
+struct pt_info {                     // one stage, written by the producer
+  int live[2];                       // live keys of the tile(s), may pass the tile's
+  int open_rows, open16;             // bf16 tile: first row past the open page's tokens, and past their padding
+  float sk[16], lsv[16], isv[16];    // per page: K scale, log2 and inverse of the V scale
+};
+
+template <int D, int NR> struct alignas(16) pt_tail {
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+  uint64_t info_full[PT_INFO], s_full[2][2], p_full[2], o_full[2], q_full;
+  uint32_t tmem_base;
+  int abort_flag;
+  long long cum[JK_MAX_ROWS + 1];    // tiles before each sequence
+  int n8[JK_MAX_ROWS], n16[JK_MAX_ROWS];
+  pt_info info[PT_INFO];
+  float q_max[8];
+  int rowoff[NR];                    // output row of each query row, -1 = none
+  alignas(16) uint32_t anc[4][NR];   // tree nodes each query row sees
+  alignas(16) float wmax[2][4][64], ref[2][64], alpha[2][2][64], beta[2][2][64], m_run[2][64], lsum[2][4][64];
+  int moved[2][2][2];                // [group][tile parity][rows / 32]: a running reference moved in this tile
+};
+
+// The stages of a segment [t0, t1) of a unit with n8 8-bit tiles in front: every role walks them.
+template <bool ROWS2> struct pt_iter {
+  int tile, t1, n8, single;
+  __device__ __forceinline__ void start(int t0, int end, int n8_) { tile = t0; t1 = end; n8 = n8_; single = 0; }
+  // n tiles (1 or 2) from `tile` on; with one tile, w = the group that takes it
+  __device__ __forceinline__ bool next(int& first, int& n, int& w, bool& wide) {
+    if (tile >= t1) return false;
+    first = tile;
+    wide = tile >= n8;
+    n = (!ROWS2 && !wide && tile + 1 < t1 && tile + 1 < n8) ? 2 : 1;
+    w = single;
+    if (n == 1) single ^= 1;
+    tile += n;
+    return true;
+  }
+};
+
+// Tiles of every sequence, and their prefix sums, by one warp.  wk: keys of a bf16 tile.
+__device__ __forceinline__ void pt_count(const jk_paged& c, int B, int M, int wk, int units, int lane, long long* cum,
+                                         int* n8, int* n16, int32_t* status) {
+  long long run = 0;
+  for (int b0 = 0; b0 < B; b0 += 32) {
+    const int b = b0 + lane;
+    int a = 0, w = 0;
+    if (b < B) {
+      const int P = c.kv_len[b];
+      if (P < 0 || P > c.max_pages * c.page_size) {
+        if (status) jk_set_status(status, JK_ERR_BOUNDS);
+      } else {
+        const int nf = P / c.page_size * c.page_size;
+        a = (nf + PT_KEYS - 1) / PT_KEYS;
+        w = (((P - nf + 15) & ~15) + M + wk - 1) / wk;
+      }
+    }
+    long long incl = (long long)(a + w) * units;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    if (b < B) {
+      cum[b + 1] = run + incl;
+      n8[b] = a;
+      if (n16) n16[b] = w;
+    }
+    run += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane == 0) cum[0] = 0;
+}
+
+// ------------------------------------------------------------------------------------------ kernel
+template <int D, int NR>
+__global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
+    const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+    const __grid_constant__ CUtensorMap map_ko, const __grid_constant__ CUtensorMap map_vo,
+    const __grid_constant__ CUtensorMap map_kt, const __grid_constant__ CUtensorMap map_vt, const jk_paged c,
+    int layer, const __nv_bfloat16* __restrict__ q, const int32_t* __restrict__ parent, float scale, int B, int M,
+    int Hq, int Hkv, int n_qblk, __nv_bfloat16* __restrict__ out, float* __restrict__ part_o,
+    float* __restrict__ part_ml, int32_t* status) {
+  typedef pt_cfg<D, NR> F;
+  constexpr int RW = F::RW, KST = F::KST, VST = F::VST, WK = F::WK;
+  constexpr bool ROWS2 = F::ROWS2;
+  constexpr int KB = D / 64;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  unsigned char* sk = smem + F::OFF_K;
+  unsigned char* sv = smem + F::OFF_V;
+  typedef pt_tail<D, NR> tail_t;
+  tail_t& X = *reinterpret_cast<tail_t*>(smem + F::OFF_X);
+  volatile int* abort_flag = &X.abort_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = Hq / Hkv, units = Hkv * n_qblk, ps = c.page_size;
+
+  if (tid == 0) {
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&X.k_full[i], 1); mbar_init(&X.k_empty[i], 1);
+      mbar_init(&X.v_full[i], 1); mbar_init(&X.v_empty[i], 1);
+    }
+    for (int i = 0; i < PT_INFO; ++i) mbar_init(&X.info_full[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&X.s_full[i][0], 1); mbar_init(&X.s_full[i][1], 1);
+      mbar_init(&X.p_full[i], 128); mbar_init(&X.o_full[i], 1);
+    }
+    mbar_init(&X.q_full, 256);
+    X.abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    tmem_alloc(&X.tmem_base, F::COLS);
+    tmem_relinquish();
+  }
+  jk_pdl_wait();
+  if (warp == 0) pt_count(c, B, M, F::WK, units, lane, X.cum, X.n8, X.n16, blockIdx.x == 0 ? status : nullptr);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = X.tmem_base;
+  const long long total = X.cum[B];
+  // with fewer tiles than CTAs the first `total` CTAs take one each (an empty share would leave a gap)
+  const long long ctas = total < gridDim.x ? total : gridDim.x;
+  const bool idle = blockIdx.x >= ctas;
+  const long long w0 = idle ? 0 : total * blockIdx.x / ctas, w1 = idle ? 0 : total * (blockIdx.x + 1) / ctas;
+  bool ok = true;
+
+  // a segment of the CTA's range: unit (b, u), tiles [t0, t1)
+  auto segment = [&](long long t, int& b, int& u, int& t0, int& t1, int& nt) {
+    b = 0;
+    while (X.cum[b + 1] <= t) ++b;
+    nt = X.n8[b] + X.n16[b];
+    const long long off = t - X.cum[b];
+    u = (int)(off / nt);
+    t0 = (int)(off - (long long)u * nt);
+    const long long left = w1 - t;
+    t1 = left < nt - t0 ? t0 + (int)left : nt;
+  };
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0) {
+      // ================================================================== TMA producer
+      int sc = 0;                                       // stages so far
+      const uint64_t pol = l2_policy_evict_first();
+      for (long long t = w0; t < w1 && ok;) {
+        int b, u, t0, t1, nt;
+        segment(t, b, u, t0, t1, nt);
+        t += t1 - t0;
+        const int h = u / n_qblk, n8 = X.n8[b];
+        const int P = c.kv_len[b], nf = P / ps * ps, n_pg = P / ps;
+        const int open_rows = P - nf, open16 = (open_rows + 15) & ~15;
+        const int32_t* tab = c.page_table + (size_t)b * c.max_pages;
+        pt_iter<ROWS2> it;
+        it.start(t0, t1, n8);
+        int first, n, w;
+        bool wide;
+        const int per = PT_KEYS / ps;                   // pages of a tile
+        // page id and scales of this lane's page, one stage ahead
+        int page = 0;
+        float ksc = 1.f, vsc = 1.f;
+        auto fetch = [&](int tile) {
+          const int pi = tile * per + lane;
+          page = -1;
+          if (tile < n8 && lane < 2 * per && pi < n_pg) {
+            page = tab[pi];
+            if (page < 0 || page >= c.n_pages) {
+              jk_set_status(status, JK_ERR_BOUNDS);
+              page = 0;
+            }
+            const size_t blk = ((size_t)layer * c.n_pages + page) * Hkv + h;
+            ksc = c.k_scale[blk];
+            vsc = c.v_scale[blk];
+          }
+        };
+        fetch(t0);
+        while (ok && it.next(first, n, w, wide)) {
+          const int ks = sc % KST, vs = sc % VST;
+          pt_info& I = X.info[sc % PT_INFO];
+          ok = __all_sync(0xffffffffu, mbar_wait(&X.k_empty[ks], ((sc / KST) & 1) ^ 1, abort_flag, status));
+          unsigned char* kd = sk + ks * F::SLOT;
+          unsigned char* vd = sv + vs * F::SLOT;
+          if (!wide) {
+            const int np = min(n * per, n_pg - first * per);
+            const uint32_t bytes = (uint32_t)np * ps * D;
+            const bool mine = ok && lane < np;
+            if (ok && lane == 0) mbar_expect_tx(&X.k_full[ks], bytes);
+            __syncwarp();
+            if (mine)
+              tma_load_4d_hint(kd + lane * ps * D, &map_k, 0, 0, h, layer * c.n_pages + page, &X.k_full[ks], pol);
+            if (lane < 16) {
+              const int e = (int)(__float_as_uint(vsc) >> 23) - 127;
+              I.sk[lane] = ksc;
+              I.lsv[lane] = (float)e;
+              I.isv[lane] = paged_pow2(-e);
+            }
+            if (lane < 2) I.live[lane] = min(PT_KEYS, nf - (first + lane) * PT_KEYS);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&X.info_full[sc % PT_INFO]);
+            ok = __all_sync(0xffffffffu, ok && mbar_wait(&X.v_empty[vs], ((sc / VST) & 1) ^ 1, abort_flag, status));
+            if (ok && lane == 0) mbar_expect_tx(&X.v_full[vs], bytes);
+            __syncwarp();
+            if (ok && lane < np)
+              tma_load_4d_hint(vd + lane * ps * D, &map_v, 0, 0, h, layer * c.n_pages + page, &X.v_full[vs], pol);
+            fetch(first + n);
+          } else {
+            // bf16 tile: rows g of (open rows, padded to 16, then tree rows) in boxes of 16
+            const int base = (first - n8) * WK;
+            const int g = base + (lane / KB) * 16, kb = lane % KB;
+            const bool in_open = g < open16;
+            const bool mine = lane < WK / 16 * KB && (in_open || g - open16 < M);
+            const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * 16 * 64 * 2;
+            const int row = in_open ? (nf & (2 * ps - 1)) + g : g - open16;
+            const int outer = in_open ? layer * c.max_seqs + b : b;
+            const uint32_t at = (uint32_t)kb * (WK * 128) + (lane / KB) * 16 * 128;
+            if (ok && lane == 0) mbar_expect_tx(&X.k_full[ks], bytes);
+            __syncwarp();
+            if (ok && mine)
+              tma_load_4d(kd + at, in_open ? &map_ko : &map_kt, kb * 64, row, h, outer, &X.k_full[ks]);
+            if (lane == 0) {
+              I.live[0] = open16 + M - base;
+              I.open_rows = open_rows - base;
+              I.open16 = open16 - base;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&X.info_full[sc % PT_INFO]);
+            ok = __all_sync(0xffffffffu, ok && mbar_wait(&X.v_empty[vs], ((sc / VST) & 1) ^ 1, abort_flag, status));
+            if (ok && lane == 0) mbar_expect_tx(&X.v_full[vs], bytes);
+            __syncwarp();
+            if (ok && mine)
+              tma_load_4d(vd + at, in_open ? &map_vo : &map_vt, kb * 64, row, h, outer, &X.v_full[vs]);
+          }
+          ++sc;
+        }
+      }
+      if (!ok) {
+        // gave up, possibly with copies still in flight: give them a bounded time to land
+        const unsigned long long ts = global_ns();
+        while (global_ns() - ts < 2000000ull) { /* 2 ms: far longer than any TMA copy */ }
+      }
+    } else if (warp == 1 && lane == 0) {
+      // ================================================================== MMA issuer
+      const uint32_t q8 = smem_u32(smem), q16 = smem_u32(smem + F::OFF_Q16), pb = smem_u32(smem + F::OFF_P);
+      const uint32_t ka0 = smem_u32(sk), va0 = smem_u32(sv);
+      const uint32_t id_s8 = pt_idesc(0, NR, 0, 0), id_s16 = pt_idesc(1, NR, 0, 0);
+      const uint32_t id_p8 = pt_idesc(0, RW, 1, 1), id_p16 = pt_idesc(1, RW, 1, 1);
+      int ks_n = 0, vs_n = 0, cs[2] = {0, 0}, cp[2] = {0, 0}, segs = 0;
+      auto issue_s = [&](int n, int w, bool wide) {
+        const int slot = ks_n % KST;
+        if (!mbar_wait(&X.k_full[slot], (ks_n / KST) & 1, abort_flag, status)) { ok = false; return; }
+        tc_fence_after();
+        const uint32_t ka = ka0 + slot * F::SLOT;
+        for (int j = 0; j < n; ++j) {
+          const int g = ROWS2 ? 0 : (n == 2 ? j : w);   // group whose columns take the tile
+          const uint32_t d = tmem + (cs[g] & 1) * 2 * RW + g * RW;
+          if (!wide) {
+            const uint32_t kt = ka + j * (PT_KEYS * D);
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int k = 0; k < D / 32; ++k)
+                pt_mma_f8(d, pt_desc(kt + k * 32, 16, 8 * D, pt_layout(D)),
+                          pt_desc(q8 + part * F::Q8 + k * 32, 16, 8 * D, pt_layout(D)), id_s8, (part | k) ? 1u : 0u);
+          } else {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                tc_mma_bf16(d, pt_desc(ka + kb * (WK * 128) + k * 32, 16, 1024, 2),
+                            pt_desc(q16 + kb * (NR * 128) + k * 32, 16, 1024, 2), id_s16, (kb | k) ? 1u : 0u);
+          }
+          tc_commit(&X.s_full[g][cs[g] & 1]);
+          ++cs[g];
+          if (ROWS2) {
+            tc_commit(&X.s_full[1][cs[1] & 1]);
+            ++cs[1];
+          }
+        }
+        tc_commit(&X.k_empty[slot]);
+        ++ks_n;
+      };
+      auto issue_pv = [&](int n, int w, bool wide) {
+        const int slot = vs_n % VST;
+        if (!mbar_wait(&X.v_full[slot], (vs_n / VST) & 1, abort_flag, status)) { ok = false; return; }
+        const uint32_t va = va0 + slot * F::SLOT;
+        for (int j = 0; j < (ROWS2 ? 2 : n); ++j) {
+          const int g = (ROWS2 || n == 2) ? j : w;
+          if (!mbar_wait(&X.p_full[g], cp[g] & 1, abort_flag, status)) { ok = false; return; }
+          tc_fence_after();
+          const uint32_t d = tmem + 4 * RW + (cp[g] & 1) * 2 * RW + g * RW;
+          const uint32_t p = pb + g * F::PB;
+          if (!wide) {
+            const uint32_t vt = va + (ROWS2 ? 0 : j) * (PT_KEYS * D);
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int k = 0; k < PT_KEYS / 32; ++k)
+                pt_mma_f8(d, pt_desc(vt + k * 32 * D, 8 * D, 8 * D, pt_layout(D)),
+                          pt_desc(p + part * (PT_KEYS * RW) + k * 32 * RW, 8 * RW, 8 * RW, pt_layout(RW)), id_p8,
+                          (part | k) ? 1u : 0u);
+          } else {
+#pragma unroll
+            for (int k = 0; k < WK / 16; ++k)
+              tc_mma_bf16(d, pt_desc(va + k * 2048, KB == 2 ? WK * 128 : 1024, 1024, 2),
+                          pt_desc(p + k * 32 * RW, 16 * RW, 16 * RW, pt_layout(2 * RW)), id_p16, k ? 1u : 0u);
+          }
+          tc_commit(&X.o_full[g]);
+          ++cp[g];
+        }
+        tc_commit(&X.v_empty[slot]);
+        ++vs_n;
+      };
+      for (long long t = w0; t < w1 && ok;) {
+        int b, u, t0, t1, nt;
+        segment(t, b, u, t0, t1, nt);
+        t += t1 - t0;
+        ok = mbar_wait(&X.q_full, segs & 1, abort_flag, status);
+        ++segs;
+        if (!ok) break;
+        tc_fence_after();
+        pt_iter<ROWS2> is, ip;
+        is.start(t0, t1, X.n8[b]);
+        ip.start(t0, t1, X.n8[b]);
+        int first, n, w, ahead = 0;
+        bool wide, more = true;
+        // S runs two stages ahead of the second product: S of stage i + 2 reuses the columns of stage i,
+        // which are free once the weights of stage i have been written
+        while (ok) {
+          if (more && (more = is.next(first, n, w, wide))) {
+            issue_s(n, w, wide);
+            ++ahead;
+          }
+          if (!ok) break;
+          if (ahead == 2 || (!more && ahead > 0)) {
+            ip.next(first, n, w, wide);
+            issue_pv(n, w, wide);
+            --ahead;
+          }
+          if (!more && ahead == 0) break;
+        }
+      }
+      if (!ok) {                                        // products still in flight get a bounded time to end
+        const unsigned long long ts = global_ns();
+        while (global_ns() - ts < 2000000ull) { }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    // ==================================================================== softmax groups
+    const int g = (warp - 4) >> 2, wq = warp & 3;       // group, tensor-memory lane quarter
+    const int kl = wq * 32 + lane;                      // this thread's key of a tile / head dim of O
+    const int st = tid - 128;                           // 0 .. 255
+    const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
+    unsigned char* pbuf = smem + F::OFF_P + g * F::PB;
+    const int grow = ROWS2 ? g * 64 : 0;                // first row of this group in the block
+    int cnt = 0, sc = 0;                                // tiles of this group, stages of the CTA
+    for (long long t = w0; t < w1;) {
+      int b, u, t0, t1, nt;
+      segment(t, b, u, t0, t1, nt);
+      const bool whole = t0 == 0 && t1 == nt;
+      // a partial that does not start its unit is this CTA's first, else its last
+      const int slot = (int)(blockIdx.x * 2 + (t0 == 0 ? 1 : 0));
+      t += t1 - t0;
+      const int h = u / n_qblk, row0 = (u % n_qblk) * NR, n_rows = G * M, n8 = X.n8[b];
+      // ------------------------------------------------ queries of the unit
+      constexpr int QV = (NR * (D / 8) + 255) / 256;
+      uint4 qv[QV];
+      float amax = 0.f;
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const int idx = st + i * 256, r = idx / (D / 8), ch = idx % (D / 8);
+        qv[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < NR && row0 + r < n_rows) {
+          const int gg = (row0 + r) / M, ii = (row0 + r) % M;
+          qv[i] = *reinterpret_cast<const uint4*>(q + (((size_t)b * M + ii) * Hq + h * G + gg) * D + ch * 8);
+        }
+        const uint32_t qw[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          amax = fmaxf(amax, fmaxf(paged_mag(__uint_as_float(qw[j] << 16)),
+                                   paged_mag(__uint_as_float(qw[j] & 0xffff0000u))));
+      }
+      amax = jk_warp_max(amax);
+      if (lane == 0) X.q_max[warp - 4] = amax;
+      // (also: both groups are done with the previous unit's queries, sums and row tables)
+      pt_bar<3, 256>();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) amax = fmaxf(amax, X.q_max[i]);
+      int qe = (int)(__float_as_uint(amax) >> 23) - 127 - 8 + ((__float_as_uint(amax) & 0x7fffffu) > 0x600000u ? 1 : 0);
+      qe = max(-100, min(100, qe));
+      const float qinv = paged_pow2(-qe);
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const int idx = st + i * 256, r = idx / (D / 8), ch = idx % (D / 8);
+        if (r < NR) {
+          *reinterpret_cast<uint4*>(smem + F::OFF_Q16 + (ch >> 3) * (NR * 128) + pt_piece<128>(r, ch & 7)) = qv[i];
+          const uint32_t qw[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+          uint32_t hi[2], lo[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float v[4], back[4];
+            v[0] = __uint_as_float(qw[2 * j] << 16) * qinv;
+            v[1] = __uint_as_float(qw[2 * j] & 0xffff0000u) * qinv;
+            v[2] = __uint_as_float(qw[2 * j + 1] << 16) * qinv;
+            v[3] = __uint_as_float(qw[2 * j + 1] & 0xffff0000u) * qinv;
+            hi[j] = paged_pack4(v[0], v[1], v[2], v[3]);
+            const float2 b0 = paged_unpack2(hi[j]), b1 = paged_unpack2(hi[j] >> 16);
+            back[0] = b0.x; back[1] = b0.y; back[2] = b1.x; back[3] = b1.y;
+            lo[j] = paged_pack4(v[0] - back[0], v[1] - back[1], v[2] - back[2], v[3] - back[3]);
+          }
+          const uint32_t at = pt_piece<D>(r, ch >> 1) + (ch & 1) * 8;
+          *reinterpret_cast<uint2*>(smem + at) = make_uint2(hi[0], hi[1]);
+          *reinterpret_cast<uint2*>(smem + F::Q8 + at) = make_uint2(lo[0], lo[1]);
+        }
+      }
+      if (st < NR) {
+        const bool live = row0 + st < n_rows;
+        const int gg = live ? (row0 + st) / M : 0, ii = live ? (row0 + st) % M : 0;
+        X.rowoff[st] = live ? ii * Hq + h * G + gg : -1;
+        uint32_t a[4] = {0u, 0u, 0u, 0u};
+        if (live && t1 > n8) {                          // (only the last tiles look at it)
+          int node = ii;
+          for (int guard = 0; node >= 0 && guard <= JK_MAX_TREE; ++guard) {
+            a[node >> 5] |= 1u << (node & 31);
+            const int pp = parent[(size_t)b * M + node];
+            node = pp < node ? pp : -1;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) X.anc[i][st] = a[i];
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(&X.q_full);
+      pt_bar<3, 256>();                                 // row tables are visible
+      const float c16 = scale * 1.4426950408889634f, c8 = c16 * paged_pow2(qe);
+
+      float acc[RW], lacc[RW];
+#pragma unroll
+      for (int i = 0; i < RW; ++i) acc[i] = lacc[i] = 0.f;
+      float run = -INFINITY;                            // running reference of row kl (threads kl < RW)
+      bool pending = false;                             // the last tile's product is still to be added
+      auto take_o = [&](int count) {                    // acc = alpha acc + beta O of tile `count`
+        const int sb = count & 1;
+        if (ok) ok = mbar_wait(&X.o_full[g], count & 1, abort_flag, status);
+        __syncwarp();
+        tc_fence_after();
+        const bool moved = (X.moved[g][sb][0] | (RW == 64 ? X.moved[g][sb][1] : 0)) != 0;
+        const uint32_t oa = tmem + lane_base + 4 * RW + sb * 2 * RW + g * RW;
+        constexpr int CH = RW < 32 ? RW : 32;
+#pragma unroll
+        for (int c0 = 0; c0 < RW; c0 += CH) {
+          uint32_t r[CH];
+          if constexpr (CH == 32) tmem_ld32(oa + c0, r); else tmem_ld16(oa + c0, r);
+          tmem_ld_wait();
+          if (moved) {
+#pragma unroll
+            for (int j = 0; j < CH; j += 4) {
+              const float4 al = *reinterpret_cast<const float4*>(&X.alpha[g][sb][c0 + j]);
+              acc[c0 + j] *= al.x; acc[c0 + j + 1] *= al.y; acc[c0 + j + 2] *= al.z; acc[c0 + j + 3] *= al.w;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < CH; j += 4) {
+            const float4 be = *reinterpret_cast<const float4*>(&X.beta[g][sb][c0 + j]);
+            acc[c0 + j] = fmaf(__uint_as_float(r[j]), be.x, acc[c0 + j]);
+            acc[c0 + j + 1] = fmaf(__uint_as_float(r[j + 1]), be.y, acc[c0 + j + 1]);
+            acc[c0 + j + 2] = fmaf(__uint_as_float(r[j + 2]), be.z, acc[c0 + j + 2]);
+            acc[c0 + j + 3] = fmaf(__uint_as_float(r[j + 3]), be.w, acc[c0 + j + 3]);
+          }
+        }
+      };
+
+      pt_iter<ROWS2> it;
+      it.start(t0, t1, n8);
+      int first, n, w;
+      bool wide;
+      for (; it.next(first, n, w, wide); ++sc) {
+        if (!ROWS2 && n == 1 && w != g) continue;
+        const int part = (!ROWS2 && n == 2) ? g : 0;    // tile of the stage
+        const pt_info& I = X.info[sc % PT_INFO];
+        const int sb = cnt & 1;
+        if (ok) ok = mbar_wait(&X.info_full[sc % PT_INFO], (sc / PT_INFO) & 1, abort_flag, status);
+        float ck = c16, lsv = 0.f, isv = 1.f;
+        bool dead;
+        int tree_row = -1;
+        if (!wide) {
+          const int pg = (part * PT_KEYS + kl) / ps;
+          dead = kl >= I.live[part];
+          if (!dead) {
+            ck = c8 * I.sk[pg];
+            lsv = I.lsv[pg];
+            isv = I.isv[pg];
+          }
+        } else {
+          dead = kl >= min(WK, I.live[0]) || (kl >= I.open_rows && kl < I.open16);
+          if (kl >= I.open16) tree_row = kl - I.open16;
+        }
+        if (ok) ok = mbar_wait(&X.s_full[g][sb], (cnt >> 1) & 1, abort_flag, status);
+        __syncwarp();
+        tc_fence_after();
+        // ---- logits of this key against all rows, their maxima over the tile
+        float x[RW];
+        {
+          const uint32_t sa = tmem + lane_base + sb * 2 * RW + g * RW;
+          constexpr int CH = RW < 32 ? RW : 32;
+#pragma unroll
+          for (int c0 = 0; c0 < RW; c0 += CH) {
+            uint32_t r[CH];
+            if constexpr (CH == 32) tmem_ld32(sa + c0, r); else tmem_ld16(sa + c0, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < CH; ++j) x[c0 + j] = fmaf(__uint_as_float(r[j]), ck, lsv);
+          }
+          if (dead) {
+#pragma unroll
+            for (int j = 0; j < RW; ++j) x[j] = -INFINITY;
+          } else if (tree_row >= 0) {
+            const uint4* aw = reinterpret_cast<const uint4*>(&X.anc[(tree_row >> 5) & 3][grow]);
+            const uint32_t bit = 1u << (tree_row & 31);
+#pragma unroll
+            for (int j = 0; j < RW; j += 4) {
+              const uint4 a = aw[j >> 2];
+              if (!(a.x & bit)) x[j] = -INFINITY;
+              if (!(a.y & bit)) x[j + 1] = -INFINITY;
+              if (!(a.z & bit)) x[j + 2] = -INFINITY;
+              if (!(a.w & bit)) x[j + 3] = -INFINITY;
+            }
+          }
+        }
+        float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < RW; ++j) {
+          const float m = pt_warp_max(x[j]);
+          if (j < 32) m0 = lane == j ? m : m0; else m1 = lane == j - 32 ? m : m1;
+        }
+        if (lane < RW) X.wmax[g][wq][lane] = m0;
+        if (RW == 64) X.wmax[g][wq][32 + lane] = m1;
+        if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
+        if (kl < ((RW + 31) & ~31)) {                   // whole warps
+          bool moved = false;
+          if (kl < RW) {
+            const float m = fmaxf(fmaxf(X.wmax[g][0][kl], X.wmax[g][1][kl]), fmaxf(X.wmax[g][2][kl], X.wmax[g][3][kl]));
+            float ref = 0.f, be = 0.f, al = 1.f;
+            if (m != -INFINITY) {
+              ref = ceilf(m);
+              const float now = fmaxf(run, ref);
+              al = run == -INFINITY ? 0.f : fast_exp2(run - now);
+              be = fast_exp2(ref - now);
+              moved = run != now;
+              run = now;
+            }
+            X.ref[g][kl] = ref - PT_PSHIFT;
+            X.alpha[g][sb][kl] = al;
+            X.beta[g][sb][kl] = be;
+          }
+          const bool any = __any_sync(0xffffffffu, moved);
+          if (lane == 0) X.moved[g][sb][wq] = any;
+        }
+        if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
+        const bool moved = (X.moved[g][sb][0] | (RW == 64 ? X.moved[g][sb][1] : 0)) != 0;
+        // ---- the previous product is complete: its weights may be overwritten
+        if (pending && ok) ok = mbar_wait(&X.o_full[g], (cnt - 1) & 1, abort_flag, status);
+        if (moved) {
+#pragma unroll
+          for (int j = 0; j < RW; j += 4) {
+            const float4 al = *reinterpret_cast<const float4*>(&X.alpha[g][sb][j]);
+            lacc[j] *= al.x; lacc[j + 1] *= al.y; lacc[j + 2] *= al.z; lacc[j + 3] *= al.w;
+          }
+        }
+#pragma unroll
+        for (int j0 = 0; j0 < RW; j0 += 16) {
+          float e[16];
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) {
+            const float4 rf = *reinterpret_cast<const float4*>(&X.ref[g][j0 + j]);
+            const float4 be = *reinterpret_cast<const float4*>(&X.beta[g][sb][j0 + j]);
+            e[j] = fast_exp2(x[j0 + j] - rf.x);
+            e[j + 1] = fast_exp2(x[j0 + j + 1] - rf.y);
+            e[j + 2] = fast_exp2(x[j0 + j + 2] - rf.z);
+            e[j + 3] = fast_exp2(x[j0 + j + 3] - rf.w);
+            lacc[j0 + j] = fmaf(e[j], isv * be.x, lacc[j0 + j]);
+            lacc[j0 + j + 1] = fmaf(e[j + 1], isv * be.y, lacc[j0 + j + 1]);
+            lacc[j0 + j + 2] = fmaf(e[j + 2], isv * be.z, lacc[j0 + j + 2]);
+            lacc[j0 + j + 3] = fmaf(e[j + 3], isv * be.w, lacc[j0 + j + 3]);
+          }
+          if (!wide) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              // the remainder is formed in fp16 (11 significant bits where 8 are kept)
+              const __half2 h0 = __floats2half2_rn(e[4 * j], e[4 * j + 1]);
+              const __half2 h1 = __floats2half2_rn(e[4 * j + 2], e[4 * j + 3]);
+              const uint32_t p0 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&h0), __NV_SATFINITE, __NV_E4M3);
+              const uint32_t p1 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&h1), __NV_SATFINITE, __NV_E4M3);
+              const __half2_raw r0 = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)p0, __NV_E4M3);
+              const __half2_raw r1 = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)p1, __NV_E4M3);
+              const __half2 d0 = __hsub2(h0, *reinterpret_cast<const __half2*>(&r0));
+              const __half2 d1 = __hsub2(h1, *reinterpret_cast<const __half2*>(&r1));
+              const uint32_t l0 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&d0), __NV_SATFINITE, __NV_E4M3);
+              const uint32_t l1 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&d1), __NV_SATFINITE, __NV_E4M3);
+              hi[j] = p0 | (p1 << 16);
+              lo[j] = l0 | (l1 << 16);
+            }
+            const uint32_t at = pt_piece<RW>(kl, j0 >> 4);
+            *reinterpret_cast<uint4*>(pbuf + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(pbuf + PT_KEYS * RW + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          } else {
+            uint32_t pk[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(e[2 * j], e[2 * j + 1]);
+              pk[j] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+            *reinterpret_cast<uint4*>(pbuf + pt_piece<2 * RW>(kl, j0 >> 3)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            *reinterpret_cast<uint4*>(pbuf + pt_piece<2 * RW>(kl, (j0 >> 3) + 1)) = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+          }
+        }
+        // rows of V that no live key owns may hold anything, NaN included, and 0 * NaN would reach every row
+        if (dead && (!wide || kl < WK)) {
+          if (ok) ok = mbar_wait(&X.v_full[sc % VST], (sc / VST) & 1, abort_flag, status);
+          unsigned char* row = sv + (sc % VST) * F::SLOT + (wide ? kl * 128 : part * (PT_KEYS * D) + kl * D);
+          if (ok) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (wide) *reinterpret_cast<uint4*>(row + kb * (WK * 128) + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+                else if (kb * 8 + j < D / 16) *reinterpret_cast<uint4*>(row + (kb * 8 + j) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        mbar_arrive(&X.p_full[g]);
+        if (pending) take_o(cnt - 1);
+        pending = true;
+        ++cnt;
+      }
+      if (pending) take_o(cnt - 1);
+      tc_fence_before();
+
+      // ------------------------------------------------ the segment's result
+      if (kl < RW) X.m_run[g][kl] = run;
+      {
+        float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < RW; ++j) {
+          const float l = jk_warp_sum(lacc[j]);
+          if (j < 32) l0 = lane == j ? l : l0; else l1 = lane == j - 32 ? l : l1;
+        }
+        if (lane < RW) X.lsum[g][wq][lane] = l0;
+        if (RW == 64) X.lsum[g][wq][32 + lane] = l1;
+      }
+      float* po = part_o + (size_t)slot * NR * D;
+      float* pml = part_ml + (size_t)slot * NR * 2;
+      // weights of the two groups' sums (one group with ROWS2) for row kl; threads kl < RW
+      auto finish_row = [&](float wa, float wb, float l, float m) {
+        const float inv = whole ? 1.f / l : 1.f;
+        X.alpha[g][0][kl] = wa * inv;
+        X.beta[g][0][kl] = wb * inv;
+        if (!whole) {
+          pml[(grow + kl) * 2] = m;
+          pml[(grow + kl) * 2 + 1] = l;
+        }
+      };
+      auto store = [&](int j, float v) {                // element (row j of the group, head dim kl)
+        if (kl >= D) return;
+        if (whole) {
+          const int off = X.rowoff[grow + j];
+          if (off >= 0) out[((size_t)b * M * Hq + off) * D + kl] = __float2bfloat16_rn(v);
+        } else {
+          po[(size_t)(grow + j) * D + kl] = v;
+        }
+      };
+      if (ROWS2) {
+        if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
+        if (kl < RW)
+          finish_row(1.f, 0.f, X.lsum[g][0][kl] + X.lsum[g][1][kl] + X.lsum[g][2][kl] + X.lsum[g][3][kl], run);
+        if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
+#pragma unroll
+        for (int j = 0; j < RW; ++j) store(j, acc[j] * X.alpha[g][0][j]);
+      } else {
+        float* mb = reinterpret_cast<float*>(smem + F::OFF_P);   // [RW][128] over both groups' weights
+        pt_bar<3, 256>();                               // every product has been read: the weights are free
+        if (g == 1) {
+#pragma unroll
+          for (int j = 0; j < RW; ++j) mb[j * 128 + kl] = acc[j];
+        } else if (kl < RW) {
+          const float ma = run, mo = X.m_run[1][kl];
+          const float m = fmaxf(ma, mo);
+          const float wa = ma == -INFINITY ? 0.f : fast_exp2(ma - m), wb = mo == -INFINITY ? 0.f : fast_exp2(mo - m);
+          const float la = X.lsum[0][0][kl] + X.lsum[0][1][kl] + X.lsum[0][2][kl] + X.lsum[0][3][kl];
+          const float lb = X.lsum[1][0][kl] + X.lsum[1][1][kl] + X.lsum[1][2][kl] + X.lsum[1][3][kl];
+          finish_row(wa, wb, wa * la + wb * lb, m);
+        }
+        pt_bar<3, 256>();
+        if (g == 0) {
+#pragma unroll
+          for (int j = 0; j < RW; ++j) store(j, fmaf(acc[j], X.alpha[0][0][j], mb[j * 128 + kl] * X.beta[0][0][j]));
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, F::COLS);
+  }
+  jk_pdl_trigger();
+}
+
+// ------------------------------------------------------------------------------------------ merge
+// out = sum_s 2^(m_s - m) acc_s / sum_s 2^(m_s - m) l_s over the partials of a unit that spans CTAs; one warp
+// per query row.  CTA s holds tiles [total s / G, total (s + 1) / G), so which CTAs hold a unit's tiles, and
+// under which of its two slots, follows from the tile counts alone.
+template <int D, int NR>
+__global__ void __launch_bounds__(256) k_paged_merge(const jk_paged c, int B, int M, int Hq, int Hkv, int n_qblk,
+                                                     int grid, const float* __restrict__ part_o,
+                                                     const float* __restrict__ part_ml, __nv_bfloat16* __restrict__ out) {
+  __shared__ long long cum[JK_MAX_ROWS + 1];
+  __shared__ int n8[JK_MAX_ROWS];
+  constexpr int DPL = D / 32, NB = 8;
+  jk_pdl_wait();
+  jk_pdl_trigger();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int units = Hkv * n_qblk, G = Hq / Hkv;
+  if (warp == 0) pt_count(c, B, M, pt_cfg<D, NR>::WK, units, lane, cum, n8, nullptr, nullptr);
+  __syncthreads();
+  const int64_t row = (int64_t)blockIdx.x * 8 + warp;
+  const int64_t unit = row / NR;
+  const int r = (int)(row % NR);
+  const int b = (int)(unit / units), u = (int)(unit % units);
+  if (b >= B) return;
+  const int nr = (u % n_qblk) * NR + r;
+  if (nr >= G * M) return;
+  const long long total = cum[B], per = (cum[b + 1] - cum[b]) / units;
+  if (per == 0) return;
+  const long long a = cum[b] + (long long)u * per;
+  const long long ctas = total < grid ? total : grid;
+  const int c0 = (int)(((a + 1) * ctas - 1) / total), c1 = (int)(((a + per) * ctas - 1) / total);
+  if (c0 == c1) return;                                 // one CTA held it all and has written it
+  // slot of CTA s: its last segment where the unit begins, its first everywhere else
+  float m = -INFINITY;
+  for (int s0 = c0; s0 <= c1; s0 += 32) {
+    const int s = s0 + lane;
+    if (s <= c1) m = fmaxf(m, part_ml[((size_t)(s * 2 + (s == c0 ? 1 : 0)) * NR + r) * 2]);
+  }
+  m = jk_warp_max(m);
+  float acc[DPL], l = 0.f;
+#pragma unroll
+  for (int t = 0; t < DPL; ++t) acc[t] = 0.f;
+  for (int s0 = c0; s0 <= c1; s0 += NB) {
+    float v[NB][DPL];
+    float2 ml[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int s = s0 + j;
+      ml[j] = make_float2(-INFINITY, 0.f);
+      if (s > c1) continue;
+      const size_t at = (size_t)(s * 2 + (s == c0 ? 1 : 0)) * NR + r;
+      ml[j] = *reinterpret_cast<const float2*>(part_ml + at * 2);
+      if (DPL == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(part_o + at * D + lane * DPL);
+        v[j][0] = x.x; v[j][1] = x.y; v[j][DPL - 2] = x.z; v[j][DPL - 1] = x.w;
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(part_o + at * D + lane * DPL);
+        v[j][0] = x.x; v[j][DPL - 1] = x.y;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      if (s0 + j > c1 || ml[j].x == -INFINITY) continue;
+      const float w = fast_exp2(ml[j].x - m);
+      l = fmaf(w, ml[j].y, l);
+#pragma unroll
+      for (int t = 0; t < DPL; ++t) acc[t] = fmaf(w, v[j][t], acc[t]);
+    }
+  }
+  const float inv = 1.f / l;
+  const int gg = nr / M, ii = nr % M;
+  __nv_bfloat16* o = out + (((size_t)b * M + ii) * Hq + (u / n_qblk) * G + gg) * D + lane * DPL;
+#pragma unroll
+  for (int t = 0; t < DPL; ++t) o[t] = __float2bfloat16_rn(acc[t] * inv);
+}
+
+// ------------------------------------------------------------------------------------------ host
+int jk_tma_encode_bf16(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, const uint64_t* dims,
+                       const uint64_t* strides_bytes, const uint32_t* box);
+int jk_tma_encode_u8(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, const uint64_t* dims,
+                     const uint64_t* strides_bytes, const uint32_t* box);
+
+// Query rows of a block: the smallest of 16, 32, 64, 128 that holds the rows of a kv head, 128 past that.
+static int pt_rows(const jk_config& g, int M) {
+  const int rows = g.n_q_heads / g.n_kv_heads * M;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+}
+
+// Workspace of the partials: two slots per CTA.
+size_t jk_paged_part_floats(const jk_config& g, int with_ml) {
+  if (g.dtype != JK_BF16) return 0;
+  return (size_t)PT_MAX_CTAS * 2 * pt_rows(g, g.max_tree) * (with_ml ? 2 : g.head_dim);
+}
+
+template <int D, int NR>
+static int pt_launch(jk_ctx* ctx, cudaStream_t st, const CUtensorMap* maps, const jk_paged* c, int layer, int B, int M,
+                     const void* q, const int32_t* parent, float scale, void* out) {
+  typedef pt_cfg<D, NR> F;
+  const jk_config& g = ctx->cfg;
+  const int rows = g.n_q_heads / g.n_kv_heads * M;
+  const int n_qblk = (rows + NR - 1) / NR, units = g.n_kv_heads * n_qblk;
+  const int64_t most = (int64_t)B * units * (((int64_t)c->max_pages * c->page_size + PT_KEYS - 1) / PT_KEYS +
+                                             (c->page_size + M + F::WK - 1) / F::WK);
+  int ctas = ctx->sm_count < PT_MAX_CTAS ? ctx->sm_count : PT_MAX_CTAS;
+  if (most < ctas) ctas = (int)most;
+  const size_t smem = F::OFF_X + sizeof(pt_tail<D, NR>) + 1024;
+  static_assert(F::OFF_X + sizeof(pt_tail<D, NR>) + 1024 <= 232448, "shared memory of one CTA");
+  auto kern = k_paged_attn_tc<D, NR>;
+  JK_CUDA_CHECK(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  float* part_o = (float*)(ctx->ws + ctx->lay.paged_o);
+  float* part_ml = (float*)(ctx->ws + ctx->lay.paged_ml);
+  JK_PROF(ctx, st, JK_ST_PAGED_ATTN);
+  jk_launch_pdl(kern, dim3(ctas), dim3(PT_THREADS), smem, st, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], *c,
+                layer, (const __nv_bfloat16*)q, parent, scale, B, M, g.n_q_heads, g.n_kv_heads, n_qblk,
+                (__nv_bfloat16*)out, part_o, part_ml, (int32_t*)(ctx->ws + ctx->lay.status));
+  JK_LAUNCH_CHECK(ctx);
+  if (ctas == 1) return JK_OK;
+  JK_PROF(ctx, st, JK_ST_PAGED_COMBINE);
+  jk_launch_pdl(k_paged_merge<D, NR>, dim3((unsigned)((int64_t)B * units * NR / 8)), dim3(256), 0, st, *c, B, M,
+                g.n_q_heads, g.n_kv_heads, n_qblk, ctas, (const float*)part_o, (const float*)part_ml,
+                (__nv_bfloat16*)out);
+  JK_LAUNCH_CHECK(ctx);
+  return JK_OK;
+}
+
+// Arguments are checked.  Tensor maps are made per call (they are host arithmetic on the arguments).
+int jk_paged_attn_tc(jk_ctx* ctx, cudaStream_t st, const jk_paged* c, int layer, int B, int M, const void* q,
+                     const void* kt, const void* vt, int64_t sb, int64_t sh, const int32_t* parent, float scale,
+                     void* out) {
+  const jk_config& g = ctx->cfg;
+  const uint64_t D = g.head_dim, ps = c->page_size, H = g.n_kv_heads;
+  CUtensorMap maps[6];
+  {
+    const uint64_t dims[4] = {D, ps, H, (uint64_t)c->n_layers * c->n_pages};
+    const uint64_t strides[3] = {D, ps * D, H * ps * D};
+    const uint32_t box[4] = {(uint32_t)D, (uint32_t)ps, 1, 1};
+    int rc = jk_tma_encode_u8(ctx, &maps[0], c->k_pages, 4, dims, strides, box);
+    if (rc == JK_OK) rc = jk_tma_encode_u8(ctx, &maps[1], c->v_pages, 4, dims, strides, box);
+    if (rc != JK_OK) return rc;
+  }
+  const uint32_t box[4] = {64, 16, 1, 1};
+  {
+    const uint64_t dims[4] = {D, 2 * ps, H, (uint64_t)c->n_layers * c->max_seqs};
+    const uint64_t strides[3] = {D * 2, 2 * ps * D * 2, H * 2 * ps * D * 2};
+    int rc = jk_tma_encode_bf16(ctx, &maps[2], c->k_open, 4, dims, strides, box);
+    if (rc == JK_OK) rc = jk_tma_encode_bf16(ctx, &maps[3], c->v_open, 4, dims, strides, box);
+    if (rc != JK_OK) return rc;
+  }
+  {
+    // (rows behind the tree read as zero; with one sequence its stride is never used)
+    const uint64_t dims[4] = {D, (uint64_t)M, H, (uint64_t)B};
+    const uint64_t strides[3] = {D * 2, (uint64_t)sh * 2, B > 1 ? (uint64_t)sb * 2 : H * (uint64_t)sh * 2};
+    int rc = jk_tma_encode_bf16(ctx, &maps[4], kt, 4, dims, strides, box);
+    if (rc == JK_OK) rc = jk_tma_encode_bf16(ctx, &maps[5], vt, 4, dims, strides, box);
+    if (rc != JK_OK) return rc;
+  }
+#define PT_CASE(DD, NN) \
+  if (g.head_dim == DD && nr == NN) return pt_launch<DD, NN>(ctx, st, maps, c, layer, B, M, q, parent, scale, out)
+  const int nr = pt_rows(g, M);
+  PT_CASE(128, 16); PT_CASE(128, 32); PT_CASE(128, 64); PT_CASE(128, 128);
+  PT_CASE(64, 16); PT_CASE(64, 32); PT_CASE(64, 64); PT_CASE(64, 128);
+#undef PT_CASE
+  return JK_ERR_SHAPE;
+}
