@@ -49,10 +49,30 @@ __device__ __forceinline__ void pt_mma_f8(uint32_t d, uint64_t a, uint64_t b, ui
       ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
       : "memory");
 }
-__device__ __forceinline__ float pt_warp_max(float x) {
-  float y;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-  return y;
+// Maxima (sums) over the warp's lanes of N = 16 or 32 rows held one value per lane: lane l ends up with
+// row l mod N.  Half of the rows changes sides at every step, so 31 exchanges serve 32 rows.
+template <int N, bool SUM> __device__ __forceinline__ float pt_rows_reduce(const float* x, int lane) {
+  float v[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = x[j];
+  if (N == 16) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float y = __shfl_xor_sync(0xffffffffu, v[j], 16);
+      v[j] = SUM ? v[j] + y : fmaxf(v[j], y);
+    }
+  }
+#pragma unroll
+  for (int h = N / 2; h >= 1; h >>= 1) {
+    const bool up = lane & h;
+#pragma unroll
+    for (int j = 0; j < h; ++j) {
+      const float keep = up ? v[j + h] : v[j], send = up ? v[j] : v[j + h];
+      const float y = __shfl_xor_sync(0xffffffffu, send, h);
+      v[j] = SUM ? keep + y : fmaxf(keep, y);
+    }
+  }
+  return v[0];
 }
 template <int ID, int N> __device__ __forceinline__ void pt_bar() {
   asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(N) : "memory");
@@ -540,9 +560,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       for (int i = 0; i < RW; ++i) acc[i] = lacc[i] = 0.f;
       float run = -INFINITY;                            // running reference of row kl (threads kl < RW)
       bool pending = false;                             // the last tile's product is still to be added
-      auto take_o = [&](int count) {                    // acc = alpha acc + beta O of tile `count`
+      // acc = alpha acc + beta O of tile `count`.  Its completion has been waited for by every thread of
+      // the group: a wait here, after the arrival for the next tile, could find the barrier two phases on.
+      auto take_o = [&](int count) {
         const int sb = count & 1;
-        if (ok) ok = mbar_wait(&X.o_full[g], count & 1, abort_flag, status);
         __syncwarp();
         tc_fence_after();
         const bool moved = (X.moved[g][sb][0] | (RW == 64 ? X.moved[g][sb][1] : 0)) != 0;
@@ -628,14 +649,13 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
             }
           }
         }
-        float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < RW; ++j) {
-          const float m = pt_warp_max(x[j]);
-          if (j < 32) m0 = lane == j ? m : m0; else m1 = lane == j - 32 ? m : m1;
+        if constexpr (RW >= 32) {
+          X.wmax[g][wq][lane] = pt_rows_reduce<32, false>(x, lane);
+          if (RW == 64) X.wmax[g][wq][32 + lane] = pt_rows_reduce<32, false>(x + (RW - 32), lane);
+        } else {
+          const float m = pt_rows_reduce<16, false>(x, lane);
+          if (lane < 16) X.wmax[g][wq][lane] = m;
         }
-        if (lane < RW) X.wmax[g][wq][lane] = m0;
-        if (RW == 64) X.wmax[g][wq][32 + lane] = m1;
         if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
         if (kl < ((RW + 31) & ~31)) {                   // whole warps
           bool moved = false;
@@ -736,20 +756,20 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         pending = true;
         ++cnt;
       }
-      if (pending) take_o(cnt - 1);
+      if (pending) {
+        if (ok) ok = mbar_wait(&X.o_full[g], (cnt - 1) & 1, abort_flag, status);
+        take_o(cnt - 1);
+      }
       tc_fence_before();
 
       // ------------------------------------------------ the segment's result
       if (kl < RW) X.m_run[g][kl] = run;
-      {
-        float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-        for (int j = 0; j < RW; ++j) {
-          const float l = jk_warp_sum(lacc[j]);
-          if (j < 32) l0 = lane == j ? l : l0; else l1 = lane == j - 32 ? l : l1;
-        }
-        if (lane < RW) X.lsum[g][wq][lane] = l0;
-        if (RW == 64) X.lsum[g][wq][32 + lane] = l1;
+      if constexpr (RW >= 32) {
+        X.lsum[g][wq][lane] = pt_rows_reduce<32, true>(lacc, lane);
+        if (RW == 64) X.lsum[g][wq][32 + lane] = pt_rows_reduce<32, true>(lacc + (RW - 32), lane);
+      } else {
+        const float l = pt_rows_reduce<16, true>(lacc, lane);
+        if (lane < 16) X.lsum[g][wq][lane] = l;
       }
       float* po = part_o + (size_t)slot * NR * D;
       float* pml = part_ml + (size_t)slot * NR * 2;
