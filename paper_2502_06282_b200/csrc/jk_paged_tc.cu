@@ -27,15 +27,18 @@
 // One CTA per SM; all tiles of the call are dealt out evenly in order (sequence, kv head, row block,
 // tile), so a unit (sequence, kv head, row block) spans CTAs where it has to; such a CTA leaves an
 // unnormalised partial, which k_paged_merge adds up, and a unit inside one CTA is written directly.
-// Warps: TMA producer, MMA issuer, two idle, two softmax groups of four.  Up to 64 rows the groups take
-// the two tiles of a stage (256 keys); with 128 rows each takes 64 rows of every tile.
+// Warps: four softmax groups of four, TMA producers for K and for V, an MMA issuer.  A group takes 32 rows (16 where the block
+// has no more) of every NP-th tile: 128 rows 4 x 32, 64 rows 2 x 32 with two tiles at a time, fewer rows
+// with four.  Two groups of 64 rows each had 168 registers and spilled, two warps per scheduler to hide
+// every wait, and took twice as long.
 #include <math.h>
 
 #include "jk_paged.cuh"
 #include "jk_tcgen05.cuh"
 
 #define PT_KEYS 128
-#define PT_THREADS 384
+#define PT_SOFTMAX 512              // threads of the softmax groups
+#define PT_THREADS (PT_SOFTMAX + 96)
 #define PT_MAX_CTAS 160
 #define PT_INFO 8                    // ring of stage descriptions
 #define PT_PSHIFT 8.f                // weights are scaled by 2^8: the largest lie in (2^7, 2^8]
@@ -104,21 +107,26 @@ __device__ __forceinline__ uint32_t pt_idesc(uint32_t fmt, int n, int a_mn, int 
 
 // ------------------------------------------------------------------------------------------ layout
 template <int D, int NR> struct pt_cfg {
-  static constexpr bool ROWS2 = NR == 128;             // the softmax groups split the rows, not the keys
-  static constexpr int RW = ROWS2 ? 64 : NR;           // rows of a softmax group
-  static constexpr int WK = ROWS2 ? 64 : 128;          // keys of a bf16 tile
-  static constexpr int SLOT = WK * D * 2;              // a bf16 tile; two 8-bit tiles (one with ROWS2)
-  static constexpr int KST = ROWS2 || NR == 16 ? 3 : 2;
-  static constexpr int VST = ROWS2 ? 4 : NR <= 32 ? 3 : 2;
+  static constexpr int RW = NR < 32 ? NR : 32;         // rows of a softmax group
+  static constexpr int NRG = NR / RW;                  // groups that share a tile
+  static constexpr int NP = 4 / NRG;                   // tiles in the groups' hands at a time
+  static constexpr int TPS = NP == 1 ? 1 : 2;          // 8-bit tiles of a stage
+  static constexpr int WK = NP == 1 ? 64 : 128;        // keys of a bf16 tile
+  static constexpr int SLOT = WK * D * 2;              // a bf16 tile, or TPS 8-bit tiles
+  static constexpr int KST = NR == 128 ? 3 : 2;
+  static constexpr int VST = NR == 128 || NR == 16 ? 3 : 2;
   static constexpr int Q8 = NR * D;                    // one of the two e4m3 parts of the queries
   static constexpr int Q16 = NR * D * 2;
-  static constexpr int PB = PT_KEYS * RW * 2;          // a group's weights: two e4m3 parts, or bf16
+  static constexpr int PG = PT_KEYS * RW * 2;          // a group's weights: two e4m3 parts, or bf16
+  static constexpr int PT = NRG * PG;                  // the weights of a tile
+  static constexpr int MB = (NP - 1) * NR * 512;       // sums handed over at a unit's end, over the weights
+  static constexpr int PBYTES = 4 * PG > MB ? 4 * PG : MB;
   static constexpr int OFF_Q16 = 2 * Q8;
   static constexpr int OFF_P = OFF_Q16 + Q16;
-  static constexpr int OFF_K = OFF_P + 2 * PB;
+  static constexpr int OFF_K = OFF_P + PBYTES;
   static constexpr int OFF_V = OFF_K + KST * SLOT;
   static constexpr int OFF_X = OFF_V + VST * SLOT + 1024;   // (a head size of 64 reads one row group further)
-  static constexpr uint32_t COLS = 8 * RW < 32 ? 32 : 8 * RW;
+  static constexpr uint32_t COLS = 16 * RW;            // S and O, two buffers each, of four groups
 };
 
 struct pt_info {                     // one stage, written by the producer
@@ -129,31 +137,33 @@ struct pt_info {                     // one stage, written by the producer
 
 template <int D, int NR> struct alignas(16) pt_tail {
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
-  uint64_t info_full[PT_INFO], s_full[2][2], p_full[2], o_full[2], q_full;
+  uint64_t info_full[PT_INFO], s_full[4][2], p_full[4], o_full[4], q_full;
   uint32_t tmem_base;
   int abort_flag;
   long long cum[JK_MAX_ROWS + 1];    // tiles before each sequence
   int n8[JK_MAX_ROWS], n16[JK_MAX_ROWS];
   pt_info info[PT_INFO];
-  float q_max[8];
+  float q_max[16];
   int rowoff[NR];                    // output row of each query row, -1 = none
+  int parent[JK_MAX_TREE];
   alignas(16) uint32_t anc[4][NR];   // tree nodes each query row sees
-  alignas(16) float wmax[2][4][64], ref[2][64], alpha[2][2][64], beta[2][2][64], m_run[2][64], lsum[2][4][64];
-  int moved[2][2][2];                // [group][tile parity][rows / 32]: a running reference moved in this tile
+  // per warp and row, so that a step has one barrier: the four warps of a group form the same values
+  alignas(16) float ref[16][32], alpha[16][2][32], beta[16][2][32];
+  float wmax[4][2][4][32], m_run[4][32], lsum[16][32];
 };
 
 // The stages of a segment [t0, t1) of a unit with n8 8-bit tiles in front: every role walks them.
-template <bool ROWS2> struct pt_iter {
-  int tile, t1, n8, single;
-  __device__ __forceinline__ void start(int t0, int end, int n8_) { tile = t0; t1 = end; n8 = n8_; single = 0; }
-  // n tiles (1 or 2) from `tile` on; with one tile, w = the group that takes it
+template <int TPS, int NP> struct pt_iter {
+  int tile, t1, n8, turn;
+  __device__ __forceinline__ void start(int t0, int end, int n8_) { tile = t0; t1 = end; n8 = n8_; turn = 0; }
+  // n tiles from `first` on; tile j is worked on by the groups of turn (w + j) mod NP
   __device__ __forceinline__ bool next(int& first, int& n, int& w, bool& wide) {
     if (tile >= t1) return false;
     first = tile;
     wide = tile >= n8;
-    n = (!ROWS2 && !wide && tile + 1 < t1 && tile + 1 < n8) ? 2 : 1;
-    w = single;
-    if (n == 1) single ^= 1;
+    n = (TPS == 2 && !wide && tile + 1 < t1 && tile + 1 < n8) ? 2 : 1;
+    w = turn;
+    turn = (turn + n) & (NP - 1);
     tile += n;
     return true;
   }
@@ -202,9 +212,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     int Hq, int Hkv, int n_qblk, __nv_bfloat16* __restrict__ out, float* __restrict__ part_o,
     float* __restrict__ part_ml, int32_t* status) {
   typedef pt_cfg<D, NR> F;
-  constexpr int RW = F::RW, KST = F::KST, VST = F::VST, WK = F::WK;
-  constexpr bool ROWS2 = F::ROWS2;
+  constexpr int RW = F::RW, NRG = F::NRG, NP = F::NP, KST = F::KST, VST = F::VST, WK = F::WK;
   constexpr int KB = D / 64;
+  constexpr uint32_t O_COL = 8 * RW;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   unsigned char* sk = smem + F::OFF_K;
@@ -221,20 +231,20 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       mbar_init(&X.v_full[i], 1); mbar_init(&X.v_empty[i], 1);
     }
     for (int i = 0; i < PT_INFO; ++i) mbar_init(&X.info_full[i], 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&X.s_full[i][0], 1); mbar_init(&X.s_full[i][1], 1);
-      mbar_init(&X.p_full[i], 128); mbar_init(&X.o_full[i], 1);
+      mbar_init(&X.p_full[i], 4 * NRG); mbar_init(&X.o_full[i], 1);
     }
-    mbar_init(&X.q_full, 256);
+    mbar_init(&X.q_full, PT_SOFTMAX / 32);
     X.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) {
+  if (warp == 17) {
     tmem_alloc(&X.tmem_base, F::COLS);
     tmem_relinquish();
   }
   jk_pdl_wait();
-  if (warp == 0) pt_count(c, B, M, F::WK, units, lane, X.cum, X.n8, X.n16, blockIdx.x == 0 ? status : nullptr);
+  if (warp == 16) pt_count(c, B, M, F::WK, units, lane, X.cum, X.n8, X.n16, blockIdx.x == 0 ? status : nullptr);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -258,122 +268,136 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     t1 = left < nt - t0 ? t0 + (int)left : nt;
   };
 
-  if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0) {
-      // ================================================================== TMA producer
-      int sc = 0;                                       // stages so far
-      const uint64_t pol = l2_policy_evict_first();
-      for (long long t = w0; t < w1 && ok;) {
-        int b, u, t0, t1, nt;
-        segment(t, b, u, t0, t1, nt);
-        t += t1 - t0;
-        const int h = u / n_qblk, n8 = X.n8[b];
-        const int P = c.kv_len[b], nf = P / ps * ps, n_pg = P / ps;
-        const int open_rows = P - nf, open16 = (open_rows + 15) & ~15;
-        const int32_t* tab = c.page_table + (size_t)b * c.max_pages;
-        pt_iter<ROWS2> it;
-        it.start(t0, t1, n8);
-        int first, n, w;
-        bool wide;
-        const int per = PT_KEYS / ps;                   // pages of a tile
-        // page id and scales of this lane's page, one stage ahead
-        int page = 0;
-        float ksc = 1.f, vsc = 1.f;
-        auto fetch = [&](int tile) {
-          const int pi = tile * per + lane;
-          page = -1;
-          if (tile < n8 && lane < 2 * per && pi < n_pg) {
-            page = tab[pi];
-            if (page < 0 || page >= c.n_pages) {
-              jk_set_status(status, JK_ERR_BOUNDS);
-              page = 0;
-            }
-            const size_t blk = ((size_t)layer * c.n_pages + page) * Hkv + h;
-            ksc = c.k_scale[blk];
-            vsc = c.v_scale[blk];
+  if (warp == 16 || warp == 18) {
+    // ==================================================================== TMA producers: K (16), V (18)
+    const bool is_k = warp == 16;
+    const int NST = is_k ? KST : VST;
+    uint64_t* full = is_k ? X.k_full : X.v_full;
+    uint64_t* empty = is_k ? X.k_empty : X.v_empty;
+    unsigned char* ring = is_k ? sk : sv;
+    const CUtensorMap* map = is_k ? &map_k : &map_v;
+    int sc = 0, s_slot = 0, s_par = 1;                  // stages so far, their slot and its parity
+    // pages are read once, unless several row blocks of a kv head come by
+    const uint64_t pol = l2_policy_evict_first();
+    const bool once = n_qblk == 1;
+    const int per = PT_KEYS / ps;                       // pages of a tile
+    for (long long t = w0; t < w1 && ok;) {
+      int b, u, t0, t1, nt;
+      segment(t, b, u, t0, t1, nt);
+      t += t1 - t0;
+      const int h = u / n_qblk, n8 = X.n8[b];
+      const int P = c.kv_len[b], nf = P / ps * ps, n_pg = P / ps;
+      const int open_rows = P - nf, open16 = (open_rows + 15) & ~15;
+      const int32_t* tab = c.page_table + (size_t)b * c.max_pages;
+      pt_iter<F::TPS, NP> it;
+      it.start(t0, t1, n8);
+      int first, n, w;
+      bool wide;
+      // Page ids and scales in batches of 32 pages, lane l the batch's page l, the ids of the next batch
+      // asked for a batch ahead: two dependent loads per stage would be the stage's time.
+      int at = t0 * per, id = 0, id_next = 0;
+      float ksc = 1.f, vsc = 1.f;
+      auto ask = [&](int p0) { return p0 + lane < n_pg ? tab[p0 + lane] : 0; };
+      auto take = [&](int raw) {                        // the batch from `at` on
+        id = raw;
+        if (id < 0 || id >= c.n_pages) {
+          jk_set_status(status, JK_ERR_BOUNDS);
+          id = 0;
+        }
+        if (is_k) {
+          const size_t blk = ((size_t)layer * c.n_pages + id) * Hkv + h;
+          ksc = c.k_scale[blk];
+          vsc = c.v_scale[blk];
+        }
+        id_next = ask(at + 32);
+      };
+      if (t0 < n8) take(ask(at));
+      while (ok && it.next(first, n, w, wide)) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&empty[s_slot], s_par, abort_flag, status));
+        unsigned char* dst = ring + s_slot * F::SLOT;
+        pt_info& I = X.info[sc % PT_INFO];
+        if (!wide) {
+          const int p0 = first * per, np = min(n * per, n_pg - p0);
+          // a stage has at most 16 pages and starts at a multiple of its tile: it may span two batches
+          if (p0 >= at + 32) { at += 32; take(id_next); }
+          int page = __shfl_sync(0xffffffffu, id, (p0 - at + lane) & 31);
+          float k1 = __shfl_sync(0xffffffffu, ksc, (p0 - at + lane) & 31);
+          float v1 = __shfl_sync(0xffffffffu, vsc, (p0 - at + lane) & 31);
+          if (p0 + np > at + 32) {
+            const int split = at + 32 - p0;             // lanes from here on belong to the next batch
+            at += 32;
+            take(id_next);
+            const int pg2 = __shfl_sync(0xffffffffu, id, (p0 - at + lane) & 31);
+            const float k2 = __shfl_sync(0xffffffffu, ksc, (p0 - at + lane) & 31);
+            const float v2 = __shfl_sync(0xffffffffu, vsc, (p0 - at + lane) & 31);
+            if (lane >= split) { page = pg2; k1 = k2; v1 = v2; }
           }
-        };
-        fetch(t0);
-        while (ok && it.next(first, n, w, wide)) {
-          const int ks = sc % KST, vs = sc % VST;
-          pt_info& I = X.info[sc % PT_INFO];
-          ok = __all_sync(0xffffffffu, mbar_wait(&X.k_empty[ks], ((sc / KST) & 1) ^ 1, abort_flag, status));
-          unsigned char* kd = sk + ks * F::SLOT;
-          unsigned char* vd = sv + vs * F::SLOT;
-          if (!wide) {
-            const int np = min(n * per, n_pg - first * per);
-            const uint32_t bytes = (uint32_t)np * ps * D;
-            const bool mine = ok && lane < np;
-            if (ok && lane == 0) mbar_expect_tx(&X.k_full[ks], bytes);
-            __syncwarp();
-            if (mine)
-              tma_load_4d_hint(kd + lane * ps * D, &map_k, 0, 0, h, layer * c.n_pages + page, &X.k_full[ks], pol);
+          if (ok && lane == 0) mbar_expect_tx(&full[s_slot], (uint32_t)np * ps * D);
+          __syncwarp();
+          if (ok && lane < np) {
+            const int row = layer * c.n_pages + page;
+            if (once) tma_load_4d_hint(dst + lane * ps * D, map, 0, 0, h, row, &full[s_slot], pol);
+            else tma_load_4d(dst + lane * ps * D, map, 0, 0, h, row, &full[s_slot]);
+          }
+          if (is_k) {
             if (lane < 16) {
-              const int e = (int)(__float_as_uint(vsc) >> 23) - 127;
-              I.sk[lane] = ksc;
+              const int e = (int)(__float_as_uint(v1) >> 23) - 127;
+              I.sk[lane] = k1;
               I.lsv[lane] = (float)e;
               I.isv[lane] = paged_pow2(-e);
             }
             if (lane < 2) I.live[lane] = min(PT_KEYS, nf - (first + lane) * PT_KEYS);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&X.info_full[sc % PT_INFO]);
-            ok = __all_sync(0xffffffffu, ok && mbar_wait(&X.v_empty[vs], ((sc / VST) & 1) ^ 1, abort_flag, status));
-            if (ok && lane == 0) mbar_expect_tx(&X.v_full[vs], bytes);
-            __syncwarp();
-            if (ok && lane < np)
-              tma_load_4d_hint(vd + lane * ps * D, &map_v, 0, 0, h, layer * c.n_pages + page, &X.v_full[vs], pol);
-            fetch(first + n);
-          } else {
-            // bf16 tile: rows g of (open rows, padded to 16, then tree rows) in boxes of 16
-            const int base = (first - n8) * WK;
-            const int g = base + (lane / KB) * 16, kb = lane % KB;
-            const bool in_open = g < open16;
-            const bool mine = lane < WK / 16 * KB && (in_open || g - open16 < M);
-            const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * 16 * 64 * 2;
-            const int row = in_open ? (nf & (2 * ps - 1)) + g : g - open16;
-            const int outer = in_open ? layer * c.max_seqs + b : b;
-            const uint32_t at = (uint32_t)kb * (WK * 128) + (lane / KB) * 16 * 128;
-            if (ok && lane == 0) mbar_expect_tx(&X.k_full[ks], bytes);
-            __syncwarp();
-            if (ok && mine)
-              tma_load_4d(kd + at, in_open ? &map_ko : &map_kt, kb * 64, row, h, outer, &X.k_full[ks]);
-            if (lane == 0) {
-              I.live[0] = open16 + M - base;
-              I.open_rows = open_rows - base;
-              I.open16 = open16 - base;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&X.info_full[sc % PT_INFO]);
-            ok = __all_sync(0xffffffffu, ok && mbar_wait(&X.v_empty[vs], ((sc / VST) & 1) ^ 1, abort_flag, status));
-            if (ok && lane == 0) mbar_expect_tx(&X.v_full[vs], bytes);
-            __syncwarp();
-            if (ok && mine)
-              tma_load_4d(vd + at, in_open ? &map_vo : &map_vt, kb * 64, row, h, outer, &X.v_full[vs]);
           }
-          ++sc;
+        } else {
+          // bf16 tile: rows g of (open rows, padded to 16, then tree rows) in boxes of 16
+          const int base = (first - n8) * WK;
+          const int g = base + (lane / KB) * 16, kb = lane % KB;
+          const bool in_open = g < open16;
+          const bool mine = lane < WK / 16 * KB && (in_open || g - open16 < M);
+          const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * 16 * 64 * 2;
+          const int row = in_open ? (nf & (2 * ps - 1)) + g : g - open16;
+          const int outer = in_open ? layer * c.max_seqs + b : b;
+          if (ok && lane == 0) mbar_expect_tx(&full[s_slot], bytes);
+          __syncwarp();
+          if (ok && mine)
+            tma_load_4d(dst + kb * (WK * 128) + (lane / KB) * 16 * 128,
+                        is_k ? (in_open ? &map_ko : &map_kt) : (in_open ? &map_vo : &map_vt), kb * 64, row, h, outer,
+                        &full[s_slot]);
+          if (is_k && lane == 0) {
+            I.live[0] = open16 + M - base;
+            I.open_rows = open_rows - base;
+            I.open16 = open16 - base;
+          }
         }
+        __syncwarp();
+        if (is_k && lane == 0) mbar_arrive(&X.info_full[sc % PT_INFO]);
+        ++sc;
+        if (++s_slot == NST) { s_slot = 0; s_par ^= 1; }
       }
-      if (!ok) {
-        // gave up, possibly with copies still in flight: give them a bounded time to land
-        const unsigned long long ts = global_ns();
-        while (global_ns() - ts < 2000000ull) { /* 2 ms: far longer than any TMA copy */ }
-      }
-    } else if (warp == 1 && lane == 0) {
+    }
+    if (!ok) {
+      // gave up, possibly with copies still in flight: give them a bounded time to land
+      const unsigned long long ts = global_ns();
+      while (global_ns() - ts < 2000000ull) { /* 2 ms: far longer than any TMA copy */ }
+    }
+  } else if (warp == 17) {
+    if (lane == 0) {
       // ================================================================== MMA issuer
       const uint32_t q8 = smem_u32(smem), q16 = smem_u32(smem + F::OFF_Q16), pb = smem_u32(smem + F::OFF_P);
       const uint32_t ka0 = smem_u32(sk), va0 = smem_u32(sv);
       const uint32_t id_s8 = pt_idesc(0, NR, 0, 0), id_s16 = pt_idesc(1, NR, 0, 0);
-      const uint32_t id_p8 = pt_idesc(0, RW, 1, 1), id_p16 = pt_idesc(1, RW, 1, 1);
-      int ks_n = 0, vs_n = 0, cs[2] = {0, 0}, cp[2] = {0, 0}, segs = 0;
+      const uint32_t id_p8 = pt_idesc(0, NR, 1, 1), id_p16 = pt_idesc(1, NR, 1, 1);
+      int ks_n = 0, vs_n = 0, segs = 0;
+      uint32_t cs = 0, cp = 0;                          // tiles per turn so far, a byte each (mod 256)
       auto issue_s = [&](int n, int w, bool wide) {
         const int slot = ks_n % KST;
         if (!mbar_wait(&X.k_full[slot], (ks_n / KST) & 1, abort_flag, status)) { ok = false; return; }
         tc_fence_after();
         const uint32_t ka = ka0 + slot * F::SLOT;
         for (int j = 0; j < n; ++j) {
-          const int g = ROWS2 ? 0 : (n == 2 ? j : w);   // group whose columns take the tile
-          const uint32_t d = tmem + (cs[g] & 1) * 2 * RW + g * RW;
+          const int tp = (w + j) & (NP - 1);
+          const uint32_t buf = (cs >> (8 * tp)) & 1;
+          const uint32_t d = tmem + (buf * NP + tp) * NR;
           if (!wide) {
             const uint32_t kt = ka + j * (PT_KEYS * D);
 #pragma unroll
@@ -390,12 +414,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
                 tc_mma_bf16(d, pt_desc(ka + kb * (WK * 128) + k * 32, 16, 1024, 2),
                             pt_desc(q16 + kb * (NR * 128) + k * 32, 16, 1024, 2), id_s16, (kb | k) ? 1u : 0u);
           }
-          tc_commit(&X.s_full[g][cs[g] & 1]);
-          ++cs[g];
-          if (ROWS2) {
-            tc_commit(&X.s_full[1][cs[1] & 1]);
-            ++cs[1];
-          }
+          tc_commit(&X.s_full[tp][buf]);
+          cs = (cs & ~(0xffu << (8 * tp))) | ((((cs >> (8 * tp)) + 1) & 0xffu) << (8 * tp));
         }
         tc_commit(&X.k_empty[slot]);
         ++ks_n;
@@ -404,29 +424,30 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         const int slot = vs_n % VST;
         if (!mbar_wait(&X.v_full[slot], (vs_n / VST) & 1, abort_flag, status)) { ok = false; return; }
         const uint32_t va = va0 + slot * F::SLOT;
-        for (int j = 0; j < (ROWS2 ? 2 : n); ++j) {
-          const int g = (ROWS2 || n == 2) ? j : w;
-          if (!mbar_wait(&X.p_full[g], cp[g] & 1, abort_flag, status)) { ok = false; return; }
+        for (int j = 0; j < n; ++j) {
+          const int tp = (w + j) & (NP - 1);
+          const uint32_t buf = (cp >> (8 * tp)) & 1;
+          if (!mbar_wait(&X.p_full[tp], buf, abort_flag, status)) { ok = false; return; }
           tc_fence_after();
-          const uint32_t d = tmem + 4 * RW + (cp[g] & 1) * 2 * RW + g * RW;
-          const uint32_t p = pb + g * F::PB;
+          const uint32_t d = tmem + O_COL + (buf * NP + tp) * NR;
+          const uint32_t p = pb + tp * F::PT;
           if (!wide) {
-            const uint32_t vt = va + (ROWS2 ? 0 : j) * (PT_KEYS * D);
+            const uint32_t vt = va + j * (PT_KEYS * D);
 #pragma unroll
             for (int part = 0; part < 2; ++part)
 #pragma unroll
               for (int k = 0; k < PT_KEYS / 32; ++k)
                 pt_mma_f8(d, pt_desc(vt + k * 32 * D, 8 * D, 8 * D, pt_layout(D)),
-                          pt_desc(p + part * (PT_KEYS * RW) + k * 32 * RW, 8 * RW, 8 * RW, pt_layout(RW)), id_p8,
-                          (part | k) ? 1u : 0u);
+                          pt_desc(p + part * (PT_KEYS * RW) + k * 32 * RW, NRG > 1 ? F::PG : 8 * RW, 8 * RW, pt_layout(RW)),
+                          id_p8, (part | k) ? 1u : 0u);
           } else {
 #pragma unroll
             for (int k = 0; k < WK / 16; ++k)
               tc_mma_bf16(d, pt_desc(va + k * 2048, KB == 2 ? WK * 128 : 1024, 1024, 2),
-                          pt_desc(p + k * 32 * RW, 16 * RW, 16 * RW, pt_layout(2 * RW)), id_p16, k ? 1u : 0u);
+                          pt_desc(p + k * 32 * RW, NRG > 1 ? F::PG : 16 * RW, 16 * RW, pt_layout(2 * RW)), id_p16, k ? 1u : 0u);
           }
-          tc_commit(&X.o_full[g]);
-          ++cp[g];
+          tc_commit(&X.o_full[tp]);
+          cp = (cp & ~(0xffu << (8 * tp))) | ((((cp >> (8 * tp)) + 1) & 0xffu) << (8 * tp));
         }
         tc_commit(&X.v_empty[slot]);
         ++vs_n;
@@ -439,7 +460,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         ++segs;
         if (!ok) break;
         tc_fence_after();
-        pt_iter<ROWS2> is, ip;
+        pt_iter<F::TPS, NP> is, ip;
         is.start(t0, t1, X.n8[b]);
         ip.start(t0, t1, X.n8[b]);
         int first, n, w, ahead = 0;
@@ -465,15 +486,15 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         while (global_ns() - ts < 2000000ull) { }
       }
     }
-  } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+  } else if (warp < 16) {
     // ==================================================================== softmax groups
-    const int g = (warp - 4) >> 2, wq = warp & 3;       // group, tensor-memory lane quarter
+    const int grp = warp >> 2, wq = warp & 3;           // group, tensor-memory lane quarter
+    const int rg = grp % NRG, tp = grp / NRG;           // its rows of the block, its turn among the tiles
     const int kl = wq * 32 + lane;                      // this thread's key of a tile / head dim of O
-    const int st = tid - 128;                           // 0 .. 255
     const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
-    unsigned char* pbuf = smem + F::OFF_P + g * F::PB;
-    const int grow = ROWS2 ? g * 64 : 0;                // first row of this group in the block
+    unsigned char* pbuf = smem + F::OFF_P + tp * F::PT + rg * F::PG;
+    const int grow = rg * RW;                           // first row of this group in the block
+    auto group_bar = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory"); };
     int cnt = 0, sc = 0;                                // tiles of this group, stages of the CTA
     for (long long t = w0; t < w1;) {
       int b, u, t0, t1, nt;
@@ -484,17 +505,21 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       t += t1 - t0;
       const int h = u / n_qblk, row0 = (u % n_qblk) * NR, n_rows = G * M, n8 = X.n8[b];
       // ------------------------------------------------ queries of the unit
-      constexpr int QV = (NR * (D / 8) + 255) / 256;
+      constexpr int QV = (NR * (D / 8) + PT_SOFTMAX - 1) / PT_SOFTMAX;
       uint4 qv[QV];
       float amax = 0.f;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
-        const int idx = st + i * 256, r = idx / (D / 8), ch = idx % (D / 8);
+        const int idx = tid + i * PT_SOFTMAX, r = idx / (D / 8), ch = idx % (D / 8);
         qv[i] = make_uint4(0u, 0u, 0u, 0u);
         if (r < NR && row0 + r < n_rows) {
           const int gg = (row0 + r) / M, ii = (row0 + r) % M;
           qv[i] = *reinterpret_cast<const uint4*>(q + (((size_t)b * M + ii) * Hq + h * G + gg) * D + ch * 8);
         }
+      }
+      if (t1 > n8 && tid < M) X.parent[tid] = parent[(size_t)b * M + tid];
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
         const uint32_t qw[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -502,103 +527,98 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
                                    paged_mag(__uint_as_float(qw[j] & 0xffff0000u))));
       }
       amax = jk_warp_max(amax);
-      if (lane == 0) X.q_max[warp - 4] = amax;
-      // (also: both groups are done with the previous unit's queries, sums and row tables)
-      pt_bar<3, 256>();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) amax = fmaxf(amax, X.q_max[i]);
+      if (lane == 0) X.q_max[warp] = amax;
+      // (also: all groups are done with the previous unit's queries, sums and row tables)
+      pt_bar<5, PT_SOFTMAX>();
+      amax = jk_warp_max(X.q_max[lane & 15]);
       int qe = (int)(__float_as_uint(amax) >> 23) - 127 - 8 + ((__float_as_uint(amax) & 0x7fffffu) > 0x600000u ? 1 : 0);
       qe = max(-100, min(100, qe));
       const float qinv = paged_pow2(-qe);
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
-        const int idx = st + i * 256, r = idx / (D / 8), ch = idx % (D / 8);
+        const int idx = tid + i * PT_SOFTMAX, r = idx / (D / 8), ch = idx % (D / 8);
         if (r < NR) {
           *reinterpret_cast<uint4*>(smem + F::OFF_Q16 + (ch >> 3) * (NR * 128) + pt_piece<128>(r, ch & 7)) = qv[i];
           const uint32_t qw[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
           uint32_t hi[2], lo[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            float v[4], back[4];
-            v[0] = __uint_as_float(qw[2 * j] << 16) * qinv;
-            v[1] = __uint_as_float(qw[2 * j] & 0xffff0000u) * qinv;
-            v[2] = __uint_as_float(qw[2 * j + 1] << 16) * qinv;
-            v[3] = __uint_as_float(qw[2 * j + 1] & 0xffff0000u) * qinv;
-            hi[j] = paged_pack4(v[0], v[1], v[2], v[3]);
+            const float v0 = __uint_as_float(qw[2 * j] << 16) * qinv, v1 = __uint_as_float(qw[2 * j] & 0xffff0000u) * qinv;
+            const float v2 = __uint_as_float(qw[2 * j + 1] << 16) * qinv;
+            const float v3 = __uint_as_float(qw[2 * j + 1] & 0xffff0000u) * qinv;
+            hi[j] = paged_pack4(v0, v1, v2, v3);
             const float2 b0 = paged_unpack2(hi[j]), b1 = paged_unpack2(hi[j] >> 16);
-            back[0] = b0.x; back[1] = b0.y; back[2] = b1.x; back[3] = b1.y;
-            lo[j] = paged_pack4(v[0] - back[0], v[1] - back[1], v[2] - back[2], v[3] - back[3]);
+            lo[j] = paged_pack4(v0 - b0.x, v1 - b0.y, v2 - b1.x, v3 - b1.y);
           }
           const uint32_t at = pt_piece<D>(r, ch >> 1) + (ch & 1) * 8;
           *reinterpret_cast<uint2*>(smem + at) = make_uint2(hi[0], hi[1]);
           *reinterpret_cast<uint2*>(smem + F::Q8 + at) = make_uint2(lo[0], lo[1]);
         }
       }
-      if (st < NR) {
-        const bool live = row0 + st < n_rows;
-        const int gg = live ? (row0 + st) / M : 0, ii = live ? (row0 + st) % M : 0;
-        X.rowoff[st] = live ? ii * Hq + h * G + gg : -1;
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&X.q_full);
+      if (tid < NR) {
+        const bool live = row0 + tid < n_rows;
+        const int gg = live ? (row0 + tid) / M : 0, ii = live ? (row0 + tid) % M : 0;
+        X.rowoff[tid] = live ? ii * Hq + h * G + gg : -1;
         uint32_t a[4] = {0u, 0u, 0u, 0u};
         if (live && t1 > n8) {                          // (only the last tiles look at it)
           int node = ii;
           for (int guard = 0; node >= 0 && guard <= JK_MAX_TREE; ++guard) {
-            a[node >> 5] |= 1u << (node & 31);
-            const int pp = parent[(size_t)b * M + node];
+            const uint32_t bit = 1u << (node & 31);
+            const int wd = node >> 5;
+            a[0] |= wd == 0 ? bit : 0u; a[1] |= wd == 1 ? bit : 0u;
+            a[2] |= wd == 2 ? bit : 0u; a[3] |= wd == 3 ? bit : 0u;
+            const int pp = X.parent[node];
             node = pp < node ? pp : -1;
           }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) X.anc[i][st] = a[i];
+        for (int i = 0; i < 4; ++i) X.anc[i][tid] = a[i];
       }
-      fence_proxy_async_smem();
-      mbar_arrive(&X.q_full);
-      pt_bar<3, 256>();                                 // row tables are visible
+      pt_bar<5, PT_SOFTMAX>();                          // row tables are visible
       const float c16 = scale * 1.4426950408889634f, c8 = c16 * paged_pow2(qe);
 
       float acc[RW], lacc[RW];
 #pragma unroll
       for (int i = 0; i < RW; ++i) acc[i] = lacc[i] = 0.f;
-      float run = -INFINITY;                            // running reference of row kl (threads kl < RW)
-      bool pending = false;                             // the last tile's product is still to be added
+      float run = -INFINITY;                            // running reference of row lane (mod RW)
+      bool pending = false, moved_before = false;       // the last tile's product is still to be added
       // acc = alpha acc + beta O of tile `count`.  Its completion has been waited for by every thread of
       // the group: a wait here, after the arrival for the next tile, could find the barrier two phases on.
-      auto take_o = [&](int count) {
+      auto take_o = [&](int count, bool moved) {
         const int sb = count & 1;
         __syncwarp();
         tc_fence_after();
-        const bool moved = (X.moved[g][sb][0] | (RW == 64 ? X.moved[g][sb][1] : 0)) != 0;
-        const uint32_t oa = tmem + lane_base + 4 * RW + sb * 2 * RW + g * RW;
-        constexpr int CH = RW < 32 ? RW : 32;
+        const uint32_t oa = tmem + lane_base + O_COL + (sb * NP + tp) * NR + grow;
+        uint32_t r[RW];
+        if constexpr (RW == 32) tmem_ld32(oa, r); else tmem_ld16(oa, r);
+        tmem_ld_wait();
+        if (moved) {
 #pragma unroll
-        for (int c0 = 0; c0 < RW; c0 += CH) {
-          uint32_t r[CH];
-          if constexpr (CH == 32) tmem_ld32(oa + c0, r); else tmem_ld16(oa + c0, r);
-          tmem_ld_wait();
-          if (moved) {
-#pragma unroll
-            for (int j = 0; j < CH; j += 4) {
-              const float4 al = *reinterpret_cast<const float4*>(&X.alpha[g][sb][c0 + j]);
-              acc[c0 + j] *= al.x; acc[c0 + j + 1] *= al.y; acc[c0 + j + 2] *= al.z; acc[c0 + j + 3] *= al.w;
-            }
+          for (int j = 0; j < RW; j += 4) {
+            const float4 al = *reinterpret_cast<const float4*>(&X.alpha[warp][sb][j]);
+            acc[j] *= al.x; acc[j + 1] *= al.y; acc[j + 2] *= al.z; acc[j + 3] *= al.w;
           }
+        }
 #pragma unroll
-          for (int j = 0; j < CH; j += 4) {
-            const float4 be = *reinterpret_cast<const float4*>(&X.beta[g][sb][c0 + j]);
-            acc[c0 + j] = fmaf(__uint_as_float(r[j]), be.x, acc[c0 + j]);
-            acc[c0 + j + 1] = fmaf(__uint_as_float(r[j + 1]), be.y, acc[c0 + j + 1]);
-            acc[c0 + j + 2] = fmaf(__uint_as_float(r[j + 2]), be.z, acc[c0 + j + 2]);
-            acc[c0 + j + 3] = fmaf(__uint_as_float(r[j + 3]), be.w, acc[c0 + j + 3]);
-          }
+        for (int j = 0; j < RW; j += 4) {
+          const float4 be = *reinterpret_cast<const float4*>(&X.beta[warp][sb][j]);
+          acc[j] = fmaf(__uint_as_float(r[j]), be.x, acc[j]);
+          acc[j + 1] = fmaf(__uint_as_float(r[j + 1]), be.y, acc[j + 1]);
+          acc[j + 2] = fmaf(__uint_as_float(r[j + 2]), be.z, acc[j + 2]);
+          acc[j + 3] = fmaf(__uint_as_float(r[j + 3]), be.w, acc[j + 3]);
         }
       };
 
-      pt_iter<ROWS2> it;
+      pt_iter<F::TPS, NP> it;
       it.start(t0, t1, n8);
       int first, n, w;
       bool wide;
       for (; it.next(first, n, w, wide); ++sc) {
-        if (!ROWS2 && n == 1 && w != g) continue;
-        const int part = (!ROWS2 && n == 2) ? g : 0;    // tile of the stage
+        const int part = (tp - w) & (NP - 1);           // tile of the stage
+        if (part >= n) continue;
         const pt_info& I = X.info[sc % PT_INFO];
         const int sb = cnt & 1;
         if (ok) ok = mbar_wait(&X.info_full[sc % PT_INFO], (sc / PT_INFO) & 1, abort_flag, status);
@@ -608,97 +628,110 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         if (!wide) {
           const int pg = (part * PT_KEYS + kl) / ps;
           dead = kl >= I.live[part];
-          if (!dead) {
-            ck = c8 * I.sk[pg];
-            lsv = I.lsv[pg];
-            isv = I.isv[pg];
-          }
+          ck = c8 * I.sk[pg];
+          lsv = I.lsv[pg];
+          isv = I.isv[pg];
         } else {
           dead = kl >= min(WK, I.live[0]) || (kl >= I.open_rows && kl < I.open16);
           if (kl >= I.open16) tree_row = kl - I.open16;
         }
-        if (ok) ok = mbar_wait(&X.s_full[g][sb], (cnt >> 1) & 1, abort_flag, status);
+        if (ok) ok = mbar_wait(&X.s_full[tp][sb], (cnt >> 1) & 1, abort_flag, status);
         __syncwarp();
         tc_fence_after();
-        // ---- logits of this key against all rows, their maxima over the tile
-        float x[RW];
+        const uint32_t sa = tmem + lane_base + (sb * NP + tp) * NR + grow;
+        const bool masked = __any_sync(0xffffffffu, dead || tree_row >= 0);
+        // rows of V that no live key owns may hold anything, NaN included, and 0 * NaN would reach every row
+        if (dead && (!wide || kl < WK)) {
+          if (ok) ok = mbar_wait(&X.v_full[sc % VST], (sc / VST) & 1, abort_flag, status);
+          unsigned char* row = sv + (sc % VST) * F::SLOT + (wide ? kl * 128 : part * (PT_KEYS * D) + kl * D);
+          if (ok) {
+#pragma unroll 1
+            for (int j = 0; j < (wide ? D / 8 : D / 16); ++j)
+              *reinterpret_cast<uint4*>(row + (wide ? (j >> 3) * (WK * 128) + (j & 7) * 16 : j * 16)) = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        __syncwarp();
+        // rows of the block this key is visible to
+        uint32_t vis = 0xffffffffu;
+        if (masked) {
+          if (dead) vis = 0u;
+          else if (tree_row >= 0) {
+            const uint32_t* aw = &X.anc[(tree_row >> 5) & 3][grow];
+            vis = 0u;
+#pragma unroll
+            for (int j = 0; j < RW; ++j) vis |= ((aw[j] >> (tree_row & 31)) & 1u) << j;
+          }
+        }
+        // ---- maxima over the tile of the logits of each row (base 2, with log2 of the V scale)
         {
-          const uint32_t sa = tmem + lane_base + sb * 2 * RW + g * RW;
-          constexpr int CH = RW < 32 ? RW : 32;
+          float x[RW];
+          uint32_t r[RW];
+          if constexpr (RW == 32) tmem_ld32(sa, r); else tmem_ld16(sa, r);
+          tmem_ld_wait();
 #pragma unroll
-          for (int c0 = 0; c0 < RW; c0 += CH) {
-            uint32_t r[CH];
-            if constexpr (CH == 32) tmem_ld32(sa + c0, r); else tmem_ld16(sa + c0, r);
-            tmem_ld_wait();
+          for (int j = 0; j < RW; ++j) x[j] = fmaf(__uint_as_float(r[j]), ck, lsv);
+          if (masked) {
 #pragma unroll
-            for (int j = 0; j < CH; ++j) x[c0 + j] = fmaf(__uint_as_float(r[j]), ck, lsv);
+            for (int j = 0; j < RW; ++j)
+              if (!((vis >> j) & 1u)) x[j] = -INFINITY;
           }
-          if (dead) {
-#pragma unroll
-            for (int j = 0; j < RW; ++j) x[j] = -INFINITY;
-          } else if (tree_row >= 0) {
-            const uint4* aw = reinterpret_cast<const uint4*>(&X.anc[(tree_row >> 5) & 3][grow]);
-            const uint32_t bit = 1u << (tree_row & 31);
-#pragma unroll
-            for (int j = 0; j < RW; j += 4) {
-              const uint4 a = aw[j >> 2];
-              if (!(a.x & bit)) x[j] = -INFINITY;
-              if (!(a.y & bit)) x[j + 1] = -INFINITY;
-              if (!(a.z & bit)) x[j + 2] = -INFINITY;
-              if (!(a.w & bit)) x[j + 3] = -INFINITY;
-            }
+          const float m = pt_rows_reduce<RW, false>(x, lane);
+          if (lane < RW) X.wmax[grp][sb][wq][lane] = m;
+        }
+        group_bar();
+        bool moved = false;
+        {
+          const float* wm = &X.wmax[grp][sb][0][lane & (RW - 1)];
+          const float m = fmaxf(fmaxf(wm[0], wm[32]), fmaxf(wm[64], wm[96]));
+          float ref = 0.f, be = 0.f, al = 1.f;
+          if (m != -INFINITY) {
+            ref = ceilf(m);
+            const float now = fmaxf(run, ref);
+            al = run == -INFINITY ? 0.f : fast_exp2(run - now);
+            be = fast_exp2(ref - now);
+            moved = run != now;
+            run = now;
+          }
+          if (lane < RW) {
+            X.ref[warp][lane] = ref - PT_PSHIFT;
+            X.alpha[warp][sb][lane] = al;
+            X.beta[warp][sb][lane] = be;
           }
         }
-        if constexpr (RW >= 32) {
-          X.wmax[g][wq][lane] = pt_rows_reduce<32, false>(x, lane);
-          if (RW == 64) X.wmax[g][wq][32 + lane] = pt_rows_reduce<32, false>(x + (RW - 32), lane);
-        } else {
-          const float m = pt_rows_reduce<16, false>(x, lane);
-          if (lane < 16) X.wmax[g][wq][lane] = m;
-        }
-        if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
-        if (kl < ((RW + 31) & ~31)) {                   // whole warps
-          bool moved = false;
-          if (kl < RW) {
-            const float m = fmaxf(fmaxf(X.wmax[g][0][kl], X.wmax[g][1][kl]), fmaxf(X.wmax[g][2][kl], X.wmax[g][3][kl]));
-            float ref = 0.f, be = 0.f, al = 1.f;
-            if (m != -INFINITY) {
-              ref = ceilf(m);
-              const float now = fmaxf(run, ref);
-              al = run == -INFINITY ? 0.f : fast_exp2(run - now);
-              be = fast_exp2(ref - now);
-              moved = run != now;
-              run = now;
-            }
-            X.ref[g][kl] = ref - PT_PSHIFT;
-            X.alpha[g][sb][kl] = al;
-            X.beta[g][sb][kl] = be;
-          }
-          const bool any = __any_sync(0xffffffffu, moved);
-          if (lane == 0) X.moved[g][sb][wq] = any;
-        }
-        if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
-        const bool moved = (X.moved[g][sb][0] | (RW == 64 ? X.moved[g][sb][1] : 0)) != 0;
+        moved = __any_sync(0xffffffffu, moved);         // (orders the writes above within the warp)
+        __syncwarp();
         // ---- the previous product is complete: its weights may be overwritten
-        if (pending && ok) ok = mbar_wait(&X.o_full[g], (cnt - 1) & 1, abort_flag, status);
+        if (pending && ok) ok = mbar_wait(&X.o_full[tp], (cnt - 1) & 1, abort_flag, status);
+        __syncwarp();
         if (moved) {
 #pragma unroll
           for (int j = 0; j < RW; j += 4) {
-            const float4 al = *reinterpret_cast<const float4*>(&X.alpha[g][sb][j]);
+            const float4 al = *reinterpret_cast<const float4*>(&X.alpha[warp][sb][j]);
             lacc[j] *= al.x; lacc[j + 1] *= al.y; lacc[j + 2] *= al.z; lacc[j + 3] *= al.w;
           }
         }
 #pragma unroll
         for (int j0 = 0; j0 < RW; j0 += 16) {
+          uint32_t r[16];
           float e[16];
+          tmem_ld16(sa + j0, r);
+          tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
-            const float4 rf = *reinterpret_cast<const float4*>(&X.ref[g][j0 + j]);
-            const float4 be = *reinterpret_cast<const float4*>(&X.beta[g][sb][j0 + j]);
-            e[j] = fast_exp2(x[j0 + j] - rf.x);
-            e[j + 1] = fast_exp2(x[j0 + j + 1] - rf.y);
-            e[j + 2] = fast_exp2(x[j0 + j + 2] - rf.z);
-            e[j + 3] = fast_exp2(x[j0 + j + 3] - rf.w);
+            const float4 rf = *reinterpret_cast<const float4*>(&X.ref[warp][j0 + j]);
+            e[j] = fast_exp2(fmaf(__uint_as_float(r[j]), ck, lsv - rf.x));
+            e[j + 1] = fast_exp2(fmaf(__uint_as_float(r[j + 1]), ck, lsv - rf.y));
+            e[j + 2] = fast_exp2(fmaf(__uint_as_float(r[j + 2]), ck, lsv - rf.z));
+            e[j + 3] = fast_exp2(fmaf(__uint_as_float(r[j + 3]), ck, lsv - rf.w));
+          }
+          if (masked) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (!((vis >> (j0 + j)) & 1u)) e[j] = 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) {
+            const float4 be = *reinterpret_cast<const float4*>(&X.beta[warp][sb][j0 + j]);
             lacc[j0 + j] = fmaf(e[j], isv * be.x, lacc[j0 + j]);
             lacc[j0 + j + 1] = fmaf(e[j + 1], isv * be.y, lacc[j0 + j + 1]);
             lacc[j0 + j + 2] = fmaf(e[j + 2], isv * be.z, lacc[j0 + j + 2]);
@@ -736,94 +769,78 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
             *reinterpret_cast<uint4*>(pbuf + pt_piece<2 * RW>(kl, (j0 >> 3) + 1)) = make_uint4(pk[4], pk[5], pk[6], pk[7]);
           }
         }
-        // rows of V that no live key owns may hold anything, NaN included, and 0 * NaN would reach every row
-        if (dead && (!wide || kl < WK)) {
-          if (ok) ok = mbar_wait(&X.v_full[sc % VST], (sc / VST) & 1, abort_flag, status);
-          unsigned char* row = sv + (sc % VST) * F::SLOT + (wide ? kl * 128 : part * (PT_KEYS * D) + kl * D);
-          if (ok) {
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (wide) *reinterpret_cast<uint4*>(row + kb * (WK * 128) + j * 16) = make_uint4(0u, 0u, 0u, 0u);
-                else if (kb * 8 + j < D / 16) *reinterpret_cast<uint4*>(row + (kb * 8 + j) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-        }
         fence_proxy_async_smem();
         tc_fence_before();
-        mbar_arrive(&X.p_full[g]);
-        if (pending) take_o(cnt - 1);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&X.p_full[tp]);
+        if (pending) take_o(cnt - 1, moved_before);
         pending = true;
+        moved_before = moved;
         ++cnt;
       }
       if (pending) {
-        if (ok) ok = mbar_wait(&X.o_full[g], (cnt - 1) & 1, abort_flag, status);
-        take_o(cnt - 1);
+        if (ok) ok = mbar_wait(&X.o_full[tp], (cnt - 1) & 1, abort_flag, status);
+        take_o(cnt - 1, moved_before);
       }
       tc_fence_before();
 
       // ------------------------------------------------ the segment's result
-      if (kl < RW) X.m_run[g][kl] = run;
-      if constexpr (RW >= 32) {
-        X.lsum[g][wq][lane] = pt_rows_reduce<32, true>(lacc, lane);
-        if (RW == 64) X.lsum[g][wq][32 + lane] = pt_rows_reduce<32, true>(lacc + (RW - 32), lane);
-      } else {
-        const float l = pt_rows_reduce<16, true>(lacc, lane);
-        if (lane < 16) X.lsum[g][wq][lane] = l;
+      {
+        const float l = pt_rows_reduce<RW, true>(lacc, lane);
+        if (lane < RW) {
+          X.lsum[warp][lane] = l;
+          if (wq == 0) X.m_run[grp][lane] = run;
+        }
       }
       float* po = part_o + (size_t)slot * NR * D;
       float* pml = part_ml + (size_t)slot * NR * 2;
-      // weights of the two groups' sums (one group with ROWS2) for row kl; threads kl < RW
-      auto finish_row = [&](float wa, float wb, float l, float m) {
+      float* mb = reinterpret_cast<float*>(smem + F::OFF_P);     // [NP - 1][NR][128] over the weights
+      pt_bar<5, PT_SOFTMAX>();                          // every product has been read: the weights are free
+      if (NP > 1 && tp > 0) {
+#pragma unroll
+        for (int j = 0; j < RW; ++j) mb[((tp - 1) * NR + grow + j) * 128 + kl] = acc[j];
+      }
+      if (tp == 0 && kl < RW) {
+        // row kl of this group: what each turn's sum weighs
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) m = fmaxf(m, X.m_run[i * NRG + rg][kl]);
+        float wt[NP], l = 0.f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const int g = i * NRG + rg;
+          const float mi = X.m_run[g][kl];
+          wt[i] = mi == -INFINITY ? 0.f : fast_exp2(mi - m);
+          l = fmaf(wt[i], (X.lsum[g * 4][kl] + X.lsum[g * 4 + 1][kl]) + (X.lsum[g * 4 + 2][kl] + X.lsum[g * 4 + 3][kl]), l);
+        }
         const float inv = whole ? 1.f / l : 1.f;
-        X.alpha[g][0][kl] = wa * inv;
-        X.beta[g][0][kl] = wb * inv;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) X.beta[grp * 4 + i][0][kl] = wt[i] * inv;
         if (!whole) {
           pml[(grow + kl) * 2] = m;
           pml[(grow + kl) * 2 + 1] = l;
         }
-      };
-      auto store = [&](int j, float v) {                // element (row j of the group, head dim kl)
-        if (kl >= D) return;
-        if (whole) {
-          const int off = X.rowoff[grow + j];
-          if (off >= 0) out[((size_t)b * M * Hq + off) * D + kl] = __float2bfloat16_rn(v);
-        } else {
-          po[(size_t)(grow + j) * D + kl] = v;
-        }
-      };
-      if (ROWS2) {
-        if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
-        if (kl < RW)
-          finish_row(1.f, 0.f, X.lsum[g][0][kl] + X.lsum[g][1][kl] + X.lsum[g][2][kl] + X.lsum[g][3][kl], run);
-        if (g == 0) pt_bar<1, 128>(); else pt_bar<2, 128>();
+      }
+      pt_bar<5, PT_SOFTMAX>();
+      if (tp == 0 && kl < D) {
 #pragma unroll
-        for (int j = 0; j < RW; ++j) store(j, acc[j] * X.alpha[g][0][j]);
-      } else {
-        float* mb = reinterpret_cast<float*>(smem + F::OFF_P);   // [RW][128] over both groups' weights
-        pt_bar<3, 256>();                               // every product has been read: the weights are free
-        if (g == 1) {
+        for (int j = 0; j < RW; ++j) {
+          float v = acc[j] * X.beta[grp * 4][0][j];
 #pragma unroll
-          for (int j = 0; j < RW; ++j) mb[j * 128 + kl] = acc[j];
-        } else if (kl < RW) {
-          const float ma = run, mo = X.m_run[1][kl];
-          const float m = fmaxf(ma, mo);
-          const float wa = ma == -INFINITY ? 0.f : fast_exp2(ma - m), wb = mo == -INFINITY ? 0.f : fast_exp2(mo - m);
-          const float la = X.lsum[0][0][kl] + X.lsum[0][1][kl] + X.lsum[0][2][kl] + X.lsum[0][3][kl];
-          const float lb = X.lsum[1][0][kl] + X.lsum[1][1][kl] + X.lsum[1][2][kl] + X.lsum[1][3][kl];
-          finish_row(wa, wb, wa * la + wb * lb, m);
-        }
-        pt_bar<3, 256>();
-        if (g == 0) {
-#pragma unroll
-          for (int j = 0; j < RW; ++j) store(j, fmaf(acc[j], X.alpha[0][0][j], mb[j * 128 + kl] * X.beta[0][0][j]));
+          for (int i = 1; i < NP; ++i) v = fmaf(mb[((i - 1) * NR + grow + j) * 128 + kl], X.beta[grp * 4 + i][0][j], v);
+          if (whole) {
+            const int off = X.rowoff[grow + j];
+            if (off >= 0) out[((size_t)b * M * Hq + off) * D + kl] = __float2bfloat16_rn(v);
+          } else {
+            po[(size_t)(grow + j) * D + kl] = v;
+          }
         }
       }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) {
+  if (warp == 17) {
     tc_fence_after();
     tmem_dealloc(tmem, F::COLS);
   }
