@@ -2,80 +2,131 @@
 //
 // For a block of query rows (pairs of a q head of the group and a tree node) and tiles of 128 keys:
 //   S^T = K Q^T   (keys on the 128 lanes, query rows on the columns), then
-//   O^T = V^T P^T (head dims on the lanes, query rows on the columns).
-// Keys on the lanes because a call has few query rows (1 .. 128 per kv head): with rows on the lanes a
-// block of 60 would leave half of the SM's sub-partitions idle in the softmax, and a single token
-// 127 of 128 lanes.  A thread owns one key: its page's scales are two constants of the thread.
+//   O^T += V^T P^T (head dims on the lanes, query rows on the columns).
+// Keys on the lanes because a call has few query rows (1 .. 64 per block): with rows on the lanes a block of 60
+// would leave half of the SM's sub-partitions idle in the softmax, and a single token 127 of 128 lanes.
+// A thread owns one key: its page's scales are constants of the thread.
 //
-// Full pages stay 8-bit up to the tensor core.  A bf16 query has 8 significant bits, an e4m3 number 4, so
+// K stays 8-bit up to the tensor core.  A bf16 query has 8 significant bits, an e4m3 number 4, so
 // q 2^a = hi + lo with hi = e4m3(q 2^a) and lo = e4m3(q 2^a - hi) is exact down to 2^-17 of the block's
-// largest q, and S is two e4m3 products into one fp32 accumulator.  The softmax weights go the same
-// way: p = hi + lo keeps 8 significant bits, as bf16 would.  Two e4m3 products cost what one bf16
-// product costs, and no code is ever widened.  V's scale (a power of two) is added to the logit, so
-// that p already carries it: x = s scale_k + log2(scale_v), p = 2^(x - ref), and the row sum takes
-// 2^(x - ref) / scale_v.
+// largest q, and S is two e4m3 products into one fp32 accumulator, the price of one bf16 product.
+// V is widened to fp16 (exact) by a warpgroup of its own, 32 KB per tile, because the softmax weights need more
+// than 8 bits: two 8-bit parts per weight cost the softmax three times as many instructions as one
+// conversion to fp16, and their range (2^-17) made every few stages form new maxima.
+//   x = s scale_k + log2(scale_v),  p = 2^(x - ref + 6) in fp16 (11 significant bits),
+// so p carries V's scale (a power of two); the row sum takes p / scale_v in fp32.  ref is the rounded-up
+// maximum of the row's first tile in this CTA and only rises: when a weight passes fp16's range (2^10 above the
+// reference) the references follow, sums and products so far are scaled, and the tile's weights are formed
+// again.  Weights down to 2^-20 of 2^ref keep 11 bits, below 2^-31 they become 0: the tail behind one
+// dominant key survives to lengths of 2^20.
 //
-// ref is the (rounded up) maximum of this row in this tile, not the running one: e4m3 reaches down to
-// 2^-18 of the tile's largest weight, so what is lost of a tile is below 2^-11 of its own weight,
-// however small that is against another tile (with a running reference a long prefix behind one
-// dominant key would vanish).  So every tile has its own product O_t, and the running output is
-// kept in registers: acc = alpha acc + beta O_t with powers of two alpha, beta.
-//
-// The open page and the tree tokens are bf16 tiles at the end of the sequence (16-row boxes of either
-// array, dead rows cleared in V): the same pipeline with kind::f16 products.
+// The open page and the tree tokens are bf16 tiles of 64 keys at the end of the sequence (16-row boxes of
+// either array, dead rows cleared in V): the same pipeline with bf16 products.
 //
 // One CTA per SM; all tiles of the call are dealt out evenly in order (sequence, kv head, row block,
 // tile), so a unit (sequence, kv head, row block) spans CTAs where it has to; such a CTA leaves an
 // unnormalised partial, which k_paged_merge adds up, and a unit inside one CTA is written directly.
-// Warps: four softmax groups of four, TMA producers for K and for V, an MMA issuer.  A group takes 32 rows (16 where the block
-// has no more) of every NP-th tile: 128 rows 4 x 32, 64 rows 2 x 32 with two tiles at a time, fewer rows
-// with four.  Two groups of 64 rows each had 168 registers and spilled, two warps per scheduler to hide
-// every wait, and took twice as long.
+// Warps: two softmax groups of four that take tiles in turn, four that widen V, TMA producers for K and for V,
+// an MMA issuer.  Registers are moved to the softmax warps: 20 warps of 96 spilled, and with the shared
+// memory this kernel takes a spill is a trip to L2.
 #include <math.h>
 
 #include "jk_paged.cuh"
 #include "jk_tcgen05.cuh"
 
 #define PT_KEYS 128
-#define PT_SOFTMAX 512              // threads of the softmax groups
-#define PT_THREADS (PT_SOFTMAX + 96)
+#define PT_WKEYS 64                  // keys of a bf16 tile
+#define PT_SOFTMAX 256               // threads of the softmax groups
+#define PT_THREADS 512
 #define PT_MAX_CTAS 160
-#define PT_INFO 8                    // ring of stage descriptions
-#define PT_PSHIFT 8.f                // weights are scaled by 2^8: the largest lie in (2^7, 2^8]
+#define PT_INFO 16                   // ring of tile descriptions: more than K slots + tiles that S runs ahead + 1
+#define PT_AHEAD 4                   // tiles whose S may run ahead of their weights: two buffers per group
+#define PT_SHIFT 6.f                 // a weight at its reference is 2^6
 
 // ------------------------------------------------------------------------------------------ PTX
-__device__ __forceinline__ void pt_mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// The whole warp runs the issuing code and one lane issues: with values the compiler knows to be the same in
+// all lanes, descriptors live in uniform registers.  (Issued from inside `if (lane == 0)`, every product
+// cost its thread about 90 cycles of register moves, and the tensor core waited.)
+__device__ __forceinline__ uint32_t pt_elect() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void pt_mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t lead) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
       : "memory");
 }
-// Maxima (sums) over the warp's lanes of N = 16 or 32 rows held one value per lane: lane l ends up with
-// row l mod N.  Half of the rows changes sides at every step, so 31 exchanges serve 32 rows.
-template <int N, bool SUM> __device__ __forceinline__ float pt_rows_reduce(const float* x, int lane) {
-  float v[N];
+__device__ __forceinline__ void pt_mma_16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void pt_commit(uint64_t* bar, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+      ::"r"(smem_u32(bar)), "r"(lead)
+      : "memory");
+}
+// Maxima (sums) over lanes of rows held one value per lane and row.  Half of the rows changes sides at every
+// step, so each step costs what is left of the rows: pt_fold sends rows j and j + N/2 to the two halves of
+// the lanes that differ in bit h, pt_rows_reduce goes on from N rows to one.
+template <bool SUM> __device__ __forceinline__ float pt_fold(float a, float b, int h, bool up) {
+  const float keep = up ? b : a, send = up ? a : b;
+  const float y = __shfl_xor_sync(0xffffffffu, send, h);
+  return SUM ? keep + y : fmaxf(keep, y);
+}
+template <int N, bool SUM> __device__ __forceinline__ float pt_rows_reduce(float (&v)[N], int lane) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) v[j] = x[j];
-  if (N == 16) {
+  for (int h = N / 2; h >= 1; h >>= 1)
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float y = __shfl_xor_sync(0xffffffffu, v[j], 16);
-      v[j] = SUM ? v[j] + y : fmaxf(v[j], y);
-    }
-  }
-#pragma unroll
-  for (int h = N / 2; h >= 1; h >>= 1) {
-    const bool up = lane & h;
-#pragma unroll
-    for (int j = 0; j < h; ++j) {
-      const float keep = up ? v[j + h] : v[j], send = up ? v[j] : v[j + h];
-      const float y = __shfl_xor_sync(0xffffffffu, send, h);
-      v[j] = SUM ? keep + y : fmaxf(keep, y);
-    }
-  }
+    for (int j = 0; j < h; ++j) v[j] = pt_fold<SUM>(v[j], v[j + h], h, lane & h);
   return v[0];
+}
+// Two fp32 values at a time.
+__device__ __forceinline__ uint64_t pt_pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 pt_unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t pt_fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t pt_mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t pt_add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+template <int N> __device__ __forceinline__ void pt_ld(uint32_t addr, uint32_t (&r)[N]) {
+  if constexpr (N == 16) tmem_ld16(addr, r);
+  else tmem_ld32(addr, r);
+}
+__device__ __forceinline__ void pt_st16(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15, %16};"
+      ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
 }
 template <int ID, int N> __device__ __forceinline__ void pt_bar() {
   asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(N) : "memory");
@@ -99,78 +150,62 @@ template <int BYTES> __device__ __forceinline__ uint32_t pt_piece(int r, int c) 
   const int x = BYTES == 128 ? (r & 7) : BYTES == 64 ? ((r >> 1) & 3) : BYTES == 32 ? ((r >> 2) & 1) : 0;
   return (uint32_t)(r * BYTES + ((c ^ x) << 4));
 }
-// Instruction descriptor, fp32 accumulate, M = 128; fmt 1 = bf16 (kind::f16), 0 = e4m3 (kind::f8f6f4).
-__device__ __forceinline__ uint32_t pt_idesc(uint32_t fmt, int n, int a_mn, int b_mn) {
-  return (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+// Instruction descriptor, fp32 accumulate, M = 128; formats: kind::f16 1 = bf16, kind::f8f6f4 0 = e4m3, 1 = e5m2.
+__device__ __forceinline__ uint32_t pt_idesc(uint32_t fmt_a, uint32_t fmt_b, int n, int a_mn, int b_mn) {
+  return (1u << 4) | (fmt_a << 7) | (fmt_b << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
          ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
 // ------------------------------------------------------------------------------------------ layout
 template <int D, int NR> struct pt_cfg {
-  static constexpr int RW = NR < 32 ? NR : 32;         // rows of a softmax group
-  static constexpr int NRG = NR / RW;                  // groups that share a tile
-  static constexpr int NP = 4 / NRG;                   // tiles in the groups' hands at a time
-  static constexpr int TPS = NP == 1 ? 1 : 2;          // 8-bit tiles of a stage
-  static constexpr int WK = NP == 1 ? 64 : 128;        // keys of a bf16 tile
-  static constexpr int SLOT = WK * D * 2;              // a bf16 tile, or TPS 8-bit tiles
-  static constexpr int KST = NR == 128 ? 3 : 2;
-  static constexpr int VST = NR == 128 || NR == 16 ? 3 : 2;
+  static constexpr int SLOT = PT_KEYS * D;             // an 8-bit tile of 128 keys or a bf16 tile of 64
+  static constexpr int KST = NR == 64 ? 3 : 4;
+  static constexpr int VST = NR == 64 ? 2 : NR == 32 ? 3 : 4;
   static constexpr int Q8 = NR * D;                    // one of the two e4m3 parts of the queries
-  static constexpr int Q16 = NR * D * 2;
-  static constexpr int PG = PT_KEYS * RW * 2;          // a group's weights: two e4m3 parts, or bf16
-  static constexpr int PT = NRG * PG;                  // the weights of a tile
-  static constexpr int MB = (NP - 1) * NR * 512;       // sums handed over at a unit's end, over the weights
-  static constexpr int PBYTES = 4 * PG > MB ? 4 * PG : MB;
+  static constexpr int PROW = 2 * NR;                  // bytes of a key's weights
+  static constexpr int PB = PT_KEYS * PROW;            // a group's weights of a tile
+  static constexpr int VB = PT_KEYS * D * 2;           // a tile of V in fp16
   static constexpr int OFF_Q16 = 2 * Q8;
-  static constexpr int OFF_P = OFF_Q16 + Q16;
-  static constexpr int OFF_K = OFF_P + PBYTES;
+  static constexpr int OFF_P = OFF_Q16 + NR * D * 2;   // (the second group hands its sums over in the same place)
+  static constexpr int OFF_W = OFF_P + 2 * PB;
+  static constexpr int OFF_K = OFF_W + 2 * VB;
   static constexpr int OFF_V = OFF_K + KST * SLOT;
-  static constexpr int OFF_X = OFF_V + VST * SLOT + 1024;   // (a head size of 64 reads one row group further)
-  static constexpr uint32_t COLS = 16 * RW;            // S and O, two buffers each, of four groups
+  // (behind the rings: a bf16 K tile is read as 128 rows, a head size of 64 one row group further in V)
+  static constexpr int OFF_X = OFF_V + VST * SLOT + 1024;
+  static constexpr uint32_t O_COL = 4 * NR;            // S: two buffers per group
+  static constexpr uint32_t COLS = 6 * NR <= 128 ? 128 : 6 * NR <= 256 ? 256 : 512;
 };
 
-struct pt_info {                     // one stage, written by the producer
-  int live[2];                       // live keys of the tile(s), may pass the tile's
-  int open_rows, open16;             // bf16 tile: first row past the open page's tokens, and past their padding
-  float sk[16], lsv[16], isv[16];    // per page: K scale, log2 and inverse of the V scale
+struct pt_info {                     // one tile, written by the producer; bf16 tiles: rows of the tile
+  int live;                          // live keys (may pass the tile's)
+  int open_rows, open16;             // first row past the open page's tokens, and past their padding
+  int pad;
+  float sk[8], sv[8], lsv[8];        // per page: K scale, V scale and its log2
 };
 
 template <int D, int NR> struct alignas(16) pt_tail {
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
-  uint64_t info_full[PT_INFO], s_full[4][2], p_full[4], o_full[4], q_full;
+  uint64_t info_full[PT_INFO], s_full[2][2], p_full[2], p_empty[2], w_full[8], w_empty[2], q_full;
   uint32_t tmem_base;
   int abort_flag;
   long long cum[JK_MAX_ROWS + 1];    // tiles before each sequence
   int n8[JK_MAX_ROWS], n16[JK_MAX_ROWS];
   pt_info info[PT_INFO];
-  float q_max[16];
+  float q_max[8];
+  // of the unit at work, for what comes after its tiles
+  int seg_b, seg_slot, seg_whole;
+  float c8;                          // logits per product of codes, in units of log2
+  uint32_t vis[2][PT_SOFTMAX];       // masked tiles: rows (of either half) that see the thread's key
   int rowoff[NR];                    // output row of each query row, -1 = none
   int parent[JK_MAX_TREE];
   alignas(16) uint32_t anc[4][NR];   // tree nodes each query row sees
-  // per warp and row, so that a step has one barrier: the four warps of a group form the same values
-  alignas(16) float ref[16][32], alpha[16][2][32], beta[16][2][32];
-  float wmax[4][2][4][32], m_run[4][32], lsum[16][32];
+  // per warp and row (the four warps of a group form the same values)
+  alignas(16) float nref[8][NR], alpha[8][NR];
+  float wmax[2][4][NR], m_run[2][NR], lsum[8][NR], wt[2][NR];
 };
 
-// The stages of a segment [t0, t1) of a unit with n8 8-bit tiles in front: every role walks them.
-template <int TPS, int NP> struct pt_iter {
-  int tile, t1, n8, turn;
-  __device__ __forceinline__ void start(int t0, int end, int n8_) { tile = t0; t1 = end; n8 = n8_; turn = 0; }
-  // n tiles from `first` on; tile j is worked on by the groups of turn (w + j) mod NP
-  __device__ __forceinline__ bool next(int& first, int& n, int& w, bool& wide) {
-    if (tile >= t1) return false;
-    first = tile;
-    wide = tile >= n8;
-    n = (TPS == 2 && !wide && tile + 1 < t1 && tile + 1 < n8) ? 2 : 1;
-    w = turn;
-    turn = (turn + n) & (NP - 1);
-    tile += n;
-    return true;
-  }
-};
-
-// Tiles of every sequence, and their prefix sums, by one warp.  wk: keys of a bf16 tile.
-__device__ __forceinline__ void pt_count(const jk_paged& c, int B, int M, int wk, int units, int lane, long long* cum,
+// Tiles of every sequence, and their prefix sums, by one warp.
+__device__ __forceinline__ void pt_count(const jk_paged& c, int B, int M, int units, int lane, long long* cum,
                                          int* n8, int* n16, int32_t* status) {
   long long run = 0;
   for (int b0 = 0; b0 < B; b0 += 32) {
@@ -183,7 +218,7 @@ __device__ __forceinline__ void pt_count(const jk_paged& c, int B, int M, int wk
       } else {
         const int nf = P / c.page_size * c.page_size;
         a = (nf + PT_KEYS - 1) / PT_KEYS;
-        w = (((P - nf + 15) & ~15) + M + wk - 1) / wk;
+        w = (((P - nf + 15) & ~15) + M + PT_WKEYS - 1) / PT_WKEYS;
       }
     }
     long long incl = (long long)(a + w) * units;
@@ -212,9 +247,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     int Hq, int Hkv, int n_qblk, __nv_bfloat16* __restrict__ out, float* __restrict__ part_o,
     float* __restrict__ part_ml, int32_t* status) {
   typedef pt_cfg<D, NR> F;
-  constexpr int RW = F::RW, NRG = F::NRG, NP = F::NP, KST = F::KST, VST = F::VST, WK = F::WK;
+  constexpr int KST = F::KST, VST = F::VST;
   constexpr int KB = D / 64;
-  constexpr uint32_t O_COL = 8 * RW;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   unsigned char* sk = smem + F::OFF_K;
@@ -222,7 +256,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
   typedef pt_tail<D, NR> tail_t;
   tail_t& X = *reinterpret_cast<tail_t*>(smem + F::OFF_X);
   volatile int* abort_flag = &X.abort_flag;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = Hq / Hkv, units = Hkv * n_qblk, ps = c.page_size;
 
   if (tid == 0) {
@@ -231,20 +265,22 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       mbar_init(&X.v_full[i], 1); mbar_init(&X.v_empty[i], 1);
     }
     for (int i = 0; i < PT_INFO; ++i) mbar_init(&X.info_full[i], 1);
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) mbar_init(&X.w_full[i], 1);
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&X.s_full[i][0], 1); mbar_init(&X.s_full[i][1], 1);
-      mbar_init(&X.p_full[i], 4 * NRG); mbar_init(&X.o_full[i], 1);
+      mbar_init(&X.p_full[i], 4); mbar_init(&X.p_empty[i], 1);
+      mbar_init(&X.w_empty[i], 1);
     }
     mbar_init(&X.q_full, PT_SOFTMAX / 32);
     X.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 17) {
+  if (warp == 13) {
     tmem_alloc(&X.tmem_base, F::COLS);
     tmem_relinquish();
   }
   jk_pdl_wait();
-  if (warp == 16) pt_count(c, B, M, F::WK, units, lane, X.cum, X.n8, X.n16, blockIdx.x == 0 ? status : nullptr);
+  if (warp == 12) pt_count(c, B, M, units, lane, X.cum, X.n8, X.n16, blockIdx.x == 0 ? status : nullptr);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -253,49 +289,49 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
   // with fewer tiles than CTAs the first `total` CTAs take one each (an empty share would leave a gap)
   const long long ctas = total < gridDim.x ? total : gridDim.x;
   const bool idle = blockIdx.x >= ctas;
-  const long long w0 = idle ? 0 : total * blockIdx.x / ctas, w1 = idle ? 0 : total * (blockIdx.x + 1) / ctas;
+  const long long w0 = idle ? 0 : total * blockIdx.x / ctas;
+  const int share = idle ? 0 : (int)(total * (blockIdx.x + 1) / ctas - w0);
   bool ok = true;
 
-  // a segment of the CTA's range: unit (b, u), tiles [t0, t1)
-  auto segment = [&](long long t, int& b, int& u, int& t0, int& t1, int& nt) {
+  // a segment of the CTA's share: unit (b, u), tiles [t0, t1) of its nt; n8 of them 8-bit
+  auto segment = [&](int done, int& b, int& u, int& t0, int& t1, int& nt) {
+    const long long t = w0 + done;
     b = 0;
     while (X.cum[b + 1] <= t) ++b;
     nt = X.n8[b] + X.n16[b];
     const long long off = t - X.cum[b];
     u = (int)(off / nt);
     t0 = (int)(off - (long long)u * nt);
-    const long long left = w1 - t;
-    t1 = left < nt - t0 ? t0 + (int)left : nt;
+    t1 = share - done < nt - t0 ? t0 + share - done : nt;
   };
 
-  if (warp == 16 || warp == 18) {
-    // ==================================================================== TMA producers: K (16), V (18)
-    const bool is_k = warp == 16;
+  // registers: 512 x 128 at launch = 256 x 72 + 256 x 184 (each warpgroup sets its own at the top of its roles)
+  if (warp >= 12) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  if (warp == 12 || warp == 14) {
+    // ==================================================================== TMA producers: K (12), V (14)
+    const bool is_k = warp == 12;
     const int NST = is_k ? KST : VST;
     uint64_t* full = is_k ? X.k_full : X.v_full;
     uint64_t* empty = is_k ? X.k_empty : X.v_empty;
     unsigned char* ring = is_k ? sk : sv;
     const CUtensorMap* map = is_k ? &map_k : &map_v;
-    int sc = 0, s_slot = 0, s_par = 1;                  // stages so far, their slot and its parity
+    int tc = 0, s_slot = 0, s_par = 1;                  // tiles so far, the slot and its parity
     // pages are read once, unless several row blocks of a kv head come by
     const uint64_t pol = l2_policy_evict_first();
     const bool once = n_qblk == 1;
     const int per = PT_KEYS / ps;                       // pages of a tile
-    for (long long t = w0; t < w1 && ok;) {
+    for (int done = 0; done < share && ok;) {
       int b, u, t0, t1, nt;
-      segment(t, b, u, t0, t1, nt);
-      t += t1 - t0;
+      segment(done, b, u, t0, t1, nt);
+      done += t1 - t0;
       const int h = u / n_qblk, n8 = X.n8[b];
       const int P = c.kv_len[b], nf = P / ps * ps, n_pg = P / ps;
       const int open_rows = P - nf, open16 = (open_rows + 15) & ~15;
       const int32_t* tab = c.page_table + (size_t)b * c.max_pages;
-      pt_iter<F::TPS, NP> it;
-      it.start(t0, t1, n8);
-      int first, n, w;
-      bool wide;
       // Page ids and scales in batches of 32 pages, lane l the batch's page l, the ids of the next batch
-      // asked for a batch ahead: two dependent loads per stage would be the stage's time.
-      int at = t0 * per, id = 0, id_next = 0;
+      // asked for a batch ahead: two dependent loads per tile would be the tile's time.
+      int at = t0 * per / 32 * 32, id = 0, id_next = 0;
       float ksc = 1.f, vsc = 1.f;
       auto ask = [&](int p0) { return p0 + lane < n_pg ? tab[p0 + lane] : 0; };
       auto take = [&](int raw) {                        // the batch from `at` on
@@ -312,26 +348,15 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         id_next = ask(at + 32);
       };
       if (t0 < n8) take(ask(at));
-      while (ok && it.next(first, n, w, wide)) {
+      for (int tile = t0; tile < t1 && ok; ++tile, ++tc) {
+        pt_info& I = X.info[tc % PT_INFO];
         ok = __all_sync(0xffffffffu, mbar_wait(&empty[s_slot], s_par, abort_flag, status));
         unsigned char* dst = ring + s_slot * F::SLOT;
-        pt_info& I = X.info[sc % PT_INFO];
-        if (!wide) {
-          const int p0 = first * per, np = min(n * per, n_pg - p0);
-          // a stage has at most 16 pages and starts at a multiple of its tile: it may span two batches
+        if (tile < n8) {
+          // (a tile's pages never span two batches: both start at multiples of the tile's page count)
+          const int p0 = tile * per, np = min(per, n_pg - p0);
           if (p0 >= at + 32) { at += 32; take(id_next); }
-          int page = __shfl_sync(0xffffffffu, id, (p0 - at + lane) & 31);
-          float k1 = __shfl_sync(0xffffffffu, ksc, (p0 - at + lane) & 31);
-          float v1 = __shfl_sync(0xffffffffu, vsc, (p0 - at + lane) & 31);
-          if (p0 + np > at + 32) {
-            const int split = at + 32 - p0;             // lanes from here on belong to the next batch
-            at += 32;
-            take(id_next);
-            const int pg2 = __shfl_sync(0xffffffffu, id, (p0 - at + lane) & 31);
-            const float k2 = __shfl_sync(0xffffffffu, ksc, (p0 - at + lane) & 31);
-            const float v2 = __shfl_sync(0xffffffffu, vsc, (p0 - at + lane) & 31);
-            if (lane >= split) { page = pg2; k1 = k2; v1 = v2; }
-          }
+          const int page = __shfl_sync(0xffffffffu, id, (p0 - at + lane) & 31);
           if (ok && lane == 0) mbar_expect_tx(&full[s_slot], (uint32_t)np * ps * D);
           __syncwarp();
           if (ok && lane < np) {
@@ -340,38 +365,38 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
             else tma_load_4d(dst + lane * ps * D, map, 0, 0, h, row, &full[s_slot]);
           }
           if (is_k) {
-            if (lane < 16) {
-              const int e = (int)(__float_as_uint(v1) >> 23) - 127;
+            const float k1 = __shfl_sync(0xffffffffu, ksc, (p0 - at + lane) & 31);
+            const float v1 = __shfl_sync(0xffffffffu, vsc, (p0 - at + lane) & 31);
+            if (lane < per) {
               I.sk[lane] = k1;
-              I.lsv[lane] = (float)e;
-              I.isv[lane] = paged_pow2(-e);
+              I.sv[lane] = v1;
+              I.lsv[lane] = (float)((int)(__float_as_uint(v1) >> 23) - 127);
             }
-            if (lane < 2) I.live[lane] = min(PT_KEYS, nf - (first + lane) * PT_KEYS);
+            if (lane == 0) I.live = nf - tile * PT_KEYS;
           }
         } else {
           // bf16 tile: rows g of (open rows, padded to 16, then tree rows) in boxes of 16
-          const int base = (first - n8) * WK;
+          const int base = (tile - n8) * PT_WKEYS;
           const int g = base + (lane / KB) * 16, kb = lane % KB;
           const bool in_open = g < open16;
-          const bool mine = lane < WK / 16 * KB && (in_open || g - open16 < M);
+          const bool mine = lane < PT_WKEYS / 16 * KB && (in_open || g - open16 < M);
           const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * 16 * 64 * 2;
           const int row = in_open ? (nf & (2 * ps - 1)) + g : g - open16;
           const int outer = in_open ? layer * c.max_seqs + b : b;
           if (ok && lane == 0) mbar_expect_tx(&full[s_slot], bytes);
           __syncwarp();
           if (ok && mine)
-            tma_load_4d(dst + kb * (WK * 128) + (lane / KB) * 16 * 128,
+            tma_load_4d(dst + kb * (PT_WKEYS * 128) + (lane / KB) * 16 * 128,
                         is_k ? (in_open ? &map_ko : &map_kt) : (in_open ? &map_vo : &map_vt), kb * 64, row, h, outer,
                         &full[s_slot]);
           if (is_k && lane == 0) {
-            I.live[0] = open16 + M - base;
+            I.live = open16 + M - base;
             I.open_rows = open_rows - base;
             I.open16 = open16 - base;
           }
         }
         __syncwarp();
-        if (is_k && lane == 0) mbar_arrive(&X.info_full[sc % PT_INFO]);
-        ++sc;
+        if (is_k && lane == 0) mbar_arrive(&X.info_full[tc % PT_INFO]);
         if (++s_slot == NST) { s_slot = 0; s_par ^= 1; }
       }
     }
@@ -380,105 +405,101 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       const unsigned long long ts = global_ns();
       while (global_ns() - ts < 2000000ull) { /* 2 ms: far longer than any TMA copy */ }
     }
-  } else if (warp == 17) {
-    if (lane == 0) {
+  } else if (warp == 13) {
+    {
       // ================================================================== MMA issuer
       const uint32_t q8 = smem_u32(smem), q16 = smem_u32(smem + F::OFF_Q16), pb = smem_u32(smem + F::OFF_P);
-      const uint32_t ka0 = smem_u32(sk), va0 = smem_u32(sv);
-      const uint32_t id_s8 = pt_idesc(0, NR, 0, 0), id_s16 = pt_idesc(1, NR, 0, 0);
-      const uint32_t id_p8 = pt_idesc(0, NR, 1, 1), id_p16 = pt_idesc(1, NR, 1, 1);
-      int ks_n = 0, vs_n = 0, segs = 0;
-      uint32_t cs = 0, cp = 0;                          // tiles per turn so far, a byte each (mod 256)
-      auto issue_s = [&](int n, int w, bool wide) {
-        const int slot = ks_n % KST;
-        if (!mbar_wait(&X.k_full[slot], (ks_n / KST) & 1, abort_flag, status)) { ok = false; return; }
+      const uint32_t ka0 = smem_u32(sk), va0 = smem_u32(sv), wa0 = smem_u32(smem + F::OFF_W);
+      const uint32_t id_s8 = pt_idesc(0, 0, NR, 0, 0), id_s16 = pt_idesc(1, 1, NR, 0, 0);
+      const uint32_t id_p = pt_idesc(0, 0, NR, 1, 1), id_p16 = pt_idesc(1, 1, NR, 1, 1);
+      int k_slot = 0, k_par = 0, v_slot = 0, v_tile = 0, w_buf = 0, segs = 0;
+      int cs0 = 0, cs1 = 0, cp0 = 0, cp1 = 0;           // tiles per group so far
+      const uint32_t lead = pt_elect();
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      auto waits = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status)) != 0; };
+      auto ready = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(bar, parity)) != 0; };
+      auto issue_s = [&](int tp, bool wide) {
+        const int buf = (tp ? cs1 : cs0) & 1;
+        if (!waits(&X.k_full[k_slot], k_par)) { ok = false; return; }
         tc_fence_after();
-        const uint32_t ka = ka0 + slot * F::SLOT;
-        for (int j = 0; j < n; ++j) {
-          const int tp = (w + j) & (NP - 1);
-          const uint32_t buf = (cs >> (8 * tp)) & 1;
-          const uint32_t d = tmem + (buf * NP + tp) * NR;
-          if (!wide) {
-            const uint32_t kt = ka + j * (PT_KEYS * D);
+        const uint32_t d = tm + (tp * 2 + buf) * NR, kt = ka0 + k_slot * F::SLOT;
+        if (!wide) {
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+          for (int part = 0; part < 2; ++part)
 #pragma unroll
-              for (int k = 0; k < D / 32; ++k)
-                pt_mma_f8(d, pt_desc(kt + k * 32, 16, 8 * D, pt_layout(D)),
-                          pt_desc(q8 + part * F::Q8 + k * 32, 16, 8 * D, pt_layout(D)), id_s8, (part | k) ? 1u : 0u);
-          } else {
+            for (int k = 0; k < D / 32; ++k)
+              pt_mma_f8(d, pt_desc(kt + k * 32, 16, 8 * D, pt_layout(D)),
+                        pt_desc(q8 + part * F::Q8 + k * 32, 16, 8 * D, pt_layout(D)), id_s8, (part | k) ? 1u : 0u, lead);
+        } else {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
+          for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                tc_mma_bf16(d, pt_desc(ka + kb * (WK * 128) + k * 32, 16, 1024, 2),
-                            pt_desc(q16 + kb * (NR * 128) + k * 32, 16, 1024, 2), id_s16, (kb | k) ? 1u : 0u);
-          }
-          tc_commit(&X.s_full[tp][buf]);
-          cs = (cs & ~(0xffu << (8 * tp))) | ((((cs >> (8 * tp)) + 1) & 0xffu) << (8 * tp));
+            for (int k = 0; k < 4; ++k)
+              pt_mma_16(d, pt_desc(kt + kb * (PT_WKEYS * 128) + k * 32, 16, 1024, 2),
+                          pt_desc(q16 + kb * (NR * 128) + k * 32, 16, 1024, 2), id_s16, (kb | k) ? 1u : 0u, lead);
         }
-        tc_commit(&X.k_empty[slot]);
-        ++ks_n;
+        pt_commit(&X.k_empty[k_slot], lead);
+        if (++k_slot == KST) { k_slot = 0; k_par ^= 1; }
+        pt_commit(&X.s_full[tp][buf], lead);
+        if (tp) ++cs1; else ++cs0;
       };
-      auto issue_pv = [&](int n, int w, bool wide) {
-        const int slot = vs_n % VST;
-        if (!mbar_wait(&X.v_full[slot], (vs_n / VST) & 1, abort_flag, status)) { ok = false; return; }
-        const uint32_t va = va0 + slot * F::SLOT;
-        for (int j = 0; j < n; ++j) {
-          const int tp = (w + j) & (NP - 1);
-          const uint32_t buf = (cp >> (8 * tp)) & 1;
-          if (!mbar_wait(&X.p_full[tp], buf, abort_flag, status)) { ok = false; return; }
-          tc_fence_after();
-          const uint32_t d = tmem + O_COL + (buf * NP + tp) * NR;
-          const uint32_t p = pb + tp * F::PT;
-          if (!wide) {
-            const uint32_t vt = va + j * (PT_KEYS * D);
+      auto issue_pv = [&](int tp, bool wide, bool add) {
+        if (!waits(&X.p_full[tp], (tp ? cp1 : cp0) & 1) || !waits(&X.w_full[v_tile & 7], (v_tile >> 3) & 1)) { ok = false; return; }
+        tc_fence_after();
+        const uint32_t d = tm + F::O_COL + tp * NR, p = pb + tp * F::PB;
+        if (!wide) {
+          const uint32_t vt = wa0 + w_buf * F::VB;
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+          for (int k = 0; k < PT_KEYS / 16; ++k)
+            pt_mma_16(d, pt_desc(vt + k * 2048, KB == 2 ? PT_KEYS * 128 : 1024, 1024, 2),
+                        pt_desc(p + k * 16 * F::PROW, 8 * F::PROW, 8 * F::PROW, pt_layout(F::PROW)), id_p, (add || k) ? 1u : 0u, lead);
+          pt_commit(&X.w_empty[w_buf], lead);
+          w_buf ^= 1;
+        } else {
+          const uint32_t vt = va0 + v_slot * F::SLOT;
 #pragma unroll
-              for (int k = 0; k < PT_KEYS / 32; ++k)
-                pt_mma_f8(d, pt_desc(vt + k * 32 * D, 8 * D, 8 * D, pt_layout(D)),
-                          pt_desc(p + part * (PT_KEYS * RW) + k * 32 * RW, NRG > 1 ? F::PG : 8 * RW, 8 * RW, pt_layout(RW)),
-                          id_p8, (part | k) ? 1u : 0u);
-          } else {
-#pragma unroll
-            for (int k = 0; k < WK / 16; ++k)
-              tc_mma_bf16(d, pt_desc(va + k * 2048, KB == 2 ? WK * 128 : 1024, 1024, 2),
-                          pt_desc(p + k * 32 * RW, NRG > 1 ? F::PG : 16 * RW, 16 * RW, pt_layout(2 * RW)), id_p16, k ? 1u : 0u);
-          }
-          tc_commit(&X.o_full[tp]);
-          cp = (cp & ~(0xffu << (8 * tp))) | ((((cp >> (8 * tp)) + 1) & 0xffu) << (8 * tp));
+          for (int k = 0; k < PT_WKEYS / 16; ++k)
+            pt_mma_16(d, pt_desc(vt + k * 2048, KB == 2 ? PT_WKEYS * 128 : 1024, 1024, 2),
+                        pt_desc(p + k * 16 * F::PROW, 8 * F::PROW, 8 * F::PROW, pt_layout(F::PROW)), id_p16, (add || k) ? 1u : 0u, lead);
+          pt_commit(&X.v_empty[v_slot], lead);
         }
-        tc_commit(&X.v_empty[slot]);
-        ++vs_n;
+        if (++v_slot == VST) v_slot = 0;
+        ++v_tile;
+        pt_commit(&X.p_empty[tp], lead);
+        if (tp) ++cp1; else ++cp0;
       };
-      for (long long t = w0; t < w1 && ok;) {
+      for (int done = 0; done < share && ok;) {
         int b, u, t0, t1, nt;
-        segment(t, b, u, t0, t1, nt);
-        t += t1 - t0;
-        ok = mbar_wait(&X.q_full, segs & 1, abort_flag, status);
+        segment(done, b, u, t0, t1, nt);
+        done += t1 - t0;
+        ok = waits(&X.q_full, segs & 1);
         ++segs;
-        if (!ok) break;
         tc_fence_after();
-        pt_iter<F::TPS, NP> is, ip;
-        is.start(t0, t1, X.n8[b]);
-        ip.start(t0, t1, X.n8[b]);
-        int first, n, w, ahead = 0;
-        bool wide, more = true;
-        // S runs two stages ahead of the second product: S of stage i + 2 reuses the columns of stage i,
-        // which are free once the weights of stage i have been written
-        while (ok) {
-          if (more && (more = is.next(first, n, w, wide))) {
-            issue_s(n, w, wide);
-            ++ahead;
+        const int n8 = __shfl_sync(0xffffffffu, X.n8[b], 0);
+        t0 = __shfl_sync(0xffffffffu, t0, 0);
+        t1 = __shfl_sync(0xffffffffu, t1, 0);
+        int ts = t0, tv = t0;                           // next tile of either product
+        // Whichever has its inputs goes first: the oldest tile's second product, or the next tile's S, whose
+        // columns are free once the weights of the tile PT_AHEAD before it have been written.
+        long long c0 = clock64();
+        while (ok && tv < t1) {
+          const bool can_s = ts < t1 && ts - tv < PT_AHEAD, can_v = tv < ts;
+          const int sp = (ts - t0) & 1, vp = (tv - t0) & 1;
+          if (can_v && (!can_s || ready(&X.p_full[vp], (vp ? cp1 : cp0) & 1))) {
+            issue_pv(vp, tv >= n8, tv - t0 >= 2);
+            ++tv;
+            c0 = clock64();
+          } else if (can_s && (!can_v || ready(&X.k_full[k_slot], k_par))) {
+            issue_s(sp, ts >= n8);
+            ++ts;
+            c0 = clock64();
+          } else if (__any_sync(0xffffffffu, *abort_flag)) {
+            ok = false;
+          } else if (__any_sync(0xffffffffu, clock64() - c0 > TC_WAIT_CYCLES)) {
+            *abort_flag = 1;
+            jk_set_status(status, JK_ERR_TIMEOUT);
+            ok = false;
           }
-          if (!ok) break;
-          if (ahead == 2 || (!more && ahead > 0)) {
-            ip.next(first, n, w, wide);
-            issue_pv(n, w, wide);
-            --ahead;
-          }
-          if (!more && ahead == 0) break;
         }
       }
       if (!ok) {                                        // products still in flight get a bounded time to end
@@ -486,24 +507,96 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         while (global_ns() - ts < 2000000ull) { }
       }
     }
-  } else if (warp < 16) {
+  }
+  } else if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    // ==================================================================== V to fp16
+    const int ct = tid - 256;                           // 0 .. 127
+    // Four pieces of 16 codes of rows r and r ^ 5 go through eight lanes: both the 16-byte loads (8 pieces of a
+    // swizzled row of codes) and the 16-byte stores (every other piece of a swizzled row of fp16) of such a
+    // group fall into different banks.
+    const int cw = ct >> 5, qw = lane >> 3, rr = (lane & 4) ? qw ^ 5 : qw;
+    int tc = 0, v_slot = 0, v_par = 0, w_n = 0;
+    for (int done = 0; done < share;) {
+      int b, u, t0, t1, nt;
+      segment(done, b, u, t0, t1, nt);
+      done += t1 - t0;
+      const int n8 = X.n8[b];
+      for (int tile = t0; tile < t1; ++tile, ++tc) {
+        const pt_info& I = X.info[tc % PT_INFO];
+        if (ok) ok = mbar_wait(&X.info_full[tc % PT_INFO], (tc / PT_INFO) & 1, abort_flag, status);
+        if (ok) ok = mbar_wait(&X.v_full[v_slot], v_par, abort_flag, status);
+        unsigned char* src = sv + v_slot * F::SLOT;
+        if (tile < n8) {
+          const int buf = w_n & 1, live = I.live;
+          if (ok && w_n >= 2) ok = mbar_wait(&X.w_empty[buf], ((w_n >> 1) & 1) ^ 1, abort_flag, status);
+          unsigned char* dst = smem + F::OFF_W + buf * F::VB;
+          // a warp's step: 8 rows, four pieces (64 dims); D / 64 such halves of 16 groups of rows
+#pragma unroll 4
+          for (int i = cw; i < 16 * KB; i += 4) {
+            const int kb = i % KB, r = (i / KB) * 8 + rr, pc = lane & 3;
+            uint4 v = *reinterpret_cast<const uint4*>(src + pt_piece<D>(r, kb * 4 + pc));
+            if (r >= live) v = make_uint4(0u, 0u, 0u, 0u);   // rows behind the last page may hold anything
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t o[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j] & 0xffffu), __NV_E4M3);
+              const __half2_raw e = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j] >> 16), __NV_E4M3);
+              o[2 * j] = *reinterpret_cast<const uint32_t*>(&a);
+              o[2 * j + 1] = *reinterpret_cast<const uint32_t*>(&e);
+            }
+            unsigned char* d = dst + kb * (PT_KEYS * 128);
+            *reinterpret_cast<uint4*>(d + pt_piece<128>(r, pc * 2)) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(d + pt_piece<128>(r, pc * 2 + 1)) = make_uint4(o[4], o[5], o[6], o[7]);
+          }
+          ++w_n;
+        } else if (ct < PT_WKEYS) {
+          // rows that no live key owns may hold anything, NaN included, and 0 * NaN would reach every row
+          if (ct >= I.live || (ct >= I.open_rows && ct < I.open16)) {
+#pragma unroll 1
+            for (int i = 0; i < D / 8; ++i)
+              *reinterpret_cast<uint4*>(src + (i >> 3) * (PT_WKEYS * 128) + ct * 128 + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        fence_proxy_async_smem();
+        pt_bar<4, 128>();
+        if (ct == 0) {
+          mbar_arrive(&X.w_full[tc & 7]);
+          if (tile < n8) mbar_arrive(&X.v_empty[v_slot]);   // (a bf16 tile is read where it is)
+        }
+        if (++v_slot == VST) { v_slot = 0; v_par ^= 1; }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     // ==================================================================== softmax groups
-    const int grp = warp >> 2, wq = warp & 3;           // group, tensor-memory lane quarter
-    const int rg = grp % NRG, tp = grp / NRG;           // its rows of the block, its turn among the tiles
+    const int tp = warp >> 2, wq = warp & 3;            // group, tensor-memory lane quarter
     const int kl = wq * 32 + lane;                      // this thread's key of a tile / head dim of O
     const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
-    unsigned char* pbuf = smem + F::OFF_P + tp * F::PT + rg * F::PG;
-    const int grow = rg * RW;                           // first row of this group in the block
-    auto group_bar = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory"); };
-    int cnt = 0, sc = 0;                                // tiles of this group, stages of the CTA
-    for (long long t = w0; t < w1;) {
+    unsigned char* pbuf = smem + F::OFF_P + tp * F::PB;
+    const uint32_t oa = tmem + lane_base + F::O_COL + tp * NR;
+    const int pg = kl / ps;                             // page of the key within a tile
+    const float c16 = scale * 1.4426950408889634f;
+    auto group_or = [&](bool mine) {                    // a barrier that tells whether any thread said yes
+      uint32_t r;
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 128, p;\n\t"
+          "selp.u32 %0, 1, 0, q;\n\t}"
+          : "=r"(r)
+          : "r"((uint32_t)mine), "r"(tp + 1)
+          : "memory");
+      return r != 0;
+    };
+    auto group_bar = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(tp + 1) : "memory"); };
+    auto scale_pow2 = [](float from, float to) { return from == -INFINITY ? 0.f : fast_exp2(from - to); };
+    int cnt = 0, tc = 0;                                // tiles of this group, tiles of the CTA
+    for (int done = 0; done < share;) {
       int b, u, t0, t1, nt;
-      segment(t, b, u, t0, t1, nt);
-      const bool whole = t0 == 0 && t1 == nt;
-      // a partial that does not start its unit is this CTA's first, else its last
-      const int slot = (int)(blockIdx.x * 2 + (t0 == 0 ? 1 : 0));
-      t += t1 - t0;
-      const int h = u / n_qblk, row0 = (u % n_qblk) * NR, n_rows = G * M, n8 = X.n8[b];
+      segment(done, b, u, t0, t1, nt);
+      done += t1 - t0;
+      const int n8 = X.n8[b];
+      const int h = u / n_qblk, row0 = (u % n_qblk) * NR, n_rows = G * M;
       // ------------------------------------------------ queries of the unit
       constexpr int QV = (NR * (D / 8) + PT_SOFTMAX - 1) / PT_SOFTMAX;
       uint4 qv[QV];
@@ -529,8 +622,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       amax = jk_warp_max(amax);
       if (lane == 0) X.q_max[warp] = amax;
       // (also: all groups are done with the previous unit's queries, sums and row tables)
-      pt_bar<5, PT_SOFTMAX>();
-      amax = jk_warp_max(X.q_max[lane & 15]);
+      pt_bar<3, PT_SOFTMAX>();
+      amax = jk_warp_max(X.q_max[lane & 7]);
       int qe = (int)(__float_as_uint(amax) >> 23) - 127 - 8 + ((__float_as_uint(amax) & 0x7fffffu) > 0x600000u ? 1 : 0);
       qe = max(-100, min(100, qe));
       const float qinv = paged_pow2(-qe);
@@ -577,270 +670,292 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
 #pragma unroll
         for (int i = 0; i < 4; ++i) X.anc[i][tid] = a[i];
       }
-      pt_bar<5, PT_SOFTMAX>();                          // row tables are visible
-      const float c16 = scale * 1.4426950408889634f, c8 = c16 * paged_pow2(qe);
+      if (tid == 0) {
+        X.seg_b = b;
+        // a partial that does not start its unit is this CTA's first, else its last
+        X.seg_slot = (int)(blockIdx.x * 2 + (t0 == 0 ? 1 : 0));
+        X.seg_whole = t0 == 0 && t1 == nt;
+        X.c8 = scale * 1.4426950408889634f * paged_pow2(qe);
+      }
+      pt_bar<3, PT_SOFTMAX>();                          // row tables are visible
 
-      float acc[RW], lacc[RW];
+      constexpr int CH = NR < 32 ? NR : 32, SL = NR / CH;   // rows of a lane's share of row values, shares
+      float2 lacc[NR / 2];                              // sums of the weights of this thread's keys, unit 2^ref
 #pragma unroll
-      for (int i = 0; i < RW; ++i) acc[i] = lacc[i] = 0.f;
-      float run = -INFINITY;                            // running reference of row lane (mod RW)
-      bool pending = false, moved_before = false;       // the last tile's product is still to be added
-      // acc = alpha acc + beta O of tile `count`.  Its completion has been waited for by every thread of
-      // the group: a wait here, after the arrival for the next tile, could find the barrier two phases on.
-      auto take_o = [&](int count, bool moved) {
-        const int sb = count & 1;
-        __syncwarp();
-        tc_fence_after();
-        const uint32_t oa = tmem + lane_base + O_COL + (sb * NP + tp) * NR + grow;
-        uint32_t r[RW];
-        if constexpr (RW == 32) tmem_ld32(oa, r); else tmem_ld16(oa, r);
-        tmem_ld_wait();
-        if (moved) {
+      for (int i = 0; i < NR / 2; ++i) lacc[i] = make_float2(0.f, 0.f);
+      float ref[SL];                                    // of rows i * CH + lane (mod CH)
 #pragma unroll
-          for (int j = 0; j < RW; j += 4) {
-            const float4 al = *reinterpret_cast<const float4*>(&X.alpha[warp][sb][j]);
-            acc[j] *= al.x; acc[j + 1] *= al.y; acc[j + 2] *= al.z; acc[j + 3] *= al.w;
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < RW; j += 4) {
-          const float4 be = *reinterpret_cast<const float4*>(&X.beta[warp][sb][j]);
-          acc[j] = fmaf(__uint_as_float(r[j]), be.x, acc[j]);
-          acc[j + 1] = fmaf(__uint_as_float(r[j + 1]), be.y, acc[j + 1]);
-          acc[j + 2] = fmaf(__uint_as_float(r[j + 2]), be.z, acc[j + 2]);
-          acc[j + 3] = fmaf(__uint_as_float(r[j + 3]), be.w, acc[j + 3]);
-        }
-      };
+      for (int i = 0; i < SL; ++i) ref[i] = -INFINITY;
+      bool unseen = true;                               // some row has no reference yet
+      const int cnt0 = cnt;                             // tiles before this unit
 
-      pt_iter<F::TPS, NP> it;
-      it.start(t0, t1, n8);
-      int first, n, w;
-      bool wide;
-      for (; it.next(first, n, w, wide); ++sc) {
-        const int part = (tp - w) & (NP - 1);           // tile of the stage
-        if (part >= n) continue;
-        const pt_info& I = X.info[sc % PT_INFO];
-        const int sb = cnt & 1;
-        if (ok) ok = mbar_wait(&X.info_full[sc % PT_INFO], (sc / PT_INFO) & 1, abort_flag, status);
-        float ck = c16, lsv = 0.f, isv = 1.f;
-        bool dead;
-        int tree_row = -1;
-        if (!wide) {
-          const int pg = (part * PT_KEYS + kl) / ps;
-          dead = kl >= I.live[part];
-          ck = c8 * I.sk[pg];
-          lsv = I.lsv[pg];
-          isv = I.isv[pg];
-        } else {
-          dead = kl >= min(WK, I.live[0]) || (kl >= I.open_rows && kl < I.open16);
-          if (kl >= I.open16) tree_row = kl - I.open16;
-        }
-        if (ok) ok = mbar_wait(&X.s_full[tp][sb], (cnt >> 1) & 1, abort_flag, status);
-        __syncwarp();
-        tc_fence_after();
-        const uint32_t sa = tmem + lane_base + (sb * NP + tp) * NR + grow;
-        const bool masked = __any_sync(0xffffffffu, dead || tree_row >= 0);
-        // rows of V that no live key owns may hold anything, NaN included, and 0 * NaN would reach every row
-        if (dead && (!wide || kl < WK)) {
-          if (ok) ok = mbar_wait(&X.v_full[sc % VST], (sc / VST) & 1, abort_flag, status);
-          unsigned char* row = sv + (sc % VST) * F::SLOT + (wide ? kl * 128 : part * (PT_KEYS * D) + kl * D);
-          if (ok) {
-#pragma unroll 1
-            for (int j = 0; j < (wide ? D / 8 : D / 16); ++j)
-              *reinterpret_cast<uint4*>(row + (wide ? (j >> 3) * (WK * 128) + (j & 7) * 16 : j * 16)) = make_uint4(0u, 0u, 0u, 0u);
-          }
-        }
-        __syncwarp();
-        // rows of the block this key is visible to
-        uint32_t vis = 0xffffffffu;
+      for (int tile = t0; tile < t1; ++tile, ++tc) {
+        if (((tile - t0) & 1) != tp) continue;
+        const bool wide = tile >= n8;
+        const pt_info& I = X.info[tc % PT_INFO];
+        if (ok) ok = mbar_wait(&X.info_full[tc % PT_INFO], (tc / PT_INFO) & 1, abort_flag, status);
+        // A tile with keys that not every row sees (dead ones behind the last, tree nodes) leaves the rows that
+        // see this thread's key in vis.
+        const bool masked = wide || I.live < PT_KEYS;
         if (masked) {
-          if (dead) vis = 0u;
-          else if (tree_row >= 0) {
-            const uint32_t* aw = &X.anc[(tree_row >> 5) & 3][grow];
-            vis = 0u;
-#pragma unroll
-            for (int j = 0; j < RW; ++j) vis |= ((aw[j] >> (tree_row & 31)) & 1u) << j;
+          bool dead = kl >= I.live;
+          int node = -1;
+          if (wide) {
+            dead = dead || kl >= PT_WKEYS || (kl >= I.open_rows && kl < I.open16);
+            if (!dead && kl >= I.open16) node = kl - I.open16;
           }
-        }
-        // ---- maxima over the tile of the logits of each row (base 2, with log2 of the V scale)
-        {
-          float x[RW];
-          uint32_t r[RW];
-          if constexpr (RW == 32) tmem_ld32(sa, r); else tmem_ld16(sa, r);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < RW; ++j) x[j] = fmaf(__uint_as_float(r[j]), ck, lsv);
-          if (masked) {
-#pragma unroll
-            for (int j = 0; j < RW; ++j)
-              if (!((vis >> j) & 1u)) x[j] = -INFINITY;
-          }
-          const float m = pt_rows_reduce<RW, false>(x, lane);
-          if (lane < RW) X.wmax[grp][sb][wq][lane] = m;
-        }
-        group_bar();
-        bool moved = false;
-        {
-          const float* wm = &X.wmax[grp][sb][0][lane & (RW - 1)];
-          const float m = fmaxf(fmaxf(wm[0], wm[32]), fmaxf(wm[64], wm[96]));
-          float ref = 0.f, be = 0.f, al = 1.f;
-          if (m != -INFINITY) {
-            ref = ceilf(m);
-            const float now = fmaxf(run, ref);
-            al = run == -INFINITY ? 0.f : fast_exp2(run - now);
-            be = fast_exp2(ref - now);
-            moved = run != now;
-            run = now;
-          }
-          if (lane < RW) {
-            X.ref[warp][lane] = ref - PT_PSHIFT;
-            X.alpha[warp][sb][lane] = al;
-            X.beta[warp][sb][lane] = be;
-          }
-        }
-        moved = __any_sync(0xffffffffu, moved);         // (orders the writes above within the warp)
-        __syncwarp();
-        // ---- the previous product is complete: its weights may be overwritten
-        if (pending && ok) ok = mbar_wait(&X.o_full[tp], (cnt - 1) & 1, abort_flag, status);
-        __syncwarp();
-        if (moved) {
-#pragma unroll
-          for (int j = 0; j < RW; j += 4) {
-            const float4 al = *reinterpret_cast<const float4*>(&X.alpha[warp][sb][j]);
-            lacc[j] *= al.x; lacc[j + 1] *= al.y; lacc[j + 2] *= al.z; lacc[j + 3] *= al.w;
-          }
-        }
-#pragma unroll
-        for (int j0 = 0; j0 < RW; j0 += 16) {
-          uint32_t r[16];
-          float e[16];
-          tmem_ld16(sa + j0, r);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            const float4 rf = *reinterpret_cast<const float4*>(&X.ref[warp][j0 + j]);
-            e[j] = fast_exp2(fmaf(__uint_as_float(r[j]), ck, lsv - rf.x));
-            e[j + 1] = fast_exp2(fmaf(__uint_as_float(r[j + 1]), ck, lsv - rf.y));
-            e[j + 2] = fast_exp2(fmaf(__uint_as_float(r[j + 2]), ck, lsv - rf.z));
-            e[j + 3] = fast_exp2(fmaf(__uint_as_float(r[j + 3]), ck, lsv - rf.w));
-          }
-          if (masked) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (!((vis >> (j0 + j)) & 1u)) e[j] = 0.f;
-          }
-#pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            const float4 be = *reinterpret_cast<const float4*>(&X.beta[warp][sb][j0 + j]);
-            lacc[j0 + j] = fmaf(e[j], isv * be.x, lacc[j0 + j]);
-            lacc[j0 + j + 1] = fmaf(e[j + 1], isv * be.y, lacc[j0 + j + 1]);
-            lacc[j0 + j + 2] = fmaf(e[j + 2], isv * be.z, lacc[j0 + j + 2]);
-            lacc[j0 + j + 3] = fmaf(e[j + 3], isv * be.w, lacc[j0 + j + 3]);
-          }
-          if (!wide) {
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              // the remainder is formed in fp16 (11 significant bits where 8 are kept)
-              const __half2 h0 = __floats2half2_rn(e[4 * j], e[4 * j + 1]);
-              const __half2 h1 = __floats2half2_rn(e[4 * j + 2], e[4 * j + 3]);
-              const uint32_t p0 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&h0), __NV_SATFINITE, __NV_E4M3);
-              const uint32_t p1 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&h1), __NV_SATFINITE, __NV_E4M3);
-              const __half2_raw r0 = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)p0, __NV_E4M3);
-              const __half2_raw r1 = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)p1, __NV_E4M3);
-              const __half2 d0 = __hsub2(h0, *reinterpret_cast<const __half2*>(&r0));
-              const __half2 d1 = __hsub2(h1, *reinterpret_cast<const __half2*>(&r1));
-              const uint32_t l0 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&d0), __NV_SATFINITE, __NV_E4M3);
-              const uint32_t l1 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&d1), __NV_SATFINITE, __NV_E4M3);
-              hi[j] = p0 | (p1 << 16);
-              lo[j] = l0 | (l1 << 16);
+#pragma unroll 1
+          for (int i = 0; i < SL; ++i) {
+            uint32_t v = 0xffffffffu;
+            if (node >= 0) {
+              const uint4* aw = reinterpret_cast<const uint4*>(&X.anc[(node >> 5) & 3][i * CH]);
+              const int sh = node & 31;
+              v = 0u;
+#pragma unroll 1
+              for (int e = 0; e < CH; e += 4) {
+                const uint4 a = aw[e >> 2];
+                v |= (((a.x >> sh) & 1u) | ((a.y >> sh) & 1u) << 1 | ((a.z >> sh) & 1u) << 2 | ((a.w >> sh) & 1u) << 3) << e;
+              }
             }
-            const uint32_t at = pt_piece<RW>(kl, j0 >> 4);
-            *reinterpret_cast<uint4*>(pbuf + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(pbuf + PT_KEYS * RW + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          } else {
-            uint32_t pk[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const __nv_bfloat162 v = __floats2bfloat162_rn(e[2 * j], e[2 * j + 1]);
-              pk[j] = *reinterpret_cast<const uint32_t*>(&v);
-            }
-            *reinterpret_cast<uint4*>(pbuf + pt_piece<2 * RW>(kl, j0 >> 3)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-            *reinterpret_cast<uint4*>(pbuf + pt_piece<2 * RW>(kl, (j0 >> 3) + 1)) = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+            X.vis[i][tid] = dead ? 0u : v;
           }
+        }
+        const float k1 = wide ? c16 : X.c8 * I.sk[pg], l1 = wide ? 0.f : I.lsv[pg], f1 = wide ? 1.f : I.sv[pg];
+        if (ok) ok = mbar_wait(&X.s_full[tp][cnt & 1], (cnt >> 1) & 1, abort_flag, status);
+        __syncwarp();
+        tc_fence_after();
+        const uint32_t sa = tmem + lane_base + (tp * 2 + (cnt & 1)) * NR;
+
+        // References, raised to the rounded-up maximum of the tile where that is higher; sums follow.
+        auto references = [&]() {
+#pragma unroll 1
+          for (int i = 0; i < SL; ++i) {
+            uint32_t r[CH];
+            float m[CH];
+            pt_ld<CH>(sa + i * CH, r);
+            tmem_ld_wait();
+            const uint32_t v1 = masked ? X.vis[i][tid] : 0xffffffffu;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) m[j] = (v1 >> j) & 1u ? fmaf(__uint_as_float(r[j]), k1, l1) : -INFINITY;
+            float top = pt_rows_reduce<CH, false>(m, lane);
+            if (CH == 16) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            if (lane < CH) X.wmax[tp][wq][i * CH + lane] = top;
+          }
+          group_bar();
+          bool moved = false;
+          unseen = false;
+#pragma unroll
+          for (int i = 0; i < SL; ++i) {
+            const float* wm = &X.wmax[tp][0][i * CH + (lane & (CH - 1))];
+            const float top = ceilf(fmaxf(fmaxf(wm[0], wm[NR]), fmaxf(wm[2 * NR], wm[3 * NR])));
+            const float now = fmaxf(ref[i], top);
+            if (lane < CH) {
+              // (a row that sees nothing here has a reference of 0 meanwhile: its weights are all 0)
+              X.nref[warp][i * CH + lane] = PT_SHIFT - (now == -INFINITY ? 0.f : now);
+              X.alpha[warp][i * CH + lane] = scale_pow2(ref[i], now);
+            }
+            moved |= ref[i] != now;
+            unseen |= now == -INFINITY;
+            ref[i] = now;
+          }
+          moved = __any_sync(0xffffffffu, moved);
+          unseen = __any_sync(0xffffffffu, unseen);
+          __syncwarp();
+          if (moved && cnt > cnt0) {
+#pragma unroll
+            for (int j = 0; j < NR / 2; ++j) {
+              const float2 al = *reinterpret_cast<const float2*>(&X.alpha[warp][2 * j]);
+              lacc[j].x *= al.x;
+              lacc[j].y *= al.y;
+            }
+            // (the group's last product is complete: its weights' buffer has been waited for)
+#pragma unroll 1
+            for (int j0 = 0; j0 < NR; j0 += 16) {
+              uint32_t r[16];
+              tmem_ld16(oa + j0, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * X.alpha[warp][j0 + j]);
+              pt_st16(oa + j0, r);
+            }
+            tmem_st_wait();
+          }
+          group_bar();                                  // wmax may be written again
+        };
+        if (cnt > 0) {                                  // the weights of the group's last tile have been read
+          if (ok) ok = mbar_wait(&X.p_empty[tp], (cnt - 1) & 1, abort_flag, status);
+          __syncwarp();
+          tc_fence_after();
+        }
+        // ---- weights; a second time, with higher references, if one passed the range.  The row sums are fp32 and
+        // right the first time unless a weight was infinite; such a sum (`lost`) starts again, what it held
+        // is below 2^-80 of what comes in.
+        unsigned long long lost = 0ull;
+        bool anew = unseen;
+        for (int attempt = 0; attempt < 2; ++attempt) {
+          if (anew) references();
+          __half2 most = __float2half2_rn(0.f);
+          uint32_t r[2][16];                            // this block's logits, the next one's on their way
+          tmem_ld16(sa, r[0]);
+          const uint64_t kk = pt_pack2(k1, k1), ff = pt_pack2(f1, f1);
+          float2 e[8], w[8];
+          // 16 rows at a time: the exponentials of a block (e) are issued among the conversions of the one before (w)
+#pragma unroll
+          for (int j0 = 0; j0 <= NR; j0 += 16) {
+            if (j0 < NR) {
+              const uint32_t (&x)[16] = r[(j0 >> 4) & 1];
+              tmem_ld_wait();
+              if (j0 + 16 < NR) tmem_ld16(sa + j0 + 16, r[((j0 >> 4) + 1) & 1]);
+#pragma unroll
+              for (int j = 0; j < 8; j += 2) {
+                const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(&X.nref[warp][j0 + 2 * j]);
+                e[j] = pt_unpack2(pt_fma2(pt_pack2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), kk, rf.x));
+                e[j + 1] = pt_unpack2(pt_fma2(pt_pack2(__uint_as_float(x[2 * j + 2]), __uint_as_float(x[2 * j + 3])), kk, rf.y));
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) e[j] = make_float2(fast_exp2(e[j].x), fast_exp2(e[j].y));
+            }
+            if (j0 > 0) {
+              const int jw = j0 - 16;                   // rows of w
+              uint32_t pk[8];
+              if (!wide) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const __half2 v = __float22half2_rn(pt_unpack2(pt_mul2(pt_pack2(w[j].x, w[j].y), ff)));
+                  most = __hmax2(most, v);
+                  pk[j] = *reinterpret_cast<const uint32_t*>(&v);
+                }
+              } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const __nv_bfloat162 v = __float22bfloat162_rn(w[j]);
+                  most = __hmax2(most, __float22half2_rn(w[j]));
+                  pk[j] = *reinterpret_cast<const uint32_t*>(&v);
+                }
+              }
+              *reinterpret_cast<uint4*>(pbuf + pt_piece<F::PROW>(kl, jw >> 3)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+              *reinterpret_cast<uint4*>(pbuf + pt_piece<F::PROW>(kl, (jw >> 3) + 1)) = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+            }
+            if (j0 < NR) {
+              if (masked) {
+                const uint32_t v1 = X.vis[j0 >> 5][tid] >> (j0 & 16);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  if (!((v1 >> (2 * j)) & 1u)) e[j].x = 0.f;
+                  if (!((v1 >> (2 * j + 1)) & 1u)) e[j].y = 0.f;
+                }
+              }
+              if (attempt == 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  lacc[(j0 / 2 + j) % (NR / 2)] = pt_unpack2(pt_add2(pt_pack2(lacc[(j0 / 2 + j) % (NR / 2)].x, lacc[(j0 / 2 + j) % (NR / 2)].y), pt_pack2(e[j].x, e[j].y)));
+              } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  if ((lost >> (j0 + 2 * j)) & 1ull) lacc[(j0 / 2 + j) % (NR / 2)].x += e[j].x;
+                  if ((lost >> (j0 + 2 * j + 1)) & 1ull) lacc[(j0 / 2 + j) % (NR / 2)].y += e[j].y;
+                }
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) w[j] = e[j];
+            }
+          }
+          if (attempt == 1) break;
+          const bool over = __hgt(__hmax(__low2half(most), __high2half(most)), __float2half(65504.f));
+          if (!group_or(over)) break;
+#pragma unroll
+          for (int j = 0; j < NR / 2; ++j) {
+            if (lacc[j].x == INFINITY) { lacc[j].x = 0.f; lost |= 1ull << (2 * j); }
+            if (lacc[j].y == INFINITY) { lacc[j].y = 0.f; lost |= 2ull << (2 * j); }
+          }
+          anew = true;
         }
         fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&X.p_full[tp]);
-        if (pending) take_o(cnt - 1, moved_before);
-        pending = true;
-        moved_before = moved;
         ++cnt;
       }
-      if (pending) {
-        if (ok) ok = mbar_wait(&X.o_full[tp], (cnt - 1) & 1, abort_flag, status);
-        take_o(cnt - 1, moved_before);
+      if (cnt > cnt0) {
+        if (ok) ok = mbar_wait(&X.p_empty[tp], (cnt - 1) & 1, abort_flag, status);
+        __syncwarp();
+        tc_fence_after();
       }
-      tc_fence_before();
 
       // ------------------------------------------------ the segment's result
-      {
-        const float l = pt_rows_reduce<RW, true>(lacc, lane);
-        if (lane < RW) {
-          X.lsum[warp][lane] = l;
-          if (wq == 0) X.m_run[grp][lane] = run;
+#pragma unroll
+      for (int i = 0; i < SL; ++i) {
+        float l[CH];
+#pragma unroll
+        for (int j = 0; j < CH / 2; ++j) { l[2 * j] = lacc[i * CH / 2 + j].x; l[2 * j + 1] = lacc[i * CH / 2 + j].y; }
+        float sum = pt_rows_reduce<CH, true>(l, lane);
+        if (CH == 16) sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+        if (lane < CH) {
+          X.lsum[warp][i * CH + lane] = sum;
+          if (wq == 0) X.m_run[tp][i * CH + lane] = ref[i];
         }
       }
-      float* po = part_o + (size_t)slot * NR * D;
-      float* pml = part_ml + (size_t)slot * NR * 2;
-      float* mb = reinterpret_cast<float*>(smem + F::OFF_P);     // [NP - 1][NR][128] over the weights
-      pt_bar<5, PT_SOFTMAX>();                          // every product has been read: the weights are free
-      if (NP > 1 && tp > 0) {
+      const int seg_b = X.seg_b;
+      const bool whole = X.seg_whole != 0;
+      float* po = part_o + (size_t)X.seg_slot * NR * D;
+      float* pml = part_ml + (size_t)X.seg_slot * NR * 2;
+      float* mb = reinterpret_cast<float*>(smem + F::OFF_P);     // [NR][128] over the weights
+      pt_bar<3, PT_SOFTMAX>();                          // every product has been read: the weights are free
+      if (tp == 1 && cnt > cnt0) {
+#pragma unroll 1
+        for (int j0 = 0; j0 < NR; j0 += 16) {
+          uint32_t v[16];
+          tmem_ld16(oa + j0, v);
+          tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < RW; ++j) mb[((tp - 1) * NR + grow + j) * 128 + kl] = acc[j];
-      }
-      if (tp == 0 && kl < RW) {
-        // row kl of this group: what each turn's sum weighs
-        float m = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) m = fmaxf(m, X.m_run[i * NRG + rg][kl]);
-        float wt[NP], l = 0.f;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const int g = i * NRG + rg;
-          const float mi = X.m_run[g][kl];
-          wt[i] = mi == -INFINITY ? 0.f : fast_exp2(mi - m);
-          l = fmaf(wt[i], (X.lsum[g * 4][kl] + X.lsum[g * 4 + 1][kl]) + (X.lsum[g * 4 + 2][kl] + X.lsum[g * 4 + 3][kl]), l);
+          for (int j = 0; j < 16; ++j) mb[(j0 + j) * 128 + kl] = __uint_as_float(v[j]);
         }
+      }
+      if (tid < NR) {
+        // row tid: what each group's sum weighs
+        const float m0 = X.m_run[0][tid], m1 = X.m_run[1][tid], m = fmaxf(m0, m1);
+        const float a0 = scale_pow2(m0, m), a1 = scale_pow2(m1, m);
+        const float l = a0 * ((X.lsum[0][tid] + X.lsum[1][tid]) + (X.lsum[2][tid] + X.lsum[3][tid])) +
+                        a1 * ((X.lsum[4][tid] + X.lsum[5][tid]) + (X.lsum[6][tid] + X.lsum[7][tid]));
         const float inv = whole ? 1.f / l : 1.f;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) X.beta[grp * 4 + i][0][kl] = wt[i] * inv;
+        X.wt[0][tid] = a0 * inv;
+        X.wt[1][tid] = a1 * inv;
         if (!whole) {
-          pml[(grow + kl) * 2] = m;
-          pml[(grow + kl) * 2 + 1] = l;
+          pml[tid * 2] = m;
+          pml[tid * 2 + 1] = l;
         }
       }
-      pt_bar<5, PT_SOFTMAX>();
-      if (tp == 0 && kl < D) {
+      tc_fence_before();
+      pt_bar<3, PT_SOFTMAX>();
+      if (tp == 0) {                                    // (the first tile was this group's: there is a sum)
+#pragma unroll 1
+        for (int j0 = 0; j0 < NR; j0 += 16) {
+          uint32_t x[16];
+          tmem_ld16(oa + j0, x);
+          tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < RW; ++j) {
-          float v = acc[j] * X.beta[grp * 4][0][j];
-#pragma unroll
-          for (int i = 1; i < NP; ++i) v = fmaf(mb[((i - 1) * NR + grow + j) * 128 + kl], X.beta[grp * 4 + i][0][j], v);
-          if (whole) {
-            const int off = X.rowoff[grow + j];
-            if (off >= 0) out[((size_t)b * M * Hq + off) * D + kl] = __float2bfloat16_rn(v);
-          } else {
-            po[(size_t)(grow + j) * D + kl] = v;
+          for (int j = 0; j < 16; ++j) {
+            const int row = j0 + j;
+            float v = __uint_as_float(x[j]) * X.wt[0][row];
+            const float w1 = X.wt[1][row];
+            if (w1 != 0.f) v = fmaf(mb[row * 128 + kl], w1, v);
+            if (kl < D) {
+              if (whole) {
+                const int off = X.rowoff[row];
+                if (off >= 0) out[((size_t)seg_b * M * Hq + off) * D + kl] = __float2bfloat16_rn(v);
+              } else {
+                po[(size_t)row * D + kl] = v;
+              }
+            }
           }
         }
+        tc_fence_before();
       }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 17) {
+  if (warp == 13) {
     tc_fence_after();
     tmem_dealloc(tmem, F::COLS);
   }
@@ -862,7 +977,7 @@ __global__ void __launch_bounds__(256) k_paged_merge(const jk_paged c, int B, in
   jk_pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int units = Hkv * n_qblk, G = Hq / Hkv;
-  if (warp == 0) pt_count(c, B, M, pt_cfg<D, NR>::WK, units, lane, cum, n8, nullptr, nullptr);
+  if (warp == 0) pt_count(c, B, M, units, lane, cum, n8, nullptr, nullptr);
   __syncthreads();
   const int64_t row = (int64_t)blockIdx.x * 8 + warp;
   const int64_t unit = row / NR;
@@ -927,10 +1042,10 @@ int jk_tma_encode_bf16(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank,
 int jk_tma_encode_u8(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, const uint64_t* dims,
                      const uint64_t* strides_bytes, const uint32_t* box);
 
-// Query rows of a block: the smallest of 16, 32, 64, 128 that holds the rows of a kv head, 128 past that.
+// Query rows of a block: the smallest of 16, 32, 64 that holds the rows of a kv head, 64 past that.
 static int pt_rows(const jk_config& g, int M) {
   const int rows = g.n_q_heads / g.n_kv_heads * M;
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
 // Workspace of the partials: two slots per CTA.
@@ -947,7 +1062,7 @@ static int pt_launch(jk_ctx* ctx, cudaStream_t st, const CUtensorMap* maps, cons
   const int rows = g.n_q_heads / g.n_kv_heads * M;
   const int n_qblk = (rows + NR - 1) / NR, units = g.n_kv_heads * n_qblk;
   const int64_t most = (int64_t)B * units * (((int64_t)c->max_pages * c->page_size + PT_KEYS - 1) / PT_KEYS +
-                                             (c->page_size + M + F::WK - 1) / F::WK);
+                                             (c->page_size + M + PT_WKEYS - 1) / PT_WKEYS);
   int ctas = ctx->sm_count < PT_MAX_CTAS ? ctx->sm_count : PT_MAX_CTAS;
   if (most < ctas) ctas = (int)most;
   const size_t smem = F::OFF_X + sizeof(pt_tail<D, NR>) + 1024;
@@ -1004,8 +1119,8 @@ int jk_paged_attn_tc(jk_ctx* ctx, cudaStream_t st, const jk_paged* c, int layer,
 #define PT_CASE(DD, NN) \
   if (g.head_dim == DD && nr == NN) return pt_launch<DD, NN>(ctx, st, maps, c, layer, B, M, q, parent, scale, out)
   const int nr = pt_rows(g, M);
-  PT_CASE(128, 16); PT_CASE(128, 32); PT_CASE(128, 64); PT_CASE(128, 128);
-  PT_CASE(64, 16); PT_CASE(64, 32); PT_CASE(64, 64); PT_CASE(64, 128);
+  PT_CASE(128, 16); PT_CASE(128, 32); PT_CASE(128, 64);
+  PT_CASE(64, 16); PT_CASE(64, 32); PT_CASE(64, 64);
 #undef PT_CASE
   return JK_ERR_SHAPE;
 }
