@@ -27,7 +27,7 @@
 // tile), so a unit (sequence, kv head, row block) spans CTAs where it has to; such a CTA leaves an
 // unnormalised partial, which k_paged_merge adds up, and a unit inside one CTA is written directly.
 // Warps: two softmax groups of four that take tiles in turn, four that widen V, TMA producers for K and for V,
-// an MMA issuer.  Registers are moved to the softmax warps: 20 warps of 96 spilled, and with the shared
+// an issuer of either product.  Registers are moved to the softmax warps: 20 warps of 96 spilled, and with the shared
 // memory this kernel takes a spill is a trip to L2.
 #include <math.h>
 
@@ -40,7 +40,6 @@
 #define PT_THREADS 512
 #define PT_MAX_CTAS 160
 #define PT_INFO 16                   // ring of tile descriptions: more than K slots + tiles that S runs ahead + 1
-#define PT_AHEAD 4                   // tiles whose S may run ahead of their weights: two buffers per group
 #define PT_SHIFT 6.f                 // a weight at its reference is 2^6
 
 // ------------------------------------------------------------------------------------------ PTX
@@ -74,6 +73,20 @@ __device__ __forceinline__ void pt_commit(uint64_t* bar, uint32_t lead) {
       "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
       ::"r"(smem_u32(bar)), "r"(lead)
       : "memory");
+}
+// Bounded wait, kept short (the 32-bit cycle counter, about a second): the loops of this kernel are long, and what
+// does not fit the instruction caches is fetched again for every tile.
+__device__ __forceinline__ bool pt_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  uint32_t t0, t;
+  asm volatile("mov.u32 %0, %%clock;" : "=r"(t0));
+  do {
+    if (mbar_try_wait(bar, parity)) return true;
+    asm volatile("mov.u32 %0, %%clock;" : "=r"(t));
+  } while (t - t0 < 2000000000u && !*abort_flag);
+  *abort_flag = 1;
+  jk_set_status(status, JK_ERR_TIMEOUT);
+  return false;
 }
 // Maxima (sums) over lanes of rows held one value per lane and row.  Half of the rows changes sides at every
 // step, so each step costs what is left of the rows: pt_fold sends rows j and j + N/2 to the two halves of
@@ -185,7 +198,7 @@ struct pt_info {                     // one tile, written by the producer; bf16 
 
 template <int D, int NR> struct alignas(16) pt_tail {
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
-  uint64_t info_full[PT_INFO], s_full[2][2], p_full[2], p_empty[2], w_full[8], w_empty[2], q_full;
+  uint64_t info_full[PT_INFO], s_full[2][2], s_empty[2][2], p_full[2], p_empty[2], w_full[8], w_empty[2], q_full;
   uint32_t tmem_base;
   int abort_flag;
   long long cum[JK_MAX_ROWS + 1];    // tiles before each sequence
@@ -268,6 +281,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     for (int i = 0; i < 8; ++i) mbar_init(&X.w_full[i], 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&X.s_full[i][0], 1); mbar_init(&X.s_full[i][1], 1);
+      mbar_init(&X.s_empty[i][0], 4); mbar_init(&X.s_empty[i][1], 4);
       mbar_init(&X.p_full[i], 4); mbar_init(&X.p_empty[i], 1);
       mbar_init(&X.w_empty[i], 1);
     }
@@ -299,9 +313,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     b = 0;
     while (X.cum[b + 1] <= t) ++b;
     nt = X.n8[b] + X.n16[b];
-    const long long off = t - X.cum[b];
-    u = (int)(off / nt);
-    t0 = (int)(off - (long long)u * nt);
+    const uint32_t off = (uint32_t)(t - X.cum[b]);      // tiles of one sequence: below 2^32
+    u = (int)(off / (uint32_t)nt);
+    t0 = (int)(off - (uint32_t)u * (uint32_t)nt);
     t1 = share - done < nt - t0 ? t0 + share - done : nt;
   };
 
@@ -350,7 +364,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       if (t0 < n8) take(ask(at));
       for (int tile = t0; tile < t1 && ok; ++tile, ++tc) {
         pt_info& I = X.info[tc % PT_INFO];
-        ok = __all_sync(0xffffffffu, mbar_wait(&empty[s_slot], s_par, abort_flag, status));
+        ok = __all_sync(0xffffffffu, pt_wait(&empty[s_slot], s_par, abort_flag, status));
         unsigned char* dst = ring + s_slot * F::SLOT;
         if (tile < n8) {
           // (a tile's pages never span two batches: both start at multiples of the tile's page count)
@@ -406,106 +420,104 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       while (global_ns() - ts < 2000000ull) { /* 2 ms: far longer than any TMA copy */ }
     }
   } else if (warp == 13) {
-    {
-      // ================================================================== MMA issuer
-      const uint32_t q8 = smem_u32(smem), q16 = smem_u32(smem + F::OFF_Q16), pb = smem_u32(smem + F::OFF_P);
-      const uint32_t ka0 = smem_u32(sk), va0 = smem_u32(sv), wa0 = smem_u32(smem + F::OFF_W);
-      const uint32_t id_s8 = pt_idesc(0, 0, NR, 0, 0), id_s16 = pt_idesc(1, 1, NR, 0, 0);
-      const uint32_t id_p = pt_idesc(0, 0, NR, 1, 1), id_p16 = pt_idesc(1, 1, NR, 1, 1);
-      int k_slot = 0, k_par = 0, v_slot = 0, v_tile = 0, w_buf = 0, segs = 0;
-      int cs0 = 0, cs1 = 0, cp0 = 0, cp1 = 0;           // tiles per group so far
-      const uint32_t lead = pt_elect();
-      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-      auto waits = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status)) != 0; };
-      auto ready = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(bar, parity)) != 0; };
-      auto issue_s = [&](int tp, bool wide) {
-        const int buf = (tp ? cs1 : cs0) & 1;
-        if (!waits(&X.k_full[k_slot], k_par)) { ok = false; return; }
+    // ==================================================================== S issuer
+    const uint32_t lead = pt_elect();
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint64_t k8 = pt_desc(smem_u32(sk), 16, 8 * D, pt_layout(D)), q8 = pt_desc(smem_u32(smem), 16, 8 * D, pt_layout(D));
+    const uint64_t k16 = pt_desc(smem_u32(sk), 16, 1024, 2), q16 = pt_desc(smem_u32(smem + F::OFF_Q16), 16, 1024, 2);
+    const uint32_t id_8 = pt_idesc(0, 0, NR, 0, 0), id_16 = pt_idesc(1, 1, NR, 0, 0);
+    int k_slot = 0, k_par = 0, segs = 0, n = 0;         // n: tiles so far, n0: at the unit's start
+    for (int done = 0; done < share && ok;) {
+      int b, u, t0, t1, nt;
+      segment(done, b, u, t0, t1, nt);
+      done += t1 - t0;
+      ok = pt_wait(&X.q_full, segs & 1, abort_flag, status);
+      ++segs;
+      const int n8 = X.n8[b];
+      for (int tile = t0; tile < t1 && ok; ++tile) {
+        const int tp = (tile - t0) & 1;
+        const int cg = tp ? n >> 16 : n & 0xffff;       // tiles of the group so far (mod 2^16)
+        const int buf = cg & 1;
+        // the columns are free when the weights of the group's tile before last have been written
+        ok = pt_wait(&X.s_empty[tp][buf], ((cg >> 1) & 1) ^ 1, abort_flag, status) &&
+             pt_wait(&X.k_full[k_slot], k_par, abort_flag, status);
+        ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
-        const uint32_t d = tm + (tp * 2 + buf) * NR, kt = ka0 + k_slot * F::SLOT;
-        if (!wide) {
+        const uint32_t d = tm + (tp * 2 + buf) * NR;
+        const uint32_t at = k_slot * (F::SLOT >> 4);
+        if (ok && tile < n8) {
 #pragma unroll
           for (int part = 0; part < 2; ++part)
 #pragma unroll
             for (int k = 0; k < D / 32; ++k)
-              pt_mma_f8(d, pt_desc(kt + k * 32, 16, 8 * D, pt_layout(D)),
-                        pt_desc(q8 + part * F::Q8 + k * 32, 16, 8 * D, pt_layout(D)), id_s8, (part | k) ? 1u : 0u, lead);
-        } else {
+              pt_mma_f8(d, k8 + at + k * 2, q8 + part * (F::Q8 >> 4) + k * 2, id_8, (part | k) ? 1u : 0u, lead);
+        } else if (ok) {
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              pt_mma_16(d, pt_desc(kt + kb * (PT_WKEYS * 128) + k * 32, 16, 1024, 2),
-                          pt_desc(q16 + kb * (NR * 128) + k * 32, 16, 1024, 2), id_s16, (kb | k) ? 1u : 0u, lead);
+              pt_mma_16(d, k16 + at + kb * (PT_WKEYS * 8) + k * 2, q16 + kb * (NR * 8) + k * 2, id_16, (kb | k) ? 1u : 0u, lead);
         }
         pt_commit(&X.k_empty[k_slot], lead);
-        if (++k_slot == KST) { k_slot = 0; k_par ^= 1; }
         pt_commit(&X.s_full[tp][buf], lead);
-        if (tp) ++cs1; else ++cs0;
-      };
-      auto issue_pv = [&](int tp, bool wide, bool add) {
-        if (!waits(&X.p_full[tp], (tp ? cp1 : cp0) & 1) || !waits(&X.w_full[v_tile & 7], (v_tile >> 3) & 1)) { ok = false; return; }
+        if (++k_slot == KST) { k_slot = 0; k_par ^= 1; }
+        n = tp ? n + 0x10000 : (n & ~0xffff) | ((n + 1) & 0xffff);
+      }
+    }
+    if (!ok) {                                          // products still in flight get a bounded time to end
+      const unsigned long long ts = global_ns();
+      while (global_ns() - ts < 2000000ull) { }
+    }
+  } else {
+    // ==================================================================== O issuer (warp 15)
+    const uint32_t lead = pt_elect();
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint64_t p0 = pt_desc(smem_u32(smem + F::OFF_P), 8 * F::PROW, 8 * F::PROW, pt_layout(F::PROW));
+    const uint64_t v16 = pt_desc(smem_u32(smem + F::OFF_W), KB == 2 ? PT_KEYS * 128 : 1024, 1024, 2);
+    const uint64_t vw = pt_desc(smem_u32(sv), KB == 2 ? PT_WKEYS * 128 : 1024, 1024, 2);
+    const uint32_t id_h = pt_idesc(0, 0, NR, 1, 1), id_b = pt_idesc(1, 1, NR, 1, 1);
+    int v_slot = 0, v_tile = 0, w_buf = 0, n = 0;
+    for (int done = 0; done < share && ok;) {
+      int b, u, t0, t1, nt;
+      segment(done, b, u, t0, t1, nt);
+      done += t1 - t0;
+      const int n8 = X.n8[b];
+      for (int tile = t0; tile < t1 && ok; ++tile) {
+        const int tp = (tile - t0) & 1;
+        const int cg = tp ? n >> 16 : n & 0xffff;
+        ok = pt_wait(&X.w_full[v_tile & 7], (v_tile >> 3) & 1, abort_flag, status) &&
+             pt_wait(&X.p_full[tp], cg & 1, abort_flag, status);
+        ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
-        const uint32_t d = tm + F::O_COL + tp * NR, p = pb + tp * F::PB;
-        if (!wide) {
-          const uint32_t vt = wa0 + w_buf * F::VB;
+        const uint32_t d = tm + F::O_COL + tp * NR;
+        const uint64_t p = p0 + tp * (F::PB >> 4);
+        const bool add = tile - t0 >= 2;
+        if (ok && tile < n8) {
+          const uint64_t v = v16 + w_buf * (F::VB >> 4);
 #pragma unroll
           for (int k = 0; k < PT_KEYS / 16; ++k)
-            pt_mma_16(d, pt_desc(vt + k * 2048, KB == 2 ? PT_KEYS * 128 : 1024, 1024, 2),
-                        pt_desc(p + k * 16 * F::PROW, 8 * F::PROW, 8 * F::PROW, pt_layout(F::PROW)), id_p, (add || k) ? 1u : 0u, lead);
+            pt_mma_16(d, v + k * 128, p + k * F::PROW, id_h, (add || k) ? 1u : 0u, lead);
+        } else if (ok) {
+          const uint64_t v = vw + v_slot * (F::SLOT >> 4);
+#pragma unroll
+          for (int k = 0; k < PT_WKEYS / 16; ++k)
+            pt_mma_16(d, v + k * 128, p + k * F::PROW, id_b, (add || k) ? 1u : 0u, lead);
+        }
+        pt_commit(&X.p_empty[tp], lead);
+        if (tile < n8) {
           pt_commit(&X.w_empty[w_buf], lead);
           w_buf ^= 1;
         } else {
-          const uint32_t vt = va0 + v_slot * F::SLOT;
-#pragma unroll
-          for (int k = 0; k < PT_WKEYS / 16; ++k)
-            pt_mma_16(d, pt_desc(vt + k * 2048, KB == 2 ? PT_WKEYS * 128 : 1024, 1024, 2),
-                        pt_desc(p + k * 16 * F::PROW, 8 * F::PROW, 8 * F::PROW, pt_layout(F::PROW)), id_p16, (add || k) ? 1u : 0u, lead);
           pt_commit(&X.v_empty[v_slot], lead);
         }
         if (++v_slot == VST) v_slot = 0;
         ++v_tile;
-        pt_commit(&X.p_empty[tp], lead);
-        if (tp) ++cp1; else ++cp0;
-      };
-      for (int done = 0; done < share && ok;) {
-        int b, u, t0, t1, nt;
-        segment(done, b, u, t0, t1, nt);
-        done += t1 - t0;
-        ok = waits(&X.q_full, segs & 1);
-        ++segs;
-        tc_fence_after();
-        const int n8 = __shfl_sync(0xffffffffu, X.n8[b], 0);
-        t0 = __shfl_sync(0xffffffffu, t0, 0);
-        t1 = __shfl_sync(0xffffffffu, t1, 0);
-        int ts = t0, tv = t0;                           // next tile of either product
-        // Whichever has its inputs goes first: the oldest tile's second product, or the next tile's S, whose
-        // columns are free once the weights of the tile PT_AHEAD before it have been written.
-        long long c0 = clock64();
-        while (ok && tv < t1) {
-          const bool can_s = ts < t1 && ts - tv < PT_AHEAD, can_v = tv < ts;
-          const int sp = (ts - t0) & 1, vp = (tv - t0) & 1;
-          if (can_v && (!can_s || ready(&X.p_full[vp], (vp ? cp1 : cp0) & 1))) {
-            issue_pv(vp, tv >= n8, tv - t0 >= 2);
-            ++tv;
-            c0 = clock64();
-          } else if (can_s && (!can_v || ready(&X.k_full[k_slot], k_par))) {
-            issue_s(sp, ts >= n8);
-            ++ts;
-            c0 = clock64();
-          } else if (__any_sync(0xffffffffu, *abort_flag)) {
-            ok = false;
-          } else if (__any_sync(0xffffffffu, clock64() - c0 > TC_WAIT_CYCLES)) {
-            *abort_flag = 1;
-            jk_set_status(status, JK_ERR_TIMEOUT);
-            ok = false;
-          }
-        }
+        n = tp ? n + 0x10000 : (n & ~0xffff) | ((n + 1) & 0xffff);
       }
-      if (!ok) {                                        // products still in flight get a bounded time to end
-        const unsigned long long ts = global_ns();
-        while (global_ns() - ts < 2000000ull) { }
-      }
+    }
+    if (!ok) {
+      const unsigned long long ts = global_ns();
+      while (global_ns() - ts < 2000000ull) { }
     }
   }
   } else if (warp >= 8) {
@@ -524,20 +536,26 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       const int n8 = X.n8[b];
       for (int tile = t0; tile < t1; ++tile, ++tc) {
         const pt_info& I = X.info[tc % PT_INFO];
-        if (ok) ok = mbar_wait(&X.info_full[tc % PT_INFO], (tc / PT_INFO) & 1, abort_flag, status);
-        if (ok) ok = mbar_wait(&X.v_full[v_slot], v_par, abort_flag, status);
+        if (ok) ok = pt_wait(&X.info_full[tc % PT_INFO], (tc / PT_INFO) & 1, abort_flag, status);
+        if (ok) ok = pt_wait(&X.v_full[v_slot], v_par, abort_flag, status);
         unsigned char* src = sv + v_slot * F::SLOT;
         if (tile < n8) {
           const int buf = w_n & 1, live = I.live;
-          if (ok && w_n >= 2) ok = mbar_wait(&X.w_empty[buf], ((w_n >> 1) & 1) ^ 1, abort_flag, status);
+          if (ok && w_n >= 2) ok = pt_wait(&X.w_empty[buf], ((w_n >> 1) & 1) ^ 1, abort_flag, status);
           unsigned char* dst = smem + F::OFF_W + buf * F::VB;
-          // a warp's step: 8 rows, four pieces (64 dims); D / 64 such halves of 16 groups of rows
-#pragma unroll 4
-          for (int i = cw; i < 16 * KB; i += 4) {
-            const int kb = i % KB, r = (i / KB) * 8 + rr, pc = lane & 3;
-            uint4 v = *reinterpret_cast<const uint4*>(src + pt_piece<D>(r, kb * 4 + pc));
-            if (r >= live) v = make_uint4(0u, 0u, 0u, 0u);   // rows behind the last page may hold anything
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          // a warp's step: 8 rows, four pieces (64 dims); D / 64 such halves of 16 groups of rows.  All of a
+          // thread's loads are asked for before the first conversion.
+          uint4 v[4 * KB];
+#pragma unroll
+          for (int i = 0; i < 4 * KB; ++i) {
+            const int st = i * 4 + cw, r = (st / KB) * 8 + rr;
+            v[i] = *reinterpret_cast<const uint4*>(src + pt_piece<D>(r, (st % KB) * 4 + (lane & 3)));
+          }
+#pragma unroll
+          for (int i = 0; i < 4 * KB; ++i) {
+            const int st = i * 4 + cw, r = (st / KB) * 8 + rr, pc = lane & 3;
+            if (r >= live) v[i] = make_uint4(0u, 0u, 0u, 0u);   // rows behind the last page may hold anything
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
             uint32_t o[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -546,7 +564,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
               o[2 * j] = *reinterpret_cast<const uint32_t*>(&a);
               o[2 * j + 1] = *reinterpret_cast<const uint32_t*>(&e);
             }
-            unsigned char* d = dst + kb * (PT_KEYS * 128);
+            unsigned char* d = dst + (st % KB) * (PT_KEYS * 128);
             *reinterpret_cast<uint4*>(d + pt_piece<128>(r, pc * 2)) = make_uint4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<uint4*>(d + pt_piece<128>(r, pc * 2 + 1)) = make_uint4(o[4], o[5], o[6], o[7]);
           }
@@ -693,7 +711,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         if (((tile - t0) & 1) != tp) continue;
         const bool wide = tile >= n8;
         const pt_info& I = X.info[tc % PT_INFO];
-        if (ok) ok = mbar_wait(&X.info_full[tc % PT_INFO], (tc / PT_INFO) & 1, abort_flag, status);
+        if (ok) ok = pt_wait(&X.info_full[tc % PT_INFO], (tc / PT_INFO) & 1, abort_flag, status);
         // A tile with keys that not every row sees (dead ones behind the last, tree nodes) leaves the rows that
         // see this thread's key in vis.
         const bool masked = wide || I.live < PT_KEYS;
@@ -721,7 +739,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
           }
         }
         const float k1 = wide ? c16 : X.c8 * I.sk[pg], l1 = wide ? 0.f : I.lsv[pg], f1 = wide ? 1.f : I.sv[pg];
-        if (ok) ok = mbar_wait(&X.s_full[tp][cnt & 1], (cnt >> 1) & 1, abort_flag, status);
+        if (ok) ok = pt_wait(&X.s_full[tp][cnt & 1], (cnt >> 1) & 1, abort_flag, status);
         __syncwarp();
         tc_fence_after();
         const uint32_t sa = tmem + lane_base + (tp * 2 + (cnt & 1)) * NR;
@@ -783,7 +801,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
           group_bar();                                  // wmax may be written again
         };
         if (cnt > 0) {                                  // the weights of the group's last tile have been read
-          if (ok) ok = mbar_wait(&X.p_empty[tp], (cnt - 1) & 1, abort_flag, status);
+          if (ok) ok = pt_wait(&X.p_empty[tp], (cnt - 1) & 1, abort_flag, status);
           __syncwarp();
           tc_fence_after();
         }
@@ -873,11 +891,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&X.p_full[tp]);
+        if (lane == 0) {
+          mbar_arrive(&X.s_empty[tp][cnt & 1]);
+          mbar_arrive(&X.p_full[tp]);
+        }
         ++cnt;
       }
       if (cnt > cnt0) {
-        if (ok) ok = mbar_wait(&X.p_empty[tp], (cnt - 1) & 1, abort_flag, status);
+        if (ok) ok = pt_wait(&X.p_empty[tp], (cnt - 1) & 1, abort_flag, status);
         __syncwarp();
         tc_fence_after();
       }
