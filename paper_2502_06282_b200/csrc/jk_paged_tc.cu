@@ -744,6 +744,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         tc_fence_after();
         const uint32_t sa = tmem + lane_base + (tp * 2 + (cnt & 1)) * NR;
 
+        // the weights of the group's last tile have been read, and its product is complete
+        auto last_product = [&]() {
+          if (cnt > 0) {
+            if (ok) ok = pt_wait(&X.p_empty[tp], (cnt - 1) & 1, abort_flag, status);
+            __syncwarp();
+            tc_fence_after();
+          }
+        };
         // References, raised to the rounded-up maximum of the tile where that is higher; sums follow.
         auto references = [&]() {
 #pragma unroll 1
@@ -786,7 +794,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
               lacc[j].x *= al.x;
               lacc[j].y *= al.y;
             }
-            // (the group's last product is complete: its weights' buffer has been waited for)
+            last_product();
 #pragma unroll 1
             for (int j0 = 0; j0 < NR; j0 += 16) {
               uint32_t r[16];
@@ -800,11 +808,6 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
           }
           group_bar();                                  // wmax may be written again
         };
-        if (cnt > 0) {                                  // the weights of the group's last tile have been read
-          if (ok) ok = pt_wait(&X.p_empty[tp], (cnt - 1) & 1, abort_flag, status);
-          __syncwarp();
-          tc_fence_after();
-        }
         // ---- weights; a second time, with higher references, if one passed the range.  The row sums are fp32 and
         // right the first time unless a weight was infinite; such a sum (`lost`) starts again, what it held
         // is below 2^-80 of what comes in.
@@ -835,14 +838,17 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
             }
             if (j0 > 0) {
               const int jw = j0 - 16;                   // rows of w
+              if (jw == 0) last_product();
               uint32_t pk[8];
               if (!wide) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                   const __half2 v = __float22half2_rn(pt_unpack2(pt_mul2(pt_pack2(w[j].x, w[j].y), ff)));
-                  most = __hmax2(most, v);
                   pk[j] = *reinterpret_cast<const uint32_t*>(&v);
                 }
+                auto h = [&](int j) { return *reinterpret_cast<const __half2*>(&pk[j]); };
+                most = __hmax2(most, __hmax2(__hmax2(__hmax2(h(0), h(1)), __hmax2(h(2), h(3))),
+                                             __hmax2(__hmax2(h(4), h(5)), __hmax2(h(6), h(7)))));
               } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
