@@ -26,9 +26,9 @@
 // One CTA per SM; all tiles of the call are dealt out evenly in order (sequence, kv head, row block,
 // tile), so a unit (sequence, kv head, row block) spans CTAs where it has to; such a CTA leaves an
 // unnormalised partial, which k_paged_merge adds up, and a unit inside one CTA is written directly.
-// Warps: two softmax groups of four that take tiles in turn, four that widen V, TMA producers for K and for V,
-// an issuer of either product.  Registers are moved to the softmax warps: 20 warps of 96 spilled, and with the shared
-// memory this kernel takes a spill is a trip to L2.
+// Warps: four softmax groups of four (32 rows of every second tile, with up to 16 rows every fourth tile), four that
+// widen V, TMA producers for K and for V, an issuer of either product.  Registers are moved to the softmax
+// warps, each role setting its own: with the shared memory this kernel takes a spill is a trip to L2.
 #include <math.h>
 
 #include "jk_paged.cuh"
@@ -36,10 +36,10 @@
 
 #define PT_KEYS 128
 #define PT_WKEYS 64                  // keys of a bf16 tile
-#define PT_SOFTMAX 256               // threads of the softmax groups
-#define PT_THREADS 512
+#define PT_SOFTMAX 512               // threads of the softmax groups
+#define PT_THREADS 768
 #define PT_MAX_CTAS 160
-#define PT_INFO 16                   // ring of tile descriptions: more than K slots + tiles that S runs ahead + 1
+#define PT_INFO 16                   // tile descriptions: at least K slots + 3 tiles per turn (S is two ahead of the weights)
 #define PT_SHIFT 6.f                 // a weight at its reference is 2^6
 
 // ------------------------------------------------------------------------------------------ PTX
@@ -171,22 +171,29 @@ __device__ __forceinline__ uint32_t pt_idesc(uint32_t fmt_a, uint32_t fmt_b, int
 
 // ------------------------------------------------------------------------------------------ layout
 template <int D, int NR> struct pt_cfg {
+  static constexpr int RW = NR == 64 ? 32 : 16;        // rows of a softmax group
+  static constexpr int NRG = NR / RW;                  // groups that share a tile
+  static constexpr int NP = 4 / NRG;                   // tiles in the groups' hands: their turns
   static constexpr int SLOT = PT_KEYS * D;             // an 8-bit tile of 128 keys or a bf16 tile of 64
   static constexpr int KST = NR == 64 ? 3 : 4;
-  static constexpr int VST = NR == 64 ? 2 : NR == 32 ? 3 : 4;
+  static constexpr int VST = NR == 64 ? 2 : 3;
   static constexpr int Q8 = NR * D;                    // one of the two e4m3 parts of the queries
   static constexpr int PROW = 2 * NR;                  // bytes of a key's weights
-  static constexpr int PB = PT_KEYS * PROW;            // a group's weights of a tile
+  static constexpr int PB = PT_KEYS * PROW;            // the weights of a tile, a buffer per turn
+  static constexpr int MB = (NP - 1) * NR * 512;       // sums that the other turns hand to the first, in the same place
+  static constexpr int PBYTES = NP * PB > MB ? NP * PB : MB;
   static constexpr int VB = PT_KEYS * D * 2;           // a tile of V in fp16
   static constexpr int OFF_Q16 = 2 * Q8;
-  static constexpr int OFF_P = OFF_Q16 + NR * D * 2;   // (the second group hands its sums over in the same place)
-  static constexpr int OFF_W = OFF_P + 2 * PB;
+  static constexpr int OFF_P = OFF_Q16 + NR * D * 2;
+  static constexpr int OFF_W = OFF_P + PBYTES;
   static constexpr int OFF_K = OFF_W + 2 * VB;
   static constexpr int OFF_V = OFF_K + KST * SLOT;
   // (behind the rings: a bf16 K tile is read as 128 rows, a head size of 64 one row group further in V)
   static constexpr int OFF_X = OFF_V + VST * SLOT + 1024;
-  static constexpr uint32_t O_COL = 4 * NR;            // S: two buffers per group
-  static constexpr uint32_t COLS = 6 * NR <= 128 ? 128 : 6 * NR <= 256 ? 256 : 512;
+  static constexpr uint32_t O_COL = NP * 2 * NR;       // S: two buffers per turn
+  static constexpr uint32_t COLS = NR == 64 ? 512 : 256;
+  static_assert(3 * NP * NR <= COLS, "tensor memory");
+  static_assert(KST + 3 * NP <= PT_INFO, "tile descriptions");
 };
 
 struct pt_info {                     // one tile, written by the producer; bf16 tiles: rows of the tile
@@ -198,23 +205,23 @@ struct pt_info {                     // one tile, written by the producer; bf16 
 
 template <int D, int NR> struct alignas(16) pt_tail {
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
-  uint64_t info_full[PT_INFO], s_full[2][2], s_empty[2][2], p_full[2], p_empty[2], w_full[8], w_empty[2], q_full;
+  uint64_t info_full[PT_INFO], s_full[4][2], s_empty[4][2], p_full[4], p_empty[4], w_full[8], w_empty[2], q_full;
   uint32_t tmem_base;
   int abort_flag;
   long long cum[JK_MAX_ROWS + 1];    // tiles before each sequence
   int n8[JK_MAX_ROWS], n16[JK_MAX_ROWS];
   pt_info info[PT_INFO];
-  float q_max[8];
+  float q_max[16];
   // of the unit at work, for what comes after its tiles
   int seg_b, seg_slot, seg_whole;
   float c8;                          // logits per product of codes, in units of log2
-  uint32_t vis[2][PT_SOFTMAX];       // masked tiles: rows (of either half) that see the thread's key
+  uint32_t vis[PT_SOFTMAX];          // masked tiles: rows of the group that see the thread's key
   int rowoff[NR];                    // output row of each query row, -1 = none
   int parent[JK_MAX_TREE];
   alignas(16) uint32_t anc[4][NR];   // tree nodes each query row sees
-  // per warp and row (the four warps of a group form the same values)
-  alignas(16) float nref[8][NR], alpha[8][NR];
-  float wmax[2][4][NR], m_run[2][NR], lsum[8][NR], wt[2][NR];
+  // per warp and row (the four warps of a group form the same values); at the end of a unit alpha holds the sums
+  alignas(16) float nref[16][32], alpha[16][32];
+  float wmax[4][4][32], m_run[4][32], wt[4][NR];
 };
 
 // Tiles of every sequence, and their prefix sums, by one warp.
@@ -260,7 +267,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     int Hq, int Hkv, int n_qblk, __nv_bfloat16* __restrict__ out, float* __restrict__ part_o,
     float* __restrict__ part_ml, int32_t* status) {
   typedef pt_cfg<D, NR> F;
-  constexpr int KST = F::KST, VST = F::VST;
+  constexpr int KST = F::KST, VST = F::VST, RW = F::RW, NRG = F::NRG, NP = F::NP;
   constexpr int KB = D / 64;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -279,22 +286,22 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     }
     for (int i = 0; i < PT_INFO; ++i) mbar_init(&X.info_full[i], 1);
     for (int i = 0; i < 8; ++i) mbar_init(&X.w_full[i], 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&X.s_full[i][0], 1); mbar_init(&X.s_full[i][1], 1);
-      mbar_init(&X.s_empty[i][0], 4); mbar_init(&X.s_empty[i][1], 4);
-      mbar_init(&X.p_full[i], 4); mbar_init(&X.p_empty[i], 1);
-      mbar_init(&X.w_empty[i], 1);
+      mbar_init(&X.s_empty[i][0], 4 * NRG); mbar_init(&X.s_empty[i][1], 4 * NRG);
+      mbar_init(&X.p_full[i], 4 * NRG); mbar_init(&X.p_empty[i], 1);
     }
+    mbar_init(&X.w_empty[0], 1); mbar_init(&X.w_empty[1], 1);
     mbar_init(&X.q_full, PT_SOFTMAX / 32);
     X.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 13) {
+  if (warp == 21) {
     tmem_alloc(&X.tmem_base, F::COLS);
     tmem_relinquish();
   }
   jk_pdl_wait();
-  if (warp == 12) pt_count(c, B, M, units, lane, X.cum, X.n8, X.n16, blockIdx.x == 0 ? status : nullptr);
+  if (warp == 20) pt_count(c, B, M, units, lane, X.cum, X.n8, X.n16, blockIdx.x == 0 ? status : nullptr);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -319,12 +326,12 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     t1 = share - done < nt - t0 ? t0 + share - done : nt;
   };
 
-  // registers: 512 x 128 at launch = 256 x 72 + 256 x 184 (each warpgroup sets its own at the top of its roles)
-  if (warp >= 12) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-  if (warp == 12 || warp == 14) {
-    // ==================================================================== TMA producers: K (12), V (14)
-    const bool is_k = warp == 12;
+  // registers: 768 x 80 at launch = 512 x 96 + 256 x 48 (each warpgroup sets its own at the top of its roles)
+  if (warp >= 20) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+  if (warp == 20 || warp == 22) {
+    // ==================================================================== TMA producers: K (20), V (22)
+    const bool is_k = warp == 20;
     const int NST = is_k ? KST : VST;
     uint64_t* full = is_k ? X.k_full : X.v_full;
     uint64_t* empty = is_k ? X.k_empty : X.v_empty;
@@ -419,14 +426,15 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       const unsigned long long ts = global_ns();
       while (global_ns() - ts < 2000000ull) { /* 2 ms: far longer than any TMA copy */ }
     }
-  } else if (warp == 13) {
+  } else if (warp == 21) {
     // ==================================================================== S issuer
     const uint32_t lead = pt_elect();
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     const uint64_t k8 = pt_desc(smem_u32(sk), 16, 8 * D, pt_layout(D)), q8 = pt_desc(smem_u32(smem), 16, 8 * D, pt_layout(D));
     const uint64_t k16 = pt_desc(smem_u32(sk), 16, 1024, 2), q16 = pt_desc(smem_u32(smem + F::OFF_Q16), 16, 1024, 2);
     const uint32_t id_8 = pt_idesc(0, 0, NR, 0, 0), id_16 = pt_idesc(1, 1, NR, 0, 0);
-    int k_slot = 0, k_par = 0, segs = 0, n = 0;         // n: tiles so far, n0: at the unit's start
+    int k_slot = 0, k_par = 0, segs = 0;
+    uint32_t n = 0;                                     // tiles per turn so far, a byte each
     for (int done = 0; done < share && ok;) {
       int b, u, t0, t1, nt;
       segment(done, b, u, t0, t1, nt);
@@ -435,9 +443,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       ++segs;
       const int n8 = X.n8[b];
       for (int tile = t0; tile < t1 && ok; ++tile) {
-        const int tp = (tile - t0) & 1;
-        const int cg = tp ? n >> 16 : n & 0xffff;       // tiles of the group so far (mod 2^16)
-        const int buf = cg & 1;
+        const int tp = (tile - t0) & (NP - 1);
+        const int cg = (n >> (8 * tp)) & 0xff, buf = cg & 1;
         // the columns are free when the weights of the group's tile before last have been written
         ok = pt_wait(&X.s_empty[tp][buf], ((cg >> 1) & 1) ^ 1, abort_flag, status) &&
              pt_wait(&X.k_full[k_slot], k_par, abort_flag, status);
@@ -461,7 +468,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         pt_commit(&X.k_empty[k_slot], lead);
         pt_commit(&X.s_full[tp][buf], lead);
         if (++k_slot == KST) { k_slot = 0; k_par ^= 1; }
-        n = tp ? n + 0x10000 : (n & ~0xffff) | ((n + 1) & 0xffff);
+        n = (n & ~(0xffu << (8 * tp))) | (((cg + 1u) & 0xffu) << (8 * tp));
       }
     }
     if (!ok) {                                          // products still in flight get a bounded time to end
@@ -469,29 +476,30 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       while (global_ns() - ts < 2000000ull) { }
     }
   } else {
-    // ==================================================================== O issuer (warp 15)
+    // ==================================================================== O issuer (warp 23)
     const uint32_t lead = pt_elect();
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     const uint64_t p0 = pt_desc(smem_u32(smem + F::OFF_P), 8 * F::PROW, 8 * F::PROW, pt_layout(F::PROW));
     const uint64_t v16 = pt_desc(smem_u32(smem + F::OFF_W), KB == 2 ? PT_KEYS * 128 : 1024, 1024, 2);
     const uint64_t vw = pt_desc(smem_u32(sv), KB == 2 ? PT_WKEYS * 128 : 1024, 1024, 2);
     const uint32_t id_h = pt_idesc(0, 0, NR, 1, 1), id_b = pt_idesc(1, 1, NR, 1, 1);
-    int v_slot = 0, v_tile = 0, w_buf = 0, n = 0;
+    int v_slot = 0, v_tile = 0, w_buf = 0;
+    uint32_t n = 0;                                     // tiles per turn so far, a byte each
     for (int done = 0; done < share && ok;) {
       int b, u, t0, t1, nt;
       segment(done, b, u, t0, t1, nt);
       done += t1 - t0;
       const int n8 = X.n8[b];
       for (int tile = t0; tile < t1 && ok; ++tile) {
-        const int tp = (tile - t0) & 1;
-        const int cg = tp ? n >> 16 : n & 0xffff;
+        const int tp = (tile - t0) & (NP - 1);
+        const int cg = (n >> (8 * tp)) & 0xff;
         ok = pt_wait(&X.w_full[v_tile & 7], (v_tile >> 3) & 1, abort_flag, status) &&
              pt_wait(&X.p_full[tp], cg & 1, abort_flag, status);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         const uint32_t d = tm + F::O_COL + tp * NR;
         const uint64_t p = p0 + tp * (F::PB >> 4);
-        const bool add = tile - t0 >= 2;
+        const bool add = tile - t0 >= NP;
         if (ok && tile < n8) {
           const uint64_t v = v16 + w_buf * (F::VB >> 4);
 #pragma unroll
@@ -512,7 +520,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         }
         if (++v_slot == VST) v_slot = 0;
         ++v_tile;
-        n = tp ? n + 0x10000 : (n & ~0xffff) | ((n + 1) & 0xffff);
+        n = (n & ~(0xffu << (8 * tp))) | (((cg + 1u) & 0xffu) << (8 * tp));
       }
     }
     if (!ok) {
@@ -520,10 +528,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       while (global_ns() - ts < 2000000ull) { }
     }
   }
-  } else if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  } else if (warp >= 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     // ==================================================================== V to fp16
-    const int ct = tid - 256;                           // 0 .. 127
+    const int ct = tid - PT_SOFTMAX;                    // 0 .. 127
     // Four pieces of 16 codes of rows r and r ^ 5 go through eight lanes: both the 16-byte loads (8 pieces of a
     // swizzled row of codes) and the 16-byte stores (every other piece of a swizzled row of fp16) of such a
     // group fall into different banks.
@@ -543,17 +551,19 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
           const int buf = w_n & 1, live = I.live;
           if (ok && w_n >= 2) ok = pt_wait(&X.w_empty[buf], ((w_n >> 1) & 1) ^ 1, abort_flag, status);
           unsigned char* dst = smem + F::OFF_W + buf * F::VB;
-          // a warp's step: 8 rows, four pieces (64 dims); D / 64 such halves of 16 groups of rows.  All of a
-          // thread's loads are asked for before the first conversion.
-          uint4 v[4 * KB];
+          // a warp's step: 8 rows, four pieces (64 dims); D / 64 such halves of 16 groups of rows.  Four
+          // loads are asked for before the first conversion.
+#pragma unroll 1
+          for (int i0 = 0; i0 < 4 * KB; i0 += 4) {
+          uint4 v[4];
 #pragma unroll
-          for (int i = 0; i < 4 * KB; ++i) {
-            const int st = i * 4 + cw, r = (st / KB) * 8 + rr;
+          for (int i = 0; i < 4; ++i) {
+            const int st = (i0 + i) * 4 + cw, r = (st / KB) * 8 + rr;
             v[i] = *reinterpret_cast<const uint4*>(src + pt_piece<D>(r, (st % KB) * 4 + (lane & 3)));
           }
 #pragma unroll
-          for (int i = 0; i < 4 * KB; ++i) {
-            const int st = i * 4 + cw, r = (st / KB) * 8 + rr, pc = lane & 3;
+          for (int i = 0; i < 4; ++i) {
+            const int st = (i0 + i) * 4 + cw, r = (st / KB) * 8 + rr, pc = lane & 3;
             if (r >= live) v[i] = make_uint4(0u, 0u, 0u, 0u);   // rows behind the last page may hold anything
             const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
             uint32_t o[8];
@@ -568,6 +578,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
             *reinterpret_cast<uint4*>(d + pt_piece<128>(r, pc * 2)) = make_uint4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<uint4*>(d + pt_piece<128>(r, pc * 2 + 1)) = make_uint4(o[4], o[5], o[6], o[7]);
           }
+          }
           ++w_n;
         } else if (ct < PT_WKEYS) {
           // rows that no live key owns may hold anything, NaN included, and 0 * NaN would reach every row
@@ -578,7 +589,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
           }
         }
         fence_proxy_async_smem();
-        pt_bar<4, 128>();
+        pt_bar<6, 128>();
         if (ct == 0) {
           mbar_arrive(&X.w_full[tc & 7]);
           if (tile < n8) mbar_arrive(&X.v_empty[v_slot]);   // (a bf16 tile is read where it is)
@@ -587,13 +598,15 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
     // ==================================================================== softmax groups
-    const int tp = warp >> 2, wq = warp & 3;            // group, tensor-memory lane quarter
+    const int grp = warp >> 2, wq = warp & 3;           // group, tensor-memory lane quarter
+    const int rg = grp & (NRG - 1), tp = grp / NRG;     // its rows of the block, its turn among the tiles
+    const int grow = rg * RW;                           // first row of the group in the block
     const int kl = wq * 32 + lane;                      // this thread's key of a tile / head dim of O
     const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
     unsigned char* pbuf = smem + F::OFF_P + tp * F::PB;
-    const uint32_t oa = tmem + lane_base + F::O_COL + tp * NR;
+    const uint32_t oa = tmem + lane_base + F::O_COL + tp * NR + grow;
     const int pg = kl / ps;                             // page of the key within a tile
     const float c16 = scale * 1.4426950408889634f;
     auto group_or = [&](bool mine) {                    // a barrier that tells whether any thread said yes
@@ -602,11 +615,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
           "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 128, p;\n\t"
           "selp.u32 %0, 1, 0, q;\n\t}"
           : "=r"(r)
-          : "r"((uint32_t)mine), "r"(tp + 1)
+          : "r"((uint32_t)mine), "r"(grp + 1)
           : "memory");
       return r != 0;
     };
-    auto group_bar = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(tp + 1) : "memory"); };
+    auto group_bar = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory"); };
     auto scale_pow2 = [](float from, float to) { return from == -INFINITY ? 0.f : fast_exp2(from - to); };
     int cnt = 0, tc = 0;                                // tiles of this group, tiles of the CTA
     for (int done = 0; done < share;) {
@@ -640,8 +653,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       amax = jk_warp_max(amax);
       if (lane == 0) X.q_max[warp] = amax;
       // (also: all groups are done with the previous unit's queries, sums and row tables)
-      pt_bar<3, PT_SOFTMAX>();
-      amax = jk_warp_max(X.q_max[lane & 7]);
+      pt_bar<5, PT_SOFTMAX>();
+      amax = jk_warp_max(X.q_max[lane & 15]);
       int qe = (int)(__float_as_uint(amax) >> 23) - 127 - 8 + ((__float_as_uint(amax) & 0x7fffffu) > 0x600000u ? 1 : 0);
       qe = max(-100, min(100, qe));
       const float qinv = paged_pow2(-qe);
@@ -695,20 +708,17 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         X.seg_whole = t0 == 0 && t1 == nt;
         X.c8 = scale * 1.4426950408889634f * paged_pow2(qe);
       }
-      pt_bar<3, PT_SOFTMAX>();                          // row tables are visible
+      pt_bar<5, PT_SOFTMAX>();                          // row tables are visible
 
-      constexpr int CH = NR < 32 ? NR : 32, SL = NR / CH;   // rows of a lane's share of row values, shares
-      float2 lacc[NR / 2];                              // sums of the weights of this thread's keys, unit 2^ref
+      float2 lacc[RW / 2];                              // sums of the weights of this thread's keys, unit 2^ref
 #pragma unroll
-      for (int i = 0; i < NR / 2; ++i) lacc[i] = make_float2(0.f, 0.f);
-      float ref[SL];                                    // of rows i * CH + lane (mod CH)
-#pragma unroll
-      for (int i = 0; i < SL; ++i) ref[i] = -INFINITY;
+      for (int i = 0; i < RW / 2; ++i) lacc[i] = make_float2(0.f, 0.f);
+      float ref = -INFINITY;                            // of row lane (mod RW)
       bool unseen = true;                               // some row has no reference yet
       const int cnt0 = cnt;                             // tiles before this unit
 
       for (int tile = t0; tile < t1; ++tile, ++tc) {
-        if (((tile - t0) & 1) != tp) continue;
+        if (((tile - t0) & (NP - 1)) != tp) continue;
         const bool wide = tile >= n8;
         const pt_info& I = X.info[tc % PT_INFO];
         if (ok) ok = pt_wait(&X.info_full[tc % PT_INFO], (tc / PT_INFO) & 1, abort_flag, status);
@@ -722,27 +732,24 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
             dead = dead || kl >= PT_WKEYS || (kl >= I.open_rows && kl < I.open16);
             if (!dead && kl >= I.open16) node = kl - I.open16;
           }
+          uint32_t v = 0xffffffffu;
+          if (node >= 0) {
+            const uint4* aw = reinterpret_cast<const uint4*>(&X.anc[(node >> 5) & 3][grow]);
+            const int sh = node & 31;
+            v = 0u;
 #pragma unroll 1
-          for (int i = 0; i < SL; ++i) {
-            uint32_t v = 0xffffffffu;
-            if (node >= 0) {
-              const uint4* aw = reinterpret_cast<const uint4*>(&X.anc[(node >> 5) & 3][i * CH]);
-              const int sh = node & 31;
-              v = 0u;
-#pragma unroll 1
-              for (int e = 0; e < CH; e += 4) {
-                const uint4 a = aw[e >> 2];
-                v |= (((a.x >> sh) & 1u) | ((a.y >> sh) & 1u) << 1 | ((a.z >> sh) & 1u) << 2 | ((a.w >> sh) & 1u) << 3) << e;
-              }
+            for (int e = 0; e < RW; e += 4) {
+              const uint4 a = aw[e >> 2];
+              v |= (((a.x >> sh) & 1u) | ((a.y >> sh) & 1u) << 1 | ((a.z >> sh) & 1u) << 2 | ((a.w >> sh) & 1u) << 3) << e;
             }
-            X.vis[i][tid] = dead ? 0u : v;
           }
+          X.vis[tid] = dead ? 0u : v;
         }
         const float k1 = wide ? c16 : X.c8 * I.sk[pg], l1 = wide ? 0.f : I.lsv[pg], f1 = wide ? 1.f : I.sv[pg];
         if (ok) ok = pt_wait(&X.s_full[tp][cnt & 1], (cnt >> 1) & 1, abort_flag, status);
         __syncwarp();
         tc_fence_after();
-        const uint32_t sa = tmem + lane_base + (tp * 2 + (cnt & 1)) * NR;
+        const uint32_t sa = tmem + lane_base + (tp * 2 + (cnt & 1)) * NR + grow;
 
         // the weights of the group's last tile have been read, and its product is complete
         auto last_product = [&]() {
@@ -754,49 +761,40 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         };
         // References, raised to the rounded-up maximum of the tile where that is higher; sums follow.
         auto references = [&]() {
-#pragma unroll 1
-          for (int i = 0; i < SL; ++i) {
-            uint32_t r[CH];
-            float m[CH];
-            pt_ld<CH>(sa + i * CH, r);
+          {
+            uint32_t r[RW];
+            float m[RW];
+            pt_ld<RW>(sa, r);
             tmem_ld_wait();
-            const uint32_t v1 = masked ? X.vis[i][tid] : 0xffffffffu;
+            const uint32_t v1 = masked ? X.vis[tid] : 0xffffffffu;
 #pragma unroll
-            for (int j = 0; j < CH; ++j) m[j] = (v1 >> j) & 1u ? fmaf(__uint_as_float(r[j]), k1, l1) : -INFINITY;
-            float top = pt_rows_reduce<CH, false>(m, lane);
-            if (CH == 16) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-            if (lane < CH) X.wmax[tp][wq][i * CH + lane] = top;
+            for (int j = 0; j < RW; ++j) m[j] = (v1 >> j) & 1u ? fmaf(__uint_as_float(r[j]), k1, l1) : -INFINITY;
+            float top = pt_rows_reduce<RW, false>(m, lane);
+            if (RW == 16) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            if (lane < RW) X.wmax[grp][wq][lane] = top;
           }
           group_bar();
-          bool moved = false;
-          unseen = false;
-#pragma unroll
-          for (int i = 0; i < SL; ++i) {
-            const float* wm = &X.wmax[tp][0][i * CH + (lane & (CH - 1))];
-            const float top = ceilf(fmaxf(fmaxf(wm[0], wm[NR]), fmaxf(wm[2 * NR], wm[3 * NR])));
-            const float now = fmaxf(ref[i], top);
-            if (lane < CH) {
-              // (a row that sees nothing here has a reference of 0 meanwhile: its weights are all 0)
-              X.nref[warp][i * CH + lane] = PT_SHIFT - (now == -INFINITY ? 0.f : now);
-              X.alpha[warp][i * CH + lane] = scale_pow2(ref[i], now);
-            }
-            moved |= ref[i] != now;
-            unseen |= now == -INFINITY;
-            ref[i] = now;
+          const float* wm = &X.wmax[grp][0][lane & (RW - 1)];
+          const float now = fmaxf(ref, ceilf(fmaxf(fmaxf(wm[0], wm[32]), fmaxf(wm[64], wm[96]))));
+          if (lane < RW) {
+            // (a row that sees nothing here has a reference of 0 meanwhile: its weights are all 0)
+            X.nref[warp][lane] = PT_SHIFT - (now == -INFINITY ? 0.f : now);
+            X.alpha[warp][lane] = scale_pow2(ref, now);
           }
-          moved = __any_sync(0xffffffffu, moved);
-          unseen = __any_sync(0xffffffffu, unseen);
+          const bool moved = __any_sync(0xffffffffu, ref != now);
+          unseen = __any_sync(0xffffffffu, now == -INFINITY);
+          ref = now;
           __syncwarp();
           if (moved && cnt > cnt0) {
 #pragma unroll
-            for (int j = 0; j < NR / 2; ++j) {
+            for (int j = 0; j < RW / 2; ++j) {
               const float2 al = *reinterpret_cast<const float2*>(&X.alpha[warp][2 * j]);
               lacc[j].x *= al.x;
               lacc[j].y *= al.y;
             }
             last_product();
 #pragma unroll 1
-            for (int j0 = 0; j0 < NR; j0 += 16) {
+            for (int j0 = 0; j0 < RW; j0 += 16) {
               uint32_t r[16];
               tmem_ld16(oa + j0, r);
               tmem_ld_wait();
@@ -811,86 +809,74 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         // ---- weights; a second time, with higher references, if one passed the range.  The row sums are fp32 and
         // right the first time unless a weight was infinite; such a sum (`lost`) starts again, what it held
         // is below 2^-80 of what comes in.
-        unsigned long long lost = 0ull;
+        uint32_t lost = 0u;
         bool anew = unseen;
         for (int attempt = 0; attempt < 2; ++attempt) {
           if (anew) references();
           __half2 most = __float2half2_rn(0.f);
-          uint32_t r[2][16];                            // this block's logits, the next one's on their way
-          tmem_ld16(sa, r[0]);
           const uint64_t kk = pt_pack2(k1, k1), ff = pt_pack2(f1, f1);
-          float2 e[8], w[8];
-          // 16 rows at a time: the exponentials of a block (e) are issued among the conversions of the one before (w)
 #pragma unroll
-          for (int j0 = 0; j0 <= NR; j0 += 16) {
-            if (j0 < NR) {
-              const uint32_t (&x)[16] = r[(j0 >> 4) & 1];
-              tmem_ld_wait();
-              if (j0 + 16 < NR) tmem_ld16(sa + j0 + 16, r[((j0 >> 4) + 1) & 1]);
+          for (int j0 = 0; j0 < RW; j0 += 16) {
+            uint32_t x[16], pk[8];
+            float2 e[8];
+            tmem_ld16(sa + j0, x);
+            tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 8; j += 2) {
-                const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(&X.nref[warp][j0 + 2 * j]);
-                e[j] = pt_unpack2(pt_fma2(pt_pack2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), kk, rf.x));
-                e[j + 1] = pt_unpack2(pt_fma2(pt_pack2(__uint_as_float(x[2 * j + 2]), __uint_as_float(x[2 * j + 3])), kk, rf.y));
-              }
-#pragma unroll
-              for (int j = 0; j < 8; ++j) e[j] = make_float2(fast_exp2(e[j].x), fast_exp2(e[j].y));
+            for (int j = 0; j < 8; j += 2) {
+              const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(&X.nref[warp][j0 + 2 * j]);
+              e[j] = pt_unpack2(pt_fma2(pt_pack2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), kk, rf.x));
+              e[j + 1] = pt_unpack2(pt_fma2(pt_pack2(__uint_as_float(x[2 * j + 2]), __uint_as_float(x[2 * j + 3])), kk, rf.y));
             }
-            if (j0 > 0) {
-              const int jw = j0 - 16;                   // rows of w
-              if (jw == 0) last_product();
-              uint32_t pk[8];
-              if (!wide) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const __half2 v = __float22half2_rn(pt_unpack2(pt_mul2(pt_pack2(w[j].x, w[j].y), ff)));
-                  pk[j] = *reinterpret_cast<const uint32_t*>(&v);
-                }
-                auto h = [&](int j) { return *reinterpret_cast<const __half2*>(&pk[j]); };
-                most = __hmax2(most, __hmax2(__hmax2(__hmax2(h(0), h(1)), __hmax2(h(2), h(3))),
-                                             __hmax2(__hmax2(h(4), h(5)), __hmax2(h(6), h(7)))));
-              } else {
+            for (int j = 0; j < 8; ++j) e[j] = make_float2(fast_exp2(e[j].x), fast_exp2(e[j].y));
+            if (masked) {
+              const uint32_t v1 = X.vis[tid] >> j0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const __nv_bfloat162 v = __float22bfloat162_rn(w[j]);
-                  most = __hmax2(most, __float22half2_rn(w[j]));
-                  pk[j] = *reinterpret_cast<const uint32_t*>(&v);
-                }
+              for (int j = 0; j < 8; ++j) {
+                if (!((v1 >> (2 * j)) & 1u)) e[j].x = 0.f;
+                if (!((v1 >> (2 * j + 1)) & 1u)) e[j].y = 0.f;
               }
-              *reinterpret_cast<uint4*>(pbuf + pt_piece<F::PROW>(kl, jw >> 3)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-              *reinterpret_cast<uint4*>(pbuf + pt_piece<F::PROW>(kl, (jw >> 3) + 1)) = make_uint4(pk[4], pk[5], pk[6], pk[7]);
             }
-            if (j0 < NR) {
-              if (masked) {
-                const uint32_t v1 = X.vis[j0 >> 5][tid] >> (j0 & 16);
+            if (attempt == 0) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  if (!((v1 >> (2 * j)) & 1u)) e[j].x = 0.f;
-                  if (!((v1 >> (2 * j + 1)) & 1u)) e[j].y = 0.f;
-                }
+              for (int j = 0; j < 8; ++j)
+                lacc[j0 / 2 + j] = pt_unpack2(pt_add2(pt_pack2(lacc[j0 / 2 + j].x, lacc[j0 / 2 + j].y), pt_pack2(e[j].x, e[j].y)));
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                if ((lost >> (j0 + 2 * j)) & 1u) lacc[j0 / 2 + j].x += e[j].x;
+                if ((lost >> (j0 + 2 * j + 1)) & 1u) lacc[j0 / 2 + j].y += e[j].y;
               }
-              if (attempt == 0) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                  lacc[(j0 / 2 + j) % (NR / 2)] = pt_unpack2(pt_add2(pt_pack2(lacc[(j0 / 2 + j) % (NR / 2)].x, lacc[(j0 / 2 + j) % (NR / 2)].y), pt_pack2(e[j].x, e[j].y)));
-              } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  if ((lost >> (j0 + 2 * j)) & 1ull) lacc[(j0 / 2 + j) % (NR / 2)].x += e[j].x;
-                  if ((lost >> (j0 + 2 * j + 1)) & 1ull) lacc[(j0 / 2 + j) % (NR / 2)].y += e[j].y;
-                }
-              }
-#pragma unroll
-              for (int j = 0; j < 8; ++j) w[j] = e[j];
             }
+            __half2 top[4];
+            if (!wide) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const __half2 v = __float22half2_rn(pt_unpack2(pt_mul2(pt_pack2(e[j].x, e[j].y), ff)));
+                pk[j] = *reinterpret_cast<const uint32_t*>(&v);
+                top[j & 3] = j < 4 ? v : __hmax2(top[j & 3], v);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const __nv_bfloat162 v = __float22bfloat162_rn(e[j]);
+                const __half2 t = __float22half2_rn(e[j]);
+                pk[j] = *reinterpret_cast<const uint32_t*>(&v);
+                top[j & 3] = j < 4 ? t : __hmax2(top[j & 3], t);
+              }
+            }
+            most = __hmax2(most, __hmax2(__hmax2(top[0], top[1]), __hmax2(top[2], top[3])));
+            if (j0 == 0) last_product();
+            *reinterpret_cast<uint4*>(pbuf + pt_piece<F::PROW>(kl, (grow + j0) >> 3)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            *reinterpret_cast<uint4*>(pbuf + pt_piece<F::PROW>(kl, ((grow + j0) >> 3) + 1)) = make_uint4(pk[4], pk[5], pk[6], pk[7]);
           }
           if (attempt == 1) break;
           const bool over = __hgt(__hmax(__low2half(most), __high2half(most)), __float2half(65504.f));
           if (!group_or(over)) break;
 #pragma unroll
-          for (int j = 0; j < NR / 2; ++j) {
-            if (lacc[j].x == INFINITY) { lacc[j].x = 0.f; lost |= 1ull << (2 * j); }
-            if (lacc[j].y == INFINITY) { lacc[j].y = 0.f; lost |= 2ull << (2 * j); }
+          for (int j = 0; j < RW / 2; ++j) {
+            if (lacc[j].x == INFINITY) { lacc[j].x = 0.f; lost |= 1u << (2 * j); }
+            if (lacc[j].y == INFINITY) { lacc[j].y = 0.f; lost |= 2u << (2 * j); }
           }
           anew = true;
         }
@@ -910,62 +896,70 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       }
 
       // ------------------------------------------------ the segment's result
+      {
+        float l[RW];
 #pragma unroll
-      for (int i = 0; i < SL; ++i) {
-        float l[CH];
-#pragma unroll
-        for (int j = 0; j < CH / 2; ++j) { l[2 * j] = lacc[i * CH / 2 + j].x; l[2 * j + 1] = lacc[i * CH / 2 + j].y; }
-        float sum = pt_rows_reduce<CH, true>(l, lane);
-        if (CH == 16) sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-        if (lane < CH) {
-          X.lsum[warp][i * CH + lane] = sum;
-          if (wq == 0) X.m_run[tp][i * CH + lane] = ref[i];
+        for (int j = 0; j < RW / 2; ++j) { l[2 * j] = lacc[j].x; l[2 * j + 1] = lacc[j].y; }
+        float sum = pt_rows_reduce<RW, true>(l, lane);
+        if (RW == 16) sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+        if (lane < RW) {
+          X.alpha[warp][lane] = sum;
+          if (wq == 0) X.m_run[grp][lane] = ref;
         }
       }
       const int seg_b = X.seg_b;
       const bool whole = X.seg_whole != 0;
       float* po = part_o + (size_t)X.seg_slot * NR * D;
       float* pml = part_ml + (size_t)X.seg_slot * NR * 2;
-      float* mb = reinterpret_cast<float*>(smem + F::OFF_P);     // [NR][128] over the weights
-      pt_bar<3, PT_SOFTMAX>();                          // every product has been read: the weights are free
-      if (tp == 1 && cnt > cnt0) {
+      float* mb = reinterpret_cast<float*>(smem + F::OFF_P);     // [NP - 1][NR][128] over the weights
+      pt_bar<5, PT_SOFTMAX>();                          // every product has been read: the weights are free
+      if (tp > 0 && cnt > cnt0) {
 #pragma unroll 1
-        for (int j0 = 0; j0 < NR; j0 += 16) {
+        for (int j0 = 0; j0 < RW; j0 += 16) {
           uint32_t v[16];
           tmem_ld16(oa + j0, v);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) mb[(j0 + j) * 128 + kl] = __uint_as_float(v[j]);
+          for (int j = 0; j < 16; ++j) mb[((tp - 1) * NR + grow + j0 + j) * 128 + kl] = __uint_as_float(v[j]);
         }
       }
       if (tid < NR) {
-        // row tid: what each group's sum weighs
-        const float m0 = X.m_run[0][tid], m1 = X.m_run[1][tid], m = fmaxf(m0, m1);
-        const float a0 = scale_pow2(m0, m), a1 = scale_pow2(m1, m);
-        const float l = a0 * ((X.lsum[0][tid] + X.lsum[1][tid]) + (X.lsum[2][tid] + X.lsum[3][tid])) +
-                        a1 * ((X.lsum[4][tid] + X.lsum[5][tid]) + (X.lsum[6][tid] + X.lsum[7][tid]));
+        // row tid: what each turn's sum weighs
+        const int g0 = tid / RW, r = tid & (RW - 1);
+        float m = -INFINITY, l = 0.f, a[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) m = fmaxf(m, X.m_run[i * NRG + g0][r]);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const int w = (i * NRG + g0) * 4;
+          a[i] = scale_pow2(X.m_run[i * NRG + g0][r], m);
+          l = fmaf(a[i], (X.alpha[w][r] + X.alpha[w + 1][r]) + (X.alpha[w + 2][r] + X.alpha[w + 3][r]), l);
+        }
         const float inv = whole ? 1.f / l : 1.f;
-        X.wt[0][tid] = a0 * inv;
-        X.wt[1][tid] = a1 * inv;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) X.wt[i][tid] = a[i] * inv;
         if (!whole) {
           pml[tid * 2] = m;
           pml[tid * 2 + 1] = l;
         }
       }
       tc_fence_before();
-      pt_bar<3, PT_SOFTMAX>();
-      if (tp == 0) {                                    // (the first tile was this group's: there is a sum)
+      pt_bar<5, PT_SOFTMAX>();
+      if (tp == 0) {                                    // (the first tile was this turn's: there is a sum)
 #pragma unroll 1
-        for (int j0 = 0; j0 < NR; j0 += 16) {
+        for (int j0 = 0; j0 < RW; j0 += 16) {
           uint32_t x[16];
           tmem_ld16(oa + j0, x);
           tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            const int row = j0 + j;
+            const int row = grow + j0 + j;
             float v = __uint_as_float(x[j]) * X.wt[0][row];
-            const float w1 = X.wt[1][row];
-            if (w1 != 0.f) v = fmaf(mb[row * 128 + kl], w1, v);
+#pragma unroll
+            for (int i = 1; i < NP; ++i) {
+              const float w1 = X.wt[i][row];
+              if (w1 != 0.f) v = fmaf(mb[((i - 1) * NR + row) * 128 + kl], w1, v);
+            }
             if (kl < D) {
               if (whole) {
                 const int off = X.rowoff[row];
@@ -982,7 +976,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 13) {
+  if (warp == 21) {
     tc_fence_after();
     tmem_dealloc(tmem, F::COLS);
   }
