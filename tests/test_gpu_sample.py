@@ -91,6 +91,32 @@ def test_equal_logits(V):
     run(ctx, -steps, "f32", m=[0.1, 0.2, 0.4, 0.9, 1.0, 0.0], u=rng.random(6))
 
 
+@pytest.mark.parametrize("V", [6001, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_crowded_values(V, dtype):
+    """Rows whose values crowd where a threshold is looked for: a narrow band, next to zero, far below the weights that
+    count, all negative, a scale of logits that one temperature leaves flat and another one sharp."""
+    rng = np.random.default_rng(V)
+    ctx = make_ctx(V)
+    n = rng.standard_normal((10, V))
+    z = np.empty((10, V))
+    z[0] = 5.0 + 1e-4 * n[0]
+    z[1] = 1e-6 * n[1]
+    z[2] = -3.0 - 1e-5 * np.abs(n[2])
+    z[3] = np.where(n[3] > -1.0, -1e4 - 1e3 * np.abs(n[3]), 2.0 * n[3])
+    z[4] = 1e4 * n[4]
+    z[5] = np.where(n[5] > 0, np.finfo(np.float32).min, n[5])
+    z[6] = -50.0 * np.abs(n[6])
+    z[7] = 1e-38 * n[7]
+    z[8] = 1e30 * n[8]
+    z[9] = np.round(n[9] * 8) / 8
+    z = synth.store_round(z, dtype).astype(np.float64)
+    f32 = np.float32
+    for T in (1.0, 100.0, np.array([1e-4, 1e-6, 1e-5, 1e3, 1e4, 0.3, 50.0, 1e-38, 1e30, 0.2])):
+        for f in (dict(p=0.5003), dict(k=300), dict(k=V // 2, p=0.731), dict(k=V - 3, p=0.99, m=0.2), dict(k=40, p=0.6)):
+            run(ctx, z, dtype, T=T, u=rng.random(10).astype(f32), **f)
+
+
 def test_infinities_nan_and_empty_rows():
     V = 1003
     rng = np.random.default_rng(7)
