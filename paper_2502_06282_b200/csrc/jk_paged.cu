@@ -81,22 +81,75 @@ __device__ __forceinline__ void plan_verdict(const jk_paged& c, int32_t* status,
 }
 
 // ---------------------------------------------------------------------------- quantisation
-// `tpu` threads (16 .. 256, a power of two) quantise one block of tpu * 64 elements: each holds four
-// runs of 16 elements from their load to their rounding.  Threads of inactive units take part in
-// the barriers.  red: 8 floats.
-template <typename T>
-__device__ __forceinline__ void paged_quantise(const T* src, uint8_t* dst, float* scale, int t, int tpu,
-                                             bool active, float* red) {
-  float v[4][16];
+// Largest finite |x| of raw 16-byte pieces.  bf16: as 16-bit integers, two at a time; only where an infinity or a
+// NaN shows are the elements looked at one by one.
+template <typename T, int N> __device__ __forceinline__ float paged_max(const uint4 (&r)[N]) {
   float amax = 0.f;
-  if (active) {
+  if (sizeof(T) == 2) {
+    uint32_t m = 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) paged_load16(src + (size_t)(i * tpu + t) * 16, v[i]);
+    for (int i = 0; i < N; ++i) {
+      m = __vmaxu2(m, r[i].x & 0x7fff7fffu);
+      m = __vmaxu2(m, r[i].y & 0x7fff7fffu);
+      m = __vmaxu2(m, r[i].z & 0x7fff7fffu);
+      m = __vmaxu2(m, r[i].w & 0x7fff7fffu);
+    }
+    const uint32_t top = max(m & 0xffffu, m >> 16);
+    amax = __uint_as_float(top << 16);
+    if (top >= 0x7f80u) {
+      amax = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < N; ++i) {
+        uint4 q = r[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int j = 1; j < N; ++j)
+          if (i == j) q = r[j];
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int j = 0; j < 16; ++j) amax = fmaxf(amax, paged_mag(v[i][j]));
+        for (int j = 0; j < 4; ++j)
+          amax = fmaxf(amax, fmaxf(paged_mag(__uint_as_float(w[j] << 16)), paged_mag(__uint_as_float(w[j] & 0xffff0000u))));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      amax = fmaxf(fmaxf(fmaxf(amax, paged_mag(__uint_as_float(r[i].x))), fmaxf(paged_mag(__uint_as_float(r[i].y)),
+                   paged_mag(__uint_as_float(r[i].z)))), paged_mag(__uint_as_float(r[i].w)));
   }
+  return amax;
+}
+// 4 codes of 4 elements from element 4 k of raw pieces on
+template <typename T, int N> __device__ __forceinline__ uint32_t paged_codes(const uint4* r, int k, float inv) {
+  float v[4];
+  if (sizeof(T) == 2) {
+    const uint4 q = r[k >> 1];
+    const uint32_t a = k & 1 ? q.z : q.x, b = k & 1 ? q.w : q.y;
+    v[0] = __uint_as_float(a << 16); v[1] = __uint_as_float(a & 0xffff0000u);
+    v[2] = __uint_as_float(b << 16); v[3] = __uint_as_float(b & 0xffff0000u);
+  } else {
+    const uint4 q = r[k];
+    v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+  }
+  return paged_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+}
+
+// `tpu` threads (16 .. 256, a power of two) quantise one block of tpu * 64 elements: each holds four
+// runs of 16 elements, as they are in memory, from their load to their rounding: held as floats, bf16 took twice the
+// registers, and an SM held two thread blocks instead of four.  Threads of inactive units take part in the
+// barriers.  red: 8 floats.
+template <typename T>
+__device__ __forceinline__ void paged_load_block(const T* src, int t, int tpu, uint4 (&raw)[4 * sizeof(T)]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T); ++j)
+      raw[i * sizeof(T) + j] = __ldcs(reinterpret_cast<const uint4*>(src + (size_t)(i * tpu + t) * 16) + j);
+}
+template <typename T>
+__device__ __forceinline__ void paged_quantise(const uint4 (&raw)[4 * sizeof(T)], uint8_t* dst, float* scale, int t, int tpu,
+                                               bool active, float* red) {
+  constexpr int RUN = sizeof(T);                         // pieces of 16 elements
+  float amax = active ? paged_max<T>(raw) : 0.f;
   const int lanes = tpu < 32 ? tpu : 32;
   for (int o = lanes >> 1; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
   if (tpu > 32) {
@@ -112,12 +165,13 @@ __device__ __forceinline__ void paged_quantise(const T* src, uint8_t* dst, float
   const float inv = paged_pow2(-e);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
+    const uint4* r = raw + i * RUN;
     uint4 o;
-    o.x = paged_pack4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
-    o.y = paged_pack4(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
-    o.z = paged_pack4(v[i][8] * inv, v[i][9] * inv, v[i][10] * inv, v[i][11] * inv);
-    o.w = paged_pack4(v[i][12] * inv, v[i][13] * inv, v[i][14] * inv, v[i][15] * inv);
-    *reinterpret_cast<uint4*>(dst + (size_t)(i * tpu + t) * 16) = o;
+    o.x = paged_codes<T, RUN>(r, 0, inv);
+    o.y = paged_codes<T, RUN>(r, 1, inv);
+    o.z = paged_codes<T, RUN>(r, 2, inv);
+    o.w = paged_codes<T, RUN>(r, 3, inv);
+    __stcs(reinterpret_cast<uint4*>(dst + (size_t)(i * tpu + t) * 16), o);
   }
   if (t == 0) *scale = paged_pow2(e);
 }
@@ -226,21 +280,24 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_plan(
 // Block (x = (page group, sequence, head), y = (layer, K or V)); the last page group copies the
 // tokens behind the last full page to the open rows.
 template <typename T>
-__global__ void __launch_bounds__(256) k_paged_import(
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_paged_import(
     jk_paged c, int Hkv, int d, int groups, int first_layer, const int32_t* __restrict__ seqs,
     const int32_t* __restrict__ n_tokens, void* const* __restrict__ k_src,
     void* const* __restrict__ v_src, long long sb, long long sh) {
   __shared__ float red[8];
   jk_pdl_wait();
   jk_pdl_trigger();
-  if (!c.scratch[PAGED_OK]) return;
+  // (what the block needs to know is asked for at once, and the data before the verdict and the page: one after
+  // the other these were longer than the movement)
   const int grp = blockIdx.x % groups, bh = blockIdx.x / groups;
   const int i = bh / Hkv, h = bh % Hkv;
   const int layer = first_layer + (blockIdx.y >> 1);
   const bool is_v = blockIdx.y & 1;
+  const int ok = c.scratch[PAGED_OK], n = n_tokens[i];
   const int row = seqs ? seqs[i] : i;
-  const int ps = c.page_size, n = n_tokens[i], nf = n / ps;
   const T* src = (const T*)(is_v ? v_src : k_src)[blockIdx.y >> 1] + (size_t)i * sb + (size_t)h * sh;
+  if (!ok) return;
+  const int ps = c.page_size, nf = n / ps;
   if (grp == groups - 1) {
     T* dst = (T*)(is_v ? c.v_open : c.k_open) +
              ((((size_t)layer * c.max_seqs + row) * Hkv + h) * 2 * ps + (size_t)(nf & 1) * ps) * d;
@@ -253,48 +310,61 @@ __global__ void __launch_bounds__(256) k_paged_import(
   const int t = grp * upb + (int)threadIdx.x / tpu;
   if (grp * upb >= nf) return;
   const bool active = t < nf;
+  uint4 raw[4 * sizeof(T)] = {};
+  if (active) paged_load_block<T>(src + (size_t)t * be, threadIdx.x & (tpu - 1), tpu, raw);
   const int page = active ? c.page_table[(size_t)row * c.max_pages + t] : 0;
   const size_t blk = ((size_t)layer * c.n_pages + page) * Hkv + h;
-  paged_quantise<T>(src + (size_t)(active ? t : 0) * be, (uint8_t*)(is_v ? c.v_pages : c.k_pages) + blk * be,
-                  (is_v ? c.v_scale : c.k_scale) + blk, threadIdx.x & (tpu - 1), tpu, active, red);
+  paged_quantise<T>(raw, (uint8_t*)(is_v ? c.v_pages : c.k_pages) + blk * be, (is_v ? c.v_scale : c.k_scale) + blk,
+                    threadIdx.x & (tpu - 1), tpu, active, red);
 }
 
 // ---------------------------------------------------------------------------- commit: movement
-// Block (x = (sequence, head), y = (layer, K or V)): the new rows join the open rows, then the pages
-// they complete are quantised from there.  At most 17 new rows: at most two pages.
+// Block (x = (sequence, head), y = layer), K and V: the new rows join the open rows, then the pages
+// they complete are quantised from there.  At most 17 new rows: at most two pages.  Bound by latency: what a
+// block needs to know is asked for at once, the rows behind it, and the grid is a few blocks per SM.
 template <typename T>
-__global__ void __launch_bounds__(256) k_paged_commit(
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_paged_commit(
     jk_paged c, int Hkv, int d, void* const* __restrict__ k_tree, void* const* __restrict__ v_tree,
     long long sb, long long sh, const int32_t* __restrict__ n_acc, const int32_t* __restrict__ acc_idx,
     int max_depth) {
   __shared__ float red[8];
+  __shared__ int s_node[33];
   jk_pdl_wait();
   jk_pdl_trigger();
-  if (!c.scratch[PAGED_OK]) return;
-  const int b = blockIdx.x / Hkv, h = blockIdx.x % Hkv;
-  const int layer = blockIdx.y >> 1;
-  const bool is_v = blockIdx.y & 1;
-  const int n = n_acc[b];
-  if (n < 0) return;
-  const int ps = c.page_size, len = c.kv_len[b], old = len - 1 - n;
-  const T* src = (const T*)(is_v ? v_tree : k_tree)[layer] + (size_t)b * sb + (size_t)h * sh;
-  T* open = (T*)(is_v ? c.v_open : c.k_open) + (((size_t)layer * c.max_seqs + b) * Hkv + h) * 2 * ps * d;
-  const int row16 = d * (int)sizeof(T) / 16;
-  for (int k = threadIdx.x; k < (n + 1) * row16; k += 256) {
-    const int j = k / row16, p = k % row16;
-    const int node = j == 0 ? 0 : acc_idx[(size_t)b * max_depth + j - 1];
-    const int at = (old + j) & (2 * ps - 1);
-    reinterpret_cast<uint4*>(open + (size_t)at * d)[p] =
-        reinterpret_cast<const uint4*>(src + (size_t)node * d)[p];
-  }
+  const int b = blockIdx.x / Hkv, h = blockIdx.x % Hkv, tid = threadIdx.x;
+  const int layer = blockIdx.y;
+  const int ok = c.scratch[PAGED_OK], n = n_acc[b], len = c.kv_len[b];
+  const T* ksrc = (const T*)k_tree[layer] + (size_t)b * sb + (size_t)h * sh;
+  const T* vsrc = (const T*)v_tree[layer] + (size_t)b * sb + (size_t)h * sh;
+  if (tid <= max_depth && tid < 33) s_node[tid] = tid == 0 ? 0 : acc_idx[(size_t)b * max_depth + tid - 1];
+  if (!ok || n < 0) return;
   __syncthreads();
-  const int be = ps * d, tpu = be / 64;
-  for (int t = old / ps; t < len / ps; ++t) {
-    const int page = c.page_table[(size_t)b * c.max_pages + t];
+  const int ps = c.page_size, old = len - 1 - n;
+  const size_t at_open = (((size_t)layer * c.max_seqs + b) * Hkv + h) * 2 * ps * d;
+  T* kopen = (T*)c.k_open + at_open;
+  T* vopen = (T*)c.v_open + at_open;
+  const int row16 = d * (int)sizeof(T) / 16, half = (n + 1) * row16;
+#pragma unroll 2
+  for (int k = tid; k < 2 * half; k += 256) {
+    const bool is_v = k >= half;
+    const int e = is_v ? k - half : k, j = e / row16, p = e % row16;
+    const int at = (old + j) & (2 * ps - 1);
+    reinterpret_cast<uint4*>((is_v ? vopen : kopen) + (size_t)at * d)[p] =
+        reinterpret_cast<const uint4*>((is_v ? vsrc : ksrc) + (size_t)s_node[j] * d)[p];
+  }
+  const int t0 = old / ps, units = 2 * (len / ps - t0);     // (page, K or V)
+  if (units == 0) return;
+  __syncthreads();
+  const int be = ps * d, tpu = be / 64, upb = 256 / tpu;
+  for (int u0 = 0; u0 < units; u0 += upb) {
+    const int u = u0 + tid / tpu, t = t0 + (u >> 1);
+    const bool active = u < units, is_v = u & 1;
+    uint4 raw[4 * sizeof(T)] = {};
+    if (active) paged_load_block<T>((is_v ? vopen : kopen) + (size_t)(t & 1) * be, tid & (tpu - 1), tpu, raw);
+    const int page = active ? c.page_table[(size_t)b * c.max_pages + t] : 0;
     const size_t blk = ((size_t)layer * c.n_pages + page) * Hkv + h;
-    paged_quantise<T>(open + (size_t)(t & 1) * be, (uint8_t*)(is_v ? c.v_pages : c.k_pages) + blk * be,
-                    (is_v ? c.v_scale : c.k_scale) + blk, threadIdx.x & (tpu - 1), tpu,
-                    (int)threadIdx.x < tpu, red);
+    paged_quantise<T>(raw, (uint8_t*)(is_v ? c.v_pages : c.k_pages) + blk * be, (is_v ? c.v_scale : c.k_scale) + blk,
+                      tid & (tpu - 1), tpu, active, red);
   }
 }
 
@@ -635,7 +705,7 @@ extern "C" int jk_paged_commit(jk_ctx* ctx, void* stream, const jk_paged* c, int
                 (const int32_t*)nullptr, 0, n_acc, acc_idx, g.max_depth, tree_size, paged_status(ctx));
   JK_LAUNCH_CHECK(ctx);
   JK_PROF(ctx, st, JK_ST_PAGED_MOVE);
-  const dim3 grid(batch * g.n_kv_heads, 2 * c->n_layers);
+  const dim3 grid(batch * g.n_kv_heads, c->n_layers);
   if (g.dtype == JK_BF16)
     jk_launch_pdl(k_paged_commit<__nv_bfloat16>, grid, dim3(256), 0, st, *c, g.n_kv_heads, g.head_dim,
                   k_tree, v_tree, (long long)sb, (long long)sh, n_acc, acc_idx, g.max_depth);
