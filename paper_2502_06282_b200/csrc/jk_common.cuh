@@ -185,6 +185,12 @@ static inline cudaError_t jk_launch_pdl_cluster(void (*kernel)(KArgs...), dim3 g
 }
 
 // ---------------------------------------------------------------- device helpers
+// A generic address of the shared variable at `p` in block `rank` of the cluster.
+template <typename P> __device__ __forceinline__ P* jk_cluster_map(P* p, uint32_t rank) {
+  unsigned long long a;
+  asm("mapa.u64 %0, %1, %2;" : "=l"(a) : "l"((unsigned long long)p), "r"(rank));
+  return reinterpret_cast<P*>(a);
+}
 __device__ __forceinline__ float jk_warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -164,6 +164,304 @@ __global__ void __launch_bounds__(256) k_paged_attn(
   }
 }
 
+// ---------------------------------------------------------------------------- few query rows
+// A cluster of C blocks per (sequence, kv head, R query rows); one launch, no partials in memory.  A key's D codes lie
+// in D / 16 lanes, 16 bytes each, so a warp reads 512 contiguous bytes per access; each such group of lanes goes
+// through its own keys, KU at a time (within a page), with its own running maximum, and holds R rows of its 16
+// dims of query and output.  What groups, warps and blocks found is merged at the end, in a fixed order.
+// Per key and row this takes about 2 instructions per dim on top of 3 to widen the codes of K and V: with one row the
+// bytes bound it, with more the instructions.
+#define KR_THREADS 256
+#define KR_WARPS (KR_THREADS / 32)
+#define KR_CLUSTER 8
+#define KR_MAX_ROWS 16                // without the tensor path: beyond, the keys are read too often
+
+__device__ __forceinline__ uint4 kr_load(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void kr_widen(const uint4& w, float* o) {
+  const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = paged_unpack2(a[i]), y = paged_unpack2(a[i] >> 16);
+    o[4 * i] = x.x; o[4 * i + 1] = x.y; o[4 * i + 2] = y.x; o[4 * i + 3] = y.y;
+  }
+}
+
+template <typename T, int D, int R>
+__global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
+    jk_paged c, int layer, const T* __restrict__ q, const T* __restrict__ k_tree, const T* __restrict__ v_tree,
+    long long tsb, long long tsh, const int32_t* __restrict__ parent, float scale, int M, int Hq, int Hkv, int C,
+    T* __restrict__ out, int32_t* status) {
+  constexpr int LPK = D / 16, GR = 32 / LPK, KU = R == 1 ? 8 : 4, STEP = GR * KU;
+  __shared__ float s_o[KR_WARPS][R][D];
+  __shared__ float s_m[KR_WARPS][R], s_l[KR_WARPS][R];
+  __shared__ float c_o[R][D], c_m[R], c_l[R];            // of the block, read by the cluster's first
+  __shared__ uint32_t s_anc[R][4];
+  jk_pdl_wait();
+  jk_pdl_trigger();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint32_t rank = 0;
+  if (C > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  auto sync = [&]() {
+    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else __syncthreads();
+  };
+  const int row0 = blockIdx.x / C * R, h = blockIdx.y, b = blockIdx.z;
+  const int G = Hq / Hkv, n_rows = G * M, ps = c.page_size;
+  const int P = c.kv_len[b];
+  if (P < 0 || P > c.max_pages * ps) {                   // (the same for the whole cluster)
+    if (tid == 0) jk_set_status(status, JK_ERR_BOUNDS);
+    return;
+  }
+  const int nf = P / ps * ps, n_open = P - nf, tail = n_open + M;
+  const int grp = lane / LPK, x0 = lane % LPK * 16;
+  float qf[R][16];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = min(row0 + r, n_rows - 1), g = row / M, i = row % M;
+    paged_load16(q + (((size_t)b * M + i) * Hq + h * G + g) * D + x0, qf[r]);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) qf[r][x] *= scale * 1.4426950408889634f;
+  }
+  if (tid < R) {
+    uint32_t a[4] = {0u, 0u, 0u, 0u};
+    int n = min(row0 + tid, n_rows - 1) % M;
+    for (int guard = 0; n >= 0 && guard <= JK_MAX_TREE; ++guard) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) a[w] |= w == n >> 5 ? 1u << (n & 31) : 0u;
+      const int p = parent[(size_t)b * M + n];
+      n = p < n ? p : -1;
+    }
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s_anc[tid][w] = a[w];
+  }
+  __syncthreads();
+  float acc[R][16], m[R], l[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) acc[r][x] = 0.f;
+  }
+  // KU keys: scores s (log2, -inf = not seen), values v(u)[16] times sv
+  auto take = [&](float (*s)[R], auto value) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float top = m[r];
+#pragma unroll
+      for (int u = 0; u < KU; ++u) top = fmaxf(top, s[u][r]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      const float corr = exp2f(m[r] - ref);
+      m[r] = top;
+      l[r] *= corr;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) acc[r][x] *= corr;
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        s[u][r] = exp2f(s[u][r] - ref);
+        l[r] += s[u][r];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < KU; ++u) {
+      float v[16];
+      const float sv = value(u, v);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float w = s[u][r] * sv;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) acc[r][x] = fmaf(w, v[x], acc[r][x]);
+      }
+    }
+  };
+  auto dot = [&](const float* k, float* s) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+      for (int x = 0; x < 16; x += 2) {
+        a0 = fmaf(qf[r][x], k[x], a0);
+        a1 = fmaf(qf[r][x + 1], k[x + 1], a1);
+      }
+      s[r] = a0 + a1;
+#pragma unroll
+      for (int o = LPK / 2; o > 0; o >>= 1) s[r] += __shfl_xor_sync(0xffffffffu, s[r], o);
+    }
+  };
+  const int W = C * KR_WARPS, gw = (int)rank * KR_WARPS + warp;
+  const int n_it = (nf + STEP - 1) / STEP;
+  // ------------------------------------------------ pages
+  {
+    const int32_t* tab = c.page_table + (size_t)b * c.max_pages;
+    auto page_of = [&](int it) {
+      const int key = it * STEP + grp * KU;
+      int id = key < nf ? tab[key / ps] : 0;
+      if (id < 0 || id >= c.n_pages) {
+        jk_set_status(status, JK_ERR_BOUNDS);
+        id = 0;
+      }
+      return id;
+    };
+    int next = gw < n_it ? page_of(gw) : 0;
+    for (int it = gw; it < n_it; it += W) {
+      const int key = it * STEP + grp * KU, id = next;
+      const bool live = key < nf;
+      const size_t blk = ((size_t)layer * c.n_pages + id) * Hkv + h;
+      const size_t at = (blk * ps + (key & (ps - 1))) * D + x0;
+      uint4 kw[KU], vw[KU];
+#pragma unroll
+      for (int u = 0; u < KU; ++u) kw[u] = kr_load((const uint8_t*)c.k_pages + at + (size_t)u * D);
+#pragma unroll
+      for (int u = 0; u < KU; ++u) vw[u] = kr_load((const uint8_t*)c.v_pages + at + (size_t)u * D);
+      const float sk = live ? c.k_scale[blk] : 0.f, sv = live ? c.v_scale[blk] : 0.f;
+      if (it + W < n_it) next = page_of(it + W);
+      float s[KU][R];
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        float k[16];
+        kr_widen(kw[u], k);
+        dot(k, s[u]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[u][r] = live ? s[u][r] * sk : -INFINITY;
+      }
+      take(s, [&](int u, float* v) {
+        kr_widen(vw[u], v);
+        return sv;
+      });
+    }
+  }
+  // ------------------------------------------------ the open page's tokens, the tree
+  {
+    const size_t open_off = (((size_t)layer * c.max_seqs + b) * Hkv + h) * 2 * ps * D + x0;
+    const size_t tree_off = (size_t)b * tsb + (size_t)h * tsh + x0;
+    const int turn = (gw + W - n_it % W) % W;            // the turns go on where the pages' end
+    for (int it = turn; it * STEP < tail; it += W) {
+      const int e0 = it * STEP + grp * KU;
+      float s[KU][R];
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int e = e0 + u, node = e - n_open;
+        float k[16];
+#pragma unroll
+        for (int x = 0; x < 16; ++x) k[x] = 0.f;
+        if (e < n_open) paged_load16((const T*)c.k_open + open_off + (size_t)((nf + e) & (2 * ps - 1)) * D, k);
+        else if (e < tail) paged_load16(k_tree + tree_off + (size_t)node * D, k);
+        dot(k, s[u]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const bool seen = e < n_open || (e < tail && ((s_anc[r][(node >> 5) & 3] >> (node & 31)) & 1u));
+          if (!seen) s[u][r] = -INFINITY;
+        }
+      }
+      take(s, [&](int u, float* o) {
+        const int e = e0 + u;
+        float v[16];
+#pragma unroll
+        for (int x = 0; x < 16; ++x) v[x] = 0.f;
+        if (e < n_open) paged_load16((const T*)c.v_open + open_off + (size_t)((nf + e) & (2 * ps - 1)) * D, v);
+        else if (e < tail) paged_load16(v_tree + tree_off + (size_t)(e - n_open) * D, v);
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[x] = v[x];
+        return 1.f;
+      });
+    }
+  }
+  // ------------------------------------------------ groups of a warp, warps of a block, blocks of the cluster
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float top = m[r];
+#pragma unroll
+    for (int o = LPK; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float corr = m[r] == -INFINITY ? 0.f : exp2f(m[r] - top);
+    l[r] *= corr;
+#pragma unroll
+    for (int o = LPK; o < 32; o <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      acc[r][x] *= corr;
+#pragma unroll
+      for (int o = LPK; o < 32; o <<= 1) acc[r][x] += __shfl_xor_sync(0xffffffffu, acc[r][x], o);
+    }
+    if (grp == 0) {
+#pragma unroll
+      for (int x = 0; x < 16; x += 4)
+        *reinterpret_cast<float4*>(&s_o[warp][r][x0 + x]) = make_float4(acc[r][x], acc[r][x + 1], acc[r][x + 2], acc[r][x + 3]);
+    }
+    if (lane == 0) { s_m[warp][r] = top; s_l[warp][r] = l[r]; }
+  }
+  __syncthreads();
+  for (int i = tid; i < R * D; i += KR_THREADS) {
+    const int r = i / D, x = i % D;
+    float top = -INFINITY, sum = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < KR_WARPS; ++w) top = fmaxf(top, s_m[w][r]);
+#pragma unroll
+    for (int w = 0; w < KR_WARPS; ++w) {
+      const float f = s_m[w][r] == -INFINITY ? 0.f : exp2f(s_m[w][r] - top);
+      sum = fmaf(f, s_l[w][r], sum);
+      o = fmaf(f, s_o[w][r][x], o);
+    }
+    c_o[r][x] = o;
+    if (x == 0) { c_m[r] = top; c_l[r] = sum; }
+  }
+  sync();
+  if (rank == 0) {
+    for (int i = tid; i < R * D; i += KR_THREADS) {
+      const int r = i / D, x = i % D, row = row0 + r;
+      float pm[KR_CLUSTER], pl[KR_CLUSTER], po[KR_CLUSTER], top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < KR_CLUSTER; ++k) {
+        pm[k] = -INFINITY;
+        pl[k] = po[k] = 0.f;
+        if (k < C) {
+          pm[k] = *jk_cluster_map(&c_m[r], k);
+          pl[k] = *jk_cluster_map(&c_l[r], k);
+          po[k] = *jk_cluster_map(&c_o[r][x], k);
+        }
+        top = fmaxf(top, pm[k]);
+      }
+      float sum = 0.f, o = 0.f;
+#pragma unroll
+      for (int k = 0; k < KR_CLUSTER; ++k) {
+        const float f = pm[k] == -INFINITY ? 0.f : exp2f(pm[k] - top);
+        sum = fmaf(f, pl[k], sum);
+        o = fmaf(f, po[k], o);
+      }
+      if (row < n_rows) {
+        const int g = row / M, n = row % M;
+        out[(((size_t)b * M + n) * Hq + h * G + g) * D + x] = jk_from_float<T>(o / sum);
+      }
+    }
+  }
+  sync();                                                // the blocks' sums are read until here
+}
+
+template <typename T, int D, int R>
+static int kr_launch(jk_ctx* ctx, cudaStream_t st, const jk_paged* c, int layer, int B, int M, const void* q,
+                     const void* kt, const void* vt, int64_t sb, int64_t sh, const int32_t* parent, float scale,
+                     void* out) {
+  const jk_config& g = ctx->cfg;
+  const int n_rb = (g.n_q_heads / g.n_kv_heads * M + R - 1) / R;
+  const int64_t base = (int64_t)n_rb * g.n_kv_heads * B;
+  const int64_t keys = (int64_t)c->max_pages * c->page_size;
+  // one wave of two blocks per SM, 128 keys a block at least: 4 sequences of 2048 with the 7B heads 17.7 us, with
+  // two waves 23, with four 34; 8 blocks for 1024 keys 7.6 us, 4 blocks 8.9
+  int C = KR_CLUSTER;
+  while (C > 1 && (base * C > 2ll * ctx->sm_count || keys / C < 128)) C >>= 1;
+  JK_PROF(ctx, st, JK_ST_PAGED_ATTN);
+  jk_launch_pdl_cluster(k_paged_attn_rows<T, D, R>, dim3((unsigned)(n_rb * C), g.n_kv_heads, B), dim3(KR_THREADS),
+                        (unsigned)C, 0, st, *c, layer, (const T*)q, (const T*)kt, (const T*)vt, (long long)sb,
+                        (long long)sh, parent, scale, M, g.n_q_heads, g.n_kv_heads, C, (T*)out,
+                        (int32_t*)(ctx->ws + ctx->lay.status));
+  JK_LAUNCH_CHECK(ctx);
+  return JK_OK;
+}
+
 int jk_attn_combine_launch(jk_ctx* ctx, cudaStream_t st, int n_split, size_t n_out, void* out);
 
 template <typename T, int D>
@@ -222,7 +520,30 @@ extern "C" int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_pag
   if ((tree_stride_b * es) % 16 || (tree_stride_h * es) % 16) return JK_ERR_ALIGN;
   if ((rc = jk_ensure_device_info(ctx)) != JK_OK) return rc;
   cudaStream_t st = (cudaStream_t)stream;
-  if (g.dtype == JK_BF16 && ctx->tensor_path)
+  const int rows = g.n_q_heads / g.n_kv_heads * tree_size;
+#define KR_CASE(T, D, R)                                                                           \
+  return kr_launch<T, D, R>(ctx, st, c, layer, batch, tree_size, q, k_tree, v_tree, tree_stride_b, \
+                            tree_stride_h, parent, softmax_scale, out)
+#define KR_ROWS(T, D)                                                                              \
+  do {                                                                                             \
+    if (rows == 1) KR_CASE(T, D, 1);                                                               \
+    KR_CASE(T, D, 4);                                                                              \
+  } while (0)
+  // One query row per kv head (single tokens without grouped heads): the CUDA cores keep up with the pages, 7B heads,
+  // prefix 1024 7.6 us (tensor cores 16.8), 13B heads, batch 16, prefix 4096 122 (141).  Two rows at prefix 8192, batch
+  // 16: 109, tensor cores 58.  In fp32, 16 rows over 4096 keys, batch 4: 98, by tiles of 64 rows 175; 60 rows: the tiles.
+  const bool tensor = g.dtype == JK_BF16 && ctx->tensor_path;
+  if (rows <= (tensor ? 1 : KR_MAX_ROWS)) {
+    if (g.dtype == JK_BF16) {
+      if (g.head_dim == 128) KR_ROWS(__nv_bfloat16, 128);
+      KR_ROWS(__nv_bfloat16, 64);
+    }
+    if (g.head_dim == 128) KR_ROWS(float, 128);
+    KR_ROWS(float, 64);
+  }
+#undef KR_ROWS
+#undef KR_CASE
+  if (tensor)
     return jk_paged_attn_tc(ctx, st, c, layer, batch, tree_size, q, k_tree, v_tree, tree_stride_b, tree_stride_h,
                             parent, softmax_scale, out);
 #define KA_CASE(T, D)                                                                              \

@@ -84,12 +84,6 @@ __device__ __forceinline__ uint32_t smp_rank() {
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-// a generic address of the same variable in block `rank` of the cluster
-template <typename P> __device__ __forceinline__ P* smp_map(P* p, uint32_t rank) {
-  u64 a;
-  asm("mapa.u64 %0, %1, %2;" : "=l"(a) : "l"((u64)p), "r"(rank));
-  return reinterpret_cast<P*>(a);
-}
 
 // Weights: exp((z - zmax) / T) in units of 2^-sh.  2^(n / 16) from a table, the rest (at most ln2 / 32) by the power
 // series to the sixth term: 5e-16 off, next to the 4e-15 of the reduced argument.
@@ -202,7 +196,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
   smp_shared& S = *reinterpret_cast<smp_shared*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / C, rank = C > 1 ? (int)smp_rank() : 0;
-  smp_shared* S0 = C > 1 ? smp_map(&S, 0) : &S;          // the first block's
+  smp_shared* S0 = C > 1 ? jk_cluster_map(&S, 0) : &S;          // the first block's
   auto sync = [&]() {
     if (C > 1) {
       asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -216,7 +210,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
     if (C > 1) {
       constexpr int WORDS = sizeof(smp_state) / 4;
       for (int i = tid; i < (C - 1) * WORDS; i += SMP_THREADS)
-        reinterpret_cast<uint32_t*>(&smp_map(&S, 1 + i / WORDS)->st)[i % WORDS] = reinterpret_cast<const uint32_t*>(&S.st)[i % WORDS];
+        reinterpret_cast<uint32_t*>(&jk_cluster_map(&S, 1 + i / WORDS)->st)[i % WORDS] = reinterpret_cast<const uint32_t*>(&S.st)[i % WORDS];
     }
   };
   for (int i = tid; i < SMP_BINS / 4; i += SMP_THREADS) {
@@ -289,7 +283,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
   }
   sync();
   uint32_t kmax = 0u;
-  for (int i = 0; i < C; ++i) kmax = max(kmax, C > 1 ? smp_map(&S.kmax, i)[0] : S.kmax);
+  for (int i = 0; i < C; ++i) kmax = max(kmax, C > 1 ? jk_cluster_map(&S.kmax, i)[0] : S.kmax);
   auto fill = [&](int keep_index, float value) {         // one token, or none
     if (!out) return;
     each([&](int v, const float (&)[VEC]) {
@@ -461,7 +455,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
           uint32_t n[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
           for (int i = 0; i < SMP_CLUSTER; ++i) {
-            const uint4 c = reinterpret_cast<const uint4*>(smp_map(&S, i < C ? i : 0)->cnt)[q];
+            const uint4 c = reinterpret_cast<const uint4*>(jk_cluster_map(&S, i < C ? i : 0)->cnt)[q];
             if (i < C) { n[0] += c.x; n[1] += c.y; n[2] += c.z; n[3] += c.w; }
           }
           reinterpret_cast<uint4*>(S0->cnt)[q] = make_uint4(n[0], n[1], n[2], n[3]);
@@ -471,7 +465,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
             u64 m[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
             for (int i = 0; i < SMP_CLUSTER; ++i) {
-              const smp_shared* o = smp_map(&S, i < C ? i : 0);
+              const smp_shared* o = jk_cluster_map(&S, i < C ? i : 0);
               const uint4 l = reinterpret_cast<const uint4*>(o->lo)[q], h = reinterpret_cast<const uint4*>(o->hi)[q];
               if (i < C) {
                 m[0] += (u64)h.x << 32 | l.x; m[1] += (u64)h.y << 32 | l.y;
