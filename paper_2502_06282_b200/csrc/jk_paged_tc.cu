@@ -984,77 +984,105 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
 }
 
 // ------------------------------------------------------------------------------------------ merge
-// out = sum_s 2^(m_s - m) acc_s / sum_s 2^(m_s - m) l_s over the partials of a unit that spans CTAs; one warp
-// per query row.  CTA s holds tiles [total s / G, total (s + 1) / G), so which CTAs hold a unit's tiles, and
-// under which of its two slots, follows from the tile counts alone.
-template <int D, int NR>
+// out = sum_s 2^(m_s - m) acc_s / sum_s 2^(m_s - m) l_s over the partials of a unit that spans CTAs.  CTA s holds
+// tiles [total s / G, total (s + 1) / G), so which CTAs hold a unit's tiles, and under which of its two
+// slots, follows from the tile counts alone.  A warp takes RPW rows with all their loads under way together: one
+// where the rows are few (7B heads, prefix 1024: 5 us against 7 with four), four where each block's search for
+// the unit's CTAs would be for few rows (13B heads, batch 8: 10 us against 13 with one).
+template <int D, int NR, int RPW>
 __global__ void __launch_bounds__(256) k_paged_merge(const jk_paged c, int B, int M, int Hq, int Hkv, int n_qblk,
                                                      int grid, const float* __restrict__ part_o,
                                                      const float* __restrict__ part_ml, __nv_bfloat16* __restrict__ out) {
   __shared__ long long cum[JK_MAX_ROWS + 1];
   __shared__ int n8[JK_MAX_ROWS];
-  constexpr int DPL = D / 32, NB = 8;
+  __shared__ int s_c[2];
+  constexpr int DPL = D / 32, RB = 8 * RPW, NB = RPW == 1 ? 8 : 4;
+  static_assert(NR % RB == 0, "a block's rows are of one unit");
   jk_pdl_wait();
   jk_pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int units = Hkv * n_qblk, G = Hq / Hkv;
-  if (warp == 0) pt_count(c, B, M, units, lane, cum, n8, nullptr, nullptr);
+  const int unit = blockIdx.x / (NR / RB), r0 = (blockIdx.x % (NR / RB)) * RB + warp * RPW;
+  const int b = unit / units, u = unit % units;
+  if (warp == 0) {
+    pt_count(c, B, M, units, lane, cum, n8, nullptr, nullptr);
+    __syncwarp();
+    if (lane < 2) {
+      const long long total = cum[B], per = (cum[b + 1] - cum[b]) / units;
+      const long long a = cum[b] + (long long)u * per;
+      const long long ctas = total < grid ? total : grid;
+      s_c[lane] = per == 0 ? 0 : (int)(((lane == 0 ? a + 1 : a + per) * ctas - 1) / total);
+    }
+  }
   __syncthreads();
-  const int64_t row = (int64_t)blockIdx.x * 8 + warp;
-  const int64_t unit = row / NR;
-  const int r = (int)(row % NR);
-  const int b = (int)(unit / units), u = (int)(unit % units);
-  if (b >= B) return;
-  const int nr = (u % n_qblk) * NR + r;
-  if (nr >= G * M) return;
-  const long long total = cum[B], per = (cum[b + 1] - cum[b]) / units;
-  if (per == 0) return;
-  const long long a = cum[b] + (long long)u * per;
-  const long long ctas = total < grid ? total : grid;
-  const int c0 = (int)(((a + 1) * ctas - 1) / total), c1 = (int)(((a + per) * ctas - 1) / total);
-  if (c0 == c1) return;                                 // one CTA held it all and has written it
+  const int c0 = s_c[0], c1 = s_c[1];
+  if (c0 == c1) return;                                 // one CTA held it all and has written it (or there is nothing)
+  const int live = min(RPW, G * M - ((u % n_qblk) * NR + r0));   // rows of this warp
+  if (live <= 0) return;
   // slot of CTA s: its last segment where the unit begins, its first everywhere else
-  float m = -INFINITY;
+  auto slot = [&](int s, int r) { return (size_t)(s * 2 + (s == c0 ? 1 : 0)) * NR + r; };
+  float m[RPW], l[RPW], acc[RPW][DPL];
+#pragma unroll
+  for (int q = 0; q < RPW; ++q) {
+    m[q] = -INFINITY;
+    l[q] = 0.f;
+#pragma unroll
+    for (int t = 0; t < DPL; ++t) acc[q][t] = 0.f;
+  }
   for (int s0 = c0; s0 <= c1; s0 += 32) {
-    const int s = s0 + lane;
-    if (s <= c1) m = fmaxf(m, part_ml[((size_t)(s * 2 + (s == c0 ? 1 : 0)) * NR + r) * 2]);
+#pragma unroll
+    for (int q = 0; q < RPW; ++q)
+      if (s0 + lane <= c1 && q < live) m[q] = fmaxf(m[q], part_ml[slot(s0 + lane, r0 + q) * 2]);
   }
-  m = jk_warp_max(m);
-  float acc[DPL], l = 0.f;
 #pragma unroll
-  for (int t = 0; t < DPL; ++t) acc[t] = 0.f;
-  for (int s0 = c0; s0 <= c1; s0 += NB) {
-    float v[NB][DPL];
-    float2 ml[NB];
+  for (int q = 0; q < RPW; ++q) m[q] = jk_warp_max(m[q]);
+  for (int s0 = c0; s0 <= c1; s0 += 32) {
+    float w[RPW];                                       // of slot s0 + lane
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const int s = s0 + j;
-      ml[j] = make_float2(-INFINITY, 0.f);
-      if (s > c1) continue;
-      const size_t at = (size_t)(s * 2 + (s == c0 ? 1 : 0)) * NR + r;
-      ml[j] = *reinterpret_cast<const float2*>(part_ml + at * 2);
-      if (DPL == 4) {
-        const float4 x = *reinterpret_cast<const float4*>(part_o + at * D + lane * DPL);
-        v[j][0] = x.x; v[j][1] = x.y; v[j][DPL - 2] = x.z; v[j][DPL - 1] = x.w;
-      } else {
-        const float2 x = *reinterpret_cast<const float2*>(part_o + at * D + lane * DPL);
-        v[j][0] = x.x; v[j][DPL - 1] = x.y;
-      }
+    for (int q = 0; q < RPW; ++q) {
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (s0 + lane <= c1 && q < live) ml = *reinterpret_cast<const float2*>(part_ml + slot(s0 + lane, r0 + q) * 2);
+      w[q] = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m[q]);
+      l[q] += w[q] == 0.f ? 0.f : w[q] * ml.y;
     }
+    const int n = min(32, c1 - s0 + 1);
+    for (int j0 = 0; j0 < n; j0 += NB) {
+      float4 v[NB][RPW];
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      if (s0 + j > c1 || ml[j].x == -INFINITY) continue;
-      const float w = fast_exp2(ml[j].x - m);
-      l = fmaf(w, ml[j].y, l);
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int t = 0; t < DPL; ++t) acc[t] = fmaf(w, v[j][t], acc[t]);
+        for (int q = 0; q < RPW; ++q)
+          if (j0 + j < n && q < live) {
+            const float* p = part_o + slot(s0 + j0 + j, r0 + q) * D + lane * DPL;
+            if (DPL == 4) {
+              v[j][q] = *reinterpret_cast<const float4*>(p);
+            } else {
+              const float2 x = *reinterpret_cast<const float2*>(p);
+              v[j][q] = make_float4(x.x, x.y, 0.f, 0.f);
+            }
+          }
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int q = 0; q < RPW; ++q) {
+          const float wj = __shfl_sync(0xffffffffu, w[q], (j0 + j) & 31);
+          if (j0 + j >= n || q >= live || wj == 0.f) continue;
+          const float x[4] = {v[j][q].x, v[j][q].y, v[j][q].z, v[j][q].w};
+#pragma unroll
+          for (int t = 0; t < DPL; ++t) acc[q][t] = fmaf(wj, x[t], acc[q][t]);
+        }
     }
   }
-  const float inv = 1.f / l;
-  const int gg = nr / M, ii = nr % M;
-  __nv_bfloat16* o = out + (((size_t)b * M + ii) * Hq + (u / n_qblk) * G + gg) * D + lane * DPL;
 #pragma unroll
-  for (int t = 0; t < DPL; ++t) o[t] = __float2bfloat16_rn(acc[t] * inv);
+  for (int q = 0; q < RPW; ++q) {
+    const float inv = 1.f / jk_warp_sum(l[q]);
+    if (q >= live) continue;
+    const int nr = (u % n_qblk) * NR + r0 + q, gg = nr / M, ii = nr % M;
+    __nv_bfloat162* o = reinterpret_cast<__nv_bfloat162*>(
+        out + (((size_t)b * M + ii) * Hq + (u / n_qblk) * G + gg) * D + lane * DPL);
+#pragma unroll
+    for (int t = 0; t < DPL / 2; ++t) o[t] = __floats2bfloat162_rn(acc[q][2 * t] * inv, acc[q][2 * t + 1] * inv);
+  }
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -1099,9 +1127,12 @@ static int pt_launch(jk_ctx* ctx, cudaStream_t st, const CUtensorMap* maps, cons
   JK_LAUNCH_CHECK(ctx);
   if (ctas == 1) return JK_OK;
   JK_PROF(ctx, st, JK_ST_PAGED_COMBINE);
-  jk_launch_pdl(k_paged_merge<D, NR>, dim3((unsigned)((int64_t)B * units * NR / 8)), dim3(256), 0, st, *c, B, M,
-                g.n_q_heads, g.n_kv_heads, n_qblk, ctas, (const float*)part_o, (const float*)part_ml,
-                (__nv_bfloat16*)out);
+  const int64_t m_rows = (int64_t)B * units * NR;
+  constexpr int WIDE = NR == 16 ? 2 : 4;
+  const bool few = m_rows / 8 <= 4ll * ctx->sm_count;
+  auto merge = few ? k_paged_merge<D, NR, 1> : k_paged_merge<D, NR, WIDE>;
+  jk_launch_pdl(merge, dim3((unsigned)(m_rows / (few ? 8 : 8 * WIDE))), dim3(256), 0, st, *c, B, M, g.n_q_heads,
+                g.n_kv_heads, n_qblk, ctas, (const float*)part_o, (const float*)part_ml, (__nv_bfloat16*)out);
   JK_LAUNCH_CHECK(ctx);
   return JK_OK;
 }
