@@ -329,11 +329,12 @@ def test_copy_between_pools_and_inside_one():
 # attention
 # ------------------------------------------------------------------------------------------
 def bound(out, size, dtype):
-    """How far an element may be off.  bf16: the result is rounded once (2^-8 of it) and every softmax weight once
-    to 8 significant bits (2^-8 of sum p|v|); 2^-10 of that sum covers the rest: weights below 2^-18 of their
-    tile's largest that become 0 (at most 127 in a tile: 2^-11), fp32 products over 128 elements (logits off by
-    under 128 2^-24 sum|q k| scale = 2^-14 for these inputs) and the exponential (2^-22).  f32: the products'
-    2^-14 and as much for sums and the fast exponential."""
+    """How far an element may be off.  bf16: the result is rounded once (2^-8 of it) and every softmax weight once:
+    to bf16 over open and tree rows (2^-8 of sum p|v|), to fp16 over pages (2^-11); 2^-10 of that sum covers the rest:
+    weights below 2^-31 of their row's reference that become 0 (2^-14 for 2^17 keys), fp32 products over 128
+    elements (logits off by under 128 2^-24 sum|q k| scale = 2^-14 for these inputs) and the exponential (2^-22).
+    f32, and one query row per kv head in bf16 (which rounds its result alone): the products' 2^-14 and as much for sums
+    and the fast exponential."""
     if dtype == "bf16":
         return 2.0 ** -8 * np.abs(out) + (2.0 ** -8 + 2.0 ** -10) * size + 1e-30
     return 2.0 ** -13 * size + 1e-30
@@ -413,6 +414,34 @@ def test_attention(case, path):
     a = check_attention(*parts)
     b = check_attention(*parts)
     assert torch.equal(a, b)                            # the same bits again
+
+
+MORE = [
+    # one query row per kv head: one to eight blocks of a cluster, runs that end inside a warp's step
+    ("bf16", 16, 64, 3, 3, 1, [2049, 0, 127, 1024]),
+    ("bf16", 64, 128, 1, 1, 1, [9000]),
+    ("bf16", 128, 128, 40, 40, 1, [129] * 9),
+    ("f32", 32, 64, 2, 2, 1, [4100, 3]),
+    # few rows in fp32, and the first count that is not few
+    ("f32", 32, 128, 4, 4, 4, [1500, 31]),
+    ("f32", 16, 64, 8, 2, 4, [700, 3, 0]),
+    ("f32", 64, 128, 1, 1, 17, [300]),
+    # many units, so that partials are merged several rows per warp, in blocks of 16, 32 and 64 rows
+    ("bf16", 16, 128, 16, 16, 9, [40, 7, 64, 0, 33] * 4),
+    ("bf16", 16, 128, 16, 16, 20, [100, 16, 0, 47, 200, 31, 5, 64, 80, 1]),
+    ("bf16", 32, 128, 10, 5, 60, [300, 17, 0, 129, 500, 64, 33, 200]),
+    ("bf16", 32, 64, 10, 5, 60, [300, 17, 0, 129, 500, 64, 33, 200]),
+    # a single unit over every CTA
+    ("bf16", 64, 128, 1, 1, 5, [20000]),
+]
+
+
+@pytest.mark.parametrize("case", range(len(MORE)))
+def test_attention_of_few_rows_and_of_many_units(case):
+    parts = attention_case(*MORE[case], seed=200 + case)
+    a = check_attention(*parts)
+    b = check_attention(*parts)
+    assert torch.equal(a, b)
 
 
 def test_attention_with_a_sink_token_keeps_the_tail():
