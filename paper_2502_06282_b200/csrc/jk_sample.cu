@@ -5,7 +5,7 @@
 // is a prefix of (logit descending, index ascending), so the kept set is a threshold on the image plus a number of
 // tokens equal to the threshold, lowest index first.  Both thresholds (by count for top-k, by weight for top-p) are
 // found in a histogram of the row:
-//   - a bin is the upper half of the image (sign, exponent, 7 bits), over the 20 octaves that hold the largest
+//   - a bin is the upper half of the image (sign, exponent, 7 bits), over the 18 octaves that hold the largest
 //     magnitude with a weight; what is nearer to zero falls into two bins of its own, zero into one, what weighs
 //     nothing into a last one;
 //   - the bin that holds the threshold is resolved exactly: if it has one value (every bf16 bin) there is nothing
@@ -19,11 +19,11 @@
 //
 // A row belongs to a cluster of 1 to 8 blocks; histograms are added up in its first block's shared memory.
 //
-// Measured (B200, graph replay, inputs in L2 or behind it as they come): one row of 32000 in fp32 with top-k 50 and
-// top-p 12.7 us, of which a pass over the row takes 1 us and each of the cluster's barriers 0.7; 240 rows of
-// 128256 in bf16 (62 MB in, 123 MB out: 29 us of HBM time) with top-p, min-p, draw and filtered rows 118 us: largest
-// logit 15, histogram 40 (bound by its shared-memory atomics), scan of the bins 7, output and draw 45; some SMs hold two
-// rows, others one.
+// Measured (B200, graph replay): one row of 32000 in fp32 with top-k 50 and top-p 12.6 us, of which a pass over the row
+// takes 1 us and each of the cluster's barriers 0.7; 240 rows of 128256 in bf16 (62 MB in, 123 MB out: 29 us of
+// HBM time) with top-p, min-p, draw and filtered rows 109 us: largest logit 10, histogram 33 (bound by its
+// shared-memory atomics, 8 cycles for a warp's), scan of the bins 8, output and weights 32, search for the token
+// 7; some SMs hold two rows, others one.
 #include <math.h>
 
 #include "jk_common.cuh"
@@ -32,8 +32,8 @@
 #define SMP_WARPS (SMP_THREADS / 32)
 #define SMP_CLUSTER 8
 #define SMP_LIST 256                  // candidates that are compared with one another
-#define SMP_OCTAVES 20
-#define SMP_BINS 5632                 // >= 2 * 128 * SMP_OCTAVES + 4, a multiple of SMP_THREADS
+#define SMP_OCTAVES 18
+#define SMP_BINS 5120                 // >= 2 * 128 * SMP_OCTAVES + 4, a multiple of SMP_THREADS
 #define SMP_LEVEL 4096                // bins of a histogram of images
 #define SMP_NOTHING 0x007fffffu       // the image of -inf
 #define SMP_BIG 3.402823466e38f
@@ -492,12 +492,14 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
         };
         if (by_weight) {
           // (bins by turns: the ones that hold anything stand together)
-          for (int b = tid; b < nb; b += SMP_THREADS) {
-            const uint32_t c = S.cnt[b];
-            if (c && (level == 0 ? map.single(b) : shift == 0)) {
-              uint32_t lo, hi;
-              range(b, lo, hi);
-              const u64 w = (u64)c * weight(smp_value(lo));
+          // (fp32 has one such bin there, that of zero)
+          const bool one = sizeof(T) == 4 && level == 0;
+#pragma unroll 2
+          for (int b = one ? map.np + 1 + (tid ? nb : 0) : tid; b < nb; b += SMP_THREADS) {
+            uint32_t lo, hi;
+            range(b, lo, hi);
+            const u64 w = (u64)S.cnt[b] * weight(smp_value(lo));
+            if (level == 0 ? map.single(b) : shift == 0) {
               S.lo[b] = (uint32_t)w;
               S.hi[b] = (uint32_t)(w >> 32);
             }
@@ -763,45 +765,55 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
       sync();
       tie = S0->weq[gw];
     }
-    // f(vector or -1, values, kept): the whole warp over vectors [v_begin, v_end), in index order, with t tokens equal to
-    // the threshold in front of them
-    auto kept_each = [&](int v_begin, int v_end, int t, auto f) {
-      for (int v4 = v_begin + lane; v4 - lane < v_end; v4 += 128) {
-        uint32_t raw[4][RAW] = {};
+    // The kept tokens of vector v (none where !in), t: tokens equal to the threshold in front of the warp's vectors
+    auto kept_of = [&](bool in, const float (&z)[VEC], int& t) {
+      uint32_t keep = 0u;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (v4 + 32 * q < v_end) load(v4 + 32 * q, raw[q]);
+      for (int i = 0; i < VEC; ++i) keep |= z[i] >= zt ? 1u << i : 0u;
+      if (!in) keep = 0u;
+      if (some) {
+        uint32_t same = 0u;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) same |= fminf(z[i], SMP_BIG) == zt ? 1u << i : 0u;
+        same &= keep;
+        if (__any_sync(0xffffffffu, same != 0u)) {
+          int x = __popc(same);
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+          }
+          int at = t + x - __popc(same);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i)
+            if ((same >> i) & 1u) { if (at >= ties) keep &= ~(1u << i); ++at; }
+          t += __shfl_sync(0xffffffffu, x, 31);
+        }
+      }
+      return keep;
+    };
+    // f(vector, values, kept) for vectors [va, vb), in index order; the whole warp takes part
+    auto kept_each = [&](int va, int vb, int t, auto f) {
+      int v = va + lane;
+      for (; v - lane + 128 <= vb; v += 128) {
+        uint32_t raw[4][RAW];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load(v + 32 * q, raw[q]);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int v = v4 + 32 * q;
-          if (v - lane >= v_end) break;
           float z[VEC];
           smp_unpack<T, VEC>(raw[q], z);
-          uint32_t keep = 0u;
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) keep |= z[i] >= zt ? 1u << i : 0u;
-          if (v >= v_end) keep = 0u;
-          if (some) {
-            uint32_t same = 0u;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) same |= fminf(z[i], SMP_BIG) == zt ? 1u << i : 0u;
-            same &= keep;
-            if (__any_sync(0xffffffffu, same != 0u)) {
-              int x = __popc(same);
-#pragma unroll
-              for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-              }
-              int at = t + x - __popc(same);
-#pragma unroll
-              for (int i = 0; i < VEC; ++i)
-                if ((same >> i) & 1u) { if (at >= ties) keep &= ~(1u << i); ++at; }
-              t += __shfl_sync(0xffffffffu, x, 31);
-            }
-          }
-          if (!f(v < v_end ? v : -1, z, keep)) return;
+          const uint32_t keep = kept_of(true, z, t);
+          f(v + 32 * q, z, keep);
         }
+      }
+      for (; v - lane < vb; v += 32) {
+        uint32_t raw[RAW] = {};
+        if (v < vb) load(v, raw);
+        float z[VEC];
+        smp_unpack<T, VEC>(raw, z);
+        const uint32_t keep = kept_of(v < vb, z, t);
+        if (v < vb) f(v, z, keep);
       }
     };
     auto write = [&](int v, const float (&z)[VEC], uint32_t keep) {
@@ -812,13 +824,18 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
       if constexpr (VEC == 4) __stcs(reinterpret_cast<float4*>(out) + v, make_float4(o[0], o[1], o[2], o[3]));
       else __stcs(out + v, o[0]);
     };
+    auto write_nothing = [&](int v) {
+      if constexpr (VEC == 4) __stcs(reinterpret_cast<float4*>(out) + v, make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY));
+      else __stcs(out + v, -INFINITY);
+    };
     if (!draw && !some) {
       each([&](int v, const float (&z)[VEC]) {
         uint32_t keep = 0u;
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
           if (z[i] >= zt) keep |= 1u << i;
-        write(v, z, keep);
+        if (keep) write(v, z, keep);
+        else write_nothing(v);
       });
     } else {
       // Weights of kept tokens.  bf16 takes them from a table by bin; fp32 forms those of a vector together, whether or
@@ -844,7 +861,11 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
       for (int round = 0; round < 2; ++round) {
         u64 sum = 0ull;
         kept_each(v0, v1, tie, [&](int v, const float (&z)[VEC], uint32_t keep) {
-          if (v >= 0 && out && round == 0) write(v, z, keep);
+          if (out && round == 0) {
+            if (keep) write(v, z, keep);
+            else write_nothing(v);
+          }
+          if (!keep) return;
           if (by_bin) {
             const int np3 = map.np + 3 - (int)map.mn, mb = (int)map.mb, mz = (int)map.mz;
             uint32_t odd = 0u;
@@ -860,14 +881,13 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
               for (int i = 0; i < VEC; ++i)
                 if ((odd >> i) & 1u) sum += weight(fminf(z[i], SMP_BIG));
             }
-          } else if (draw && __any_sync(0xffffffffu, keep != 0u)) {
+          } else if (draw) {
             u64 w[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) w[i] = weight(fminf(z[i], SMP_BIG));
 #pragma unroll
             for (int i = 0; i < VEC; ++i) sum += (keep >> i) & 1u ? w[i] : 0ull;
           }
-          return true;
         });
         if (!draw) break;
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -935,7 +955,13 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
           u64 run = S.st.win_before;
           for (int i = 0; i < warp; ++i) run += S.red[i];
           if ((long long)run <= goal && (long long)(run + sum) > goal) {
-            kept_each(v0, v1, tie, [&](int v, const float (&z)[VEC], uint32_t keep) {
+            int t = tie;
+            for (int v = v0 + lane; v - lane < v1; v += 32) {
+              uint32_t raw[RAW] = {};
+              if (v < v1) load(v, raw);
+              float z[VEC];
+              smp_unpack<T, VEC>(raw, z);
+              const uint32_t keep = kept_of(v < v1, z, t);
               u64 w[VEC], x = 0ull;
 #pragma unroll
               for (int i = 0; i < VEC; ++i) {
@@ -960,11 +986,10 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
                   }
                   out_tok[r] = tok;
                 }
-                return false;
+                break;
               }
               run += __shfl_sync(0xffffffffu, x, 31);
-              return true;
-            });
+            }
           }
         }
       }
