@@ -13,6 +13,11 @@
  *   jk_accept_and_compact  acceptance walk, bonus token and KV-cache compaction
  *                          (Sec. 2.1 steps 2-3)
  *
+ * and, for a server around it:
+ *
+ *   jk_tree_verify_attn_paged, jk_paged_*   the attention over a paged 8-bit cache, and its upkeep
+ *   jk_sample              temperature, top-k, top-p, min-p: the token, or the filtered target rows
+ *
  * Conventions that hold for every call
  *   - Returns 0 (JK_OK) or a negative jk_status.  Nothing throws or aborts.
  *   - Pointers named "host" are host memory; every other pointer is DEVICE memory on the
@@ -462,8 +467,10 @@ int jk_paged_import(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32
  *   k_tree, v_tree  T [B, Hkv, >= M, d] with the strides given (elements): this layer's keys and
  *            values of the tree tokens; they have to be finite
  * kv_len[b] < 0 or past max_pages * page_size, and a page id outside the pool, set JK_ERR_BOUNDS.
- * With bf16 and the tensor path, softmax weights are carried with 8 significant bits, sums in
- * fp32; otherwise everything in fp32.
+ * With bf16 and the tensor path, queries meet the pages' keys in two e4m3 parts (8 significant
+ * bits, as many as bf16 has) and softmax weights are rounded once, to fp16 over pages and to bf16
+ * over open and tree rows; sums are fp32.  One query row per kv head, fp32 contexts and the CUDA-core
+ * path carry everything in fp32.
  */
 int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t layer,
                             int32_t batch, int32_t tree_size, const void* q, const void* k_tree,
@@ -516,8 +523,9 @@ int jk_paged_copy(jk_ctx* ctx, void* stream, const jk_paged* host_src, const jk_
  * the draw of a next token, and the filtered target rows that jk_accept_and_compact (mode 1,
  * temperature 1) takes as target_logits.
  *   Tokens are ordered by (logit descending, index ascending).  Weights w = exp((z - z_max) / T) are
- *   formed and summed in 64 bits (a vocabulary of 1e5 has cumulative sums 1e-5 apart, where
- *   fp32 sums are off by 1e-6).  The kept set is the shortest of three prefixes of the order,
+ *   formed in double precision and summed as 64-bit fixed-point numbers, unit 2^-45 (2^(n-62) for
+ *   2^n > 2^17 tokens): a vocabulary of 1e5 has cumulative sums 1e-5 apart, where fp32 sums are off
+ *   by 1e-6.  The kept set is the shortest of three prefixes of the order,
  *   never empty:
  *     top_k > 0:    the first top_k tokens
  *     top_p < 1:    the tokens before which less than top_p of the weight of the first top_k lies

@@ -120,6 +120,38 @@ def test_import_takes_prompts_of_any_length(dtype, ps, d, Hkv):
     assert ctx.read_status() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_import_of_infinities_nan_and_tiny_values(dtype):
+    """The scale follows the finite values; infinities become the largest code, NaN stays NaN."""
+    rng = np.random.default_rng(6)
+    ps, d = 32, 64
+    ctx = make_ctx(2, 2, d, 1, 4, dtype)
+    p = Pair(ctx, 1, 8, ps, 1, 7)
+    big = float(np.finfo(np.float32).max) if dtype == "f32" else float(torch.finfo(torch.bfloat16).max)
+    src = []
+    for which in "kv":
+        x, _ = p.draw(rng, (1, 1, 2, 6 * ps, d))
+        x[0, 0, :, 3] = np.inf
+        x[0, 0, :, ps + 1, ::3] = -np.inf
+        x[0, 0, :, ps + 2, 5] = np.nan
+        x[0, 0, :, 2 * ps:3 * ps] = np.nan             # nothing finite in the block
+        x[0, 0, :, 3 * ps:4 * ps] *= np.float32(2.0 ** -40)
+        x[0, 0, :, 4 * ps, 0] = big
+        x[0, 0, :, 5 * ps:] = -0.0
+        x = synth.store_round(x, dtype)
+        src.append((x, dev(x, dtype)))
+    model, _ = do_import(p, rng, None, [6 * ps], 6 * ps, src=src)
+    model()
+    torch.cuda.synchronize()
+    p.guard.check()
+    for i, name in enumerate("kv"):
+        got, want = host(getattr(p.dev, name + "_pages"))[:, :6], p.ref.pages[i][:, :6]
+        nan = (want & 0x7F) == 0x7F
+        assert np.array_equal((got & 0x7F) == 0x7F, nan) and np.array_equal(got[~nan], want[~nan])
+        assert np.array_equal(host(getattr(p.dev, name + "_scale"))[:, :6], p.ref.scale[i][:, :6])
+    assert ctx.read_status() == 0
+
+
 def test_import_layer_by_layer_and_again():
     rng = np.random.default_rng(5)
     ctx = make_ctx(2, 2, 64, 2, 4, "bf16")

@@ -78,6 +78,20 @@ def test_many_rows_with_their_own_parameters(dtype):
         k=rng.integers(-1, 60, R), p=rng.uniform(0.1, 1.1, R), m=rng.uniform(-0.1, 0.2, R), u=rng.random(R))
 
 
+@pytest.mark.parametrize("R", [60, 130, 250])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_one_two_and_four_blocks(R, dtype):
+    """Enough rows that a row gets fewer blocks than the machine could give it."""
+    rng = np.random.default_rng(R)
+    V = 8300
+    ctx = make_ctx(V)
+    z = rows_of(rng, R, V, dtype)
+    z[::5] = np.round(z[::5])                           # ties
+    run(ctx, z, dtype, T=rng.uniform(0.4, 1.5, R), k=rng.integers(-1, 900, R), p=rng.uniform(0.3, 1.1, R),
+        m=rng.uniform(-0.1, 0.05, R), u=rng.random(R))
+    run(ctx, z, dtype, T=rng.uniform(0.4, 1.5, R), p=rng.uniform(0.6, 1.0, R), u=rng.random(R))
+
+
 @pytest.mark.parametrize("V", [257, 32000])
 def test_equal_logits(V):
     """Ties go to the lower index, whatever the filter cuts through them."""
@@ -149,6 +163,37 @@ def test_strides_alignment_and_missing_arguments():
         run(ctx, z, dtype, k=30, p=0.9, u=None)
         run(ctx, z, dtype, p=0.9, u=rng.random(4), filtered=False)
         run(ctx, z, dtype, u=rng.random(4), filtered=False)
+
+
+def test_replayed_from_a_graph_and_on_another_stream():
+    """A captured call reads its inputs anew; a call on a side stream gives the same bits."""
+    rng = np.random.default_rng(15)
+    V, R = 32000, 5
+    ctx = make_ctx(V)
+    z, u = rows_of(rng, R, V, "f32"), rng.random(R).astype(np.float32)
+    kw = dict(k=200, p=0.93, m=0.001)
+    tok, out = run(ctx, z, "f32", T=0.9, u=u, **kw)
+    f = lambda x, t: dev(np.full(R, x, t))
+    zd, ud, par = dev(z.astype(np.float32)), dev(u), (f(0.9, np.float32), f(200, np.int32), f(0.93, np.float32), f(0.001, np.float32))
+    tok2, out2 = torch.zeros_like(tok), torch.zeros_like(out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ctx.sample(zd, *par, ud, tok2, out2)
+    side.synchronize()
+    assert torch.equal(tok, tok2) and torch.equal(out, out2)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ctx.sample(zd, *par, ud, tok2, out2)
+    for seed in (16, 17):
+        z = rows_of(np.random.default_rng(seed), R, V, "f32")
+        zd.copy_(dev(z.astype(np.float32)))
+        g.replay()
+        torch.cuda.synchronize()
+        for r in range(R):
+            want, kept = pg.sample_row(z[r], np.float32(0.9).item(), 200, np.float32(0.93).item(), np.float32(0.001).item(), u[r].item())
+            assert int(tok2[r]) == want and np.array_equal(host(out2[r]) > -np.inf, kept)
+    assert ctx.read_status() == 0
 
 
 def test_the_draw_follows_the_distribution():
