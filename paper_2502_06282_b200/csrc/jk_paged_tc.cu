@@ -163,6 +163,12 @@ template <int BYTES> __device__ __forceinline__ uint32_t pt_piece(int r, int c) 
   const int x = BYTES == 128 ? (r & 7) : BYTES == 64 ? ((r >> 1) & 3) : BYTES == 32 ? ((r >> 2) & 1) : 0;
   return (uint32_t)(r * BYTES + ((c ^ x) << 4));
 }
+// Four e4m3 codes as fp16.
+__device__ __forceinline__ void pt_widen(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi) : "r"(codes));
+}
 // Instruction descriptor, fp32 accumulate, M = 128; formats: kind::f16 1 = bf16, kind::f8f6f4 0 = e4m3, 1 = e5m2.
 __device__ __forceinline__ uint32_t pt_idesc(uint32_t fmt_a, uint32_t fmt_b, int n, int a_mn, int b_mn) {
   return (1u << 4) | (fmt_a << 7) | (fmt_b << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
@@ -536,6 +542,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
     // swizzled row of codes) and the 16-byte stores (every other piece of a swizzled row of fp16) of such a
     // group fall into different banks.
     const int cw = ct >> 5, qw = lane >> 3, rr = (lane & 4) ? qw ^ 5 : qw;
+    // row, piece and so the swizzles' terms of a thread's first step; further steps are whole groups of 8 rows on
+    const int half = KB == 2 ? cw & 1 : 0, row0 = (KB == 2 ? cw >> 1 : cw) * 8 + rr;
+    const uint32_t at_s = pt_piece<D>(row0, half * 4 + (lane & 3));
+    const uint32_t at_d = half * (PT_KEYS * 128) + pt_piece<128>(row0, (lane & 3) * 2);
     int tc = 0, v_slot = 0, v_par = 0, w_n = 0;
     for (int done = 0; done < share;) {
       int b, u, t0, t1, nt;
@@ -551,33 +561,28 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
           const int buf = w_n & 1, live = I.live;
           if (ok && w_n >= 2) ok = pt_wait(&X.w_empty[buf], ((w_n >> 1) & 1) ^ 1, abort_flag, status);
           unsigned char* dst = smem + F::OFF_W + buf * F::VB;
-          // a warp's step: 8 rows, four pieces (64 dims); D / 64 such halves of 16 groups of rows.  Four
-          // loads are asked for before the first conversion.
+          // a warp's step: 8 rows, four pieces (64 dims), then the next 16 (d = 64: 32) rows; four loads are asked for
+          // before the first conversion
 #pragma unroll 1
           for (int i0 = 0; i0 < 4 * KB; i0 += 4) {
-          uint4 v[4];
+            uint4 v[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int st = (i0 + i) * 4 + cw, r = (st / KB) * 8 + rr;
-            v[i] = *reinterpret_cast<const uint4*>(src + pt_piece<D>(r, (st % KB) * 4 + (lane & 3)));
-          }
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint4*>(src + at_s + (i0 + i) * 2048);
+            if (live < PT_KEYS) {                       // rows behind the last page may hold anything
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int st = (i0 + i) * 4 + cw, r = (st / KB) * 8 + rr, pc = lane & 3;
-            if (r >= live) v[i] = make_uint4(0u, 0u, 0u, 0u);   // rows behind the last page may hold anything
-            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-            uint32_t o[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j] & 0xffffu), __NV_E4M3);
-              const __half2_raw e = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j] >> 16), __NV_E4M3);
-              o[2 * j] = *reinterpret_cast<const uint32_t*>(&a);
-              o[2 * j + 1] = *reinterpret_cast<const uint32_t*>(&e);
+              for (int i = 0; i < 4; ++i)
+                if ((i0 + i) * (32 / KB) + row0 >= live) v[i] = make_uint4(0u, 0u, 0u, 0u);
             }
-            unsigned char* d = dst + (st % KB) * (PT_KEYS * 128);
-            *reinterpret_cast<uint4*>(d + pt_piece<128>(r, pc * 2)) = make_uint4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<uint4*>(d + pt_piece<128>(r, pc * 2 + 1)) = make_uint4(o[4], o[5], o[6], o[7]);
-          }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t o[8];
+              pt_widen(v[i].x, o[0], o[1]);
+              pt_widen(v[i].y, o[2], o[3]);
+              pt_widen(v[i].z, o[4], o[5]);
+              pt_widen(v[i].w, o[6], o[7]);
+              *reinterpret_cast<uint4*>(dst + at_d + (i0 + i) * (32 / KB * 128)) = make_uint4(o[0], o[1], o[2], o[3]);
+              *reinterpret_cast<uint4*>(dst + (at_d ^ 16u) + (i0 + i) * (32 / KB * 128)) = make_uint4(o[4], o[5], o[6], o[7]);
+            }
           }
           ++w_n;
         } else if (ct < PT_WKEYS) {
@@ -813,7 +818,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         bool anew = unseen;
         for (int attempt = 0; attempt < 2; ++attempt) {
           if (anew) references();
-          __half2 most = __float2half2_rn(0.f);
+          uint32_t most = 0u;                           // two maxima of 16-bit patterns: no weight is negative
           const uint64_t kk = pt_pack2(k1, k1), ff = pt_pack2(f1, f1);
 #pragma unroll
           for (int j0 = 0; j0 < RW; j0 += 16) {
@@ -848,30 +853,29 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
                 if ((lost >> (j0 + 2 * j + 1)) & 1u) lacc[j0 / 2 + j].y += e[j].y;
               }
             }
-            __half2 top[4];
             if (!wide) {
 #pragma unroll
               for (int j = 0; j < 8; ++j) {
                 const __half2 v = __float22half2_rn(pt_unpack2(pt_mul2(pt_pack2(e[j].x, e[j].y), ff)));
                 pk[j] = *reinterpret_cast<const uint32_t*>(&v);
-                top[j & 3] = j < 4 ? v : __hmax2(top[j & 3], v);
               }
             } else {
 #pragma unroll
               for (int j = 0; j < 8; ++j) {
                 const __nv_bfloat162 v = __float22bfloat162_rn(e[j]);
-                const __half2 t = __float22half2_rn(e[j]);
                 pk[j] = *reinterpret_cast<const uint32_t*>(&v);
-                top[j & 3] = j < 4 ? t : __hmax2(top[j & 3], t);
               }
             }
-            most = __hmax2(most, __hmax2(__hmax2(top[0], top[1]), __hmax2(top[2], top[3])));
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) most = __vimax3_u16x2(most, pk[j], pk[j + 1]);
             if (j0 == 0) last_product();
             *reinterpret_cast<uint4*>(pbuf + pt_piece<F::PROW>(kl, (grow + j0) >> 3)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
             *reinterpret_cast<uint4*>(pbuf + pt_piece<F::PROW>(kl, ((grow + j0) >> 3) + 1)) = make_uint4(pk[4], pk[5], pk[6], pk[7]);
           }
           if (attempt == 1) break;
-          const bool over = __hgt(__hmax(__low2half(most), __high2half(most)), __float2half(65504.f));
+          // fp16 infinity; 65536 in bf16
+          const uint32_t limit = wide ? 0x4780u : 0x7c00u;
+          const bool over = (most & 0xffffu) >= limit || (most >> 16) >= limit;
           if (!group_or(over)) break;
 #pragma unroll
           for (int j = 0; j < RW / 2; ++j) {
