@@ -2,9 +2,10 @@
 // paged 8-bit KV cache.  Columns of sequence b: full pages (e4m3 codes times a scale per page and kv
 // head), the open page's tokens in T, the tree tokens in T.
 //
-// This file holds the entry point and the CUDA-core kernel (fp32 contexts, and bf16 with the tensor
-// path off).  One CTA = (sequence, kv head, 64 query rows, slice of the key range); the partials of
-// the slices are merged by the kernel of jk_attn.cu.  Bound by its shared-memory reads, not by HBM.
+// This file holds the entry point and two CUDA-core kernels.  For many rows (fp32 contexts, and bf16 with the tensor
+// path off) one CTA = (sequence, kv head, 64 query rows, slice of the key range), the partials of the slices are merged
+// by the kernel of jk_attn.cu; bound by its shared-memory reads, not by HBM (fp32, 60 rows, prefix 2048, batch 2, 8
+// heads: 122 us).  For few rows a cluster of blocks per kv head, below.
 #include <math.h>
 
 #include "jk_paged.cuh"

@@ -29,6 +29,12 @@
 // Warps: four softmax groups of four (32 rows of every second tile, with up to 16 rows every fourth tile), four that
 // widen V, TMA producers for K and for V, an issuer of either product.  Registers are moved to the softmax
 // warps, each role setting its own: with the shared memory this kernel takes a spill is a trip to L2.
+//
+// Measured (B200, graph replay): 13B heads, batch 8, prefix 8192, trees of 60 (690 MB): 169 us = 4.1 TB/s, 0.63 of the
+// measured copy bandwidth; 70B heads, 32 ragged sequences up to 16384, single tokens: 138 us, 0.82 of it.  A 64-row tile
+// takes about 1700 cycles in the steady state: its share of HBM bandwidth 1424, its shared-memory traffic of 190 KB
+// (K read twice, V copied, widened and read, weights written and read) 1490, its 4700 warp instructions 1180 issue
+// slots per sub-partition; no stage alone is the limit (leaving the widening of V out, as a probe, saved 8 %).
 #include <math.h>
 
 #include "jk_paged.cuh"
