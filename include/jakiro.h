@@ -466,6 +466,7 @@ int jk_paged_import(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32
  *   q, out   T [B, M, Hq, d];  parent i32 [B, M], parent[i] < i, -1 for the root
  *   k_tree, v_tree  T [B, Hkv, >= M, d] with the strides given (elements): this layer's keys and
  *            values of the tree tokens; they have to be finite
+ *   out must not overlap the inputs
  * kv_len[b] < 0 or past max_pages * page_size, and a page id outside the pool, set JK_ERR_BOUNDS.
  * With bf16 and the tensor path, queries meet the pages' keys in two e4m3 parts (8 significant
  * bits, as many as bf16 has) and softmax weights are rounded once, to fp16 over pages and to bf16
@@ -539,7 +540,7 @@ int jk_paged_copy(jk_ctx* ctx, void* stream, const jk_paged* host_src, const jk_
  *   u            f32 [rows] in [0, 1); may be NULL when out_tok is
  *   out_tok      i32 [rows] (opt)
  *   out_logits   f32 [rows, V], dense (opt): z / T for kept tokens (0 for a greedy row's), -inf for
- *                the others.  At least one of the two outputs has to be given.
+ *                the others.  Must not overlap logits (JK_ERR_SHAPE).  At least one of the two outputs has to be given.
  */
 int jk_sample(jk_ctx* ctx, void* stream, int32_t rows, const void* logits, int32_t logits_dtype,
               int64_t row_stride, const float* temperature, const int32_t* top_k,

@@ -36,6 +36,7 @@
 // (K read twice, V copied, widened and read, weights written and read) 1490, its 4700 warp instructions 1180 issue
 // slots per sub-partition; no stage alone is the limit (leaving the widening of V out, as a probe, saved 8 %).
 #include <math.h>
+#include <stdio.h>
 
 #include "jk_paged.cuh"
 #include "jk_tcgen05.cuh"
@@ -1128,6 +1129,13 @@ static int pt_launch(jk_ctx* ctx, cudaStream_t st, const CUtensorMap* maps, cons
   static_assert(F::OFF_X + sizeof(pt_tail<D, NR>) + 1024 <= 232448, "shared memory of one CTA");
   auto kern = k_paged_attn_tc<D, NR>;
   JK_CUDA_CHECK(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  // what the roles take (512 x 96 + 256 x 48) has to be there at launch, or the kernel would wait for it
+  cudaFuncAttributes attr;
+  JK_CUDA_CHECK(ctx, cudaFuncGetAttributes(&attr, kern));
+  if (attr.numRegs * PT_THREADS < 512 * 96 + 256 * 48) {
+    snprintf(ctx->cuda_err, sizeof(ctx->cuda_err), "k_paged_attn_tc was built with %d registers", attr.numRegs);
+    return JK_ERR_CUDA;
+  }
   float* part_o = (float*)(ctx->ws + ctx->lay.paged_o);
   float* part_ml = (float*)(ctx->ws + ctx->lay.paged_ml);
   JK_PROF(ctx, st, JK_ST_PAGED_ATTN);

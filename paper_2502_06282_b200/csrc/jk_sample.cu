@@ -1032,6 +1032,12 @@ extern "C" int jk_sample(jk_ctx* ctx, void* stream, int32_t rows, const void* lo
   const void* words[] = {temperature, top_k, top_p, min_p, u, out_tok, out_logits};
   for (const void* p : words)
     if ((uintptr_t)p & 3) return JK_ERR_ALIGN;
+  if (out_logits) {
+    // the filtered rows are written while the logits are still read
+    const uintptr_t z0 = (uintptr_t)logits, z1 = z0 + ((size_t)(rows - 1) * row_stride + V) * jk_elem_size(logits_dtype);
+    const uintptr_t o0 = (uintptr_t)out_logits, o1 = o0 + (size_t)rows * V * 4;
+    if (z0 < o1 && o0 < z1) return JK_ERR_SHAPE;
+  }
   const int rc = jk_ensure_device_info(ctx);
   if (rc != JK_OK) return rc;
   cudaStream_t st = (cudaStream_t)stream;

@@ -187,3 +187,15 @@ def test_sample_refusals():
     assert s(rows=0) == E["SHAPE"] and s(stride=63) == E["SHAPE"] and s(dt=2) == E["DTYPE"]
     assert s(z=None) == E["NULL"] and s(u=None) == E["NULL"] and s(tok=None) == E["NULL"]
     assert s(z=A + 2) == E["ALIGN"] and s(T=A + 1) == E["ALIGN"] and s(tok=A + 2) == E["ALIGN"]
+
+
+@no_gpu
+def test_sample_refuses_filtered_rows_over_its_input():
+    ctx = _context()
+    L, E, A = jk.lib(), jk.ERR, ALIGNED
+    s = lambda out, rows=3, dt=0, stride=80: L.jk_sample(ctx._h, None, rows, A, dt, stride, None, None, None, None, None, None, out)
+    V = ctx.cfg.vocab
+    end = (2 * 80 + V) * 4                              # of the logits, from their start
+    for at in (0, 4, -4, end - 4, 4 - 3 * V * 4):
+        assert s(A + at) == E["SHAPE"]
+    assert s(A + (2 * 80 + V) * 2 - 4, dt=1) == E["SHAPE"]
