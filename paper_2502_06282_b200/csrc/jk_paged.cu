@@ -43,6 +43,7 @@ extern "C" int64_t jk_paged_scratch_ints(int32_t n_pages) {
 
 // ---------------------------------------------------------------------------- block-wide helpers
 #define PLAN_THREADS 1024
+#define PLAN_STEPS 8
 
 // Exclusive prefix sum over the block; *total gets the sum.  red: 33 ints of shared memory.
 __device__ __forceinline__ int plan_scan(int v, int* red, int* total) {
@@ -481,20 +482,32 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_free(jk_paged c, int n,
     if (lane == 0) c.kv_len[r] = 0;
   }
   // pages whose count the marks use up go to the free list, ascending
+  // (PLAN_STEPS times the block's pages are looked at together: most of a large pool is not concerned)
   int at = n_free;
-  for (int i0 = 0; i0 < c.n_pages; i0 += PLAN_THREADS) {
-    const int e = i0 + tid;
-    int empty = 0;
-    if (e < c.n_pages && mark[e] > 0) {
-      const int left = c.refcount[e] - mark[e];
-      c.refcount[e] = left;
-      empty = left == 0;
+  for (int i0 = 0; i0 < c.n_pages; i0 += PLAN_STEPS * PLAN_THREADS) {
+    int named[PLAN_STEPS], any = 0;
+#pragma unroll
+    for (int s = 0; s < PLAN_STEPS; ++s) {
+      const int e = i0 + s * PLAN_THREADS + tid;
+      named[s] = e < c.n_pages ? mark[e] : 0;
+      any |= named[s];
     }
-    if (!__syncthreads_or(empty)) continue;
-    int total;
-    const int k = plan_scan(empty, red, &total);
-    if (empty && at + k < c.n_pages) c.free_list[at + k] = e;
-    at += total;
+    if (!__syncthreads_or(any)) continue;
+#pragma unroll
+    for (int s = 0; s < PLAN_STEPS; ++s) {
+      const int e = i0 + s * PLAN_THREADS + tid;
+      int empty = 0;
+      if (named[s] > 0) {
+        const int left = c.refcount[e] - named[s];
+        c.refcount[e] = left;
+        empty = left == 0;
+      }
+      if (!__syncthreads_or(empty)) continue;
+      int total;
+      const int k = plan_scan(empty, red, &total);
+      if (empty && at + k < c.n_pages) c.free_list[at + k] = e;
+      at += total;
+    }
   }
   if (tid == 0) *c.n_free = at < c.n_pages ? at : c.n_pages;
 }
@@ -508,24 +521,33 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_compact_plan(jk_paged c,
   int32_t* from = map + c.n_pages;
   int32_t* to = from + c.n_pages;
   int mine = 0, live;
+#pragma unroll 8
   for (int e = tid; e < c.n_pages; e += PLAN_THREADS) {
     mine += c.refcount[e] > 0;
     map[e] = e;
   }
   plan_scan(mine, red, &live);
   int holes = 0, movers = 0;
-  for (int e0 = 0; e0 < c.n_pages; e0 += PLAN_THREADS) {
-    const int e = e0 + tid;
-    const bool used = e < c.n_pages && c.refcount[e] > 0;
-    const int hole = e < live && !used, mover = e >= live && used;
-    if (!__syncthreads_or(hole | mover)) continue;
-    int th, tm;
-    const int kh = plan_scan(hole, red, &th);
-    const int km = plan_scan(mover, red, &tm);
-    if (hole) to[holes + kh] = e;
-    if (mover) from[movers + km] = e;
-    holes += th;
-    movers += tm;
+  for (int e0 = 0; e0 < c.n_pages; e0 += PLAN_STEPS * PLAN_THREADS) {
+    unsigned kind = 0u;                                  // two bits a step: hole, mover
+#pragma unroll
+    for (int s = 0; s < PLAN_STEPS; ++s) {
+      const int e = e0 + s * PLAN_THREADS + tid;
+      const bool used = e < c.n_pages && c.refcount[e] > 0;
+      kind |= (unsigned)((e < live && !used) | (e >= live && used) << 1) << (2 * s);
+    }
+    if (!__syncthreads_or(kind != 0u)) continue;
+    for (int s = 0; s < PLAN_STEPS; ++s) {
+      const int e = e0 + s * PLAN_THREADS + tid, hole = (kind >> (2 * s)) & 1u, mover = (kind >> (2 * s + 1)) & 1u;
+      if (!__syncthreads_or(hole | mover)) continue;
+      int th, tm;
+      const int kh = plan_scan(hole, red, &th);
+      const int km = plan_scan(mover, red, &tm);
+      if (hole) to[holes + kh] = e;
+      if (mover) from[movers + km] = e;
+      holes += th;
+      movers += tm;
+    }
   }
   __syncthreads();
   for (int i = tid; i < movers; i += PLAN_THREADS) {

@@ -200,26 +200,24 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
   constexpr int LPK = D / 16, GR = 32 / LPK, KU = R == 1 ? 8 : 4, STEP = GR * KU;
   __shared__ float s_o[KR_WARPS][R][D];
   __shared__ float s_m[KR_WARPS][R], s_l[KR_WARPS][R];
-  __shared__ float c_o[R][D], c_m[R], c_l[R];            // of the block, read by the cluster's first
+  __shared__ float c_o[KR_CLUSTER][R][D], c_m[KR_CLUSTER][R], c_l[KR_CLUSTER][R];   // of the blocks, in the first one
   __shared__ uint32_t s_anc[R][4];
-  jk_pdl_wait();
-  jk_pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint32_t rank = 0;
   if (C > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  auto sync = [&]() {
-    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    else __syncthreads();
-  };
+  // (a block's memory may be written once it runs: waited for before that)
+  if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  jk_pdl_wait();
+  jk_pdl_trigger();
   const int row0 = blockIdx.x / C * R, h = blockIdx.y, b = blockIdx.z;
   const int G = Hq / Hkv, n_rows = G * M, ps = c.page_size;
-  const int P = c.kv_len[b];
-  if (P < 0 || P > c.max_pages * ps) {                   // (the same for the whole cluster)
-    if (tid == 0) jk_set_status(status, JK_ERR_BOUNDS);
-    return;
-  }
-  const int nf = P / ps * ps, n_open = P - nf, tail = n_open + M;
   const int grp = lane / LPK, x0 = lane % LPK * 16;
+  const int W = C * KR_WARPS, gw = (int)rank * KR_WARPS + warp;
+  const int32_t* tab = c.page_table + (size_t)b * c.max_pages;
+  // length, queries, parents and the first page's id are asked for together: one after the other these trips took longer
+  // than a short prefix
+  const int P = c.kv_len[b];
+  const int t_first = (gw * STEP + grp * KU) / ps, first = t_first < c.max_pages ? tab[t_first] : -1;
   float qf[R][16];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -240,6 +238,12 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
 #pragma unroll
     for (int w = 0; w < 4; ++w) s_anc[tid][w] = a[w];
   }
+  if (P < 0 || P > c.max_pages * ps) {                   // (the same for the whole cluster)
+    if (tid == 0) jk_set_status(status, JK_ERR_BOUNDS);
+    if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    return;
+  }
+  const int nf = P / ps * ps, n_open = P - nf, tail = n_open + M;
   __syncthreads();
   float acc[R][16], m[R], l[R];
 #pragma unroll
@@ -294,21 +298,18 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
       for (int o = LPK / 2; o > 0; o >>= 1) s[r] += __shfl_xor_sync(0xffffffffu, s[r], o);
     }
   };
-  const int W = C * KR_WARPS, gw = (int)rank * KR_WARPS + warp;
   const int n_it = (nf + STEP - 1) / STEP;
   // ------------------------------------------------ pages
   {
-    const int32_t* tab = c.page_table + (size_t)b * c.max_pages;
-    auto page_of = [&](int it) {
-      const int key = it * STEP + grp * KU;
-      int id = key < nf ? tab[key / ps] : 0;
+    auto page_of = [&](int key, int id) {                // id: the table's entry, if there is such a key
+      if (key >= nf) return 0;
       if (id < 0 || id >= c.n_pages) {
         jk_set_status(status, JK_ERR_BOUNDS);
         id = 0;
       }
       return id;
     };
-    int next = gw < n_it ? page_of(gw) : 0;
+    int next = page_of(gw * STEP + grp * KU, first);
     for (int it = gw; it < n_it; it += W) {
       const int key = it * STEP + grp * KU, id = next;
       const bool live = key < nf;
@@ -320,7 +321,8 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
 #pragma unroll
       for (int u = 0; u < KU; ++u) vw[u] = kr_load((const uint8_t*)c.v_pages + at + (size_t)u * D);
       const float sk = live ? c.k_scale[blk] : 0.f, sv = live ? c.v_scale[blk] : 0.f;
-      if (it + W < n_it) next = page_of(it + W);
+      const int key_next = key + W * STEP;
+      next = page_of(key_next, key_next < nf ? tab[key_next / ps] : 0);
       float s[KU][R];
 #pragma unroll
       for (int u = 0; u < KU; ++u) {
@@ -396,6 +398,7 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
     if (lane == 0) { s_m[warp][r] = top; s_l[warp][r] = l[r]; }
   }
   __syncthreads();
+  if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // every block runs
   for (int i = tid; i < R * D; i += KR_THREADS) {
     const int r = i / D, x = i % D;
     float top = -INFINITY, sum = 0.f, o = 0.f;
@@ -407,39 +410,33 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
       sum = fmaf(f, s_l[w][r], sum);
       o = fmaf(f, s_o[w][r][x], o);
     }
-    c_o[r][x] = o;
-    if (x == 0) { c_m[r] = top; c_l[r] = sum; }
+    float *po = &c_o[rank][r][x], *pm = &c_m[rank][r], *pl = &c_l[rank][r];
+    if (C > 1) { po = jk_cluster_map(po, 0); pm = jk_cluster_map(pm, 0); pl = jk_cluster_map(pl, 0); }
+    *po = o;
+    if (x == 0) { *pm = top; *pl = sum; }
   }
-  sync();
-  if (rank == 0) {
-    for (int i = tid; i < R * D; i += KR_THREADS) {
-      const int r = i / D, x = i % D, row = row0 + r;
-      float pm[KR_CLUSTER], pl[KR_CLUSTER], po[KR_CLUSTER], top = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < KR_CLUSTER; ++k) {
-        pm[k] = -INFINITY;
-        pl[k] = po[k] = 0.f;
-        if (k < C) {
-          pm[k] = *jk_cluster_map(&c_m[r], k);
-          pl[k] = *jk_cluster_map(&c_l[r], k);
-          po[k] = *jk_cluster_map(&c_o[r][x], k);
-        }
-        top = fmaxf(top, pm[k]);
-      }
-      float sum = 0.f, o = 0.f;
-#pragma unroll
-      for (int k = 0; k < KR_CLUSTER; ++k) {
-        const float f = pm[k] == -INFINITY ? 0.f : exp2f(pm[k] - top);
-        sum = fmaf(f, pl[k], sum);
-        o = fmaf(f, po[k], o);
-      }
-      if (row < n_rows) {
-        const int g = row / M, n = row % M;
-        out[(((size_t)b * M + n) * Hq + h * G + g) * D + x] = jk_from_float<T>(o / sum);
-      }
+  if (C > 1) {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (rank != 0) return;                               // (blocks that left before the others made calls in a row 8 % slower)
+  } else {
+    __syncthreads();
+  }
+  for (int i = tid; i < R * D; i += KR_THREADS) {
+    const int r = i / D, x = i % D, row = row0 + r;
+    float top = -INFINITY, sum = 0.f, o = 0.f;
+    for (int k = 0; k < C; ++k) top = fmaxf(top, c_m[k][r]);
+#pragma unroll 4
+    for (int k = 0; k < C; ++k) {
+      const float f = c_m[k][r] == -INFINITY ? 0.f : exp2f(c_m[k][r] - top);
+      sum = fmaf(f, c_l[k][r], sum);
+      o = fmaf(f, c_o[k][r][x], o);
+    }
+    if (row < n_rows) {
+      const int g = row / M, n = row % M;
+      out[(((size_t)b * M + n) * Hq + h * G + g) * D + x] = jk_from_float<T>(o / sum);
     }
   }
-  sync();                                                // the blocks' sums are read until here
 }
 
 template <typename T, int D, int R>
@@ -450,8 +447,8 @@ static int kr_launch(jk_ctx* ctx, cudaStream_t st, const jk_paged* c, int layer,
   const int n_rb = (g.n_q_heads / g.n_kv_heads * M + R - 1) / R;
   const int64_t base = (int64_t)n_rb * g.n_kv_heads * B;
   const int64_t keys = (int64_t)c->max_pages * c->page_size;
-  // one wave of two blocks per SM, 128 keys a block at least: 4 sequences of 2048 with the 7B heads 17.7 us, with
-  // two waves 23, with four 34; 8 blocks for 1024 keys 7.6 us, 4 blocks 8.9
+  // one wave of two blocks per SM, 128 keys a block at least: 4 sequences of 2048 with the 7B heads 17.1 us, with
+  // two waves 23, with four 34; 8 blocks for 1024 keys 7.4 us, 4 blocks 8.9
   int C = KR_CLUSTER;
   while (C > 1 && (base * C > 2ll * ctx->sm_count || keys / C < 128)) C >>= 1;
   JK_PROF(ctx, st, JK_ST_PAGED_ATTN);
@@ -531,8 +528,8 @@ extern "C" int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_pag
     KR_CASE(T, D, 4);                                                                              \
   } while (0)
   // One query row per kv head (single tokens without grouped heads): the CUDA cores keep up with the pages, 7B heads,
-  // prefix 1024 7.6 us (tensor cores 16.8), 13B heads, batch 16, prefix 4096 122 (141).  Two rows at prefix 8192, batch
-  // 16: 109, tensor cores 58.  In fp32, 16 rows over 4096 keys, batch 4: 98, by tiles of 64 rows 175; 60 rows: the tiles.
+  // prefix 1024 7.4 us (tensor cores 16.8), 13B heads, batch 16, prefix 4096 122 (141).  Two rows at prefix 8192, batch
+  // 16: 109, tensor cores 58.  In fp32, 16 rows over 4096 keys, batch 4: 76, by tiles of 64 rows 175; 60 rows: the tiles.
   const bool tensor = g.dtype == JK_BF16 && ctx->tensor_path;
   if (rows <= (tensor ? 1 : KR_MAX_ROWS)) {
     if (g.dtype == JK_BF16) {

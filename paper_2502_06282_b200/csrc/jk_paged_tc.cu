@@ -292,21 +292,16 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = Hq / Hkv, units = Hkv * n_qblk, ps = c.page_size;
 
-  if (tid == 0) {
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(&X.k_full[i], 1); mbar_init(&X.k_empty[i], 1);
-      mbar_init(&X.v_full[i], 1); mbar_init(&X.v_empty[i], 1);
+  if (warp == 0) {
+    // all barriers stand in a row from k_full on; a lane takes two or three
+    uint64_t* bars = X.k_full;
+    const int n_bars = (int)(&X.q_full - bars) + 1;
+    for (int i = lane; i < n_bars; i += 32) {
+      uint64_t* bar = bars + i;
+      const bool groups = (bar >= &X.s_empty[0][0] && bar <= &X.s_empty[3][1]) || (bar >= X.p_full && bar < X.p_full + 4);
+      mbar_init(bar, bar == &X.q_full ? PT_SOFTMAX / 32 : groups ? 4 * NRG : 1);
     }
-    for (int i = 0; i < PT_INFO; ++i) mbar_init(&X.info_full[i], 1);
-    for (int i = 0; i < 8; ++i) mbar_init(&X.w_full[i], 1);
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(&X.s_full[i][0], 1); mbar_init(&X.s_full[i][1], 1);
-      mbar_init(&X.s_empty[i][0], 4 * NRG); mbar_init(&X.s_empty[i][1], 4 * NRG);
-      mbar_init(&X.p_full[i], 4 * NRG); mbar_init(&X.p_empty[i], 1);
-    }
-    mbar_init(&X.w_empty[0], 1); mbar_init(&X.w_empty[1], 1);
-    mbar_init(&X.q_full, PT_SOFTMAX / 32);
-    X.abort_flag = 0;
+    if (lane == 0) X.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 21) {

@@ -337,6 +337,41 @@ def test_compact_over_many_pages():
     p.same()
 
 
+def test_free_and_compact_in_a_large_pool():
+    """Pages far apart in a pool of many rounds of the plans' block; most rounds hold nothing."""
+    rng = np.random.default_rng(18)
+    ctx = make_ctx(1, 1, 64, 1, 1, "bf16")
+    n_pages, seqs = 40000, 6
+    p = Pair(ctx, 1, n_pages, 16, seqs, 30)
+    perm = rng.permutation(n_pages)
+    used = np.concatenate([perm[:100], np.arange(20), [n_pages - 1, 8191, 8192, 16384]])
+    used = rng.permutation(np.unique(used))
+    p.ref.refcount = [0] * n_pages
+    for b in range(seqs):
+        for t, e in enumerate(used[b * 20:(b + 1) * 20].tolist()):
+            p.ref.table[b][t] = e
+            p.ref.refcount[e] = 1
+        p.ref.kv_len[b] = 16 * len(used[b * 20:(b + 1) * 20])
+    p.ref.free = [e for e in perm.tolist() if not p.ref.refcount[e]]
+    p.dev.page_table.copy_(i32(p.ref.table))
+    p.dev.refcount.copy_(i32(p.ref.refcount))
+    p.dev.kv_len.copy_(i32(p.ref.kv_len))
+    p.dev.free_list[:len(p.ref.free)] = i32(p.ref.free)
+    p.dev.n_free.fill_(len(p.ref.free))
+    for x, kv in (("k", 0), ("v", 1)):
+        p.ref.pages[kv] = rng.integers(0, 126, size=p.ref.pages[kv].shape)
+        getattr(p.dev, x + "_pages").copy_(dev(p.ref.pages[kv]))
+    for gone in ([1, 4], [0]):
+        ctx.paged_free(p.dev, i32(gone))
+        p.ref.release(gone)
+        p.same()
+        n_moved = torch.zeros(1, dtype=torch.int32, device="cuda")
+        ctx.paged_compact(p.dev, n_moved)
+        assert int(n_moved[0]) == p.ref.compact() > 0
+        p.same()
+    assert ctx.read_status() == 0
+
+
 def test_copy_between_pools_and_inside_one():
     rng = np.random.default_rng(19)
     ctx = make_ctx(3, 3, 64, 2, 1, "bf16")
