@@ -496,6 +496,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_free(jk_paged c, int n,
 #pragma unroll
     for (int s = 0; s < PLAN_STEPS; ++s) {
       const int e = i0 + s * PLAN_THREADS + tid;
+      if (e - tid >= c.n_pages) break;
       int empty = 0;
       if (named[s] > 0) {
         const int left = c.refcount[e] - named[s];
@@ -538,6 +539,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_compact_plan(jk_paged c,
     }
     if (!__syncthreads_or(kind != 0u)) continue;
     for (int s = 0; s < PLAN_STEPS; ++s) {
+      if (e0 + s * PLAN_THREADS >= c.n_pages) break;
       const int e = e0 + s * PLAN_THREADS + tid, hole = (kind >> (2 * s)) & 1u, mover = (kind >> (2 * s + 1)) & 1u;
       if (!__syncthreads_or(hole | mover)) continue;
       int th, tm;
