@@ -362,8 +362,8 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
     return (int)min(n, (u64)most);
   };
 
-  // Finds the threshold among the tokens above floor_key (tokens that are equal to it add `extra` of weight, and
-  // ties_f of eq_f of them count).  Everything that is decided is decided by the first block.
+  // Finds the threshold among the tokens above floor_key; ties_f of the eq_f tokens equal to it take part in the
+  // total and come last.  Everything that is decided is decided by the first block.
   auto select = [&](bool by_weight, uint32_t floor_key, int ties_f, int eq_f) {
     smp_map1 map;
     map.set(kmax, floor_key, weight.cut, sizeof(T) == 2);
