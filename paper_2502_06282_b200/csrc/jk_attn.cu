@@ -252,7 +252,7 @@ int jk_attn_tc(jk_ctx* ctx, cudaStream_t st, int B, int M, const void* q, const 
                const int32_t* parent, float scale, void* out);
 int jk_tc_available(const jk_ctx* ctx);
 
-// Merge launch shared with the tensor-core and the paged 8-bit kernels.
+// Merge launch shared with the tensor-core kernel (bf16 output).
 int jk_attn_combine_launch(jk_ctx* ctx, cudaStream_t st, int n_split, size_t n_out, void* out) {
   const jk_ws_layout& L = ctx->lay;
   const float* part_o = (const float*)(ctx->ws + L.attn_o);
@@ -262,14 +262,7 @@ int jk_attn_combine_launch(jk_ctx* ctx, cudaStream_t st, int n_split, size_t n_o
 #define JK_COMBINE(DD, NBB)                                                                    \
   jk_launch_pdl(k_attn_combine<__nv_bfloat16, DD, NBB>, grid, dim3(256), 0, st, part_o, part_ml, \
                 n_split, n_out, (__nv_bfloat16*)out)
-  if (ctx->cfg.dtype == JK_F32) {
-    if (ctx->cfg.head_dim == 128)
-      jk_launch_pdl(k_attn_combine<float, 128, 8>, grid, dim3(256), 0, st, part_o, part_ml, n_split,
-                    n_out, (float*)out);
-    else
-      jk_launch_pdl(k_attn_combine<float, 64, 8>, grid, dim3(256), 0, st, part_o, part_ml, n_split,
-                    n_out, (float*)out);
-  } else if (ctx->cfg.head_dim == 128) {
+  if (ctx->cfg.head_dim == 128) {
     if (n_split <= 8) JK_COMBINE(128, 8);
     else if (n_split <= 10) JK_COMBINE(128, 10);
     else JK_COMBINE(128, 12);
