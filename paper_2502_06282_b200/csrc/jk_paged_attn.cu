@@ -13,9 +13,9 @@
 // through its own keys, KU at a time (within a page), with its own running maximum, and holds R rows of its 16
 // dims of query and output.  What groups, warps and blocks found is merged at the end, in a fixed order.
 // Per key and row this takes about 2 instructions per dim on top of 3 to widen the codes of K and V: with one row the
-// bytes bound it, with more the instructions.  More than four rows are more clusters, which read the pages again, from L2:
-// fp32, 60 rows, prefix 8192, batch 4, 4 heads 216 us (234 without paired multiply-adds); tiles of 64 rows and 32 keys in shared memory took 458, and were
-// slower at every size from 16 rows on.
+// bytes bound it, with more the instructions.  More than four rows are more clusters, which read the pages again, from
+// L2: fp32, 60 rows, prefix 8192, batch 4, 4 heads 216 us (234 without paired multiply-adds); tiles of 64 rows and 32
+// keys in shared memory took 458, and were slower at every size from 16 rows on.
 #define KR_THREADS 256
 #define KR_WARPS (KR_THREADS / 32)
 #define KR_CLUSTER 8
