@@ -589,6 +589,26 @@ def test_attention_replayed_from_a_graph_and_on_another_stream():
         assert np.all(np.abs(host(out) - want) <= bound(want, size, "bf16"))
 
 
+@pytest.mark.parametrize("M", [1, 20])
+def test_two_contexts_read_one_cache_at_once(M):
+    """Attention calls of different contexts may overlap on one cache: each has its own workspace."""
+    parts = attention_case("bf16", 32, 128, 4, 4, M, [900, 333, 64], seed=51)
+    ctx, p, q, qd, kt, ktd, vt, vtd, parent, layer = parts
+    want = check_attention(*parts)
+    other = make_ctx(4, 4, 128, 3, M, "bf16")
+    seen = jk.PagedCache.from_tensors(other, {n: getattr(p.dev, n) for n in jk.PagedCache._NAMES})
+    par, outs = dev(parent), [torch.zeros_like(qd) for _ in range(12)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        c, cache = (ctx, p.dev) if i % 2 else (other, seen)
+        with torch.cuda.stream(streams[i % 2]):
+            c.tree_verify_attn_paged(cache, layer, 3, M, qd, ktd, vtd, par, 1.0 / math.sqrt(128), out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want) for out in outs)
+    assert ctx.read_status() == 0 and other.read_status() == 0
+
+
 def test_verify_qkv_tree_is_verify_qkv_at_other_rows():
     for dtype in ("f32", "bf16"):
         w = synth.scaled(synth.WORKLOADS["tiny" if dtype == "f32" else "tiny_bf16"], batch=2)
