@@ -28,10 +28,13 @@ __device__ __forceinline__ float2 kr_fma2(float2 a, float2 b, float2 c) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return d;
 }
-__device__ __forceinline__ uint4 kr_load(const void* p) {
+// 16 bytes, or zeros where !live (codes of pages that are not the sequence's may be NaN, and a weight of 0 does not undo that).
+__device__ __forceinline__ uint4 kr_load(const void* p, bool live) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+               "mov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+               "@q ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+               : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((uint32_t)live));
   return v;
 }
 __device__ __forceinline__ void kr_widen(const uint4& w, float* o) {
@@ -169,9 +172,9 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
       const size_t at = (blk * ps + (key & (ps - 1))) * D + x0;
       uint4 kw[KU], vw[KU];
 #pragma unroll
-      for (int u = 0; u < KU; ++u) kw[u] = kr_load((const uint8_t*)c.k_pages + at + (size_t)u * D);
+      for (int u = 0; u < KU; ++u) kw[u] = kr_load((const uint8_t*)c.k_pages + at + (size_t)u * D, live);
 #pragma unroll
-      for (int u = 0; u < KU; ++u) vw[u] = kr_load((const uint8_t*)c.v_pages + at + (size_t)u * D);
+      for (int u = 0; u < KU; ++u) vw[u] = kr_load((const uint8_t*)c.v_pages + at + (size_t)u * D, live);
       const float sk = live ? c.k_scale[blk] : 0.f, sv = live ? c.v_scale[blk] : 0.f;
       const int key_next = key + W * STEP;
       next = page_of(key_next, key_next < nf ? tab[key_next / ps] : 0);

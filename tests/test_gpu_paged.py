@@ -632,6 +632,49 @@ def test_verify_qkv_tree_is_verify_qkv_at_other_rows():
         assert not kt[:, :, M:].any() and not vt[:, :, M:].any()
 
 
+# dtype, path, tree rows: one row per kv head, one row block of four and two of them, tensor blocks of 16 and 64 rows
+FEW = [("bf16", "tensor", 1), ("f32", "cuda_core", 1), ("f32", "cuda_core", 3), ("bf16", "cuda_core", 5), ("bf16", "tensor", 5),
+       ("bf16", "tensor", 40)]
+
+
+def check_without_page_0(ps, d, dtype, path, M, owner):
+    """Sequences that do not hold page 0, next to whatever lies there, at lengths that end inside a warp's step and a tile."""
+    rng = np.random.default_rng(ps + d + M)
+    lens = [ps, 3 * ps + 5, 0, 5 * ps, 9 * ps + 1]
+    B, rows, Hkv = len(lens), 9 * ps + 1, 2
+    ctx = make_ctx(Hkv, Hkv, d, B, M, dtype)
+    ctx.set_tensor_path(path == "tensor")
+    p = Pair(ctx, 2, sum(n // ps for n in lens) + 2, ps, B + 1, 11)
+    seqs = list(range(B))
+    if owner == "another sequence":                     # the row behind the call's takes page 0
+        seqs, lens = [B] + seqs, [ps] + lens
+    else:
+        p.ref.free = [0] + list(range(p.ref.n_pages - 1, 0, -1))
+        p.dev.free_list.copy_(i32(p.ref.free))
+        for x in "kv":
+            getattr(p.dev, x + "_scale").fill_(float("nan"))
+    src = []
+    for _ in "kv":
+        x, _keep = p.draw(rng, (2, len(lens), Hkv, rows, d))
+        if owner == "another sequence":
+            x[:, 0, :, ::3] = np.nan
+        src.append((x, dev(x, dtype)))
+    model, _keep = do_import(p, rng, seqs, lens, rows, src=src)
+    model()
+    assert all(0 not in p.ref.table[b] for b in range(B))
+    q, qd = p.draw(rng, (B, M, Hkv, d))
+    (kt, ktd), (vt, vtd) = p.draw(rng, (B, Hkv, M + 1, d)), p.draw(rng, (B, Hkv, M + 1, d))
+    parent = np.stack([synth.random_tree(M, 6, b) for b in range(B)])
+    check_attention(ctx, p, q, qd, kt, ktd, vt, vtd, parent, 1)
+
+
+@pytest.mark.parametrize("dtype,path,M", FEW)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ps", [16, 32, 64, 128])
+def test_attention_next_to_a_sequence_with_nan(ps, d, dtype, path, M):
+    check_without_page_0(ps, d, dtype, path, M, "another sequence")
+
+
 # ------------------------------------------------------------------------------------------
 # the calls together, as a server uses them
 # ------------------------------------------------------------------------------------------
