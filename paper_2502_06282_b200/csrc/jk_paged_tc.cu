@@ -370,9 +370,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
           id = 0;
         }
         if (is_k) {
+          // (1 behind the last page: no scale of another's page, which may hold anything, reaches a weight of 0)
           const size_t blk = ((size_t)layer * c.n_pages + id) * Hkv + h;
-          ksc = c.k_scale[blk];
-          vsc = c.v_scale[blk];
+          const bool live = at + lane < n_pg;
+          ksc = live ? c.k_scale[blk] : 1.f;
+          vsc = live ? c.v_scale[blk] : 1.f;
         }
         id_next = ask(at + 32);
       };

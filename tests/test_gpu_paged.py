@@ -675,6 +675,14 @@ def test_attention_next_to_a_sequence_with_nan(ps, d, dtype, path, M):
     check_without_page_0(ps, d, dtype, path, M, "another sequence")
 
 
+@pytest.mark.parametrize("dtype,path,M", FEW)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ps", [16, 32, 64, 128])
+def test_attention_next_to_a_page_nobody_filled(ps, d, dtype, path, M):
+    """Codes and scales of NaN in the pages that no sequence holds."""
+    check_without_page_0(ps, d, dtype, path, M, "nobody")
+
+
 # ------------------------------------------------------------------------------------------
 # the calls together, as a server uses them
 # ------------------------------------------------------------------------------------------
