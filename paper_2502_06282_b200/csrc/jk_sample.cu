@@ -332,9 +332,20 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
   if (mp > 0.f) {
     const double bound = fmin(0.0, (double)temp * log((double)mp));
     auto ok = [&](uint32_t key) { return (double)smp_value(key) - (double)zmax >= bound; };
+    // The sum's image or, where the sum was rounded down, the next one.  Not where zmax + bound is next to zero: the
+    // difference to zmax is then the same for every float around zero, 2^29 of them and more, and all of them pass.
+    const uint32_t low = kb;
     kb = smp_key(fmaxf((float)((double)zmax + bound), -SMP_BIG));
-    while (kb > SMP_NOTHING + 1u && ok(kb - 1u)) --kb;
-    while (!ok(kb)) ++kb;
+    if (!ok(kb)) ++kb;                                   // (zmax passes: kb is not above it)
+    if (!ok(kb) || (kb > low && ok(kb - 1u))) {
+      uint32_t fails = low, passes = kmax;               // (larger images pass if smaller ones do)
+      while (fails < passes) {
+        const uint32_t mid = fails + (passes - fails) / 2u;
+        if (ok(mid)) passes = mid;
+        else fails = mid + 1u;
+      }
+      kb = passes;
+    }
   }
   auto block_sum = [&](u64 v) {                          // of one block, every thread
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

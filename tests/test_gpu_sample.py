@@ -152,6 +152,27 @@ def test_infinities_nan_and_empty_rows():
     run(ctx, z, "f32", T=[0.0, -1.0, np.nan, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0], u=0.3)
 
 
+def test_min_p_whose_bound_is_zero():
+    """z_max + T ln(min_p) is 0 to the last bit, and the difference to z_max the same for hundreds of millions of floats around
+    zero: finding the threshold must not go through them one by one.  (Tokens keep 1e-9 away from the border, where the
+    logarithm's last bit decides nothing.)"""
+    V = 1001
+    rng = np.random.default_rng(19)
+    ctx = make_ctx(V)
+    T = np.array([0x3E8E9C82, 0x3F0E9C82, 0x3F0E9C82], np.uint32).view(np.float32)
+    top = np.array([0x3F242FF9, 0x3FA42FF9, 0x3FA42FF9], np.uint32).view(np.float32)
+    m = np.float32(0.1)
+    assert all(float(z) + float(t) * np.log(float(m)) == 0.0 for z, t in zip(top, T))
+    z = -np.abs(rng.standard_normal((3, V))) - 1e-3
+    z[:, 5:400] = np.abs(rng.standard_normal((3, 395))) * 0.1 + 1e-3
+    z[:, 600:604] = [1e-9, -1e-9, 1e-5, -1e-5]
+    z[np.arange(3), [77, 0, V - 1]] = top
+    z = synth.store_round(np.minimum(z, top[:, None]), "f32").astype(np.float64)
+    for f in (dict(m=m), dict(m=m, p=0.9), dict(m=m, k=500)):
+        run(ctx, z, "f32", T=T, u=rng.random(3), **f)
+    assert ctx.read_status() == 0
+
+
 def test_strides_alignment_and_missing_arguments():
     rng = np.random.default_rng(9)
     V = 1000
