@@ -149,7 +149,17 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # (the handle alone: torch.cuda.current_stream() makes a Stream object, 3 us against 0.3)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _array(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, name: str) -> Optional[int]:
+    """The pointer of an array the library reads as n elements of one type in a row (None: not given)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of at least {n} elements")
+    return t.data_ptr()
 
 
 def torch_dtype(dtype: str) -> torch.dtype:
@@ -170,6 +180,8 @@ class Context:
                             float(contrast_alpha), float(contrast_beta))
         self.dtype = dtype
         self.tdtype = torch_dtype(dtype)
+        self.kv_kind = (n_kv_heads, head_dim, self.tdtype)     # what a paged cache has to hold
+        self.q_row_bytes = n_q_heads * head_dim * self.tdtype.itemsize
         self._h = C.c_void_p()
         rc = lib().jk_create(C.byref(self._h), C.byref(self.cfg))
         if rc != JK_OK:
@@ -311,75 +323,121 @@ class Context:
                                       _ptr(n_acc), _ptr(acc_idx), rows_out, _ptr(out))
         self._check(rc, "jk_gather_accepted")
 
+    def _tree_arrays(self, k_tree, v_tree, batch, tree_size):
+        """Strides of the tree tokens' K and V, T [>= batch, Hkv, >= tree_size, d]: one pair for both."""
+        Hkv, d, T = self.kv_kind
+        s, shape = k_tree.stride(), k_tree.shape
+        if k_tree.dtype is T and v_tree.dtype is T and v_tree.shape == shape and len(shape) == 4:
+            b, h, m, x = shape
+            if b >= batch and h == Hkv and m >= tree_size and x == d:
+                if v_tree.stride() == s and s[2] == d and s[3] == 1:
+                    return s
+                # (the stride of a dimension of one does not count)
+                if s[3] == 1 and (s[2] == d or m == 1) and all(
+                        p == r or n == 1 for p, r, n in zip(s, v_tree.stride(), shape)):
+                    return s
+                raise ValueError("k_tree and v_tree must have the same strides and dense rows")
+        raise ValueError(f"k_tree, v_tree: expected {T} tensors of one shape, [batch, {Hkv}, tree rows, {d}]")
+
     def verify_qkv_tree(self, w_qkv, batch, tree_size, x, depth, q_out, k_tree, v_tree, kv_len,
                         rope_theta):
         """jk_verify_qkv_tree: as verify_qkv, K and V of node i at row i of k_tree / v_tree."""
-        rc = lib().jk_verify_qkv_tree(self._h, _stream(), _ptr(w_qkv), batch, tree_size, _ptr(x),
-                                      _ptr(depth), _ptr(q_out), _ptr(k_tree), _ptr(v_tree),
-                                      k_tree.stride(0), k_tree.stride(1), _ptr(kv_len),
-                                      float(rope_theta))
+        s = self._tree_arrays(k_tree, v_tree, batch, tree_size)
+        n, c, T = batch * tree_size, self.cfg, self.tdtype
+        rc = lib().jk_verify_qkv_tree(
+            self._h, _stream(),
+            _array(w_qkv, T, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim * c.hidden, "w_qkv"), batch, tree_size,
+            _array(x, T, n * c.hidden, "x"), _array(depth, torch.int32, n, "depth"),
+            _array(q_out, T, n * c.n_q_heads * c.head_dim, "q_out"), k_tree.data_ptr(), v_tree.data_ptr(), s[0], s[1],
+            _array(kv_len, torch.int32, batch, "kv_len"), float(rope_theta))
         self._check(rc, "jk_verify_qkv_tree")
 
     def tree_verify_attn_paged(self, cache: "PagedCache", layer, batch, tree_size, q, k_tree, v_tree,
                              parent, scale, out):
+        """q, out [batch, tree_size, Hq, d]; k_tree, v_tree [batch, Hkv, tree rows, d] with the same strides and dense
+        rows; parent i32 [batch, tree_size] (i64 is converted)."""
+        s = self._tree_arrays(k_tree, v_tree, batch, tree_size)
+        T, n = self.tdtype, batch * tree_size
+        if parent.dtype is not torch.int32 or parent.nbytes < 4 * n or not parent.is_contiguous():
+            if parent.dtype is not torch.int64:
+                raise ValueError("parent: expected a contiguous int32 tensor [batch, tree_size]")
+            parent = parent.int()
+            _array(parent, torch.int32, n, "parent")
+        n *= self.q_row_bytes
+        if (q.dtype is not T or out.dtype is not T or q.nbytes < n or out.nbytes < n or not q.is_contiguous()
+                or not out.is_contiguous()):
+            raise ValueError(f"q, out: expected contiguous {T} tensors [batch, tree_size, {self.cfg.n_q_heads}, {self.cfg.head_dim}]")
         rc = lib().jk_tree_verify_attn_paged(
-            self._h, _stream(), cache.ref, layer, batch, tree_size, q.data_ptr(),
-            k_tree.data_ptr(), v_tree.data_ptr(), k_tree.stride(0), k_tree.stride(1),
-            parent.data_ptr(), scale, out.data_ptr())
+            self._h, _stream(), cache.of(self), layer, batch, tree_size, q.data_ptr(), k_tree.data_ptr(),
+            v_tree.data_ptr(), s[0], s[1], parent.data_ptr(), scale, out.data_ptr())
         if rc:
             self._check(rc, "jk_tree_verify_attn_paged")
 
     def paged_init(self, cache: "PagedCache"):
-        self._check(lib().jk_paged_init(self._h, _stream(), cache.ref), "jk_paged_init")
+        self._check(lib().jk_paged_init(self._h, _stream(), cache.of(self)), "jk_paged_init")
 
     def paged_import(self, cache: "PagedCache", batch, n_tokens, first_layer, n_layers, k_ptrs, v_ptrs,
                    stride_b, stride_h, src_rows, seqs=None):
         """k_ptrs, v_ptrs: int64 device tensors of n_layers pointers to T [batch, Hkv, src_rows, d]."""
-        rc = lib().jk_paged_import(self._h, _stream(), cache.ref, batch, _ptr(seqs), _ptr(n_tokens),
-                                 first_layer, n_layers, _ptr(k_ptrs), _ptr(v_ptrs), stride_b,
-                                 stride_h, src_rows)
+        rc = lib().jk_paged_import(self._h, _stream(), cache.of(self), batch,
+                                 _array(seqs, torch.int32, batch, "seqs"),
+                                 _array(n_tokens, torch.int32, batch, "n_tokens"), first_layer, n_layers,
+                                 _array(k_ptrs, torch.int64, n_layers, "k_ptrs"),
+                                 _array(v_ptrs, torch.int64, n_layers, "v_ptrs"), stride_b, stride_h, src_rows)
         self._check(rc, "jk_paged_import")
 
     def paged_commit(self, cache: "PagedCache", batch, tree_size, k_ptrs, v_ptrs, stride_b, stride_h,
                    n_acc, acc_idx):
-        """k_ptrs, v_ptrs: int64 device tensors of n_layers pointers to the layers' tree arrays."""
-        rc = lib().jk_paged_commit(self._h, _stream(), cache.ref, batch, tree_size, _ptr(k_ptrs),
-                                 _ptr(v_ptrs), stride_b, stride_h, _ptr(n_acc), _ptr(acc_idx))
+        """k_ptrs, v_ptrs: int64 device tensors of n_layers pointers to the layers' tree arrays; n_acc i32 [batch],
+        acc_idx i32 [batch, max_depth]."""
+        rc = lib().jk_paged_commit(self._h, _stream(), cache.of(self), batch, tree_size,
+                                 _array(k_ptrs, torch.int64, cache.n_layers, "k_ptrs"),
+                                 _array(v_ptrs, torch.int64, cache.n_layers, "v_ptrs"), stride_b, stride_h,
+                                 _array(n_acc, torch.int32, batch, "n_acc"),
+                                 _array(acc_idx, torch.int32, batch * self.cfg.max_depth, "acc_idx"))
         self._check(rc, "jk_paged_commit")
 
     def paged_fork(self, cache: "PagedCache", src, dst):
         if src.numel() != dst.numel():
             raise ValueError("src and dst name different numbers of sequences")
-        rc = lib().jk_paged_fork(self._h, _stream(), cache.ref, src.numel(), _ptr(src), _ptr(dst))
+        n = src.numel()
+        rc = lib().jk_paged_fork(self._h, _stream(), cache.of(self), n, _array(src, torch.int32, n, "src"),
+                               _array(dst, torch.int32, n, "dst"))
         self._check(rc, "jk_paged_fork")
 
     def paged_free(self, cache: "PagedCache", seqs):
-        rc = lib().jk_paged_free(self._h, _stream(), cache.ref, seqs.numel(), _ptr(seqs))
+        n = seqs.numel()
+        rc = lib().jk_paged_free(self._h, _stream(), cache.of(self), n, _array(seqs, torch.int32, n, "seqs"))
         self._check(rc, "jk_paged_free")
 
     def paged_compact(self, cache: "PagedCache", n_moved=None):
-        self._check(lib().jk_paged_compact(self._h, _stream(), cache.ref, _ptr(n_moved)),
-                    "jk_paged_compact")
+        self._check(lib().jk_paged_compact(self._h, _stream(), cache.of(self),
+                                         _array(n_moved, torch.int32, 1, "n_moved")), "jk_paged_compact")
 
     def paged_copy(self, src: "PagedCache", dst: "PagedCache", src_ids, dst_ids):
         if src_ids.numel() != dst_ids.numel():
             raise ValueError("src_ids and dst_ids name different numbers of pages")
-        rc = lib().jk_paged_copy(self._h, _stream(), src.ref, dst.ref, src_ids.numel(),
-                                     _ptr(src_ids), _ptr(dst_ids))
+        n = src_ids.numel()
+        rc = lib().jk_paged_copy(self._h, _stream(), src.of(self), dst.of(self), n,
+                                     _array(src_ids, torch.int32, n, "src_ids"),
+                                     _array(dst_ids, torch.int32, n, "dst_ids"))
         self._check(rc, "jk_paged_copy")
 
     def sample(self, logits, temperature=None, top_k=None, top_p=None, min_p=None, u=None,
                out_tok=None, out_logits=None):
-        """jk_sample on logits [rows, V] (f32 or bf16; rows may be strided).  The per-row arrays
-        and the outputs are device tensors or None."""
+        """jk_sample on logits [rows, V] (f32 or bf16; rows may be strided).  The per-row arrays (f32 [rows], top_k
+        i32) and the outputs (i32 [rows], f32 [rows, V]) are contiguous device tensors or None."""
         if logits.dim() != 2 or logits.shape[1] != self.cfg.vocab or (
                 logits.shape[1] > 1 and logits.stride(1) != 1):
             raise ValueError("logits must be [rows, vocab] with contiguous rows")
         dt = {torch.bfloat16: JK_BF16, torch.float32: JK_F32}.get(logits.dtype, -1)
         stride = logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
-        rc = lib().jk_sample(self._h, _stream(), logits.shape[0], _ptr(logits), dt, stride,
-                             _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u),
-                             _ptr(out_tok), _ptr(out_logits))
+        R, f32, i32 = logits.shape[0], torch.float32, torch.int32
+        rc = lib().jk_sample(self._h, _stream(), R, logits.data_ptr(), dt, stride,
+                             _array(temperature, f32, R, "temperature"), _array(top_k, i32, R, "top_k"),
+                             _array(top_p, f32, R, "top_p"), _array(min_p, f32, R, "min_p"), _array(u, f32, R, "u"),
+                             _array(out_tok, i32, R, "out_tok"),
+                             _array(out_logits, f32, R * self.cfg.vocab, "out_logits"))
         self._check(rc, "jk_sample")
 
     def tree_finalize(self, batch, pool, pool_n, root_tok, tree_size, tok, parent, depth, branch,
@@ -483,6 +541,8 @@ class PagedCache:
             ok = t[n].element_size() == 1 if dtype is None else t[n].dtype == dtype
             if not ok or tuple(t[n].shape) != shape or not t[n].is_contiguous():
                 raise ValueError(f"{n}: expected a contiguous {shape} tensor of its type")
+            if t[n].device != t["k_pages"].device:
+                raise ValueError(f"{n} is on another device than k_pages")
             setattr(self, n, t[n])
         self.page_size, self.n_pages, self.n_layers = ps, n_pages, L
         self.max_seqs, self.max_pages = max_seqs, max_pages
@@ -491,6 +551,13 @@ class PagedCache:
         self.struct = JkPaged(L, n_pages, ps, max_seqs, max_pages,
                             *[t[n].data_ptr() for n in self._NAMES], self.scratch.data_ptr())
         self.ref = C.byref(self.struct)
+        self.kind = ctx.kv_kind
+
+    def of(self, ctx):
+        """The descriptor, for a context of the same kv heads, head size and type."""
+        if self.kind is not ctx.kv_kind and self.kind != ctx.kv_kind:
+            raise ValueError("the cache was made for other kv heads, another head size or type")
+        return self.ref
 
 
 class StepBuffers:

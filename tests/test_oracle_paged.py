@@ -199,3 +199,143 @@ def test_sample_refuses_filtered_rows_over_its_input():
     for at in (0, 4, -4, end - 4, 4 - 3 * V * 4):
         assert s(A + at) == E["SHAPE"]
     assert s(A + (2 * 80 + V) * 2 - 4, dt=1) == E["SHAPE"]
+
+
+# ------------------------------------------------------------------------------------------
+# what the binding refuses before the library is called (a stand-in records the calls; nothing runs)
+# ------------------------------------------------------------------------------------------
+class _Recorder:
+    def __init__(self):
+        self.calls, self.real = [], jk.lib()
+
+    def __getattr__(self, name):
+        if name in ("jk_destroy", "jk_paged_scratch_ints"):
+            return getattr(self.real, name)
+
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    ctx = jk.Context(hidden=64, n_experts=2, top_k=1, inter=64, vocab=64, n_q_heads=4, n_kv_heads=2, head_dim=64,
+                     max_batch=2, max_tree=8, max_depth=4, max_frontier=2, k_per_expert=2, dtype="bf16", allocate=False)
+    rec = _Recorder()
+    monkeypatch.setattr(jk, "lib", lambda: rec)
+    monkeypatch.setattr(jk, "_stream", lambda: 0)
+    return ctx, rec
+
+
+def _tensors(Hkv=2, d=64, T=torch.bfloat16):
+    L, n, ps, seqs, cols = 2, 8, 16, 4, 4
+    i32 = dict(dtype=torch.int32)
+    page = lambda: torch.zeros(L, n, Hkv, ps, d, dtype=torch.uint8)
+    opened = lambda: torch.zeros(L, seqs, Hkv, 2 * ps, d, dtype=T)
+    return dict(k_pages=page(), v_pages=page(), k_scale=torch.zeros(L, n, Hkv), v_scale=torch.zeros(L, n, Hkv),
+                k_open=opened(), v_open=opened(), kv_len=torch.zeros(seqs, **i32),
+                page_table=torch.zeros(seqs, cols, **i32), refcount=torch.zeros(n, **i32),
+                free_list=torch.zeros(n, **i32), n_free=torch.zeros(1, **i32))
+
+
+def test_binding_refuses_tree_arrays_that_do_not_go_together(recorded):
+    ctx, rec = recorded
+    cache = jk.PagedCache.from_tensors(ctx, _tensors())
+    B, M, T = 2, 3, torch.bfloat16
+    z = lambda *s, t=T: torch.zeros(*s, dtype=t)
+    good = dict(q=z(B, M, 4, 64), k=z(B, 2, 5, 64), v=z(B, 2, 5, 64), parent=z(B, M, t=torch.int32), out=z(B, M, 4, 64))
+    wide = z(B, 2, 5, 128)
+    bad = [dict(v=z(B, 2, 6, 64)), dict(v=z(B, 2, 6, 64)[:, :, :5]), dict(v=z(B, 5, 2, 64).transpose(1, 2)),
+           dict(k=wide[..., :64], v=wide[..., :64]), dict(k=wide[..., ::2], v=wide[..., ::2]),
+           dict(k=z(B, 2, 5, 64, t=torch.float32)), dict(v=z(B, 2, 5, 64, t=torch.float16)),
+           dict(k=z(B, 2, 2, 64), v=z(B, 2, 2, 64)), dict(k=z(1, 2, 5, 64), v=z(1, 2, 5, 64)),
+           dict(k=z(B, 3, 5, 64), v=z(B, 3, 5, 64)), dict(parent=z(B, M, t=torch.float32)), dict(parent=z(B, 2, t=torch.int32)),
+           dict(parent=z(M, B, t=torch.int32).t()), dict(q=z(B, M, 4, 64, t=torch.float32)), dict(q=z(B, M, 3, 64)),
+           dict(q=z(B, 4, M, 64).transpose(1, 2)), dict(out=z(B, M, 4, 64, t=torch.float32)),
+           dict(out=z(B, M, 8, 64)[:, :, ::2])]
+
+    def attn(change={}):
+        a = {**good, **change}
+        ctx.tree_verify_attn_paged(cache, 0, B, M, a["q"], a["k"], a["v"], a["parent"], 0.1, a["out"])
+
+    for change in bad:
+        with pytest.raises(ValueError):
+            attn(change)
+    wq, x, depth = z(8 * 64, 64), z(B, M, 64), z(B, M, t=torch.int32)
+    n = z(B, t=torch.int32)
+    ok = dict(w=wq, x=x, depth=depth, q=good["q"], k=good["k"], v=good["v"], n=n)
+
+    def qkv(change={}):
+        a = {**ok, **change}
+        ctx.verify_qkv_tree(a["w"], B, M, a["x"], a["depth"], a["q"], a["k"], a["v"], a["n"], 1e4)
+
+    for change in [b for b in bad if b.keys() <= {"k", "v"}] + [
+            dict(depth=depth.long()), dict(x=x.float()), dict(x=z(B, M, 32)), dict(n=n.long()), dict(n=n[:1]), dict(w=wq[:7 * 64])]:
+        with pytest.raises(ValueError):
+            qkv(change)
+    assert not rec.calls
+    attn()
+    qkv()
+    wide_parent = z(B, M, t=torch.int64)
+    attn(dict(parent=wide_parent))                      # converted, not read as 32-bit words
+    assert rec.calls.pop()[1][11] != wide_parent.data_ptr()
+    # the stride of a dimension of one does not count
+    single = torch.zeros(B, 2, 64, dtype=T)
+    both = dict(k=z(B, 2, 5, 64)[:, :, :1], v=torch.as_strided(z(B * 2 * 5 * 64), (B, 2, 1, 64), (640, 320, 7, 1)))
+    ctx.tree_verify_attn_paged(cache, 0, B, 1, good["q"], both["k"], both["v"], good["parent"], 0.1, good["out"])
+    ctx.tree_verify_attn_paged(cache, 0, B, 1, good["q"], single[:, :, None], single[:, :, None], good["parent"], 0.1, good["out"])
+    assert [n for n, _ in rec.calls] == ["jk_tree_verify_attn_paged", "jk_verify_qkv_tree"] + 2 * ["jk_tree_verify_attn_paged"]
+    assert rec.calls[0][1][9:11] == (640, 320) and rec.calls[3][1][9:11] == (128, 64)
+
+
+def test_binding_refuses_lists_of_another_type_or_length(recorded):
+    ctx, rec = recorded
+    cache = jk.PagedCache.from_tensors(ctx, _tensors())
+    i = lambda *s, t=torch.int32: torch.zeros(*s, dtype=t)
+    p = i(2, t=torch.int64)
+    bad = [lambda: ctx.paged_import(cache, 2, i(2, t=torch.int64), 0, 2, p, p, 2048, 1024, 16),
+           lambda: ctx.paged_import(cache, 2, i(1), 0, 2, p, p, 2048, 1024, 16),
+           lambda: ctx.paged_import(cache, 2, i(2), 0, 2, p, p, 2048, 1024, 16, seqs=i(1)),
+           lambda: ctx.paged_import(cache, 2, i(2), 0, 2, p, p, 2048, 1024, 16, seqs=i(2, t=torch.int64)),
+           lambda: ctx.paged_import(cache, 2, i(2), 0, 2, p[:1], p, 2048, 1024, 16),
+           lambda: ctx.paged_import(cache, 2, i(2), 0, 2, p, p.float(), 2048, 1024, 16),
+           lambda: ctx.paged_commit(cache, 2, 1, p, p, 128, 64, i(1), i(2, 4)),
+           lambda: ctx.paged_commit(cache, 2, 1, p, p, 128, 64, i(2), i(2, 3)),
+           lambda: ctx.paged_commit(cache, 2, 1, p, p, 128, 64, i(2), i(4, 2).t()),
+           lambda: ctx.paged_commit(cache, 2, 1, p[:1], p, 128, 64, i(2), i(2, 4)),
+           lambda: ctx.paged_fork(cache, i(2, t=torch.int64), i(2)), lambda: ctx.paged_fork(cache, i(4)[::2], i(2)),
+           lambda: ctx.paged_free(cache, i(2, t=torch.int64)), lambda: ctx.paged_free(cache, i(4)[::2]),
+           lambda: ctx.paged_compact(cache, i(1, t=torch.int64)),
+           lambda: ctx.paged_copy(cache, cache, i(1), i(1, t=torch.int64))]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    z, f = torch.zeros(3, 64), torch.zeros(3)
+    good = dict(temperature=f, top_k=i(3), top_p=f, min_p=f, u=f, out_tok=i(3), out_logits=torch.zeros(3, 64))
+    for change in [{n: good[n].double()} for n in good] + [{n: good[n][:2]} for n in good] + [
+            dict(top_k=f), dict(u=torch.zeros(6)[::2]), dict(out_tok=i(3, t=torch.int64)),
+            dict(out_logits=torch.zeros(3, 128)[:, :64]), dict(out_logits=torch.zeros(64, 3).t())]:
+        with pytest.raises(ValueError):
+            ctx.sample(z, **{**good, **change})
+    assert not rec.calls
+    ctx.sample(z, **good)
+    ctx.sample(z, u=f, out_tok=i(3))
+    assert len(rec.calls) == 2
+
+
+def test_binding_refuses_a_cache_of_another_context(recorded):
+    ctx, rec = recorded
+    other = jk.Context.__new__(jk.Context)
+    other.cfg, other.tdtype, other._h = jk.JkConfig(n_kv_heads=1, head_dim=64), torch.bfloat16, None
+    other.kv_kind = (1, 64, torch.bfloat16)
+    cache = jk.PagedCache.from_tensors(other, _tensors(Hkv=1))
+    i = torch.zeros(1, dtype=torch.int32)
+    q, k = torch.zeros(1, 1, 4, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 1, 64, dtype=torch.bfloat16)
+    mine = jk.PagedCache.from_tensors(ctx, _tensors())
+    for call in (lambda: ctx.paged_init(cache), lambda: ctx.paged_free(cache, i), lambda: ctx.paged_fork(cache, i, i),
+                 lambda: ctx.paged_compact(cache), lambda: ctx.paged_copy(mine, cache, i, i),
+                 lambda: ctx.tree_verify_attn_paged(cache, 0, 1, 1, q, k, k, i, 0.1, q.clone())):
+        with pytest.raises(ValueError):
+            call()
+    assert not rec.calls
