@@ -468,9 +468,9 @@ int jk_paged_import(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32
  *            values of the tree tokens; they have to be finite
  *   out must not overlap the inputs
  * kv_len[b] < 0 or past max_pages * page_size, and a page id outside the pool, set JK_ERR_BOUNDS.
- * With bf16 and the tensor path, queries meet the pages' keys in two e4m3 parts (8 significant
- * bits, as many as bf16 has) and softmax weights are rounded once, to fp16 over pages and to bf16
- * over open and tree rows; sums are fp32.  One query row per kv head, fp32 contexts and the CUDA-core
+ * With bf16 and the tensor path, queries meet the pages' keys in two e4m3 parts (a value is off
+ * by at most 2^-13 of the largest in its row, whatever the other rows hold) and softmax weights
+ * are rounded once, to fp16 over pages and to bf16 over open and tree rows; sums are fp32.  One query row per kv head, fp32 contexts and the CUDA-core
  * path carry everything in fp32.
  */
 int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t layer,

@@ -7,9 +7,12 @@
 // would leave half of the SM's sub-partitions idle in the softmax, and a single token 127 of 128 lanes.
 // A thread owns one key: its page's scales are constants of the thread.
 //
-// K stays 8-bit up to the tensor core.  A bf16 query has 8 significant bits, an e4m3 number 4, so
-// q 2^a = hi + lo with hi = e4m3(q 2^a) and lo = e4m3(q 2^a - hi) is exact down to 2^-17 of the block's
-// largest q, and S is two e4m3 products into one fp32 accumulator, the price of one bf16 product.
+// K stays 8-bit up to the tensor core.  A bf16 query has 8 significant bits, an e4m3 number 4, so q becomes two of them,
+// q 2^a = hi + lo with hi = e4m3(q 2^a) and lo = e4m3(q 2^a - hi), and S is two e4m3 products into one fp32
+// accumulator, the price of one bf16 product.  The block's largest q is put between 224 and 448, where the low part's
+// steps of 2^-9 end: values down to 2^-2 there are exact (2^-10 of the largest), smaller ones off by 2^-10 at most.
+// Rows whose largest values lie within 2^4 of each other share the power of two, so that a value is off by at most
+// 2^-13 of its row's largest; rows further apart take one each (2^-17), and S is multiplied by the difference.
 // V is widened to fp16 (exact) by a warpgroup of its own, 32 KB per tile, because the softmax weights need more
 // than 8 bits: two 8-bit parts per weight cost the softmax three times as many instructions as one
 // conversion to fp16, and their range (2^-17) made every few stages form new maxima.
@@ -224,7 +227,7 @@ template <int D, int NR> struct alignas(16) pt_tail {
   long long cum[JK_MAX_ROWS + 1];    // tiles before each sequence
   int n8[JK_MAX_ROWS], n16[JK_MAX_ROWS];
   pt_info info[PT_INFO];
-  float q_max[16];
+  uint2 q_max[16];                     // per warp, as bits: the largest of the rows' largest magnitudes; the least but 0, less 1
   // of the unit at work, for what comes after its tiles
   int seg_b, seg_slot, seg_whole;
   float c8;                          // logits per product of codes, in units of log2
@@ -234,6 +237,7 @@ template <int D, int NR> struct alignas(16) pt_tail {
   alignas(16) uint32_t anc[4][NR];   // tree nodes each query row sees
   // per warp and row (the four warps of a group form the same values); at the end of a unit alpha holds the sums
   alignas(16) float nref[16][32], alpha[16][32];
+  alignas(16) float rowf[NR];          // a row's own power of two over the block's, where they are far apart
   float wmax[4][4][32], m_run[4][32], wt[4][NR];
 };
 
@@ -640,7 +644,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       // ------------------------------------------------ queries of the unit
       constexpr int QV = (NR * (D / 8) + PT_SOFTMAX - 1) / PT_SOFTMAX;
       uint4 qv[QV];
-      float amax = 0.f;
+      uint32_t rmax[QV];                                // largest magnitude of each piece's row, as bits
+      auto q_exp = [](uint32_t a) {                     // the least e with a <= 448 2^e
+        return max(-100, min(100, (int)(a >> 23) - 127 - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0)));
+      };
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const int idx = tid + i * PT_SOFTMAX, r = idx / (D / 8), ch = idx % (D / 8);
@@ -651,27 +658,42 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         }
       }
       if (t1 > n8 && tid < M) X.parent[tid] = parent[(size_t)b * M + tid];
+      uint32_t most = 0u, least = ~0u;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const uint32_t qw[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+        float a = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          amax = fmaxf(amax, fmaxf(paged_mag(__uint_as_float(qw[j] << 16)),
-                                   paged_mag(__uint_as_float(qw[j] & 0xffff0000u))));
+          a = fmaxf(a, fmaxf(paged_mag(__uint_as_float(qw[j] << 16)), paged_mag(__uint_as_float(qw[j] & 0xffff0000u))));
+#pragma unroll
+        for (int o = D / 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+        rmax[i] = __float_as_uint(a);
+        most = max(most, rmax[i]);
+        least = min(least, rmax[i] - 1u);
       }
-      amax = jk_warp_max(amax);
-      if (lane == 0) X.q_max[warp] = amax;
+      most = __reduce_max_sync(0xffffffffu, most);
+      least = __reduce_min_sync(0xffffffffu, least);
+      if (lane == 0) X.q_max[warp] = make_uint2(most, least);
       // (also: all groups are done with the previous unit's queries, sums and row tables)
       pt_bar<5, PT_SOFTMAX>();
-      amax = jk_warp_max(X.q_max[lane & 15]);
-      int qe = (int)(__float_as_uint(amax) >> 23) - 127 - 8 + ((__float_as_uint(amax) & 0x7fffffu) > 0x600000u ? 1 : 0);
-      qe = max(-100, min(100, qe));
-      const float qinv = paged_pow2(-qe);
+      {
+        const uint2 w = X.q_max[lane & 15];
+        most = __reduce_max_sync(0xffffffffu, w.x);
+        least = __reduce_min_sync(0xffffffffu, w.y);
+      }
+      const int qe = q_exp(most);
+      // Rows within 2^4 of each other share a power of two.  Else each takes its own, and S is brought to the block's where
+      // weights are formed: one row's size must not cost another one its bits.
+      const bool apart = least != ~0u && q_exp(least + 1u) < qe - 4;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const int idx = tid + i * PT_SOFTMAX, r = idx / (D / 8), ch = idx % (D / 8);
         if (r < NR) {
           *reinterpret_cast<uint4*>(smem + F::OFF_Q16 + (ch >> 3) * (NR * 128) + pt_piece<128>(r, ch & 7)) = qv[i];
+          const int re = apart && rmax[i] ? q_exp(rmax[i]) : qe;
+          if (apart && ch == 0) X.rowf[r] = re - qe < -126 ? 0.f : paged_pow2(re - qe);
+          const float qinv = paged_pow2(-re);
           const uint32_t qw[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
           uint32_t hi[2], lo[2];
 #pragma unroll
@@ -759,6 +781,19 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         __syncwarp();
         tc_fence_after();
         const uint32_t sa = tmem + lane_base + (tp * 2 + (cnt & 1)) * NR + grow;
+        if (__builtin_expect(apart && !wide, 0)) {
+          // S from the rows' own powers of two to the block's, where it stands: the loops below do not know of it
+#pragma unroll 1
+          for (int j0 = 0; j0 < RW; j0 += 16) {
+            uint32_t r[16];
+            tmem_ld16(sa + j0, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * X.rowf[grow + j0 + j]);
+            pt_st16(sa + j0, r);
+          }
+          tmem_st_wait();
+        }
 
         // the weights of the group's last tile have been read, and its product is complete
         auto last_product = [&]() {

@@ -538,6 +538,29 @@ def test_attention_with_small_and_large_queries(spread):
     check_attention(*parts, scale=scale)
 
 
+@pytest.mark.parametrize("d,Hq,M", [(128, 8, 6), (64, 4, 20), (128, 2, 3), (64, 1, 9)])
+def test_attention_of_rows_of_very_different_size(d, Hq, M):
+    """Rows 2^14 times as large as others of their block must not cost these their bits.  A query value may be off by 2^-13 of
+    its row's largest, sums of products by 2^-16 of the products' sizes (256 additions in fp32): logits by Delta, weights and
+    the result by exp(2 Delta) - 1 of sum p|v|."""
+    ctx, p, q, qd, kt, ktd, vt, vtd, parent, layer = attention_case("bf16", 32, d, Hq, 1, M, [200, 70], seed=33)
+    size_of = np.where(np.arange(Hq * M).reshape(M, Hq) % 3 == 0, 1.0, 2.0 ** -14)
+    size_of[-1] = [0.0] + [2.0 ** -6] * (Hq - 1)        # a row of zeros, and rows between
+    q = (q * size_of[None, :, :, None]).astype(np.float32)
+    scale = 2.0 ** 12 / math.sqrt(d)
+    out = torch.empty_like(qd)
+    ctx.tree_verify_attn_paged(p.dev, layer, 2, M, dev(q, "bf16"), ktd, vtd, dev(parent), scale, out)
+    want, size = pg.tree_attention(p.ref, layer, q, kt[:, :, :M], vt[:, :, :M], parent, scale)
+    assert ctx.read_status() == 0
+    for b in range(2):
+        k = np.abs(p.ref.columns(0, layer, b, 0, kt[b, 0, :M]))
+        aq = np.abs(q[b].astype(np.float64))
+        delta = scale * (2.0 ** -13 * aq.max(-1) * k.sum(1).max() + 2.0 ** -16 * (aq @ k.T).max(-1))
+        assert delta[size_of == 2.0 ** -14].max() < 2.0 ** -7
+        off = np.abs(host(out)[b] - want[b])
+        assert np.all(off <= bound(want[b], size[b], "bf16") + np.expm1(np.minimum(2 * delta, 50.0))[..., None] * size[b])
+
+
 def test_attention_refuses_what_is_out_of_range():
     parts = attention_case("bf16", 16, 128, 2, 2, 8, [40, 20], seed=41)
     ctx, p, q, qd, kt, ktd, vt, vtd, parent, layer = parts
