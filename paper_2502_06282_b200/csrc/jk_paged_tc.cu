@@ -703,7 +703,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
             const float v3 = __uint_as_float(qw[2 * j + 1] & 0xffff0000u) * qinv;
             hi[j] = paged_pack4(v0, v1, v2, v3);
             const float2 b0 = paged_unpack2(hi[j]), b1 = paged_unpack2(hi[j] >> 16);
-            lo[j] = paged_pack4(v0 - b0.x, v1 - b0.y, v2 - b1.x, v3 - b1.y);
+            // (0 times an infinite value is NaN, which 8 bits hold: no infinity is made finite)
+            lo[j] = paged_pack4(fmaf(v0, 0.f, v0 - b0.x), fmaf(v1, 0.f, v1 - b0.y), fmaf(v2, 0.f, v2 - b1.x),
+                                fmaf(v3, 0.f, v3 - b1.y));
           }
           const uint32_t at = pt_piece<D>(r, ch >> 1) + (ch & 1) * 8;
           *reinterpret_cast<uint2*>(smem + at) = make_uint2(hi[0], hi[1]);

@@ -561,6 +561,27 @@ def test_attention_of_rows_of_very_different_size(d, Hq, M):
         assert np.all(off <= bound(want[b], size[b], "bf16") + np.expm1(np.minimum(2 * delta, 50.0))[..., None] * size[b])
 
 
+@pytest.mark.parametrize("path", ["tensor", "cuda_core"])
+def test_attention_of_an_infinite_query_is_nan(path):
+    """An infinite query value makes every logit of its row infinite or NaN, and the softmax NaN: not a number that was
+    made finite on the way to 8 bits.  The other rows stay what they are."""
+    ctx, p, q, qd, kt, ktd, vt, vtd, parent, layer = attention_case("bf16", 32, 128, 4, 1, 6, [200, 70], seed=34)
+    ctx.set_tensor_path(path == "tensor")
+    q[0, 2, 1, 7], q[1, 0, 3, 100] = np.inf, -np.inf
+    kt[..., 7] = -1.0                                    # (the open and tree keys' logits -inf, the pages' of either sign)
+    ktd[..., 7] = -1.0
+    p.ref.open[0, ..., 7] = -1.0
+    p.dev.k_open[..., 7] = -1.0
+    out = torch.empty_like(qd)
+    ctx.tree_verify_attn_paged(p.dev, layer, 2, 6, dev(q, "bf16"), ktd, vtd, dev(parent), 0.1, out)
+    with np.errstate(invalid="ignore"):
+        want, size = pg.tree_attention(p.ref, layer, q, kt[:, :, :6], vt[:, :, :6], parent, 0.1)
+    got, nan = host(out), np.isnan(want)
+    assert nan[0, 2, 1].all() and nan[1, 0, 3].all() and nan.sum() == 2 * 128
+    assert np.array_equal(np.isnan(got), nan)
+    assert np.all(np.abs(got - want)[~nan] <= bound(want, size, "bf16")[~nan])
+
+
 def test_attention_refuses_what_is_out_of_range():
     parts = attention_case("bf16", 16, 128, 2, 2, 8, [40, 20], seed=41)
     ctx, p, q, qd, kt, ktd, vt, vtd, parent, layer = parts
