@@ -1087,7 +1087,8 @@ __global__ void __launch_bounds__(256) k_paged_merge(const jk_paged c, int B, in
     for (int q = 0; q < RPW; ++q) {
       float2 ml = make_float2(-INFINITY, 0.f);
       if (s0 + lane <= c1 && q < live) ml = *reinterpret_cast<const float2*>(part_ml + slot(s0 + lane, r0 + q) * 2);
-      w[q] = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m[q]);
+      // (a maximum of -inf: nothing seen, the sum is 0; or nothing but NaN, and so is the sum)
+      w[q] = ml.x == -INFINITY ? ml.y * 0.f : fast_exp2(ml.x - m[q]);
       l[q] += w[q] == 0.f ? 0.f : w[q] * ml.y;
     }
     const int n = min(32, c1 - s0 + 1);

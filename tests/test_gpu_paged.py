@@ -582,6 +582,26 @@ def test_attention_of_an_infinite_query_is_nan(path):
     assert np.all(np.abs(got - want)[~nan] <= bound(want, size, "bf16")[~nan])
 
 
+@pytest.mark.parametrize("dtype,path,M", [("bf16", "tensor", 5), ("bf16", "tensor", 60), ("bf16", "tensor", 1),
+                                          ("bf16", "cuda_core", 5), ("f32", "cuda_core", 1)])
+@pytest.mark.parametrize("at", [0, 9984, 19840])
+def test_attention_over_a_run_of_keys_that_are_nan(dtype, path, M, at):
+    """A run of NaN keys that one block of threads has to itself is not lost when the blocks' parts are put together."""
+    rng = np.random.default_rng(M)
+    n, d = 20000, 128
+    ctx = make_ctx(1, 1, d, 1, M, dtype)
+    ctx.set_tensor_path(path == "tensor")
+    p = Pair(ctx, 1, 157, 128, 1, 157)
+    (k, kd), src_v = p.draw(rng, (1, 1, 1, n, d), 0.25), p.draw(rng, (1, 1, 1, n, d))
+    kd[:, :, :, at:at + 128] = float("nan")
+    _, _keep = do_import(p, rng, None, [n], n, src=[(k, kd), src_v])
+    q, qd = p.draw(rng, (1, M, 1, d))
+    (kt, ktd), (vt, vtd) = p.draw(rng, (1, 1, M, d)), p.draw(rng, (1, 1, M, d))
+    out = torch.empty_like(qd)
+    ctx.tree_verify_attn_paged(p.dev, 0, 1, M, qd, ktd, vtd, dev(synth.random_tree(M, 6, 1)[None]), 0.1, out)
+    assert ctx.read_status() == 0 and bool(out.isnan().all())
+
+
 def test_attention_refuses_what_is_out_of_range():
     parts = attention_case("bf16", 16, 128, 2, 2, 8, [40, 20], seed=41)
     ctx, p, q, qd, kt, ktd, vt, vtd, parent, layer = parts
