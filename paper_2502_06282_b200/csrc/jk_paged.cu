@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_plan(
     } else {
       const int n = n_acc[tid], len = c.kv_len[tid];
       if (n >= 0) {
-        bad = n > max_depth || n >= M || len > cap || len - 1 - n < 0;
+        bad = n > max_depth || n >= M || len > cap || len <= n;
         if (!bad) {
           for (int j = 0; j < n; ++j) {
             const int a = acc_idx[(size_t)tid * max_depth + j];

@@ -270,6 +270,19 @@ def test_requests_that_cannot_be_met_change_nothing():
     refuses(p, lambda: do_import(p, rng, [1], [16], 48), "BOUNDS")
 
 
+@pytest.mark.parametrize("length", [-2 ** 31, -2 ** 31 + 1, -1, 0, 1, 2 ** 31 - 1])
+def test_commit_refuses_lengths_that_cannot_be(length):
+    rng = np.random.default_rng(12)
+    ctx = make_ctx(1, 1, 64, 1, 4, "bf16", depth=4)
+    p = Pair(ctx, 1, 4, 16, 1, 3)
+    model, _keep = do_import(p, rng, None, [20], 20)
+    model()
+    kt = torch.zeros(1, 1, 1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    p.dev.kv_len.fill_(length)
+    refuses(p, lambda: ctx.paged_commit(p.dev, 1, 4, ptrs(kt), ptrs(kt), kt.stride(1), kt.stride(2), i32([1]), i32([[1, 0, 0, 0]])),
+            "BOUNDS")
+
+
 @pytest.mark.parametrize("dtype,ps,d,Hkv", [("bf16", 16, 128, 2), ("f32", 32, 64, 1), ("bf16", 128, 64, 3)])
 def test_fork_free_compact(dtype, ps, d, Hkv):
     rng = np.random.default_rng(13 + ps)
