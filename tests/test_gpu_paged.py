@@ -828,3 +828,128 @@ def test_steps_of_a_server(dtype):
     assert torch.equal(first[0], second[1]) or np.all(
         np.abs(host(first[0]) - host(second[1])) <= 2 * bound(host(first[0]), np.abs(host(first[0])) + 1.0, dtype))
     assert ctx.read_status() == 0
+
+
+@pytest.mark.parametrize("dtype,path,M", FEW)
+def test_attention_after_the_pool_was_packed(dtype, path, M):
+    """Rows that came from forks, over pages that were shared, freed and moved, against the model within the bound."""
+    rng = np.random.default_rng(61 + M)
+    ps, d, Hq, Hkv, B = 16, 64, 4, 2, 3
+    ctx = make_ctx(Hq, Hkv, d, B, M, dtype)
+    ctx.set_tensor_path(path == "tensor")
+    p = Pair(ctx, 2, 40, ps, 7, 9)
+    model, _keep = do_import(p, rng, [0, 3, 1, 5, 2], [40, 133, 16, 90, 7], 133)
+    model()
+    for op, a, b in (("free", [0, 1], None), ("fork", [3, 5], [0, 1]), ("free", [3, 2], None), ("fork", [0, 5], [2, 6]), ("free", [5], None)):
+        if op == "free":
+            ctx.paged_free(p.dev, i32(a))
+            p.ref.release(a)
+        else:
+            ctx.paged_fork(p.dev, i32(a), i32(b))
+            p.ref.fork(a, b)
+    moved = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ctx.paged_compact(p.dev, moved)
+    assert int(moved[0]) == p.ref.compact() > 0
+    p.same()
+    assert p.ref.kv_len[:B] == [133, 90, 133] and p.ref.table[0][:8] == p.ref.table[2][:8]
+    q, qd = p.draw(rng, (B, M, Hq, d))
+    (kt, ktd), (vt, vtd) = p.draw(rng, (B, Hkv, M + 1, d)), p.draw(rng, (B, Hkv, M + 1, d))
+    parent = np.stack([synth.random_tree(M, 6, b) for b in range(B)])
+    check_attention(ctx, p, q, qd, kt, ktd, vt, vtd, parent, 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_steps_replayed_from_a_graph(dtype):
+    """Acceptance, commit and the next attention captured once; every replay works on the tree and the lengths it finds."""
+    rng = np.random.default_rng(71)
+    B, M, L, ps, Hq, Hkv, d, V = 2, 9, 2, 16, 4, 2, 64, 64
+    ctx = make_ctx(Hq, Hkv, d, B, M, dtype, vocab=V)
+    p = Pair(ctx, L, 24, ps, 3, 8)
+    model, _keep = do_import(p, rng, None, [30, 15], 48)
+    model()
+    z32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    n_acc, acc_idx, acc_tok, bonus = z32(B), z32(B, 6), z32(B, 6), z32(B)
+    parent, depth = z32(B, M), z32(B, M)
+    tree = {"tok": dev(np.tile(np.arange(M, dtype=np.int32), (B, 1))), "parent": parent, "depth": depth, "branch": z32(B, M),
+            "qslot": z32(B, M)}
+    logits = torch.zeros(B, M, V, device="cuda")
+    kd, vd = (torch.zeros(L, B, Hkv, M, d, dtype=ctx.tdtype, device="cuda") for _ in "kv")
+    qd, out = (torch.zeros(B, M, Hq, d, dtype=ctx.tdtype, device="cuda") for _ in "ab")
+    kp, vp = ptrs(kd), ptrs(vd)
+
+    def step():
+        ctx.accept_and_compact(B, M, 0, 1.0, logits, tree, None, 0, None, None, 0, None, None, 0, 0, p.ref.max_pages * ps,
+                               p.dev.kv_len, n_acc, acc_idx, acc_tok, bonus)
+        ctx.paged_commit(p.dev, B, M, kp, vp, kd.stride(1), kd.stride(2), n_acc, acc_idx)
+        ctx.tree_verify_attn_paged(p.dev, 1, B, M, qd, kd[1], vd[1], parent, d ** -0.5, out)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(5):
+        par = np.stack([synth.random_tree(M, 6, 80 + 10 * turn + b) for b in range(B)])
+        dep, lg = np.zeros((B, M), np.int32), rng.standard_normal((B, M, V)).astype(np.float32)
+        for b in range(B):
+            for i in range(1, M):
+                dep[b, i] = dep[b, par[b, i]] + 1
+                if rng.random() < 0.6:
+                    lg[b, par[b, i], i] = 9.0 + rng.random()
+        (k, kx), (v, vx), (q, qx) = p.draw(rng, kd.shape), p.draw(rng, vd.shape), p.draw(rng, qd.shape)
+        for t, x in ((parent, dev(par)), (depth, dev(dep)), (logits, dev(lg)), (kd, kx), (vd, vx), (qd, qx)):
+            t.copy_(x)
+        before = list(p.ref.kv_len)
+        if turn < 4:
+            graph.replay()
+        else:
+            step()                                       # and a call outside the graph goes on from there
+        torch.cuda.synchronize()
+        na, idx = host(n_acc).tolist(), host(acc_idx).tolist()
+        p.ref.kv_len[:B] = [n + 1 + a for n, a in zip(before, na)]
+        p.ref.commit(k, v, na, idx, M)
+        p.same()
+        want, size = pg.tree_attention(p.ref, 1, q, k[1], v[1], par, d ** -0.5)
+        assert np.all(np.abs(host(out) - want) <= bound(want, size, dtype))
+    assert ctx.read_status() == 0
+
+
+@pytest.mark.parametrize("dtype,path,M", FEW)
+def test_pages_past_32_bits_of_offset(dtype, path, M):
+    """Pools of more than 4 GB, the pages in use at their end: the same bits as from a small pool."""
+    rng = np.random.default_rng(81)
+    ps, d, Hkv, L = 128, 128, 8, 2
+    ctx = make_ctx(Hkv, Hkv, d, 2, M, dtype)
+    ctx.set_tensor_path(path == "tensor")
+    small = jk.PagedCache(ctx, n_layers=L, n_pages=8, page_size=ps, max_seqs=2, max_pages=5)
+    large = jk.PagedCache(ctx, n_layers=L, n_pages=17000, page_size=ps, max_seqs=2, max_pages=5)
+    assert large.k_pages.numel() > 2 ** 32
+    large.free_list.copy_(torch.arange(17000, dtype=torch.int32, device="cuda"))      # 16999 first
+    lens, rows = i32([3 * ps + 17, 2 * ps + 127]), 4 * ps
+    T = ctx.tdtype
+    r = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).cuda().to(T)
+    k, v, q = r(L, 2, Hkv, rows, d), r(L, 2, Hkv, rows, d), r(2, M, Hkv, d)
+    kt, vt = r(L, 2, Hkv, M, d), r(L, 2, Hkv, M, d)
+    parent = dev(np.stack([synth.random_tree(M, 6, b) for b in range(2)]))
+    n_acc, idx = i32([0, 0]), torch.full((2, 6), -1, dtype=torch.int32, device="cuda")
+
+    def attn(cache):
+        out = torch.empty_like(q)
+        ctx.tree_verify_attn_paged(cache, L - 1, 2, M, q, kt[-1], vt[-1], parent, d ** -0.5, out)
+        return out
+
+    first = []
+    for cache in (small, large):
+        ctx.paged_import(cache, 2, lens, 0, L, ptrs(k), ptrs(v), k.stride(1), k.stride(2), rows)
+        first.append(attn(cache))
+        cache.kv_len += 1                                # the root joins; sequence 1 completes a page
+        ctx.paged_commit(cache, 2, M, ptrs(kt), ptrs(vt), kt.stride(1), kt.stride(2), n_acc, idx)
+    assert torch.equal(*first) and not first[0].isnan().any()
+    want = attn(small)
+    assert host(large.page_table)[1].tolist() == [16996, 16995, 16994, -1, -1]
+    assert torch.equal(attn(large), want)
+    ctx.paged_copy(large, small, i32([16994, 16999]), i32([6, 7]))
+    for n in ("k_pages", "v_pages", "k_scale", "v_scale"):
+        assert torch.equal(getattr(small, n)[:, 6], getattr(large, n)[:, 16994])
+        assert torch.equal(getattr(small, n)[:, 7], getattr(large, n)[:, 16999])
+    ctx.paged_compact(large)
+    assert sorted(host(large.page_table)[:, :3].ravel().tolist()) == list(range(6))
+    assert torch.equal(attn(large), want) and ctx.read_status() == 0
