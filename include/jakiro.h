@@ -513,8 +513,8 @@ int jk_paged_free(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t
  * free list hands out n_live, n_live + 1, ...  n_moved i32 [1] (opt) receives the pages moved. */
 int jk_paged_compact(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t* n_moved);
 /* Copy page src_ids[i] of host_src to page dst_ids[i] of host_dst, i < n, codes and scales of all
- * layers; the two pools agree in L, page_size, Hkv and d and may be the same.  No bookkeeping is
- * touched.  A dst id named twice, or (same pool) also named as a source, sets JK_ERR_BOUNDS and
+ * layers; the two pools agree in L, page_size, Hkv and d and may be the same, but not overlap in
+ * part (JK_ERR_SHAPE).  No bookkeeping is touched.  A dst id named twice, or (same pool) also named as a source, sets JK_ERR_BOUNDS and
  * nothing is copied. */
 int jk_paged_copy(jk_ctx* ctx, void* stream, const jk_paged* host_src, const jk_paged* host_dst,
                       int32_t n, const int32_t* src_ids, const int32_t* dst_ids);

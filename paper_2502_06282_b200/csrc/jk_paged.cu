@@ -804,8 +804,21 @@ extern "C" int jk_paged_copy(jk_ctx* ctx, void* stream, const jk_paged* src, con
   if (n > dst->n_pages) return JK_ERR_CAPACITY;
   const int same = src->k_pages == dst->k_pages || src->v_pages == dst->v_pages;
   if (same && (src->k_pages != dst->k_pages || src->v_pages != dst->v_pages ||
+               src->k_scale != dst->k_scale || src->v_scale != dst->v_scale ||
                src->n_pages != dst->n_pages))
     return JK_ERR_SHAPE;
+  if (!same) {
+    // (pools that overlap in part: a page may be read here and written there, in any order)
+    const size_t heads = (size_t)src->n_layers * ctx->cfg.n_kv_heads, block = paged_block_elems(ctx, src);
+    const void* from[] = {src->k_pages, src->v_pages, src->k_scale, src->v_scale};
+    const void* to[] = {dst->k_pages, dst->v_pages, dst->k_scale, dst->v_scale};
+    for (int i = 0; i < 4; ++i)
+      for (int j = 0; j < 4; ++j) {
+        const uintptr_t a = (uintptr_t)from[i], b = (uintptr_t)to[j];
+        if (a < b + heads * dst->n_pages * (j < 2 ? block : 4) && b < a + heads * src->n_pages * (i < 2 ? block : 4))
+          return JK_ERR_SHAPE;
+      }
+  }
   cudaStream_t st = (cudaStream_t)stream;
   JK_PROF(ctx, st, JK_ST_PAGED_PLAN);
   jk_launch_pdl(k_paged_copy_plan, dim3(1), dim3(PLAN_THREADS), 0, st, *src, *dst, same, n, src_ids,

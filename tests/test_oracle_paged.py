@@ -179,6 +179,26 @@ def test_argument_refusals():
 
 
 @no_gpu
+def test_copy_refuses_pools_that_overlap_in_part():
+    ctx = _context()                                    # 2 heads of 64: a block of codes is 1024 bytes, a pool 2 x 8 x 2 of them
+    L, E, MB = jk.lib(), jk.ERR, 1 << 20
+    at = dict(k_pages=1 * MB, v_pages=2 * MB, k_scale=3 * MB, v_scale=4 * MB)
+    other = dict(k_pages=5 * MB, v_pages=6 * MB, k_scale=7 * MB, v_scale=8 * MB)
+    copy = lambda **kw: L.jk_paged_copy(ctx._h, None, C.byref(_cache(**at)), C.byref(_cache(**{**other, **kw})), 1, ALIGNED, ALIGNED)
+    codes, scales = 2 * 8 * 2 * 1024, 2 * 8 * 2 * 4
+    for name in ("k_pages", "v_pages"):
+        for a in (MB, 2 * MB):
+            assert copy(**{name: a + codes - 16}) == E["SHAPE"] and copy(**{name: a - codes + 16}) == E["SHAPE"]
+            assert copy(**{name: a + codes}) == E["CUDA"] and copy(**{name: a - codes}) == E["CUDA"]      # (no device here)
+    for name in ("k_scale", "v_scale"):
+        for a in (3 * MB, 4 * MB):
+            assert copy(**{name: a}) == E["SHAPE"] and copy(**{name: a + scales - 16}) == E["SHAPE"]
+            assert copy(**{name: a + scales}) == E["CUDA"]
+    one = lambda **kw: L.jk_paged_copy(ctx._h, None, C.byref(_cache(**at)), C.byref(_cache(**{**at, **kw})), 1, ALIGNED, ALIGNED)
+    assert one(k_scale=9 * MB) == E["SHAPE"] and one(v_scale=9 * MB) == E["SHAPE"] and one() == E["CUDA"]
+
+
+@no_gpu
 def test_sample_refusals():
     ctx = _context()
     L, E, A = jk.lib(), jk.ERR, ALIGNED
