@@ -412,11 +412,13 @@ int jk_accept_and_compact(jk_ctx* ctx, void* stream, int32_t batch, int32_t tree
  *
  * All arrays are the caller's.  Pages are taken from the end of free_list
  * (free_list[n_free - 1] first) in the order (sequence, page), so results repeat bit for bit.
- * The calls that change a cache check everything first and then change all or nothing: on an
- * index out of range, a row that does not fit or a page that others share they set JK_ERR_BOUNDS
- * in the status word of the context, and JK_ERR_CAPACITY when the free pages do not suffice; the
- * cache is then as it was and the call can be repeated.  Calls on one cache must not overlap on
- * the device unless all of them are jk_tree_verify_attn_paged.
+ * The calls that change a cache check what they are given and the rows that it names first, and
+ * then change all or nothing: on an index out of range, a row that does not fit or a page that
+ * others share they set JK_ERR_BOUNDS in the status word of the context, and JK_ERR_CAPACITY when
+ * the free pages do not suffice; the cache is then as it was and the call can be repeated.  Calls
+ * on one cache must not overlap on the device unless all of them are jk_tree_verify_attn_paged.
+ * Attention, jk_verify_qkv_tree and jk_paged_commit work on the rows 0 .. batch - 1: a sequence
+ * gets to another row by jk_paged_fork and jk_paged_free.
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
   int32_t n_layers;         /* L                                                             */
@@ -510,7 +512,8 @@ int jk_paged_fork(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t
 int jk_paged_free(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t n, const int32_t* seqs);
 /* Pack the pool: with n_live pages in use, the i-th unused id below n_live takes over the i-th
  * used page at or above it (data of all layers, reference count, table entries); afterwards the
- * free list hands out n_live, n_live + 1, ...  n_moved i32 [1] (opt) receives the pages moved. */
+ * free list hands out n_live, n_live + 1, ...  n_moved i32 [1] (opt) receives the pages moved.
+ * It names no sequence and refuses nothing: the reference counts are taken as they are. */
 int jk_paged_compact(jk_ctx* ctx, void* stream, const jk_paged* host_cache, int32_t* n_moved);
 /* Copy page src_ids[i] of host_src to page dst_ids[i] of host_dst, i < n, codes and scales of all
  * layers; the two pools agree in L, page_size, Hkv and d and may be the same, but not overlap in

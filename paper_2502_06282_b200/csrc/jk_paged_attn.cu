@@ -344,8 +344,16 @@ extern "C" int jk_tree_verify_attn_paged(jk_ctx* ctx, void* stream, const jk_pag
   cudaStream_t st = (cudaStream_t)stream;
   const int rows = g.n_q_heads / g.n_kv_heads * tree_size;
   // One query row per kv head (single tokens without grouped heads): the CUDA cores keep up with the pages, 7B heads,
-  // prefix 1024 7.4 us (tensor cores 16.8), 13B heads, batch 16, prefix 4096 122 (141).  Two rows at prefix 8192, batch
-  // 16: 109, tensor cores 58.
+  // prefix 1024 7.4 us (tensor cores 16.8), 13B heads, batch 16, prefix 4096 122 (141).  More rows take the tensor cores
+  // whatever the lengths, which the host does not know.  Both, 8 kv heads of 128, pages of 64, graph replay, CUDA cores
+  // (tensor cores), us, by prefix:
+  //                        128           512           1024          2048          4096          8192
+  //   2 rows, batch 1      8.4 (10.2)    8.7 (10.3)    8.9 (10.8)    10.7 (11.9)   14.3 (12.7)   21.3 (17.1)
+  //           batch 4      8.3 (10.5)    9.1 (11.4)    23.7 (15.7)   29.1 (16.9)   40.5 (19.1)   61.5 (24.4)
+  //           batch 16     8.6 (16.5)    21.1 (18.2)   28.6 (20.6)   43.2 (25.6)   72.2 (34.9)   129 (53.4)
+  //   8 rows, batch 1      8.4 (10.4)    9.0 (10.5)    16.3 (11.0)   19.8 (12.2)   26.7 (12.9)   41.1 (17.4)
+  //           batch 16     16.3 (16.7)   26.8 (18.5)   41.3 (20.8)   68.7 (25.5)   124 (35.2)    230 (53.9)
+  // 4 rows are within 3 % of 2.  So the tensor cores lose up to 2 us (8 at batch 16, prefix 128) and win up to a factor of 4.
   if (rows > 1 && g.dtype == JK_BF16 && ctx->tensor_path)
     return jk_paged_attn_tc(ctx, st, c, layer, batch, tree_size, q, k_tree, v_tree, tree_stride_b, tree_stride_h,
                             parent, softmax_scale, out);

@@ -24,7 +24,10 @@
 // dominant key survives to lengths of 2^20.
 //
 // The open page and the tree tokens are bf16 tiles of 64 keys at the end of the sequence (16-row boxes of
-// either array, dead rows cleared in V): the same pipeline with bf16 products.
+// either array, dead rows cleared in V): the same pipeline with bf16 products.  V is bf16 there, so the weights are too, as
+// in the attention over a 16-bit cache.  Where these keys carry the result (short prefixes) its error against 64 bits is 0.0024
+// instead of the 0.0017 of its own rounding; a second bf16 part of the weights gives 0.0017, and was measured at 3.5 % of
+// the 7B tree's time at prefix 1024, 5 % of the ragged batch's with G = 4, 1.7 % of 13B's: not taken.
 //
 // One CTA per SM; all tiles of the call are dealt out evenly in order (sequence, kv head, row block,
 // tile), so a unit (sequence, kv head, row block) spans CTAs where it has to; such a CTA leaves an
@@ -33,11 +36,15 @@
 // widen V, TMA producers for K and for V, an issuer of either product.  Registers are moved to the softmax
 // warps, each role setting its own: with the shared memory this kernel takes a spill is a trip to L2.
 //
-// Measured (B200, graph replay): 13B heads, batch 8, prefix 8192, trees of 60 (690 MB): 169 us = 4.1 TB/s, 0.63 of the
-// measured copy bandwidth; 70B heads, 32 ragged sequences up to 16384, single tokens: 138 us, 0.82 of it.  A 64-row tile
-// takes about 1700 cycles in the steady state: its share of HBM bandwidth 1424, its shared-memory traffic of 190 KB
-// (K read twice, V copied, widened and read, weights written and read) 1490, its 4700 warp instructions 1180 issue
-// slots per sub-partition; no stage alone is the limit (leaving the widening of V out, as a probe, saved 8 %).
+// Measured (B200, graph replay on the same inputs; in brackets calls one after the other on inputs that leave L2 in
+// between, by machine): 13B heads, batch 8, prefix 8192, trees of 60 (690 MB): 169 us = 4.1 TB/s, 0.63 of the measured copy
+// bandwidth (190 to 200 us, 0.54 to 0.56); 70B heads, 32 ragged sequences up to 16384, single tokens: 134 us, 0.84 of it (137
+// to 147).  A 64-row tile takes about 1700 cycles in the steady state: its share of HBM bandwidth 1424, its
+// shared-memory traffic of 190 KB (K read twice, V copied, widened and read, weights written and read) 1490, its 4700
+// warp instructions 1180 issue slots per sub-partition; no stage alone is the limit (leaving the widening of V out, as a
+// probe, saved 8 %).  At 13B those tiles are 124 us (143 per CTA), the start and the merge 14; the other 30 are the ends of
+// units, 3.2 per CTA: both products drain, the softmax groups meet twice, and the next unit's queries and parents are
+// loaded, converted and walked before its first weight is formed.
 #include <math.h>
 #include <stdio.h>
 

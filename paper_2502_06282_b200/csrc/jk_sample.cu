@@ -19,9 +19,10 @@
 //
 // A row belongs to a cluster of 1 to 8 blocks; histograms are added up in its first block's shared memory.
 //
-// Measured (B200, graph replay): one row of 32000 in fp32 with top-k 50 and top-p 12.6 us, of which a pass over the row
-// takes 1 us and each of the cluster's barriers 0.7; 240 rows of 128256 in bf16 (62 MB in, 123 MB out: 29 us of
-// HBM time) with top-p, min-p, draw and filtered rows 109 us: largest logit 10, histogram 33 (the latency of its
+// Measured (B200, graph replay on the same inputs; in brackets calls one after the other on inputs that leave L2 in
+// between): one row of 32000 in fp32 with top-k 50 and top-p 12.4 us (12.9), of which a pass over the row takes 1 us and
+// each of the cluster's barriers 0.7; 240 rows of 128256 in bf16 (62 MB in, 123 MB out: 29 us of HBM time) with top-p,
+// min-p, draw and filtered rows 108 us (115): largest logit 10, histogram 33 (the latency of its
 // shared-memory atomics, 2.4 cycles of bank conflicts each, and instruction fetch), scan of the bins 8, output and weights 32, search for the token
 // 7; some SMs hold two rows, others one.
 #include <math.h>
@@ -228,7 +229,6 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
   const int nv = V / VEC;
   const int W = C * SMP_WARPS, chunk = ((nv + W - 1) / W + 31) / 32 * 32, gw = rank * SMP_WARPS + warp;
   const int v_begin = (int)min((long long)nv, (long long)gw * chunk), v_end = (int)min((long long)nv, (long long)v_begin + chunk);
-  // f(index of the lane's vector, its VEC values); lanes behind the run's end get NaN and index -1 where `all`
   auto load = [&](int v, uint32_t (&raw)[RAW]) {
     if constexpr (VEC == 1) {
       raw[0] = __float_as_uint(jk_to_float(z0[v]));
@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) k_sample(
       raw[0] = x.x; raw[1] = x.y;
     }
   };
+  // f(index of the lane's vector, its VEC values) for the vectors of the warp's run
   auto each = [&](auto f) {
     int v = v_begin + lane;
     for (; v + 96 < v_end; v += 128) {                   // four loads on their way at a time
