@@ -162,6 +162,14 @@ def _array(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, name: str) -> 
     return t.data_ptr()
 
 
+def _second_dim(n: int, **tensors):
+    """Tensors of several rows of n: more dimensions than one, and a second one that is not n, would be read with a
+    wrong distance between rows.  (A flat tensor is taken as it is.)"""
+    for name, t in tensors.items():
+        if t is not None and t.dim() > 1 and t.shape[1] != n:
+            raise ValueError(f"{name}: the second dimension is {t.shape[1]}, not {n}")
+
+
 def torch_dtype(dtype: str) -> torch.dtype:
     return torch.bfloat16 if dtype == "bf16" else torch.float32
 
@@ -343,6 +351,8 @@ class Context:
                         rope_theta):
         """jk_verify_qkv_tree: as verify_qkv, K and V of node i at row i of k_tree / v_tree."""
         s = self._tree_arrays(k_tree, v_tree, batch, tree_size)
+        if batch > 1:
+            _second_dim(tree_size, x=x, depth=depth, q_out=q_out)
         n, c, T = batch * tree_size, self.cfg, self.tdtype
         rc = lib().jk_verify_qkv_tree(
             self._h, _stream(),
@@ -357,6 +367,8 @@ class Context:
         """q, out [batch, tree_size, Hq, d]; k_tree, v_tree [batch, Hkv, tree rows, d] with the same strides and dense
         rows; parent i32 [batch, tree_size] (i64 is converted)."""
         s = self._tree_arrays(k_tree, v_tree, batch, tree_size)
+        if batch > 1:
+            _second_dim(tree_size, q=q, parent=parent, out=out)
         T, n = self.tdtype, batch * tree_size
         if parent.dtype is not torch.int32 or parent.nbytes < 4 * n or not parent.is_contiguous():
             if parent.dtype is not torch.int64:
@@ -390,6 +402,8 @@ class Context:
                    n_acc, acc_idx):
         """k_ptrs, v_ptrs: int64 device tensors of n_layers pointers to the layers' tree arrays; n_acc i32 [batch],
         acc_idx i32 [batch, max_depth]."""
+        if batch > 1:
+            _second_dim(self.cfg.max_depth, acc_idx=acc_idx)
         rc = lib().jk_paged_commit(self._h, _stream(), cache.of(self), batch, tree_size,
                                  _array(k_ptrs, torch.int64, cache.n_layers, "k_ptrs"),
                                  _array(v_ptrs, torch.int64, cache.n_layers, "v_ptrs"), stride_b, stride_h,
@@ -433,6 +447,8 @@ class Context:
         dt = {torch.bfloat16: JK_BF16, torch.float32: JK_F32}.get(logits.dtype, -1)
         stride = logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
         R, f32, i32 = logits.shape[0], torch.float32, torch.int32
+        if R > 1:
+            _second_dim(self.cfg.vocab, out_logits=out_logits)
         rc = lib().jk_sample(self._h, _stream(), R, logits.data_ptr(), dt, stride,
                              _array(temperature, f32, R, "temperature"), _array(top_k, i32, R, "top_k"),
                              _array(top_p, f32, R, "top_p"), _array(min_p, f32, R, "min_p"), _array(u, f32, R, "u"),

@@ -303,8 +303,9 @@ def test_binding_refuses_tree_arrays_that_do_not_go_together(recorded):
     # the stride of a dimension of one does not count
     single = torch.zeros(B, 2, 64, dtype=T)
     both = dict(k=z(B, 2, 5, 64)[:, :, :1], v=torch.as_strided(z(B * 2 * 5 * 64), (B, 2, 1, 64), (640, 320, 7, 1)))
-    ctx.tree_verify_attn_paged(cache, 0, B, 1, good["q"], both["k"], both["v"], good["parent"], 0.1, good["out"])
-    ctx.tree_verify_attn_paged(cache, 0, B, 1, good["q"], single[:, :, None], single[:, :, None], good["parent"], 0.1, good["out"])
+    q, root, out = z(B, 1, 4, 64), z(B, 1, t=torch.int32), z(B, 1, 4, 64)
+    ctx.tree_verify_attn_paged(cache, 0, B, 1, q, both["k"], both["v"], root, 0.1, out)
+    ctx.tree_verify_attn_paged(cache, 0, B, 1, q, single[:, :, None], single[:, :, None], root, 0.1, out)
     assert [n for n, _ in rec.calls] == ["jk_tree_verify_attn_paged", "jk_verify_qkv_tree"] + 2 * ["jk_tree_verify_attn_paged"]
     assert rec.calls[0][1][9:11] == (640, 320) and rec.calls[3][1][9:11] == (128, 64)
 
@@ -342,6 +343,34 @@ def test_binding_refuses_lists_of_another_type_or_length(recorded):
     ctx.sample(z, **good)
     ctx.sample(z, u=f, out_tok=i(3))
     assert len(rec.calls) == 2
+
+
+def test_binding_refuses_rows_laid_out_for_another_size(recorded):
+    """Larger tensors, dense, whose rows lie further apart than the library reads them."""
+    ctx, rec = recorded
+    cache = jk.PagedCache.from_tensors(ctx, _tensors())
+    B, M, T = 2, 3, torch.bfloat16
+    z = lambda *s, t=T: torch.zeros(*s, dtype=t)
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    k, p = z(B, 2, 5, 64), torch.zeros(2, dtype=torch.int64)
+    attn = lambda q=z(B, M, 4, 64), par=i(B, M), out=z(B, M, 4, 64), B=B: \
+        ctx.tree_verify_attn_paged(cache, 0, B, M, q, k, k.clone(), par, 0.1, out)
+    qkv = lambda x=z(B, M, 64), depth=i(B, M), q=z(B, M, 4, 64), B=B: \
+        ctx.verify_qkv_tree(z(8 * 64, 64), B, M, x, depth, q, k, k.clone(), i(B), 1e4)
+    f = torch.zeros(3)
+    for call in (lambda: attn(q=z(B, 5, 4, 64)), lambda: attn(par=i(B, 5)), lambda: attn(out=z(B, 5, 4, 64)),
+                 lambda: attn(par=torch.zeros(B, 5, dtype=torch.int64)), lambda: qkv(x=z(B, 5, 64)), lambda: qkv(depth=i(B, 5)),
+                 lambda: qkv(q=z(B, 5, 4, 64)), lambda: ctx.paged_commit(cache, B, M, p, p, 640, 320, i(B), i(B, 6)),
+                 lambda: ctx.sample(torch.zeros(3, 64), u=f, out_tok=i(3), out_logits=torch.zeros(3, 80))):
+        with pytest.raises(ValueError):
+            call()
+    assert not rec.calls
+    attn()
+    attn(q=z(B * 5 * 4 * 64), par=i(B * 5))              # flat
+    attn(q=z(1, 5, 4, 64), par=i(1, 5), out=z(1, 5, 4, 64), B=1)      # one sequence has one row
+    qkv()
+    ctx.paged_commit(cache, B, M, p, p, 640, 320, i(B), i(B, 4))
+    assert len(rec.calls) == 5
 
 
 def test_binding_refuses_a_cache_of_another_context(recorded):
