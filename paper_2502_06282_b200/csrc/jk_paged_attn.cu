@@ -14,7 +14,7 @@
 // dims of query and output.  What groups, warps and blocks found is merged at the end, in a fixed order.
 // Per key and row this takes about 2 instructions per dim on top of 3 to widen the codes of K and V: with one row the
 // bytes bound it, with more the instructions.  More than four rows are more clusters, which read the pages again, from
-// L2: fp32, 60 rows, prefix 8192, batch 4, 4 heads 216 us (234 without paired multiply-adds); tiles of 64 rows and 32
+// L2: fp32, 60 rows, prefix 8192, batch 4, 4 heads 220 us (234 without paired multiply-adds); tiles of 64 rows and 32
 // keys in shared memory took 458, and were slower at every size from 16 rows on.
 #define KR_THREADS 256
 #define KR_WARPS (KR_THREADS / 32)
@@ -28,13 +28,18 @@ __device__ __forceinline__ float2 kr_fma2(float2 a, float2 b, float2 c) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return d;
 }
-// 16 bytes, or zeros where !live (codes of pages that are not the sequence's may be NaN, and a weight of 0 does not undo that).
-__device__ __forceinline__ uint4 kr_load(const void* p, bool live) {
+// 16 bytes; where they may be missing, zeros if !live (codes of pages that are not the sequence's may be NaN, and a weight of
+// 0 does not undo that).
+template <bool MISSING> __device__ __forceinline__ uint4 kr_load(const void* p, bool live) {
   uint4 v;
-  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
-               "mov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
-               "@q ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-               : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((uint32_t)live));
+  if constexpr (MISSING)
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+                 "mov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+                 "@q ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((uint32_t)live));
+  else
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
 __device__ __forceinline__ void kr_widen(const uint4& w, float* o) {
@@ -52,6 +57,7 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
     long long tsb, long long tsh, const int32_t* __restrict__ parent, float scale, int M, int Hq, int Hkv, int C,
     T* __restrict__ out, int32_t* status) {
   constexpr int LPK = D / 16, GR = 32 / LPK, KU = R == 1 ? 8 : 4, STEP = GR * KU;
+  constexpr bool ENDS = STEP > 16;       // a step may reach past the last page: pages hold 16 tokens or a multiple
   __shared__ float s_o[KR_WARPS][R][D];
   __shared__ float s_m[KR_WARPS][R], s_l[KR_WARPS][R];
   __shared__ float c_o[KR_CLUSTER][R][D], c_m[KR_CLUSTER][R], c_l[KR_CLUSTER][R];   // of the blocks, in the first one
@@ -167,14 +173,14 @@ __global__ void __launch_bounds__(KR_THREADS, R == 1 ? 2 : 1) k_paged_attn_rows(
     int next = page_of(gw * STEP + grp * KU, first);
     for (int it = gw; it < n_it; it += W) {
       const int key = it * STEP + grp * KU, id = next;
-      const bool live = key < nf;
+      const bool live = !ENDS || key < nf;
       const size_t blk = ((size_t)layer * c.n_pages + id) * Hkv + h;
       const size_t at = (blk * ps + (key & (ps - 1))) * D + x0;
       uint4 kw[KU], vw[KU];
 #pragma unroll
-      for (int u = 0; u < KU; ++u) kw[u] = kr_load((const uint8_t*)c.k_pages + at + (size_t)u * D, live);
+      for (int u = 0; u < KU; ++u) kw[u] = kr_load<ENDS>((const uint8_t*)c.k_pages + at + (size_t)u * D, live);
 #pragma unroll
-      for (int u = 0; u < KU; ++u) vw[u] = kr_load((const uint8_t*)c.v_pages + at + (size_t)u * D, live);
+      for (int u = 0; u < KU; ++u) vw[u] = kr_load<ENDS>((const uint8_t*)c.v_pages + at + (size_t)u * D, live);
       const float sk = live ? c.k_scale[blk] : 0.f, sv = live ? c.v_scale[blk] : 0.f;
       const int key_next = key + W * STEP;
       next = page_of(key_next, key_next < nf ? tab[key_next / ps] : 0);

@@ -651,7 +651,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
       // ------------------------------------------------ queries of the unit
       constexpr int QV = (NR * (D / 8) + PT_SOFTMAX - 1) / PT_SOFTMAX;
       uint4 qv[QV];
-      uint32_t rmax[QV];                                // largest magnitude of each piece's row, as bits
+      static_assert(QV <= 2, "row maxima of all pieces share a word");
       auto q_exp = [](uint32_t a) {                     // the least e with a <= 448 2^e
         return max(-100, min(100, (int)(a >> 23) - 127 - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0)));
       };
@@ -665,19 +665,25 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         }
       }
       if (t1 > n8 && tid < M) X.parent[tid] = parent[(size_t)b * M + tid];
+      // largest magnitude of each piece's row, 16 bits each; infinities and NaN are above all numbers
+      uint32_t rmax = 0u;
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const uint32_t m = __vmaxu2(__vmaxu2(qv[i].x & 0x7fff7fffu, qv[i].y & 0x7fff7fffu),
+                                    __vmaxu2(qv[i].z & 0x7fff7fffu, qv[i].w & 0x7fff7fffu));
+        rmax |= max(m & 0xffffu, m >> 16) << (16 * i);
+      }
+#pragma unroll
+      for (int o = D / 16; o > 0; o >>= 1) rmax = __vmaxu2(rmax, __shfl_xor_sync(0xffffffffu, rmax, o));
+      auto row_max = [&](int i) { return rmax >> (16 * i) << 16; };      // as the bits of a float
       uint32_t most = 0u, least = ~0u;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
-        const uint32_t qw[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
-        float a = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          a = fmaxf(a, fmaxf(paged_mag(__uint_as_float(qw[j] << 16)), paged_mag(__uint_as_float(qw[j] & 0xffff0000u))));
-#pragma unroll
-        for (int o = D / 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        rmax[i] = __float_as_uint(a);
-        most = max(most, rmax[i]);
-        least = min(least, rmax[i] - 1u);
+        const uint32_t a = row_max(i);
+        if (a < 0x7f800000u) {
+          most = max(most, a);
+          least = min(least, a - 1u);
+        }
       }
       most = __reduce_max_sync(0xffffffffu, most);
       least = __reduce_min_sync(0xffffffffu, least);
@@ -698,9 +704,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
         const int idx = tid + i * PT_SOFTMAX, r = idx / (D / 8), ch = idx % (D / 8);
         if (r < NR) {
           *reinterpret_cast<uint4*>(smem + F::OFF_Q16 + (ch >> 3) * (NR * 128) + pt_piece<128>(r, ch & 7)) = qv[i];
-          const int re = apart && rmax[i] ? q_exp(rmax[i]) : qe;
+          const uint32_t a = row_max(i);
+          const bool number = a < 0x7f800000u;          // (else all of the row's logits are infinite or NaN: NaN)
+          const int re = apart && number && a ? q_exp(a) : qe;
           if (apart && ch == 0) X.rowf[r] = re - qe < -126 ? 0.f : paged_pow2(re - qe);
-          const float qinv = paged_pow2(-re);
+          const float qinv = number ? paged_pow2(-re) : __int_as_float(0x7fffffff);
           const uint32_t qw[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
           uint32_t hi[2], lo[2];
 #pragma unroll
@@ -710,9 +718,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_paged_attn_tc(
             const float v3 = __uint_as_float(qw[2 * j + 1] & 0xffff0000u) * qinv;
             hi[j] = paged_pack4(v0, v1, v2, v3);
             const float2 b0 = paged_unpack2(hi[j]), b1 = paged_unpack2(hi[j] >> 16);
-            // (0 times an infinite value is NaN, which 8 bits hold: no infinity is made finite)
-            lo[j] = paged_pack4(fmaf(v0, 0.f, v0 - b0.x), fmaf(v1, 0.f, v1 - b0.y), fmaf(v2, 0.f, v2 - b1.x),
-                                fmaf(v3, 0.f, v3 - b1.y));
+            lo[j] = paged_pack4(v0 - b0.x, v1 - b0.y, v2 - b1.x, v3 - b1.y);
           }
           const uint32_t at = pt_piece<D>(r, ch >> 1) + (ch & 1) * 8;
           *reinterpret_cast<uint2*>(smem + at) = make_uint2(hi[0], hi[1]);
