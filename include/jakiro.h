@@ -17,6 +17,9 @@
  *
  *   jk_tree_verify_attn_paged, jk_paged_*   the attention over a paged 8-bit cache, and its upkeep
  *   jk_sample              temperature, top-k, top-p, min-p: the token, or the filtered target rows
+ *   jk_add_norm, jk_linear, jk_rope_qkv, jk_quantize_rows   the rest of a target layer around its
+ *                          attention: norm with the residual's addition, projections and FFN, rotary
+ *                          positions; in T or with 8-bit operands
  *
  * Conventions that hold for every call
  *   - Returns 0 (JK_OK) or a negative jk_status.  Nothing throws or aborts.
@@ -549,6 +552,105 @@ int jk_sample(jk_ctx* ctx, void* stream, int32_t rows, const void* logits, int32
               int64_t row_stride, const float* temperature, const int32_t* top_k,
               const float* top_p, const float* min_p, const float* u, int32_t* out_tok,
               float* out_logits);
+
+/* ------------------------------------------------------------------------------------------
+ * The rest of a target layer.  (The paper has no counterpart: it takes the target model's forward
+ * pass as given.)  With jk_tree_verify_attn or jk_tree_verify_attn_paged between them these calls
+ * are a whole layer, for the nodes of a tree, for single tokens and for a prompt's rows alike:
+ *   add_norm -> linear (qkv) -> rope_qkv -> attention -> linear (output projection + residual) ->
+ *   add_norm -> linear (gated) -> linear (down + residual).
+ *
+ * 8-bit rows ("mx8"): an array [rows, n], n a multiple of 32, as e4m3 codes, u8 [rows, n] dense, and
+ * one power-of-two scale for each block of 32 consecutive elements of a row: the smallest
+ * s >= 2^-32 with max|x| <= 448 s over the block's finite values, so that x / s is exact and a
+ * value is rounded once, to code = e4m3(x / s), ties to even.  Values under 2^-42 become 0,
+ * infinities the largest code, NaN stays NaN.  A scale is stored as the byte log2(s) + 127, in
+ * tiles of 128 rows x 4 blocks, the order in which the tensor cores take them: row r, block k
+ * lies at byte (r/128 * ceil(n/128) + k/4) * 512 + r%32 * 16 + r%128/32 * 4 + k%4.  Bytes of the
+ * tiles that belong to no row or block are neither written nor do they reach a result.  (Arrays made
+ * elsewhere may hold any scale byte from 1 to 254.)
+ * ------------------------------------------------------------------------------------------ */
+
+/* Bytes of the scale tiles of an mx8 array: ceil(rows/128) * ceil(n/128) * 512 (0 for sizes out of
+ * range: rows 1 .. 2^24, n a multiple of 32 up to 2^20). */
+int64_t jk_row_scale_bytes(int64_t rows, int64_t n);
+
+/* x T [rows, n] (x_stride elements between rows, 0 = n) to mx8: weights once, activations that no
+ * other call hands out in 8 bits.  16-byte aligned rows.  rows <= 2^24. */
+int jk_quantize_rows(jk_ctx* ctx, void* stream, int64_t rows, int32_t n, const void* x,
+                    int64_t x_stride, void* out, uint8_t* out_scale);
+
+/*
+ * RMS norm with the residual's addition, per row:
+ *   s = x + delta;  y = s / sqrt(mean(s^2) + rms_eps) * weight      (rms_eps of the context, f32)
+ *   x, delta     T [rows, n], dense; delta may be NULL (s = x)
+ *   weight       T [n] or NULL (= ones)
+ *   out_sum      T [rows, n] (opt): s, the new residual stream; may be x or delta itself
+ *   out          T [rows, n] (opt): y; may be x or delta itself
+ *   out_mx8, out_scale  (opt, together): y as mx8, rounded from the f32 value, not from out
+ * At least one output.  The norm is that of the f32 sum, not of the rounded one.  n a multiple of 8
+ * (of 32 with mx8) up to 32768.  Outputs must not overlap one another, nor an input in part.
+ */
+int jk_add_norm(jk_ctx* ctx, void* stream, int32_t rows, int32_t n, const void* x, const void* delta,
+                const void* weight, void* out_sum, void* out, void* out_mx8, uint8_t* out_scale);
+
+typedef enum { JK_ACT_NONE = 0, JK_ACT_SILU = 1, JK_ACT_GELU = 2 } jk_act;   /* GELU: z Phi(z), by erf */
+typedef enum { JK_ROWS_T = 0, JK_ROWS_F32 = 1, JK_ROWS_MX8 = 2 } jk_rows_type;
+
+/* A projection: weights of the target model, device pointers, read-only, output-major. */
+typedef struct {
+  int32_t n_out, n_in;      /* weights [n_out, n_in]                                          */
+  int32_t operands;         /* JK_ROWS_T: w and x are T; JK_ROWS_MX8: both are mx8            */
+  int32_t act;              /* jk_act                                                         */
+  const void* w;
+  const uint8_t* w_scale;   /* scale tiles of w (mx8)                                         */
+  const void* bias;         /* T [n_out] or NULL                                              */
+  const void* w_up;         /* second weights [n_out, n_in] of a gated block, or NULL         */
+  const uint8_t* w_up_scale;
+  const void* bias_up;      /* T [n_out] or NULL                                              */
+} jk_linear_op;
+
+/*
+ * Matrix product with its epilogue, gated or not, in one kernel:
+ *   z = x w^T + bias;  y = act(z) [* (x w_up^T + bias_up)] [+ residual]
+ *   x            [rows, n_in]: T with x_stride elements between rows (0 = n_in), or mx8 (dense, with
+ *                x_scale)
+ *   residual     T [rows, n_out] or NULL, residual_stride elements between rows (0 = n_out)
+ *   out          [rows, n_out] as out_type says: T or f32 with out_stride elements between rows
+ *                (0 = n_out), or mx8 (dense, with out_scale; n_out a multiple of 32)
+ * n_in is a multiple of 8 (T) or 32 (mx8) up to 131072, n_out any number up to 2^20, rows up to
+ * 2^20; rows of x are 16-byte aligned.  Products are exact and summed in f32 (f32 contexts: f32
+ * multiply-adds), the epilogue is f32, y is rounded once.  out may be residual itself (same
+ * stride); any other overlap of out with an input is refused (JK_ERR_SHAPE).  bf16 contexts and mx8 operands run on
+ * the tensor cores while the tensor path is on (mx8: in bf16 contexts).
+ */
+int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* host_op, int32_t rows, const void* x,
+              const uint8_t* x_scale, int64_t x_stride, const void* residual, int64_t residual_stride,
+              void* out, int32_t out_type, uint8_t* out_scale, int64_t out_stride);
+
+/*
+ * Rotary positions with one or several axes (time, height, width of images and video), and the place
+ * of K and V: what lies between a qkv projection and the attention.
+ *   qkv          T [batch, n_tokens, (Hq + 2 Hkv) d] rows of q, then k, then v heads, row_stride
+ *                elements between tokens (0 = dense, a multiple of 16 bytes)
+ *   pos          i32 [batch, n_tokens, n_axes], each >= 0
+ *   host_sections  n_axes counts with the sum d/2: the first host_sections[0] of the d/2 frequencies
+ *                turn with axis 0, the next with axis 1, ...  n_axes 1 .. 4
+ *   Pair (i, i + d/2) of every q and k head turns by pos[axis of i] * rope_theta^(-2i/d); angles are
+ *   formed and reduced in 64 bits.
+ *   q_out        T [batch, n_tokens, Hq, d]
+ *   k_out, v_out T [batch, Hkv, >= rows, d] with the strides given (elements): token i goes to row
+ *                first_row[b] + i (first_row i32 [batch], e.g. kv_len; NULL = 0)
+ *   rows         rows addressable in k_out, v_out; first_row[b] < 0, first_row[b] + n_tokens > rows
+ *                or a negative position sets JK_ERR_BOUNDS, and that sequence's K and V (that
+ *                token) are not written.
+ * n_tokens up to 2^20, not bound to max_tree; batch up to 65535, not bound to max_batch.  Outputs
+ * must not overlap qkv (JK_ERR_SHAPE).
+ */
+int jk_rope_qkv(jk_ctx* ctx, void* stream, int32_t batch, int32_t n_tokens, const void* qkv,
+                int64_t row_stride, const int32_t* pos, int32_t n_axes, const int32_t* host_sections,
+                float rope_theta, void* q_out, void* k_out, void* v_out, int64_t stride_b,
+                int64_t stride_h, int32_t rows, const int32_t* first_row);
 
 #ifdef __cplusplus
 }

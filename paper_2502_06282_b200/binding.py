@@ -29,7 +29,8 @@ EXPORTS = ["jk_create", "jk_destroy", "jk_workspace_bytes", "jk_set_workspace", 
            "jk_set_attn_kernel", "jk_profile_read", "jk_draft_pre",
            "jk_verify_qkv", "jk_gather_accepted", "jk_paged_scratch_ints", "jk_paged_init",
            "jk_paged_import", "jk_tree_verify_attn_paged", "jk_verify_qkv_tree", "jk_paged_commit",
-           "jk_paged_fork", "jk_paged_free", "jk_paged_compact", "jk_paged_copy", "jk_sample"]
+           "jk_paged_fork", "jk_paged_free", "jk_paged_compact", "jk_paged_copy", "jk_sample",
+           "jk_row_scale_bytes", "jk_quantize_rows", "jk_add_norm", "jk_linear", "jk_rope_qkv"]
 
 
 class JkConfig(C.Structure):
@@ -66,6 +67,14 @@ class JkPaged(C.Structure):
                                   "kv_len", "page_table", "refcount", "free_list", "n_free",
                                   "scratch")]
 
+
+class JkLinearOp(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_out", "n_in", "operands", "act")] + [
+        (n, C.c_void_p) for n in ("w", "w_scale", "bias", "w_up", "w_up_scale", "bias_up")]
+
+
+JK_ROWS_T, JK_ROWS_F32, JK_ROWS_MX8 = 0, 1, 2
+ACTS = {"none": 0, "silu": 1, "gelu": 2}
 
 _lib = None
 
@@ -122,6 +131,11 @@ def lib() -> C.CDLL:
         L.jk_paged_compact.argtypes = [vp, vp, kv, vp]
         L.jk_paged_copy.argtypes = [vp, vp, kv, kv, i32, vp, vp]
         L.jk_sample.argtypes = [vp, vp, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp]
+        L.jk_row_scale_bytes.argtypes = [i64, i64]
+        L.jk_quantize_rows.argtypes = [vp, vp, i64, i32, vp, i64, vp, vp]
+        L.jk_add_norm.argtypes = [vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.jk_linear.argtypes = [vp, vp, C.POINTER(JkLinearOp), i32, vp, vp, i64, vp, i64, vp, i32, vp, i64]
+        L.jk_rope_qkv.argtypes = [vp, vp, i32, i32, vp, i64, vp, i32, C.POINTER(i32), f32, vp, vp, vp, i64, i64, i32, vp]
         L.jk_profile_enable.argtypes = [vp, i32]
         L.jk_profile_collect.argtypes = [vp, vp, C.POINTER(f32), C.POINTER(i32)]
         L.jk_profile_read.argtypes = [vp, vp, C.POINTER(f32), C.POINTER(i32)]
@@ -130,9 +144,10 @@ def lib() -> C.CDLL:
         L.jk_profile_stage_name.restype = C.c_char_p
         for name in EXPORTS:
             if name not in ("jk_workspace_bytes", "jk_strerror", "jk_last_cuda_error",
-                            "jk_profile_stage_name", "jk_paged_scratch_ints"):
+                            "jk_profile_stage_name", "jk_paged_scratch_ints", "jk_row_scale_bytes"):
                 getattr(L, name).restype = C.c_int
         L.jk_paged_scratch_ints.restype = i64
+        L.jk_row_scale_bytes.restype = i64
         _lib = L
     return _lib
 
@@ -456,6 +471,106 @@ class Context:
                              _array(out_logits, f32, R * self.cfg.vocab, "out_logits"))
         self._check(rc, "jk_sample")
 
+    # ------------------------------------------------------------------ a target layer around its attention
+    def _rows(self, t, name, dtype=None, shape=None):
+        """[rows, n] with contiguous rows: the distance between rows (0 where there is one)."""
+        if t.dtype is not (dtype or self.tdtype) or t.dim() != 2 or (shape is not None and t.shape != shape):
+            raise ValueError(f"{name}: expected a {dtype or self.tdtype} tensor {list(shape) if shape else '[rows, n]'}")
+        if not t.is_cuda:
+            raise ValueError(f"{name} is not on a CUDA device")
+        s = t.stride()
+        if s[1] != 1 and t.shape[1] > 1:
+            raise ValueError(f"{name}: expected contiguous rows")
+        return s[0] if t.shape[0] > 1 else 0
+
+    def _dense(self, t, shape, name):
+        if t is None:
+            return None
+        if t.dtype is not self.tdtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous {self.tdtype} tensor {list(shape)}")
+        if not t.is_cuda:
+            raise ValueError(f"{name} is not on a CUDA device")
+        return t.data_ptr()
+
+    def add_norm(self, x, weight=None, delta=None, out_sum=None, out=None, out_mx8: "Optional[Mx8]" = None):
+        """jk_add_norm: x, delta, out_sum, out [rows, n] dense, weight [n], out_mx8 an Mx8 of [rows, n]."""
+        if x.dim() != 2:
+            raise ValueError("x: expected a tensor [rows, n]")
+        shape = x.shape
+        if out_mx8 is not None and out_mx8.shape != shape:
+            raise ValueError(f"out_mx8: expected an array of {list(shape)}")
+        ptrs = (self._dense(x, shape, "x"), self._dense(delta, shape, "delta"), self._dense(weight, shape[1:], "weight"),
+                self._dense(out_sum, shape, "out_sum"), self._dense(out, shape, "out"))
+        rc = lib().jk_add_norm(self._h, _stream(), shape[0], shape[1], *ptrs,
+                               *((None, None) if out_mx8 is None else out_mx8.ptrs))
+        if rc:
+            self._check(rc, "jk_add_norm")
+
+    def quantize_mx8(self, x, out: "Mx8"):
+        """jk_quantize_rows: x [rows, n] (rows may lie apart) to an Mx8 of the same shape."""
+        stride = self._rows(x, "x", shape=out.shape)
+        rc = lib().jk_quantize_rows(self._h, _stream(), x.shape[0], x.shape[1], x.data_ptr(), stride, *out.ptrs)
+        if rc:
+            self._check(rc, "jk_quantize_rows")
+
+    def linear(self, op: "Linear", x, out, residual=None):
+        """jk_linear: x [rows, n_in] (T, rows may lie apart; or Mx8, as op's weights are), out [rows, n_out] (T, f32
+        or Mx8), residual T [rows, n_out] or None; out may be the residual itself."""
+        if op.kind != self.tdtype:
+            raise ValueError("the projection was made for a context of another type")
+        if op.mx8:
+            if not isinstance(x, Mx8) or x.shape[1] != op.n_in:
+                raise ValueError(f"x: expected an Mx8 [rows, {op.n_in}], as the weights are")
+            rows, xs = x.shape[0], 0
+            xp, xsp = x.ptrs
+        else:
+            if isinstance(x, Mx8) or x.dim() != 2 or x.shape[1] != op.n_in:
+                raise ValueError(f"x: expected a {self.tdtype} tensor [rows, {op.n_in}]")
+            rows, xs, xp, xsp = x.shape[0], self._rows(x, "x"), x.data_ptr(), None
+        shape = (rows, op.n_out)
+        rp, rs, os = None, 0, 0
+        if residual is not None:
+            rs, rp = self._rows(residual, "residual", shape=shape), residual.data_ptr()
+        if isinstance(out, Mx8):
+            if out.shape != shape:
+                raise ValueError(f"out: expected an array of {list(shape)}")
+            kind, (o, osp) = JK_ROWS_MX8, out.ptrs
+        else:
+            kind = JK_ROWS_F32 if out.dtype is torch.float32 else JK_ROWS_T
+            os, o, osp = self._rows(out, "out", out.dtype if kind == JK_ROWS_F32 else None, shape), out.data_ptr(), None
+        rc = lib().jk_linear(self._h, _stream(), op.ref, rows, xp, xsp, xs, rp, rs, o, kind, osp, os)
+        if rc:
+            self._check(rc, "jk_linear")
+
+    def rope_qkv(self, batch, n_tokens, qkv, pos, sections, rope_theta, q_out, k_out, v_out, first_row=None):
+        """jk_rope_qkv: qkv [batch * n_tokens rows, (Hq + 2 Hkv) d], rows evenly apart; pos i32 [batch, n_tokens,
+        axes] (one axis: [batch, n_tokens] too); sections the frequencies of each axis; q_out [batch, n_tokens, Hq,
+        d]; k_out, v_out [batch, Hkv, rows, d] with the same strides and dense rows; first_row i32 [batch]."""
+        c, T, n = self.cfg, self.tdtype, batch * n_tokens
+        width = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
+        if qkv.dtype is not T or qkv.shape[-1] != width or qkv.numel() != n * width or qkv.stride(-1) != 1:
+            raise ValueError(f"qkv: expected a {T} tensor [batch, n_tokens, {width}]")
+        if qkv.is_contiguous():
+            stride = width
+        else:
+            stride = qkv.stride(-2) if n_tokens > 1 or qkv.dim() == 2 else qkv.stride(0)
+            if qkv.dim() > 3 or (qkv.dim() == 3 and batch > 1 and n_tokens > 1 and qkv.stride(0) != n_tokens * stride):
+                raise ValueError("qkv: its rows do not lie evenly apart")
+        axes = len(sections)
+        if pos.dim() == 3 and pos.shape[2] != axes:
+            raise ValueError(f"pos: expected {axes} positions for each token")
+        if q_out.dtype is not T or q_out.numel() != n * c.n_q_heads * c.head_dim or not q_out.is_contiguous():
+            raise ValueError(f"q_out: expected a contiguous {T} tensor [batch, n_tokens, {c.n_q_heads}, {c.head_dim}]")
+        if not (qkv.is_cuda and pos.is_cuda and q_out.is_cuda and k_out.is_cuda and v_out.is_cuda):
+            raise ValueError("qkv, pos and the outputs must be on a CUDA device")
+        s = self._tree_arrays(k_out, v_out, batch, n_tokens)
+        rc = lib().jk_rope_qkv(
+            self._h, _stream(), batch, n_tokens, qkv.data_ptr(), stride, _array(pos, torch.int32, n * axes, "pos"), axes,
+            (C.c_int32 * axes)(*sections), rope_theta, q_out.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+            s[0], s[1], k_out.shape[2], _array(first_row, torch.int32, batch, "first_row"))
+        if rc:
+            self._check(rc, "jk_rope_qkv")
+
     def tree_finalize(self, batch, pool, pool_n, root_tok, tree_size, tok, parent, depth, branch,
                       qslot, anc, static_keep=None):
         ps = pool if isinstance(pool, JkPool) else self.pool_struct(pool)
@@ -503,6 +618,57 @@ class Context:
             cache_stride_h, cache_rows, _ptr(kv_len), _ptr(n_acc), _ptr(acc_idx), _ptr(acc_tok),
             _ptr(bonus_tok))
         self._check(rc, "jk_accept_and_compact")
+
+
+class Mx8:
+    """8-bit rows: codes u8 [rows, n] and their scale tiles (include/jakiro.h has the layout)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dim() != 2 or codes.element_size() != 1 or not codes.is_contiguous():
+            raise ValueError("codes: expected a contiguous 8-bit tensor [rows, n]")
+        n = lib().jk_row_scale_bytes(codes.shape[0], codes.shape[1])
+        if n == 0:
+            raise ValueError("8-bit rows have a multiple of 32 elements")
+        if scales.element_size() != 1 or scales.numel() != n or not scales.is_contiguous():
+            raise ValueError(f"scales: expected {n} contiguous bytes")
+        if scales.device != codes.device or not codes.is_cuda:
+            raise ValueError("codes and scales must be on one CUDA device")
+        self.codes, self.scales, self.shape = codes, scales, codes.shape
+        self.ptrs = (codes.data_ptr(), scales.data_ptr())
+
+    @classmethod
+    def empty(cls, rows, n, device="cuda") -> "Mx8":
+        u8 = dict(dtype=torch.uint8, device=device)
+        return cls(torch.empty(rows, n, **u8), torch.empty(max(1, lib().jk_row_scale_bytes(rows, n)), **u8))
+
+
+class Linear:
+    """The weights of one projection and its epilogue (jk_linear_op): w [n_out, n_in] in the context's type or as Mx8,
+    bias [n_out]; with w_up (and bias_up) a gated block, act(x w^T + bias) * (x w_up^T + bias_up)."""
+
+    def __init__(self, ctx: Context, w, bias=None, act="none", w_up=None, bias_up=None):
+        self.mx8 = isinstance(w, Mx8)
+        self.kind, self.keep = ctx.tdtype, (w, bias, w_up, bias_up)
+        self.n_out, self.n_in = w.shape
+        if act not in ACTS:
+            raise ValueError(f"act: expected one of {sorted(ACTS)}")
+        if bias_up is not None and w_up is None:
+            raise ValueError("bias_up is the bias of w_up")
+        ptrs = []
+        for name, m in (("w", w), ("w_up", w_up)):
+            if m is None:
+                ptrs.append((None, None))
+            elif isinstance(m, Mx8) is not self.mx8 or tuple(m.shape) != (self.n_out, self.n_in):
+                raise ValueError("w and w_up must be of one shape and type")
+            elif self.mx8:
+                ptrs.append(m.ptrs)
+            else:
+                ptrs.append((ctx._dense(m, (self.n_out, self.n_in), name), None))
+        for name, b in (("bias", bias), ("bias_up", bias_up)):
+            ctx._dense(b, (self.n_out,), name)
+        self.struct = JkLinearOp(self.n_out, self.n_in, JK_ROWS_MX8 if self.mx8 else JK_ROWS_T, ACTS[act],
+                                 *ptrs[0], _ptr(bias), *ptrs[1], _ptr(bias_up))
+        self.ref = C.byref(self.struct)
 
 
 class PagedCache:
@@ -711,3 +877,54 @@ def run_draft_chained(ctx: Context, bufs: StepBuffers, pre: PreBuffers, weights,
         ctx.tree_finalize(B, bufs.pool_struct, bufs.pool_n, root_tok, w.tree_size,
                           bufs.tree["tok"], bufs.tree["parent"], bufs.tree["depth"],
                           bufs.tree["branch"], bufs.tree["qslot"], bufs.anc)
+
+
+class TargetLayer:
+    """The weights of one target layer: norms T [H]; Linear objects qkv ([(Hq + 2 Hkv) d, H]), o ([H, Hq d], no
+    activation), up (gated, [I, H]) and down ([H, I]).  All four projections take T, or all take Mx8."""
+
+    def __init__(self, norm1, qkv: Linear, o: Linear, norm2, up: Linear, down: Linear):
+        if len({p.mx8 for p in (qkv, o, up, down)}) != 1:
+            raise ValueError("the projections of a layer take one type of rows")
+        self.norm1, self.qkv, self.o, self.norm2, self.up, self.down = norm1, qkv, o, norm2, up, down
+
+
+class LayerBuffers:
+    """Device buffers of run_target_layer for batch x tree_size rows, shared by all layers of a pass."""
+
+    def __init__(self, ctx: Context, layer: TargetLayer, batch, tree_size, device="cuda"):
+        c, R = ctx.cfg, batch * tree_size
+        T = dict(dtype=ctx.tdtype, device=device)
+        rows = Mx8.empty if layer.qkv.mx8 else lambda r, n: torch.empty(r, n, **T)
+        self.xn = rows(R, layer.qkv.n_in)
+        self.qkv = torch.empty(R, layer.qkv.n_out, **T)
+        self.pos = torch.empty(batch, tree_size, dtype=torch.int32, device=device)
+        self.q = torch.empty(batch, tree_size, c.n_q_heads, c.head_dim, **T)
+        self.att = torch.empty(batch, tree_size, c.n_q_heads, c.head_dim, **T)
+        self.att_rows = rows(R, layer.o.n_in) if layer.qkv.mx8 else self.att.view(R, -1)
+        self.h = rows(R, layer.up.n_out)
+
+
+def run_target_layer(ctx: Context, layer: TargetLayer, bufs: LayerBuffers, batch, tree_size, x, parent, depth,
+                     rope_theta, scale, kv_len, k, v, paged: Optional[PagedCache] = None, index=0):
+    """One target layer over the tree's nodes: x T [batch * tree_size, H], the residual stream, is updated in place.
+    Without `paged`, k and v are the layer's caches [batch, Hkv, rows, d] and the nodes' K and V go to rows kv_len
+    on; with it they are the tree arrays [batch, Hkv, >= tree_size, d] of layer `index`, and kv_len is
+    paged.kv_len."""
+    mx8 = layer.qkv.mx8
+    out = {"out_mx8": bufs.xn} if mx8 else {"out": bufs.xn}
+    ctx.add_norm(x, layer.norm1, **out)
+    ctx.linear(layer.qkv, bufs.xn, bufs.qkv)
+    torch.add(kv_len[:batch, None], depth, out=bufs.pos)
+    ctx.rope_qkv(batch, tree_size, bufs.qkv, bufs.pos, (ctx.cfg.head_dim // 2,), rope_theta, bufs.q, k, v,
+                 first_row=kv_len if paged is None else None)
+    if paged is None:
+        ctx.tree_verify_attn(batch, tree_size, bufs.q, k, v, kv_len, parent, scale, bufs.att)
+    else:
+        ctx.tree_verify_attn_paged(paged, index, batch, tree_size, bufs.q, k, v, parent, scale, bufs.att)
+    if mx8:
+        ctx.quantize_mx8(bufs.att.view(x.shape[0], -1), bufs.att_rows)
+    ctx.linear(layer.o, bufs.att_rows, x, residual=x)
+    ctx.add_norm(x, layer.norm2, **out)
+    ctx.linear(layer.up, bufs.xn, bufs.h)
+    ctx.linear(layer.down, bufs.h, x, residual=x)

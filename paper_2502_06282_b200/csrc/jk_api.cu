@@ -259,7 +259,8 @@ extern "C" const char* jk_profile_stage_name(int32_t stage) {
       "router", "expert_gate_up", "expert_down", "branch_features", "lm_head", "topk_partial",
       "expand_finish", "tree_finalize", "tree_attn", "attn_combine", "row_stats", "accept_walk",
       "kv_compact", "gemm_fixup", "pre_gather", "pre_gemm", "pre_fixup", "pre_rope", "pre_attn",
-      "pre_attn_combine", "paged_plan", "paged_move", "paged_attn", "paged_attn_combine", "sample"};
+      "pre_attn_combine", "paged_plan", "paged_move", "paged_attn", "paged_attn_combine", "sample",
+      "norm", "linear"};
   return (stage >= 0 && stage < JK_N_STAGES) ? names[stage] : "?";
 }
 

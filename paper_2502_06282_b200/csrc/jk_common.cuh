@@ -68,7 +68,7 @@ enum jk_stage {
   JK_ST_FINISH, JK_ST_FINALIZE, JK_ST_ATTN, JK_ST_ATTN_COMBINE, JK_ST_ROWSTATS, JK_ST_WALK,
   JK_ST_COMPACT, JK_ST_GEMM_FIXUP, JK_ST_PRE_GATHER, JK_ST_PRE_GEMM, JK_ST_PRE_FIXUP,
   JK_ST_PRE_ROPE, JK_ST_PRE_ATTN, JK_ST_PRE_ATTN_COMBINE, JK_ST_PAGED_PLAN, JK_ST_PAGED_MOVE,
-  JK_ST_PAGED_ATTN, JK_ST_PAGED_COMBINE, JK_ST_SAMPLE, JK_N_STAGES
+  JK_ST_PAGED_ATTN, JK_ST_PAGED_COMBINE, JK_ST_SAMPLE, JK_ST_NORM, JK_ST_LINEAR, JK_N_STAGES
 };
 struct jk_prof {
   cudaEvent_t* ev;        // 2 * cap events

@@ -1,0 +1,561 @@
+"""A target layer's steps around its attention against their 64-bit definitions: norm with the residual's addition and
+8-bit rows, matrix products with their epilogue, rotary positions; and the whole layer.
+
+Tolerances count roundings.  A value stored in a type is off by at most half a step (f32 2^-24, bf16 2^-8, e4m3
+2^-4 relative, 2^-10 scales at the bottom of its grid).  A sum of K products in f32 is off by at most K steps of 2^-23
+of the sum of their magnitudes (every addition may round, and a tensor core may cut instead of rounding)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as lo
+from paper_2502_06282_b200 import binding as jk
+from paper_2502_06282_b200 import synth
+from tests.jk_testutil import Guard, dev, host
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+TD = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def make_ctx(dtype, Hq=1, Hkv=1, d=64, hidden=8, eps=1e-5, **kw):
+    kw = {**dict(max_batch=1, max_tree=1), **kw}
+    return jk.Context(hidden=hidden, n_experts=1, top_k=1, inter=8, vocab=8, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=d,
+                      max_depth=1, max_frontier=1, k_per_expert=1, dtype=dtype, rms_eps=eps, **kw)
+
+
+def store(a, dtype):
+    return synth.store_round(np.asarray(a, dtype=np.float32), dtype).astype(np.float64)
+
+
+def to_dev(a, dtype):
+    return dev(np.asarray(a, dtype=np.float32)).to(TD[dtype])
+
+
+def mx8_guard(g, R, n):
+    n_b = jk.lib().jk_row_scale_bytes(R, n)
+    return jk.Mx8(g.alloc((R, n), torch.uint8), g.alloc((n_b,), torch.uint8))
+
+
+def mx8_of(codes, e):
+    """An array of the library's layout from the model's codes and exponents; bytes of no row or block are 0xFF."""
+    R, n = codes.shape
+    c = dev(codes.astype(np.float32)).to(torch.float8_e4m3fn).view(torch.uint8)
+    s = np.full(jk.lib().jk_row_scale_bytes(R, n), 255, dtype=np.uint8)
+    s[lo.tile_index(R, n).reshape(-1)] = (e + 127).reshape(-1).astype(np.uint8)
+    return jk.Mx8(c.contiguous(), dev(s))
+
+
+def read_mx8(m):
+    """(codes' values, exponents) of a device array; the bytes that belong to no row or block are untouched."""
+    R, n = m.shape
+    codes = m.codes.view(torch.float8_e4m3fn).float().cpu().numpy().astype(np.float64)
+    raw = m.scales.cpu().numpy()
+    at = lo.tile_index(R, n)
+    rest = np.ones(raw.size, bool)
+    rest[at.reshape(-1)] = False
+    assert np.all(raw[rest] == Guard.POISON), "a scale byte that belongs to no block was written"
+    return codes, raw[at].astype(np.int64) - 127
+
+
+def check_mx8(m, y, err):
+    """y the exact rows, err what the f32 values may be off by: the scale is that of a value within err, the codes are
+    off by half a step of the grid."""
+    codes, e = read_mx8(m)
+    fine = np.isfinite(y)
+    mag = np.where(fine, np.abs(y), 0.0)
+    low = lo.scale_exponents(np.maximum(mag - np.where(fine, err, 0), 0.0))
+    high = lo.scale_exponents(mag + np.where(fine, err, 0))
+    assert np.all((e >= low) & (e <= high))
+    got, s = lo.dequantize(codes, e), np.repeat(np.exp2(e.astype(np.float64)), 32, axis=1)
+    assert np.array_equal(np.isnan(got), np.isnan(y))
+    inf = np.isinf(y)
+    assert np.all(codes[inf] == np.sign(y[inf]) * 448.0)
+    off = np.abs(got - np.where(fine, y, 0.0))
+    assert np.all(off[fine] <= (2.0 ** -4 * (np.abs(y) + err) + 2.0 ** -10 * s + err)[fine])
+
+
+def check_t(t, y, err, dtype):
+    got = host(t).astype(np.float64)
+    fine = np.isfinite(y)
+    assert np.array_equal(np.isnan(got), np.isnan(y)) and np.array_equal(got[np.isinf(y)], y[np.isinf(y)])
+    bound = HALF[dtype] * (np.abs(np.where(fine, y, 0.0)) + err) + err + 2.0 ** -133
+    off = np.abs(got - y)
+    assert np.all(off[fine] <= bound[fine]), float(np.max((off / bound)[fine]))
+
+
+# ------------------------------------------------------------------------------------------ norm
+def run_norm(dtype, R, n, add=True, weight=True, outs=("sum", "out", "mx8"), eps=1e-5, x=None, seed=0):
+    rng = np.random.default_rng(seed + R * 7 + n)
+    ctx, g = make_ctx(dtype, eps=eps), Guard()
+    x = store(rng.standard_normal((R, n)) * np.exp(rng.standard_normal((R, 1))) if x is None else x, dtype)
+    delta = store(rng.standard_normal((R, n)), dtype) if add else None
+    w = store(1 + 0.2 * rng.standard_normal(n), dtype) if weight else None
+    o_sum = g.alloc((R, n), TD[dtype]) if "sum" in outs else None
+    o = g.alloc((R, n), TD[dtype]) if "out" in outs else None
+    m = mx8_guard(g, R, n) if "mx8" in outs else None
+    ctx.add_norm(to_dev(x, dtype), None if w is None else to_dev(w, dtype), None if delta is None else to_dev(delta, dtype),
+                 o_sum, o, m)
+    g.check()
+    with np.errstate(invalid="ignore", over="ignore"):
+        s, y = lo.add_norm(x, delta, w, float(np.float32(eps)))
+    # s: one rounding.  The sum of squares: 8 + 4 + 5 + 5 + 2 steps in a row and a half step for each s, halved by the
+    # root; root, quotient and two products four half steps
+    rel = (24 + 2 + 4) * 2.0 ** -24
+    err = np.where(np.isfinite(y), np.abs(y) * rel, 0.0)
+    if delta is not None:
+        err = err + np.where(np.isfinite(s), np.abs(s), 0) * 2.0 ** -24 * np.where(np.isfinite(y / s), np.abs(y / s), 0)
+    if o_sum is not None:
+        check_t(o_sum, s, np.where(np.isfinite(s), np.abs(s) * 2.0 ** -24, 0), dtype)
+    if o is not None:
+        check_t(o, y, err, dtype)
+    if m is not None:
+        check_mx8(m, y, err)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,n", [(1, 32), (3, 96), (129, 512), (2, 4096), (5, 5120), (300, 8192), (2, 16416), (3, 32768)])
+def test_norm(R, n, dtype):
+    run_norm(dtype, R, n)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [8, 24, 1000, 4104])
+def test_norm_widths_without_blocks(n, dtype):
+    run_norm(dtype, 5, n, outs=("sum", "out"))
+
+
+@pytest.mark.parametrize("add,weight,outs", [(False, True, ("out",)), (False, False, ("mx8",)), (True, False, ("sum",)),
+                                             (True, True, ("sum", "mx8")), (False, True, ("sum", "out"))])
+def test_norm_forms(add, weight, outs):
+    run_norm("bf16", 7, 256, add, weight, outs, eps=0.5)
+
+
+def test_norm_of_zeros_infinities_and_nan():
+    x = np.random.default_rng(1).standard_normal((6, 128))
+    x[0] = 0.0
+    x[1, 5] = np.nan
+    x[2, 7] = np.inf
+    x[3] *= 1e-30
+    x[4, :64] = 0.0
+    run_norm("bf16", 6, 128, add=False, x=x)
+
+
+def test_norm_in_place():
+    rng = np.random.default_rng(4)
+    ctx = make_ctx("bf16")
+    x, d, w = (to_dev(rng.standard_normal(s), "bf16") for s in ((33, 512), (33, 512), (512,)))
+    s, o = torch.empty_like(x), torch.empty_like(x)
+    ctx.add_norm(x, w, d, s, o)
+    x2, d2 = x.clone(), d.clone()
+    ctx.add_norm(x2, w, d2, x2, d2)
+    assert torch.equal(x2, s) and torch.equal(d2, o)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,n,wide", [(1, 32, 0), (130, 160, 8), (257, 1376, 0), (3, 28672, 64)])
+def test_quantize(R, n, wide, dtype):
+    """Exact: a scale is a power of two, a value is rounded once."""
+    rng = np.random.default_rng(n)
+    x = rng.standard_normal((R, n)) * np.exp2(rng.integers(-60, 40, (R, n // 32)).repeat(32, 1).astype(np.float64))
+    x[0, :32] = 0.0
+    x[-1, 3], x[-1, 4], x[-1, 5] = np.inf, -np.inf, np.nan
+    x[0, -32:] = 448.0 * 2.0 ** rng.integers(-3, 3)      # on the border of a scale
+    x = store(x, dtype)
+    room = torch.full((R, n + wide), float("nan"), dtype=TD[dtype], device="cuda")
+    room[:, :n] = to_dev(x, dtype)
+    g, ctx = Guard(), make_ctx(dtype)
+    m = mx8_guard(g, R, n)
+    ctx.quantize_mx8(room[:, :n], m)
+    g.check()
+    codes, e = read_mx8(m)
+    want, we = lo.quantize(x)
+    assert np.array_equal(e, we)
+    assert np.array_equal(codes, want, equal_nan=True)
+
+
+# ------------------------------------------------------------------------------------------ product
+def operands(rng, R, N, K, kind, dtype):
+    """x, w as f64 values and as device arrays."""
+    x = rng.standard_normal((R, K)) * np.exp(0.5 * rng.standard_normal((1, K)))
+    w = 0.1 * rng.standard_normal((N, K))
+    if kind == "mx8":
+        (xc, xe), (wc, we) = lo.quantize(x), lo.quantize(w)
+        return lo.dequantize(xc, xe), lo.dequantize(wc, we), mx8_of(xc, xe), mx8_of(wc, we)
+    x, w = store(x, dtype), store(w, dtype)
+    return x, w, to_dev(x, dtype), to_dev(w, dtype)
+
+
+def run_linear(R, N, K, kind="T", dtype="bf16", gated=False, act="none", bias=False, residual=False, out="T", wide=0,
+               in_place=False, seed=0, tensor=True):
+    rng = np.random.default_rng(seed + R + 3 * N + 5 * K)
+    ctx, g = make_ctx(dtype), Guard()
+    ctx.set_tensor_path(tensor)
+    x, w, xd, wd = operands(rng, R, N, K, kind, dtype)
+    wu = bu = wud = None
+    if gated:
+        _, wu, _, wud = operands(rng, 1, N, K, kind, dtype)
+    b = store(rng.standard_normal(N), dtype) if bias else None
+    bu = store(rng.standard_normal(N), dtype) if bias and gated else None
+    res = store(3 * rng.standard_normal((R, N)), dtype) if residual else None
+    if wide and kind == "T":
+        room = torch.full((R, K + wide), float("nan"), dtype=TD[dtype], device="cuda")
+        room[:, :K] = xd
+        xd = room[:, :K]
+    dv = lambda a: None if a is None else to_dev(a, dtype)
+    op = jk.Linear(ctx, wd, bias=dv(b), act=act, w_up=wud, bias_up=dv(bu))
+    rd = dv(res)
+    if out == "mx8":
+        od = mx8_guard(g, R, N)
+    else:
+        room = g.alloc((R, N + wide), torch.float32 if out == "f32" else TD[dtype])
+        od = room[:, :N]
+        if in_place:
+            od.copy_(rd)
+            rd = od
+    ctx.linear(op, xd, od, residual=rd)
+    g.check()
+    assert ctx.read_status() == 0
+    if wide and out != "mx8":
+        assert bool((room[:, N:].contiguous().view(torch.uint8) == Guard.POISON).all()), "wrote between the rows"
+    y = lo.linear(x, w, b, act, wu, bu, res)
+    ax = np.abs(x)
+    ez = (K + 4) * 2.0 ** -23 * (ax @ np.abs(w).T + (0 if b is None else np.abs(b)))
+    z = lo.linear(x, w, b)
+    a = lo.act(z, act)
+    # SiLU and GELU have slopes below 1.13; what the functions themselves are off by is below 2^-19 of |z| + 1
+    e = 1.13 * ez + (2.0 ** -19 * (np.abs(a) + 2.0 ** -20) if act != "none" else 0.0)
+    if gated:
+        u = lo.linear(x, wu, bu)
+        eu = (K + 4) * 2.0 ** -23 * (ax @ np.abs(wu).T + (0 if bu is None else np.abs(bu)))
+        e = e * np.abs(u) + np.abs(a) * eu + e * eu + 2.0 ** -23 * np.abs(a * u)
+    e = e + 2.0 ** -23 * (np.abs(y) + (0 if res is None else np.abs(res)))
+    if out == "mx8":
+        check_mx8(od, y, e)
+    else:
+        check_t(od, y, e, "f32" if out == "f32" else dtype)
+    return od
+
+
+ROWS = [1, 2, 15, 16, 17, 60, 127, 128, 129, 240, 256, 257, 480, 513]
+
+
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("R", ROWS)
+def test_linear_rows(R, kind):
+    run_linear(R, 160, 416, kind, residual=True)
+
+
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("R", [1, 17, 60, 129, 257, 513])
+def test_gated_rows(R, kind):
+    run_linear(R, 160, 416, kind, gated=True, act="silu", out="mx8")
+
+
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("N", [1, 7, 32, 127, 128, 129, 255, 1000, 2053])
+def test_linear_outputs(N, kind):
+    run_linear(60, N, 256, kind, bias=True, residual=True, act="gelu")
+    run_linear(3, N, 256, kind, gated=True, bias=True, act="silu")
+
+
+@pytest.mark.parametrize("kind,K", [("T", 8), ("T", 24), ("T", 72), ("T", 1376), ("T", 5000), ("T", 14336),
+                                    ("mx8", 32), ("mx8", 96), ("mx8", 160), ("mx8", 1376), ("mx8", 14336)])
+def test_linear_inner(kind, K):
+    run_linear(33, 200, K, kind, residual=True)
+    run_linear(5, 96, K, kind, gated=True, act="silu", out="mx8")
+
+
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("out", ["T", "f32", "mx8"])
+def test_linear_epilogues(kind, act, gated, out):
+    run_linear(70, 288, 192, kind, gated=gated, act=act, bias=True, residual=True, out=out)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+def test_linear_many_tiles(kind, gated):
+    """More tiles than SMs, and tiles whose sum is split."""
+    run_linear(300, 5000 if not gated else 4992, 640, kind, gated=gated, act="silu", out="mx8" if gated else "T")
+    run_linear(31, 4096, 2048, kind, gated=gated, bias=True, residual=True)
+
+
+@pytest.mark.parametrize("R,N", [(1, 97), (60, 130), (300, 97)])
+def test_linear_strides(R, N):
+    run_linear(R, N, 136, wide=24, residual=True)
+    run_linear(R, N, 136, wide=8, residual=True, in_place=True)
+    run_linear(R, N, 136, wide=8, residual=True, out="f32")
+
+
+@pytest.mark.parametrize("gated,act,out", [(False, "none", "T"), (True, "silu", "T"), (False, "gelu", "mx8"),
+                                           (True, "none", "mx8")])
+@pytest.mark.parametrize("R,N,K", [(1, 32, 8), (16, 1376, 512), (33, 96, 1000), (130, 64, 40)])
+def test_linear_f32(R, N, K, gated, act, out):
+    run_linear(R, N, K, dtype="f32", gated=gated, act=act, bias=True, residual=True, out=out, wide=4 if R < 20 else 0)
+
+
+@pytest.mark.parametrize("dtype,tensor", [("f32", True), ("bf16", False)])
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+def test_linear_cuda_cores(kind, dtype, tensor):
+    run_linear(37, 160, 352, kind, dtype=dtype, gated=True, act="silu", out="T", bias=True, tensor=tensor)
+    run_linear(37, 160, 352, kind, dtype=dtype, out="mx8", residual=True, tensor=tensor)
+
+
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+def test_linear_nan_and_infinities_stay_in_their_row(kind):
+    """A row of x with a NaN, and one with the type's largest value, reach no other row; padding reaches none."""
+    rng = np.random.default_rng(5)
+    R, N, K = 40, 96, 160
+    x, w, _, wd = operands(rng, R, N, K, kind, "bf16")
+    ctx = make_ctx("bf16")
+    out = torch.empty(R, N, dtype=torch.bfloat16, device="cuda")
+
+    def product(a):
+        xd = mx8_of(*lo.quantize(a)) if kind == "mx8" else to_dev(a, "bf16")
+        ctx.linear(jk.Linear(ctx, wd), xd, out)
+        return host(out)
+
+    want = product(x)
+    y = x.copy()
+    y[7, 3] = np.nan
+    y[20, :] = 448.0 * 2.0 ** 100
+    got = product(y)
+    rest = [r for r in range(R) if r not in (7, 20)]
+    assert np.array_equal(got[rest], want[rest])
+    assert np.all(np.isnan(got[7]))
+
+
+def test_linear_same_bits_every_time_replayed_and_on_another_stream():
+    rng = np.random.default_rng(6)
+    R, N, K = 60, 1000, 2048
+    ctx = make_ctx("bf16")
+    for kind in ("T", "mx8"):
+        x, w, xd, wd = operands(rng, R, N, K, kind, "bf16")
+        op = jk.Linear(ctx, wd)
+        outs = [torch.empty(R, N, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+        ctx.linear(op, xd, outs[0])
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            ctx.linear(op, xd, outs[1])
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(3):
+                ctx.linear(op, xd, outs[2])
+        for _ in range(4):
+            outs[2].zero_()
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    assert ctx.read_status() == 0
+
+
+def test_linear_chain_without_waiting():
+    """Calls in a row on one stream, each reading what the one before wrote, against the same calls one by one."""
+    rng = np.random.default_rng(7)
+    R, H, I = 48, 256, 704
+    ctx = make_ctx("bf16")
+    up = jk.Linear(ctx, operands(rng, 1, I, H, "mx8", "bf16")[3], act="silu", w_up=operands(rng, 1, I, H, "mx8", "bf16")[3])
+    down = jk.Linear(ctx, operands(rng, 1, H, I, "mx8", "bf16")[3])
+    x0 = to_dev(rng.standard_normal((R, H)), "bf16")
+    res = []
+    for wait in (False, True):
+        x, xn, h = x0.clone(), jk.Mx8.empty(R, H), jk.Mx8.empty(R, I)
+        torch.cuda.synchronize()
+        for _ in range(12):
+            for call in (lambda: ctx.add_norm(x, out_mx8=xn), lambda: ctx.linear(up, xn, h),
+                         lambda: ctx.linear(down, h, x, residual=x)):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        res.append(x)
+    assert torch.equal(*res)
+
+
+# ------------------------------------------------------------------------------------------ rotary positions
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hq,Hkv,d", [(1, 1, 64), (8, 2, 128), (5, 5, 64), (40, 40, 128)])
+@pytest.mark.parametrize("B,M,sections", [(1, 1, None), (3, 7, (0.25, 0.75)), (2, 61, (0.25, 0.375, 0.375)),
+                                          (2, 5, (0.0, 0.5, 0.25, 0.25))])
+def test_rope(B, M, sections, Hq, Hkv, d, dtype):
+    rng = np.random.default_rng(B * 100 + M + Hq)
+    half = d // 2
+    sec = (half,) if sections is None else tuple(int(s * half) for s in sections)
+    A, theta, wide = len(sec), (10000.0, 500000.0)[M % 2], 16 * (M % 3)
+    ctx, g = make_ctx(dtype, Hq, Hkv, d), Guard()
+    W = (Hq + 2 * Hkv) * d
+    x = store(rng.standard_normal((B, M, W)), dtype)
+    pos = rng.integers(0, 1 << 20, (B, M, A)).astype(np.int32)
+    room = torch.full((B, M, W + wide), float("nan"), dtype=TD[dtype], device="cuda")
+    room[..., :W] = to_dev(x, dtype)
+    rows, first = M + 5, (np.arange(B) * 2 % 6).astype(np.int32)
+    q = g.alloc((B, M, Hq, d), TD[dtype])
+    k, v = (g.alloc((B, Hkv, rows, d), TD[dtype]) for _ in range(2))
+    ctx.rope_qkv(B, M, room[..., :W], dev(pos if A > 1 else pos[..., 0]), sec, theta, q, k, v, first_row=dev(first))
+    g.check()
+    assert ctx.read_status() == 0
+    wq, wk, wv = lo.rope(x, pos, sec, float(np.float32(theta)), Hq, Hkv, d)
+    # angle: 64 bits (2^20 2^-53 at most), reduced to 32 (2^-24 of pi); sine and cosine 2 units; two products and a sum
+    mag = np.abs(x).max()
+    err = 2 * mag * (np.pi * 2.0 ** -24 + 2.0 ** -22 + 2.0 ** -23)
+    check_t(q, wq, np.full(wq.shape, err), dtype)
+    for b in range(B):
+        r0 = int(first[b])
+        check_t(k[b, :, r0:r0 + M], wk[b], np.full(wk[b].shape, err), dtype)
+        assert np.array_equal(host(v[b, :, r0:r0 + M]), wv[b].astype(np.float32))
+        for t in (k, v):
+            other = torch.cat([t[b, :, :r0], t[b, :, r0 + M:]], 1).contiguous().view(torch.uint8)
+            assert bool((other == Guard.POISON).all()), "rows beside the tokens' were written"
+
+
+def test_rope_refuses_rows_and_positions_on_the_device():
+    ctx = make_ctx("bf16", 2, 2, 64)
+    qkv = torch.randn(2, 3, 6 * 64, device="cuda").bfloat16()
+    pos = torch.ones(2, 3, dtype=torch.int32, device="cuda")
+    for first, bad_pos, lost in (([0, 2], None, 1), ([-1, 0], None, 0), ([0, 0], (1, 2), None)):
+        q = torch.full((2, 3, 2, 64), 7.0, device="cuda", dtype=torch.bfloat16)
+        k, v = (torch.full((2, 2, 4, 64), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+        p = pos.clone()
+        if bad_pos:
+            p[bad_pos] = -1
+        ctx.rope_qkv(2, 3, qkv, p, (32,), 10000.0, q, k, v, first_row=torch.tensor(first, dtype=torch.int32, device="cuda"))
+        assert ctx.read_status() == jk.ERR["BOUNDS"]
+        if lost is not None:
+            assert bool((k[lost] == 7).all()) and bool((v[lost] == 7).all())
+            assert not bool((k[1 - lost] == 7).all())
+        else:
+            assert bool((k[1, :, 2] == 7).all()) and bool((v[1, :, 2] == 7).all()) and bool((q[1, 2] == 7).all())
+            assert not bool((k[1, :, 1] == 7).any())
+    ctx.rope_qkv(2, 3, qkv, pos, (32,), 10000.0, q, k, v)
+    assert ctx.read_status() == 0
+
+
+def test_rope_agrees_with_verify_qkv():
+    """Projection by jk_linear and placing by jk_rope_qkv give what jk_verify_qkv gives, but for the projection's own
+    rounding (qkv passes through T once: half a step of each of the two elements of a pair, and half a step at the end)."""
+    rng = np.random.default_rng(9)
+    B, M, Hq, Hkv, d, H = 2, 9, 4, 2, 64, 128
+    ctx = make_ctx("bf16", Hq, Hkv, d, hidden=H, max_batch=B, max_tree=M)
+    w = to_dev(0.1 * rng.standard_normal(((Hq + 2 * Hkv) * d, H)), "bf16")
+    x = to_dev(rng.standard_normal((B, M, H)), "bf16")
+    depth = dev(rng.integers(0, 5, (B, M)).astype(np.int32))
+    kv_len = dev(np.array([3, 11], dtype=np.int32))
+    new = lambda: [torch.zeros(s, device="cuda", dtype=torch.bfloat16) for s in ((B, M, Hq, d), (B, Hkv, 24, d), (B, Hkv, 24, d))]
+    a, b = new(), new()
+    ctx.verify_qkv(w, B, M, x, depth, *a, kv_len, 10000.0)
+    qkv = torch.empty(B * M, w.shape[0], device="cuda", dtype=torch.bfloat16)
+    ctx.linear(jk.Linear(ctx, w), x.view(B * M, H), qkv)
+    ctx.rope_qkv(B, M, qkv, kv_len[:, None] + depth, (32,), 10000.0, *b, first_row=kv_len)
+    assert ctx.read_status() == 0
+    top = float(qkv.float().abs().max())
+    for s, t in zip(a, b):
+        assert float((s.float() - t.float()).abs().max()) <= 4 * 2.0 ** -8 * top
+
+
+# ------------------------------------------------------------------------------------------ the whole layer
+def exact_layer(x, p, parent, depth, kv_len, kc, vc, scale, Hq, Hkv, d, mx8, eps):
+    """The layer in 64 bits; with mx8 its rows are quantised where the library's are."""
+    q8 = (lambda a: lo.dequantize(*lo.quantize(a))) if mx8 else (lambda a: a)
+    B, M = depth.shape
+    _, xn = lo.add_norm(x, None, p["norm1"], eps)
+    qkv = lo.linear(q8(xn), p["qkv"])
+    q, k, v = lo.rope(qkv.reshape(B, M, -1), (kv_len[:, None] + depth)[..., None], (d // 2,), 10000.0, Hq, Hkv, d)
+    att = np.empty((B, M, Hq, d))
+    for b in range(B):
+        n = int(kv_len[b])
+        vis = np.zeros((M, n + M), bool)
+        vis[:, :n] = True
+        for i in range(M):
+            j = i
+            while j >= 0:
+                vis[i, n + j] = True
+                j = int(parent[b, j])
+        for h in range(Hq):
+            g = h // (Hq // Hkv)
+            K = np.concatenate([kc[b, g, :n], k[b, g]])
+            V = np.concatenate([vc[b, g, :n], v[b, g]])
+            s = np.where(vis, q[b, :, h] @ K.T * scale, -np.inf)
+            s = np.exp(s - s.max(1, keepdims=True))
+            att[b, :, h] = (s / s.sum(1, keepdims=True)) @ V
+    x = lo.linear(q8(att.reshape(B * M, -1)), p["o"], residual=x)
+    _, xn = lo.add_norm(x, None, p["norm2"], eps)
+    h = lo.linear(q8(xn), p["gate"], None, "silu", p["up"])
+    return lo.linear(q8(h), p["down"], residual=x)
+
+
+@pytest.mark.parametrize("mx8", [False, True])
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("dtype,B,M", [("bf16", 2, 13), ("bf16", 1, 1), ("bf16", 4, 60), ("f32", 2, 7)])
+def test_target_layer(dtype, B, M, paged, mx8):
+    """The calls as a pass makes them, twice in a row (two layers), eager and replayed from a graph."""
+    rng = np.random.default_rng(B * M + mx8)
+    H, I, Hq, Hkv, d, P = 256, 704, 4, 2, 64, 70
+    ctx = make_ctx(dtype, Hq, Hkv, d, hidden=H, max_batch=B, max_tree=M)
+    p = {"norm1": 1 + 0.1 * rng.standard_normal(H), "norm2": 1 + 0.1 * rng.standard_normal(H)}
+    for n, s in (("qkv", ((Hq + 2 * Hkv) * d, H)), ("o", (H, Hq * d)), ("gate", (I, H)), ("up", (I, H)), ("down", (H, I))):
+        p[n] = rng.standard_normal(s) / np.sqrt(s[1])
+        p[n] = lo.dequantize(*lo.quantize(p[n])) if mx8 else store(p[n], dtype)
+    p["norm1"], p["norm2"] = store(p["norm1"], dtype), store(p["norm2"], dtype)
+    dv = (lambda a: mx8_of(*lo.quantize(a))) if mx8 else (lambda a: to_dev(a, dtype))
+    layer = jk.TargetLayer(to_dev(p["norm1"], dtype), jk.Linear(ctx, dv(p["qkv"])), jk.Linear(ctx, dv(p["o"])),
+                           to_dev(p["norm2"], dtype), jk.Linear(ctx, dv(p["gate"]), act="silu", w_up=dv(p["up"])),
+                           jk.Linear(ctx, dv(p["down"])))
+    bufs = jk.LayerBuffers(ctx, layer, B, M)
+    x0 = store(rng.standard_normal((B * M, H)), dtype)
+    kv_len = np.array([P - 3 * b for b in range(B)], dtype=np.int32)
+    parent = np.array([[-1] + [int(rng.integers(0, i)) for i in range(1, M)] for _ in range(B)], dtype=np.int32)
+    depth = np.zeros((B, M), dtype=np.int32)
+    for i in range(1, M):
+        depth[:, i] = depth[np.arange(B), parent[:, i]] + 1
+    kc, vc = (store(rng.standard_normal((B, Hkv, P + M, d)), dtype) for _ in range(2))
+    want = x0
+    if paged:
+        cache = jk.PagedCache(ctx, n_layers=1, n_pages=B * 6, page_size=16, max_seqs=B, max_pages=8)
+        kd, vd = to_dev(kc, dtype), to_dev(vc, dtype)
+        ptr = lambda t: torch.tensor([t.data_ptr()], dtype=torch.int64, device="cuda")
+        ctx.paged_import(cache, B, dev(kv_len), 0, 1, ptr(kd), ptr(vd), kd.stride(0), kd.stride(1), P + M)
+        ps, lens = 16, kv_len // 16 * 16
+        for t in (kc, vc):                      # what the pages hold: one scale per page and head
+            for b in range(B):
+                for h in range(Hkv):
+                    for a in range(0, int(lens[b]), ps):
+                        blk = t[b, h, a:a + ps]
+                        e = lo.scale_exponents(blk.reshape(1, -1)).max()
+                        t[b, h, a:a + ps] = lo.e4m3(blk / 2.0 ** e) * 2.0 ** e
+        lengths = cache.kv_len
+        k, v = (torch.zeros(B, Hkv, M, d, dtype=TD[dtype], device="cuda") for _ in range(2))
+    else:
+        cache, lengths = None, dev(kv_len)
+        k, v = to_dev(kc, dtype), to_dev(vc, dtype)
+    for _ in range(2):
+        want = exact_layer(want, p, parent, depth, kv_len, kc, vc, 0.125, Hq, Hkv, d, mx8, 1e-5)
+    x = to_dev(x0, dtype)
+    pd, dd = dev(parent), dev(depth)
+
+    def run_pass():
+        for _ in range(2):
+            jk.run_target_layer(ctx, layer, bufs, B, M, x, pd, dd, 10000.0, 0.125, lengths, k, v, cache)
+
+    run_pass()
+    torch.cuda.synchronize()
+    assert ctx.read_status() == 0
+    got = host(x).astype(np.float64)
+    # roundings to bf16 have an rms of 2^-8 / sqrt(3); about nine of them lie one behind the other in a layer, each of
+    # at most the size of the stream: 2 * 9 * 0.00226 = 0.041 if all added up.  8-bit rows: a value that is off by
+    # 2^-8 takes the next code in one of 2^-5 / 2^-8 = 8 cases, 2^-4 off: an rms of 0.022 at four places of each layer
+    tol = {"f32": 1e-4, "bf16": 0.041}[dtype] + (2 * 4 * 0.022 if mx8 else 0.0)
+    assert np.linalg.norm(got - want) <= tol * np.linalg.norm(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run_pass()
+    for _ in range(2):
+        x.copy_(to_dev(x0, dtype))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(host(x).astype(np.float64), got)
+    assert ctx.read_status() == 0

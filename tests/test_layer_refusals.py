@@ -1,0 +1,143 @@
+"""What the calls of a target layer refuse, before anything is launched (host only: no call here reaches a device)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2502_06282_b200 import binding as jk
+
+E = jk.ERR
+X, W, OUT, SCALE, RES, BIAS = 1 << 32, 2 << 32, 3 << 32, 4 << 32, 5 << 32, 6 << 32
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2502_06282_b200 import build
+    build.build()
+    return jk.lib()
+
+
+def make_ctx(dtype="bf16", d=64):
+    return jk.Context(hidden=8, n_experts=1, top_k=1, inter=8, vocab=8, n_q_heads=4, n_kv_heads=2, head_dim=d, max_batch=1,
+                      max_tree=1, max_depth=1, max_frontier=1, k_per_expert=1, dtype=dtype, allocate=False)
+
+
+@pytest.mark.parametrize("rows,n,want", [(1, 32, 512), (128, 128, 512), (129, 128, 1024), (1, 160, 1024), (0, 32, 0),
+                                         (1, 0, 0), (1, 33, 0), (1 << 24, 32, (1 << 17) * 512), ((1 << 24) + 1, 32, 0),
+                                         (1, (1 << 20) + 32, 0), (-5, 32, 0)])
+def test_scale_bytes(lib, rows, n, want):
+    assert lib.jk_row_scale_bytes(rows, n) == want
+
+
+NORM = dict(rows=4, n=64, x=X, delta=None, weight=W, out_sum=None, out=OUT, mx8=None, scale=None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("change,code", [
+    (dict(x=None), "NULL"), (dict(out=None), "NULL"), (dict(mx8=SCALE), "NULL"), (dict(scale=SCALE), "NULL"),
+    (dict(rows=0), "SHAPE"), (dict(rows=-1), "SHAPE"), (dict(n=0), "SHAPE"), (dict(n=12), "SHAPE"),
+    (dict(n=32776), "SHAPE"), (dict(n=40, mx8=SCALE, scale=RES), "SHAPE"),
+    (dict(x=X + 8), "ALIGN"), (dict(weight=W + 2), "ALIGN"), (dict(out=OUT + 8), "ALIGN"),
+    (dict(out=X + 16), "SHAPE"), (dict(out=W), "SHAPE"), (dict(out_sum=OUT), "SHAPE"),
+    (dict(delta=RES, out=RES + 32), "SHAPE"), (dict(mx8=X, scale=SCALE), "SHAPE"), (dict(mx8=SCALE, scale=SCALE), "SHAPE")])
+def test_norm_refuses(lib, dtype, change, code):
+    a, ctx = {**NORM, **change}, make_ctx(dtype)
+    rc = lib.jk_add_norm(ctx._h, None, a["rows"], a["n"], a["x"], a["delta"], a["weight"], a["out_sum"], a["out"],
+                         a["mx8"], a["scale"])
+    assert rc == E[code]
+
+
+@pytest.mark.parametrize("rows,n,x,stride,out,scale,code", [
+    (1, 32, None, 0, OUT, SCALE, "NULL"), (1, 32, X, 0, None, SCALE, "NULL"), (1, 32, X, 0, OUT, None, "NULL"),
+    (0, 32, X, 0, OUT, SCALE, "SHAPE"), (1, 40, X, 0, OUT, SCALE, "SHAPE"), (2, 64, X, 32, OUT, SCALE, "SHAPE"),
+    (2, 64, X, 65, OUT, SCALE, "ALIGN"), (2, 64, X + 2, 0, OUT, SCALE, "ALIGN"), (2, 64, X, 0, X + 64, SCALE, "SHAPE"),
+    (2, 64, X, 0, OUT, OUT + 16, "SHAPE")])
+def test_quantize_refuses(lib, rows, n, x, stride, out, scale, code):
+    ctx = make_ctx()
+    assert lib.jk_quantize_rows(ctx._h, None, rows, n, x, stride, out, scale) == E[code]
+
+
+OP = dict(n_out=64, n_in=64, operands=0, act=0, w=W, w_scale=None, bias=None, w_up=None, w_up_scale=None, bias_up=None)
+CALL = dict(rows=4, x=X, x_scale=None, x_stride=0, residual=None, r_stride=0, out=OUT, out_type=0, out_scale=None, o_stride=0)
+MX = dict(operands=2, w_scale=SCALE, x_scale=SCALE + (1 << 20))
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(w=None), "NULL"), (dict(x=None), "NULL"), (dict(out=None), "NULL"), (dict(operands=1), "DTYPE"),
+    (dict(operands=7), "DTYPE"), (dict(out_type=3), "DTYPE"), (dict(out_type=2), "NULL"), ({**MX, "x_scale": None}, "NULL"),
+    ({**MX, "w_scale": None}, "NULL"), ({**MX, "w_up": RES}, "NULL"), (dict(act=3), "SHAPE"), (dict(act=-1), "SHAPE"),
+    (dict(bias_up=BIAS), "SHAPE"), (dict(rows=0), "SHAPE"), (dict(rows=(1 << 20) + 1), "SHAPE"), (dict(n_out=0), "SHAPE"),
+    (dict(n_in=0), "SHAPE"), (dict(n_in=20), "SHAPE"), (dict(n_in=(1 << 17) + 8), "SHAPE"), ({**MX, "n_in": 72}, "SHAPE"),
+    (dict(n_out=(1 << 20) + 1), "SHAPE"), (dict(n_out=40, out_type=2, out_scale=SCALE), "SHAPE"), (dict(x_stride=32), "SHAPE"),
+    (dict(x_stride=-64), "SHAPE"), (dict(residual=RES, r_stride=63), "SHAPE"), (dict(o_stride=63), "SHAPE"),
+    ({**MX, "x_stride": 128}, "SHAPE"), (dict(out_type=2, out_scale=SCALE, o_stride=96), "SHAPE"), (dict(x_stride=68), "ALIGN"),
+    (dict(x=X + 8), "ALIGN"), (dict(w=W + 4), "ALIGN"), (dict(bias=BIAS + 2), "ALIGN"), (dict(out=OUT + 2), "ALIGN"),
+    (dict(out=X), "SHAPE"), (dict(out=W + 128), "SHAPE"), (dict(residual=OUT + 128), "SHAPE"),
+    (dict(residual=OUT, r_stride=128), "SHAPE"), (dict(residual=OUT, out_type=1), "SHAPE"), (dict(bias=OUT + 16), "SHAPE"),
+    (dict(out_type=2, out_scale=OUT + 16), "SHAPE"), (dict(out_type=2, out_scale=X), "SHAPE"),
+    ({**MX, "out": SCALE}, "SHAPE"), ({}, "WORKSPACE"), (dict(residual=OUT), "WORKSPACE"), (MX, "WORKSPACE")])
+def test_linear_refuses(lib, change, code):
+    a, ctx = {**OP, **CALL, **change}, make_ctx()
+    op = jk.JkLinearOp(*[a[k] for k in OP])
+    rc = lib.jk_linear(ctx._h, None, C.byref(op), a["rows"], a["x"], a["x_scale"], a["x_stride"], a["residual"],
+                       a["r_stride"], a["out"], a["out_type"], a["out_scale"], a["o_stride"])
+    assert rc == E[code]
+
+
+def test_linear_refuses_null_context_and_projection(lib):
+    op, ctx = jk.JkLinearOp(*OP.values()), make_ctx()
+    tail = (4, X, None, 0, None, 0, OUT, 0, None, 0)
+    assert lib.jk_linear(None, None, C.byref(op), *tail) == E["NULL"]
+    assert lib.jk_linear(ctx._h, None, None, *tail) == E["NULL"]
+
+
+Q, K, V, POS = 7 << 32, 8 << 32, 9 << 32, 10 << 32
+ROPE = dict(batch=2, n=3, qkv=X, stride=0, pos=POS, sections=(32,), theta=1e4, q=Q, k=K, v=V, sb=2 * 640, sh=640, rows=10,
+            first=None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(qkv=None), "NULL"), (dict(pos=None), "NULL"), (dict(sections=None), "NULL"), (dict(q=None), "NULL"),
+    (dict(k=None), "NULL"), (dict(v=None), "NULL"), (dict(batch=0), "SHAPE"), (dict(batch=65536), "SHAPE"), (dict(n=0), "SHAPE"),
+    (dict(n=11), "SHAPE"), (dict(sections=()), "SHAPE"), (dict(sections=(8, 8, 8, 4, 4)), "SHAPE"), (dict(sections=(31,)), "SHAPE"),
+    (dict(sections=(40, -8)), "SHAPE"), (dict(sections=(16, 8)), "SHAPE"), (dict(theta=0.0), "SHAPE"),
+    (dict(theta=float("nan")), "SHAPE"), (dict(theta=float("inf")), "SHAPE"), (dict(stride=504), "SHAPE"),
+    (dict(stride=516), "ALIGN"), (dict(sh=632), "SHAPE"), (dict(sb=640), "SHAPE"), (dict(sb=-1280), "SHAPE"),
+    (dict(sb=1284), "ALIGN"), (dict(q=Q + 8), "ALIGN"), (dict(pos=POS + 2), "ALIGN"), (dict(first=POS + 1), "ALIGN"),
+    (dict(q=X + 512), "SHAPE"), (dict(k=X), "SHAPE"), (dict(v=K), "SHAPE"), (dict(q=K + 512), "SHAPE"), ({}, "WORKSPACE"),
+    (dict(sb=640, sh=1280), "WORKSPACE")])
+def test_rope_refuses(lib, change, code):
+    a, ctx = {**ROPE, **change}, make_ctx()
+    s = a["sections"]
+    rc = lib.jk_rope_qkv(ctx._h, None, a["batch"], a["n"], a["qkv"], a["stride"], a["pos"], 1 if s is None else len(s),
+                         None if s is None else (C.c_int32 * max(1, len(s)))(*s), a["theta"], a["q"], a["k"], a["v"], a["sb"],
+                         a["sh"], a["rows"], a["first"])
+    assert rc == E[code]
+
+
+def test_binding_refuses_other_arrays(lib):
+    """The binding's own checks, on host tensors (which it refuses as well)."""
+    ctx = make_ctx()
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="multiple of 32"):
+        jk.Mx8(torch.zeros(2, 40, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="512 contiguous bytes"):
+        jk.Mx8(torch.zeros(2, 64, dtype=torch.uint8), torch.zeros(8, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="contiguous 8-bit"):
+        jk.Mx8(torch.zeros(2, 64), torch.zeros(512, dtype=torch.uint8))
+    for bad in (torch.zeros(4, 64), bf(4, 128)[:, :64], bf(4, 64)):
+        with pytest.raises(ValueError):
+            jk.Linear(ctx, bad)
+    with pytest.raises(ValueError, match="act"):
+        jk.Linear(ctx, bf(4, 64), act="tanh")
+    with pytest.raises(ValueError, match="bias_up"):
+        jk.Linear(ctx, bf(4, 64), bias_up=bf(4))
+    for x, kw in ((bf(4, 64), {}), (torch.zeros(4, 64), {}), (bf(64), {}), (bf(4, 128)[:, ::2], {})):
+        with pytest.raises(ValueError):
+            ctx.add_norm(x, out=x, **kw)
+    with pytest.raises(ValueError):
+        ctx.rope_qkv(1, 2, bf(1, 2, 512), torch.zeros(1, 2, 2, dtype=torch.int32), (32,), 1e4, bf(1, 2, 4, 64), bf(1, 2, 2, 64),
+                     bf(1, 2, 2, 64))
+    with pytest.raises(ValueError):
+        ctx.rope_qkv(1, 2, bf(1, 3, 512), torch.zeros(1, 2, dtype=torch.int32), (32,), 1e4, bf(1, 2, 4, 64), bf(1, 2, 2, 64),
+                     bf(1, 2, 2, 64))
