@@ -7,6 +7,8 @@
 size_t jk_tc_partial_bytes(const jk_config& c);   // jk_gemm_tc.cu
 void jk_tc_destroy(jk_ctx* ctx);                  // jk_gemm_tc.cu
 size_t jk_paged_part_floats(const jk_config& c, int with_ml);   // jk_paged_tc.cu
+size_t jk_linear_part_bytes();                    // jk_linear_tc.cu
+size_t jk_linear_flag_bytes();                    // jk_linear_tc.cu
 static void prof_free(jk_ctx* ctx);
 void jk_attn_tc_destroy(jk_ctx* ctx);             // jk_attn_tc.cu
 void jk_attn_cl_destroy(jk_ctx* ctx);             // jk_attn_cl.cu
@@ -97,6 +99,8 @@ static void build_layout(const jk_config& c, jk_ws_layout* L) {
   L->pre_ao = take(Rp * qd * es);
   L->paged_o = take(jk_paged_part_floats(c, 0) * 4);
   L->paged_ml = take(jk_paged_part_floats(c, 1) * 4);
+  L->lin_part = take(c.dtype == JK_BF16 ? jk_linear_part_bytes() : 0);
+  L->lin_flag = take(jk_linear_flag_bytes());
   L->total = off;
 }
 
@@ -136,6 +140,7 @@ extern "C" int jk_set_workspace(jk_ctx* ctx, void* stream, void* dev_ptr, size_t
   jk_tc_destroy(ctx);   // tensor maps over an earlier workspace are stale
   JK_CUDA_CHECK(ctx, cudaMemsetAsync(ctx->ws + ctx->lay.status, 0, 16, (cudaStream_t)stream));
   JK_CUDA_CHECK(ctx, cudaMemsetAsync(ctx->ws + ctx->lay.gemm_cnt, 0, 16, (cudaStream_t)stream));
+  JK_CUDA_CHECK(ctx, cudaMemsetAsync(ctx->ws + ctx->lay.lin_flag, 0, jk_linear_flag_bytes(), (cudaStream_t)stream));
   return JK_OK;
 }
 

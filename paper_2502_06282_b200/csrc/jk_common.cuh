@@ -53,6 +53,8 @@ struct jk_ws_layout {
   size_t pre_ao;        // T   [Rp, Hq d]    attention outputs of this pass's nodes (O-proj input)
   size_t paged_o;       // f32 partials of the paged attention's CTAs, two slots each
   size_t paged_ml;
+  size_t lin_part;      // f32 partial tiles of jk_linear, one per CTA
+  size_t lin_flag;      // i32 per CTA: its partial is there (zero between launches)
   size_t total;
   int attn_max_split;
   size_t gemm_cnt;       // four item counters of the streaming GEMM (zero between launches)
@@ -86,6 +88,7 @@ struct jk_ctx {
   int sm_count;           // filled at the first launch
   int attn_smem_set;
   int attn_sk_smem_set;
+  int lin_smem_set;       // one bit for each kernel of jk_linear
   unsigned gemm_seq;     // GEMM launches so far: picks the item counter
   int st_attn, st_combine;  // profiling stages the attention kernels are booked under
   int attn_kernel;        // 0 = by size, 1 = CTA per (query block, key slice), 2 = persistent,

@@ -643,6 +643,12 @@ int jk_tc_available(const jk_ctx* ctx) {
   return s && !s->failed;
 }
 
+// 1 if tensor maps can be made (whatever the context's rows).
+int jk_tma_available(jk_ctx* ctx) {
+  tc_state* s = tc_get_state(ctx);
+  return s && !s->failed;
+}
+
 extern "C" int jk_tensor_path_active(jk_ctx* ctx) {
   return (ctx && ctx->tensor_path && jk_tc_available(ctx)) ? 1 : 0;
 }

@@ -2,7 +2,8 @@
 // tensor path is off).
 #include "jk_linear.cuh"
 
-int jk_tc_available(const jk_ctx* ctx);                                        // jk_gemm_tc.cu
+int jk_tma_available(jk_ctx* ctx);                                             // jk_gemm_tc.cu
+int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx);    // jk_linear_tc.cu
 
 // ------------------------------------------------------------------------------------------ operands
 // Four consecutive elements of a row as f32; element types: float, bf16, uint8_t (mx8 codes, k a
@@ -165,7 +166,10 @@ extern "C" int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* op, int3
   a.x_stride = x_stride; a.r_stride = residual_stride; a.o_stride = out_stride;
   a.k_tiles_in = mx_k_tiles(K); a.k_tiles_out = mx_k_tiles(N);
   if (!ctx->ws) return JK_ERR_WORKSPACE;
+  int rc = jk_ensure_device_info(ctx);
+  if (rc != JK_OK) return rc;
   cudaStream_t st = (cudaStream_t)stream;
+  if (ctx->tensor_path && ctx->cfg.dtype == JK_BF16 && jk_tma_available(ctx)) return jk_linear_tc(ctx, st, a, mx);
   JK_PROF(ctx, st, JK_ST_LINEAR);
   if (ctx->cfg.dtype == JK_F32) {
     if (mx) launch_cc<uint8_t, float>(st, a);
