@@ -15,7 +15,7 @@
 // CTA behind it asks; it waits only for CTAs of lower index, which were launched before it.  Sums
 // are formed in the same order on every run.
 //
-// Roles: warp 0 loads (TMA), warp 1 issues products, warps 2-5 drain accumulators and do the epilogue.  Every
+// Roles: warp 0 loads (TMA), warp 1 issues products, warps 2-17 drain accumulators and do the epilogue.  Every
 // wait is bounded: after about 2 s it records JK_ERR_TIMEOUT, the CTA lets its copies land, frees its
 // tensor memory and returns.
 #include <cuda.h>
@@ -29,7 +29,9 @@ int jk_tma_available(jk_ctx* ctx);
 
 #define LT_M 128                          // weights of a tile
 #define LT_BOX 128                        // bytes of a box row
-#define LT_THREADS 192
+#define LT_EPI_WARPS 16                   // four for each quarter of the lanes of tensor memory
+#define LT_THREADS (64 + 32 * LT_EPI_WARPS)   // and two warps that load and multiply
+#define LT_MAX_SPLIT 8                    // CTAs that share a tile, at most
 #define LT_MAX_STAGES 12
 #define LT_SMEM (224 * 1024)
 #define LT_ACC_COLS 256                   // columns of the accumulators of one tile, at most
@@ -58,9 +60,9 @@ struct lt_params {
 struct __align__(16) lt_tail {
   uint64_t full[LT_MAX_STAGES], empty[LT_MAX_STAGES];
   uint64_t acc_full[2], acc_empty[2];
+  uint64_t part_full, part_empty;         // others' partials in the ring, and read
   uint32_t tmem_base;
   int abort_flag;
-  unsigned done, seen;                    // epilogue warps that handed over their partials / have added up others'
 };
 
 // ------------------------------------------------------------------------------------------ PTX
@@ -99,25 +101,18 @@ __host__ __device__ inline uint32_t lt_idesc_mx8(int n, int k) {
   return ((uint32_t)k << 4) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(LT_M >> 7) << 27) |
          ((uint32_t)k << 29);
 }
+// More bytes for the running phase, without an arrival.
+__device__ __forceinline__ void mbar_add_tx(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ int ld_acquire(const int32_t* p) {
   int v;
   asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
   return v;
 }
-__device__ __forceinline__ void st_release(int32_t* p, int v) {
-  asm volatile("st.release.gpu.global.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+__device__ __forceinline__ void add_release(int32_t* p, int v) {
+  asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
-// True in the last of the four epilogue warps to come by (in its lane 0): what the warps before it did is
-// ordered before what follows.  Nobody waits, so a warp that gave up holds up no other.
-__device__ __forceinline__ bool last_of_four(unsigned* count) {
-  __syncwarp();
-  if ((threadIdx.x & 31) != 0) return false;
-  __threadfence();
-  const bool last = (atomicAdd(count, 1u) & 3u) == 3u;
-  __threadfence();
-  return last;
-}
-
 // ------------------------------------------------------------------------------------------ the deal
 // CTA i has the units [i U / G, (i + 1) U / G); unit u is stage u % ks of tile u / ks.
 __device__ __forceinline__ long long lt_first(const lt_params& p, int i) { return p.units * i / gridDim.x; }
@@ -136,45 +131,58 @@ struct lt_walk {                           // a CTA's segments, last tile first
   }
 };
 
+// The first of the CTAs that have the first k steps of a tile this CTA finishes from step k0 on (itself at k0 = 0).
+__device__ __forceinline__ int lt_from(const lt_params& p, int tile, int k0) {
+  int from = blockIdx.x;
+  const long long t0 = (long long)tile * p.ks;
+  while (k0 > 0 && from > 0 && lt_first(p, from) > t0) --from;
+  return from;
+}
+// Their partials come through the ring, as many columns at a time as it holds.
+__device__ __forceinline__ int lt_round_cols(const lt_params& p, int parts, int G) {
+  return max(16, min(p.nt, p.stages * p.stage_bytes / (parts * G * LT_M * 4) / 16 * 16));
+}
+
 // ------------------------------------------------------------------------------------------ epilogue
-// One thread holds output n of up to 32 rows.
+// One thread holds output n of up to 16 rows.
+#define LT_COLS 16
 template <bool GATED>
-__device__ __forceinline__ void lt_store(const lin_args& a, float (&v)[32], float (&u)[GATED ? 32 : 1], int cols, int r0, int n,
-                                         float bias, float bias_up, const uint16_t (&res)[32]) {
+__device__ __forceinline__ void lt_store(const lin_args& a, float (&v)[LT_COLS], float (&u)[GATED ? LT_COLS : 1], int cols,
+                                         int r0, int n, float bias, float bias_up, const uint16_t (&res)[LT_COLS]) {
   const bool live = n < a.n_out;
   const int lane = threadIdx.x & 31;
+  lin_act_all(v, bias, a.act);
+  if constexpr (GATED) {
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    float y = v[j] + bias;
-    if (a.act == JK_ACT_SILU) y = __fdividef(y, 1.f + __expf(-y));
-    else if (a.act == JK_ACT_GELU) y = 0.5f * y * erfcf(-0.70710678118654752f * y);
-    if (GATED) y *= u[j] + bias_up;
-    if (a.residual) y += __uint_as_float((uint32_t)res[j] << 16);
-    v[j] = y;
+    for (int j = 0; j < LT_COLS; ++j) v[j] *= u[j] + bias_up;
+  }
+  if (a.residual) {
+#pragma unroll
+    for (int j = 0; j < LT_COLS; ++j) v[j] += __uint_as_float((uint32_t)res[j] << 16);
   }
   if (a.out_type == JK_ROWS_MX8) {
     if (!live) return;                       // n_out is a multiple of 32: a warp is live as a whole
     int my_e = 0;
     uint8_t* o = (uint8_t*)a.out + (size_t)r0 * a.n_out + n;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
+    for (int j = 0; j < LT_COLS; ++j) {
       const uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(paged_mag(v[j])));
       const int e = paged_scale_exp(__uint_as_float(m));
       if (lane == j) my_e = e;
-      const uint32_t c = __nv_cvt_float_to_fp8(v[j] * paged_pow2(-e), __NV_SATFINITE, __NV_E4M3);
-      if (j < cols) o[(size_t)j * a.n_out] = (uint8_t)c;
+      if (j < cols) *o = (uint8_t)__nv_cvt_float_to_fp8(v[j] * paged_pow2(-e), __NV_SATFINITE, __NV_E4M3);
+      o += a.n_out;
     }
     if (lane < cols) a.out_scale[mx_scale_at(r0 + lane, n >> 5, a.k_tiles_out)] = (uint8_t)(my_e + 127);
   } else if (a.out_type == JK_ROWS_F32) {
     float* o = (float*)a.out + (size_t)r0 * a.o_stride + n;
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (live && j < cols) o[(size_t)j * a.o_stride] = v[j];
+    for (int j = 0; j < LT_COLS; ++j, o += a.o_stride)
+      if (live && j < cols) *o = v[j];
   } else {
     __nv_bfloat16* o = (__nv_bfloat16*)a.out + (size_t)r0 * a.o_stride + n;
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (live && j < cols) o[(size_t)j * a.o_stride] = __float2bfloat16_rn(v[j]);
+    for (int j = 0; j < LT_COLS; ++j, o += a.o_stride)
+      if (live && j < cols) *o = __float2bfloat16_rn(v[j]);
   }
 }
 
@@ -195,48 +203,56 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
   // a stage: kb boxes of w, kb of w_up, kb of x, then the scale tiles in the same order
   const int off_x = G * p.kb * p.a_box, off_sw = off_x + p.kb * p.b_box, off_sx = off_sw + G * p.kb * MX_TILE_BYTES;
 
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < p.stages; ++s) { mbar_init(&T.full[s], 1); mbar_init(&T.empty[s], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&T.acc_full[i], 1); mbar_init(&T.acc_empty[i], 4); }
-    T.abort_flag = 0;
-    T.done = T.seen = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == 1) {
-    tmem_alloc(&T.tmem_base, (uint32_t)p.tmem_cols);
-    tmem_relinquish();
-  }
-  if (warp == 0 && lane == 0) {
-    // The first ring of weights is asked into L2 while the kernel before still runs.  (Into L2 only: were
-    // the weights that kernel's output, nothing stale would be kept.)
-    lt_walk walk(p);
-    int tile, k0, k1, left = p.stages;
-    while (left > 0 && walk.next(p, tile, k0, k1)) {
-      const int row = tile / p.r_tiles * LT_M;
-      for (int k = k0; k < k1 && left > 0; ++k, --left)
-        for (int b = k * p.kb; b < min(p.boxes, (k + 1) * p.kb); ++b) {
-          l2_prefetch_box(&map_w, b * BOX_EL, row);
-          if (GATED) l2_prefetch_box(&map_u, b * BOX_EL, row);
-        }
+  if (warp == 0) {
+    // This warp needs nothing of the others: it does not wait for them (nor for tensor memory) before it
+    // asks for the first boxes.
+    if (lane == 0) {
+      for (int s = 0; s < p.stages; ++s) { mbar_init(&T.full[s], 1); mbar_init(&T.empty[s], 1); }
+      for (int i = 0; i < 2; ++i) { mbar_init(&T.acc_full[i], 1); mbar_init(&T.acc_empty[i], LT_EPI_WARPS); }
+      mbar_init(&T.part_full, 1);
+      mbar_init(&T.part_empty, LT_EPI_WARPS);
+      T.abort_flag = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncwarp();
+    asm volatile("bar.arrive 1, %0;" ::"n"(LT_THREADS) : "memory");
+  } else {
+    if (warp == 1) {
+      tmem_alloc(&T.tmem_base, (uint32_t)p.tmem_cols);
+      tmem_relinquish();
+    }
+    tc_fence_before();
+    asm volatile("bar.sync 1, %0;" ::"n"(LT_THREADS) : "memory");
+    tc_fence_after();
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem_base = T.tmem_base;
+  lt_walk walk(p);
+  int tile, k0, k1;
+  bool more = walk.next(p, tile, k0, k1);
+  if (warp == 2) {
+    // The boxes of the first ring are asked into L2 while the kernel before still runs.  (Into L2 only: what
+    // that kernel writes meanwhile, it writes there.)
+    const int k = k0 + lane / p.kb, b = k * p.kb + lane % p.kb;
+    if (lane < p.stages * p.kb && k < k1 && b < p.boxes) {
+      const int row = tile / p.r_tiles;
+      l2_prefetch_box(&map_w, b * BOX_EL, row * LT_M);
+      if (GATED) l2_prefetch_box(&map_u, b * BOX_EL, row * LT_M);
+      l2_prefetch_box(&map_x, b * BOX_EL, (tile - row * p.r_tiles) * p.nt);
+    }
+    __syncwarp();
+  }
+  const uint32_t tmem_base = warp ? T.tmem_base : 0;       // (warp 0 may be ahead of the allocation; it needs no address)
   jk_pdl_wait();
   jk_pdl_trigger();
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 0) {
     // ------------------------------------------------------------------ copies
     const uint64_t once = l2_policy_evict_first();
     bool ok = true;
     int s = 0;
     long long issued = 0;
     uint32_t ph = 0;
-    lt_walk walk(p);
-    int tile, k0, k1;
-    while (ok && walk.next(p, tile, k0, k1)) {
+    if (lane != 0) more = false;
+    for (; ok && more; more = walk.next(p, tile, k0, k1)) {
       const int wt = tile / p.r_tiles, rt = tile - wt * p.r_tiles;
       for (int k = k0; k < k1; ++k) {
         if (issued >= p.stages) ok = mbar_wait(&T.empty[s], ph ^ 1u, abort_flag, status);
@@ -271,7 +287,58 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
         if (++s == p.stages) { s = 0; ph ^= 1u; }
       }
     }
-    if (!ok) {
+    __syncwarp();
+    ok = __shfl_sync(0xffffffffu, ok, 0);
+    issued = __shfl_sync(0xffffffffu, issued, 0);
+    // The tile this CTA finishes last may have begun in others: once its products are done and the ring is free,
+    // their partials come through it, one lane looking after each.
+    const long long lo = lt_first(p, blockIdx.x);
+    tile = (int)(lo / p.ks);
+    k0 = (int)(lo - (long long)tile * p.ks);
+    if (ok && k0 > 0 && lt_first(p, blockIdx.x + 1) - lo >= p.ks - k0) {
+      const int parts = (int)blockIdx.x - lt_from(p, tile, k0), cols = lt_round_cols(p, parts, G);
+      const int rows = min(p.nt, a.rows - tile % p.r_tiles * p.nt);
+      const int other = (int)blockIdx.x - 1 - lane;
+      // (products end in order: when the last stage has been read, all have)
+      ok = mbar_wait(&T.empty[(issued - 1) % p.stages], (uint32_t)((issued - 1) / p.stages) & 1u, abort_flag, status);
+      ok = __all_sync(0xffffffffu, ok);
+      uint32_t round = 0;
+      for (int c = 0; c < rows && ok; c += cols, ++round) {
+        if (round > 0) ok = mbar_wait(&T.part_empty, (round & 1u) ^ 1u, abort_flag, status);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        if (lane < parts) {
+          if (round == 0) {
+            const long long c0 = clock64();
+            while (ok && ld_acquire(flags + other) != LT_EPI_WARPS) {
+              if (*abort_flag) ok = false;
+              else if (clock64() - c0 > TC_WAIT_CYCLES) {
+                *abort_flag = 1;
+                jk_set_status(status, JK_ERR_TIMEOUT);
+                ok = false;
+              }
+            }
+            asm volatile("fence.proxy.async;" ::: "memory");     // the partials were written by ordinary stores
+          }
+          if (ok) {
+            const uint32_t bytes = (uint32_t)min(cols, p.nt - c) * LT_M * 4;
+            mbar_add_tx(&T.part_full, bytes * G);
+            for (int g = 0; g < G; ++g)
+              bulk_load(smem + (size_t)(lane * G + g) * cols * LT_M * 4,
+                        partial + (size_t)other * LT_SLOT + (size_t)(g * p.nt + c) * LT_M, bytes, &T.part_full);
+            if (round == 0) flags[other] = 0;    // for the next call; nobody else looks at it in this one
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&T.part_full);            // every piece has been announced
+        ok = __all_sync(0xffffffffu, ok);
+      }
+      if (!ok && round > 0 && lane == 0) {
+        const unsigned long long t0 = global_ns();
+        while (!mbar_try_wait(&T.part_full, (round - 1) & 1u))
+          if (global_ns() - t0 > TC_WAIT_NS) break;
+      }
+    }
+    if (!ok && lane == 0) {
       // gave up: the copies in flight land before the CTA's memory goes away
       for (long long i = issued > p.stages ? issued - p.stages : 0; i < issued; ++i) {
         const unsigned long long t0 = global_ns();
@@ -284,10 +351,8 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
     bool ok = true;
     int s = 0, seg = 0, par = 0;
     uint32_t ph = 0;
-    lt_walk walk(p);
-    int tile, k0, k1;
     const uint32_t idesc = lt_idesc_bf16(p.nt);
-    while (ok && walk.next(p, tile, k0, k1)) {
+    for (; ok && more; more = walk.next(p, tile, k0, k1)) {
       const int buf = p.bufs == 2 ? seg & 1 : 0;
       const int use = p.bufs == 2 ? seg >> 1 : seg;
       if (use > 0) ok = mbar_wait(&T.acc_empty[buf], ((uint32_t)use & 1u) ^ 1u, abort_flag, status);
@@ -338,12 +403,11 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
   } else if (warp >= 2) {
     // ------------------------------------------------------------------ epilogue
     const int quarter = warp & 3;          // the lanes of tensor memory this warp may read
+    const int sub = (warp - 2) >> 2;       // its warps take 16 columns in turn
     const int m = quarter * 32 + lane;
     int seg = 0;
     bool ok = true;
-    lt_walk walk(p);
-    int tile, k0, k1;
-    while (ok && walk.next(p, tile, k0, k1)) {
+    for (; ok && more; more = walk.next(p, tile, k0, k1)) {
       const int wt = tile / p.r_tiles, rt = tile - wt * p.r_tiles;
       const int n = wt * LT_M + m, r0 = rt * p.nt, rows = min(p.nt, a.rows - r0);
       const int buf = p.bufs == 2 ? seg & 1 : 0;
@@ -353,90 +417,72 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
       float bias = 0.f, bias_up = 0.f;
       if (whole && live && a.bias) bias = __bfloat162float(((const __nv_bfloat16*)a.bias)[n]);
       if (GATED && whole && live && a.bias_up) bias_up = __bfloat162float(((const __nv_bfloat16*)a.bias_up)[n]);
-      // the CTAs that have the tile's first k steps: all between the one with its first unit and this one
-      int from = blockIdx.x;
-      if (whole && k0 > 0) {
-        const long long t0 = (long long)tile * p.ks;
-        while (from > 0 && lt_first(p, from) > t0) --from;
-        for (int j = from; j < (int)blockIdx.x && ok; ++j) {
-          const long long c0 = clock64();
-          while (ld_acquire(flags + j) == 0) {
-            if (*abort_flag) ok = false;
-            else if (clock64() - c0 > TC_WAIT_CYCLES) {
-              *abort_flag = 1;
-              jk_set_status(status, JK_ERR_TIMEOUT);
-              ok = false;
-            }
-            if (!ok) break;
-          }
-        }
-      }
-      ok = ok && mbar_wait(&T.acc_full[buf], (uint32_t)use & 1u, abort_flag, status);
+      const int parts = whole ? (int)blockIdx.x - lt_from(p, tile, k0) : 0;
+      const int round_cols = parts ? lt_round_cols(p, parts, G) : p.nt;
+      uint16_t res[LT_COLS];
+      auto ask_residual = [&](int c) {
+        const uint16_t* rp = (const uint16_t*)a.residual + (size_t)(r0 + c) * a.r_stride + n;
+#pragma unroll
+        for (int j = 0; j < LT_COLS; ++j, rp += a.r_stride) res[j] = live && c + j < rows ? *rp : (uint16_t)0;
+      };
+      if (whole && a.residual) ask_residual(sub * LT_COLS);      // the first of them ahead of the wait
+      ok = mbar_wait(&T.acc_full[buf], (uint32_t)use & 1u, abort_flag, status);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
       const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * G * p.nt);
-      for (int c = 0; c < rows; c += 32) {
-        const int cols = min(32, rows - c);
-        uint16_t res[32];
-        if (whole && a.residual) {
-          const uint16_t* rp = (const uint16_t*)a.residual + (size_t)(r0 + c) * a.r_stride + n;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) res[j] = live && j < cols ? rp[(size_t)j * a.r_stride] : (uint16_t)0;
+      uint32_t round = 0;
+      for (int c0 = 0; c0 < rows; c0 += round_cols, ++round) {
+        if (parts) {
+          ok = mbar_wait(&T.part_full, round & 1u, abort_flag, status);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
         }
-        // (a tile of 16 more rows than a multiple of 32 reads 16 columns that are not its own and leaves them)
-        float v[32], u[GATED ? 32 : 1];
-        {
-          uint32_t t[32];
-          tmem_ld32(t_addr + (uint32_t)c, t);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(t[j]);
-          if constexpr (GATED) {
-            tmem_ld32(t_addr + (uint32_t)(p.nt + c), t);
+        const int c1 = min(rows, c0 + round_cols);
+        for (int c = c0 + sub * LT_COLS; c < c1; c += LT_EPI_WARPS / 4 * LT_COLS) {
+          const int cols = min(LT_COLS, rows - c);
+          if (whole && a.residual && c != sub * LT_COLS) ask_residual(c);
+          float v[LT_COLS], u[GATED ? LT_COLS : 1];
+          {
+            uint32_t t[LT_COLS], t2[LT_COLS];
+            tmem_ld16(t_addr + (uint32_t)c, t);
+            if constexpr (GATED) tmem_ld16(t_addr + (uint32_t)(p.nt + c), t2);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) u[j] = __uint_as_float(t[j]);
-          }
-        }
-        if (c + 32 >= rows) {              // all of the accumulator has been read
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&T.acc_empty[buf]);
-        }
-        if (!whole) {
-          float* o = partial + (size_t)blockIdx.x * LT_SLOT + m;
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (j < cols) {
-              __stcg(o + (size_t)(c + j) * LT_M, v[j]);
-              if constexpr (GATED) __stcg(o + (size_t)(p.nt + c + j) * LT_M, u[j]);
+            for (int j = 0; j < LT_COLS; ++j) {
+              v[j] = __uint_as_float(t[j]);
+              if constexpr (GATED) u[j] = __uint_as_float(t2[j]);
             }
-          continue;
-        }
-        for (int i = (int)blockIdx.x - 1; i >= from; --i) {
-          const float* o = partial + (size_t)i * LT_SLOT + m;
-          float t[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) t[j] = j < cols ? __ldcg(o + (size_t)(c + j) * LT_M) : 0.f;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] += t[j];
-          if constexpr (GATED) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) t[j] = j < cols ? __ldcg(o + (size_t)(p.nt + c + j) * LT_M) : 0.f;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) u[j] += t[j];
           }
+          if (!whole) {
+            float* o = partial + (size_t)blockIdx.x * LT_SLOT + (size_t)c * LT_M + m;
+#pragma unroll
+            for (int j = 0; j < LT_COLS; ++j) {
+              __stcg(o + (size_t)j * LT_M, v[j]);
+              if constexpr (GATED) __stcg(o + (size_t)(p.nt + j) * LT_M, u[j]);
+            }
+            continue;
+          }
+          const float* o = reinterpret_cast<const float*>(smem) + (size_t)(c - c0) * LT_M + m;
+          for (int i = 0; i < parts; ++i, o += (size_t)G * round_cols * LT_M) {
+#pragma unroll
+            for (int j = 0; j < LT_COLS; ++j) {
+              v[j] += o[j * LT_M];
+              if constexpr (GATED) u[j] += o[(round_cols + j) * LT_M];
+            }
+          }
+          lt_store<GATED>(a, v, u, cols, r0 + c, n, bias, bias_up, res);
         }
-        lt_store<GATED>(a, v, u, cols, r0 + c, n, bias, bias_up, res);
+        if (parts) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&T.part_empty);
+        }
       }
-      if (!whole) {
-        if (last_of_four(&T.done)) st_release(flags + blockIdx.x, 1);
-      } else if (from < (int)blockIdx.x) {
-        // everyone has seen the flags: they are put back for the next call
-        if (last_of_four(&T.seen))
-          for (int j = from; j < (int)blockIdx.x; ++j) flags[j] = 0;
-      }
+      if (!ok) break;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&T.acc_empty[buf]);       // all of the accumulator has been read
+      if (!whole && lane == 0) add_release(flags + blockIdx.x, 1);      // (behind the warp's stores: the barrier above)
       ++seg;
     }
   }
@@ -472,12 +518,13 @@ int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   p.bufs = 2 * G * p.nt + sf_cols <= 512 ? 2 : 1;
   p.sf_col = p.bufs * G * p.nt;
   p.tmem_cols = 32;
-  // (the epilogue reads 32 columns at a time: up to 16 past the accumulators' end)
-  while (p.tmem_cols < p.sf_col + sf_cols || p.tmem_cols < jk_align_up(p.sf_col, 32)) p.tmem_cols <<= 1;
+  while (p.tmem_cols < p.sf_col + sf_cols) p.tmem_cols <<= 1;
   p.stream = p.r_tiles == 1;
   p.units = (long long)p.w_tiles * p.r_tiles * p.ks;
   int grid = ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS;
-  if (p.units < grid) grid = (int)p.units;
+  // (at most LT_MAX_SPLIT CTAs for a tile: the last of them adds up what the others hand over)
+  const long long useful = (long long)p.w_tiles * p.r_tiles * (p.ks < LT_MAX_SPLIT ? p.ks : LT_MAX_SPLIT);
+  if (useful < grid) grid = (int)useful;
   CUtensorMap mw, mu, mx_;
   auto map = [&](CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t stride, uint32_t box_rows) {
     const uint64_t dims[2] = {(uint64_t)a.n_in, rows}, str[1] = {stride * es};
