@@ -66,32 +66,69 @@ struct __align__(16) lt_tail {
 };
 
 // ------------------------------------------------------------------------------------------ PTX
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                   smem_u32(dst)),
-               "l"(src), "r"(bytes), "r"(smem_u32(bar))
+// The warps that load and multiply run their loops with all lanes and one lane issues (`lead`): with values
+// that the compiler knows to be the same in all lanes, addresses and descriptors live in uniform registers.
+// (Issued from inside `if (lane == 0)`, every product cost about 126 cycles, whatever its size, and every
+// box of a copy as much; a product of 128 x 64 x 16 takes 32.)
+__device__ __forceinline__ uint32_t lt_elect() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r));
+  return r;
+}
+#define LT_IF(arg) "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, " arg ", 0;\n\t@q "
+__device__ __forceinline__ void lt_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t lead) {
+  asm volatile(LT_IF("%4")
+               "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "r"(lead)
+               : "memory");
+}
+__device__ __forceinline__ void lt_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar, uint32_t lead) {
+  asm volatile(LT_IF("%5")
+               "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "r"(lead)
+               : "memory");
+}
+__device__ __forceinline__ void lt_box_once(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar, uint64_t policy,
+                                            uint32_t lead) {
+  asm volatile(LT_IF("%6")
+               "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, "
+               "%3}], [%4], %5;\n\t}"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy), "r"(lead)
+               : "memory");
+}
+__device__ __forceinline__ void lt_expect(uint32_t bar, uint32_t bytes, uint32_t lead) {
+  asm volatile(LT_IF("%2") "mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes), "r"(lead)
+               : "memory");
+}
+__device__ __forceinline__ void lt_commit(uint32_t bar, uint32_t lead) {
+  asm volatile(LT_IF("%1") "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(lead)
                : "memory");
 }
 __device__ __forceinline__ void l2_prefetch_box(const CUtensorMap* map, int x, int y) {
   asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
 }
-// D[tmem] (+)= A[smem] B[smem]^T over 32 codes along k, each operand's block scale from tensor memory
-__device__ __forceinline__ void tc_mma_mx8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                           uint32_t accumulate) {
+// D[tmem] (+)= A[smem] B[smem]^T over 16 bf16 along k
+__device__ __forceinline__ void lt_mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t lead) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
       : "memory");
 }
-// 512 bytes of shared memory, 32 rows of 16, to 4 columns of tensor memory, the same for all four quarters of the lanes
-__device__ __forceinline__ void tc_copy_scales(uint32_t dst, uint32_t smem_addr) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(128 >> 4) << 32;                       // groups of 8 rows are 128 bytes apart
-  d |= (uint64_t)1 << 46;                                // no swizzle
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(d) : "memory");
+// ... over 32 codes along k, each operand's block scale from tensor memory
+__device__ __forceinline__ void lt_mma_mx8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                           uint32_t acc, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(acc), "r"(lead)
+      : "memory");
+}
+// 512 bytes of shared memory, 32 rows of 16, to 4 columns of tensor memory, the same for all four quarters of the
+// lanes; the descriptor: no swizzle, groups of 8 rows 128 bytes apart
+#define LT_SCALE_DESC (((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46))
+__device__ __forceinline__ void lt_copy_scales(uint32_t dst, uint64_t desc, uint32_t lead) {
+  asm volatile(LT_IF("%2") "tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(dst), "l"(desc), "r"(lead) : "memory");
 }
 __host__ __device__ inline uint32_t lt_idesc_bf16(int n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(LT_M >> 4) << 24);
@@ -198,7 +235,7 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   lt_tail& T = *reinterpret_cast<lt_tail*>(smem + (size_t)p.stages * p.stage_bytes);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   volatile int* abort_flag = &T.abort_flag;
   // a stage: kb boxes of w, kb of w_up, kb of x, then the scale tiles in the same order
   const int off_x = G * p.kb * p.a_box, off_sw = off_x + p.kb * p.b_box, off_sx = off_sw + G * p.kb * MX_TILE_BYTES;
@@ -247,49 +284,49 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
   if (warp == 0) {
     // ------------------------------------------------------------------ copies
     const uint64_t once = l2_policy_evict_first();
+    const uint32_t lead = lt_elect(), base = smem_u32(smem), full0 = smem_u32(T.full);
     bool ok = true;
     int s = 0;
     long long issued = 0;
     uint32_t ph = 0;
-    if (lane != 0) more = false;
     for (; ok && more; more = walk.next(p, tile, k0, k1)) {
       const int wt = tile / p.r_tiles, rt = tile - wt * p.r_tiles;
+      // (a tile of x begins at a multiple of 128 rows wherever there is more than one; the last may have fewer
+      // scale tiles, and reads the first in place of those)
+      const uint8_t* sw = MX ? a.w_scale + (size_t)wt * a.k_tiles_in * MX_TILE_BYTES : nullptr;
+      const uint8_t* su = MX && GATED ? a.w_up_scale + (size_t)wt * a.k_tiles_in * MX_TILE_BYTES : nullptr;
+      const uint8_t* sx0 = MX ? a.x_scale + (size_t)(rt * (p.nt >> 7)) * a.k_tiles_in * MX_TILE_BYTES : nullptr;
+      const uint8_t* sx1 = MX && rt * p.nt + 128 < a.rows ? sx0 + (size_t)a.k_tiles_in * MX_TILE_BYTES : sx0;
       for (int k = k0; k < k1; ++k) {
         if (issued >= p.stages) ok = mbar_wait(&T.empty[s], ph ^ 1u, abort_flag, status);
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        unsigned char* st = smem + (size_t)s * p.stage_bytes;
+        const uint32_t st = base + (uint32_t)s * (uint32_t)p.stage_bytes, bar = full0 + 8u * (uint32_t)s;
         const int b0 = k * p.kb, nb = min(p.kb, p.boxes - b0);
-        mbar_expect_tx(&T.full[s], (uint32_t)(nb * (G * p.a_box + p.b_box + (MX ? (G + p.sfb) * MX_TILE_BYTES : 0))));
+        lt_expect(bar, (uint32_t)(nb * (G * p.a_box + p.b_box + (MX ? (G + p.sfb) * MX_TILE_BYTES : 0))), lead);
         for (int b = 0; b < nb; ++b) {
           const int x = (b0 + b) * BOX_EL;
           if (p.stream) {
-            tma_load_2d_hint(st + b * p.a_box, &map_w, x, wt * LT_M, &T.full[s], once);
-            if (GATED) tma_load_2d_hint(st + (p.kb + b) * p.a_box, &map_u, x, wt * LT_M, &T.full[s], once);
+            lt_box_once(st + b * p.a_box, &map_w, x, wt * LT_M, bar, once, lead);
+            if (GATED) lt_box_once(st + (p.kb + b) * p.a_box, &map_u, x, wt * LT_M, bar, once, lead);
           } else {
-            tma_load_2d(st + b * p.a_box, &map_w, x, wt * LT_M, &T.full[s]);
-            if (GATED) tma_load_2d(st + (p.kb + b) * p.a_box, &map_u, x, wt * LT_M, &T.full[s]);
+            lt_box(st + b * p.a_box, &map_w, x, wt * LT_M, bar, lead);
+            if (GATED) lt_box(st + (p.kb + b) * p.a_box, &map_u, x, wt * LT_M, bar, lead);
           }
-          tma_load_2d(st + off_x + b * p.b_box, &map_x, x, rt * p.nt, &T.full[s]);
+          lt_box(st + off_x + b * p.b_box, &map_x, x, rt * p.nt, bar, lead);
         }
         if (MX) {
           // scale tiles of neighbouring boxes lie side by side
-          const size_t at = ((size_t)wt * a.k_tiles_in + b0) * MX_TILE_BYTES;
-          bulk_load(st + off_sw, a.w_scale + at, nb * MX_TILE_BYTES, &T.full[s]);
-          if (GATED) bulk_load(st + off_sw + p.kb * MX_TILE_BYTES, a.w_up_scale + at, nb * MX_TILE_BYTES, &T.full[s]);
-          for (int i = 0; i < p.sfb; ++i) {
-            // (a tile of x begins at a multiple of 128 rows wherever there is more than one)
-            const size_t ax = ((size_t)(rt * (p.nt >> 7) + i) * a.k_tiles_in + b0) * MX_TILE_BYTES;
-            const bool in = rt * p.nt + i * 128 < a.rows;            // the last tile of x may have fewer scale tiles
-            bulk_load(st + off_sx + i * p.kb * MX_TILE_BYTES, a.x_scale + (in ? ax : 0), nb * MX_TILE_BYTES, &T.full[s]);
-          }
+          const int at = b0 * MX_TILE_BYTES, bytes = nb * MX_TILE_BYTES, step = p.kb * MX_TILE_BYTES;
+          lt_bulk(st + off_sw, sw + at, bytes, bar, lead);
+          if (GATED) lt_bulk(st + off_sw + step, su + at, bytes, bar, lead);
+          lt_bulk(st + off_sx, sx0 + at, bytes, bar, lead);
+          if (p.sfb > 1) lt_bulk(st + off_sx + step, sx1 + at, bytes, bar, lead);
         }
         ++issued;
         if (++s == p.stages) { s = 0; ph ^= 1u; }
       }
     }
-    __syncwarp();
-    ok = __shfl_sync(0xffffffffu, ok, 0);
-    issued = __shfl_sync(0xffffffffu, issued, 0);
     // The tile this CTA finishes last may have begun in others: once its products are done and the ring is free,
     // their partials come through it, one lane looking after each.
     const long long lo = lt_first(p, blockIdx.x);
@@ -323,8 +360,8 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
             const uint32_t bytes = (uint32_t)min(cols, p.nt - c) * LT_M * 4;
             mbar_add_tx(&T.part_full, bytes * G);
             for (int g = 0; g < G; ++g)
-              bulk_load(smem + (size_t)(lane * G + g) * cols * LT_M * 4,
-                        partial + (size_t)other * LT_SLOT + (size_t)(g * p.nt + c) * LT_M, bytes, &T.part_full);
+              lt_bulk(base + (uint32_t)((lane * G + g) * cols * LT_M * 4),
+                      partial + (size_t)other * LT_SLOT + (size_t)(g * p.nt + c) * LT_M, bytes, smem_u32(&T.part_full), 1u);
             if (round == 0) flags[other] = 0;    // for the next call; nobody else looks at it in this one
           }
         }
@@ -346,58 +383,68 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
           if (global_ns() - t0 > TC_WAIT_NS) break;
       }
     }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1) {
     // ------------------------------------------------------------------ products
+    const uint32_t lead = lt_elect(), tm = __shfl_sync(0xffffffffu, tmem_base, 0);
+    const uint32_t empty0 = smem_u32(T.empty);
+    const uint64_t d0 = smem_desc_sw128(smem_u32(smem));   // further descriptors: sixteenths of bytes are added
+    const uint64_t s0 = LT_SCALE_DESC | (uint64_t)((smem_u32(smem) & 0x3FFFFu) >> 4);
+    const uint32_t idesc = lt_idesc_bf16(p.nt);
     bool ok = true;
     int s = 0, seg = 0, par = 0;
     uint32_t ph = 0;
-    const uint32_t idesc = lt_idesc_bf16(p.nt);
     for (; ok && more; more = walk.next(p, tile, k0, k1)) {
       const int buf = p.bufs == 2 ? seg & 1 : 0;
       const int use = p.bufs == 2 ? seg >> 1 : seg;
       if (use > 0) ok = mbar_wait(&T.acc_empty[buf], ((uint32_t)use & 1u) ^ 1u, abort_flag, status);
+      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t d = tmem_base + (uint32_t)(buf * G * p.nt);
+      const uint32_t d = tm + (uint32_t)(buf * G * p.nt);
       uint32_t acc = 0;
       for (int k = k0; k < k1; ++k) {
         ok = mbar_wait(&T.full[s], ph, abort_flag, status);
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t st = smem_u32(smem + (size_t)s * p.stage_bytes);
+        const uint32_t st = (uint32_t)s * (uint32_t)(p.stage_bytes >> 4);
         const int b0 = k * p.kb, nb = min(p.kb, p.boxes - b0);
         for (int b = 0; b < nb; ++b) {
-          const uint64_t dw = smem_desc_sw128(st + b * p.a_box), du = smem_desc_sw128(st + (p.kb + b) * p.a_box);
-          const uint64_t dx = smem_desc_sw128(st + off_x + b * p.b_box);
-          const int n_sub = min(4, p.subs - (b0 + b) * 4);           // products past the end of k are left out
+          const uint64_t dw = d0 + (st + (uint32_t)(b * p.a_box >> 4)), du = dw + (uint32_t)(p.kb * p.a_box >> 4);
+          const uint64_t dx = d0 + (st + (uint32_t)((off_x + b * p.b_box) >> 4));
+          const int n_sub = p.subs - (b0 + b) * 4;                   // products past the end of k are left out
           uint32_t sf = 0;
           if (MX) {
             // two sets of scale columns take turns: a box's scales do not land on those that the products
             // of the box before may still read
-            sf = tmem_base + (uint32_t)(p.sf_col + par * 4 * (G + p.sfb));
+            sf = tm + (uint32_t)(p.sf_col + par * 4 * (G + p.sfb));
             par ^= 1;
-            tc_copy_scales(sf, st + off_sw + b * MX_TILE_BYTES);
-            if (GATED) tc_copy_scales(sf + 4, st + off_sw + (p.kb + b) * MX_TILE_BYTES);
-            for (int i = 0; i < p.sfb; ++i)
-              tc_copy_scales(sf + 4 * (G + i), st + off_sx + (i * p.kb + b) * MX_TILE_BYTES);
+            const uint64_t ds = s0 + (st + (uint32_t)((off_sw + b * MX_TILE_BYTES) >> 4));
+            const uint32_t step = (uint32_t)(p.kb * MX_TILE_BYTES) >> 4;
+            lt_copy_scales(sf, ds, lead);
+            lt_copy_scales(sf + 4, ds + step, lead);                 // gated: of w_up; else the first of x
+            if (GATED || p.sfb > 1) lt_copy_scales(sf + 8, ds + 2 * step, lead);
+            if (GATED && p.sfb > 1) lt_copy_scales(sf + 12, ds + 3 * step, lead);
           }
-          for (int k4 = 0; k4 < n_sub; ++k4) {
+#pragma unroll
+          for (int k4 = 0; k4 < 4; ++k4) {
+            if (k4 >= n_sub) break;
             const uint64_t step = (uint64_t)(2 * k4);                // 32 bytes along k
             if (MX) {
               const uint32_t id = lt_idesc_mx8(p.nt, k4);
-              tc_mma_mx8(d, dw + step, dx + step, id, sf, sf + 4 * G, acc);
-              if (GATED) tc_mma_mx8(d + p.nt, du + step, dx + step, id, sf + 4, sf + 4 * G, acc);
+              lt_mma_mx8(d, dw + step, dx + step, id, sf, sf + 4 * G, acc, lead);
+              if (GATED) lt_mma_mx8(d + p.nt, du + step, dx + step, id, sf + 4, sf + 4 * G, acc, lead);
             } else {
-              tc_mma_bf16(d, dw + step, dx + step, idesc, acc);
-              if (GATED) tc_mma_bf16(d + p.nt, du + step, dx + step, idesc, acc);
+              lt_mma_bf16(d, dw + step, dx + step, idesc, acc, lead);
+              if (GATED) lt_mma_bf16(d + p.nt, du + step, dx + step, idesc, acc, lead);
             }
             acc = 1;
           }
         }
-        tc_commit(&T.empty[s]);            // the stage is free once these products have read it
+        lt_commit(empty0 + 8u * (uint32_t)s, lead);        // the stage is free once these products have read it
         if (++s == p.stages) { s = 0; ph ^= 1u; }
       }
-      if (ok) tc_commit(&T.acc_full[buf]);
+      if (ok) lt_commit(smem_u32(&T.acc_full[buf]), lead);
       ++seg;
     }
   } else if (warp >= 2) {
