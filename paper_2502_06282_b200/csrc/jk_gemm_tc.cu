@@ -909,3 +909,10 @@ int jk_tma_encode_u8(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, c
                     box[0] == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, ptr, rank, dims,
                     strides_bytes, box);
 }
+
+// Scale tiles of 8-bit rows: 512 bytes each, one after the other; a box is a tile.
+int jk_tma_encode_scales(jk_ctx* ctx, CUtensorMap* out, const void* ptr, uint64_t tiles) {
+  const uint64_t dims[2] = {128, tiles}, str[1] = {512};
+  const uint32_t box[2] = {128, 1};
+  return tma_encode(ctx, out, CU_TENSOR_MAP_DATA_TYPE_UINT32, CU_TENSOR_MAP_SWIZZLE_NONE, ptr, 2, dims, str, box);
+}

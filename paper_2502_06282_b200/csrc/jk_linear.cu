@@ -4,6 +4,7 @@
 
 int jk_tma_available(jk_ctx* ctx);                                             // jk_gemm_tc.cu
 int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx);    // jk_linear_tc.cu
+int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx);  // jk_linear_pair.cu
 
 // ------------------------------------------------------------------------------------------ operands
 // Four consecutive elements of a row as f32; element types: float, bf16, uint8_t (mx8 codes, k a
@@ -169,7 +170,8 @@ extern "C" int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* op, int3
   int rc = jk_ensure_device_info(ctx);
   if (rc != JK_OK) return rc;
   cudaStream_t st = (cudaStream_t)stream;
-  if (ctx->tensor_path && ctx->cfg.dtype == JK_BF16 && jk_tma_available(ctx)) return jk_linear_tc(ctx, st, a, mx);
+  if (ctx->tensor_path && ctx->cfg.dtype == JK_BF16 && jk_tma_available(ctx))
+    return rows > 256 ? jk_linear_pair(ctx, st, a, mx) : jk_linear_tc(ctx, st, a, mx);
   JK_PROF(ctx, st, JK_ST_LINEAR);
   if (ctx->cfg.dtype == JK_F32) {
     if (mx) launch_cc<uint8_t, float>(st, a);

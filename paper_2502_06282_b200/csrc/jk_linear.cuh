@@ -42,9 +42,7 @@ __device__ __forceinline__ float lin_erfc(float x) {
   const float e = t * __expf(fmaf(-z, z, q));
   return x >= 0.f ? e : 2.f - e;
 }
-template <int N> __device__ __forceinline__ void lin_act_all(float (&v)[N], float bias, int act) {
-#pragma unroll
-  for (int j = 0; j < N; ++j) v[j] += bias;
+template <int N> __device__ __forceinline__ void lin_act_all(float (&v)[N], int act) {
   if (act == JK_ACT_SILU) {
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = __fdividef(v[j], 1.f + __expf(-v[j]));

@@ -1,0 +1,577 @@
+// jk_linear for many rows: the kernel whose time is the tensor cores'.
+//
+// A pair of CTAs (a cluster of two SMs) makes a tile of 256 rows of x times 256 weight rows with tcgen05.mma
+// cta_group::2: each CTA brings 128 rows of x and 128 weight rows and holds the sums of its 128 rows,
+// so a byte that arrives in shared memory serves twice the products of a single CTA's tile (64 bytes a
+// clock and SM at the full rate, where 128 x 256 tiles of single CTAs ask for 96).  A gated block takes 128
+// rows of w and 128 of w_up as the 256: one CTA brings the one, the other the other, and the two sums of an
+// output stand in the same lane.  Rows of x stand on the lanes here: a thread of the epilogue holds 32
+// consecutive outputs of a row, which are a scale block of 8-bit rows, without any exchange.
+//
+// Tiles are dealt to the pairs in turn, in bands of 8 tiles of x, so that what runs at one time shares
+// its operands in L2.  The tiles left over for a last, incomplete turn come first and are cut along k
+// into even shares: the pair that has a tile's end finishes it from the others' f32 partials, as in the
+// kernel for few rows.
+//
+// Accumulators: two of 256 columns for bf16.  8-bit rows need 24 columns for scales; there the second
+// accumulator begins at column 232, and of the 24 columns that both use the epilogue reads first.
+//
+// Roles: warp 0 loads, warp 1 (of the pair's first CTA) multiplies, warps 2-9 are the epilogue.  Waits are bounded as
+// in the kernel for few rows.
+#include "jk_linear_tc.cuh"
+
+int jk_tma_encode_u8(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, const uint64_t* dims,
+                     const uint64_t* strides_bytes, const uint32_t* box);
+int jk_tma_encode_scales(jk_ctx* ctx, CUtensorMap* out, const void* ptr, uint64_t tiles);
+
+#define LP_ROWS 256                       // rows of x of a pair's tile
+#define LP_N 256                          // weight rows of a pair's tile
+#define LP_BAND 8                         // tiles of x of a band
+#define LP_MAX_SPLIT 4                    // pairs that share a tile, at most
+#define LP_EPI_WARPS 8
+#define LP_THREADS (64 + 32 * LP_EPI_WARPS)
+#define LP_A_BYTES (LT_M * LT_BOX)        // of each operand in a box
+#define LP_STAGES 6
+#define LP_SF_COL 488                     // 8-bit rows: first column of the scales, two sets of 12
+#define LP_ACC2_MX 232                    // 8-bit rows: first column of the second accumulator
+#define LP_STAGE_PITCH 34                 // elements of a row in an epilogue warp's 32 x 32 exchange
+
+struct lp_params {
+  int r_tiles, w_tiles;
+  int boxes, subs;                        // boxes and products along k
+  int n_tile;                             // outputs of a tile: 256, gated 128
+  int full;                               // tiles dealt whole
+  int left, sk_pairs;                     // tiles cut along k, and the pairs that share them
+};
+
+struct __align__(16) lp_tail {
+  uint64_t full[LP_STAGES], empty[LP_STAGES];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t shared_free;                   // the columns both accumulators use have been read
+  uint32_t tmem_base;
+  int abort_flag;
+  unsigned seen;                          // epilogue warps that have seen all flags
+};
+struct __align__(16) lp_exchange { uint16_t v[32 * LP_STAGE_PITCH]; };
+
+template <bool MX> struct lp_stage { static constexpr int BYTES = 2 * LP_A_BYTES + (MX ? 2048 : 0); };
+
+// ------------------------------------------------------------------------------------------ PTX
+// Loads of a pair: the barrier is the first CTA's, whichever CTA the data is for.
+__device__ __forceinline__ void lp_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar, uint32_t lead) {
+  asm volatile(LT_IF("%5")
+               "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], "
+               "[%4];\n\t}"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "r"(lead)
+               : "memory");
+}
+__device__ __forceinline__ void lp_mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void lp_mma_mx8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                           uint32_t acc, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(acc), "r"(lead)
+      : "memory");
+}
+// (each CTA's scales from its own shared memory to its own tensor memory)
+__device__ __forceinline__ void lp_copy_scales(uint32_t dst, uint64_t desc, uint32_t lead) {
+  asm volatile(LT_IF("%2") "tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(dst), "l"(desc), "r"(lead) : "memory");
+}
+// An arrival on the barrier at this place in both CTAs, when the products issued so far have completed.
+__device__ __forceinline__ void lp_commit(uint32_t bar, uint32_t lead) {
+  asm volatile(LT_IF("%1")
+               "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}"
+               ::"r"(bar), "r"(lead), "h"((uint16_t)3)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lp_map(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void lp_arrive(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void lp_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__host__ __device__ inline uint32_t lp_idesc_bf16() {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(LP_N >> 3) << 17) | ((uint32_t)(LP_ROWS >> 4) << 24);
+}
+__host__ __device__ inline uint32_t lp_idesc_mx8(int k) {
+  return ((uint32_t)k << 4) | ((uint32_t)(LP_N >> 3) << 17) | (1u << 23) | ((uint32_t)(LP_ROWS >> 7) << 27) | ((uint32_t)k << 29);
+}
+// 32 bytes at once
+__device__ __forceinline__ void st32b(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
+// ------------------------------------------------------------------------------------------ the deal
+// Of pair i: its share of the tiles cut along k (unit u = box u % boxes of tile full + u / boxes), last tile first;
+// then the whole tiles i, i + pairs, ...
+struct lp_walk {
+  long long lo, hi;
+  int next_full;
+  static __device__ __forceinline__ long long first(const lp_params& p, int i) {
+    return i >= p.sk_pairs ? (long long)p.left * p.boxes : (long long)p.left * p.boxes * i / p.sk_pairs;
+  }
+  __device__ __forceinline__ lp_walk(const lp_params& p, int pair)
+      : lo(p.left ? first(p, pair) : 0), hi(p.left ? first(p, pair + 1) : 0), next_full(pair) {}
+  __device__ __forceinline__ bool next(const lp_params& p, int pairs, int& tile, int& k0, int& k1) {
+    if (hi > lo) {
+      const int t = (int)((hi - 1) / p.boxes);
+      const long long t0 = (long long)t * p.boxes;
+      k1 = (int)(hi - t0);
+      k0 = lo > t0 ? (int)(lo - t0) : 0;
+      hi = t0 + k0;
+      tile = p.full + t;
+      return true;
+    }
+    if (next_full >= p.full) return false;
+    tile = next_full;
+    next_full += pairs;
+    k0 = 0;
+    k1 = p.boxes;
+    return true;
+  }
+};
+// Tile of x and tile of weights.
+__device__ __forceinline__ void lp_place(const lp_params& p, int tile, int& rt, int& wt) {
+  const int band = tile / (LP_BAND * p.w_tiles), in = tile - band * LP_BAND * p.w_tiles;
+  const int rows = min(LP_BAND, p.r_tiles - band * LP_BAND);
+  wt = in / rows;
+  rt = band * LP_BAND + in - wt * rows;
+}
+
+// ------------------------------------------------------------------------------------------ epilogue
+// 32 elements of T at p as f32; those from `most` on are 0.
+__device__ __forceinline__ void lp_load32(const uint16_t* p, int most, float (&o)[32]) {
+  if (most >= 32 && ((uintptr_t)p & 15) == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 r = reinterpret_cast<const uint4*>(p)[i];
+      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
+        o[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) o[j] = j < most ? __uint_as_float((uint32_t)p[j] << 16) : 0.f;
+  }
+}
+__device__ __forceinline__ uint32_t lp_pack(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The lane's row (row0 + lane), outputs n .. n + 31.
+template <bool GATED>
+__device__ __forceinline__ void lp_store(const lin_args& a, float (&v)[32], float (&u)[GATED ? 32 : 1], int row0, int n,
+                                         lp_exchange& X, bool wide) {
+  const int lane = threadIdx.x & 31, row = row0 + lane, most = a.n_out - n;
+  const bool live = row < a.rows;
+  if (a.bias) {
+    float b[32];
+    lp_load32((const uint16_t*)a.bias + n, most, b);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] += b[j];
+  }
+  lin_act_all(v, a.act);
+  if constexpr (GATED) {
+    if (a.bias_up) {
+      float b[32];
+      lp_load32((const uint16_t*)a.bias_up + n, most, b);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) u[j] += b[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] *= u[j];
+  }
+  if (a.residual) {
+    float r[32];
+    const uint16_t* rp = (const uint16_t*)a.residual + n;
+    if (wide && most >= 32) {
+      lp_load32(rp + (size_t)(live ? row : row0) * a.r_stride, 32, r);
+    } else {
+      // rows that begin anywhere: read along the rows, handed out through shared memory
+      __syncwarp();
+      for (int j = 0; j < 32; ++j)
+        X.v[j * LP_STAGE_PITCH + lane] = row0 + j < a.rows && lane < most ? rp[(size_t)(row0 + j) * a.r_stride + lane] : (uint16_t)0;
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 32; ++j) r[j] = __uint_as_float((uint32_t)X.v[lane * LP_STAGE_PITCH + j] << 16);
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] += r[j];
+  }
+  if (a.out_type == JK_ROWS_MX8) {           // n_out is a multiple of 32: all of the block or nothing
+    if (!live || most < 32) return;
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) m = fmaxf(m, paged_mag(v[j]));
+    const int e = paged_scale_exp(m);
+    const float inv = paged_pow2(-e);
+    uint32_t o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = paged_pack4(v[4 * j] * inv, v[4 * j + 1] * inv, v[4 * j + 2] * inv, v[4 * j + 3] * inv);
+    uint8_t* p = (uint8_t*)a.out + (size_t)row * a.n_out + n;
+    if (wide) {
+      st32b(p, o);
+    } else {
+      reinterpret_cast<uint4*>(p)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      reinterpret_cast<uint4*>(p)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+    a.out_scale[mx_scale_at(row, n >> 5, a.k_tiles_out)] = (uint8_t)(e + 127);
+  } else if (a.out_type == JK_ROWS_F32) {
+    if (wide && most >= 32) {
+      if (!live) return;
+      float* p = (float*)a.out + (size_t)row * a.o_stride + n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(v[8 * i + j]);
+        st32b(p + 8 * i, o);
+      }
+    } else {
+      float* p = (float*)a.out + (size_t)row * a.o_stride + n;
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (live && j < most) p[j] = v[j];
+    }
+  } else if (wide && most >= 32) {
+    if (!live) return;
+    __nv_bfloat16* p = (__nv_bfloat16*)a.out + (size_t)row * a.o_stride + n;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = lp_pack(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]);
+      st32b(p + 16 * i, o);
+    }
+  } else {
+    __syncwarp();
+    uint32_t* x32 = reinterpret_cast<uint32_t*>(&X.v[lane * LP_STAGE_PITCH]);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x32[j] = lp_pack(v[2 * j], v[2 * j + 1]);
+    __syncwarp();
+    uint16_t* p = (uint16_t*)a.out + (size_t)row0 * a.o_stride + n + lane;
+    for (int j = 0; j < 32; ++j, p += a.o_stride)
+      if (row0 + j < a.rows && lane < most) *p = X.v[j * LP_STAGE_PITCH + lane];
+    __syncwarp();
+  }
+}
+
+// ------------------------------------------------------------------------------------------ the kernel
+template <bool MX, bool GATED>
+__global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
+    const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u,
+    const __grid_constant__ CUtensorMap map_sx, const __grid_constant__ CUtensorMap map_sw,
+    const __grid_constant__ CUtensorMap map_su, const lp_params p, const lin_args a, int wide, float* __restrict__ partial,
+    int32_t* flags, int32_t* status) {
+  constexpr int BOX_EL = MX ? 128 : 64, STAGE = lp_stage<MX>::BYTES;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  lp_exchange* X = reinterpret_cast<lp_exchange*>(smem + LP_STAGES * STAGE);
+  lp_tail& T = *reinterpret_cast<lp_tail*>(X + LP_EPI_WARPS);
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  volatile int* abort_flag = &T.abort_flag;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < LP_STAGES; ++s) { mbar_init(&T.full[s], 1); mbar_init(&T.empty[s], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&T.acc_full[i], 1); mbar_init(&T.acc_empty[i], 2 * LP_EPI_WARPS); }
+    mbar_init(&T.shared_free, LP_EPI_WARPS);           // four warps of each CTA
+    T.abort_flag = 0;
+    T.seen = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&T.tmem_base)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  lp_cluster_sync();                       // the barriers of both CTAs exist
+  tc_fence_after();
+  const uint32_t tmem_base = T.tmem_base;
+  lp_walk walk(p, pair);
+  int tile, k0, k1;
+  bool more = walk.next(p, pairs, tile, k0, k1);
+  jk_pdl_wait();
+  jk_pdl_trigger();
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ copies
+    const uint32_t lead = lt_elect(), base = smem_u32(smem);
+    const uint32_t full0 = lp_map(smem_u32(T.full), 0), own_full0 = smem_u32(T.full);
+    bool ok = true;
+    int s = 0;
+    long long issued = 0;
+    uint32_t ph = 0;
+    for (; ok && more; more = walk.next(p, pairs, tile, k0, k1)) {
+      int rt, wt;
+      lp_place(p, tile, rt, wt);
+      const int xr = rt * LP_ROWS + rank * LT_M;
+      const int wr = GATED ? wt * LT_M : wt * LP_N + rank * LT_M;
+      const CUtensorMap* mw = GATED && rank ? &map_u : &map_w;
+      for (int k = k0; k < k1; ++k) {
+        if (issued >= LP_STAGES) ok = mbar_wait(&T.empty[s], ph ^ 1u, abort_flag, status);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t st = base + (uint32_t)s * STAGE, bar = full0 + 8u * (uint32_t)s;
+        // (both CTAs' bytes; what the other's copies bring may arrive before it is expected)
+        if (rank == 0) lt_expect(own_full0 + 8u * (uint32_t)s, 2u * (2 * LP_A_BYTES + (MX ? 3 * MX_TILE_BYTES : 0)), lead);
+        lp_box(st, &map_x, k * BOX_EL, xr, bar, lead);
+        lp_box(st + LP_A_BYTES, mw, k * BOX_EL, wr, bar, lead);
+        if (MX) {
+          // scales: of this CTA's rows of x, and of all 256 weight rows
+          lp_box(st + 2 * LP_A_BYTES, &map_sx, 0, (rt * 2 + rank) * a.k_tiles_in + k, bar, lead);
+          lp_box(st + 2 * LP_A_BYTES + MX_TILE_BYTES, &map_sw, 0, (GATED ? wt : 2 * wt) * a.k_tiles_in + k, bar, lead);
+          lp_box(st + 2 * LP_A_BYTES + 2 * MX_TILE_BYTES, GATED ? &map_su : &map_sw, 0,
+                 (GATED ? wt : 2 * wt + 1) * a.k_tiles_in + k, bar, lead);
+        }
+        ++issued;
+        if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
+      }
+    }
+    // (the last stages' releases come from the other CTA: they have to be there before this one's memory goes)
+    for (long long i = issued > LP_STAGES ? issued - LP_STAGES : 0; i < issued && ok; ++i)
+      ok = mbar_wait(&T.empty[i % LP_STAGES], (uint32_t)(i / LP_STAGES) & 1u, abort_flag, status);
+    if (!ok && rank == 0) {
+      // gave up: the copies in flight land before the CTA's memory goes away (the second CTA's are waited for
+      // here too: the barriers count both)
+      for (long long i = issued > LP_STAGES ? issued - LP_STAGES : 0; i < issued; ++i) {
+        const unsigned long long t0 = global_ns();
+        while (!mbar_try_wait(&T.full[i % LP_STAGES], (uint32_t)(i / LP_STAGES) & 1u))
+          if (global_ns() - t0 > TC_WAIT_NS) break;
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ products
+    if (rank == 0) {
+      const uint32_t lead = lt_elect(), tm = __shfl_sync(0xffffffffu, tmem_base, 0);
+      const uint32_t empty0 = smem_u32(T.empty);
+      const uint64_t d0 = smem_desc_sw128(smem_u32(smem));
+      const uint64_t s0 = LT_SCALE_DESC | (uint64_t)(((smem_u32(smem) + 2 * LP_A_BYTES) & 0x3FFFFu) >> 4);
+      bool ok = true;
+      int s = 0, seg = 0, par = 0;
+      uint32_t ph = 0;
+      for (; ok && more; more = walk.next(p, pairs, tile, k0, k1)) {
+        const int buf = seg & 1, use = seg >> 1;
+        if (use > 0) ok = mbar_wait(&T.acc_empty[buf], ((uint32_t)use & 1u) ^ 1u, abort_flag, status);
+        if (MX && seg > 0) ok = ok && mbar_wait(&T.shared_free, ((uint32_t)seg & 1u) ^ 1u, abort_flag, status);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d = tm + (uint32_t)(buf * (MX ? LP_ACC2_MX : LP_N));
+        uint32_t acc = 0;
+        for (int k = k0; k < k1; ++k) {
+          ok = mbar_wait(&T.full[s], ph, abort_flag, status);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t st = (uint32_t)s * (uint32_t)(STAGE >> 4);
+          const uint64_t dx = d0 + st, dw = dx + (LP_A_BYTES >> 4);
+          const int n_sub = p.subs - k * 4;                          // products past the end of k are left out
+          uint32_t sf = 0;
+          if (MX) {
+            sf = tm + (uint32_t)(LP_SF_COL + par * 12);              // two sets take turns
+            par ^= 1;
+            const uint64_t ds = s0 + st;
+            lp_copy_scales(sf, ds, lead);
+            lp_copy_scales(sf + 4, ds + (MX_TILE_BYTES >> 4), lead);
+            lp_copy_scales(sf + 8, ds + (2 * MX_TILE_BYTES >> 4), lead);
+          }
+#pragma unroll
+          for (int k4 = 0; k4 < 4; ++k4) {
+            if (k4 >= n_sub) break;
+            if (MX) lp_mma_mx8(d, dx + 2 * k4, dw + 2 * k4, lp_idesc_mx8(k4), sf, sf + 4, acc, lead);
+            else lp_mma_bf16(d, dx + 2 * k4, dw + 2 * k4, lp_idesc_bf16(), acc, lead);
+            acc = 1;
+          }
+          lp_commit(empty0 + 8u * (uint32_t)s, lead);
+          if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
+        }
+        if (ok) lp_commit(smem_u32(&T.acc_full[buf]), lead);
+        ++seg;
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue
+    const int quarter = warp & 3;          // the lanes of tensor memory this warp may read
+    const int half = (warp - 2) >> 2;      // the columns 0 .. 127 upwards, or 255 .. 128 downwards
+    lp_exchange& my_x = X[warp - 2];
+    const uint32_t acc_empty0 = lp_map(smem_u32(T.acc_empty), 0), shared0 = lp_map(smem_u32(&T.shared_free), 0);
+    constexpr int CHUNKS = GATED ? 2 : 4;  // of 32 outputs, for this warp
+    int seg = 0;
+    bool ok = true;
+    for (; ok && more; more = walk.next(p, pairs, tile, k0, k1)) {
+      int rt, wt;
+      lp_place(p, tile, rt, wt);
+      const int row0 = rt * LP_ROWS + rank * LT_M + quarter * 32, n0 = wt * p.n_tile;
+      const int buf = seg & 1, use = seg >> 1;
+      const bool whole = k1 == p.boxes;    // this pair finishes the tile
+      // the pairs that have the tile's first k steps
+      int from = pair;
+      if (whole && k0 > 0) {
+        const long long t0 = (long long)(tile - p.full) * p.boxes;
+        while (from > 0 && lp_walk::first(p, from) > t0) --from;
+        for (int j = from; j < pair && ok; ++j) {
+          const long long c0 = clock64();
+          while (ok && ld_acquire(flags + 2 * j + rank) != LP_EPI_WARPS) {
+            if (*abort_flag) ok = false;
+            else if (clock64() - c0 > TC_WAIT_CYCLES) {
+              *abort_flag = 1;
+              jk_set_status(status, JK_ERR_TIMEOUT);
+              ok = false;
+            }
+          }
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        // the last warp to have seen them puts the flags back for the next call
+        if (lane == 0 && atomicAdd(&T.seen, 1u) == LP_EPI_WARPS - 1)
+          for (int j = from; j < pair; ++j) flags[2 * j + rank] = 0;
+        __syncwarp();
+      }
+      ok = mbar_wait(&T.acc_full[buf], (uint32_t)use & 1u, abort_flag, status);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * (MX ? LP_ACC2_MX : LP_N));
+#pragma unroll 1
+      for (int c = 0; c < CHUNKS; ++c) {
+        __syncwarp();
+        const int q = half ? (GATED ? 3 : 7) - c : c;                // chunk of 32 outputs
+        float v[32], u[GATED ? 32 : 1];
+        {
+          uint32_t t[32];
+          tmem_ld32(t_addr + (uint32_t)(q * 32), t);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(t[j]);
+          if constexpr (GATED) {
+            tmem_ld32(t_addr + (uint32_t)(LT_M + q * 32), t);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[j] = __uint_as_float(t[j]);
+          }
+        }
+        if ((MX && c == 0) || c == CHUNKS - 1) {
+          tc_fence_before();
+          __syncwarp();
+          // the columns that both accumulators use: the last 24 of the first, the first 24 of the second
+          if (MX && c == 0 && half != buf && lane == 0) lp_arrive(shared0);
+          if (c == CHUNKS - 1 && lane == 0) lp_arrive(acc_empty0 + 8u * (uint32_t)buf);
+        }
+        if (!whole) {
+          float* o = partial + (size_t)blockIdx.x * LT_SLOT + (size_t)(q * 32) * LT_M + quarter * 32 + lane;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            __stcg(o + j * LT_M, v[j]);
+            if constexpr (GATED) __stcg(o + (LT_M + j) * LT_M, u[j]);
+          }
+          continue;
+        }
+        for (int i = pair - 1; i >= from; --i) {
+          const float* o = partial + (size_t)(2 * i + rank) * LT_SLOT + (size_t)(q * 32) * LT_M + quarter * 32 + lane;
+          float t[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) t[j] = __ldcg(o + j * LT_M);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] += t[j];
+          if constexpr (GATED) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) t[j] = __ldcg(o + (LT_M + j) * LT_M);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[j] += t[j];
+          }
+        }
+        if (n0 + q * 32 < a.n_out && row0 < a.rows) lp_store<GATED>(a, v, u, row0, n0 + q * 32, my_x, wide != 0);
+      }
+      if (!whole) {
+        __syncwarp();
+        if (lane == 0) add_release(flags + blockIdx.x, 1);
+      }
+      ++seg;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  lp_cluster_sync();                       // nobody's memory is used any more
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------ host side
+int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
+  const bool gated = a.w_up != nullptr;
+  const int es = mx ? 1 : 2, box_el = LT_BOX / es;
+  lp_params p;
+  memset(&p, 0, sizeof(p));
+  p.n_tile = gated ? LT_M : LP_N;
+  p.r_tiles = (a.rows + LP_ROWS - 1) / LP_ROWS;
+  p.w_tiles = (a.n_out + p.n_tile - 1) / p.n_tile;
+  p.boxes = (a.n_in + box_el - 1) / box_el;
+  p.subs = (a.n_in * es + 31) / 32;
+  const long long tiles = (long long)p.r_tiles * p.w_tiles;
+  if (tiles > (1 << 28)) return JK_ERR_SHAPE;
+  int pairs = (ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS) / 2;
+  p.left = (int)(tiles % pairs);
+  p.full = (int)(tiles - p.left);
+  int most = LP_MAX_SPLIT < p.boxes ? LP_MAX_SPLIT : p.boxes;
+  p.sk_pairs = p.left * most < pairs ? p.left * most : pairs;
+  if (p.full == 0) pairs = p.sk_pairs;
+  CUtensorMap mx_map, mw, mu, msx, msw, msu;
+  auto map = [&](CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t stride) {
+    const uint64_t dims[2] = {(uint64_t)a.n_in, rows}, str[1] = {stride * es};
+    const uint32_t box[2] = {(uint32_t)box_el, LT_M};
+    return mx ? jk_tma_encode_u8(ctx, m, ptr, 2, dims, str, box) : jk_tma_encode_bf16(ctx, m, ptr, 2, dims, str, box);
+  };
+  int rc = map(&mx_map, a.x, a.rows, a.x_stride);
+  if (rc == JK_OK) rc = map(&mw, a.w, a.n_out, a.n_in);
+  mu = mw;
+  if (rc == JK_OK && gated) rc = map(&mu, a.w_up, a.n_out, a.n_in);
+  msx = msw = msu = mw;
+  if (mx) {
+    const uint64_t xt = (uint64_t)((a.rows + 127) / 128) * a.k_tiles_in, wt = (uint64_t)((a.n_out + 127) / 128) * a.k_tiles_in;
+    if (rc == JK_OK) rc = jk_tma_encode_scales(ctx, &msx, a.x_scale, xt);
+    if (rc == JK_OK) rc = jk_tma_encode_scales(ctx, &msw, a.w_scale, wt);
+    if (rc == JK_OK && gated) rc = jk_tma_encode_scales(ctx, &msu, a.w_up_scale, wt);
+  }
+  if (rc != JK_OK) return rc;
+  // rows of out (and of the residual) that begin at whole sectors are written (read) by the thread that has them
+  const int os = a.out_type == JK_ROWS_MX8 ? 1 : a.out_type == JK_ROWS_F32 ? 4 : 2;
+  int wide = ((uintptr_t)a.out % 32 == 0) && (a.o_stride * os) % 32 == 0;
+  if (a.residual && (a.r_stride * 2) % 16) wide = 0;
+  auto kernel = mx ? (gated ? k_linear_pair<true, true> : k_linear_pair<true, false>)
+                   : (gated ? k_linear_pair<false, true> : k_linear_pair<false, false>);
+  const size_t smem = (size_t)LP_STAGES * (mx ? lp_stage<true>::BYTES : lp_stage<false>::BYTES) +
+                      LP_EPI_WARPS * sizeof(lp_exchange) + sizeof(lp_tail) + 1024;
+  const int bit = 16 << (2 * mx + gated);
+  if (!(ctx->lin_smem_set & bit)) {
+    JK_CUDA_CHECK(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    ctx->lin_smem_set |= bit;
+  }
+  JK_PROF(ctx, st, JK_ST_LINEAR);
+  jk_launch_pdl_cluster(kernel, dim3(2 * pairs), dim3(LP_THREADS), 2, smem, st, mx_map, mw, mu, msx, msw, msu, p, a, wide,
+                        (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
+                        (int32_t*)(ctx->ws + ctx->lay.status));
+  JK_LAUNCH_CHECK(ctx);
+  return JK_OK;
+}
