@@ -153,24 +153,6 @@ __device__ __forceinline__ void lp_place(const lp_params& p, int tile, int& rt, 
 }
 
 // ------------------------------------------------------------------------------------------ epilogue
-// 32 elements of T at p as f32; those from `most` on are 0.
-__device__ __forceinline__ void lp_load32(const uint16_t* p, int most, float (&o)[32]) {
-  if (most >= 32 && ((uintptr_t)p & 15) == 0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 r = reinterpret_cast<const uint4*>(p)[i];
-      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        o[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-        o[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 32; ++j) o[j] = j < most ? __uint_as_float((uint32_t)p[j] << 16) : 0.f;
-  }
-}
 __device__ __forceinline__ uint32_t lp_pack(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -179,42 +161,44 @@ __device__ __forceinline__ uint32_t lp_pack(float a, float b) {
 // The lane's row (row0 + lane), outputs n .. n + 31.
 template <bool GATED>
 __device__ __forceinline__ void lp_store(const lin_args& a, float (&v)[32], float (&u)[GATED ? 32 : 1], int row0, int n,
-                                         lp_exchange& X, bool wide) {
+                                         float bias, float bias_up, const uint4 (&res)[4], lp_exchange& X, bool wide) {
   const int lane = threadIdx.x & 31, row = row0 + lane, most = a.n_out - n;
   const bool live = row < a.rows;
-  if (a.bias) {
-    float b[32];
-    lp_load32((const uint16_t*)a.bias + n, most, b);
+  if (a.bias) {                              // a lane holds the bias of output n + lane
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] += b[j];
+    for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bias, j);
   }
-  lin_act_all(v, a.act);
+  lin_act_all(v, a.act, a.out_type == JK_ROWS_F32);
   if constexpr (GATED) {
     if (a.bias_up) {
-      float b[32];
-      lp_load32((const uint16_t*)a.bias_up + n, most, b);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) u[j] += b[j];
+      for (int j = 0; j < 32; ++j) u[j] += __shfl_sync(0xffffffffu, bias_up, j);
     }
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] *= u[j];
   }
   if (a.residual) {
-    float r[32];
-    const uint16_t* rp = (const uint16_t*)a.residual + n;
     if (wide && most >= 32) {
-      lp_load32(rp + (size_t)(live ? row : row0) * a.r_stride, 32, r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w[4] = {res[i].x, res[i].y, res[i].z, res[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[8 * i + 2 * j] += __uint_as_float(w[j] << 16);
+          v[8 * i + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
+        }
+      }
     } else {
       // rows that begin anywhere: read along the rows, handed out through shared memory
+      const uint16_t* rp = (const uint16_t*)a.residual + (size_t)row0 * a.r_stride + n + lane;
       __syncwarp();
-      for (int j = 0; j < 32; ++j)
-        X.v[j * LP_STAGE_PITCH + lane] = row0 + j < a.rows && lane < most ? rp[(size_t)(row0 + j) * a.r_stride + lane] : (uint16_t)0;
+#pragma unroll 8
+      for (int j = 0; j < 32; ++j, rp += a.r_stride)
+        X.v[j * LP_STAGE_PITCH + lane] = row0 + j < a.rows && lane < most ? *rp : (uint16_t)0;
       __syncwarp();
 #pragma unroll
-      for (int j = 0; j < 32; ++j) r[j] = __uint_as_float((uint32_t)X.v[lane * LP_STAGE_PITCH + j] << 16);
+      for (int j = 0; j < 32; ++j) v[j] += __uint_as_float((uint32_t)X.v[lane * LP_STAGE_PITCH + j] << 16);
     }
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] += r[j];
   }
   if (a.out_type == JK_ROWS_MX8) {           // n_out is a multiple of 32: all of the block or nothing
     if (!live || most < 32) return;
@@ -447,6 +431,38 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
           for (int j = from; j < pair; ++j) flags[2 * j + rank] = 0;
         __syncwarp();
       }
+      // What a chunk needs beside the sums is asked for one chunk ahead: the partials of one other pair, the
+      // residual, the biases.  (Not in a gated block, whose chunk fills the registers by itself.)
+      constexpr bool AHEAD = !GATED;
+      auto chunk = [&](int c) { return half ? (GATED ? 3 : 7) - c : c; };
+      auto bias_of = [&](const void* b, int q) {
+        const int n = n0 + q * 32 + lane;
+        return b && whole && n < a.n_out ? __bfloat162float(((const __nv_bfloat16*)b)[n]) : 0.f;
+      };
+      // (a partial: 16 bytes of a lane next to the next lane's, 8 times for a chunk of 32 columns)
+      const size_t my_part = (size_t)quarter * LP_N * 32 + lane * 4;
+      float4 t[8], tu[GATED ? 8 : 1];
+      uint4 res[4];
+      float bias = 0.f, bias_up = 0.f;
+      auto ask_part = [&](int i, int q) {
+        const float* o = partial + (size_t)(2 * i + rank) * LT_SLOT + my_part + (size_t)q * 32 * 32;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          t[j] = __ldcg(reinterpret_cast<const float4*>(o + j * 128));
+          if constexpr (GATED) tu[j] = __ldcg(reinterpret_cast<const float4*>(o + LT_M * 32 + j * 128));
+        }
+      };
+      auto ask_rest = [&](int q) {
+        bias = bias_of(a.bias, q);
+        if constexpr (GATED) bias_up = bias_of(a.bias_up, q);
+        if (a.residual && wide && whole && n0 + q * 32 + 32 <= a.n_out && row0 + lane < a.rows) {
+          const uint4* rp = reinterpret_cast<const uint4*>((const uint16_t*)a.residual + (size_t)(row0 + lane) * a.r_stride + n0 + q * 32);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) res[i] = rp[i];
+        }
+      };
+      if (AHEAD && from < pair) ask_part(pair - 1, chunk(0));
+      if (AHEAD) ask_rest(chunk(0));
       ok = mbar_wait(&T.acc_full[buf], (uint32_t)use & 1u, abort_flag, status);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -455,19 +471,19 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
 #pragma unroll 1
       for (int c = 0; c < CHUNKS; ++c) {
         __syncwarp();
-        const int q = half ? (GATED ? 3 : 7) - c : c;                // chunk of 32 outputs
+        const int q = chunk(c);            // chunk of 32 outputs
         float v[32], u[GATED ? 32 : 1];
         {
-          uint32_t t[32];
-          tmem_ld32(t_addr + (uint32_t)(q * 32), t);
+          uint32_t w[32];
+          tmem_ld32(t_addr + (uint32_t)(q * 32), w);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(t[j]);
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(w[j]);
           if constexpr (GATED) {
-            tmem_ld32(t_addr + (uint32_t)(LT_M + q * 32), t);
+            tmem_ld32(t_addr + (uint32_t)(LT_M + q * 32), w);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) u[j] = __uint_as_float(t[j]);
+            for (int j = 0; j < 32; ++j) u[j] = __uint_as_float(w[j]);
           }
         }
         if ((MX && c == 0) || c == CHUNKS - 1) {
@@ -478,29 +494,32 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
           if (c == CHUNKS - 1 && lane == 0) lp_arrive(acc_empty0 + 8u * (uint32_t)buf);
         }
         if (!whole) {
-          float* o = partial + (size_t)blockIdx.x * LT_SLOT + (size_t)(q * 32) * LT_M + quarter * 32 + lane;
+          float* o = partial + (size_t)blockIdx.x * LT_SLOT + my_part + (size_t)q * 32 * 32;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            __stcg(o + j * LT_M, v[j]);
-            if constexpr (GATED) __stcg(o + (LT_M + j) * LT_M, u[j]);
+          for (int j = 0; j < 8; ++j) {
+            __stcg(reinterpret_cast<float4*>(o + j * 128), make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+            if constexpr (GATED)
+              __stcg(reinterpret_cast<float4*>(o + LT_M * 32 + j * 128),
+                     make_float4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]));
           }
           continue;
         }
         for (int i = pair - 1; i >= from; --i) {
-          const float* o = partial + (size_t)(2 * i + rank) * LT_SLOT + (size_t)(q * 32) * LT_M + quarter * 32 + lane;
-          float t[32];
+          if (!AHEAD || i < pair - 1) ask_part(i, q);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) t[j] = __ldcg(o + j * LT_M);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] += t[j];
-          if constexpr (GATED) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) t[j] = __ldcg(o + (LT_M + j) * LT_M);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) u[j] += t[j];
+          for (int j = 0; j < 8; ++j) {
+            v[4 * j] += t[j].x; v[4 * j + 1] += t[j].y; v[4 * j + 2] += t[j].z; v[4 * j + 3] += t[j].w;
+            if constexpr (GATED) {
+              u[4 * j] += tu[j].x; u[4 * j + 1] += tu[j].y; u[4 * j + 2] += tu[j].z; u[4 * j + 3] += tu[j].w;
+            }
           }
         }
-        if (n0 + q * 32 < a.n_out && row0 < a.rows) lp_store<GATED>(a, v, u, row0, n0 + q * 32, my_x, wide != 0);
+        const int qn = chunk(c + 1 < CHUNKS ? c + 1 : c);
+        if (AHEAD && from < pair && c + 1 < CHUNKS) ask_part(pair - 1, qn);
+        if (!AHEAD) ask_rest(q);
+        if (n0 + q * 32 < a.n_out && row0 < a.rows)
+          lp_store<GATED>(a, v, u, row0, n0 + q * 32, bias, bias_up, res, my_x, wide != 0);
+        if (AHEAD && c + 1 < CHUNKS) ask_rest(qn);
       }
       if (!whole) {
         __syncwarp();

@@ -104,7 +104,7 @@ __device__ __forceinline__ void lt_store(const lin_args& a, float (&v)[LT_COLS],
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int j = 0; j < LT_COLS; ++j) v[j] += bias;
-  lin_act_all(v, a.act);
+  lin_act_all(v, a.act, a.out_type == JK_ROWS_F32);
   if constexpr (GATED) {
 #pragma unroll
     for (int j = 0; j < LT_COLS; ++j) v[j] *= u[j] + bias_up;
