@@ -916,3 +916,13 @@ int jk_tma_encode_scales(jk_ctx* ctx, CUtensorMap* out, const void* ptr, uint64_
   const uint32_t box[2] = {128, 1};
   return tma_encode(ctx, out, CU_TENSOR_MAP_DATA_TYPE_UINT32, CU_TENSOR_MAP_SWIZZLE_NONE, ptr, 2, dims, str, box);
 }
+
+// Pieces of 32 rows of an array of 1-, 2- or 4-byte elements; the swizzle spans a piece's row (64 or 32 bytes).
+int jk_tma_encode_piece(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int es, uint64_t cols, uint64_t rows, uint64_t stride,
+                        uint32_t box_cols) {
+  const uint64_t dims[2] = {cols, rows}, str[1] = {stride * es};
+  const uint32_t box[2] = {box_cols, 32};
+  return tma_encode(ctx, out, es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
+                    box_cols * es == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B, ptr, 2, dims, str, box);
+}

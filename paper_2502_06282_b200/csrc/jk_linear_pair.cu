@@ -23,6 +23,8 @@
 int jk_tma_encode_u8(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, const uint64_t* dims,
                      const uint64_t* strides_bytes, const uint32_t* box);
 int jk_tma_encode_scales(jk_ctx* ctx, CUtensorMap* out, const void* ptr, uint64_t tiles);
+int jk_tma_encode_piece(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int es, uint64_t cols, uint64_t rows, uint64_t stride,
+                        uint32_t box_cols);
 
 #define LP_ROWS 256                       // rows of x of a pair's tile
 #define LP_N 256                          // weight rows of a pair's tile
@@ -31,10 +33,11 @@ int jk_tma_encode_scales(jk_ctx* ctx, CUtensorMap* out, const void* ptr, uint64_
 #define LP_EPI_WARPS 8
 #define LP_THREADS (64 + 32 * LP_EPI_WARPS)
 #define LP_A_BYTES (LT_M * LT_BOX)        // of each operand in a box
-#define LP_STAGES 6
 #define LP_SF_COL 488                     // 8-bit rows: first column of the scales, two sets of 12
 #define LP_ACC2_MX 232                    // 8-bit rows: first column of the second accumulator
-#define LP_STAGE_PITCH 34                 // elements of a row in an epilogue warp's 32 x 32 exchange
+#define LP_MAX_STAGES 6
+#define LP_OUT_BYTES 2048                 // an epilogue warp's piece of the output: 32 rows of at most 64 bytes; two of them
+#define LP_X_PITCH 34                     // the same memory as a 32 x 32 exchange: elements of a row
 
 struct lp_params {
   int r_tiles, w_tiles;
@@ -45,16 +48,16 @@ struct lp_params {
 };
 
 struct __align__(16) lp_tail {
-  uint64_t full[LP_STAGES], empty[LP_STAGES];
+  uint64_t full[LP_MAX_STAGES], empty[LP_MAX_STAGES];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t shared_free;                   // the columns both accumulators use have been read
+  uint64_t res_full[LP_EPI_WARPS][2];     // a warp's piece of the residual
   uint32_t tmem_base;
   int abort_flag;
   unsigned seen;                          // epilogue warps that have seen all flags
 };
-struct __align__(16) lp_exchange { uint16_t v[32 * LP_STAGE_PITCH]; };
 
-template <bool MX> struct lp_stage { static constexpr int BYTES = 2 * LP_A_BYTES + (MX ? 2048 : 0); };
+template <bool MX> struct lp_ring { static constexpr int BYTES = 2 * LP_A_BYTES + (MX ? 2048 : 0), STAGES = MX ? 5 : 6; };
 
 // ------------------------------------------------------------------------------------------ PTX
 // Loads of a pair: the barrier is the first CTA's, whichever CTA the data is for.
@@ -108,11 +111,14 @@ __host__ __device__ inline uint32_t lp_idesc_bf16() {
 __host__ __device__ inline uint32_t lp_idesc_mx8(int k) {
   return ((uint32_t)k << 4) | ((uint32_t)(LP_N >> 3) << 17) | (1u << 23) | ((uint32_t)(LP_ROWS >> 7) << 27) | ((uint32_t)k << 29);
 }
-// 32 bytes at once
-__device__ __forceinline__ void st32b(void* p, const uint32_t (&v)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
-               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+// A warp's piece of the output, 32 rows, from shared memory; columns and rows past the array's end are left out.
+__device__ __forceinline__ void lp_put(const CUtensorMap* map, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
                : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+template <int LEFT> __device__ __forceinline__ void lp_put_read() {        // all but the last LEFT pieces have been read
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------ the deal
@@ -158,118 +164,41 @@ __device__ __forceinline__ uint32_t lp_pack(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The lane's row (row0 + lane), outputs n .. n + 31.
-template <bool GATED>
-__device__ __forceinline__ void lp_store(const lin_args& a, float (&v)[32], float (&u)[GATED ? 32 : 1], int row0, int n,
-                                         float bias, float bias_up, const uint4 (&res)[4], lp_exchange& X, bool wide) {
-  const int lane = threadIdx.x & 31, row = row0 + lane, most = a.n_out - n;
-  const bool live = row < a.rows;
-  if (a.bias) {                              // a lane holds the bias of output n + lane
+// 32 elements of T from p as f32, the same for all lanes; those from `most` on are 0.
+__device__ __forceinline__ void lp_add32(float (&v)[32], const uint16_t* p, int most) {
+  if (most >= 32) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bias, j);
-  }
-  lin_act_all(v, a.act, a.out_type == JK_ROWS_F32);
-  if constexpr (GATED) {
-    if (a.bias_up) {
+    for (int i = 0; i < 4; ++i) {
+      const uint4 r = __ldg(reinterpret_cast<const uint4*>(p) + i);
+      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-      for (int j = 0; j < 32; ++j) u[j] += __shfl_sync(0xffffffffu, bias_up, j);
-    }
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] *= u[j];
-  }
-  if (a.residual) {
-    if (wide && most >= 32) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t w[4] = {res[i].x, res[i].y, res[i].z, res[i].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[8 * i + 2 * j] += __uint_as_float(w[j] << 16);
-          v[8 * i + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
-        }
+      for (int j = 0; j < 4; ++j) {
+        v[8 * i + 2 * j] += __uint_as_float(w[j] << 16);
+        v[8 * i + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
       }
-    } else {
-      // rows that begin anywhere: read along the rows, handed out through shared memory
-      const uint16_t* rp = (const uint16_t*)a.residual + (size_t)row0 * a.r_stride + n + lane;
-      __syncwarp();
-#pragma unroll 8
-      for (int j = 0; j < 32; ++j, rp += a.r_stride)
-        X.v[j * LP_STAGE_PITCH + lane] = row0 + j < a.rows && lane < most ? *rp : (uint16_t)0;
-      __syncwarp();
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] += __uint_as_float((uint32_t)X.v[lane * LP_STAGE_PITCH + j] << 16);
-    }
-  }
-  if (a.out_type == JK_ROWS_MX8) {           // n_out is a multiple of 32: all of the block or nothing
-    if (!live || most < 32) return;
-    float m = 0.f;
-#pragma unroll
-    for (int j = 0; j < 32; ++j) m = fmaxf(m, paged_mag(v[j]));
-    const int e = paged_scale_exp(m);
-    const float inv = paged_pow2(-e);
-    uint32_t o[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = paged_pack4(v[4 * j] * inv, v[4 * j + 1] * inv, v[4 * j + 2] * inv, v[4 * j + 3] * inv);
-    uint8_t* p = (uint8_t*)a.out + (size_t)row * a.n_out + n;
-    if (wide) {
-      st32b(p, o);
-    } else {
-      reinterpret_cast<uint4*>(p)[0] = make_uint4(o[0], o[1], o[2], o[3]);
-      reinterpret_cast<uint4*>(p)[1] = make_uint4(o[4], o[5], o[6], o[7]);
-    }
-    a.out_scale[mx_scale_at(row, n >> 5, a.k_tiles_out)] = (uint8_t)(e + 127);
-  } else if (a.out_type == JK_ROWS_F32) {
-    if (wide && most >= 32) {
-      if (!live) return;
-      float* p = (float*)a.out + (size_t)row * a.o_stride + n;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t o[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(v[8 * i + j]);
-        st32b(p + 8 * i, o);
-      }
-    } else {
-      float* p = (float*)a.out + (size_t)row * a.o_stride + n;
-#pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (live && j < most) p[j] = v[j];
-    }
-  } else if (wide && most >= 32) {
-    if (!live) return;
-    __nv_bfloat16* p = (__nv_bfloat16*)a.out + (size_t)row * a.o_stride + n;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t o[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = lp_pack(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]);
-      st32b(p + 16 * i, o);
     }
   } else {
-    __syncwarp();
-    uint32_t* x32 = reinterpret_cast<uint32_t*>(&X.v[lane * LP_STAGE_PITCH]);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) x32[j] = lp_pack(v[2 * j], v[2 * j + 1]);
-    __syncwarp();
-    uint16_t* p = (uint16_t*)a.out + (size_t)row0 * a.o_stride + n + lane;
-    for (int j = 0; j < 32; ++j, p += a.o_stride)
-      if (row0 + j < a.rows && lane < most) *p = X.v[j * LP_STAGE_PITCH + lane];
-    __syncwarp();
+    for (int j = 0; j < 32; ++j) v[j] += j < most ? __uint_as_float((uint32_t)p[j] << 16) : 0.f;
   }
 }
+// Where the copy engine has 16-byte chunk c of row r: pieces with rows of 64 bytes, and of 32.
+__device__ __forceinline__ uint32_t lp_at64(int r, int c) { return (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); }
+__device__ __forceinline__ uint32_t lp_at32(int r, int c) { return (uint32_t)(r * 32 + ((c ^ ((r >> 2) & 1)) << 4)); }
 
 // ------------------------------------------------------------------------------------------ the kernel
 template <bool MX, bool GATED>
 __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
     const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u,
     const __grid_constant__ CUtensorMap map_sx, const __grid_constant__ CUtensorMap map_sw,
-    const __grid_constant__ CUtensorMap map_su, const lp_params p, const lin_args a, int wide, float* __restrict__ partial,
-    int32_t* flags, int32_t* status) {
-  constexpr int BOX_EL = MX ? 128 : 64, STAGE = lp_stage<MX>::BYTES;
+    const __grid_constant__ CUtensorMap map_su, const __grid_constant__ CUtensorMap map_out,
+    const __grid_constant__ CUtensorMap map_res, const lp_params p, const lin_args a, int wide_out, int wide_res,
+    float* __restrict__ partial, int32_t* flags, int32_t* status) {
+  constexpr int BOX_EL = MX ? 128 : 64, STAGE = lp_ring<MX>::BYTES, LP_STAGES = lp_ring<MX>::STAGES;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  lp_exchange* X = reinterpret_cast<lp_exchange*>(smem + LP_STAGES * STAGE);
-  lp_tail& T = *reinterpret_cast<lp_tail*>(X + LP_EPI_WARPS);
+  unsigned char* pieces = smem + LP_STAGES * STAGE;
+  lp_tail& T = *reinterpret_cast<lp_tail*>(pieces + LP_EPI_WARPS * 2 * LP_OUT_BYTES);
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   volatile int* abort_flag = &T.abort_flag;
@@ -278,6 +207,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
     for (int s = 0; s < LP_STAGES; ++s) { mbar_init(&T.full[s], 1); mbar_init(&T.empty[s], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&T.acc_full[i], 1); mbar_init(&T.acc_empty[i], 2 * LP_EPI_WARPS); }
     mbar_init(&T.shared_free, LP_EPI_WARPS);           // four warps of each CTA
+    for (int i = 0; i < LP_EPI_WARPS; ++i) { mbar_init(&T.res_full[i][0], 1); mbar_init(&T.res_full[i][1], 1); }
     T.abort_flag = 0;
     T.seen = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -397,7 +327,10 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
     // ------------------------------------------------------------------ epilogue
     const int quarter = warp & 3;          // the lanes of tensor memory this warp may read
     const int half = (warp - 2) >> 2;      // the columns 0 .. 127 upwards, or 255 .. 128 downwards
-    lp_exchange& my_x = X[warp - 2];
+    unsigned char* mine = pieces + (warp - 2) * 2 * LP_OUT_BYTES;    // 1024-byte aligned: two pieces
+    const uint32_t mine_u32 = smem_u32(mine);
+    uint64_t* res_full = T.res_full[warp - 2];
+    uint32_t res_ph = 0;                   // phases of the two, a bit each
     const uint32_t acc_empty0 = lp_map(smem_u32(T.acc_empty), 0), shared0 = lp_map(smem_u32(&T.shared_free), 0);
     constexpr int CHUNKS = GATED ? 2 : 4;  // of 32 outputs, for this warp
     int seg = 0;
@@ -431,19 +364,22 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
           for (int j = from; j < pair; ++j) flags[2 * j + rank] = 0;
         __syncwarp();
       }
-      // What a chunk needs beside the sums is asked for one chunk ahead: the partials of one other pair, the
-      // residual, the biases.  (Not in a gated block, whose chunk fills the registers by itself.)
-      constexpr bool AHEAD = !GATED;
       auto chunk = [&](int c) { return half ? (GATED ? 3 : 7) - c : c; };
-      auto bias_of = [&](const void* b, int q) {
-        const int n = n0 + q * 32 + lane;
-        return b && whole && n < a.n_out ? __bfloat162float(((const __nv_bfloat16*)b)[n]) : 0.f;
+      const bool rows_live = row0 < a.rows;
+      // The residual of a chunk is brought to the piece that the chunk's outputs will take.
+      auto ask_residual = [&](int c) {
+        const int n = n0 + chunk(c) * 32;
+        if (lane == 0 && n < a.n_out && rows_live) {
+          lp_put_read<0>();                // (the piece's last outputs have been read)
+          lt_expect(smem_u32(&res_full[c & 1]), LP_OUT_BYTES, 1u);
+          lt_box(mine_u32 + (c & 1) * LP_OUT_BYTES, &map_res, n, row0, smem_u32(&res_full[c & 1]), 1u);
+        }
       };
+      const bool res_tma = whole && a.residual && wide_res;
+      if (res_tma) ask_residual(0);
       // (a partial: 16 bytes of a lane next to the next lane's, 8 times for a chunk of 32 columns)
       const size_t my_part = (size_t)quarter * LP_N * 32 + lane * 4;
       float4 t[8], tu[GATED ? 8 : 1];
-      uint4 res[4];
-      float bias = 0.f, bias_up = 0.f;
       auto ask_part = [&](int i, int q) {
         const float* o = partial + (size_t)(2 * i + rank) * LT_SLOT + my_part + (size_t)q * 32 * 32;
 #pragma unroll
@@ -452,17 +388,9 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
           if constexpr (GATED) tu[j] = __ldcg(reinterpret_cast<const float4*>(o + LT_M * 32 + j * 128));
         }
       };
-      auto ask_rest = [&](int q) {
-        bias = bias_of(a.bias, q);
-        if constexpr (GATED) bias_up = bias_of(a.bias_up, q);
-        if (a.residual && wide && whole && n0 + q * 32 + 32 <= a.n_out && row0 + lane < a.rows) {
-          const uint4* rp = reinterpret_cast<const uint4*>((const uint16_t*)a.residual + (size_t)(row0 + lane) * a.r_stride + n0 + q * 32);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) res[i] = rp[i];
-        }
-      };
+      // (one other pair's partials are asked for a chunk ahead; not in a gated block, whose chunk fills the registers)
+      constexpr bool AHEAD = !GATED;
       if (AHEAD && from < pair) ask_part(pair - 1, chunk(0));
-      if (AHEAD) ask_rest(chunk(0));
       ok = mbar_wait(&T.acc_full[buf], (uint32_t)use & 1u, abort_flag, status);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -514,19 +442,121 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
             }
           }
         }
-        const int qn = chunk(c + 1 < CHUNKS ? c + 1 : c);
-        if (AHEAD && from < pair && c + 1 < CHUNKS) ask_part(pair - 1, qn);
-        if (!AHEAD) ask_rest(q);
-        if (n0 + q * 32 < a.n_out && row0 < a.rows)
-          lp_store<GATED>(a, v, u, row0, n0 + q * 32, bias, bias_up, res, my_x, wide != 0);
-        if (AHEAD && c + 1 < CHUNKS) ask_rest(qn);
+        if (AHEAD && from < pair && c + 1 < CHUNKS) ask_part(pair - 1, chunk(c + 1));
+        if (res_tma && c + 1 < CHUNKS) ask_residual(c + 1);
+        const int n = n0 + q * 32, most = a.n_out - n;
+        if (most <= 0 || !rows_live) continue;
+        unsigned char* piece = mine + (c & 1) * LP_OUT_BYTES;
+        // ---- the epilogue proper: the lane's row, outputs n .. n + 31
+        if (a.bias) lp_add32(v, (const uint16_t*)a.bias + n, most);
+        lin_act_all(v, a.act, a.out_type == JK_ROWS_F32);
+        if constexpr (GATED) {
+          if (a.bias_up) lp_add32(u, (const uint16_t*)a.bias_up + n, most);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] *= u[j];
+        }
+        if (res_tma) {
+          ok = mbar_wait(&res_full[c & 1], (res_ph >> (c & 1)) & 1u, abort_flag, status);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          res_ph ^= 1u << (c & 1);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint4 r = *reinterpret_cast<const uint4*>(piece + lp_at64(lane, i));
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              v[8 * i + 2 * j] += __uint_as_float(w[j] << 16);
+              v[8 * i + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
+            }
+          }
+        } else {
+          if (lane == 0) {                 // the piece's last outputs have been read
+            if (wide_out && a.out_type != JK_ROWS_F32 && !a.residual) lp_put_read<1>();
+            else lp_put_read<0>();
+          }
+          __syncwarp();
+          if (a.residual) {
+            // rows that begin anywhere: read along the rows, handed out through shared memory
+            uint16_t* X = reinterpret_cast<uint16_t*>(mine);
+            const uint16_t* rp = (const uint16_t*)a.residual + (size_t)row0 * a.r_stride + n + lane;
+#pragma unroll 8
+            for (int j = 0; j < 32; ++j, rp += a.r_stride)
+              X[j * LP_X_PITCH + lane] = row0 + j < a.rows && lane < most ? *rp : (uint16_t)0;
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += __uint_as_float((uint32_t)X[lane * LP_X_PITCH + j] << 16);
+            __syncwarp();
+          }
+        }
+        if (a.out_type == JK_ROWS_MX8) {   // n_out is a multiple of 32: all of the block or nothing
+          float m = 0.f;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) m = fmaxf(m, paged_mag(v[j]));
+          const int e = paged_scale_exp(m);
+          const float inv = paged_pow2(-e);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t o[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              o[j] = paged_pack4(v[16 * i + 4 * j] * inv, v[16 * i + 4 * j + 1] * inv, v[16 * i + 4 * j + 2] * inv, v[16 * i + 4 * j + 3] * inv);
+            *reinterpret_cast<uint4*>(piece + lp_at32(lane, i)) = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+          if (row0 + lane < a.rows) a.out_scale[mx_scale_at(row0 + lane, n >> 5, a.k_tiles_out)] = (uint8_t)(e + 127);
+        } else if (a.out_type == JK_ROWS_T) {
+          if (wide_out) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<uint4*>(piece + lp_at64(lane, i)) =
+                  make_uint4(lp_pack(v[8 * i], v[8 * i + 1]), lp_pack(v[8 * i + 2], v[8 * i + 3]),
+                             lp_pack(v[8 * i + 4], v[8 * i + 5]), lp_pack(v[8 * i + 6], v[8 * i + 7]));
+          } else {
+            uint16_t* X = reinterpret_cast<uint16_t*>(mine);
+            uint32_t* x32 = reinterpret_cast<uint32_t*>(&X[lane * LP_X_PITCH]);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x32[j] = lp_pack(v[2 * j], v[2 * j + 1]);
+            __syncwarp();
+            uint16_t* o = (uint16_t*)a.out + (size_t)row0 * a.o_stride + n + lane;
+#pragma unroll 8
+            for (int j = 0; j < 32; ++j, o += a.o_stride)
+              if (row0 + j < a.rows && lane < most) *o = X[j * LP_X_PITCH + lane];
+          }
+        } else if (wide_out) {             // f32: 16 outputs to a piece
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<uint4*>(mine + h * LP_OUT_BYTES + lp_at64(lane, i)) =
+                  make_uint4(__float_as_uint(v[16 * h + 4 * i]), __float_as_uint(v[16 * h + 4 * i + 1]),
+                             __float_as_uint(v[16 * h + 4 * i + 2]), __float_as_uint(v[16 * h + 4 * i + 3]));
+        } else if (row0 + lane < a.rows) {
+          float* o = (float*)a.out + (size_t)(row0 + lane) * a.o_stride + n;
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (j < most) o[j] = v[j];
+        }
+        if (wide_out) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (a.out_type == JK_ROWS_F32) {
+              lp_put(&map_out, n, row0, mine_u32);
+              if (most > 16) lp_put(&map_out, n + 16, row0, mine_u32 + LP_OUT_BYTES);
+            } else {
+              lp_put(&map_out, n, row0, mine_u32 + (c & 1) * LP_OUT_BYTES);
+            }
+          }
+        }
       }
+      if (!ok) break;
       if (!whole) {
         __syncwarp();
         if (lane == 0) add_release(flags + blockIdx.x, 1);
       }
       ++seg;
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
@@ -574,22 +604,26 @@ int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
     if (rc == JK_OK && gated) rc = jk_tma_encode_scales(ctx, &msu, a.w_up_scale, wt);
   }
   if (rc != JK_OK) return rc;
-  // rows of out (and of the residual) that begin at whole sectors are written (read) by the thread that has them
-  const int os = a.out_type == JK_ROWS_MX8 ? 1 : a.out_type == JK_ROWS_F32 ? 4 : 2;
-  int wide = ((uintptr_t)a.out % 32 == 0) && (a.o_stride * os) % 32 == 0;
-  if (a.residual && (a.r_stride * 2) % 16) wide = 0;
+  // Outputs and residuals whose rows begin at multiples of 16 bytes go through the copy engine, in pieces of 32 rows.
+  const bool f32 = a.out_type == JK_ROWS_F32, q8 = a.out_type == JK_ROWS_MX8;
+  const int os = q8 ? 1 : f32 ? 4 : 2;
+  const int wide_out = (a.o_stride * os) % 16 == 0, wide_res = a.residual && wide_out && !f32 && (a.r_stride * 2) % 16 == 0;
+  CUtensorMap mo = mw, mr = mw;
+  if (wide_out) rc = jk_tma_encode_piece(ctx, &mo, a.out, q8 ? 1 : f32 ? 4 : 2, a.n_out, a.rows, a.o_stride, f32 ? 16 : 32);
+  if (rc == JK_OK && wide_res) rc = jk_tma_encode_piece(ctx, &mr, a.residual, 2, a.n_out, a.rows, a.r_stride, 32);
+  if (rc != JK_OK) return rc;
   auto kernel = mx ? (gated ? k_linear_pair<true, true> : k_linear_pair<true, false>)
                    : (gated ? k_linear_pair<false, true> : k_linear_pair<false, false>);
-  const size_t smem = (size_t)LP_STAGES * (mx ? lp_stage<true>::BYTES : lp_stage<false>::BYTES) +
-                      LP_EPI_WARPS * sizeof(lp_exchange) + sizeof(lp_tail) + 1024;
+  const size_t smem = (size_t)(mx ? lp_ring<true>::STAGES * lp_ring<true>::BYTES : lp_ring<false>::STAGES * lp_ring<false>::BYTES) +
+                      LP_EPI_WARPS * 2 * LP_OUT_BYTES + sizeof(lp_tail) + 1024;
   const int bit = 16 << (2 * mx + gated);
   if (!(ctx->lin_smem_set & bit)) {
     JK_CUDA_CHECK(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     ctx->lin_smem_set |= bit;
   }
   JK_PROF(ctx, st, JK_ST_LINEAR);
-  jk_launch_pdl_cluster(kernel, dim3(2 * pairs), dim3(LP_THREADS), 2, smem, st, mx_map, mw, mu, msx, msw, msu, p, a, wide,
-                        (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
+  jk_launch_pdl_cluster(kernel, dim3(2 * pairs), dim3(LP_THREADS), 2, smem, st, mx_map, mw, mu, msx, msw, msu, mo, mr, p, a,
+                        wide_out, wide_res,                        (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
                         (int32_t*)(ctx->ws + ctx->lay.status));
   JK_LAUNCH_CHECK(ctx);
   return JK_OK;
