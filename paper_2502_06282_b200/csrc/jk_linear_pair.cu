@@ -45,6 +45,7 @@ struct lp_params {
   int n_tile;                             // outputs of a tile: 256, gated 128
   int full;                               // tiles dealt whole
   int left, sk_pairs;                     // tiles cut along k, and the pairs that share them
+  int pairs;
 };
 
 struct __align__(16) lp_tail {
@@ -568,7 +569,11 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
 }
 
 // ------------------------------------------------------------------------------------------ host side
-int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
+// The deal.  The tiles of the last, incomplete turn: whole (a turn more), or cut among 2, 3 or 4 pairs each, which costs
+// the hand-over: 18, 24, 31 boxes' time (5.6, 7.5 and 9.6 us measured at 16 tiles, a box 0.31).  Cut at K = 8192 in bf16,
+// 16 tiles: 43.7 us whole, 31.9, 28.1, 27.2 among 2, 3, 4; at K = 2048: 16.4 whole, 17.5, 18.0, 19.4.  Returns the cost
+// in us, with a launch.
+double jk_linear_pair_plan(const lin_args& a, bool mx, int sms, lp_params* out) {
   const bool gated = a.w_up != nullptr;
   const int es = mx ? 1 : 2, box_el = LT_BOX / es;
   lp_params p;
@@ -579,15 +584,10 @@ int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   p.boxes = (a.n_in + box_el - 1) / box_el;
   p.subs = (a.n_in * es + 31) / 32;
   const long long tiles = (long long)p.r_tiles * p.w_tiles;
-  if (tiles > (1 << 28)) return JK_ERR_SHAPE;
-  int pairs = (ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS) / 2;
-  // The tiles of the last, incomplete turn: whole (a turn more), or cut among 2, 3 or 4 pairs each, which costs
-  // the hand-over: 18, 24, 31 boxes' time (5.6, 7.5 and 9.6 us measured at 16 tiles, a box 0.31).  Cut at K = 8192 in bf16,
-  // 16 tiles: 43.7 us whole, 31.9, 28.1, 27.2 among 2, 3, 4; at K = 2048: 16.4 whole, 17.5, 18.0, 19.4.
+  const int pairs = sms / 2, left = (int)(tiles % pairs);
   static const int hand_over[LP_MAX_SPLIT] = {0, 18, 24, 31};
-  const int left = (int)(tiles % pairs);
   int split = 1;
-  double best = p.boxes;
+  double best = left ? p.boxes : 0;
   for (int s = 2; left && s <= LP_MAX_SPLIT && s <= p.boxes && left * (s - 1) < pairs; ++s) {
     const int on = left * s < pairs ? left * s : pairs;
     const double cost = (double)left * p.boxes / on + hand_over[s - 1];
@@ -596,7 +596,17 @@ int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   p.left = split > 1 ? left : 0;
   p.full = (int)(tiles - p.left);
   p.sk_pairs = p.left * split < pairs ? p.left * split : pairs;
-  if (tiles < pairs) pairs = p.left ? p.sk_pairs : p.full;
+  p.pairs = tiles >= pairs ? pairs : p.left ? p.sk_pairs : p.full;
+  if (out) *out = p;
+  const double us = 0.31 * (best + (double)(tiles / pairs) * p.boxes), hbm_us = (double)a.n_out * a.n_in * es * (1 + gated) / 6.4e6;
+  return 6.9 + (us > hbm_us ? us : hbm_us);
+}
+
+int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
+  const bool gated = a.w_up != nullptr;
+  const int es = mx ? 1 : 2, box_el = LT_BOX / es;
+  lp_params p;
+  jk_linear_pair_plan(a, mx, ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS, &p);
   CUtensorMap mx_map, mw, mu, msx, msw, msu;
   auto map = [&](CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t stride) {
     const uint64_t dims[2] = {(uint64_t)a.n_in, rows}, str[1] = {stride * es};
@@ -633,7 +643,7 @@ int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
     ctx->lin_smem_set |= bit;
   }
   JK_PROF(ctx, st, JK_ST_LINEAR);
-  jk_launch_pdl_cluster(kernel, dim3(2 * pairs), dim3(LP_THREADS), 2, smem, st, mx_map, mw, mu, msx, msw, msu, mo, mr, p, a,
+  jk_launch_pdl_cluster(kernel, dim3(2 * p.pairs), dim3(LP_THREADS), 2, smem, st, mx_map, mw, mu, msx, msw, msu, mo, mr, p, a,
                         wide_out, wide_res,                        (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
                         (int32_t*)(ctx->ws + ctx->lay.status));
   JK_LAUNCH_CHECK(ctx);

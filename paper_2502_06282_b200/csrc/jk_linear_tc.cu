@@ -8,8 +8,8 @@
 // they belong to and are copied to tensor memory by tcgen05.cp ahead of its products.  A gated block
 // multiplies the same x box with a tile of w and a tile of w_up into two accumulators.
 //
-// The k steps of all tiles form one line, dealt out evenly over one CTA per SM: whatever the shape,
-// every SM streams the same share of the weights.  A tile that spans CTAs is finished by the CTA that
+// The k steps of all tiles form one line, dealt out evenly over one CTA per SM, or over as many CTAs as pay for
+// handing sums over (jk_linear_tc_plan).  A tile that spans CTAs is finished by the CTA that
 // has its last k step; the others hand over f32 partials through the workspace.  A CTA works its share
 // from the back, so its only unfinished tile comes first and its partial is long there when the
 // CTA behind it asks; it waits only for CTAs of lower index, which were launched before it.  Sums
@@ -46,6 +46,8 @@ struct lt_params {
   int sfb;                                // scale tiles of a tile of x (8-bit rows)
   int stream;                             // 1: weights are read once, L2 need not keep them
   long long units;                        // stages of all tiles
+  int by_tile;                            // 1: the shares end with tiles
+  int grid;
 };
 
 struct __align__(16) lt_tail {
@@ -65,8 +67,10 @@ __host__ __device__ inline uint32_t lt_idesc_mx8(int n, int k) {
          ((uint32_t)k << 29);
 }
 // ------------------------------------------------------------------------------------------ the deal
-// CTA i has the units [i U / G, (i + 1) U / G); unit u is stage u % ks of tile u / ks.
-__device__ __forceinline__ long long lt_first(const lt_params& p, int i) { return p.units * i / gridDim.x; }
+// CTA i has the units [i U / G, (i + 1) U / G), or as many tiles; unit u is stage u % ks of tile u / ks.
+__device__ __forceinline__ long long lt_first(const lt_params& p, int i) {
+  return p.by_tile ? p.units / p.ks * i / gridDim.x * p.ks : p.units * i / gridDim.x;
+}
 
 struct lt_walk {                           // a CTA's segments, last tile first
   long long lo, hi;
@@ -458,7 +462,12 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
 }
 
 // ------------------------------------------------------------------------------------------ host side
-int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
+// Into how many shares the tiles are cut.  One SM takes in about 118 bytes a nanosecond and one box in 0.19 us at best
+// (gated: two); all together 6400.  What is cut has to be handed over: 1.5 us and 0.02 for each column of the
+// accumulators, a quarter more for each further share.  Measured with 4096 outputs, 64 boxes (bf16, 4096 inputs), us:
+// 60 rows 18.3 whole, 15.1, 13.5, 12.5 with 2, 3, 4 shares, 12.5 with 4.6; 8 boxes: 7.3 whole, 8.4, 8.3, 8.8.  The costs,
+// in us and with a launch, also choose between this kernel and that for many rows.
+double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, lt_params* out) {
   const int G = a.w_up ? 2 : 1, es = mx ? 1 : 2, box_el = LT_BOX / es;
   lt_params p;
   memset(&p, 0, sizeof(p));
@@ -483,11 +492,31 @@ int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   p.tmem_cols = 32;
   while (p.tmem_cols < p.sf_col + sf_cols) p.tmem_cols <<= 1;
   p.stream = p.r_tiles == 1;
-  p.units = (long long)p.w_tiles * p.r_tiles * p.ks;
-  int grid = ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS;
-  // (at most LT_MAX_SPLIT CTAs for a tile: the last of them adds up what the others hand over)
-  const long long useful = (long long)p.w_tiles * p.r_tiles * (p.ks < LT_MAX_SPLIT ? p.ks : LT_MAX_SPLIT);
-  if (useful < grid) grid = (int)useful;
+  const long long tiles = (long long)p.w_tiles * p.r_tiles;
+  p.units = tiles * p.ks;
+  const double box_us = box_bytes / 118e3 > 0.185 * G ? box_bytes / 118e3 : 0.185 * G;
+  const double tile_us = box_us * p.boxes, hbm_us = (double)a.n_out * a.n_in * es * G / 6.4e6, per_tile_hbm = hbm_us / p.w_tiles;
+  const long long full = tiles / sms, left = tiles - full * sms;
+  const auto larger = [](double x, double y) { return x > y ? x : y; };
+  double best = full * larger(tile_us, sms * per_tile_hbm) + (left ? larger(tile_us, left * per_tile_hbm) : 0.);
+  p.by_tile = 1;
+  p.grid = tiles < sms ? (int)tiles : sms;
+  for (int s = 2; s <= LT_MAX_SPLIT && s <= p.ks; s = s < 4 ? s + 1 : 2 * s) {
+    if (s > 4 && G * p.nt > 64) break;                     // (their partials do not fit the ring at once)
+    const int grid = tiles * s < sms ? (int)(tiles * s) : sms;
+    const double shares = (double)grid / tiles, over = 1.5 + 0.02 * G * p.nt * (shares > 2. ? 0.5 + 0.25 * shares : 1.);
+    const double cost = larger(tile_us / shares, hbm_us * p.r_tiles) + over;
+    if (cost < best) { best = cost; p.by_tile = 0; p.grid = grid; }
+    if (grid == sms) break;
+  }
+  if (out) *out = p;
+  return best + 4.9 + 0.01 * G * p.nt;
+}
+
+int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
+  const int G = a.w_up ? 2 : 1, es = mx ? 1 : 2, box_el = LT_BOX / es;
+  lt_params p;
+  jk_linear_tc_plan(a, mx, ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS, &p);
   CUtensorMap mw, mu, mx_;
   auto map = [&](CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t stride, uint32_t box_rows) {
     const uint64_t dims[2] = {(uint64_t)a.n_in, rows}, str[1] = {stride * es};
@@ -507,7 +536,7 @@ int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   }
   const size_t smem = (size_t)p.stages * p.stage_bytes + sizeof(lt_tail) + 1024;
   JK_PROF(ctx, st, JK_ST_LINEAR);
-  jk_launch_pdl(kernel, dim3(grid), dim3(LT_THREADS), smem, st, mw, mu, mx_, p, a,
+  jk_launch_pdl(kernel, dim3(p.grid), dim3(LT_THREADS), smem, st, mw, mu, mx_, p, a,
                 (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
                 (int32_t*)(ctx->ws + ctx->lay.status));
   JK_LAUNCH_CHECK(ctx);
