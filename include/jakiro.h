@@ -589,7 +589,7 @@ int jk_quantize_rows(jk_ctx* ctx, void* stream, int64_t rows, int32_t n, const v
  *   out          T [rows, n] (opt): y; may be x or delta itself
  *   out_mx8, out_scale  (opt, together): y as mx8, rounded from the f32 value, not from out
  * At least one output.  The norm is that of the f32 sum, not of the rounded one.  n a multiple of 8
- * (of 32 with mx8) up to 32768.  Outputs must not overlap one another, nor an input in part.
+ * (of 32 with mx8) up to 32768, rows up to 2^24.  Outputs must not overlap one another, nor an input in part.
  */
 int jk_add_norm(jk_ctx* ctx, void* stream, int32_t rows, int32_t n, const void* x, const void* delta,
                 const void* weight, void* out_sum, void* out, void* out_mx8, uint8_t* out_scale);

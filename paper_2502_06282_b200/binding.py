@@ -76,6 +76,7 @@ class JkLinearOp(C.Structure):
 JK_ROWS_T, JK_ROWS_F32, JK_ROWS_MX8 = 0, 1, 2
 ACTS = {"none": 0, "silu": 1, "gelu": 2}
 
+_SECTIONS: Dict[tuple, C.Array] = {}      # the counts of jk_rope_qkv as the library takes them
 _lib = None
 
 
@@ -478,6 +479,8 @@ class Context:
             raise ValueError(f"{name}: expected a {dtype or self.tdtype} tensor {list(shape) if shape else '[rows, n]'}")
         if not t.is_cuda:
             raise ValueError(f"{name} is not on a CUDA device")
+        if t.is_contiguous():
+            return 0
         s = t.stride()
         if s[1] != 1 and t.shape[1] > 1:
             raise ValueError(f"{name}: expected contiguous rows")
@@ -486,23 +489,28 @@ class Context:
     def _dense(self, t, shape, name):
         if t is None:
             return None
-        if t.dtype is not self.tdtype or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous {self.tdtype} tensor {list(shape)}")
-        if not t.is_cuda:
-            raise ValueError(f"{name} is not on a CUDA device")
-        return t.data_ptr()
+        if t.dtype is self.tdtype and t.shape == shape and t.is_contiguous() and t.is_cuda:
+            return t.data_ptr()
+        raise ValueError(f"{name}: expected a contiguous {self.tdtype} tensor {list(shape)} on a CUDA device")
 
     def add_norm(self, x, weight=None, delta=None, out_sum=None, out=None, out_mx8: "Optional[Mx8]" = None):
         """jk_add_norm: x, delta, out_sum, out [rows, n] dense, weight [n], out_mx8 an Mx8 of [rows, n]."""
-        if x.dim() != 2:
-            raise ValueError("x: expected a tensor [rows, n]")
         shape = x.shape
-        if out_mx8 is not None and out_mx8.shape != shape:
+        if len(shape) != 2:
+            raise ValueError("x: expected a tensor [rows, n]")
+        if out_mx8 is None:
+            codes = scales = None
+        elif out_mx8.shape != shape:
             raise ValueError(f"out_mx8: expected an array of {list(shape)}")
-        ptrs = (self._dense(x, shape, "x"), self._dense(delta, shape, "delta"), self._dense(weight, shape[1:], "weight"),
-                self._dense(out_sum, shape, "out_sum"), self._dense(out, shape, "out"))
-        rc = lib().jk_add_norm(self._h, _stream(), shape[0], shape[1], *ptrs,
-                               *((None, None) if out_mx8 is None else out_mx8.ptrs))
+        else:
+            codes, scales = out_mx8.ptrs
+        dense = self._dense
+        px = dense(x, shape, "x")
+        rc = _lib.jk_add_norm(
+            self._h, _stream(), shape[0], shape[1], px, None if delta is None else dense(delta, shape, "delta"),
+            None if weight is None else dense(weight, shape[1:], "weight"),
+            None if out_sum is None else dense(out_sum, shape, "out_sum"),
+            None if out is None else dense(out, shape, "out"), codes, scales)
         if rc:
             self._check(rc, "jk_add_norm")
 
@@ -516,18 +524,17 @@ class Context:
     def linear(self, op: "Linear", x, out, residual=None):
         """jk_linear: x [rows, n_in] (T, rows may lie apart; or Mx8, as op's weights are), out [rows, n_out] (T, f32
         or Mx8), residual T [rows, n_out] or None; out may be the residual itself."""
-        if op.kind != self.tdtype:
+        if op.kind is not self.tdtype:
             raise ValueError("the projection was made for a context of another type")
+        shape = x.shape
+        if op.mx8 is not isinstance(x, Mx8) or len(shape) != 2 or shape[1] != op.n_in:
+            raise ValueError(f"x: expected {'an Mx8' if op.mx8 else f'a {self.tdtype} tensor'} [rows, {op.n_in}]")
+        rows, n_out = shape[0], op.n_out
         if op.mx8:
-            if not isinstance(x, Mx8) or x.shape[1] != op.n_in:
-                raise ValueError(f"x: expected an Mx8 [rows, {op.n_in}], as the weights are")
-            rows, xs = x.shape[0], 0
-            xp, xsp = x.ptrs
+            xs, (xp, xsp) = 0, x.ptrs
         else:
-            if isinstance(x, Mx8) or x.dim() != 2 or x.shape[1] != op.n_in:
-                raise ValueError(f"x: expected a {self.tdtype} tensor [rows, {op.n_in}]")
-            rows, xs, xp, xsp = x.shape[0], self._rows(x, "x"), x.data_ptr(), None
-        shape = (rows, op.n_out)
+            xs, xp, xsp = self._rows(x, "x"), x.data_ptr(), None
+        shape = (rows, n_out)
         rp, rs, os = None, 0, 0
         if residual is not None:
             rs, rp = self._rows(residual, "residual", shape=shape), residual.data_ptr()
@@ -538,7 +545,7 @@ class Context:
         else:
             kind = JK_ROWS_F32 if out.dtype is torch.float32 else JK_ROWS_T
             os, o, osp = self._rows(out, "out", out.dtype if kind == JK_ROWS_F32 else None, shape), out.data_ptr(), None
-        rc = lib().jk_linear(self._h, _stream(), op.ref, rows, xp, xsp, xs, rp, rs, o, kind, osp, os)
+        rc = _lib.jk_linear(self._h, _stream(), op.ref, rows, xp, xsp, xs, rp, rs, o, kind, osp, os)
         if rc:
             self._check(rc, "jk_linear")
 
@@ -556,6 +563,7 @@ class Context:
             stride = qkv.stride(-2) if n_tokens > 1 or qkv.dim() == 2 else qkv.stride(0)
             if qkv.dim() > 3 or (qkv.dim() == 3 and batch > 1 and n_tokens > 1 and qkv.stride(0) != n_tokens * stride):
                 raise ValueError("qkv: its rows do not lie evenly apart")
+        sections = tuple(sections)
         axes = len(sections)
         if pos.dim() == 3 and pos.shape[2] != axes:
             raise ValueError(f"pos: expected {axes} positions for each token")
@@ -564,9 +572,12 @@ class Context:
         if not (qkv.is_cuda and pos.is_cuda and q_out.is_cuda and k_out.is_cuda and v_out.is_cuda):
             raise ValueError("qkv, pos and the outputs must be on a CUDA device")
         s = self._tree_arrays(k_out, v_out, batch, n_tokens)
-        rc = lib().jk_rope_qkv(
+        host = _SECTIONS.get(sections)
+        if host is None:
+            host = _SECTIONS[sections] = (C.c_int32 * max(1, axes))(*sections)
+        rc = _lib.jk_rope_qkv(
             self._h, _stream(), batch, n_tokens, qkv.data_ptr(), stride, _array(pos, torch.int32, n * axes, "pos"), axes,
-            (C.c_int32 * axes)(*sections), rope_theta, q_out.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+            host, rope_theta, q_out.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
             s[0], s[1], k_out.shape[2], _array(first_row, torch.int32, batch, "first_row"))
         if rc:
             self._check(rc, "jk_rope_qkv")

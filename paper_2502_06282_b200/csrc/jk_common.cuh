@@ -94,6 +94,8 @@ struct jk_ctx {
   int attn_kernel;        // 0 = by size, 1 = CTA per (query block, key slice), 2 = persistent,
                           // 3 = cluster-merged
   char cuda_err[256];
+  float rope_theta;       // jk_rope_qkv: the base whose frequencies rope_freq holds (0: none yet)
+  double rope_freq[64];
   void* tc_state;         // tensor-core path bookkeeping (tensor maps), host memory
   void* attn_tc_state;    // tensor maps of the KV caches seen by the attention kernel
   void* attn_cl_state;    // cluster-merged attention kernel: occupancy answers per cluster size

@@ -29,94 +29,215 @@ __device__ __forceinline__ float4 lin_load4(const uint8_t* row, int k, const uin
 }
 
 // ------------------------------------------------------------------------------------------ CUDA cores
-// Block = 32 outputs x 32 rows, 8 warps: a lane owns an output, a warp four rows, so that a
-// warp holds the 32 outputs of a scale block.  k runs in steps of 32 through shared memory; a step's sum is
-// formed by itself and then added, which keeps long sums within a few units of f32.
-#define LS_B 32
+// A value's way out: row r, output n, from a group of lanes that hold a scale block of 32 outputs, `n_own` consecutive
+// ones each.  Every lane of the warp calls it.
+template <typename T, int OWN>
+__device__ __forceinline__ void lin_out(const lin_args& a, const float (&y)[OWN], int r, int n) {
+  constexpr int LANES = 32 / OWN;
+  const bool row_live = r < a.rows;
+  float v[OWN];
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) {
+    v[i] = y[i];
+    if (a.residual && row_live && n + i < a.n_out) v[i] += jk_to_float(((const T*)a.residual)[(size_t)r * a.r_stride + n + i]);
+  }
+  if (a.out_type == JK_ROWS_MX8) {                     // n_out is a multiple of 32: a block is live as a whole
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) m = fmaxf(m, paged_mag(v[i]));
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (!row_live || n >= a.n_out) return;
+    const int e = paged_scale_exp(m);
+    const float inv = paged_pow2(-e);
+#pragma unroll
+    for (int i = 0; i < OWN; ++i)
+      ((uint8_t*)a.out)[(size_t)r * a.n_out + n + i] = (uint8_t)__nv_cvt_float_to_fp8(v[i] * inv, __NV_SATFINITE, __NV_E4M3);
+    if ((n & 31) == 0) a.out_scale[mx_scale_at(r, n >> 5, a.k_tiles_out)] = (uint8_t)(e + 127);
+    return;
+  }
+  if (!row_live) return;
+#pragma unroll
+  for (int i = 0; i < OWN; ++i)
+    if (n + i < a.n_out) {
+      if (a.out_type == JK_ROWS_F32) ((float*)a.out)[(size_t)r * a.o_stride + n + i] = v[i];
+      else ((T*)a.out)[(size_t)r * a.o_stride + n + i] = jk_from_float<T>(v[i]);
+    }
+}
+template <typename T> __device__ __forceinline__ float lin_bias(const void* b, int n, int n_out) {
+  return b && n < n_out ? jk_to_float(((const T*)b)[n]) : 0.f;
+}
+
+// Few rows: a warp owns a weight row (gated: one of w and one of w_up) and up to 8 rows of x, its lanes go along k: every
+// weight is read once from memory, x comes from the caches.  Bound by latency at the sizes it is taken for.
+#define LR_ROWS 8
 template <typename TX, typename T, bool GATED>
-__global__ void __launch_bounds__(256) k_linear_cc(const lin_args a) {
-  __shared__ float s_w[1 + GATED][LS_B][LS_B + 1];
-  __shared__ __align__(16) float s_x[LS_B][LS_B];
+__global__ void __launch_bounds__(256) k_linear_rows(const lin_args a) {
   jk_pdl_wait();
   jk_pdl_trigger();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int n0 = blockIdx.x * LS_B, r0 = blockIdx.y * LS_B;
-  const int lr = threadIdx.x >> 3, lk = (threadIdx.x & 7) * 4;        // loading: a row, four elements
+  const int lane = threadIdx.x & 31, n = blockIdx.x * 8 + (threadIdx.x >> 5), r0 = blockIdx.y * LR_ROWS;
+  if (n >= a.n_out) return;
+  const TX* wr = (const TX*)a.w + (size_t)n * a.n_in;
+  const TX* ur = GATED ? (const TX*)a.w_up + (size_t)n * a.n_in : nullptr;
+  float acc[LR_ROWS], acc_up[LR_ROWS];
+#pragma unroll
+  for (int j = 0; j < LR_ROWS; ++j) acc[j] = acc_up[j] = 0.f;
+#pragma unroll 2
+  for (int k = lane * 4; k < a.n_in; k += 128) {
+    const float4 w = lin_load4(wr, k, a.w_scale, n, a.k_tiles_in);
+    float4 u = w;
+    if (GATED) u = lin_load4(ur, k, a.w_up_scale, n, a.k_tiles_in);
+#pragma unroll
+    for (int j = 0; j < LR_ROWS; ++j)
+      if (r0 + j < a.rows) {
+        const float4 x = lin_load4((const TX*)a.x + (size_t)(r0 + j) * a.x_stride, k, a.x_scale, r0 + j, a.k_tiles_in);
+        acc[j] += fmaf(x.x, w.x, fmaf(x.y, w.y, fmaf(x.z, w.z, x.w * w.w)));
+        if (GATED) acc_up[j] += fmaf(x.x, u.x, fmaf(x.y, u.y, fmaf(x.z, u.z, x.w * u.w)));
+      }
+  }
+  float z = 0.f, zu = 0.f;
+#pragma unroll
+  for (int j = 0; j < LR_ROWS; ++j) {
+    const float s = jk_warp_sum(acc[j]), t = GATED ? jk_warp_sum(acc_up[j]) : 0.f;
+    if (lane == j) { z = s; zu = t; }
+  }
+  const int r = r0 + lane;
+  if (lane >= LR_ROWS || r >= a.rows) return;
+  float y = lin_act(z + lin_bias<T>(a.bias, n, a.n_out), a.act);
+  if (GATED) y *= zu + lin_bias<T>(a.bias_up, n, a.n_out);
+  if (a.residual) y += jk_to_float(((const T*)a.residual)[(size_t)r * a.r_stride + n]);
+  if (a.out_type == JK_ROWS_F32) ((float*)a.out)[(size_t)r * a.o_stride + n] = y;
+  else ((T*)a.out)[(size_t)r * a.o_stride + n] = jk_from_float<T>(y);
+}
+
+// The rest: a block makes ROWS rows times 128 weight rows (gated: 64 of w and 64 of w_up, the two of an output in one
+// thread), 8 columns and ROWS / 16 rows a thread, k in steps of 16 through two buffers of shared memory, the next
+// step's loads on their way while one is multiplied.  The sum of 32 products is formed by itself and then added,
+// which keeps long sums within a few units of f32.
+#define LB_N 128
+#define LB_K 16
+template <typename TX, typename T, bool GATED, int ROWS>
+__global__ void __launch_bounds__(256) k_linear_block(const lin_args a) {
+  constexpr int RT = ROWS / 16, OUTS = GATED ? 64 : 128;
+  __shared__ __align__(16) float s_w[2][LB_K][LB_N + 4], s_x[2][LB_K][ROWS + 4];
+  jk_pdl_wait();
+  jk_pdl_trigger();
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int n0 = blockIdx.x * OUTS, r0 = blockIdx.y * ROWS;
+  const int lr = threadIdx.x >> 2, lk = (threadIdx.x & 3) * 4;         // loading: rows lr, lr + 64, four elements
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-  float acc[4] = {0.f, 0.f, 0.f, 0.f}, acc_up[4] = {0.f, 0.f, 0.f, 0.f};
-  const TX* xr = (const TX*)a.x + (size_t)(r0 + lr) * a.x_stride;
-  const TX* wr = (const TX*)a.w + (size_t)(n0 + lr) * a.n_in;
-  const TX* ur = GATED ? (const TX*)a.w_up + (size_t)(n0 + lr) * a.n_in : nullptr;
-  const bool x_live = r0 + lr < a.rows, w_live = n0 + lr < a.n_out;
-  for (int k0 = 0; k0 < a.n_in; k0 += LS_B) {
+  float4 pw[2], px[(ROWS + 63) / 64];
+  auto ask = [&](int k0) {
     const bool in = k0 + lk < a.n_in;
-    const float4 xv = x_live && in ? lin_load4(xr, k0 + lk, a.x_scale, r0 + lr, a.k_tiles_in) : zero;
-    const float4 wv = w_live && in ? lin_load4(wr, k0 + lk, a.w_scale, n0 + lr, a.k_tiles_in) : zero;
-    float4 uv = zero;
-    if (GATED && w_live && in) uv = lin_load4(ur, k0 + lk, a.w_up_scale, n0 + lr, a.k_tiles_in);
-    __syncthreads();
-    *reinterpret_cast<float4*>(&s_x[lr][lk]) = xv;
-    s_w[0][lk][lr] = wv.x; s_w[0][lk + 1][lr] = wv.y; s_w[0][lk + 2][lr] = wv.z; s_w[0][lk + 3][lr] = wv.w;
-    if (GATED) {
-      s_w[GATED][lk][lr] = uv.x; s_w[GATED][lk + 1][lr] = uv.y;
-      s_w[GATED][lk + 2][lr] = uv.z; s_w[GATED][lk + 3][lr] = uv.w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int n = n0 + lr + (GATED ? 0 : 64 * h);
+      const bool up = GATED && h;
+      pw[h] = in && n < a.n_out ? lin_load4((const TX*)(up ? a.w_up : a.w) + (size_t)n * a.n_in, k0 + lk,
+                                            up ? a.w_up_scale : a.w_scale, n, a.k_tiles_in) : zero;
     }
-    __syncthreads();
-    float part[4] = {0.f, 0.f, 0.f, 0.f}, part_up[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < LS_B; k += 4) {
-      float w[4], u[4];
+    for (int h = 0; h < (ROWS + 63) / 64; ++h) {
+      const int r = lr + 64 * h;
+      px[h] = in && r < ROWS && r0 + r < a.rows
+                  ? lin_load4((const TX*)a.x + (size_t)(r0 + r) * a.x_stride, k0 + lk, a.x_scale, r0 + r, a.k_tiles_in) : zero;
+    }
+  };
+  auto put = [&](int b) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] = s_w[0][k + i][lane];
-        if (GATED) u[i] = s_w[GATED][k + i][lane];
+    for (int h = 0; h < 2; ++h) {
+      const float v[4] = {pw[h].x, pw[h].y, pw[h].z, pw[h].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_w[b][lk + i][lr + 64 * h] = v[i];
+    }
+#pragma unroll
+    for (int h = 0; h < (ROWS + 63) / 64; ++h)
+      if (lr + 64 * h < ROWS) {
+        const float v[4] = {px[h].x, px[h].y, px[h].z, px[h].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_x[b][lk + i][lr + 64 * h] = v[i];
+      }
+  };
+  float acc[RT][8], part[RT][8];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j] = part[i][j] = 0.f;
+  ask(0);
+  put(0);
+  __syncthreads();
+  const int steps = (a.n_in + LB_K - 1) / LB_K;
+  for (int s = 0; s < steps; ++s) {
+    const int b = s & 1;
+    if (s + 1 < steps) ask((s + 1) * LB_K);
+#pragma unroll
+    for (int k = 0; k < LB_K; ++k) {
+      float w[8], x[RT];
+      *reinterpret_cast<float4*>(&w[0]) = *reinterpret_cast<const float4*>(&s_w[b][k][tx * 4]);
+      *reinterpret_cast<float4*>(&w[4]) = *reinterpret_cast<const float4*>(&s_w[b][k][64 + tx * 4]);
+      if constexpr (RT >= 4) {
+#pragma unroll
+        for (int i = 0; i < RT; i += 4)
+          *reinterpret_cast<float4*>(&x[i]) = *reinterpret_cast<const float4*>(&s_x[b][k][ty * RT + i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) x[i] = s_x[b][k][ty * RT + i];
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float4 x4 = *reinterpret_cast<const float4*>(&s_x[warp * 4 + j][k]);
-        const float xs[4] = {x4.x, x4.y, x4.z, x4.w};
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          part[j] = fmaf(xs[i], w[i], part[j]);
-          if (GATED) part_up[j] = fmaf(xs[i], u[i], part_up[j]);
-        }
-      }
+        for (int j = 0; j < 8; ++j) part[i][j] = fmaf(x[i], w[j], part[i][j]);
     }
+    if ((s & 1) || s + 1 == steps) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { acc[i][j] += part[i][j]; part[i][j] = 0.f; }
+    }
+    if (s + 1 < steps) put(b ^ 1);
+    __syncthreads();
+  }
+  // a thread has outputs tx * 4 .. + 3 (and 64 on, or their gate's partners): eight neighbouring lanes a scale block
+#pragma unroll
+  for (int h = 0; h < (GATED ? 1 : 2); ++h) {
+    const int n = n0 + 64 * h + tx * 4;
+    float bias[4], bias_up[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      acc[j] += part[j];
-      if (GATED) acc_up[j] += part_up[j];
+      bias[j] = lin_bias<T>(a.bias, n + j, a.n_out);
+      bias_up[j] = GATED ? lin_bias<T>(a.bias_up, n + j, a.n_out) : 0.f;
     }
-  }
-  const int n = n0 + lane;
-  const bool live = n < a.n_out;
-  const float b = live && a.bias ? jk_to_float(((const T*)a.bias)[n]) : 0.f;
-  const float bu = GATED && live && a.bias_up ? jk_to_float(((const T*)a.bias_up)[n]) : 0.f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int r = r0 + warp * 4 + j;
-    if (r >= a.rows) break;
-    float y = lin_act(acc[j] + b, a.act);
-    if (GATED) y *= acc_up[j] + bu;
-    if (live && a.residual) y += jk_to_float(((const T*)a.residual)[(size_t)r * a.r_stride + n]);
-    if (a.out_type == JK_ROWS_MX8) {                   // n_out is a multiple of 32: the warp is all live
-      const int e = paged_scale_exp(jk_warp_max(paged_mag(y)));
-      const float v = y * paged_pow2(-e);
-      ((uint8_t*)a.out)[(size_t)r * a.n_out + n] = (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3);
-      if (lane == 0) a.out_scale[mx_scale_at(r, n0 >> 5, a.k_tiles_out)] = (uint8_t)(e + 127);
-    } else if (live && a.out_type == JK_ROWS_F32) {
-      ((float*)a.out)[(size_t)r * a.o_stride + n] = y;
-    } else if (live) {
-      ((T*)a.out)[(size_t)r * a.o_stride + n] = jk_from_float<T>(y);
+    for (int i = 0; i < RT; ++i) {
+      float y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        y[j] = lin_act(acc[i][4 * h + j] + bias[j], a.act);
+        if (GATED) y[j] *= acc[i][4 + j] + bias_up[j];
+      }
+      lin_out<T, 4>(a, y, r0 + ty * RT + i, n);
     }
   }
 }
 
+// Few rows while a scale block's outputs need not meet (T and f32 out) and they are read by at most two passes; else
+// blocks of 32 or 128 rows: 32 while blocks of 128 would leave SMs idle.  f32, us: 16 x 1376 x 512 gated LR_US,
+// by blocks of 32 rows LB_US.
 template <typename TX, typename T>
-static void launch_cc(cudaStream_t st, const lin_args& a) {
-  const dim3 grid((unsigned)((a.n_out + LS_B - 1) / LS_B), (unsigned)((a.rows + LS_B - 1) / LS_B));
-  if (a.w_up) jk_launch_pdl(k_linear_cc<TX, T, true>, grid, dim3(256), 0, st, a);
-  else jk_launch_pdl(k_linear_cc<TX, T, false>, grid, dim3(256), 0, st, a);
+static void launch_cc(cudaStream_t st, const lin_args& a, int sms) {
+  const bool gated = a.w_up != nullptr;
+  if (a.rows <= 2 * LR_ROWS && a.out_type != JK_ROWS_MX8) {
+    const dim3 grid((unsigned)((a.n_out + 7) / 8), (unsigned)((a.rows + LR_ROWS - 1) / LR_ROWS));
+    jk_launch_pdl(gated ? k_linear_rows<TX, T, true> : k_linear_rows<TX, T, false>, grid, dim3(256), 0, st, a);
+    return;
+  }
+  const int outs = gated ? LB_N / 2 : LB_N, n_tiles = (a.n_out + outs - 1) / outs;
+  const bool large = a.rows > 32 && (long long)n_tiles * ((a.rows + 127) / 128) >= sms;
+  const int R = large ? 128 : 32;
+  const dim3 grid((unsigned)n_tiles, (unsigned)((a.rows + R - 1) / R));
+  auto k = large ? (gated ? k_linear_block<TX, T, true, 128> : k_linear_block<TX, T, false, 128>)
+                 : (gated ? k_linear_block<TX, T, true, 32> : k_linear_block<TX, T, false, 32>);
+  jk_launch_pdl(k, grid, dim3(256), 0, st, a);
 }
 
 // ------------------------------------------------------------------------------------------ host side
@@ -184,11 +305,11 @@ extern "C" int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* op, int3
   }
   JK_PROF(ctx, st, JK_ST_LINEAR);
   if (ctx->cfg.dtype == JK_F32) {
-    if (mx) launch_cc<uint8_t, float>(st, a);
-    else launch_cc<float, float>(st, a);
+    if (mx) launch_cc<uint8_t, float>(st, a, ctx->sm_count);
+    else launch_cc<float, float>(st, a, ctx->sm_count);
   } else {
-    if (mx) launch_cc<uint8_t, __nv_bfloat16>(st, a);
-    else launch_cc<__nv_bfloat16, __nv_bfloat16>(st, a);
+    if (mx) launch_cc<uint8_t, __nv_bfloat16>(st, a, ctx->sm_count);
+    else launch_cc<__nv_bfloat16, __nv_bfloat16>(st, a, ctx->sm_count);
   }
   JK_LAUNCH_CHECK(ctx);
   return JK_OK;

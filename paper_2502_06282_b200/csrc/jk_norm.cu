@@ -2,8 +2,8 @@
 //
 //   s = x + delta, y = s / sqrt(mean(s^2) + eps) * weight
 //
-// One pass: a block owns a row and keeps its f32 sums s in registers between the reduction of
-// s^2 and the output, so x and delta are read once and every output is written once.  A thread
+// One pass: a block keeps a row's f32 sums s in registers between the reduction of s^2 and the output,
+// so x and delta are read once and every output is written once.  A thread
 // holds pieces of 8 consecutive elements; four neighbouring lanes make a scale block of 32, whose
 // largest element takes two shuffles.
 #include "jk_mx8.cuh"
@@ -63,66 +63,86 @@ __device__ __forceinline__ void mx_store_piece(const float (&v)[8], bool live, u
 }
 
 // ------------------------------------------------------------------------------------------ the norm
-// Block = one row; a thread holds P pieces, blockDim.x * 8 elements apart.
-template <typename T, int P>
-__global__ void __launch_bounds__(1024) k_add_norm(
-    const T* x, const T* delta, const T* __restrict__ weight, int n, float eps,
-    T* out_sum, T* out, uint8_t* codes, uint8_t* scales, int k_tiles) {
-  __shared__ float red[33];
-  jk_pdl_wait();
-  jk_pdl_trigger();
-  const size_t row = blockIdx.x, at = row * n;
-  const int step = blockDim.x * 8;
-  float s[P][8];
-  {
-    piece<T> a[P], b[P];
+// A block takes rows blockIdx.x, + gridDim.x, ...; a thread holds P pieces of a row, blockDim.x * 8 elements apart.
+// With AHEAD the next row is asked for before the block meets over the present one, so that loads are always
+// on their way, and the weights stay in registers.
+template <typename T, int P> struct norm_row {
+  piece<T> a[P], b[P];
+  __device__ __forceinline__ void ask(const T* x, const T* delta, size_t at, int n, int step) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = threadIdx.x * 8 + p * step;
-      if (c < n) a[p].load(x + at + c);
-      if (c < n && delta) b[p].load(delta + at + c);
+      if (c < n) {
+        a[p].load(x + at + c);
+        if (delta) b[p].load(delta + at + c);
+      }
     }
+  }
+};
+template <typename T, int P, bool AHEAD>
+__global__ void __launch_bounds__(AHEAD ? 512 : 1024, AHEAD && P < 4 ? 2 : 1) k_add_norm(
+    const T* x, const T* delta, const T* __restrict__ weight, int rows, int n, float eps, T* out_sum, T* out,
+    uint8_t* codes, uint8_t* scales, int k_tiles) {
+  __shared__ float red[2][32];
+  jk_pdl_wait();
+  jk_pdl_trigger();
+  const int step = blockDim.x * 8, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  norm_row<T, P> next;
+  piece<T> w[P];
+  if (AHEAD) {
+    next.ask(x, delta, (size_t)blockIdx.x * n, n, step);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = threadIdx.x * 8 + p * step;
+      if (weight && c < n) w[p].load(weight + c);
+    }
+  }
+  int turn = 0;
+  for (int row = blockIdx.x; row < rows; row += (int)gridDim.x, turn ^= 1) {
+    const size_t at = (size_t)row * n;
+    if (!AHEAD) next.ask(x, delta, at, n, step);
+    float s[P][8];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const bool live = (int)threadIdx.x * 8 + p * step < n;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[p][i] = live ? (delta ? a[p].at(i) + b[p].at(i) : a[p].at(i)) : 0.f;
+      for (int i = 0; i < 8; ++i)
+        s[p][i] = live ? (delta ? next.a[p].at(i) + next.b[p].at(i) : next.a[p].at(i)) : 0.f;
     }
-  }
-  float sq = 0.f;
+    if (AHEAD && row + (int)gridDim.x < rows) next.ask(x, delta, at + (size_t)gridDim.x * n, n, step);
+    float sq = 0.f;
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    float part = 0.f;                      // (short sums first: the row's sum keeps its last bits)
+    for (int p = 0; p < P; ++p) {
+      float part = 0.f;                    // (short sums first: the row's sum keeps its last bits)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) part = fmaf(s[p][i], s[p][i], part);
-    sq += part;
-  }
-  // the weights are asked for before the block meets
-  piece<T> w[P];
+      for (int i = 0; i < 8; ++i) part = fmaf(s[p][i], s[p][i], part);
+      sq += part;
+    }
+    sq = jk_warp_sum(sq);
+    if (lane == 0) red[turn][warp] = sq;   // (the turns' arrays alternate: one barrier a row)
+    if (out_sum) {
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int c = threadIdx.x * 8 + p * step;
-    if (weight && c < n) w[p].load(weight + c);
-  }
-  if (out_sum) {
+      for (int p = 0; p < P; ++p) {
+        const int c = threadIdx.x * 8 + p * step;
+        if (c < n) piece<T>::store(out_sum + at + c, s[p]);
+      }
+    }
+    __syncthreads();
+    const float total = jk_warp_sum(lane < warps ? red[turn][lane] : 0.f);
+    const float r = 1.f / sqrtf(total / (float)n + eps);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = threadIdx.x * 8 + p * step;
-      if (c < n) piece<T>::store(out_sum + at + c, s[p]);
-    }
-  }
-  const float r = 1.f / sqrtf(jk_block_sum(sq, red) / (float)n + eps);
+      const bool live = c < n;
+      if (!AHEAD && weight && live) w[p].load(weight + c);
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int c = threadIdx.x * 8 + p * step;
-    const bool live = c < n;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      s[p][i] *= r;
-      if (weight && live) s[p][i] *= w[p].at(i);
+      for (int i = 0; i < 8; ++i) {
+        s[p][i] *= r;
+        if (weight && live) s[p][i] *= w[p].at(i);
+      }
+      if (out && live) piece<T>::store(out + at + c, s[p]);
+      if (codes) mx_store_piece(s[p], live, codes + at + c, scales + mx_scale_at(row, c >> 5, k_tiles));
     }
-    if (out && live) piece<T>::store(out + at + c, s[p]);
-    if (codes) mx_store_piece(s[p], live, codes + at + c, scales + mx_scale_at(row, c >> 5, k_tiles));
   }
 }
 
@@ -155,22 +175,25 @@ extern "C" int64_t jk_row_scale_bytes(int64_t rows, int64_t n) {
   return (rows + 127) / 128 * mx_k_tiles(n) * MX_TILE_BYTES;
 }
 
+// Pieces a thread holds: 1 up to n = 2048, 2 up to 8192, 4 beyond; past 16384, where a block has 1024 threads, one
+// row at a time (two do not fit the registers).  As many blocks as are resident: the rows are walked.
 template <typename T>
-static void launch_norm(cudaStream_t st, int rows, int n, const void* x, const void* delta, const void* weight,
+static void launch_norm(cudaStream_t st, int sms, int rows, int n, const void* x, const void* delta, const void* weight,
                         float eps, void* out_sum, void* out, void* codes, uint8_t* scales) {
-  const int pieces = (n + 7) / 8, k_tiles = mx_k_tiles(n);
-  // pieces a thread holds: 1, 2 or 4, the fewest that keep the block within 512 threads
-  const int P = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : 4;
+  const int pieces = n / 8, k_tiles = mx_k_tiles(n);
+  const int P = pieces <= 256 ? 1 : pieces <= 1024 ? 2 : 4;
   const int threads = (int)jk_align_up((pieces + P - 1) / P, 32);
-  auto k = P == 1 ? k_add_norm<T, 1> : P == 2 ? k_add_norm<T, 2> : k_add_norm<T, 4>;
-  jk_launch_pdl(k, dim3(rows), dim3(threads), 0, st, (const T*)x, (const T*)delta, (const T*)weight, n, eps,
-                (T*)out_sum, (T*)out, (uint8_t*)codes, scales, k_tiles);
+  const long long most = (long long)sms * (threads > 512 ? 1 : (P == 4 ? 512 : 1024) / threads);
+  auto k = P == 1 ? k_add_norm<T, 1, true> : P == 2 ? k_add_norm<T, 2, true>
+           : threads <= 512 ? k_add_norm<T, 4, true> : k_add_norm<T, 4, false>;
+  jk_launch_pdl(k, dim3((unsigned)(rows < most ? rows : most)), dim3(threads), 0, st, (const T*)x, (const T*)delta,
+                (const T*)weight, rows, n, eps, (T*)out_sum, (T*)out, (uint8_t*)codes, scales, k_tiles);
 }
 
 extern "C" int jk_add_norm(jk_ctx* ctx, void* stream, int32_t rows, int32_t n, const void* x, const void* delta,
                            const void* weight, void* out_sum, void* out, void* out_mx8, uint8_t* out_scale) {
   if (!ctx || !x || (!out_sum && !out && !out_mx8) || !out_mx8 != !out_scale) return JK_ERR_NULL;
-  if (rows < 1 || n < 8 || n > 32768 || n % 8 || (out_mx8 && n % MX_BLOCK)) return JK_ERR_SHAPE;
+  if (rows < 1 || rows > (1 << 24) || n < 8 || n > 32768 || n % 8 || (out_mx8 && n % MX_BLOCK)) return JK_ERR_SHAPE;
   const size_t es = jk_elem_size(ctx->cfg.dtype), bytes = (size_t)rows * n * es;
   const void* in[] = {x, delta, weight};
   const size_t in_b[] = {bytes, bytes, (size_t)n * es};
@@ -187,12 +210,14 @@ extern "C" int jk_add_norm(jk_ctx* ctx, void* stream, int32_t rows, int32_t n, c
     for (int j = 0; j < i; ++j)
       if (jk_overlap(o[i], o_b[i], o[j], o_b[j])) return JK_ERR_SHAPE;
   }
+  int rc = jk_ensure_device_info(ctx);
+  if (rc != JK_OK) return rc;
   cudaStream_t st = (cudaStream_t)stream;
   JK_PROF(ctx, st, JK_ST_NORM);
   if (ctx->cfg.dtype == JK_BF16)
-    launch_norm<__nv_bfloat16>(st, rows, n, x, delta, weight, ctx->cfg.rms_eps, out_sum, out, out_mx8, out_scale);
+    launch_norm<__nv_bfloat16>(st, ctx->sm_count, rows, n, x, delta, weight, ctx->cfg.rms_eps, out_sum, out, out_mx8, out_scale);
   else
-    launch_norm<float>(st, rows, n, x, delta, weight, ctx->cfg.rms_eps, out_sum, out, out_mx8, out_scale);
+    launch_norm<float>(st, ctx->sm_count, rows, n, x, delta, weight, ctx->cfg.rms_eps, out_sum, out, out_mx8, out_scale);
   JK_LAUNCH_CHECK(ctx);
   return JK_OK;
 }

@@ -10,7 +10,7 @@
 #include "jk_mx8.cuh"
 
 #define ROPE_THREADS 256
-#define ROPE_TOKENS 4                      // tokens of a block
+#define ROPE_TOKENS 4                      // tokens of a block, at most
 
 struct rope_axes {
   int axis_end[4];                         // frequencies below axis_end[a] (and not below axis_end[a - 1]) turn with axis a
@@ -20,6 +20,14 @@ struct rope_axes {
 template <typename T> struct rope_vec;     // 16 bytes of T
 template <> struct rope_vec<__nv_bfloat16> {
   static constexpr int N = 8;
+  static __device__ __forceinline__ void open(const uint4& r, float (&o)[8]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[2 * i] = __uint_as_float(w[i] << 16);
+      o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
   static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[8]) {
     uint4 o;
     uint32_t* w = reinterpret_cast<uint32_t*>(&o);
@@ -33,27 +41,33 @@ template <> struct rope_vec<__nv_bfloat16> {
 };
 template <> struct rope_vec<float> {
   static constexpr int N = 4;
+  static __device__ __forceinline__ void open(const uint4& r, float (&o)[4]) {
+    o[0] = __uint_as_float(r.x); o[1] = __uint_as_float(r.y); o[2] = __uint_as_float(r.z); o[3] = __uint_as_float(r.w);
+  }
   static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   }
 };
 
+// theta^(-2i/d), formed on the host once for each theta
+struct rope_freq { double f[64]; };
+
+// The heads that stand side by side in a row: LH lanes turn a head (VN pairs each), a block 256 / LH heads at a time.
 template <typename T, int D>
-__global__ void __launch_bounds__(ROPE_THREADS) k_rope_qkv(
-    const T* __restrict__ qkv, long long row_stride, const int32_t* __restrict__ pos, const rope_axes ax, float theta,
-    int n_tokens, int Hq, int Hkv, T* __restrict__ q_out, T* __restrict__ k_out, T* __restrict__ v_out, long long sb,
-    long long sh, int rows, const int32_t* __restrict__ first_row, int32_t* status) {
-  constexpr int VN = rope_vec<T>::N, HALF = D / 2, HV = HALF / VN;     // HV: pieces of half a head
-  __shared__ double s_inv[HALF];
+__global__ void __launch_bounds__(ROPE_THREADS, 4) k_rope_qkv(
+    const T* __restrict__ qkv, long long row_stride, const int32_t* __restrict__ pos, const rope_axes ax,
+    const __grid_constant__ rope_freq freq, int n_tokens, int per_block, int Hq, int Hkv, T* __restrict__ q_out,
+    T* __restrict__ k_out, T* __restrict__ v_out, long long sb, long long sh, int rows,
+    const int32_t* __restrict__ first_row, int32_t* status) {
+  constexpr int VN = rope_vec<T>::N, HALF = D / 2, LH = HALF / VN, HEADS = ROPE_THREADS / LH, UNROLL = 2;
   __shared__ __align__(16) float s_cos[ROPE_TOKENS][HALF], s_sin[ROPE_TOKENS][HALF];
   __shared__ int s_bad[ROPE_TOKENS];
-  for (int j = threadIdx.x; j < HALF; j += ROPE_THREADS) s_inv[j] = pow((double)theta, -2.0 * (double)j / (double)D);
   if (threadIdx.x < ROPE_TOKENS) s_bad[threadIdx.x] = 0;
   __syncthreads();
   // The successor is released when this kernel ends: the tree attention reads committed rows of a cache
   // ahead of its own wait, and a prompt's rows may be committed by what this call writes.
   jk_pdl_wait();
-  const int b = blockIdx.y, t0 = blockIdx.x * ROPE_TOKENS, nt = min(ROPE_TOKENS, n_tokens - t0);
+  const int b = blockIdx.y, t0 = blockIdx.x * per_block, nt = min(per_block, n_tokens - t0);
   const size_t tok0 = (size_t)b * n_tokens + t0;
   for (int i = threadIdx.x; i < nt * HALF; i += ROPE_THREADS) {
     const int t = i / HALF, j = i % HALF;
@@ -61,7 +75,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_rope_qkv(
     while (a + 1 < ax.n_axes && j >= ax.axis_end[a]) ++a;
     const int p = pos[(tok0 + t) * ax.n_axes + a];
     if (p < 0) s_bad[t] = 1;
-    const double ang = (double)p * s_inv[j];
+    const double ang = (double)p * freq.f[j];
     const double turns = rint(ang * 0.15915494309189535);            // 1 / (2 pi)
     double red = fma(-turns, 6.283185307179586, ang);                // 2 pi, leading part
     red = fma(-turns, 2.4492935982947064e-16, red);                  // 2 pi, the rest
@@ -71,35 +85,66 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_rope_qkv(
   const bool fits = r0 >= 0 && r0 <= rows - n_tokens;
   __syncthreads();
   if (threadIdx.x < nt && (s_bad[threadIdx.x] || !fits)) jk_set_status(status, JK_ERR_BOUNDS);
-  // the rotated heads: a thread turns VN pairs
-  const int rot = (Hq + Hkv) * HV;
-  for (int i = threadIdx.x; i < nt * rot; i += ROPE_THREADS) {
-    const int t = i / rot, h = (i - t * rot) / HV, j = (i - t * rot) % HV * VN;
-    if (s_bad[t]) continue;
-    const T* src = qkv + (tok0 + t) * row_stride + (size_t)h * D + j;
-    float x1[VN], x2[VN], o1[VN], o2[VN];
-    jk_vec<T>::load(src, x1);
-    jk_vec<T>::load(src + HALF, x2);
+  // (token, head) pairs in one line, 256 / LH at a time
+  const int j = threadIdx.x % LH * VN, heads = fits ? Hq + Hkv : Hq;
+  int t = 0, h = threadIdx.x / LH;
+  while (h >= heads && t < nt) { h -= heads; ++t; }
+  while (t < nt) {
+    uint4 lo[UNROLL], hi[UNROLL];
+    int ts[UNROLL], hs[UNROLL];
 #pragma unroll
-    for (int e = 0; e < VN; ++e) {
-      const float c = s_cos[t][j + e], s = s_sin[t][j + e];
-      o1[e] = x1[e] * c - x2[e] * s;
-      o2[e] = x2[e] * c + x1[e] * s;
+    for (int i = 0; i < UNROLL; ++i) {
+      ts[i] = t;
+      hs[i] = h;
+      if (t < nt) {
+        const T* src = qkv + (tok0 + t) * row_stride + (size_t)h * D + j;
+        lo[i] = *reinterpret_cast<const uint4*>(src);
+        hi[i] = *reinterpret_cast<const uint4*>(src + HALF);
+        h += HEADS;
+        while (h >= heads && t < nt) { h -= heads; ++t; }
+      }
     }
-    T* dst;
-    if (h < Hq) dst = q_out + ((tok0 + t) * Hq + h) * D + j;
-    else if (!fits) continue;
-    else dst = k_out + (size_t)b * sb + (size_t)(h - Hq) * sh + (size_t)(r0 + t0 + t) * D + j;
-    rope_vec<T>::store(dst, o1);
-    rope_vec<T>::store(dst + HALF, o2);
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) {
+      if (ts[i] >= nt || s_bad[ts[i]]) continue;
+      float x1[VN], x2[VN], cs[VN], sn[VN], o1[VN], o2[VN];
+#pragma unroll
+      for (int e = 0; e < VN; e += 4) {
+        *reinterpret_cast<float4*>(&cs[e]) = *reinterpret_cast<const float4*>(&s_cos[ts[i]][j + e]);
+        *reinterpret_cast<float4*>(&sn[e]) = *reinterpret_cast<const float4*>(&s_sin[ts[i]][j + e]);
+      }
+      rope_vec<T>::open(lo[i], x1);
+      rope_vec<T>::open(hi[i], x2);
+#pragma unroll
+      for (int e = 0; e < VN; ++e) {
+        o1[e] = x1[e] * cs[e] - x2[e] * sn[e];
+        o2[e] = x2[e] * cs[e] + x1[e] * sn[e];
+      }
+      T* dst = hs[i] < Hq ? q_out + ((tok0 + ts[i]) * Hq + hs[i]) * D + j
+                          : k_out + (size_t)b * sb + (size_t)(hs[i] - Hq) * sh + (size_t)(r0 + t0 + ts[i]) * D + j;
+      rope_vec<T>::store(dst, o1);
+      rope_vec<T>::store(dst + HALF, o2);
+    }
   }
   if (!fits) return;
+  // V moves as it is
   constexpr int DV = D / VN;
-  for (int i = threadIdx.x; i < nt * Hkv * DV; i += ROPE_THREADS) {
-    const int t = i / (Hkv * DV), h = (i - t * Hkv * DV) / DV, j = i % DV * VN;
+  const int per_tok = Hkv * DV;
+  for (t = 0; t < nt; ++t) {
     if (s_bad[t]) continue;
-    const uint4 v = *reinterpret_cast<const uint4*>(qkv + (tok0 + t) * row_stride + (size_t)(Hq + Hkv + h) * D + j);
-    *reinterpret_cast<uint4*>(v_out + (size_t)b * sb + (size_t)h * sh + (size_t)(r0 + t0 + t) * D + j) = v;
+    const T* row = qkv + (tok0 + t) * row_stride + (size_t)(Hq + Hkv) * D;
+    T* v = v_out + (size_t)b * sb + (size_t)(r0 + t0 + t) * D;
+    for (int i0 = threadIdx.x; i0 < per_tok; i0 += ROPE_THREADS * UNROLL) {
+      uint4 x[UNROLL];
+#pragma unroll
+      for (int i = 0; i < UNROLL; ++i)
+        if (i0 + i * ROPE_THREADS < per_tok) x[i] = *reinterpret_cast<const uint4*>(row + (size_t)(i0 + i * ROPE_THREADS) * VN);
+#pragma unroll
+      for (int i = 0; i < UNROLL; ++i) {
+        const int at = i0 + i * ROPE_THREADS;
+        if (at < per_tok) *reinterpret_cast<uint4*>(v + (size_t)(at / DV) * sh + at % DV * VN) = x[i];
+      }
+    }
   }
 }
 
@@ -143,12 +188,24 @@ extern "C" int jk_rope_qkv(jk_ctx* ctx, void* stream, int32_t batch, int32_t n_t
   if (!ctx->ws) return JK_ERR_WORKSPACE;
   int32_t* status = (int32_t*)(ctx->ws + ctx->lay.status);
   cudaStream_t st = (cudaStream_t)stream;
-  const dim3 grid((unsigned)((n_tokens + ROPE_TOKENS - 1) / ROPE_TOKENS), (unsigned)batch);
+  int rc = jk_ensure_device_info(ctx);
+  if (rc != JK_OK) return rc;
+  if (ctx->rope_theta != theta) {            // (64 powers take longer than a small call)
+    for (int j = 0; j < D / 2; ++j) ctx->rope_freq[j] = pow((double)theta, -2.0 * j / D);
+    ctx->rope_theta = theta;
+  }
+  rope_freq freq;
+  memset(&freq, 0, sizeof(freq));
+  memcpy(freq.f, ctx->rope_freq, sizeof(double) * (D / 2));
+  // tokens of a block: as many as leave four blocks to an SM
+  long long per = (long long)tokens / (4ll * ctx->sm_count);
+  const int per_block = per < 1 ? 1 : per > ROPE_TOKENS ? ROPE_TOKENS : (int)per;
+  const dim3 grid((unsigned)((n_tokens + per_block - 1) / per_block), (unsigned)batch);
   JK_PROF(ctx, st, JK_ST_PRE_ROPE);
   auto go = [&](auto kernel, auto tag) {
     typedef decltype(tag) T;
-    jk_launch_pdl(kernel, grid, dim3(ROPE_THREADS), 0, st, (const T*)qkv, (long long)row_stride, pos, ax, theta,
-                  n_tokens, Hq, Hkv, (T*)q_out, (T*)k_out, (T*)v_out, (long long)sb, (long long)sh, rows, first_row,
+    jk_launch_pdl(kernel, grid, dim3(ROPE_THREADS), 0, st, (const T*)qkv, (long long)row_stride, pos, ax, freq,
+                  n_tokens, per_block, Hq, Hkv, (T*)q_out, (T*)k_out, (T*)v_out, (long long)sb, (long long)sh, rows, first_row,
                   status);
   };
   if (c.dtype == JK_BF16) {
