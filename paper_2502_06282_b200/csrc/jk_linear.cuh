@@ -23,11 +23,12 @@ __device__ __forceinline__ float lin_act(float z, int act) {
   return z;
 }
 
-// The tensor-core kernels' form for many values (their epilogue is bound by its instructions): SiLU by the
-// approximate exponential and reciprocal, within 2^-18; GELU for outputs of 16 and 8 bits by
-// erfc(x) = t exp(-x^2 + P(t)), t = 1 / (1 + x / 2), x >= 0, with the P of degree 5 that makes the largest relative
-// error over 0 .. 10 smallest (7.6e-6, found by reweighted least squares on log erfc): 2^-16 with the roundings
-// of the exponent, a 2^-7th of what bf16 rounds.  f32 outputs take the library's erfc.
+// The tensor-core kernels' form (their epilogue is bound by fetching its instructions: everything short, in loops of
+// 8 values): SiLU by the approximate exponential and reciprocal, within 2^-18; GELU by
+// erfc(x) = t exp(-x^2 + P(t)), t = 1 / (1 + x / 2), x >= 0.  P for outputs of 16 and 8 bits: the polynomial of degree 5
+// that makes the largest relative error over 0 .. 10 smallest (7.6e-6, found by reweighted least squares on log erfc;
+// 2^-16 with the roundings of the exponent, a 2^-7th of what bf16 rounds).  P for f32 outputs: that of degree 9 of Press et
+// al., Numerical Recipes, 2nd ed., 6.2 (1.2e-7; 2^-18 with the exponent's roundings).
 __device__ __forceinline__ float lin_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -39,17 +40,31 @@ __device__ __forceinline__ float lin_rcp(float x) {
   return y;
 }
 #define LIN_LOG2E 1.4426950408889634f
-__device__ __forceinline__ float lin_gelu(float v) {
+template <bool F32> __device__ __forceinline__ float lin_gelu(float v) {
   const float a = fabsf(v), t = lin_rcp(fmaf(0.35355339059327376f, a, 1.f));     // x = |v| / sqrt 2
-  float q = LIN_LOG2E * 0.22879023753f;                                          // (exponents of 2)
-  q = fmaf(q, t, LIN_LOG2E * -0.70919065294f);
-  q = fmaf(q, t, LIN_LOG2E * 0.47449294008f);
-  q = fmaf(q, t, LIN_LOG2E * 0.25444333415f);
-  q = fmaf(q, t, LIN_LOG2E * 1.01801351084f);
-  q = fmaf(q, t, LIN_LOG2E * -1.26654175576f);
+  float q;                                                                       // (exponents of 2)
+  if (F32) {
+    q = LIN_LOG2E * 0.17087277f;
+    q = fmaf(q, t, LIN_LOG2E * -0.82215223f);
+    q = fmaf(q, t, LIN_LOG2E * 1.48851587f);
+    q = fmaf(q, t, LIN_LOG2E * -1.13520398f);
+    q = fmaf(q, t, LIN_LOG2E * 0.27886807f);
+    q = fmaf(q, t, LIN_LOG2E * -0.18628806f);
+    q = fmaf(q, t, LIN_LOG2E * 0.09678418f);
+    q = fmaf(q, t, LIN_LOG2E * 0.37409196f);
+    q = fmaf(q, t, LIN_LOG2E * 1.00002368f);
+    q = fmaf(q, t, LIN_LOG2E * -1.26551223f);
+  } else {
+    q = LIN_LOG2E * 0.22879023753f;
+    q = fmaf(q, t, LIN_LOG2E * -0.70919065294f);
+    q = fmaf(q, t, LIN_LOG2E * 0.47449294008f);
+    q = fmaf(q, t, LIN_LOG2E * 0.25444333415f);
+    q = fmaf(q, t, LIN_LOG2E * 1.01801351084f);
+    q = fmaf(q, t, LIN_LOG2E * -1.26654175576f);
+  }
   q = fmaf(a * a, -0.5f * LIN_LOG2E, q);
   const float e = t * lin_exp2(q);
-  return v * (v <= 0.f ? 0.5f * e : fmaf(-0.5f, e, 1.f));                         // Phi(v) = erfc(-v / sqrt 2) / 2
+  return v * (v <= 0.f ? 0.5f * e : fmaf(-0.5f, e, 1.f));                        // Phi(v) = erfc(-v / sqrt 2) / 2
 }
 template <int N> __device__ __forceinline__ void lin_act_all(float (&v)[N], int act, bool f32) {
   if (act == JK_ACT_SILU) {
@@ -57,9 +72,9 @@ template <int N> __device__ __forceinline__ void lin_act_all(float (&v)[N], int 
     for (int j = 0; j < N; ++j) v[j] *= lin_rcp(1.f + lin_exp2(-LIN_LOG2E * v[j]));
   } else if (act == JK_ACT_GELU && f32) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = lin_act(v[j], JK_ACT_GELU);
+    for (int j = 0; j < N; ++j) v[j] = lin_gelu<true>(v[j]);
   } else if (act == JK_ACT_GELU) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = lin_gelu(v[j]);
+    for (int j = 0; j < N; ++j) v[j] = lin_gelu<false>(v[j]);
   }
 }

@@ -18,6 +18,8 @@
 //
 // Roles: warp 0 loads, warp 1 (of the pair's first CTA) multiplies, warps 2-9 are the epilogue.  Waits are bounded as
 // in the kernel for few rows.
+#include <type_traits>
+
 #include "jk_linear_tc.cuh"
 
 int jk_tma_encode_u8(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, const uint64_t* dims,
@@ -31,12 +33,14 @@ int jk_tma_encode_piece(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int es, 
 #define LP_BAND 8                         // tiles of x of a band
 #define LP_MAX_SPLIT 4                    // pairs that share a tile, at most
 #define LP_EPI_WARPS 8
+#define LP_W 16                           // columns that an epilogue warp works on at a time
 #define LP_THREADS (64 + 32 * LP_EPI_WARPS)
 #define LP_A_BYTES (LT_M * LT_BOX)        // of each operand in a box
 #define LP_SF_COL 488                     // 8-bit rows: first column of the scales, two sets of 12
 #define LP_ACC2_MX 232                    // 8-bit rows: first column of the second accumulator
 #define LP_MAX_STAGES 6
-#define LP_OUT_BYTES 2048                 // an epilogue warp's piece of the output: 32 rows of at most 64 bytes; two of them
+#define LP_PIECE 2048                     // an epilogue warp's piece of the output: 32 rows of 64 bytes; two of them
+#define LP_PIECE8 1024                    // ... of 8-bit outputs: 32 rows of 32; behind 32 x 32 f32
 #define LP_X_PITCH 34                     // the same memory as a 32 x 32 exchange: elements of a row
 
 struct lp_params {
@@ -58,7 +62,11 @@ struct __align__(16) lp_tail {
   unsigned seen;                          // epilogue warps that have seen all flags
 };
 
-template <bool MX> struct lp_ring { static constexpr int BYTES = 2 * LP_A_BYTES + (MX ? 2048 : 0), STAGES = MX ? 5 : 6; };
+template <bool MX, bool OUT8> struct lp_smem {
+  static constexpr int STAGE = 2 * LP_A_BYTES + (MX ? 2048 : 0), STAGES = MX || OUT8 ? 5 : 6;
+  static constexpr int WARP = 2 * LP_PIECE + (OUT8 ? 2 * LP_PIECE8 : 0);           // of an epilogue warp
+  static constexpr size_t BYTES = (size_t)STAGES * STAGE + LP_EPI_WARPS * WARP + sizeof(lp_tail) + 1024;
+};
 
 // ------------------------------------------------------------------------------------------ PTX
 // Loads of a pair: the barrier is the first CTA's, whichever CTA the data is for.
@@ -165,41 +173,45 @@ __device__ __forceinline__ uint32_t lp_pack(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// 32 elements of T from p as f32, the same for all lanes; those from `most` on are 0.
-__device__ __forceinline__ void lp_add32(float (&v)[32], const uint16_t* p, int most) {
-  if (most >= 32) {
+// Elements of T added to f32: 8 of a 16-byte piece; LP_W from p, where those from `most` on do not exist.
+template <int AT> __device__ __forceinline__ void lp_add8(float (&v)[LP_W], const uint4& r) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 r = __ldg(reinterpret_cast<const uint4*>(p) + i);
-      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[8 * i + 2 * j] += __uint_as_float(w[j] << 16);
-        v[8 * i + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
-      }
-    }
+  for (int j = 0; j < 4; ++j) {
+    v[AT + 2 * j] += __uint_as_float(w[j] << 16);
+    v[AT + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void lp_add(float (&v)[LP_W], const uint16_t* p, int most) {
+  if (most >= LP_W && ((uintptr_t)p & 15) == 0) {
+    const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+    lp_add8<0>(v, a);
+    lp_add8<8>(v, b);
   } else {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] += j < most ? __uint_as_float((uint32_t)p[j] << 16) : 0.f;
+    for (int j = 0; j < LP_W; ++j) v[j] += j < most ? __uint_as_float((uint32_t)p[j] << 16) : 0.f;
   }
 }
 // Where the copy engine has 16-byte chunk c of row r: pieces with rows of 64 bytes, and of 32.
 __device__ __forceinline__ uint32_t lp_at64(int r, int c) { return (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); }
 __device__ __forceinline__ uint32_t lp_at32(int r, int c) { return (uint32_t)(r * 32 + ((c ^ ((r >> 2) & 1)) << 4)); }
+// (and where an f32 row of 128 bytes is kept, so that neighbouring rows meet in different banks)
+__device__ __forceinline__ uint32_t lp_at128(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
 
 // ------------------------------------------------------------------------------------------ the kernel
-template <bool MX, bool GATED>
+template <bool MX, bool GATED, bool OUT8>
 __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
     const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u,
     const __grid_constant__ CUtensorMap map_sx, const __grid_constant__ CUtensorMap map_sw,
     const __grid_constant__ CUtensorMap map_su, const __grid_constant__ CUtensorMap map_out,
     const __grid_constant__ CUtensorMap map_res, const lp_params p, const lin_args a, int wide_out, int wide_res,
     float* __restrict__ partial, int32_t* flags, int32_t* status) {
-  constexpr int BOX_EL = MX ? 128 : 64, STAGE = lp_ring<MX>::BYTES, LP_STAGES = lp_ring<MX>::STAGES;
+  constexpr int BOX_EL = MX ? 128 : 64, STAGE = lp_smem<MX, OUT8>::STAGE, LP_STAGES = lp_smem<MX, OUT8>::STAGES;
+  constexpr int WARP = lp_smem<MX, OUT8>::WARP;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   unsigned char* pieces = smem + LP_STAGES * STAGE;
-  lp_tail& T = *reinterpret_cast<lp_tail*>(pieces + LP_EPI_WARPS * 2 * LP_OUT_BYTES);
+  lp_tail& T = *reinterpret_cast<lp_tail*>(pieces + LP_EPI_WARPS * WARP);
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   volatile int* abort_flag = &T.abort_flag;
@@ -328,7 +340,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
     // ------------------------------------------------------------------ epilogue
     const int quarter = warp & 3;          // the lanes of tensor memory this warp may read
     const int half = (warp - 2) >> 2;      // the columns 0 .. 127 upwards, or 255 .. 128 downwards
-    unsigned char* mine = pieces + (warp - 2) * 2 * LP_OUT_BYTES;    // 1024-byte aligned: two pieces
+    unsigned char* mine = pieces + (warp - 2) * WARP;                // 1024-byte aligned
     const uint32_t mine_u32 = smem_u32(mine);
     uint64_t* res_full = T.res_full[warp - 2];
     uint32_t res_ph = 0;                   // phases of the two, a bit each
@@ -366,32 +378,33 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
         __syncwarp();
       }
       auto chunk = [&](int c) { return half ? (GATED ? 3 : 7) - c : c; };
-      const bool rows_live = row0 < a.rows;
+      const bool rows_live = row0 < a.rows, live = row0 + lane < a.rows;
       // The residual of a chunk is brought to the piece that the chunk's outputs will take.
       auto ask_residual = [&](int c) {
         const int n = n0 + chunk(c) * 32;
         if (lane == 0 && n < a.n_out && rows_live) {
           lp_put_read<0>();                // (the piece's last outputs have been read)
-          lt_expect(smem_u32(&res_full[c & 1]), LP_OUT_BYTES, 1u);
-          lt_box(mine_u32 + (c & 1) * LP_OUT_BYTES, &map_res, n, row0, smem_u32(&res_full[c & 1]), 1u);
+          lt_expect(smem_u32(&res_full[c & 1]), LP_PIECE, 1u);
+          lt_box(mine_u32 + (c & 1) * LP_PIECE, &map_res, n, row0, smem_u32(&res_full[c & 1]), 1u);
         }
       };
-      const bool res_tma = whole && a.residual && wide_res;
+      // (where neither the residual's nor the outputs' rows begin at multiples of 16 bytes, both pass through an exchange;
+      // where only one does, and for f32 and 8-bit outputs, a lane reads its row)
+      const bool res_tma = !OUT8 && whole && a.residual && wide_res;
+      const bool res_x = !OUT8 && a.residual && a.out_type == JK_ROWS_T && !wide_out;
       if (res_tma) ask_residual(0);
-      // (a partial: 16 bytes of a lane next to the next lane's, 8 times for a chunk of 32 columns)
+      // (a partial: 16 bytes of a lane next to the next lane's; one other pair's are asked for LP_W columns ahead)
       const size_t my_part = (size_t)quarter * LP_N * 32 + lane * 4;
-      float4 t[8], tu[GATED ? 8 : 1];
-      auto ask_part = [&](int i, int q) {
-        const float* o = partial + (size_t)(2 * i + rank) * LT_SLOT + my_part + (size_t)q * 32 * 32;
+      float4 t[LP_W / 4], tu[GATED ? LP_W / 4 : 1];
+      auto ask_part = [&](int i, int col) {
+        const float* o = partial + (size_t)(2 * i + rank) * LT_SLOT + my_part + (size_t)col * 32;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < LP_W / 4; ++j) {
           t[j] = __ldcg(reinterpret_cast<const float4*>(o + j * 128));
           if constexpr (GATED) tu[j] = __ldcg(reinterpret_cast<const float4*>(o + LT_M * 32 + j * 128));
         }
       };
-      // (one other pair's partials are asked for a chunk ahead; not in a gated block, whose chunk fills the registers)
-      constexpr bool AHEAD = !GATED;
-      if (AHEAD && from < pair) ask_part(pair - 1, chunk(0));
+      if (from < pair) ask_part(pair - 1, chunk(0) * 32);
       ok = mbar_wait(&T.acc_full[buf], (uint32_t)use & 1u, abort_flag, status);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -399,153 +412,179 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
       const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * (MX ? LP_ACC2_MX : LP_N));
 #pragma unroll 1
       for (int c = 0; c < CHUNKS; ++c) {
-        __syncwarp();
-        const int q = chunk(c);            // chunk of 32 outputs
-        float v[32], u[GATED ? 32 : 1];
-        {
-          uint32_t w[32];
-          tmem_ld32(t_addr + (uint32_t)(q * 32), w);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(w[j]);
-          if constexpr (GATED) {
-            tmem_ld32(t_addr + (uint32_t)(LT_M + q * 32), w);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) u[j] = __uint_as_float(w[j]);
-          }
-        }
-        if ((MX && c == 0) || c == CHUNKS - 1) {
-          tc_fence_before();
-          __syncwarp();
-          // the columns that both accumulators use: the last 24 of the first, the first 24 of the second
-          if (MX && c == 0 && half != buf && lane == 0) lp_arrive(shared0);
-          if (c == CHUNKS - 1 && lane == 0) lp_arrive(acc_empty0 + 8u * (uint32_t)buf);
-        }
-        if (!whole) {
-          float* o = partial + (size_t)blockIdx.x * LT_SLOT + my_part + (size_t)q * 32 * 32;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            __stcg(reinterpret_cast<float4*>(o + j * 128), make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-            if constexpr (GATED)
-              __stcg(reinterpret_cast<float4*>(o + LT_M * 32 + j * 128),
-                     make_float4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]));
-          }
-          continue;
-        }
-        for (int i = pair - 1; i >= from; --i) {
-          if (!AHEAD || i < pair - 1) ask_part(i, q);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            v[4 * j] += t[j].x; v[4 * j + 1] += t[j].y; v[4 * j + 2] += t[j].z; v[4 * j + 3] += t[j].w;
-            if constexpr (GATED) {
-              u[4 * j] += tu[j].x; u[4 * j + 1] += tu[j].y; u[4 * j + 2] += tu[j].z; u[4 * j + 3] += tu[j].w;
-            }
-          }
-        }
-        if (AHEAD && from < pair && c + 1 < CHUNKS) ask_part(pair - 1, chunk(c + 1));
-        if (res_tma && c + 1 < CHUNKS) ask_residual(c + 1);
-        const int n = n0 + q * 32, most = a.n_out - n;
-        if (most <= 0 || !rows_live) continue;
-        unsigned char* piece = mine + (c & 1) * LP_OUT_BYTES;
-        // ---- the epilogue proper: the lane's row, outputs n .. n + 31
-        if (a.bias) lp_add32(v, (const uint16_t*)a.bias + n, most);
-        lin_act_all(v, a.act, a.out_type == JK_ROWS_F32);
-        if constexpr (GATED) {
-          if (a.bias_up) lp_add32(u, (const uint16_t*)a.bias_up + n, most);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] *= u[j];
-        }
+        const int q = chunk(c), n = n0 + q * 32, most = a.n_out - n;
+        const bool out_live = whole && most > 0 && rows_live;
+        unsigned char* piece = mine + (OUT8 ? 2 * LP_PIECE + (c & 1) * LP_PIECE8 : (c & 1) * LP_PIECE);
+        uint16_t* X = reinterpret_cast<uint16_t*>(mine);
+        // ---- the piece's memory: its last outputs have been read, or the residual has come
         if (res_tma) {
-          ok = mbar_wait(&res_full[c & 1], (res_ph >> (c & 1)) & 1u, abort_flag, status);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          res_ph ^= 1u << (c & 1);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint4 r = *reinterpret_cast<const uint4*>(piece + lp_at64(lane, i));
-            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              v[8 * i + 2 * j] += __uint_as_float(w[j] << 16);
-              v[8 * i + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
-            }
+          if (c + 1 < CHUNKS) ask_residual(c + 1);
+          if (out_live) {
+            ok = mbar_wait(&res_full[c & 1], (res_ph >> (c & 1)) & 1u, abort_flag, status);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            res_ph ^= 1u << (c & 1);
           }
-        } else {
-          if (lane == 0) {                 // the piece's last outputs have been read
-            if (wide_out && a.out_type != JK_ROWS_F32 && !a.residual) lp_put_read<1>();
+        } else if (out_live) {
+          if (lane == 0) {
+            if (wide_out && (OUT8 || a.out_type == JK_ROWS_T)) lp_put_read<1>();
             else lp_put_read<0>();
           }
           __syncwarp();
-          if (a.residual) {
+          if (res_x) {
             // rows that begin anywhere: read along the rows, handed out through shared memory
-            uint16_t* X = reinterpret_cast<uint16_t*>(mine);
             const uint16_t* rp = (const uint16_t*)a.residual + (size_t)row0 * a.r_stride + n + lane;
-#pragma unroll 8
+#pragma unroll 4
             for (int j = 0; j < 32; ++j, rp += a.r_stride)
               X[j * LP_X_PITCH + lane] = row0 + j < a.rows && lane < most ? *rp : (uint16_t)0;
             __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] += __uint_as_float((uint32_t)X[lane * LP_X_PITCH + j] << 16);
-            __syncwarp();
           }
         }
-        if (a.out_type == JK_ROWS_MX8) {   // n_out is a multiple of 32: all of the block or nothing
-          float m = 0.f;
+        float top = 0.f;                   // 8-bit outputs: the block's largest magnitude
+#pragma unroll 1
+        for (int i = 0; i < 32; i += LP_W) {
+          const int col = q * 32 + i, nw = n + i, most_w = most - i;
+          float v[LP_W], u[LP_W];
+          // (the biases are asked for ahead of the sums; n is a multiple of 16, so they are aligned)
+          uint4 b[2], bu[2];
+          const bool bias_full = out_live && most_w >= LP_W;
+          if (bias_full && a.bias) {
+            const uint4* bp = reinterpret_cast<const uint4*>((const uint16_t*)a.bias + nw);
+            b[0] = bp[0];
+            b[1] = bp[1];
+          }
+          if (GATED && bias_full && a.bias_up) {
+            const uint4* bp = reinterpret_cast<const uint4*>((const uint16_t*)a.bias_up + nw);
+            bu[0] = bp[0];
+            bu[1] = bp[1];
+          }
+          {
+            uint32_t w[LP_W], w2[LP_W];
+            tmem_ld16(t_addr + (uint32_t)col, w);
+            if constexpr (GATED) tmem_ld16(t_addr + (uint32_t)(LT_M + col), w2);
+            tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) m = fmaxf(m, paged_mag(v[j]));
-          const int e = paged_scale_exp(m);
+            for (int j = 0; j < LP_W; ++j) {
+              v[j] = __uint_as_float(w[j]);
+              u[j] = GATED ? __uint_as_float(w2[j]) : 0.f;
+            }
+          }
+          if (i + LP_W == 32 && ((MX && c == 0) || c == CHUNKS - 1)) {
+            tc_fence_before();
+            __syncwarp();
+            // the columns that both accumulators use: the last 24 of the first, the first 24 of the second
+            if (MX && c == 0 && half != buf && lane == 0) lp_arrive(shared0);
+            if (c == CHUNKS - 1 && lane == 0) lp_arrive(acc_empty0 + 8u * (uint32_t)buf);
+          }
+          if (!whole) {
+            float* o = partial + (size_t)blockIdx.x * LT_SLOT + my_part + (size_t)col * 32;
+#pragma unroll
+            for (int j = 0; j < LP_W / 4; ++j) {
+              __stcg(reinterpret_cast<float4*>(o + j * 128), make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+              if constexpr (GATED)
+                __stcg(reinterpret_cast<float4*>(o + LT_M * 32 + j * 128),
+                       make_float4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]));
+            }
+            continue;
+          }
+          for (int k = pair - 1; k >= from; --k) {
+            if (k < pair - 1) ask_part(k, col);
+#pragma unroll
+            for (int j = 0; j < LP_W / 4; ++j) {
+              v[4 * j] += t[j].x; v[4 * j + 1] += t[j].y; v[4 * j + 2] += t[j].z; v[4 * j + 3] += t[j].w;
+              if constexpr (GATED) {
+                u[4 * j] += tu[j].x; u[4 * j + 1] += tu[j].y; u[4 * j + 2] += tu[j].z; u[4 * j + 3] += tu[j].w;
+              }
+            }
+          }
+          const bool last = i + LP_W == 32;
+          if (from < pair && (!last || c + 1 < CHUNKS)) ask_part(pair - 1, last ? chunk(c + 1) * 32 : col + LP_W);
+          if (!out_live) continue;
+          if (a.bias) {
+            if (bias_full) { lp_add8<0>(v, b[0]); lp_add8<8>(v, b[1]); }
+            else lp_add(v, (const uint16_t*)a.bias + nw, most_w);
+          }
+          lin_act_all(v, a.act, !OUT8 && a.out_type == JK_ROWS_F32);
+          if constexpr (GATED) {
+            if (a.bias_up) {
+              if (bias_full) { lp_add8<0>(u, bu[0]); lp_add8<8>(u, bu[1]); }
+              else lp_add(u, (const uint16_t*)a.bias_up + nw, most_w);
+            }
+#pragma unroll
+            for (int j = 0; j < LP_W; ++j) v[j] *= u[j];
+          }
+          if (a.residual && !res_tma && !res_x && live)
+            lp_add(v, (const uint16_t*)a.residual + (size_t)(row0 + lane) * a.r_stride + nw, most_w);
+          if constexpr (OUT8) {
+#pragma unroll
+            for (int j = 0; j < LP_W; ++j) top = fmaxf(top, paged_mag(v[j]));
+#pragma unroll
+            for (int j = 0; j < LP_W / 4; ++j)
+              *reinterpret_cast<float4*>(mine + lp_at128(lane, i / 4 + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          } else {
+            if (res_tma) {
+              lp_add8<0>(v, *reinterpret_cast<const uint4*>(piece + lp_at64(lane, i / 8)));
+              lp_add8<8>(v, *reinterpret_cast<const uint4*>(piece + lp_at64(lane, i / 8 + 1)));
+            } else if (res_x) {
+#pragma unroll
+              for (int j = 0; j < LP_W; ++j) v[j] += __uint_as_float((uint32_t)X[lane * LP_X_PITCH + i + j] << 16);
+            }
+            if (a.out_type == JK_ROWS_T) {
+              uint32_t o[LP_W / 2];
+#pragma unroll
+              for (int j = 0; j < LP_W / 2; ++j) o[j] = lp_pack(v[2 * j], v[2 * j + 1]);
+              if (wide_out) {
+                *reinterpret_cast<uint4*>(piece + lp_at64(lane, i / 8)) = make_uint4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<uint4*>(piece + lp_at64(lane, i / 8 + 1)) = make_uint4(o[4], o[5], o[6], o[7]);
+              } else {
+                uint32_t* x32 = reinterpret_cast<uint32_t*>(&X[lane * LP_X_PITCH + i]);
+#pragma unroll
+                for (int j = 0; j < LP_W / 2; ++j) x32[j] = o[j];
+              }
+            } else if (wide_out) {         // f32: 16 outputs to a piece
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<float4*>(mine + i / 16 * LP_PIECE + lp_at64(lane, j)) =
+                    make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            } else if (live) {
+              float* p32 = (float*)a.out + (size_t)(row0 + lane) * a.o_stride + nw;
+#pragma unroll
+              for (int j = 0; j < LP_W; ++j)
+                if (j < most_w) p32[j] = v[j];
+            }
+          }
+        }
+        __syncwarp();
+        if (!out_live) continue;
+        if constexpr (OUT8) {              // n_out is a multiple of 32: all of the block or nothing
+          const int e = paged_scale_exp(top);
           const float inv = paged_pow2(-e);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             uint32_t o[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              o[j] = paged_pack4(v[16 * i + 4 * j] * inv, v[16 * i + 4 * j + 1] * inv, v[16 * i + 4 * j + 2] * inv, v[16 * i + 4 * j + 3] * inv);
+            for (int j = 0; j < 4; ++j) {
+              const float4 y = *reinterpret_cast<const float4*>(mine + lp_at128(lane, 4 * i + j));
+              o[j] = paged_pack4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+            }
             *reinterpret_cast<uint4*>(piece + lp_at32(lane, i)) = make_uint4(o[0], o[1], o[2], o[3]);
           }
-          if (row0 + lane < a.rows) a.out_scale[mx_scale_at(row0 + lane, n >> 5, a.k_tiles_out)] = (uint8_t)(e + 127);
-        } else if (a.out_type == JK_ROWS_T) {
-          if (wide_out) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<uint4*>(piece + lp_at64(lane, i)) =
-                  make_uint4(lp_pack(v[8 * i], v[8 * i + 1]), lp_pack(v[8 * i + 2], v[8 * i + 3]),
-                             lp_pack(v[8 * i + 4], v[8 * i + 5]), lp_pack(v[8 * i + 6], v[8 * i + 7]));
-          } else {
-            uint16_t* X = reinterpret_cast<uint16_t*>(mine);
-            uint32_t* x32 = reinterpret_cast<uint32_t*>(&X[lane * LP_X_PITCH]);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) x32[j] = lp_pack(v[2 * j], v[2 * j + 1]);
-            __syncwarp();
-            uint16_t* o = (uint16_t*)a.out + (size_t)row0 * a.o_stride + n + lane;
-#pragma unroll 8
-            for (int j = 0; j < 32; ++j, o += a.o_stride)
-              if (row0 + j < a.rows && lane < most) *o = X[j * LP_X_PITCH + lane];
-          }
-        } else if (wide_out) {             // f32: 16 outputs to a piece
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<uint4*>(mine + h * LP_OUT_BYTES + lp_at64(lane, i)) =
-                  make_uint4(__float_as_uint(v[16 * h + 4 * i]), __float_as_uint(v[16 * h + 4 * i + 1]),
-                             __float_as_uint(v[16 * h + 4 * i + 2]), __float_as_uint(v[16 * h + 4 * i + 3]));
-        } else if (row0 + lane < a.rows) {
-          float* o = (float*)a.out + (size_t)(row0 + lane) * a.o_stride + n;
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (j < most) o[j] = v[j];
+          if (live) a.out_scale[mx_scale_at(row0 + lane, n >> 5, a.k_tiles_out)] = (uint8_t)(e + 127);
+        } else if (a.out_type == JK_ROWS_T && !wide_out) {
+          uint16_t* o = (uint16_t*)a.out + (size_t)row0 * a.o_stride + n + lane;
+#pragma unroll 4
+          for (int j = 0; j < 32; ++j, o += a.o_stride)
+            if (row0 + j < a.rows && lane < most) *o = X[j * LP_X_PITCH + lane];
         }
         if (wide_out) {
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (a.out_type == JK_ROWS_F32) {
+            if (!OUT8 && a.out_type == JK_ROWS_F32) {
               lp_put(&map_out, n, row0, mine_u32);
-              if (most > 16) lp_put(&map_out, n + 16, row0, mine_u32 + LP_OUT_BYTES);
+              if (most > 16) lp_put(&map_out, n + 16, row0, mine_u32 + LP_PIECE);
             } else {
-              lp_put(&map_out, n, row0, mine_u32 + (c & 1) * LP_OUT_BYTES);
+              lp_put(&map_out, n, row0, smem_u32(piece));
             }
           }
         }
@@ -602,6 +641,23 @@ double jk_linear_pair_plan(const lin_args& a, bool mx, int sms, lp_params* out) 
   return 6.9 + (us > hbm_us ? us : hbm_us);
 }
 
+template <typename K>
+static int launch_pair(jk_ctx* ctx, cudaStream_t st, K kernel, size_t smem, int bit, const CUtensorMap& x, const CUtensorMap& w,
+                       const CUtensorMap& u, const CUtensorMap& sx, const CUtensorMap& sw, const CUtensorMap& su,
+                       const CUtensorMap& o, const CUtensorMap& r, const lp_params& p, const lin_args& a, int wide_out,
+                       int wide_res) {
+  if (!(ctx->lin_smem_set & bit)) {
+    JK_CUDA_CHECK(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    ctx->lin_smem_set |= bit;
+  }
+  JK_PROF(ctx, st, JK_ST_LINEAR);
+  jk_launch_pdl_cluster(kernel, dim3(2 * p.pairs), dim3(LP_THREADS), 2, smem, st, x, w, u, sx, sw, su, o, r, p, a, wide_out, wide_res,
+                        (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
+                        (int32_t*)(ctx->ws + ctx->lay.status));
+  JK_LAUNCH_CHECK(ctx);
+  return JK_OK;
+}
+
 int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   const bool gated = a.w_up != nullptr;
   const int es = mx ? 1 : 2, box_el = LT_BOX / es;
@@ -633,19 +689,13 @@ int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   if (wide_out) rc = jk_tma_encode_piece(ctx, &mo, a.out, q8 ? 1 : f32 ? 4 : 2, a.n_out, a.rows, a.o_stride, f32 ? 16 : 32);
   if (rc == JK_OK && wide_res) rc = jk_tma_encode_piece(ctx, &mr, a.residual, 2, a.n_out, a.rows, a.r_stride, 32);
   if (rc != JK_OK) return rc;
-  auto kernel = mx ? (gated ? k_linear_pair<true, true> : k_linear_pair<true, false>)
-                   : (gated ? k_linear_pair<false, true> : k_linear_pair<false, false>);
-  const size_t smem = (size_t)(mx ? lp_ring<true>::STAGES * lp_ring<true>::BYTES : lp_ring<false>::STAGES * lp_ring<false>::BYTES) +
-                      LP_EPI_WARPS * 2 * LP_OUT_BYTES + sizeof(lp_tail) + 1024;
-  const int bit = 16 << (2 * mx + gated);
-  if (!(ctx->lin_smem_set & bit)) {
-    JK_CUDA_CHECK(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    ctx->lin_smem_set |= bit;
-  }
-  JK_PROF(ctx, st, JK_ST_LINEAR);
-  jk_launch_pdl_cluster(kernel, dim3(2 * p.pairs), dim3(LP_THREADS), 2, smem, st, mx_map, mw, mu, msx, msw, msu, mo, mr, p, a,
-                        wide_out, wide_res,                        (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
-                        (int32_t*)(ctx->ws + ctx->lay.status));
-  JK_LAUNCH_CHECK(ctx);
-  return JK_OK;
+  // (8-bit outputs are always wide: n_out is a multiple of 32)
+  auto pick = [&](auto m, auto g, auto o) {
+    constexpr bool M = decltype(m)::value, G = decltype(g)::value, O = decltype(o)::value;
+    return launch_pair(ctx, st, k_linear_pair<M, G, O>, lp_smem<M, O>::BYTES, 16 << (4 * M + 2 * G + O), mx_map, mw, mu, msx, msw,
+                       msu, mo, mr, p, a, wide_out, wide_res);
+  };
+  auto pick_g = [&](auto m, auto g) { return q8 ? pick(m, g, std::true_type()) : pick(m, g, std::false_type()); };
+  auto pick_m = [&](auto m) { return gated ? pick_g(m, std::true_type()) : pick_g(m, std::false_type()); };
+  return mx ? pick_m(std::true_type()) : pick_m(std::false_type());
 }

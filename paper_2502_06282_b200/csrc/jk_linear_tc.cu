@@ -99,8 +99,8 @@ __device__ __forceinline__ int lt_round_cols(const lt_params& p, int parts, int 
 }
 
 // ------------------------------------------------------------------------------------------ epilogue
-// One thread holds output n of up to 16 rows.
-#define LT_COLS 16
+// One thread holds output n of up to 8 rows.
+#define LT_COLS 8
 template <bool GATED>
 __device__ __forceinline__ void lt_store(const lin_args& a, float (&v)[LT_COLS], float (&u)[GATED ? LT_COLS : 1], int cols,
                                          int r0, int n, float bias, float bias_up, const uint16_t (&res)[LT_COLS]) {
@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
   } else if (warp >= 2) {
     // ------------------------------------------------------------------ epilogue
     const int quarter = warp & 3;          // the lanes of tensor memory this warp may read
-    const int sub = (warp - 2) >> 2;       // its warps take 16 columns in turn
+    const int sub = (warp - 2) >> 2;       // its warps take 8 columns in turn
     const int m = quarter * 32 + lane;
     int seg = 0;
     bool ok = true;
@@ -412,8 +412,8 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
           float v[LT_COLS], u[GATED ? LT_COLS : 1];
           {
             uint32_t t[LT_COLS], t2[LT_COLS];
-            tmem_ld16(t_addr + (uint32_t)c, t);
-            if constexpr (GATED) tmem_ld16(t_addr + (uint32_t)(p.nt + c), t2);
+            lt_ld8(t_addr + (uint32_t)c, t);
+            if constexpr (GATED) lt_ld8(t_addr + (uint32_t)(p.nt + c), t2);
             tmem_ld_wait();
 #pragma unroll
             for (int j = 0; j < LT_COLS; ++j) {
