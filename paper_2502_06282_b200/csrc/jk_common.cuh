@@ -89,6 +89,7 @@ struct jk_ctx {
   int attn_smem_set;
   int attn_sk_smem_set;
   int lin_smem_set;       // one bit for each kernel of jk_linear
+  int lin_clusters[3];    // clusters of 2, 4, 8 of its CTAs that run at a time (0: not asked yet)
   unsigned gemm_seq;     // GEMM launches so far: picks the item counter
   int st_attn, st_combine;  // profiling stages the attention kernels are booked under
   int attn_kernel;        // 0 = by size, 1 = CTA per (query block, key slice), 2 = persistent,

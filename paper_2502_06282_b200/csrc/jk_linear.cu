@@ -5,10 +5,7 @@
 int jk_tma_available(jk_ctx* ctx);                                             // jk_gemm_tc.cu
 int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx);    // jk_linear_tc.cu
 int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx);  // jk_linear_pair.cu
-struct lt_params;
-struct lp_params;
-double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, lt_params* out);
-double jk_linear_pair_plan(const lin_args& a, bool mx, int sms, lp_params* out);
+int jk_linear_tc_pays(jk_ctx* ctx, const lin_args& a, bool mx, bool* pays);    // jk_linear_tc.cu
 
 // ------------------------------------------------------------------------------------------ operands
 // Four consecutive elements of a row as f32; element types: float, bf16, uint8_t (mx8 codes, k a
@@ -299,8 +296,8 @@ extern "C" int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* op, int3
     // Few rows: the kernel that streams weights past them, while the rows fit one tile (256, gated 128) and by the
     // costs that the two kernels give.  Measured, us, 4096 x 4096 in bf16: 64 rows 12.4 against 21.5, 128 rows 16.1 / 22.0,
     // 256 rows 25.0 / 22.2; in 8 bits 128 rows 13.5 / 17.3, 192 rows 19.1 / 17.4; 1376 x 512: 60 rows 7.2 / 8.8.
-    const bool few = rows <= (op->w_up ? 128 : 256) &&
-                     jk_linear_tc_plan(a, mx, ctx->sm_count, nullptr) <= jk_linear_pair_plan(a, mx, ctx->sm_count, nullptr);
+    bool few = rows <= (op->w_up ? 128 : 256);
+    if (few && (rc = jk_linear_tc_pays(ctx, a, mx, &few)) != JK_OK) return rc;
     return few ? jk_linear_tc(ctx, st, a, mx) : jk_linear_pair(ctx, st, a, mx);
   }
   JK_PROF(ctx, st, JK_ST_LINEAR);

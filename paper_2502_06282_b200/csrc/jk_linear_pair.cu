@@ -103,16 +103,8 @@ __device__ __forceinline__ void lp_commit(uint32_t bar, uint32_t lead) {
                ::"r"(bar), "r"(lead), "h"((uint16_t)3)
                : "memory");
 }
-__device__ __forceinline__ uint32_t lp_map(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
 __device__ __forceinline__ void lp_arrive(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-__device__ __forceinline__ void lp_cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __host__ __device__ inline uint32_t lp_idesc_bf16() {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(LP_N >> 3) << 17) | ((uint32_t)(LP_ROWS >> 4) << 24);
@@ -231,7 +223,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
   }
   tc_fence_before();
   __syncthreads();
-  lp_cluster_sync();                       // the barriers of both CTAs exist
+  lt_cluster_sync();                       // the barriers of both CTAs exist
   tc_fence_after();
   const uint32_t tmem_base = T.tmem_base;
   lp_walk walk(p, pair);
@@ -243,7 +235,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
   if (warp == 0) {
     // ------------------------------------------------------------------ copies
     const uint32_t lead = lt_elect(), base = smem_u32(smem);
-    const uint32_t full0 = lp_map(smem_u32(T.full), 0), own_full0 = smem_u32(T.full);
+    const uint32_t full0 = lt_map(smem_u32(T.full), 0), own_full0 = smem_u32(T.full);
     bool ok = true;
     int s = 0;
     long long issued = 0;
@@ -344,7 +336,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
     const uint32_t mine_u32 = smem_u32(mine);
     uint64_t* res_full = T.res_full[warp - 2];
     uint32_t res_ph = 0;                   // phases of the two, a bit each
-    const uint32_t acc_empty0 = lp_map(smem_u32(T.acc_empty), 0), shared0 = lp_map(smem_u32(&T.shared_free), 0);
+    const uint32_t acc_empty0 = lt_map(smem_u32(T.acc_empty), 0), shared0 = lt_map(smem_u32(&T.shared_free), 0);
     constexpr int CHUNKS = GATED ? 2 : 4;  // of 32 outputs, for this warp
     int seg = 0;
     bool ok = true;
@@ -600,7 +592,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
   }
   tc_fence_before();
   __syncthreads();
-  lp_cluster_sync();                       // nobody's memory is used any more
+  lt_cluster_sync();                       // nobody's memory is used any more
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");

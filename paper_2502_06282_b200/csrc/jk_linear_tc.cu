@@ -22,7 +22,8 @@
 
 int jk_tma_encode_u8(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int rank, const uint64_t* dims,
                      const uint64_t* strides_bytes, const uint32_t* box);
-int jk_tma_available(jk_ctx* ctx);
+struct lp_params;
+double jk_linear_pair_plan(const lin_args& a, bool mx, int sms, lp_params* out);
 
 #define LT_EPI_WARPS 16                   // four for each quarter of the lanes of tensor memory
 #define LT_THREADS (64 + 32 * LT_EPI_WARPS)   // and two warps that load and multiply
@@ -48,6 +49,8 @@ struct lt_params {
   long long units;                        // stages of all tiles
   int by_tile;                            // 1: the shares end with tiles
   int grid;
+  int cluster;                            // CTAs of a cluster that share a tile; 1: none
+  int slots, exchange;                    // clusters: runs of 8 rows that a CTA finishes, and bytes of what it is handed
 };
 
 struct __align__(16) lt_tail {
@@ -74,7 +77,17 @@ __device__ __forceinline__ long long lt_first(const lt_params& p, int i) {
 
 struct lt_walk {                           // a CTA's segments, last tile first
   long long lo, hi;
-  __device__ __forceinline__ lt_walk(const lt_params& p) : lo(lt_first(p, blockIdx.x)), hi(lt_first(p, blockIdx.x + 1)) {}
+  __device__ __forceinline__ lt_walk(const lt_params& p) {
+    if (p.cluster > 1) {                   // one tile for each cluster, cut evenly
+      const int rank = blockIdx.x % p.cluster;
+      const long long t0 = (long long)(blockIdx.x / p.cluster) * p.ks;
+      lo = t0 + p.ks * rank / p.cluster;
+      hi = t0 + p.ks * (rank + 1) / p.cluster;
+    } else {
+      lo = lt_first(p, blockIdx.x);
+      hi = lt_first(p, blockIdx.x + 1);
+    }
+  }
   __device__ __forceinline__ bool next(const lt_params& p, int& tile, int& k0, int& k1) {
     if (hi <= lo) return false;
     tile = (int)((hi - 1) / p.ks);
@@ -154,7 +167,8 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
   constexpr int BOX_EL = MX ? 128 : 64;    // elements of a box row
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  lt_tail& T = *reinterpret_cast<lt_tail*>(smem + (size_t)p.stages * p.stage_bytes);
+  unsigned char* handed = smem + (size_t)p.stages * p.stage_bytes;
+  lt_tail& T = *reinterpret_cast<lt_tail*>(handed + p.exchange);
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   volatile int* abort_flag = &T.abort_flag;
   // a stage: kb boxes of w, kb of w_up, kb of x, then the scale tiles in the same order
@@ -198,8 +212,11 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
     __syncwarp();
   }
   const uint32_t tmem_base = warp ? T.tmem_base : 0;       // (warp 0 may be ahead of the allocation; it needs no address)
+  if (p.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   jk_pdl_wait();
   jk_pdl_trigger();
+  // (a CTA's memory is written from outside only once it runs)
+  if (p.cluster > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 
   if (warp == 0) {
     // ------------------------------------------------------------------ copies
@@ -252,7 +269,7 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
     const long long lo = lt_first(p, blockIdx.x);
     tile = (int)(lo / p.ks);
     k0 = (int)(lo - (long long)tile * p.ks);
-    if (ok && k0 > 0 && lt_first(p, blockIdx.x + 1) - lo >= p.ks - k0) {
+    if (ok && p.cluster == 1 && k0 > 0 && lt_first(p, blockIdx.x + 1) - lo >= p.ks - k0) {
       const int parts = (int)blockIdx.x - lt_from(p, tile, k0), cols = lt_round_cols(p, parts, G);
       const int rows = min(p.nt, a.rows - tile % p.r_tiles * p.nt);
       const int other = (int)blockIdx.x - 1 - lane;
@@ -367,7 +384,32 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
       if (ok) lt_commit(smem_u32(&T.acc_full[buf]), lead);
       ++seg;
     }
-  } else if (warp >= 2) {
+  } else if (p.cluster > 1) {
+    // ------------------------------------------------------------------ epilogue of a shared tile, first half
+    // Each CTA of the cluster finishes every cluster-th run of 8 rows: it is handed the others' sums of
+    // those in its shared memory, and its own.
+    const int quarter = warp & 3, m = quarter * 32 + lane, rank = blockIdx.x % p.cluster;
+    const int rows = min(p.nt, a.rows - tile % p.r_tiles * p.nt);
+    bool ok = mbar_wait(&T.acc_full[0], 0, abort_flag, status);
+    ok = __all_sync(0xffffffffu, ok);
+    if (ok) {
+      tc_fence_after();
+      const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+      for (int j = (warp - 2) >> 2; j * 8 < rows; j += LT_EPI_WARPS / 4) {
+        uint32_t v[8], u[8];
+        lt_ld8(t_addr + (uint32_t)(j * 8), v);
+        if constexpr (GATED) lt_ld8(t_addr + (uint32_t)(p.nt + j * 8), u);
+        tmem_ld_wait();
+        const uint32_t to = lt_map(smem_u32(handed) + (uint32_t)(((rank * p.slots + j / p.cluster) * G * 8 * LT_M + m) * 4),
+                                   (uint32_t)(j % p.cluster));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + i * LT_M * 4), "r"(v[i]) : "memory");
+          if constexpr (GATED) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + (8 + i) * LT_M * 4), "r"(u[i]) : "memory");
+        }
+      }
+    }
+  } else {
     // ------------------------------------------------------------------ epilogue
     const int quarter = warp & 3;          // the lanes of tensor memory this warp may read
     const int sub = (warp - 2) >> 2;       // its warps take 8 columns in turn
@@ -453,6 +495,49 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
       ++seg;
     }
   }
+  if (p.cluster > 1) {
+    // ------------------------------------------------------------------ ... second half
+    const int m = (warp & 3) * 32 + lane, rank = blockIdx.x % p.cluster, sub = (warp - 2) >> 2;
+    const int own = blockIdx.x / p.cluster, wt = own / p.r_tiles, rt = own - wt * p.r_tiles;
+    const int n = wt * LT_M + m, r0 = rt * p.nt, rows = min(p.nt, a.rows - r0);
+    const bool live = n < a.n_out;
+    uint16_t res[LT_COLS];
+    float bias = 0.f, bias_up = 0.f;
+    auto ask_residual = [&](int c) {
+      const uint16_t* rp = (const uint16_t*)a.residual + (size_t)(r0 + c) * a.r_stride + n;
+#pragma unroll
+      for (int j = 0; j < LT_COLS; ++j, rp += a.r_stride) res[j] = live && c + j < rows ? *rp : (uint16_t)0;
+    };
+    if (warp >= 2) {                       // (asked for ahead of the meeting)
+      if (live && a.bias) bias = __bfloat162float(((const __nv_bfloat16*)a.bias)[n]);
+      if (GATED && live && a.bias_up) bias_up = __bfloat162float(((const __nv_bfloat16*)a.bias_up)[n]);
+      if (a.residual) ask_residual((sub * p.cluster + rank) * 8);
+    }
+    __syncwarp();
+    lt_cluster_sync();
+    if (warp >= 2) {
+      for (int slot = sub; slot < p.slots; slot += LT_EPI_WARPS / 4) {
+        const int c = (slot * p.cluster + rank) * 8;
+        if (c >= rows) break;
+        if (a.residual && slot != sub) ask_residual(c);
+        float v[LT_COLS], u[GATED ? LT_COLS : 1];
+#pragma unroll
+        for (int j = 0; j < LT_COLS; ++j) {
+          v[j] = 0.f;
+          if constexpr (GATED) u[j] = 0.f;
+        }
+        for (int i = 0; i < p.cluster; ++i) {              // in the order of k
+          const float* o = reinterpret_cast<const float*>(handed) + (size_t)((i * p.slots + slot) * G * 8) * LT_M + m;
+#pragma unroll
+          for (int j = 0; j < LT_COLS; ++j) {
+            v[j] += o[j * LT_M];
+            if constexpr (GATED) u[j] += o[(8 + j) * LT_M];
+          }
+        }
+        lt_store<GATED>(a, v, u, min(LT_COLS, rows - c), r0 + c, n, bias, bias_up, res);
+      }
+    }
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -467,7 +552,7 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
 // accumulators, a quarter more for each further share.  Measured with 4096 outputs, 64 boxes (bf16, 4096 inputs), us:
 // 60 rows 18.3 whole, 15.1, 13.5, 12.5 with 2, 3, 4 shares, 12.5 with 4.6; 8 boxes: 7.3 whole, 8.4, 8.3, 8.8.  The costs,
 // in us and with a launch, also choose between this kernel and that for many rows.
-double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, lt_params* out) {
+double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, const int* clusters, lt_params* out) {
   const int G = a.w_up ? 2 : 1, es = mx ? 1 : 2, box_el = LT_BOX / es;
   lt_params p;
   memset(&p, 0, sizeof(p));
@@ -481,11 +566,15 @@ double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, lt_params* out) {
   p.b_box = p.nt * LT_BOX;
   p.sfb = mx ? (p.nt + 127) / 128 : 0;
   const int box_bytes = G * p.a_box + p.b_box + (mx ? (G + p.sfb) * MX_TILE_BYTES : 0);
+  // The ring: stages of two boxes while four of them fit.
+  auto ring = [&](int room) {
+    p.kb = room / (2 * box_bytes) >= 4 && p.boxes > 1 ? 2 : 1;
+    p.ks = (p.boxes + p.kb - 1) / p.kb;
+    p.stage_bytes = (int)jk_align_up((size_t)p.kb * box_bytes, 1024);
+    p.stages = room / p.stage_bytes < LT_MAX_STAGES ? room / p.stage_bytes : LT_MAX_STAGES;
+  };
   const int room = LT_SMEM - (int)sizeof(lt_tail) - 1024;
-  p.kb = room / (2 * box_bytes) >= 4 && p.boxes > 1 ? 2 : 1;
-  p.ks = (p.boxes + p.kb - 1) / p.kb;
-  p.stage_bytes = (int)jk_align_up((size_t)p.kb * box_bytes, 1024);
-  p.stages = room / p.stage_bytes < LT_MAX_STAGES ? room / p.stage_bytes : LT_MAX_STAGES;
+  ring(room);
   const int sf_cols = mx ? 2 * 4 * (G + p.sfb) : 0;
   p.bufs = 2 * G * p.nt + sf_cols <= 512 ? 2 : 1;
   p.sf_col = p.bufs * G * p.nt;
@@ -500,6 +589,7 @@ double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, lt_params* out) {
   const auto larger = [](double x, double y) { return x > y ? x : y; };
   double best = full * larger(tile_us, sms * per_tile_hbm) + (left ? larger(tile_us, left * per_tile_hbm) : 0.);
   p.by_tile = 1;
+  p.cluster = 1;
   p.grid = tiles < sms ? (int)tiles : sms;
   for (int s = 2; s <= LT_MAX_SPLIT && s <= p.ks; s = s < 4 ? s + 1 : 2 * s) {
     if (s > 4 && G * p.nt > 64) break;                     // (their partials do not fit the ring at once)
@@ -509,14 +599,68 @@ double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, lt_params* out) {
     if (cost < best) { best = cost; p.by_tile = 0; p.grid = grid; }
     if (grid == sms) break;
   }
+  // Few tiles: a cluster for each, whose CTAs hand their sums over through shared memory: 1.2 us and 0.01 for each column.
+  for (int i = 0; i < 3 && clusters; ++i) {
+    const int c = 2 << i;
+    if (2 * c > p.boxes || tiles > clusters[i]) continue;  // (a stage for every CTA)
+    const int slots = (p.nt / 8 + c - 1) / c, bytes = c * slots * G * 8 * LT_M * 4;
+    if (bytes > 64 * 1024) continue;                       // (the ring needs the rest)
+    const double cost = larger(tile_us / c, larger(hbm_us, hbm_us * 60 / (tiles * c))) + 1.2 + 0.01 * G * p.nt;
+    if (cost < best) {
+      best = cost;
+      p.cluster = c;
+      p.slots = slots;
+      p.exchange = bytes;
+      p.by_tile = 0;
+      p.grid = (int)tiles * c;
+    }
+  }
+  if (p.cluster > 1) ring(room - p.exchange);
   if (out) *out = p;
   return best + 4.9 + 0.01 * G * p.nt;
+}
+
+typedef void (*lt_kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const lt_params, const lin_args, float*,
+                          int32_t*, int32_t*);
+static lt_kernel lt_pick(bool mx, bool gated) {
+  return mx ? (gated ? k_linear_tc<true, true> : k_linear_tc<true, false>)
+            : (gated ? k_linear_tc<false, true> : k_linear_tc<false, false>);
+}
+// How many clusters of 2, 4 and 8 CTAs (one to an SM) run at a time; asked once for each context.
+static int lt_clusters(jk_ctx* ctx) {
+  if (ctx->lin_clusters[0]) return JK_OK;
+  const lt_kernel kernel = lt_pick(false, false);
+  JK_CUDA_CHECK(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LT_SMEM));
+  for (int i = 2; i >= 0; --i) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(8 * (LT_MAX_CTAS / 8));
+    cfg.blockDim = dim3(LT_THREADS);
+    cfg.dynamicSmemBytes = LT_SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2 << i;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    JK_CUDA_CHECK(ctx, cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
+    ctx->lin_clusters[i] = n > 0 ? n : 1;
+  }
+  return JK_OK;
+}
+// The costs of the two kernels (us): is this one's the lower?
+int jk_linear_tc_pays(jk_ctx* ctx, const lin_args& a, bool mx, bool* pays) {
+  const int rc = lt_clusters(ctx);
+  if (rc != JK_OK) return rc;
+  const int sms = ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS;
+  *pays = jk_linear_tc_plan(a, mx, sms, ctx->lin_clusters, nullptr) <= jk_linear_pair_plan(a, mx, sms, nullptr);
+  return JK_OK;
 }
 
 int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   const int G = a.w_up ? 2 : 1, es = mx ? 1 : 2, box_el = LT_BOX / es;
   lt_params p;
-  jk_linear_tc_plan(a, mx, ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS, &p);
+  jk_linear_tc_plan(a, mx, ctx->sm_count < LT_MAX_CTAS ? ctx->sm_count : LT_MAX_CTAS, ctx->lin_clusters, &p);
   CUtensorMap mw, mu, mx_;
   auto map = [&](CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t stride, uint32_t box_rows) {
     const uint64_t dims[2] = {(uint64_t)a.n_in, rows}, str[1] = {stride * es};
@@ -527,18 +671,21 @@ int jk_linear_tc(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   if (rc == JK_OK) rc = map(&mu, a.w_up ? a.w_up : a.w, a.n_out, a.n_in, LT_M);
   if (rc == JK_OK) rc = map(&mx_, a.x, a.rows, a.x_stride, p.nt);
   if (rc != JK_OK) return rc;
-  auto kernel = mx ? (G == 2 ? k_linear_tc<true, true> : k_linear_tc<true, false>)
-                   : (G == 2 ? k_linear_tc<false, true> : k_linear_tc<false, false>);
+  const lt_kernel kernel = lt_pick(mx, G == 2);
   const int bit = 1 << (2 * mx + G - 1);
   if (!(ctx->lin_smem_set & bit)) {
     JK_CUDA_CHECK(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LT_SMEM));
     ctx->lin_smem_set |= bit;
   }
-  const size_t smem = (size_t)p.stages * p.stage_bytes + sizeof(lt_tail) + 1024;
+  const size_t smem = (size_t)p.stages * p.stage_bytes + p.exchange + sizeof(lt_tail) + 1024;
   JK_PROF(ctx, st, JK_ST_LINEAR);
-  jk_launch_pdl(kernel, dim3(p.grid), dim3(LT_THREADS), smem, st, mw, mu, mx_, p, a,
-                (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
-                (int32_t*)(ctx->ws + ctx->lay.status));
+  float* part = (float*)(ctx->ws + ctx->lay.lin_part);
+  int32_t* flags = (int32_t*)(ctx->ws + ctx->lay.lin_flag);
+  int32_t* status = (int32_t*)(ctx->ws + ctx->lay.status);
+  if (p.cluster > 1)
+    jk_launch_pdl_cluster(kernel, dim3(p.grid), dim3(LT_THREADS), p.cluster, smem, st, mw, mu, mx_, p, a, part, flags, status);
+  else
+    jk_launch_pdl(kernel, dim3(p.grid), dim3(LT_THREADS), smem, st, mw, mu, mx_, p, a, part, flags, status);
   JK_LAUNCH_CHECK(ctx);
   return JK_OK;
 }
