@@ -566,9 +566,9 @@ double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, const int* cluster
   p.b_box = p.nt * LT_BOX;
   p.sfb = mx ? (p.nt + 127) / 128 : 0;
   const int box_bytes = G * p.a_box + p.b_box + (mx ? (G + p.sfb) * MX_TILE_BYTES : 0);
-  // The ring: stages of two boxes while four of them fit.
+  // The ring: stages of two boxes while four of them fit (8-bit rows, which bring scales with every stage: three).
   auto ring = [&](int room) {
-    p.kb = room / (2 * box_bytes) >= 4 && p.boxes > 1 ? 2 : 1;
+    p.kb = room / (2 * box_bytes) >= (mx ? 3 : 4) && p.boxes > 1 ? 2 : 1;
     p.ks = (p.boxes + p.kb - 1) / p.kb;
     p.stage_bytes = (int)jk_align_up((size_t)p.kb * box_bytes, 1024);
     p.stages = room / p.stage_bytes < LT_MAX_STAGES ? room / p.stage_bytes : LT_MAX_STAGES;
