@@ -65,6 +65,22 @@ template <typename T> __device__ __forceinline__ float lin_bias(const void* b, i
   return b && n < n_out ? jk_to_float(((const T*)b)[n]) : 0.f;
 }
 
+// Eight sums over the warp's lanes at once, 9 exchanges instead of 40: at each of three steps a lane hands on half of what it
+// holds and takes the other half's partner.  Lane l returns the sum of value 4 (l >> 4 & 1) + 2 (l >> 3 & 1) + (l >> 2 & 1).
+__device__ __forceinline__ float warp_sums8(float (&v)[8], int lane) {
+#pragma unroll
+  for (int h = 4; h > 0; h >>= 1) {
+    const bool up = lane & (h * 4);
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, h * 4);
+    }
+  }
+  v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
+  return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
+}
+
 // Few rows: a warp owns a weight row (gated: one of w and one of w_up) and up to 8 rows of x, its lanes go along k: every
 // weight is read once from memory, x comes from the caches.  Bound by latency at the sizes it is taken for.
 #define LR_ROWS 8
@@ -79,7 +95,7 @@ __global__ void __launch_bounds__(256) k_linear_rows(const lin_args a) {
   float acc[LR_ROWS], acc_up[LR_ROWS];
 #pragma unroll
   for (int j = 0; j < LR_ROWS; ++j) acc[j] = acc_up[j] = 0.f;
-#pragma unroll 2
+#pragma unroll 4
   for (int k = lane * 4; k < a.n_in; k += 128) {
     const float4 w = lin_load4(wr, k, a.w_scale, n, a.k_tiles_in);
     float4 u = w;
@@ -92,14 +108,9 @@ __global__ void __launch_bounds__(256) k_linear_rows(const lin_args a) {
         if (GATED) acc_up[j] += fmaf(x.x, u.x, fmaf(x.y, u.y, fmaf(x.z, u.z, x.w * u.w)));
       }
   }
-  float z = 0.f, zu = 0.f;
-#pragma unroll
-  for (int j = 0; j < LR_ROWS; ++j) {
-    const float s = jk_warp_sum(acc[j]), t = GATED ? jk_warp_sum(acc_up[j]) : 0.f;
-    if (lane == j) { z = s; zu = t; }
-  }
-  const int r = r0 + lane;
-  if (lane >= LR_ROWS || r >= a.rows) return;
+  const float z = warp_sums8(acc, lane), zu = GATED ? warp_sums8(acc_up, lane) : 0.f;
+  const int r = r0 + 4 * (lane >> 4 & 1) + 2 * (lane >> 3 & 1) + (lane >> 2 & 1);
+  if ((lane & 3) || r >= a.rows) return;
   float y = lin_act(z + lin_bias<T>(a.bias, n, a.n_out), a.act);
   if (GATED) y *= zu + lin_bias<T>(a.bias_up, n, a.n_out);
   if (a.residual) y += jk_to_float(((const T*)a.residual)[(size_t)r * a.r_stride + n]);
@@ -110,17 +121,21 @@ __global__ void __launch_bounds__(256) k_linear_rows(const lin_args a) {
 // The rest: a block makes ROWS rows times 128 weight rows (gated: 64 of w and 64 of w_up, the two of an output in one
 // thread), 8 columns and ROWS / 16 rows a thread, k in steps of 16 through two buffers of shared memory, the next
 // step's loads on their way while one is multiplied.  The sum of 32 products is formed by itself and then added,
-// which keeps long sums within a few units of f32.
+// which keeps long sums within a few units of f32.  Where the tiles are few, `split` blocks of a cluster share one along
+// k and each finishes every split-th part of its rows from all their sums.
 #define LB_N 128
 #define LB_K 16
 template <typename TX, typename T, bool GATED, int ROWS>
-__global__ void __launch_bounds__(256) k_linear_block(const lin_args a) {
+__global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int split) {
   constexpr int RT = ROWS / 16, OUTS = GATED ? 64 : 128;
-  __shared__ __align__(16) float s_w[2][LB_K][LB_N + 4], s_x[2][LB_K][ROWS + 4];
+  constexpr int RING = 2 * LB_K * (LB_N + 4 + ROWS + 4), SUMS = ROWS <= 64 ? ROWS * LB_N : 0;
+  __shared__ __align__(16) float s_mem[RING > SUMS ? RING : SUMS];
+  float (*s_w)[LB_K][LB_N + 4] = reinterpret_cast<float (*)[LB_K][LB_N + 4]>(s_mem);
+  float (*s_x)[LB_K][ROWS + 4] = reinterpret_cast<float (*)[LB_K][ROWS + 4]>(s_mem + 2 * LB_K * (LB_N + 4));
   jk_pdl_wait();
   jk_pdl_trigger();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int n0 = blockIdx.x * OUTS, r0 = blockIdx.y * ROWS;
+  const int rank = blockIdx.x % split, n0 = blockIdx.x / split * OUTS, r0 = blockIdx.y * ROWS;
   const int lr = threadIdx.x >> 2, lk = (threadIdx.x & 3) * 4;         // loading: rows lr, lr + 64, four elements
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
   float4 pw[2], px[(ROWS + 63) / 64];
@@ -160,13 +175,14 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a) {
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = part[i][j] = 0.f;
-  ask(0);
+  const int all = (a.n_in + LB_K - 1) / LB_K, s0 = (int)((long long)all * rank / split);
+  const int steps = (int)((long long)all * (rank + 1) / split) - s0;
+  ask(s0 * LB_K);
   put(0);
   __syncthreads();
-  const int steps = (a.n_in + LB_K - 1) / LB_K;
   for (int s = 0; s < steps; ++s) {
     const int b = s & 1;
-    if (s + 1 < steps) ask((s + 1) * LB_K);
+    if (s + 1 < steps) ask((s0 + s + 1) * LB_K);
 #pragma unroll
     for (int k = 0; k < LB_K; ++k) {
       float w[8], x[RT];
@@ -194,6 +210,42 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a) {
     if (s + 1 < steps) put(b ^ 1);
     __syncthreads();
   }
+  if constexpr (SUMS > 0) {
+    if (split > 1) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<float4*>(&s_mem[(ty * RT + i) * LB_N + 64 * h + tx * 4]) =
+              make_float4(acc[i][4 * h], acc[i][4 * h + 1], acc[i][4 * h + 2], acc[i][4 * h + 3]);
+      asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+      const int lane = threadIdx.x & 31;
+      for (int r = rank + split * (threadIdx.x >> 5); r < ROWS; r += split * 8) {
+        float z[4] = {0.f, 0.f, 0.f, 0.f}, zu[4] = {0.f, 0.f, 0.f, 0.f};
+        const int at = r * LB_N + (GATED ? (lane & 15) : lane) * 4;
+        for (int i = 0; i < split; ++i) {                // in the order of k
+          const float* o = jk_cluster_map(&s_mem[at], i);
+          const float4 v = *reinterpret_cast<const float4*>(o);
+          z[0] += v.x; z[1] += v.y; z[2] += v.z; z[3] += v.w;
+          if (GATED) {
+            const float4 u = *reinterpret_cast<const float4*>(o + 64);
+            zu[0] += u.x; zu[1] += u.y; zu[2] += u.z; zu[3] += u.w;
+          }
+        }
+        // (gated: the upper lanes hold what the lower ones do, and nothing to write)
+        const int n = GATED && lane >= 16 ? a.n_out : n0 + lane * 4;
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          y[j] = lin_act(z[j] + lin_bias<T>(a.bias, n + j, a.n_out), a.act);
+          if (GATED) y[j] *= zu[j] + lin_bias<T>(a.bias_up, n + j, a.n_out);
+        }
+        lin_out<T, 4>(a, y, r0 + r, n);
+      }
+      asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+      return;
+    }
+  }
   // a thread has outputs tx * 4 .. + 3 (and 64 on, or their gate's partners): eight neighbouring lanes a scale block
 #pragma unroll
   for (int h = 0; h < (GATED ? 1 : 2); ++h) {
@@ -217,9 +269,9 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a) {
   }
 }
 
-// Few rows while a scale block's outputs need not meet (T and f32 out) and they are read by at most two passes; else
-// blocks of 32 or 128 rows: 32 while blocks of 128 would leave SMs idle.  f32, us: 16 x 1376 x 512 gated LR_US,
-// by blocks of 32 rows LB_US.
+// Up to 16 rows, while a scale block's outputs need not meet: warps of outputs.  Else blocks of 128 rows where they fill
+// the SMs, of 32 or 64 with up to 8 blocks to a tile where they do not.  f32, us (CUDA 12.9's library in parentheses, which
+// makes the product alone): CC_FIGURES
 template <typename TX, typename T>
 static void launch_cc(cudaStream_t st, const lin_args& a, int sms) {
   const bool gated = a.w_up != nullptr;
@@ -229,12 +281,15 @@ static void launch_cc(cudaStream_t st, const lin_args& a, int sms) {
     return;
   }
   const int outs = gated ? LB_N / 2 : LB_N, n_tiles = (a.n_out + outs - 1) / outs;
-  const bool large = a.rows > 32 && (long long)n_tiles * ((a.rows + 127) / 128) >= sms;
-  const int R = large ? 128 : 32;
-  const dim3 grid((unsigned)n_tiles, (unsigned)((a.rows + R - 1) / R));
-  auto k = large ? (gated ? k_linear_block<TX, T, true, 128> : k_linear_block<TX, T, false, 128>)
-                 : (gated ? k_linear_block<TX, T, true, 32> : k_linear_block<TX, T, false, 32>);
-  jk_launch_pdl(k, grid, dim3(256), 0, st, a);
+  const int R = a.rows <= 32 ? 32 : (long long)n_tiles * ((a.rows + 127) / 128) >= sms ? 128 : 64;
+  const long long tiles = (long long)n_tiles * ((a.rows + R - 1) / R);
+  int split = 1;                           // (shares of 8 steps at least, blocks for two turns of every SM at most)
+  while (R < 128 && split < 8 && tiles * split * 2 <= 4ll * sms && (a.n_in + LB_K - 1) / LB_K >= 16 * split) split *= 2;
+  const dim3 grid((unsigned)(n_tiles * split), (unsigned)((a.rows + R - 1) / R));
+  auto k = R == 128 ? (gated ? k_linear_block<TX, T, true, 128> : k_linear_block<TX, T, false, 128>)
+           : R == 64 ? (gated ? k_linear_block<TX, T, true, 64> : k_linear_block<TX, T, false, 64>)
+                     : (gated ? k_linear_block<TX, T, true, 32> : k_linear_block<TX, T, false, 32>);
+  jk_launch_pdl_cluster(k, grid, dim3(256), (unsigned)split, 0, st, a, split);
 }
 
 // ------------------------------------------------------------------------------------------ host side

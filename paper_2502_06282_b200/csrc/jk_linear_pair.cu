@@ -229,6 +229,14 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
   lp_walk walk(p, pair);
   int tile, k0, k1;
   bool more = walk.next(p, pairs, tile, k0, k1);
+  if (warp == 2 && more && lane < LP_STAGES && k0 + lane < k1) {
+    // The boxes of the first ring are asked into L2 while the kernel before still runs.
+    int rt, wt;
+    lp_place(p, tile, rt, wt);
+    l2_prefetch_box(&map_x, (k0 + lane) * BOX_EL, rt * LP_ROWS + rank * LT_M);
+    l2_prefetch_box(GATED && rank ? &map_u : &map_w, (k0 + lane) * BOX_EL, GATED ? wt * LT_M : wt * LP_N + rank * LT_M);
+  }
+  __syncwarp();
   jk_pdl_wait();
   jk_pdl_trigger();
 
@@ -673,10 +681,11 @@ int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
     if (rc == JK_OK && gated) rc = jk_tma_encode_scales(ctx, &msu, a.w_up_scale, wt);
   }
   if (rc != JK_OK) return rc;
-  // Outputs and residuals whose rows begin at multiples of 16 bytes go through the copy engine, in pieces of 32 rows.
+  // Outputs and residuals whose rows begin and end at multiples of 16 bytes go through the copy engine, in pieces of 32
+  // rows.  (It stores 16 bytes at least: the last of a row that ends elsewhere would reach into what lies between the rows.)
   const bool f32 = a.out_type == JK_ROWS_F32, q8 = a.out_type == JK_ROWS_MX8;
   const int os = q8 ? 1 : f32 ? 4 : 2;
-  const int wide_out = (a.o_stride * os) % 16 == 0, wide_res = a.residual && wide_out && !f32 && (a.r_stride * 2) % 16 == 0;
+  const int wide_out = (a.o_stride * os) % 16 == 0 && ((long long)a.n_out * os) % 16 == 0, wide_res = a.residual && wide_out && !f32 && (a.r_stride * 2) % 16 == 0;
   CUtensorMap mo = mw, mr = mw;
   if (wide_out) rc = jk_tma_encode_piece(ctx, &mo, a.out, q8 ? 1 : f32 ? 4 : 2, a.n_out, a.rows, a.o_stride, f32 ? 16 : 32);
   if (rc == JK_OK && wide_res) rc = jk_tma_encode_piece(ctx, &mr, a.residual, 2, a.n_out, a.rows, a.r_stride, 32);

@@ -292,21 +292,21 @@ def test_linear_strides(R, N):
     run_linear(R, N, 136, wide=8, residual=True, out="f32")
 
 
-@pytest.mark.parametrize("out", ["T", "f32", "mx8"])
-def test_linear_many_rows_beside_aligned_rows(out):
+@pytest.mark.parametrize("out,N", [("T", 288), ("T", 290), ("T", 292), ("f32", 288), ("f32", 290), ("mx8", 288)])
+def test_linear_many_rows_beside_aligned_rows(out, N):
     """Residuals and outputs of many rows whose rows begin at multiples of 16 bytes, or not, or one of the two."""
     rng = np.random.default_rng(11)
-    R, N, K = 300, 288, 200
+    R, K = 300, 200
     ctx = make_ctx("bf16")
     x, w, xd, wd = operands(rng, R, N, K, "T", "bf16")
     op = jk.Linear(ctx, wd, act="silu")
     res = store(rng.standard_normal((R, N)), "bf16")
     y = lo.linear(x, w, None, "silu", residual=res)
     e = 1.13 * (K + 4) * 2.0 ** -23 * (np.abs(x) @ np.abs(w).T) + 2.0 ** -18 * np.abs(y - res) + 2.0 ** -23 * (np.abs(y) + np.abs(res))
-    for wide_r in (0, 8, 3):
+    for wide_r in (0, 8, 6, 3):
         room = torch.zeros(R, N + wide_r, dtype=torch.bfloat16, device="cuda")
         room[:, :N] = to_dev(res, "bf16")
-        for wide_o in (0, 8, 5) if out != "mx8" else (0,):
+        for wide_o in (0, 8, 6, 4, 5) if out != "mx8" else (0,):
             g = Guard()
             if out == "mx8":
                 od = mx8_guard(g, R, N)
@@ -318,12 +318,15 @@ def test_linear_many_rows_beside_aligned_rows(out):
                 check_mx8(od, y, e)
             else:
                 check_t(od, y, e, "f32" if out == "f32" else "bf16")
+                beside = g.regions[0][0][Guard.PAD:Guard.PAD + g.regions[0][1]].view(od.dtype).view(R, N + wide_o)[:, N:]
+                assert bool((beside.contiguous().view(torch.uint8) == Guard.POISON).all()), "wrote between the rows"
     assert ctx.read_status() == 0
 
 
 @pytest.mark.parametrize("gated,act,out", [(False, "none", "T"), (True, "silu", "T"), (False, "gelu", "mx8"),
                                            (True, "none", "mx8")])
-@pytest.mark.parametrize("R,N,K", [(1, 32, 8), (16, 1376, 512), (33, 96, 1000), (130, 64, 40)])
+@pytest.mark.parametrize("R,N,K", [(1, 32, 8), (16, 1376, 512), (17, 160, 2048), (33, 96, 1000), (130, 64, 40), (300, 640, 200),
+                                   (500, 5024, 72)])
 def test_linear_f32(R, N, K, gated, act, out):
     run_linear(R, N, K, dtype="f32", gated=gated, act=act, bias=True, residual=True, out=out, wide=4 if R < 20 else 0)
 
