@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
             lp_add(v, (const uint16_t*)a.residual + (size_t)(row0 + lane) * a.r_stride + nw, most_w);
           if constexpr (OUT8) {
 #pragma unroll
-            for (int j = 0; j < LP_W; ++j) top = fmaxf(top, paged_mag(v[j]));
+            for (int j = 0; j < LP_W; ++j) top = fmaxf(top, fabsf(v[j]));          // (leaves NaN out)
 #pragma unroll
             for (int j = 0; j < LP_W / 4; ++j)
               *reinterpret_cast<float4*>(mine + lp_at128(lane, i / 4 + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
@@ -557,6 +557,14 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
         __syncwarp();
         if (!out_live) continue;
         if constexpr (OUT8) {              // n_out is a multiple of 32: all of the block or nothing
+          if (top > 3.402823466e38f) {     // an infinity does not count for the scale
+            top = 0.f;
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+              const float4 y = *reinterpret_cast<const float4*>(mine + lp_at128(lane, j));
+              top = fmaxf(fmaxf(fmaxf(top, paged_mag(y.x)), fmaxf(paged_mag(y.y), paged_mag(y.z))), paged_mag(y.w));
+            }
+          }
           const int e = paged_scale_exp(top);
           const float inv = paged_pow2(-e);
 #pragma unroll

@@ -13,6 +13,10 @@
 template <typename T> struct piece;
 template <> struct piece<__nv_bfloat16> {
   uint4 r;
+  __device__ __forceinline__ void fill(bool one) {
+    const uint32_t w = one ? 0x3f803f80u : 0x80008000u;
+    r = make_uint4(w, w, w, w);
+  }
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { r = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ float at(int i) const {
     const uint32_t w = i < 2 ? r.x : i < 4 ? r.y : i < 6 ? r.z : r.w;
@@ -31,6 +35,10 @@ template <> struct piece<__nv_bfloat16> {
 };
 template <> struct piece<float> {
   float4 a, b;
+  __device__ __forceinline__ void fill(bool one) {
+    const float w = one ? 1.f : -0.f;
+    a = b = make_float4(w, w, w, w);
+  }
   __device__ __forceinline__ void load(const float* p) {
     a = reinterpret_cast<const float4*>(p)[0];
     b = reinterpret_cast<const float4*>(p)[1];
@@ -47,9 +55,14 @@ template <> struct piece<float> {
 // A piece's 8 codes and, by the first of the four lanes that share the block, its scale byte.
 // Every lane of the warp calls it (dead lanes with zeros).
 __device__ __forceinline__ void mx_store_piece(const float (&v)[8], bool live, uint8_t* codes, uint8_t* scale) {
-  float amax = 0.f;
+  float amax = 0.f;                        // (a maximum leaves NaN out by itself; infinities are rare)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) amax = fmaxf(amax, paged_mag(v[i]));
+  for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(v[i]));
+  if (__any_sync(0xffffffffu, amax > 3.402823466e38f)) {
+    amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, paged_mag(v[i]));
+  }
   amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
   amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
   if (!live) return;
@@ -68,6 +81,14 @@ __device__ __forceinline__ void mx_store_piece(const float (&v)[8], bool live, u
 // on their way, and the weights stay in registers.
 template <typename T, int P> struct norm_row {
   piece<T> a[P], b[P];
+  // (pieces past the row, and a delta that is not given, stay -0, which leaves every x what it is)
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      a[p].fill(false);
+      b[p].fill(false);
+    }
+  }
   __device__ __forceinline__ void ask(const T* x, const T* delta, size_t at, int n, int step) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -89,6 +110,9 @@ __global__ void __launch_bounds__(AHEAD ? 512 : 1024, AHEAD && P < 4 ? 2 : 1) k_
   const int step = blockDim.x * 8, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   norm_row<T, P> next;
   piece<T> w[P];
+  next.clear();
+#pragma unroll
+  for (int p = 0; p < P; ++p) w[p].fill(true);
   if (AHEAD) {
     next.ask(x, delta, (size_t)blockIdx.x * n, n, step);
 #pragma unroll
@@ -104,10 +128,8 @@ __global__ void __launch_bounds__(AHEAD ? 512 : 1024, AHEAD && P < 4 ? 2 : 1) k_
     float s[P][8];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const bool live = (int)threadIdx.x * 8 + p * step < n;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        s[p][i] = live ? (delta ? next.a[p].at(i) + next.b[p].at(i) : next.a[p].at(i)) : 0.f;
+      for (int i = 0; i < 8; ++i) s[p][i] = next.a[p].at(i) + next.b[p].at(i);
     }
     if (AHEAD && row + (int)gridDim.x < rows) next.ask(x, delta, at + (size_t)gridDim.x * n, n, step);
     float sq = 0.f;
@@ -136,10 +158,7 @@ __global__ void __launch_bounds__(AHEAD ? 512 : 1024, AHEAD && P < 4 ? 2 : 1) k_
       const bool live = c < n;
       if (!AHEAD && weight && live) w[p].load(weight + c);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        s[p][i] *= r;
-        if (weight && live) s[p][i] *= w[p].at(i);
-      }
+      for (int i = 0; i < 8; ++i) s[p][i] = s[p][i] * r * w[p].at(i);
       if (out && live) piece<T>::store(out + at + c, s[p]);
       if (codes) mx_store_piece(s[p], live, codes + at + c, scales + mx_scale_at(row, c >> 5, k_tiles));
     }
