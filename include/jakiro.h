@@ -621,8 +621,10 @@ typedef struct {
  * n_in is a multiple of 8 (T) or 32 (mx8) up to 131072, n_out any number up to 2^20, rows up to
  * 2^20; rows of x are 16-byte aligned.  Products are exact and summed in f32 (f32 contexts: f32
  * multiply-adds), the epilogue is f32, y is rounded once.  out may be residual itself (same
- * stride); any other overlap of out with an input is refused (JK_ERR_SHAPE).  bf16 contexts and mx8 operands run on
- * the tensor cores while the tensor path is on (mx8: in bf16 contexts).
+ * stride), or columns of one buffer of which x and residual are others; any overlap of out with an
+ * input is refused (JK_ERR_SHAPE).  bf16 contexts and mx8 operands run on the tensor cores while the
+ * tensor path is on (mx8: in bf16 contexts).  After JK_ERR_TIMEOUT in the status, set the workspace
+ * again before the next call.
  */
 int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* host_op, int32_t rows, const void* x,
               const uint8_t* x_scale, int64_t x_stride, const void* residual, int64_t residual_stride,
@@ -645,7 +647,7 @@ int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* host_op, int32_t ro
  *                or a negative position sets JK_ERR_BOUNDS, and that sequence's K and V (that
  *                token) are not written.
  * n_tokens up to 2^20, not bound to max_tree; batch up to 65535, not bound to max_batch.  Outputs
- * must not overlap qkv (JK_ERR_SHAPE).
+ * must not overlap qkv (JK_ERR_SHAPE), nor one another.
  */
 int jk_rope_qkv(jk_ctx* ctx, void* stream, int32_t batch, int32_t n_tokens, const void* qkv,
                 int64_t row_stride, const int32_t* pos, int32_t n_axes, const int32_t* host_sections,

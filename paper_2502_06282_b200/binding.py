@@ -557,7 +557,7 @@ class Context:
         width = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
         if qkv.dtype is not T or qkv.shape[-1] != width or qkv.numel() != n * width or qkv.stride(-1) != 1:
             raise ValueError(f"qkv: expected a {T} tensor [batch, n_tokens, {width}]")
-        if qkv.is_contiguous():
+        if n == 1 or qkv.is_contiguous():
             stride = width
         else:
             stride = qkv.stride(-2) if n_tokens > 1 or qkv.dim() == 2 else qkv.stride(0)
@@ -569,8 +569,9 @@ class Context:
             raise ValueError(f"pos: expected {axes} positions for each token")
         if q_out.dtype is not T or q_out.numel() != n * c.n_q_heads * c.head_dim or not q_out.is_contiguous():
             raise ValueError(f"q_out: expected a contiguous {T} tensor [batch, n_tokens, {c.n_q_heads}, {c.head_dim}]")
-        if not (qkv.is_cuda and pos.is_cuda and q_out.is_cuda and k_out.is_cuda and v_out.is_cuda):
-            raise ValueError("qkv, pos and the outputs must be on a CUDA device")
+        if not (qkv.is_cuda and pos.is_cuda and q_out.is_cuda and k_out.is_cuda and v_out.is_cuda
+                and (first_row is None or first_row.is_cuda)):
+            raise ValueError("qkv, pos, first_row and the outputs must be on a CUDA device")
         s = self._tree_arrays(k_out, v_out, batch, n_tokens)
         host = _SECTIONS.get(sections)
         if host is None:

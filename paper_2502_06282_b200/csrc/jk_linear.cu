@@ -326,11 +326,14 @@ extern "C" int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* op, int3
   const size_t in_b[] = {((size_t)(rows - 1) * x_stride + K) * xs, sc_x, (size_t)(N * K) * xs, sc_w, (size_t)N * es,
                          (size_t)(N * K) * xs, sc_w, (size_t)N * es,
                          ((size_t)(rows - 1) * residual_stride + N) * es};
+  const size_t row_b[] = {(size_t)K * xs, (size_t)N * es}, apart[] = {(size_t)x_stride * xs, (size_t)residual_stride * es};
   const size_t out_b = ((size_t)(rows - 1) * out_stride + N) * os;
   const size_t sc_o = out_type == JK_ROWS_MX8 ? jk_row_scale_bytes(rows, N) : 0;
   for (int i = 0; i < 9; ++i) {
     const bool in_place = i == 8 && out == residual && os == es && out_stride == residual_stride;
-    if ((jk_overlap(out, out_b, in[i], in_b[i]) && !in_place) || (sc_o && jk_overlap(out_scale, sc_o, in[i], in_b[i])))
+    const bool written = i == 0 || i == 8 ? jk_rows_overlap(out, rows, N * os, out_stride * os, in[i], rows, row_b[i / 8], apart[i / 8])
+                                          : jk_overlap(out, out_b, in[i], in_b[i]);
+    if ((written && !in_place) || (sc_o && jk_overlap(out_scale, sc_o, in[i], in_b[i])))
       return JK_ERR_SHAPE;
   }
   if (sc_o && jk_overlap(out, out_b, out_scale, sc_o)) return JK_ERR_SHAPE;

@@ -18,3 +18,14 @@ static inline bool jk_overlap(const void* a, size_t na, const void* b, size_t nb
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return a && b && x < y + nb && y < x + na;
 }
+
+// The same for rows of wa and wb bytes, each sa and sb bytes behind the last: rows of one stride may lie between one
+// another, as the columns of one buffer do.
+static inline bool jk_rows_overlap(const void* a, size_t rows_a, size_t wa, size_t sa, const void* b, size_t rows_b,
+                                   size_t wb, size_t sb) {
+  if (!jk_overlap(a, (rows_a - 1) * sa + wa, b, (rows_b - 1) * sb + wb)) return false;
+  if (sa != sb) return true;
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  const size_t off = y >= x ? (y - x) % sa : (sa - (x - y) % sa) % sa;      // columns from a's first to b's first
+  return off < wa || off + wb > sa;
+}

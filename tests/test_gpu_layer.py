@@ -338,6 +338,116 @@ def test_linear_cuda_cores(kind, dtype, tensor):
     run_linear(37, 160, 352, kind, dtype=dtype, out="mx8", residual=True, tensor=tensor)
 
 
+def torch_mx8(x):
+    """x [rows, n] f32 on the device -> (Mx8, the values it stands for), the exponent by frexp."""
+    R, n = x.shape
+    b = x.view(R, n // 32, 32)
+    m, e = torch.frexp(b.abs().amax(2))
+    e = torch.where(m > 0.875, e - 8, e - 9).clamp(min=-32)
+    codes = (b * torch.exp2(-e.float())[..., None]).view(R, n).to(torch.float8_e4m3fn)
+    full = torch.full((-(-R // 128) * 128, -(-n // 128) * 4), 255, dtype=torch.uint8, device="cuda")
+    full[:R, :n // 32] = (e + 127).to(torch.uint8)
+    tiles = full.view(-1, 4, 32, full.shape[1] // 4, 4).permute(0, 3, 2, 1, 4).reshape(-1).contiguous()
+    return jk.Mx8(codes.view(torch.uint8), tiles), (codes.double().view(R, n // 32, 32) * torch.exp2(e.double())[..., None]).view(R, n)
+
+
+# Shapes that take each way a call can go: clusters of 8, 4 and 2 CTAs; even shares whose tiles span CTAs (with partials that
+# come in several rounds); more tiles than SMs; many rows with whole tiles, with tiles cut among 2, 3 and 4 pairs, alone and before
+# whole turns; widths that end inside a tile
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("R,N,K,gated", [
+    (60, 640, 4096, False), (60, 4096, 4096, False), (17, 5120, 4096, False), (128, 1376, 4096, True), (60, 2048, 4096, True),
+    (128, 11008, 8192, False), (250, 9000, 4096, False), (128, 11008, 2048, True), (1, 32000, 1024, False), (5, 20001, 512, True),
+    (300, 2048, 8192, False), (300, 1300, 4096, True), (2047, 5120, 1024, False), (1500, 2500, 4096, True), (700, 5119, 2048, False),
+    (257, 9000, 8192, False), (4099, 384, 256, True)])
+def test_linear_every_deal(R, N, K, gated, kind):
+    """Against torch's product in 64 bits, twice for the same bits."""
+    g = torch.Generator(device="cuda").manual_seed(R + N + K)
+    ctx = make_ctx("bf16")
+    make = lambda r, s: torch.randn(r, K, generator=g, device="cuda") * s
+    pack = torch_mx8 if kind == "mx8" else (lambda x: (x.bfloat16(), x.bfloat16().double()))
+    (xd, x), (wd, w) = pack(make(R, 1.0)), pack(make(N, 0.05))
+    (ud, u) = pack(make(N, 0.05)) if gated else (None, None)
+    res = torch.randn(R, N, generator=g, device="cuda").bfloat16()
+    op = jk.Linear(ctx, wd, act="silu" if gated else "none", w_up=ud)
+    outs = [torch.full((R, N), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for o in outs:
+        ctx.linear(op, xd, o, residual=res)
+    assert ctx.read_status() == 0
+    assert torch.equal(*outs)
+    z = x @ w.T
+    ez = (K + 4) * 2.0 ** -23 * (x.abs() @ w.abs().T)
+    if gated:
+        a, zu = z * torch.sigmoid(z), x @ u.T
+        eu = (K + 4) * 2.0 ** -23 * (x.abs() @ u.abs().T)
+        y, e = a * zu, (1.13 * ez + 2.0 ** -18 * (a.abs() + 2.0 ** -20)) * zu.abs() + a.abs() * eu + 1.13 * ez * eu
+    else:
+        y, e = z, ez
+    y = y + res.double()
+    e = e + 2.0 ** -23 * (y.abs() + res.double().abs())
+    off = (outs[0].double() - y).abs()
+    assert bool((off <= HALF["bf16"] * (y.abs() + e) + e).all())
+
+
+def test_linear_two_contexts_at_once():
+    """Two contexts on two streams, each with calls that hand sums over between CTAs, against the same calls alone."""
+    rng = np.random.default_rng(12)
+    shapes = [(60, 11008, 2048, "T"), (60, 1000, 4096, "mx8"), (300, 2048, 4096, "T"), (128, 9000, 4096, "mx8")]
+    runs = []
+    for c in range(2):
+        ctx = make_ctx("bf16")
+        for R, N, K, kind in shapes:
+            g = torch.Generator(device="cuda").manual_seed(N + c)
+            pack = torch_mx8 if kind == "mx8" else (lambda x: (x.bfloat16(), None))
+            xd, wd = (pack(torch.randn(r, K, generator=g, device="cuda"))[0] for r in (R, N))
+            op, out = jk.Linear(ctx, wd), torch.zeros(R, N, dtype=torch.bfloat16, device="cuda")
+            ctx.linear(op, xd, out)
+            torch.cuda.synchronize()
+            runs.append((c, ctx, op, xd, out, out.clone()))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for c, ctx, op, xd, out, _ in runs:
+            with torch.cuda.stream(streams[c]):
+                ctx.linear(op, xd, out)
+    torch.cuda.synchronize()
+    for c, ctx, op, xd, out, want in runs:
+        assert torch.equal(out, want) and ctx.read_status() == 0
+
+
+def test_rows_far_apart():
+    """Offsets past 32 bits: rows 2^31 elements apart in x, residual and out; more than 2^32 elements in a norm."""
+    R, N, K, far = 2, 136, 64, 1 << 31
+    g = torch.Generator(device="cuda").manual_seed(3)
+    ctx = make_ctx("bf16")
+    x, w, res = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((R, K), (N, K), (R, N)))
+    op, want = jk.Linear(ctx, w), torch.empty(R, N, dtype=torch.bfloat16, device="cuda")
+    ctx.linear(op, x, want, residual=res)
+    room = torch.empty(far + 4096, dtype=torch.bfloat16, device="cuda")
+    at = lambda first, n: room[first:].as_strided((R, n), (far, 1), first)
+    at(0, K).copy_(x)
+    at(1024, N).copy_(res)
+    ctx.linear(op, at(0, K), at(2048, N), residual=at(1024, N))
+    assert torch.equal(at(2048, N), want)
+    m, far_m = jk.Mx8.empty(R, K), jk.Mx8.empty(R, K)
+    ctx.quantize_mx8(x, m)
+    ctx.quantize_mx8(at(0, K), far_m)
+    assert torch.equal(m.codes, far_m.codes)
+    del room
+    rows, n = (1 << 17) + 3, 32768
+    big = torch.empty(rows, n, dtype=torch.bfloat16, device="cuda")
+    big[:2].normal_(generator=g)
+    big[2:-2].zero_()
+    big[-2:].normal_(generator=g)
+    few = torch.cat([big[:2], big[-2:]])
+    out, out8 = torch.empty_like(few), jk.Mx8.empty(4, n)
+    ctx.add_norm(few, out=out, out_mx8=out8)
+    codes = jk.Mx8.empty(rows, n)
+    ctx.add_norm(big, out=big, out_mx8=codes)
+    assert torch.equal(big[-2:], out[2:]) and torch.equal(big[:2], out[:2]) and not bool(big[rows // 2].any())
+    assert torch.equal(codes.codes[-2:], out8.codes[2:])
+    assert ctx.read_status() == 0
+
+
 @pytest.mark.parametrize("kind", ["T", "mx8"])
 def test_linear_nan_and_infinities_stay_in_their_row(kind):
     """A row of x with a NaN, and one with the type's largest value, reach no other row; padding reaches none."""

@@ -84,6 +84,17 @@ def test_linear_refuses(lib, change, code):
     assert rc == E[code]
 
 
+@pytest.mark.parametrize("off,code", [(128, "WORKSPACE"), (112, "SHAPE"), (384, "WORKSPACE"), (400, "SHAPE"), (-128, "WORKSPACE"),
+                                      (-112, "SHAPE"), (-384, "WORKSPACE"), (-400, "SHAPE"), (512 + 128, "WORKSPACE"),
+                                      (512, "SHAPE"), (3 * 512 + 112, "SHAPE"), (3 * 512 + 128, "WORKSPACE"), (4 * 512, "WORKSPACE")])
+@pytest.mark.parametrize("beside", ["x", "residual"])
+def test_linear_columns_of_one_buffer(lib, beside, off, code):
+    """Rows of 128 bytes, 512 apart: out may lie between the rows of x or of the residual, and may not reach into one."""
+    op, ctx = jk.JkLinearOp(*OP.values()), make_ctx()
+    x, res = (X, RES) if beside == "x" else (RES, X)
+    assert lib.jk_linear(ctx._h, None, C.byref(op), 4, x, None, 256, res, 256, X + off, 0, None, 256) == E[code]
+
+
 def test_linear_refuses_null_context_and_projection(lib):
     op, ctx = jk.JkLinearOp(*OP.values()), make_ctx()
     tail = (4, X, None, 0, None, 0, OUT, 0, None, 0)
