@@ -560,8 +560,9 @@ class Context:
         if n == 1 or qkv.is_contiguous():
             stride = width
         else:
-            stride = qkv.stride(-2) if n_tokens > 1 or qkv.dim() == 2 else qkv.stride(0)
-            if qkv.dim() > 3 or (qkv.dim() == 3 and batch > 1 and n_tokens > 1 and qkv.stride(0) != n_tokens * stride):
+            stride = qkv.stride(1) if qkv.dim() == 3 and n_tokens > 1 else qkv.stride(0)
+            if qkv.shape[:-1] not in ((n,), (batch, n_tokens)) or (
+                    qkv.dim() == 3 and batch > 1 and n_tokens > 1 and qkv.stride(0) != n_tokens * stride):
                 raise ValueError("qkv: its rows do not lie evenly apart")
         sections = tuple(sections)
         axes = len(sections)

@@ -32,15 +32,16 @@ int jk_tma_encode_piece(jk_ctx* ctx, CUtensorMap* out, const void* ptr, int es, 
 #define LP_N 256                          // weight rows of a pair's tile
 #define LP_BAND 8                         // tiles of x of a band
 #define LP_MAX_SPLIT 4                    // pairs that share a tile, at most
-#define LP_EPI_WARPS 8
 #define LP_W 16                           // columns that an epilogue warp works on at a time
-#define LP_THREADS (64 + 32 * LP_EPI_WARPS)
 #define LP_A_BYTES (LT_M * LT_BOX)        // of each operand in a box
 #define LP_SF_COL 488                     // 8-bit rows: first column of the scales, two sets of 12
 #define LP_ACC2_MX 232                    // 8-bit rows: first column of the second accumulator
-#define LP_MAX_STAGES 6
+#define LP_MAX_STAGES 7
+#define LP_MAX_EPI 16
 #define LP_PIECE 2048                     // an epilogue warp's piece of the output: 32 rows of 64 bytes; two of them
 #define LP_PIECE8 1024                    // ... of 8-bit outputs: 32 rows of 32; behind 32 x 32 f32
+#define LP_PART 2048                      // an epilogue warp's piece of a partial: 32 rows of LP_W columns, f32
+#define LP_MAX_PARTS 5
 #define LP_X_PITCH 34                     // the same memory as a 32 x 32 exchange: elements of a row
 
 struct lp_params {
@@ -56,16 +57,22 @@ struct __align__(16) lp_tail {
   uint64_t full[LP_MAX_STAGES], empty[LP_MAX_STAGES];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t shared_free;                   // the columns both accumulators use have been read
-  uint64_t res_full[LP_EPI_WARPS][2];     // a warp's piece of the residual
+  uint64_t res_full[LP_MAX_EPI][2];       // a warp's piece of the residual
+  uint64_t part_full[LP_MAX_EPI][LP_MAX_PARTS];      // ... its pieces of the partials
   uint32_t tmem_base;
   int abort_flag;
   unsigned seen;                          // epilogue warps that have seen all flags
 };
 
-template <bool MX, bool OUT8> struct lp_smem {
-  static constexpr int STAGE = 2 * LP_A_BYTES + (MX ? 2048 : 0), STAGES = MX || OUT8 ? 5 : 6;
+// LAST: a pair finishes at most one tile, and does so last.  The ring is free by then and holds the epilogue's pieces
+// and what it is handed; it has a stage more for that, and 16 warps, not 8, get the epilogue done, which nothing hides.
+template <bool MX, bool OUT8, bool LAST> struct lp_smem {
+  static constexpr int EPI = LAST ? 16 : 8, THREADS = 64 + 32 * EPI;
+  static constexpr int STAGE = 2 * LP_A_BYTES + (MX ? 2048 : 0), STAGES = (MX || (OUT8 && !LAST) ? 5 : 6) + LAST;
   static constexpr int WARP = 2 * LP_PIECE + (OUT8 ? 2 * LP_PIECE8 : 0);           // of an epilogue warp
-  static constexpr size_t BYTES = (size_t)STAGES * STAGE + LP_EPI_WARPS * WARP + sizeof(lp_tail) + 1024;
+  static constexpr int PARTS = (STAGES * STAGE / EPI - WARP) / LP_PART < LP_MAX_PARTS ? (STAGES * STAGE / EPI - WARP) / LP_PART : LP_MAX_PARTS;
+  static constexpr size_t BYTES = (size_t)STAGES * STAGE + (LAST ? 0 : EPI * WARP) + sizeof(lp_tail) + 1024;
+  static_assert(BYTES <= LT_SMEM && STAGES <= LP_MAX_STAGES && PARTS >= 1, "shared memory");
 };
 
 // ------------------------------------------------------------------------------------------ PTX
@@ -191,28 +198,29 @@ __device__ __forceinline__ uint32_t lp_at32(int r, int c) { return (uint32_t)(r 
 __device__ __forceinline__ uint32_t lp_at128(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
 
 // ------------------------------------------------------------------------------------------ the kernel
-template <bool MX, bool GATED, bool OUT8>
-__global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
+template <bool MX, bool GATED, bool OUT8, bool LAST>
+__global__ void __launch_bounds__((lp_smem<MX, OUT8, LAST>::THREADS), 1) k_linear_pair(
     const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u,
     const __grid_constant__ CUtensorMap map_sx, const __grid_constant__ CUtensorMap map_sw,
     const __grid_constant__ CUtensorMap map_su, const __grid_constant__ CUtensorMap map_out,
     const __grid_constant__ CUtensorMap map_res, const lp_params p, const lin_args a, int wide_out, int wide_res,
     float* __restrict__ partial, int32_t* flags, int32_t* status) {
-  constexpr int BOX_EL = MX ? 128 : 64, STAGE = lp_smem<MX, OUT8>::STAGE, LP_STAGES = lp_smem<MX, OUT8>::STAGES;
-  constexpr int WARP = lp_smem<MX, OUT8>::WARP;
+  typedef lp_smem<MX, OUT8, LAST> L;
+  constexpr int BOX_EL = MX ? 128 : 64, STAGE = L::STAGE, LP_STAGES = L::STAGES, WARP = L::WARP, EPI = L::EPI, PARTS = L::PARTS;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  unsigned char* pieces = smem + LP_STAGES * STAGE;
-  lp_tail& T = *reinterpret_cast<lp_tail*>(pieces + LP_EPI_WARPS * WARP);
+  unsigned char* pieces = LAST ? smem : smem + LP_STAGES * STAGE;
+  lp_tail& T = *reinterpret_cast<lp_tail*>(smem + LP_STAGES * STAGE + (LAST ? 0 : EPI * WARP));
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   volatile int* abort_flag = &T.abort_flag;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < LP_STAGES; ++s) { mbar_init(&T.full[s], 1); mbar_init(&T.empty[s], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&T.acc_full[i], 1); mbar_init(&T.acc_empty[i], 2 * LP_EPI_WARPS); }
-    mbar_init(&T.shared_free, LP_EPI_WARPS);           // four warps of each CTA
-    for (int i = 0; i < LP_EPI_WARPS; ++i) { mbar_init(&T.res_full[i][0], 1); mbar_init(&T.res_full[i][1], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&T.acc_full[i], 1); mbar_init(&T.acc_empty[i], 2 * EPI); }
+    mbar_init(&T.shared_free, 8);          // four warps of each CTA
+    for (int i = 0; i < EPI; ++i) { mbar_init(&T.res_full[i][0], 1); mbar_init(&T.res_full[i][1], 1); }
+    for (int i = 0; LAST && i < EPI * LP_MAX_PARTS; ++i) mbar_init(&T.part_full[0][0] + i, 1);
     T.abort_flag = 0;
     T.seen = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -339,13 +347,13 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
   } else {
     // ------------------------------------------------------------------ epilogue
     const int quarter = warp & 3;          // the lanes of tensor memory this warp may read
-    const int half = (warp - 2) >> 2;      // the columns 0 .. 127 upwards, or 255 .. 128 downwards
+    const int share = (warp - 2) >> 2;     // of the columns: the first half's are taken upwards, the others downwards
     unsigned char* mine = pieces + (warp - 2) * WARP;                // 1024-byte aligned
     const uint32_t mine_u32 = smem_u32(mine);
     uint64_t* res_full = T.res_full[warp - 2];
     uint32_t res_ph = 0;                   // phases of the two, a bit each
     const uint32_t acc_empty0 = lt_map(smem_u32(T.acc_empty), 0), shared0 = lt_map(smem_u32(&T.shared_free), 0);
-    constexpr int CHUNKS = GATED ? 2 : 4;  // of 32 outputs, for this warp
+    constexpr int G = 1 + GATED, CHUNKS = 32 / EPI / G;      // of 32 outputs, for this warp
     int seg = 0;
     bool ok = true;
     for (; ok && more; more = walk.next(p, pairs, tile, k0, k1)) {
@@ -361,7 +369,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
         while (from > 0 && lp_walk::first(p, from) > t0) --from;
         for (int j = from; j < pair && ok; ++j) {
           const long long c0 = clock64();
-          while (ok && ld_acquire(flags + 2 * j + rank) != LP_EPI_WARPS) {
+          while (ok && ld_acquire(flags + 2 * j + rank) != EPI) {
             if (*abort_flag) ok = false;
             else if (clock64() - c0 > TC_WAIT_CYCLES) {
               *abort_flag = 1;
@@ -373,11 +381,11 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         // the last warp to have seen them puts the flags back for the next call
-        if (lane == 0 && atomicAdd(&T.seen, 1u) == LP_EPI_WARPS - 1)
+        if (lane == 0 && atomicAdd(&T.seen, 1u) == EPI - 1)
           for (int j = from; j < pair; ++j) flags[2 * j + rank] = 0;
         __syncwarp();
       }
-      auto chunk = [&](int c) { return half ? (GATED ? 3 : 7) - c : c; };
+      auto chunk = [&](int c) { return share < EPI / 8 ? share * CHUNKS + c : (share + 1) * CHUNKS - 1 - c; };
       const bool rows_live = row0 < a.rows, live = row0 + lane < a.rows;
       // The residual of a chunk is brought to the piece that the chunk's outputs will take.
       auto ask_residual = [&](int c) {
@@ -392,7 +400,9 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
       // where only one does, and for f32 and 8-bit outputs, a lane reads its row)
       const bool res_tma = !OUT8 && whole && a.residual && wide_res;
       const bool res_x = !OUT8 && a.residual && a.out_type == JK_ROWS_T && !wide_out;
-      if (res_tma) ask_residual(0);
+      if (res_tma && !LAST) ask_residual(0);
+      if (res_tma && LAST && lane < CHUNKS && rows_live && n0 + chunk(lane) * 32 < a.n_out)
+        l2_prefetch_box(&map_res, n0 + chunk(lane) * 32, row0);
       // (a partial: 16 bytes of a lane next to the next lane's; one other pair's are asked for LP_W columns ahead)
       const size_t my_part = (size_t)quarter * LP_N * 32 + lane * 4;
       float4 t[LP_W / 4], tu[GATED ? LP_W / 4 : 1];
@@ -404,11 +414,32 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
           if constexpr (GATED) tu[j] = __ldcg(reinterpret_cast<const float4*>(o + LT_M * 32 + j * 128));
         }
       };
-      if (from < pair) ask_part(pair - 1, chunk(0) * 32);
+      const int parts = pair - from, asks = parts * (CHUNKS * 32 / LP_W) * G;
+      unsigned char* part_smem = smem + EPI * WARP + (warp - 2) * (PARTS * LP_PART);
+      int asked = 0, taken = 0;            // (LAST: pieces come in the order in which they are added)
+      auto ask_parts = [&] {
+        for (; asked < asks && asked < taken + PARTS; ++asked) {
+          if (lane) continue;
+          const int g = asked % G, k = pair - 1 - asked / G % parts, step = asked / G / parts;
+          const uint32_t bar = smem_u32(&T.part_full[warp - 2][asked % PARTS]);
+          const int col = chunk(step * LP_W / 32) * 32 + step * LP_W % 32 + g * LT_M;
+          lt_expect(bar, LP_PART, 1u);
+          lt_bulk(smem_u32(part_smem) + (uint32_t)(asked % PARTS) * LP_PART,
+                  partial + (size_t)(2 * k + rank) * LT_SLOT + (size_t)(quarter * LP_N + col) * 32, LP_PART, bar, 1u);
+        }
+      };
+      if (!LAST && parts) ask_part(pair - 1, chunk(0) * 32);
       ok = mbar_wait(&T.acc_full[buf], (uint32_t)use & 1u, abort_flag, status);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
+      if (LAST && whole) {                 // (the products of all boxes are done)
+        if (res_tma) ask_residual(0);
+        if (parts) {
+          asm volatile("fence.proxy.async;" ::: "memory");       // the partials were written by ordinary stores
+          ask_parts();
+        }
+      }
       const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * (MX ? LP_ACC2_MX : LP_N));
 #pragma unroll 1
       for (int c = 0; c < CHUNKS; ++c) {
@@ -473,7 +504,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
             tc_fence_before();
             __syncwarp();
             // the columns that both accumulators use: the last 24 of the first, the first 24 of the second
-            if (MX && c == 0 && half != buf && lane == 0) lp_arrive(shared0);
+            if (MX && c == 0 && share == (buf ? 0 : EPI / 4 - 1) && lane == 0) lp_arrive(shared0);
             if (c == CHUNKS - 1 && lane == 0) lp_arrive(acc_empty0 + 8u * (uint32_t)buf);
           }
           if (!whole) {
@@ -487,7 +518,26 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
             }
             continue;
           }
-          for (int k = pair - 1; k >= from; --k) {
+          if constexpr (LAST) {
+            for (int k = 0; k < parts; ++k) {
+#pragma unroll
+              for (int g = 0; g < G; ++g, ++taken) {
+                ok = ok && mbar_wait(&T.part_full[warp - 2][taken % PARTS], (uint32_t)(taken / PARTS) & 1u, abort_flag, status);
+                const float4* o = reinterpret_cast<const float4*>(part_smem + taken % PARTS * LP_PART) + lane;
+                float(&to)[LP_W] = g ? u : v;
+#pragma unroll
+                for (int j = 0; j < LP_W / 4; ++j) {
+                  const float4 y = o[j * 32];
+                  to[4 * j] += y.x; to[4 * j + 1] += y.y; to[4 * j + 2] += y.z; to[4 * j + 3] += y.w;
+                }
+              }
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              __syncwarp();
+              ask_parts();
+            }
+            if (!ok) break;
+          } else for (int k = pair - 1; k >= from; --k) {
             if (k < pair - 1) ask_part(k, col);
 #pragma unroll
             for (int j = 0; j < LP_W / 4; ++j) {
@@ -498,7 +548,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
             }
           }
           const bool last = i + LP_W == 32;
-          if (from < pair && (!last || c + 1 < CHUNKS)) ask_part(pair - 1, last ? chunk(c + 1) * 32 : col + LP_W);
+          if (!LAST && parts && (!last || c + 1 < CHUNKS)) ask_part(pair - 1, last ? chunk(c + 1) * 32 : col + LP_W);
           if (!out_live) continue;
           if (a.bias) {
             if (bias_full) { lp_add8<0>(v, b[0]); lp_add8<8>(v, b[1]); }
@@ -554,6 +604,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
             }
           }
         }
+        if (!ok) break;
         __syncwarp();
         if (!out_live) continue;
         if constexpr (OUT8) {              // n_out is a multiple of 32: all of the block or nothing
@@ -597,7 +648,14 @@ __global__ void __launch_bounds__(LP_THREADS, 1) k_linear_pair(
           }
         }
       }
-      if (!ok) break;
+      if (!ok) {                           // gave up: what was asked for lands before the memory goes away
+        for (int i = taken; i < asked && lane == 0; ++i) {
+          const unsigned long long t0 = global_ns();
+          while (!mbar_try_wait(&T.part_full[warp - 2][i % PARTS], (uint32_t)(i / PARTS) & 1u))
+            if (global_ns() - t0 > TC_WAIT_NS) break;
+        }
+        break;
+      }
       if (!whole) {
         __syncwarp();
         if (lane == 0) add_release(flags + blockIdx.x, 1);
@@ -650,7 +708,7 @@ double jk_linear_pair_plan(const lin_args& a, bool mx, int sms, lp_params* out) 
 }
 
 template <typename K>
-static int launch_pair(jk_ctx* ctx, cudaStream_t st, K kernel, size_t smem, int bit, const CUtensorMap& x, const CUtensorMap& w,
+static int launch_pair(jk_ctx* ctx, cudaStream_t st, K kernel, int threads, size_t smem, int bit, const CUtensorMap& x, const CUtensorMap& w,
                        const CUtensorMap& u, const CUtensorMap& sx, const CUtensorMap& sw, const CUtensorMap& su,
                        const CUtensorMap& o, const CUtensorMap& r, const lp_params& p, const lin_args& a, int wide_out,
                        int wide_res) {
@@ -659,7 +717,7 @@ static int launch_pair(jk_ctx* ctx, cudaStream_t st, K kernel, size_t smem, int 
     ctx->lin_smem_set |= bit;
   }
   JK_PROF(ctx, st, JK_ST_LINEAR);
-  jk_launch_pdl_cluster(kernel, dim3(2 * p.pairs), dim3(LP_THREADS), 2, smem, st, x, w, u, sx, sw, su, o, r, p, a, wide_out, wide_res,
+  jk_launch_pdl_cluster(kernel, dim3(2 * p.pairs), dim3(threads), 2, smem, st, x, w, u, sx, sw, su, o, r, p, a, wide_out, wide_res,
                         (float*)(ctx->ws + ctx->lay.lin_part), (int32_t*)(ctx->ws + ctx->lay.lin_flag),
                         (int32_t*)(ctx->ws + ctx->lay.status));
   JK_LAUNCH_CHECK(ctx);
@@ -699,12 +757,15 @@ int jk_linear_pair(jk_ctx* ctx, cudaStream_t st, const lin_args& a, bool mx) {
   if (rc == JK_OK && wide_res) rc = jk_tma_encode_piece(ctx, &mr, a.residual, 2, a.n_out, a.rows, a.r_stride, 32);
   if (rc != JK_OK) return rc;
   // (8-bit outputs are always wide: n_out is a multiple of 32)
-  auto pick = [&](auto m, auto g, auto o) {
-    constexpr bool M = decltype(m)::value, G = decltype(g)::value, O = decltype(o)::value;
-    return launch_pair(ctx, st, k_linear_pair<M, G, O>, lp_smem<M, O>::BYTES, 16 << (4 * M + 2 * G + O), mx_map, mw, mu, msx, msw,
-                       msu, mo, mr, p, a, wide_out, wide_res);
+  auto pick = [&](auto m, auto g, auto o, auto l) {
+    constexpr bool M = decltype(m)::value, G = decltype(g)::value, O = decltype(o)::value, LAST = decltype(l)::value;
+    typedef lp_smem<M, O, LAST> S;
+    return launch_pair(ctx, st, k_linear_pair<M, G, O, LAST>, S::THREADS, S::BYTES, 16 << (8 * LAST + 4 * M + 2 * G + O), mx_map, mw,
+                       mu, msx, msw, msu, mo, mr, p, a, wide_out, wide_res);
   };
-  auto pick_g = [&](auto m, auto g) { return q8 ? pick(m, g, std::true_type()) : pick(m, g, std::false_type()); };
+  const bool last = (long long)p.r_tiles * p.w_tiles <= p.pairs;
+  auto pick_l = [&](auto m, auto g, auto o) { return last ? pick(m, g, o, std::true_type()) : pick(m, g, o, std::false_type()); };
+  auto pick_g = [&](auto m, auto g) { return q8 ? pick_l(m, g, std::true_type()) : pick_l(m, g, std::false_type()); };
   auto pick_m = [&](auto m) { return gated ? pick_g(m, std::true_type()) : pick_g(m, std::false_type()); };
   return mx ? pick_m(std::true_type()) : pick_m(std::false_type());
 }

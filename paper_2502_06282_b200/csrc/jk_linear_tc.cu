@@ -51,6 +51,7 @@ struct lt_params {
   int grid;
   int cluster;                            // CTAs of a cluster that share a tile; 1: none
   int slots, exchange;                    // clusters: runs of 8 rows that a CTA finishes, and bytes of what it is handed
+                                          // (0: it is handed into the ring, once all CTAs' products are done)
 };
 
 struct __align__(16) lt_tail {
@@ -167,8 +168,8 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
   constexpr int BOX_EL = MX ? 128 : 64;    // elements of a box row
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  unsigned char* handed = smem + (size_t)p.stages * p.stage_bytes;
-  lt_tail& T = *reinterpret_cast<lt_tail*>(handed + p.exchange);
+  unsigned char* handed = p.exchange ? smem + (size_t)p.stages * p.stage_bytes : smem;
+  lt_tail& T = *reinterpret_cast<lt_tail*>(smem + (size_t)p.stages * p.stage_bytes + p.exchange);
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   volatile int* abort_flag = &T.abort_flag;
   // a stage: kb boxes of w, kb of w_up, kb of x, then the scale tiles in the same order
@@ -392,6 +393,7 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
     const int rows = min(p.nt, a.rows - tile % p.r_tiles * p.nt);
     bool ok = mbar_wait(&T.acc_full[0], 0, abort_flag, status);
     ok = __all_sync(0xffffffffu, ok);
+    if (!p.exchange) lt_cluster_sync();
     if (ok) {
       tc_fence_after();
       const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
@@ -497,6 +499,10 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
   }
   if (p.cluster > 1) {
     // ------------------------------------------------------------------ ... second half
+    if (!p.exchange && warp < 2) {
+      __syncwarp();
+      lt_cluster_sync();
+    }
     const int m = (warp & 3) * 32 + lane, rank = blockIdx.x % p.cluster, sub = (warp - 2) >> 2;
     const int own = blockIdx.x / p.cluster, wt = own / p.r_tiles, rt = own - wt * p.r_tiles;
     const int n = wt * LT_M + m, r0 = rt * p.nt, rows = min(p.nt, a.rows - r0);
@@ -604,13 +610,14 @@ double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, const int* cluster
     const int c = 2 << i;
     if (2 * c > p.boxes || tiles > clusters[i]) continue;  // (a stage for every CTA)
     const int slots = (p.nt / 8 + c - 1) / c, bytes = c * slots * G * 8 * LT_M * 4;
-    if (bytes > 64 * 1024) continue;                       // (the ring needs the rest)
-    const double cost = larger(tile_us / c, larger(hbm_us, hbm_us * 60 / (tiles * c))) + 1.2 + 0.01 * G * p.nt;
+    const bool apart = bytes <= 64 * 1024;                 // (the ring needs the rest)
+    if (!apart && bytes > p.stages * p.stage_bytes) continue;
+    const double cost = larger(tile_us / c, larger(hbm_us, hbm_us * 60 / (tiles * c))) + (apart ? 1.2 : 2.0) + 0.01 * G * p.nt;
     if (cost < best) {
       best = cost;
       p.cluster = c;
       p.slots = slots;
-      p.exchange = bytes;
+      p.exchange = apart ? bytes : 0;
       p.by_tile = 0;
       p.grid = (int)tiles * c;
     }
