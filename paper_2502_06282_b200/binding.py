@@ -495,22 +495,26 @@ class Context:
 
     def add_norm(self, x, weight=None, delta=None, out_sum=None, out=None, out_mx8: "Optional[Mx8]" = None):
         """jk_add_norm: x, delta, out_sum, out [rows, n] dense, weight [n], out_mx8 an Mx8 of [rows, n]."""
-        shape = x.shape
+        shape, T, ptrs = x.shape, self.tdtype, []
         if len(shape) != 2:
             raise ValueError("x: expected a tensor [rows, n]")
+        for t in (x, delta, out_sum, out):       # (a call of _dense for each costs as much as a third of a small launch)
+            if t is None:
+                ptrs.append(None)
+            elif t.dtype is T and t.shape == shape and t.is_contiguous() and t.is_cuda:
+                ptrs.append(t.data_ptr())
+            else:
+                raise ValueError(f"x, delta, out_sum, out: expected contiguous {T} tensors {list(shape)} on a CUDA device")
         if out_mx8 is None:
             codes = scales = None
         elif out_mx8.shape != shape:
             raise ValueError(f"out_mx8: expected an array of {list(shape)}")
         else:
             codes, scales = out_mx8.ptrs
-        dense = self._dense
-        px = dense(x, shape, "x")
-        rc = _lib.jk_add_norm(
-            self._h, _stream(), shape[0], shape[1], px, None if delta is None else dense(delta, shape, "delta"),
-            None if weight is None else dense(weight, shape[1:], "weight"),
-            None if out_sum is None else dense(out_sum, shape, "out_sum"),
-            None if out is None else dense(out, shape, "out"), codes, scales)
+        px, pd, ps, po = ptrs
+        rows, n = shape
+        pw = None if weight is None else self._dense(weight, (n,), "weight")
+        rc = _lib.jk_add_norm(self._h, _stream(), rows, n, px, pd, pw, ps, po, codes, scales)
         if rc:
             self._check(rc, "jk_add_norm")
 
@@ -555,9 +559,10 @@ class Context:
         d]; k_out, v_out [batch, Hkv, rows, d] with the same strides and dense rows; first_row i32 [batch]."""
         c, T, n = self.cfg, self.tdtype, batch * n_tokens
         width = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
-        if qkv.dtype is not T or qkv.shape[-1] != width or qkv.numel() != n * width or qkv.stride(-1) != 1:
+        dense = qkv.is_contiguous()
+        if qkv.dtype is not T or qkv.shape[-1] != width or qkv.numel() != n * width or not (dense or qkv.stride(-1) == 1):
             raise ValueError(f"qkv: expected a {T} tensor [batch, n_tokens, {width}]")
-        if n == 1 or qkv.is_contiguous():
+        if dense or n == 1:
             stride = width
         else:
             stride = qkv.stride(1) if qkv.dim() == 3 and n_tokens > 1 else qkv.stride(0)

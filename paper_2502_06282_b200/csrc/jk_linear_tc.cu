@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
                 ok = false;
               }
             }
-            asm volatile("fence.proxy.async;" ::: "memory");     // the partials were written by ordinary stores
+            asm volatile("fence.proxy.async.global;" ::: "memory");     // the partials were written by ordinary stores
           }
           if (ok) {
             const uint32_t bytes = (uint32_t)min(cols, p.nt - c) * LT_M * 4;
@@ -386,29 +386,73 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
       ++seg;
     }
   } else if (p.cluster > 1) {
-    // ------------------------------------------------------------------ epilogue of a shared tile, first half
+    // ------------------------------------------------------------------ epilogue of a shared tile
     // Each CTA of the cluster finishes every cluster-th run of 8 rows: it is handed the others' sums of
-    // those in its shared memory, and its own.
-    const int quarter = warp & 3, m = quarter * 32 + lane, rank = blockIdx.x % p.cluster;
-    const int rows = min(p.nt, a.rows - tile % p.r_tiles * p.nt);
-    bool ok = mbar_wait(&T.acc_full[0], 0, abort_flag, status);
-    ok = __all_sync(0xffffffffu, ok);
-    if (!p.exchange) lt_cluster_sync();
-    if (ok) {
-      tc_fence_after();
-      const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
-      for (int j = (warp - 2) >> 2; j * 8 < rows; j += LT_EPI_WARPS / 4) {
+    // those in its shared memory, and its own.  While the products run the warps go through it once without effect, so
+    // that its instructions are there when it counts.
+    const int quarter = warp & 3, sub = (warp - 2) >> 2, m = quarter * 32 + lane, rank = blockIdx.x % p.cluster;
+    const int wt = tile / p.r_tiles, rt = tile - wt * p.r_tiles;
+    const int n = wt * LT_M + m, r0 = rt * p.nt, rows = min(p.nt, a.rows - r0);
+    const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    const bool live = n < a.n_out;
+    uint16_t res[LT_COLS];
+    float bias = 0.f, bias_up = 0.f;
+    auto ask_residual = [&](int c) {
+      const uint16_t* rp = (const uint16_t*)a.residual + (size_t)(r0 + c) * a.r_stride + n;
+#pragma unroll
+      for (int j = 0; j < LT_COLS; ++j, rp += a.r_stride) res[j] = live && c + j < rows ? *rp : (uint16_t)0;
+    };
+    if (live && a.bias) bias = __bfloat162float(((const __nv_bfloat16*)a.bias)[n]);
+    if (GATED && live && a.bias_up) bias_up = __bfloat162float(((const __nv_bfloat16*)a.bias_up)[n]);
+    if (a.residual) ask_residual((sub * p.cluster + rank) * 8);
+#pragma unroll 1
+    for (int real = 0; real < 2; ++real) {
+      bool ok = true;
+      if (real) {
+        ok = mbar_wait(&T.acc_full[0], 0, abort_flag, status);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+        if (!p.exchange) lt_cluster_sync();
+      }
+      const int end = !real ? 8 : ok ? rows : 0;
+#pragma unroll 1
+      for (int j = real ? sub : 0; j * 8 < end; j += LT_EPI_WARPS / 4) {
         uint32_t v[8], u[8];
         lt_ld8(t_addr + (uint32_t)(j * 8), v);
         if constexpr (GATED) lt_ld8(t_addr + (uint32_t)(p.nt + j * 8), u);
         tmem_ld_wait();
         const uint32_t to = lt_map(smem_u32(handed) + (uint32_t)(((rank * p.slots + j / p.cluster) * G * 8 * LT_M + m) * 4),
                                    (uint32_t)(j % p.cluster));
+        if (real) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + i * LT_M * 4), "r"(v[i]) : "memory");
-          if constexpr (GATED) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + (8 + i) * LT_M * 4), "r"(u[i]) : "memory");
+          for (int i = 0; i < 8; ++i) {
+            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + i * LT_M * 4), "r"(v[i]) : "memory");
+            if constexpr (GATED) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + (8 + i) * LT_M * 4), "r"(u[i]) : "memory");
+          }
         }
+      }
+      __syncwarp();
+      if (real) lt_cluster_sync();
+#pragma unroll 1
+      for (int slot = real ? sub : 0; slot < (real ? p.slots : 1); slot += LT_EPI_WARPS / 4) {
+        const int c = (slot * p.cluster + rank) * 8, cols = real ? min(LT_COLS, rows - c) : 0;
+        if (real && cols <= 0) break;
+        if (a.residual && real && slot != sub) ask_residual(c);
+        float v[LT_COLS], u[GATED ? LT_COLS : 1];
+#pragma unroll
+        for (int j = 0; j < LT_COLS; ++j) {
+          v[j] = 0.f;
+          if constexpr (GATED) u[j] = 0.f;
+        }
+        for (int i = 0; i < p.cluster; ++i) {              // in the order of k
+          const float* o = reinterpret_cast<const float*>(handed) + (size_t)((i * p.slots + slot) * G * 8) * LT_M + m;
+#pragma unroll
+          for (int j = 0; j < LT_COLS; ++j) {
+            v[j] += o[j * LT_M];
+            if constexpr (GATED) u[j] += o[(8 + j) * LT_M];
+          }
+        }
+        lt_store<GATED>(a, v, u, cols, r0 + c, n, bias, bias_up, res);
       }
     }
   } else {
@@ -497,52 +541,10 @@ __global__ void __launch_bounds__(LT_THREADS, 1) k_linear_tc(const __grid_consta
       ++seg;
     }
   }
-  if (p.cluster > 1) {
-    // ------------------------------------------------------------------ ... second half
-    if (!p.exchange && warp < 2) {
-      __syncwarp();
-      lt_cluster_sync();
-    }
-    const int m = (warp & 3) * 32 + lane, rank = blockIdx.x % p.cluster, sub = (warp - 2) >> 2;
-    const int own = blockIdx.x / p.cluster, wt = own / p.r_tiles, rt = own - wt * p.r_tiles;
-    const int n = wt * LT_M + m, r0 = rt * p.nt, rows = min(p.nt, a.rows - r0);
-    const bool live = n < a.n_out;
-    uint16_t res[LT_COLS];
-    float bias = 0.f, bias_up = 0.f;
-    auto ask_residual = [&](int c) {
-      const uint16_t* rp = (const uint16_t*)a.residual + (size_t)(r0 + c) * a.r_stride + n;
-#pragma unroll
-      for (int j = 0; j < LT_COLS; ++j, rp += a.r_stride) res[j] = live && c + j < rows ? *rp : (uint16_t)0;
-    };
-    if (warp >= 2) {                       // (asked for ahead of the meeting)
-      if (live && a.bias) bias = __bfloat162float(((const __nv_bfloat16*)a.bias)[n]);
-      if (GATED && live && a.bias_up) bias_up = __bfloat162float(((const __nv_bfloat16*)a.bias_up)[n]);
-      if (a.residual) ask_residual((sub * p.cluster + rank) * 8);
-    }
+  if (p.cluster > 1 && warp < 2) {         // (the meetings of the epilogue's warps are all warps')
     __syncwarp();
+    if (!p.exchange) lt_cluster_sync();
     lt_cluster_sync();
-    if (warp >= 2) {
-      for (int slot = sub; slot < p.slots; slot += LT_EPI_WARPS / 4) {
-        const int c = (slot * p.cluster + rank) * 8;
-        if (c >= rows) break;
-        if (a.residual && slot != sub) ask_residual(c);
-        float v[LT_COLS], u[GATED ? LT_COLS : 1];
-#pragma unroll
-        for (int j = 0; j < LT_COLS; ++j) {
-          v[j] = 0.f;
-          if constexpr (GATED) u[j] = 0.f;
-        }
-        for (int i = 0; i < p.cluster; ++i) {              // in the order of k
-          const float* o = reinterpret_cast<const float*>(handed) + (size_t)((i * p.slots + slot) * G * 8) * LT_M + m;
-#pragma unroll
-          for (int j = 0; j < LT_COLS; ++j) {
-            v[j] += o[j * LT_M];
-            if constexpr (GATED) u[j] += o[(8 + j) * LT_M];
-          }
-        }
-        lt_store<GATED>(a, v, u, min(LT_COLS, rows - c), r0 + c, n, bias, bias_up, res);
-      }
-    }
   }
   tc_fence_before();
   __syncthreads();
@@ -563,8 +565,8 @@ double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, const int* cluster
   lt_params p;
   memset(&p, 0, sizeof(p));
   const int most = LT_ACC_COLS / G;
-  p.nt = a.rows <= most ? (int)jk_align_up(a.rows, 16) : most;
-  p.r_tiles = (a.rows + p.nt - 1) / p.nt;
+  p.r_tiles = (a.rows + most - 1) / most;
+  p.nt = p.r_tiles > 1 && mx ? most : (int)jk_align_up((a.rows + p.r_tiles - 1) / p.r_tiles, 16);     // (scale tiles: 128 rows)
   p.w_tiles = (a.n_out + LT_M - 1) / LT_M;
   p.boxes = (a.n_in + box_el - 1) / box_el;
   p.subs = (a.n_in * es + 31) / 32;
