@@ -351,11 +351,12 @@ extern "C" int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* op, int3
   if (rc != JK_OK) return rc;
   cudaStream_t st = (cudaStream_t)stream;
   if (ctx->tensor_path && ctx->cfg.dtype == JK_BF16 && jk_tma_available(ctx)) {
-    // Few rows: the kernel that streams weights past them, while the rows fit one tile (256, gated 128) and by the
-    // costs that the two kernels give.  Measured, us, 4096 x 4096 in bf16: 64 rows 12.4 against 21.5, 128 rows 16.1 / 22.0,
-    // 256 rows 25.0 / 22.2; in 8 bits 128 rows 13.5 / 17.3, 192 rows 19.1 / 17.4; 1376 x 512: 60 rows 7.2 / 8.8.
-    bool few = rows <= (op->w_up ? 128 : 256);
-    if (few && (rc = jk_linear_tc_pays(ctx, a, mx, &few)) != JK_OK) return rc;
+    // Of the kernel that streams weights past few rows and that for many rows the one with the lower cost.  Measured, us,
+    // 4096 inputs in bf16: 4096 outputs, 64 rows 10.7 against 21.5, 256 rows 16.2 / 24.1, 512 rows 22.0 / 25.2; 1024
+    // outputs, 512 rows 14.3 / 21.4; 6144 outputs, 512 rows 31.9 / 30.4; in 8 bits 4096 outputs, 256 rows 13.3 / 16.6, 512
+    // rows 15.9 / 17.2, 768 rows 20.4 / 18.3.
+    bool few;
+    if ((rc = jk_linear_tc_pays(ctx, a, mx, &few)) != JK_OK) return rc;
     return few ? jk_linear_tc(ctx, st, a, mx) : jk_linear_pair(ctx, st, a, mx);
   }
   JK_PROF(ctx, st, JK_ST_LINEAR);

@@ -690,7 +690,8 @@ double jk_linear_pair_plan(const lin_args& a, bool mx, int sms, lp_params* out) 
   p.subs = (a.n_in * es + 31) / 32;
   const long long tiles = (long long)p.r_tiles * p.w_tiles;
   const int pairs = sms / 2, left = (int)(tiles % pairs);
-  static const int hand_over[LP_MAX_SPLIT] = {0, 18, 24, 31};
+  static const int next_turn[LP_MAX_SPLIT] = {0, 18, 24, 31}, exposed[LP_MAX_SPLIT] = {0, 28, 34, 42};
+  const int* hand_over = mx || tiles < pairs ? exposed : next_turn;
   int split = 1;
   double best = left ? p.boxes : 0;
   for (int s = 2; left && s <= LP_MAX_SPLIT && s <= p.boxes && left * (s - 1) < pairs; ++s) {

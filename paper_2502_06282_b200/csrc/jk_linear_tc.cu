@@ -607,14 +607,15 @@ double jk_linear_tc_plan(const lin_args& a, bool mx, int sms, const int* cluster
     if (cost < best) { best = cost; p.by_tile = 0; p.grid = grid; }
     if (grid == sms) break;
   }
-  // Few tiles: a cluster for each, whose CTAs hand their sums over through shared memory: 1.2 us and 0.01 for each column.
+  // Few tiles: a cluster for each, whose CTAs hand their sums over through shared memory: 0.011 us for each column, less what
+  // sharing the epilogue saves.  (4096 x 4096 in bf16, us: 60 rows 10.7, dealt evenly 12.5; 256 rows 16.2, dealt evenly 25.0.)
   for (int i = 0; i < 3 && clusters; ++i) {
     const int c = 2 << i;
     if (2 * c > p.boxes || tiles > clusters[i]) continue;  // (a stage for every CTA)
     const int slots = (p.nt / 8 + c - 1) / c, bytes = c * slots * G * 8 * LT_M * 4;
     const bool apart = bytes <= 64 * 1024;                 // (the ring needs the rest)
     if (!apart && bytes > p.stages * p.stage_bytes) continue;
-    const double cost = larger(tile_us / c, larger(hbm_us, hbm_us * 60 / (tiles * c))) + (apart ? 1.2 : 2.0) + 0.01 * G * p.nt;
+    const double cost = larger(tile_us / c, larger(hbm_us, hbm_us * 60 / (tiles * c))) + 0.011 * G * p.nt - 0.4;
     if (cost < best) {
       best = cost;
       p.cluster = c;

@@ -359,7 +359,8 @@ def torch_mx8(x):
     (60, 640, 4096, False), (60, 4096, 4096, False), (17, 5120, 4096, False), (128, 1376, 4096, True), (60, 2048, 4096, True),
     (128, 11008, 8192, False), (250, 9000, 4096, False), (128, 11008, 2048, True), (1, 32000, 1024, False), (5, 20001, 512, True),
     (300, 2048, 8192, False), (300, 1300, 4096, True), (2047, 5120, 1024, False), (1500, 2500, 4096, True), (700, 5119, 2048, False),
-    (257, 9000, 8192, False), (4099, 384, 256, True)])
+    (257, 9000, 8192, False), (4099, 384, 256, True), (320, 4096, 1024, False), (500, 1000, 4096, False), (700, 640, 2048, False),
+    (1500, 300, 1024, False), (300, 640, 1024, True), (513, 200, 4096, True), (260, 1376, 8192, False), (385, 128, 96, False)])
 def test_linear_every_deal(R, N, K, gated, kind):
     """Against torch's product in 64 bits, twice for the same bits."""
     g = torch.Generator(device="cuda").manual_seed(R + N + K)
