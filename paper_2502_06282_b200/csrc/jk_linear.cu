@@ -123,8 +123,25 @@ __global__ void __launch_bounds__(256, 2) k_linear_rows(const lin_args a) {
 // step's loads on their way while one is multiplied.  The sum of 32 products is formed by itself and then added,
 // which keeps long sums within a few units of f32.  Where the tiles are few, `split` blocks of a cluster share one along
 // k and each finishes every split-th part of its rows from all their sums.
+// Two products an instruction (fma.rn.f32x2): one each spent two thirds of the issue slots and left the multipliers idle.
 #define LB_N 128
 #define LB_K 16
+__device__ __forceinline__ uint64_t lb_pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t lb_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ void lb_add(float& a, float& b, uint64_t p) {
+  float x, y;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p));
+  a += x;
+  b += y;
+}
 template <typename TX, typename T, bool GATED, int ROWS>
 __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int split) {
   constexpr int RT = ROWS / 16, OUTS = GATED ? 64 : 128;
@@ -170,11 +187,15 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int spli
         for (int i = 0; i < 4; ++i) s_x[b][lk + i][lr + 64 * h] = v[i];
       }
   };
-  float acc[RT][8], part[RT][8];
+  float acc[RT][8];
+  uint64_t part[RT][4];                    // of outputs 2 j and 2 j + 1
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = part[i][j] = 0.f;
+    for (int j = 0; j < 4; ++j) {
+      acc[i][2 * j] = acc[i][2 * j + 1] = 0.f;
+      part[i][j] = 0;
+    }
   const int all = (a.n_in + LB_K - 1) / LB_K, s0 = (int)((long long)all * rank / split);
   const int steps = (int)((long long)all * (rank + 1) / split) - s0;
   ask(s0 * LB_K);
@@ -185,9 +206,9 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int spli
     if (s + 1 < steps) ask((s0 + s + 1) * LB_K);
 #pragma unroll
     for (int k = 0; k < LB_K; ++k) {
-      float w[8], x[RT];
-      *reinterpret_cast<float4*>(&w[0]) = *reinterpret_cast<const float4*>(&s_w[b][k][tx * 4]);
-      *reinterpret_cast<float4*>(&w[4]) = *reinterpret_cast<const float4*>(&s_w[b][k][64 + tx * 4]);
+      float x[RT];
+      const float4 w0 = *reinterpret_cast<const float4*>(&s_w[b][k][tx * 4]), w1 = *reinterpret_cast<const float4*>(&s_w[b][k][64 + tx * 4]);
+      const uint64_t w[4] = {lb_pair(w0.x, w0.y), lb_pair(w0.z, w0.w), lb_pair(w1.x, w1.y), lb_pair(w1.z, w1.w)};
       if constexpr (RT >= 4) {
 #pragma unroll
         for (int i = 0; i < RT; i += 4)
@@ -197,15 +218,17 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int spli
         for (int i = 0; i < RT; ++i) x[i] = s_x[b][k][ty * RT + i];
       }
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int i = 0; i < RT; ++i) {
+        const uint64_t xx = lb_pair(x[i], x[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) part[i][j] = fmaf(x[i], w[j], part[i][j]);
+        for (int j = 0; j < 4; ++j) part[i][j] = lb_fma(xx, w[j], part[i][j]);
+      }
     }
     if ((s & 1) || s + 1 == steps) {
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { acc[i][j] += part[i][j]; part[i][j] = 0.f; }
+        for (int j = 0; j < 4; ++j) { lb_add(acc[i][2 * j], acc[i][2 * j + 1], part[i][j]); part[i][j] = 0; }
     }
     if (s + 1 < steps) put(b ^ 1);
     __syncthreads();
@@ -269,9 +292,12 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int spli
   }
 }
 
-// Up to 16 rows, while a scale block's outputs need not meet: warps of outputs.  Else blocks of 128 rows where they fill
-// the SMs, of 32 or 64 with up to 8 blocks to a tile where they do not.  f32, us (CUDA 12.9's library in parentheses, which
-// makes the products alone): 16 x 1376 x 512 gated 5.8 (31), 60 x 4096 x 4096 71 (87), 1024 x 4096 x 4096 886 (627).
+// Up to 16 rows, while a scale block's outputs need not meet: warps of outputs.  Up to 32, blocks of 32 rows with up to 8 to
+// a tile.  Else blocks of 128 or of 64 rows, the latter with 1 to 8 to a tile, by what the SM with the most of them needs:
+// a step of 16 along k takes a block of 128 rows 1.63 us, one of 64 rows 1.13 us alone on its SM and 0.98 next to another.
+// Measured in f32, us, with 128 rows / 64 / 64 shared by 2: 1024 x 4096 x 4096 837 / 992 / 872, 256 x 4096 x 4096 417 / 289 /
+// 257, 313 x 9352 x 3456 gated 1803 / 1151 / 1143; the whole range against CUDA 12.9's library, which makes the products
+// alone: 16 x 512 x 1376 gated 5.8 (31), 60 x 4096 x 4096 68 (88), 1024 x 4096 x 4096 837 (626).
 template <typename TX, typename T>
 static void launch_cc(cudaStream_t st, const lin_args& a, int sms) {
   const bool gated = a.w_up != nullptr;
@@ -280,11 +306,21 @@ static void launch_cc(cudaStream_t st, const lin_args& a, int sms) {
     jk_launch_pdl(gated ? k_linear_rows<TX, T, true> : k_linear_rows<TX, T, false>, grid, dim3(256), 0, st, a);
     return;
   }
-  const int outs = gated ? LB_N / 2 : LB_N, n_tiles = (a.n_out + outs - 1) / outs;
-  const int R = a.rows <= 32 ? 32 : (long long)n_tiles * ((a.rows + 127) / 128) >= sms ? 128 : 64;
-  const long long tiles = (long long)n_tiles * ((a.rows + R - 1) / R);
-  int split = 1;                           // (shares of 8 steps at least, blocks for two turns of every SM at most)
-  while (R < 128 && split < 8 && tiles * split * 2 <= 4ll * sms && (a.n_in + LB_K - 1) / LB_K >= 16 * split) split *= 2;
+  const int outs = gated ? LB_N / 2 : LB_N, n_tiles = (a.n_out + outs - 1) / outs, all = (a.n_in + LB_K - 1) / LB_K;
+  int R = 32, split = 1;                   // (shares of 8 steps at least)
+  if (a.rows <= 32) {
+    const long long tiles = n_tiles;
+    while (split < 8 && tiles * split * 2 <= 4ll * sms && all >= 16 * split) split *= 2;
+  } else {
+    const auto most = [&](int rows, int s) { return ((long long)n_tiles * ((a.rows + rows - 1) / rows) * s + sms - 1) / sms; };
+    double best = 1.63 * most(128, 1) * all;
+    R = 128;
+    for (int s = 1; s <= 8 && (s == 1 || all >= 8 * s); s *= 2) {
+      const long long n = most(64, s);
+      const double us = (n == 1 ? 1.13 : 0.98 * n) * ((all + s - 1) / s) + (s > 1 ? 3 + 2 * s : 0);
+      if (us < best) { best = us; R = 64; split = s; }
+    }
+  }
   const dim3 grid((unsigned)(n_tiles * split), (unsigned)((a.rows + R - 1) / R));
   auto k = R == 128 ? (gated ? k_linear_block<TX, T, true, 128> : k_linear_block<TX, T, false, 128>)
            : R == 64 ? (gated ? k_linear_block<TX, T, true, 64> : k_linear_block<TX, T, false, 64>)

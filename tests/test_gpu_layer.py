@@ -338,6 +338,29 @@ def test_linear_cuda_cores(kind, dtype, tensor):
     run_linear(37, 160, 352, kind, dtype=dtype, out="mx8", residual=True, tensor=tensor)
 
 
+# blocks of 128 rows; of 64, alone and shared by 2, 4 and 8
+@pytest.mark.parametrize("R,N,K,gated", [(1024, 1300, 256, False), (640, 640, 192, True), (1200, 2000, 520, True), (256, 4096, 1024, False),
+                                         (100, 4101, 1032, False), (64, 512, 2048, True)])
+def test_linear_f32_deals(R, N, K, gated):
+    """Against torch's product in 64 bits; sums of 32 products, then of those sums, within the bound of K + 4 roundings."""
+    g = torch.Generator(device="cuda").manual_seed(R + N)
+    ctx = make_ctx("f32")
+    x, w, u, res = (torch.randn(s, generator=g, device="cuda") for s in ((R, K), (N, K), (N, K), (R, N)))
+    op = jk.Linear(ctx, w, w_up=u if gated else None)
+    outs = [torch.full((R, N), float("nan"), device="cuda") for _ in range(2)]
+    for o in outs:
+        ctx.linear(op, x, o, residual=res)
+    assert ctx.read_status() == 0 and torch.equal(*outs)
+    z = x.double() @ w.double().T
+    e = (K + 4) * 2.0 ** -24 * (x.abs().double() @ w.abs().double().T)
+    if gated:
+        zu = x.double() @ u.double().T
+        eu = (K + 4) * 2.0 ** -24 * (x.abs().double() @ u.abs().double().T)
+        z, e = z * zu, e * zu.abs() + z.abs() * eu + e * eu + 2.0 ** -24 * (z * zu).abs()
+    y = z + res.double()
+    assert bool(((outs[0].double() - y).abs() <= e + 2.0 ** -23 * (y.abs() + e)).all())
+
+
 def torch_mx8(x):
     """x [rows, n] f32 on the device -> (Mx8, the values it stands for), the exponent by frexp."""
     R, n = x.shape
