@@ -9,15 +9,21 @@
 // consecutive outputs of a row, which are a scale block of 8-bit rows, without any exchange.
 //
 // Tiles are dealt to the pairs in turn, in bands of 8 tiles of x, so that what runs at one time shares
-// its operands in L2.  The tiles left over for a last, incomplete turn come first and are cut along k
-// into even shares: the pair that has a tile's end finishes it from the others' f32 partials, as in the
-// kernel for few rows.
+// its operands in L2.  The tiles left over for a last, incomplete turn may come first, cut along k
+// into even shares (jk_linear_pair_plan): the pair that has a tile's end finishes it from the others' f32 partials, as in
+// the kernel for few rows.
 //
 // Accumulators: two of 256 columns for bf16.  8-bit rows need 24 columns for scales; there the second
 // accumulator begins at column 232, and of the 24 columns that both use the epilogue reads first.
 //
-// Roles: warp 0 loads, warp 1 (of the pair's first CTA) multiplies, warps 2-9 are the epilogue.  Waits are bounded as
-// in the kernel for few rows.
+// Roles: warp 0 loads, warp 1 (of the pair's first CTA) multiplies, the others (8, or 16 where nothing hides them) are the
+// epilogue.  It works on 16 columns at a time: its instructions come through a loop that stays in the cache (32 columns
+// at a time waited for instructions, 8 for latency).  Outputs and the residual go through the copy engine
+// where their rows begin and end at multiples of 16 bytes.  Waits are bounded as in the kernel for few rows.
+//
+// Bound by the tensor cores and the power they take: 2047 rows, 5120 x 5120 in bf16 79 us on a cool card (1360 TFLOP/s), 87 to
+// 92 back to back, where the clock falls to 1.5 GHz; 4099 rows, 14336 x 4096 gated in 8 bits 365 us (2640), 430 back to
+// back.  480 rows, 5120 x 13824 in 8 bits 40 us (1690): 40 tiles among 74 pairs, of which the hand-over takes 13.
 #include <type_traits>
 
 #include "jk_linear_tc.cuh"
@@ -675,9 +681,11 @@ __global__ void __launch_bounds__((lp_smem<MX, OUT8, LAST>::THREADS), 1) k_linea
 
 // ------------------------------------------------------------------------------------------ host side
 // The deal.  The tiles of the last, incomplete turn: whole (a turn more), or cut among 2, 3 or 4 pairs each, which costs
-// the hand-over: 18, 24, 31 boxes' time (5.6, 7.5 and 9.6 us measured at 16 tiles, a box 0.31).  Cut at K = 8192 in bf16,
-// 16 tiles: 43.7 us whole, 31.9, 28.1, 27.2 among 2, 3, 4; at K = 2048: 16.4 whole, 17.5, 18.0, 19.4.  Returns the cost
-// in us, with a launch.
+// the hand-over in boxes' time (a box 0.31 us): 18, 24, 31 where whole tiles follow and hide a part, 28, 34, 42 where none do
+// or, in 8 bits, the two accumulators wait for one another.  Measured, us, whole and cut among 2, 3, 4 pairs: 16 tiles in
+// bf16, K = 2048 16.4, 18.9, 19.3, 20.9, K = 4096 25.3, 24.2, 24.1, 25.2; in 8 bits, K = 4096 16.5, 19.9, 20.6, 21.6; 160
+// tiles (12 left over), K = 5120 in bf16 88.3, 81.4, 79.7, 77.4, in 8 bits 49.1, 50.6, 50.0, 50.0.  Returns the cost in us,
+// with a launch.
 double jk_linear_pair_plan(const lin_args& a, bool mx, int sms, lp_params* out) {
   const bool gated = a.w_up != nullptr;
   const int es = mx ? 1 : 2, box_el = LT_BOX / es;

@@ -4,7 +4,9 @@
 // share its d/2 angles: a block takes a few tokens, forms their sines and cosines once in shared memory
 // (the angle as a product in 64 bits, reduced to [-pi, pi] there, so that positions of a million
 // keep their last bits; sine and cosine of the remainder in 32) and then streams the heads, 16 bytes
-// per thread and access.  Bound by memory: every element is read and written once.
+// per thread and access.  Bound by memory: every element is read and written once; 2 x 2047 tokens of 96 heads of 128, 201 MB
+// in 35.6 us (5.65 TB/s), 4 x 60 tokens 2.8 us.  Four blocks to an SM: more loads in flight for each thread at fewer
+// blocks took 44 us.
 #include <math.h>
 
 #include "jk_mx8.cuh"
