@@ -559,6 +559,8 @@ int jk_sample(jk_ctx* ctx, void* stream, int32_t rows, const void* logits, int32
  * are a whole layer, for the nodes of a tree, for single tokens and for a prompt's rows alike:
  *   add_norm -> linear (qkv) -> rope_qkv -> attention -> linear (output projection + residual) ->
  *   add_norm -> linear (gated) -> linear (down + residual).
+ * jk_tree_verify_attn may read kv_len and committed rows of its caches while the call before it ends: of the
+ * calls here only jk_rope_qkv writes what it may take as committed right behind.
  *
  * 8-bit rows ("mx8"): an array [rows, n], n a multiple of 32, as e4m3 codes, u8 [rows, n] dense, and
  * one power-of-two scale for each block of 32 consecutive elements of a row: the smallest

@@ -383,7 +383,8 @@ def torch_mx8(x):
     (128, 11008, 8192, False), (250, 9000, 4096, False), (128, 11008, 2048, True), (1, 32000, 1024, False), (5, 20001, 512, True),
     (300, 2048, 8192, False), (300, 1300, 4096, True), (2047, 5120, 1024, False), (1500, 2500, 4096, True), (700, 5119, 2048, False),
     (257, 9000, 8192, False), (4099, 384, 256, True), (320, 4096, 1024, False), (500, 1000, 4096, False), (700, 640, 2048, False),
-    (1500, 300, 1024, False), (300, 640, 1024, True), (513, 200, 4096, True), (260, 1376, 8192, False), (385, 128, 96, False)])
+    (1500, 300, 1024, False), (300, 640, 1024, True), (513, 200, 4096, True), (260, 1376, 8192, False), (385, 128, 96, False),
+    (1100, 2000, 8192, False), (256, 5120, 13824, False), (1100, 1200, 8192, True), (480, 4864, 4096, True)])
 def test_linear_every_deal(R, N, K, gated, kind):
     """Against torch's product in 64 bits, twice for the same bits."""
     g = torch.Generator(device="cuda").manual_seed(R + N + K)
@@ -411,6 +412,62 @@ def test_linear_every_deal(R, N, K, gated, kind):
     e = e + 2.0 ** -23 * (y.abs() + res.double().abs())
     off = (outs[0].double() - y).abs()
     assert bool((off <= HALF["bf16"] * (y.abs() + e) + e).all())
+
+
+# Many rows: fewer tiles than pairs of SMs (1500 and 1100 rows), and more
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("R,N", [(1500, 2496), (2100, 4992)])
+def test_linear_many_rows(R, N, kind):
+    run_linear(R, N + 2, 96, kind, bias=True, residual=True, act="gelu", wide=8)
+    run_linear(R, N, 96, kind, residual=True, wide=8, in_place=True)
+    run_linear(R, N, 96, kind, residual=True, bias=True, out="f32", wide=8)
+    run_linear(R, N, 96, kind, residual=True, bias=True, act="gelu", out="mx8")
+
+
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("R,N", [(1100, 1216), (1500, 2496)])
+def test_gated_many_rows(R, N, kind):
+    run_linear(R, N + 1, 96, kind, gated=True, bias=True, residual=True, act="silu", wide=8)
+    run_linear(R, N, 96, kind, gated=True, bias=True, residual=True, act="silu", in_place=True)
+    run_linear(R, N, 96, kind, gated=True, bias=True, act="gelu", out="f32")
+    run_linear(R, N, 96, kind, gated=True, residual=True, act="silu", out="mx8")
+
+
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("R,N,K,gated", [(1100, 2016, 8192, False), (1100, 1216, 8192, True), (2047, 5120, 5120, False),
+                                         (1100, 11008, 4096, True), (250, 4096, 4096, False), (120, 2048, 4096, True), (60, 512, 4096, False),
+                                         (100, 11008, 4096, False)])
+def test_linear_outputs_agree(R, N, K, gated, kind):
+    """Tiles cut among CTAs: outputs in T and in 8 bits are those in f32, rounded; in place too."""
+    g = torch.Generator(device="cuda").manual_seed(R + N + K)
+    ctx = make_ctx("bf16")
+    make = lambda r, s: torch.randn(r, K, generator=g, device="cuda") * s
+    pack = torch_mx8 if kind == "mx8" else (lambda x: (x.bfloat16(), x.bfloat16().double()))
+    (xd, x), (wd, w) = pack(make(R, 1.0)), pack(make(N, 0.05))
+    (ud, u) = pack(make(N, 0.05)) if gated else (None, None)
+    res, bias = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((R, N), (N,)))
+    op = jk.Linear(ctx, wd, bias=bias, act="silu" if gated else "none", w_up=ud)
+    y = torch.full((R, N), float("nan"), device="cuda")
+    ctx.linear(op, xd, y, residual=res)
+    z = x @ w.T + bias.double()
+    ez = (K + 4) * 2.0 ** -23 * (x.abs() @ w.abs().T + bias.double().abs())
+    if gated:
+        a, zu = z * torch.sigmoid(z), x @ u.T
+        eu = (K + 4) * 2.0 ** -23 * (x.abs() @ u.abs().T)
+        z, ez = a * zu, (1.13 * ez + 2.0 ** -18 * (a.abs() + 2.0 ** -20)) * zu.abs() + a.abs() * eu + 1.13 * ez * eu + 2.0 ** -23 * (a * zu).abs()
+    z = z + res.double()
+    assert bool(((y.double() - z).abs() <= ez + 2.0 ** -23 * (z.abs() + res.double().abs())).all())
+    t, place = torch.zeros(R, N, dtype=torch.bfloat16, device="cuda"), res.clone()
+    ctx.linear(op, xd, t, residual=res)
+    ctx.linear(op, xd, place, residual=place)
+    assert torch.equal(t, y.bfloat16()) and torch.equal(place, t)
+    m, (want, value) = jk.Mx8.empty(R, N), torch_mx8(y)
+    ctx.linear(op, xd, m, residual=res)
+    assert torch.equal(m.codes, want.codes)
+    full = m.scales.view(-(-R // 128), -(-N // 128), 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(-(-R // 128) * 128, -1)[:R, :N // 32]
+    assert torch.equal(full.double(), torch.log2(value.abs().view(R, N // 32, 32).amax(2) / m.codes.view(torch.float8_e4m3fn).double().abs().view(
+        R, N // 32, 32).amax(2)) + 127)
+    assert ctx.read_status() == 0
 
 
 def test_linear_two_contexts_at_once():
