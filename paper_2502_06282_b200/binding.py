@@ -15,6 +15,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libjakiro.so")
+CALLS_PATH = os.path.join(_HERE, "_calls.so")
 
 JK_F32, JK_BF16 = 0, 1
 JK_OK = 0
@@ -76,17 +77,16 @@ class JkLinearOp(C.Structure):
 JK_ROWS_T, JK_ROWS_F32, JK_ROWS_MX8 = 0, 1, 2
 ACTS = {"none": 0, "silu": 1, "gelu": 2}
 
-_SECTIONS: Dict[tuple, C.Array] = {}      # the counts of jk_rope_qkv as the library takes them
-_lib = None
+_lib = _calls = None                      # the library; its target layer's calls with the checks of their tensors
 
 
 def lib() -> C.CDLL:
     """The loaded shared library.  Raises if it has not been built."""
-    global _lib
+    global _lib, _calls
     if _lib is None:
-        if not os.path.exists(LIB_PATH):
+        if not os.path.exists(LIB_PATH) or not os.path.exists(CALLS_PATH):
             raise RuntimeError(
-                f"{LIB_PATH} is missing: build it with `python -m paper_2502_06282_b200.build` "
+                f"{LIB_PATH} or {CALLS_PATH} is missing: build them with `python -m paper_2502_06282_b200.build` "
                 "(needs nvcc); there is no fallback implementation")
         L = C.CDLL(LIB_PATH)
         vp, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
@@ -149,7 +149,9 @@ def lib() -> C.CDLL:
                 getattr(L, name).restype = C.c_int
         L.jk_paged_scratch_ints.restype = i64
         L.jk_row_scale_bytes.restype = i64
-        _lib = L
+        from . import _calls as calls
+        calls.bind(*(C.cast(f, vp).value for f in (L.jk_add_norm, L.jk_quantize_rows, L.jk_linear, L.jk_rope_qkv)), Mx8)
+        _lib, _calls = L, calls
     return _lib
 
 
@@ -204,6 +206,7 @@ class Context:
                             float(contrast_alpha), float(contrast_beta))
         self.dtype = dtype
         self.tdtype = torch_dtype(dtype)
+        self.is_bf16, self.heads = dtype == "bf16", (n_q_heads, n_kv_heads, head_dim)
         self.kv_kind = (n_kv_heads, head_dim, self.tdtype)     # what a paged cache has to hold
         self.q_row_bytes = n_q_heads * head_dim * self.tdtype.itemsize
         self._h = C.c_void_p()
@@ -473,19 +476,6 @@ class Context:
         self._check(rc, "jk_sample")
 
     # ------------------------------------------------------------------ a target layer around its attention
-    def _rows(self, t, name, dtype=None, shape=None):
-        """[rows, n] with contiguous rows: the distance between rows (0 where there is one)."""
-        if t.dtype is not (dtype or self.tdtype) or t.dim() != 2 or (shape is not None and t.shape != shape):
-            raise ValueError(f"{name}: expected a {dtype or self.tdtype} tensor {list(shape) if shape else '[rows, n]'}")
-        if not t.is_cuda:
-            raise ValueError(f"{name} is not on a CUDA device")
-        if t.is_contiguous():
-            return 0
-        s = t.stride()
-        if s[1] != 1 and t.shape[1] > 1:
-            raise ValueError(f"{name}: expected contiguous rows")
-        return s[0] if t.shape[0] > 1 else 0
-
     def _dense(self, t, shape, name):
         if t is None:
             return None
@@ -495,33 +485,13 @@ class Context:
 
     def add_norm(self, x, weight=None, delta=None, out_sum=None, out=None, out_mx8: "Optional[Mx8]" = None):
         """jk_add_norm: x, delta, out_sum, out [rows, n] dense, weight [n], out_mx8 an Mx8 of [rows, n]."""
-        shape, T, ptrs = x.shape, self.tdtype, []
-        if len(shape) != 2:
-            raise ValueError("x: expected a tensor [rows, n]")
-        for t in (x, delta, out_sum, out):       # (a call of _dense for each costs as much as a third of a small launch)
-            if t is None:
-                ptrs.append(None)
-            elif t.dtype is T and t.shape == shape and t.is_contiguous() and t.is_cuda:
-                ptrs.append(t.data_ptr())
-            else:
-                raise ValueError(f"x, delta, out_sum, out: expected contiguous {T} tensors {list(shape)} on a CUDA device")
-        if out_mx8 is None:
-            codes = scales = None
-        elif out_mx8.shape != shape:
-            raise ValueError(f"out_mx8: expected an array of {list(shape)}")
-        else:
-            codes, scales = out_mx8.ptrs
-        px, pd, ps, po = ptrs
-        rows, n = shape
-        pw = None if weight is None else self._dense(weight, (n,), "weight")
-        rc = _lib.jk_add_norm(self._h, _stream(), rows, n, px, pd, pw, ps, po, codes, scales)
+        rc = _calls.add_norm(self._h.value, self.is_bf16, x, weight, delta, out_sum, out, out_mx8)
         if rc:
             self._check(rc, "jk_add_norm")
 
     def quantize_mx8(self, x, out: "Mx8"):
         """jk_quantize_rows: x [rows, n] (rows may lie apart) to an Mx8 of the same shape."""
-        stride = self._rows(x, "x", shape=out.shape)
-        rc = lib().jk_quantize_rows(self._h, _stream(), x.shape[0], x.shape[1], x.data_ptr(), stride, *out.ptrs)
+        rc = _calls.quantize(self._h.value, self.is_bf16, x, out)
         if rc:
             self._check(rc, "jk_quantize_rows")
 
@@ -530,26 +500,7 @@ class Context:
         or Mx8), residual T [rows, n_out] or None; out may be the residual itself."""
         if op.kind is not self.tdtype:
             raise ValueError("the projection was made for a context of another type")
-        shape = x.shape
-        if op.mx8 is not isinstance(x, Mx8) or len(shape) != 2 or shape[1] != op.n_in:
-            raise ValueError(f"x: expected {'an Mx8' if op.mx8 else f'a {self.tdtype} tensor'} [rows, {op.n_in}]")
-        rows, n_out = shape[0], op.n_out
-        if op.mx8:
-            xs, (xp, xsp) = 0, x.ptrs
-        else:
-            xs, xp, xsp = self._rows(x, "x"), x.data_ptr(), None
-        shape = (rows, n_out)
-        rp, rs, os = None, 0, 0
-        if residual is not None:
-            rs, rp = self._rows(residual, "residual", shape=shape), residual.data_ptr()
-        if isinstance(out, Mx8):
-            if out.shape != shape:
-                raise ValueError(f"out: expected an array of {list(shape)}")
-            kind, (o, osp) = JK_ROWS_MX8, out.ptrs
-        else:
-            kind = JK_ROWS_F32 if out.dtype is torch.float32 else JK_ROWS_T
-            os, o, osp = self._rows(out, "out", out.dtype if kind == JK_ROWS_F32 else None, shape), out.data_ptr(), None
-        rc = _lib.jk_linear(self._h, _stream(), op.ref, rows, xp, xsp, xs, rp, rs, o, kind, osp, os)
+        rc = _calls.linear(self._h.value, self.is_bf16, op.address, x, out, residual)
         if rc:
             self._check(rc, "jk_linear")
 
@@ -557,35 +508,8 @@ class Context:
         """jk_rope_qkv: qkv [batch * n_tokens rows, (Hq + 2 Hkv) d], rows evenly apart; pos i32 [batch, n_tokens,
         axes] (one axis: [batch, n_tokens] too); sections the frequencies of each axis; q_out [batch, n_tokens, Hq,
         d]; k_out, v_out [batch, Hkv, rows, d] with the same strides and dense rows; first_row i32 [batch]."""
-        c, T, n = self.cfg, self.tdtype, batch * n_tokens
-        width = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
-        dense = qkv.is_contiguous()
-        if qkv.dtype is not T or qkv.shape[-1] != width or qkv.numel() != n * width or not (dense or qkv.stride(-1) == 1):
-            raise ValueError(f"qkv: expected a {T} tensor [batch, n_tokens, {width}]")
-        if dense or n == 1:
-            stride = width
-        else:
-            stride = qkv.stride(1) if qkv.dim() == 3 and n_tokens > 1 else qkv.stride(0)
-            if qkv.shape[:-1] not in ((n,), (batch, n_tokens)) or (
-                    qkv.dim() == 3 and batch > 1 and n_tokens > 1 and qkv.stride(0) != n_tokens * stride):
-                raise ValueError("qkv: its rows do not lie evenly apart")
-        sections = tuple(sections)
-        axes = len(sections)
-        if pos.dim() == 3 and pos.shape[2] != axes:
-            raise ValueError(f"pos: expected {axes} positions for each token")
-        if q_out.dtype is not T or q_out.numel() != n * c.n_q_heads * c.head_dim or not q_out.is_contiguous():
-            raise ValueError(f"q_out: expected a contiguous {T} tensor [batch, n_tokens, {c.n_q_heads}, {c.head_dim}]")
-        if not (qkv.is_cuda and pos.is_cuda and q_out.is_cuda and k_out.is_cuda and v_out.is_cuda
-                and (first_row is None or first_row.is_cuda)):
-            raise ValueError("qkv, pos, first_row and the outputs must be on a CUDA device")
-        s = self._tree_arrays(k_out, v_out, batch, n_tokens)
-        host = _SECTIONS.get(sections)
-        if host is None:
-            host = _SECTIONS[sections] = (C.c_int32 * max(1, axes))(*sections)
-        rc = _lib.jk_rope_qkv(
-            self._h, _stream(), batch, n_tokens, qkv.data_ptr(), stride, _array(pos, torch.int32, n * axes, "pos"), axes,
-            host, rope_theta, q_out.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
-            s[0], s[1], k_out.shape[2], _array(first_row, torch.int32, batch, "first_row"))
+        rc = _calls.rope_qkv(self._h.value, self.is_bf16, *self.heads, batch, n_tokens, qkv, pos, sections, rope_theta, q_out,
+                             k_out, v_out, first_row)
         if rc:
             self._check(rc, "jk_rope_qkv")
 
@@ -652,7 +576,6 @@ class Mx8:
         if scales.device != codes.device or not codes.is_cuda:
             raise ValueError("codes and scales must be on one CUDA device")
         self.codes, self.scales, self.shape = codes, scales, codes.shape
-        self.ptrs = (codes.data_ptr(), scales.data_ptr())
 
     @classmethod
     def empty(cls, rows, n, device="cuda") -> "Mx8":
@@ -679,14 +602,14 @@ class Linear:
             elif isinstance(m, Mx8) is not self.mx8 or tuple(m.shape) != (self.n_out, self.n_in):
                 raise ValueError("w and w_up must be of one shape and type")
             elif self.mx8:
-                ptrs.append(m.ptrs)
+                ptrs.append((m.codes.data_ptr(), m.scales.data_ptr()))
             else:
                 ptrs.append((ctx._dense(m, (self.n_out, self.n_in), name), None))
         for name, b in (("bias", bias), ("bias_up", bias_up)):
             ctx._dense(b, (self.n_out,), name)
         self.struct = JkLinearOp(self.n_out, self.n_in, JK_ROWS_MX8 if self.mx8 else JK_ROWS_T, ACTS[act],
                                  *ptrs[0], _ptr(bias), *ptrs[1], _ptr(bias_up))
-        self.ref = C.byref(self.struct)
+        self.address = C.addressof(self.struct)
 
 
 class PagedCache:

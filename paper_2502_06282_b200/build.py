@@ -1,4 +1,4 @@
-"""Build libjakiro.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Build libjakiro.so (nvcc, sm_100a, cross-compiles without a GPU) and _calls.so (g++, against torch) in-tree."""
 from __future__ import annotations
 
 import os
@@ -9,6 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libjakiro.so")
+CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["jk_api.cu", "jk_expand.cu", "jk_gemm_tc.cu", "jk_attn.cu", "jk_attn_tc.cu", "jk_attn_sk.cu", "jk_attn_cl.cu",
            "jk_accept.cu", "jk_pre.cu", "jk_paged.cu", "jk_paged_attn.cu", "jk_paged_tc.cu", "jk_sample.cu",
            "jk_norm.cu", "jk_rope.cu", "jk_linear.cu", "jk_linear_tc.cu", "jk_linear_pair.cu"]
@@ -22,11 +23,24 @@ def _nvcc() -> str:
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, "jakiro.h")]
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def _calls_command() -> list:
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    dirs = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(cuda, "include"), INCLUDE]
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return (["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+            + [f"-I{d}" for d in dirs] + [os.path.join(CSRC, "jk_calls.cpp"), "-o", CALLS, f"-L{libs}"]
+            + [f"-l{n}" for n in ("torch_python", "torch_cpu", "c10", "c10_cuda")])
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -45,12 +59,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs.append(obj)
         procs.append((src, subprocess.Popen(common + ["-c", os.path.join(CSRC, src), "-o", obj],
                                             stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+    procs.append(("jk_calls.cpp", subprocess.Popen(_calls_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     for src, p in procs:
         out, _ = p.communicate()
         if verbose or p.returncode:
             sys.stderr.write(out.decode())
         if p.returncode:
-            raise RuntimeError(f"nvcc failed on {src}")
+            raise RuntimeError(f"the compiler failed on {src}")
     subprocess.check_call([_nvcc(), "-shared", "-o", LIB] + objs + ["-cudart", "static"])
     return LIB
 
