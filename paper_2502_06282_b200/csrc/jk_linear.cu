@@ -81,41 +81,51 @@ __device__ __forceinline__ float warp_sums8(float (&v)[8], int lane) {
   return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
 }
 
-// Few rows: a warp owns a weight row (gated: one of w and one of w_up) and up to 8 rows of x, its lanes go along k: every
-// weight is read once from memory, x comes from the caches.  Bound by latency at the sizes it is taken for.
+// Few rows: a warp owns OUTS weight rows (gated: of w and of w_up) and up to 8 rows of x, its lanes go along k: every
+// weight is read once from memory, x comes from the caches.  Bound by latency at the sizes it is taken for, and, at one
+// weight row a warp, by x on its way from the caches.
 #define LR_ROWS 8
-template <typename TX, typename T, bool GATED>
+template <typename TX, typename T, bool GATED, int OUTS>
 __global__ void __launch_bounds__(256, 2) k_linear_rows(const lin_args a) {
   jk_pdl_wait();
   jk_pdl_trigger();
-  const int lane = threadIdx.x & 31, n = blockIdx.x * 8 + (threadIdx.x >> 5), r0 = blockIdx.y * LR_ROWS;
+  constexpr int W = OUTS * (1 + GATED);
+  const int lane = threadIdx.x & 31, n = (blockIdx.x * 8 + (threadIdx.x >> 5)) * OUTS, r0 = blockIdx.y * LR_ROWS;
   if (n >= a.n_out) return;
-  const TX* wr = (const TX*)a.w + (size_t)n * a.n_in;
-  const TX* ur = GATED ? (const TX*)a.w_up + (size_t)n * a.n_in : nullptr;
-  float acc[LR_ROWS], acc_up[LR_ROWS];
+  float acc[W][LR_ROWS];
 #pragma unroll
-  for (int j = 0; j < LR_ROWS; ++j) acc[j] = acc_up[j] = 0.f;
-#pragma unroll 4
+  for (int i = 0; i < W; ++i)
+#pragma unroll
+    for (int j = 0; j < LR_ROWS; ++j) acc[i][j] = 0.f;
+#pragma unroll (OUTS == 1 ? 4 : 2)
   for (int k = lane * 4; k < a.n_in; k += 128) {
-    const float4 w = lin_load4(wr, k, a.w_scale, n, a.k_tiles_in);
-    float4 u = w;
-    if (GATED) u = lin_load4(ur, k, a.w_up_scale, n, a.k_tiles_in);
+    float4 w[W];
+#pragma unroll
+    for (int i = 0; i < OUTS; ++i) {
+      const int row = min(n + i, a.n_out - 1);
+      w[i] = lin_load4((const TX*)a.w + (size_t)row * a.n_in, k, a.w_scale, row, a.k_tiles_in);
+      if (GATED) w[OUTS + i] = lin_load4((const TX*)a.w_up + (size_t)row * a.n_in, k, a.w_up_scale, row, a.k_tiles_in);
+    }
 #pragma unroll
     for (int j = 0; j < LR_ROWS; ++j)
       if (r0 + j < a.rows) {
         const float4 x = lin_load4((const TX*)a.x + (size_t)(r0 + j) * a.x_stride, k, a.x_scale, r0 + j, a.k_tiles_in);
-        acc[j] += fmaf(x.x, w.x, fmaf(x.y, w.y, fmaf(x.z, w.z, x.w * w.w)));
-        if (GATED) acc_up[j] += fmaf(x.x, u.x, fmaf(x.y, u.y, fmaf(x.z, u.z, x.w * u.w)));
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+          acc[i][j] += fmaf(x.x, w[i].x, fmaf(x.y, w[i].y, fmaf(x.z, w[i].z, x.w * w[i].w)));
       }
   }
-  const float z = warp_sums8(acc, lane), zu = GATED ? warp_sums8(acc_up, lane) : 0.f;
   const int r = r0 + 4 * (lane >> 4 & 1) + 2 * (lane >> 3 & 1) + (lane >> 2 & 1);
-  if ((lane & 3) || r >= a.rows) return;
-  float y = lin_act(z + lin_bias<T>(a.bias, n, a.n_out), a.act);
-  if (GATED) y *= zu + lin_bias<T>(a.bias_up, n, a.n_out);
-  if (a.residual) y += jk_to_float(((const T*)a.residual)[(size_t)r * a.r_stride + n]);
-  if (a.out_type == JK_ROWS_F32) ((float*)a.out)[(size_t)r * a.o_stride + n] = y;
-  else ((T*)a.out)[(size_t)r * a.o_stride + n] = jk_from_float<T>(y);
+#pragma unroll
+  for (int i = 0; i < OUTS; ++i) {
+    const float z = warp_sums8(acc[i], lane), zu = GATED ? warp_sums8(acc[W - OUTS + i], lane) : 0.f;
+    if ((lane & 3) || r >= a.rows || n + i >= a.n_out) continue;
+    float y = lin_act(z + lin_bias<T>(a.bias, n + i, a.n_out), a.act);
+    if (GATED) y *= zu + lin_bias<T>(a.bias_up, n + i, a.n_out);
+    if (a.residual) y += jk_to_float(((const T*)a.residual)[(size_t)r * a.r_stride + n + i]);
+    if (a.out_type == JK_ROWS_F32) ((float*)a.out)[(size_t)r * a.o_stride + n + i] = y;
+    else ((T*)a.out)[(size_t)r * a.o_stride + n + i] = jk_from_float<T>(y);
+  }
 }
 
 // The rest: a block makes ROWS rows times 128 weight rows (gated: 64 of w and 64 of w_up, the two of an output in one
@@ -292,7 +302,9 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int spli
   }
 }
 
-// Up to 16 rows, while a scale block's outputs need not meet: warps of outputs.  Up to 32, blocks of 32 rows with up to 8 to
+// Up to 16 rows, while a scale block's outputs need not meet: warps of outputs, of two each where there are more than the SMs
+// hold at a time (16 x 1928 x 4250 31.2 us with one, 17.8 with two, 1 x 4096 x 4096 15.0 and 12.5, but 16 x 512 x 512 2.6 and
+// 3.0; gated, where two are four rows of weights, 6.4 and 9.1 for 16 x 512 x 1376).  Up to 32, blocks of 32 rows with up to 8 to
 // a tile.  Else blocks of 128 or of 64 rows, the latter with 1 to 8 to a tile, by what the SM with the most of them needs:
 // a step of 16 along k takes a block of 128 rows 1.63 us, one of 64 rows 1.13 us alone on its SM and 0.98 next to another.
 // Measured in f32, us, with 128 rows / 64 / 64 shared by 2: 1024 x 4096 x 4096 837 / 992 / 872, 256 x 4096 x 4096 417 / 289 /
@@ -302,8 +314,10 @@ template <typename TX, typename T>
 static void launch_cc(cudaStream_t st, const lin_args& a, int sms) {
   const bool gated = a.w_up != nullptr;
   if (a.rows <= 2 * LR_ROWS && a.out_type != JK_ROWS_MX8) {
-    const dim3 grid((unsigned)((a.n_out + 7) / 8), (unsigned)((a.rows + LR_ROWS - 1) / LR_ROWS));
-    jk_launch_pdl(gated ? k_linear_rows<TX, T, true> : k_linear_rows<TX, T, false>, grid, dim3(256), 0, st, a);
+    const int y = (a.rows + LR_ROWS - 1) / LR_ROWS, outs = !gated && (long long)a.n_out * y >= 16ll * sms ? 2 : 1;
+    const dim3 grid((unsigned)((a.n_out + 8 * outs - 1) / (8 * outs)), (unsigned)y);
+    jk_launch_pdl(gated ? k_linear_rows<TX, T, true, 1> : outs == 2 ? k_linear_rows<TX, T, false, 2> : k_linear_rows<TX, T, false, 1>,
+                  grid, dim3(256), 0, st, a);
     return;
   }
   const int outs = gated ? LB_N / 2 : LB_N, n_tiles = (a.n_out + outs - 1) / outs, all = (a.n_in + LB_K - 1) / LB_K;

@@ -338,9 +338,10 @@ def test_linear_cuda_cores(kind, dtype, tensor):
     run_linear(37, 160, 352, kind, dtype=dtype, out="mx8", residual=True, tensor=tensor)
 
 
-# blocks of 128 rows; of 64, alone and shared by 2, 4 and 8
+# blocks of 128 rows; of 64, alone and shared by 2, 4 and 8; warps of one and two outputs
 @pytest.mark.parametrize("R,N,K,gated", [(1024, 1300, 256, False), (640, 640, 192, True), (1200, 2000, 520, True), (256, 4096, 1024, False),
-                                         (100, 4101, 1032, False), (64, 512, 2048, True)])
+                                         (100, 4101, 1032, False), (64, 512, 2048, True), (1, 2373, 136, False), (16, 4097, 264, False),
+                                         (9, 1190, 1000, False), (5, 4099, 72, True)])
 def test_linear_f32_deals(R, N, K, gated):
     """Against torch's product in 64 bits; sums of 32 products, then of those sums, within the bound of K + 4 roundings."""
     g = torch.Generator(device="cuda").manual_seed(R + N)
