@@ -785,3 +785,52 @@ def test_target_layer(dtype, B, M, paged, mx8):
         torch.cuda.synchronize()
         assert np.array_equal(host(x).astype(np.float64), got)
     assert ctx.read_status() == 0
+
+
+def test_binding_refuses_arrays_on_the_device():
+    """Types, shapes and strides that the calls would read or write wrongly."""
+    T, d = dict(dtype=torch.bfloat16, device="cuda"), dict(device="cuda")
+    ctx = make_ctx("bf16", Hq=4, Hkv=2)
+    x, w = torch.zeros(4, 64, **T), torch.zeros(96, 64, **T)
+    m, op = jk.Mx8.empty(4, 64), jk.Linear(ctx, w)
+    out = torch.zeros(4, 96, **T)
+
+    def bad(call, *a, **kw):
+        with pytest.raises(ValueError):
+            call(*a, **kw)
+
+    for kw in (dict(weight=torch.zeros(32, **T)), dict(weight=torch.zeros(1, 64, **T)), dict(delta=torch.zeros(4, 64, **d)),
+               dict(delta=torch.zeros(4, 32, **T)), dict(out_sum=torch.zeros(2, 64, **T)), dict(out=torch.zeros(4, 128, **T)[:, ::2]),
+               dict(out=torch.zeros(4, 128, **T)[:, :64]), dict(out=torch.zeros(4, 64, dtype=torch.bfloat16)), dict(out=[0]),
+               dict(out_mx8=jk.Mx8.empty(4, 32)), dict(out_mx8=m.codes)):
+        bad(ctx.add_norm, x, **{"out": torch.zeros_like(x), **kw})
+    bad(ctx.add_norm, torch.zeros(4, 128, **T)[:, :64], out=x)
+    bad(ctx.quantize_mx8, x.float(), m)
+    bad(ctx.quantize_mx8, x[:2], m)
+    bad(ctx.quantize_mx8, torch.zeros(64, 4, **T).T, m)
+    bad(ctx.quantize_mx8, x, x)
+    for a in ((x[:, :32], out), (x.float(), out), (m, out), (torch.zeros(64, 4, **T).T, out), (x, out[:2]), (x, out[:, :64]),
+              (x, out.half()), (x, jk.Mx8.empty(4, 64)), (x, out, out[:2]), (x, out, out.float()), (x, torch.zeros(96, 4, **T).T),
+              (x.cpu(), out), (None, out), (x, None), (x[0], out)):
+        bad(ctx.linear, op, *a)
+    bad(ctx.linear, jk.Linear(ctx, jk.Mx8.empty(96, 64)), x, out)
+    bad(make_ctx("f32").linear, op, x, out)
+    Hq, Hkv, D, B, M = ctx.cfg.n_q_heads, ctx.cfg.n_kv_heads, ctx.cfg.head_dim, 2, 3
+    W = (Hq + 2 * Hkv) * D
+    good = dict(batch=B, n_tokens=M, qkv=torch.zeros(B, M, W, **T), pos=torch.zeros(B, M, 1, dtype=torch.int32, **d), sections=(D // 2,),
+                rope_theta=1e4, q_out=torch.zeros(B, M, Hq, D, **T), k_out=torch.zeros(B, Hkv, 8, D, **T),
+                v_out=torch.zeros(B, Hkv, 8, D, **T), first_row=torch.zeros(B, dtype=torch.int32, **d))
+    ctx.rope_qkv(**good)
+    for kw in (dict(qkv=torch.zeros(B, M, W, **d)), dict(qkv=torch.zeros(B, M, W + D, **T)), dict(qkv=torch.zeros(B, M + 1, W, **T)),
+               dict(qkv=torch.zeros(M, B, W, **T).transpose(0, 1)), dict(qkv=torch.zeros(B, 2 * M, W, **T)[:, :M]),
+               dict(qkv=torch.zeros(M, B, 2 * W, **T)[:, :, :W]), dict(pos=torch.zeros(B, M, 2, dtype=torch.int32, **d)),
+               dict(pos=torch.zeros(B, M, **d)), dict(pos=torch.zeros(B, 1, dtype=torch.int32, **d)), dict(sections=(1,) * 17),
+               dict(q_out=torch.zeros(B, M, Hq, 2 * D, **T)[..., :D]), dict(q_out=torch.zeros(B, M, Hq, D, **d)),
+               dict(k_out=torch.zeros(B, Hkv, 2, D, **T), v_out=torch.zeros(B, Hkv, 2, D, **T)), dict(k_out=torch.zeros(B, Hkv, 9, D, **T)),
+               dict(k_out=torch.zeros(B, 8, Hkv, D, **T).transpose(1, 2)), dict(v_out=torch.zeros(B, Hkv, 8, D, **d)),
+               dict(k_out=torch.zeros(1, Hkv, 8, D, **T), v_out=torch.zeros(1, Hkv, 8, D, **T)),
+               dict(first_row=torch.zeros(B, dtype=torch.int64, **d)), dict(first_row=torch.zeros(1, dtype=torch.int32, **d)),
+               dict(first_row=torch.zeros(B, dtype=torch.int32)), dict(batch=-1), dict(qkv=None)):
+        bad(ctx.rope_qkv, **{**good, **kw})
+    torch.cuda.synchronize()
+    assert ctx.read_status() == 0
