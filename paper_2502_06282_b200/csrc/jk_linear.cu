@@ -97,15 +97,16 @@ __global__ void __launch_bounds__(256, 2) k_linear_rows(const lin_args a) {
   for (int i = 0; i < W; ++i)
 #pragma unroll
     for (int j = 0; j < LR_ROWS; ++j) acc[i][j] = 0.f;
+  const int last = OUTS > 1 ? min(n + OUTS, a.n_out) - 1 : n;
+  const TX *w0 = (const TX*)a.w + (size_t)n * a.n_in, *w1 = (const TX*)a.w + (size_t)last * a.n_in;
+  const TX* u0 = GATED ? (const TX*)a.w_up + (size_t)n * a.n_in : nullptr;
+  static_assert(OUTS <= 2 && (OUTS == 1 || !GATED), "two outputs, plain ones");
 #pragma unroll (OUTS == 1 ? 4 : 2)
   for (int k = lane * 4; k < a.n_in; k += 128) {
     float4 w[W];
-#pragma unroll
-    for (int i = 0; i < OUTS; ++i) {
-      const int row = min(n + i, a.n_out - 1);
-      w[i] = lin_load4((const TX*)a.w + (size_t)row * a.n_in, k, a.w_scale, row, a.k_tiles_in);
-      if (GATED) w[OUTS + i] = lin_load4((const TX*)a.w_up + (size_t)row * a.n_in, k, a.w_up_scale, row, a.k_tiles_in);
-    }
+    w[0] = lin_load4(w0, k, a.w_scale, n, a.k_tiles_in);
+    if (GATED) w[W - 1] = lin_load4(u0, k, a.w_up_scale, n, a.k_tiles_in);
+    if (OUTS > 1) w[W - 1] = lin_load4(w1, k, a.w_scale, last, a.k_tiles_in);
 #pragma unroll
     for (int j = 0; j < LR_ROWS; ++j)
       if (r0 + j < a.rows) {
@@ -303,8 +304,8 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int spli
 }
 
 // Up to 16 rows, while a scale block's outputs need not meet: warps of outputs, of two each where there are more than the SMs
-// hold at a time (16 x 1928 x 4250 31.2 us with one, 17.8 with two, 1 x 4096 x 4096 15.0 and 12.5, but 16 x 512 x 512 2.6 and
-// 3.0; gated, where two are four rows of weights, 6.4 and 9.1 for 16 x 512 x 1376).  Up to 32, blocks of 32 rows with up to 8 to
+// hold at a time (16 x 1928 x 4250 31.2 us with one, 17.8 with two, 1 x 4096 x 4096 15.0 and 12.3, 5 x 8192 x 8192 80
+// and 86, 16 x 512 x 512 2.5 and 3.0; gated, where two are four rows of weights, 5.8 and 9.1 for 16 x 512 x 1376).  Up to 32, blocks of 32 rows with up to 8 to
 // a tile.  Else blocks of 128 or of 64 rows, the latter with 1 to 8 to a tile, by what the SM with the most of them needs:
 // a step of 16 along k takes a block of 128 rows 1.63 us, one of 64 rows 1.13 us alone on its SM and 0.98 next to another.
 // Measured in f32, us, with 128 rows / 64 / 64 shared by 2: 1024 x 4096 x 4096 837 / 992 / 872, 256 x 4096 x 4096 417 / 289 /

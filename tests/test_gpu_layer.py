@@ -834,3 +834,26 @@ def test_binding_refuses_arrays_on_the_device():
         bad(ctx.rope_qkv, **{**good, **kw})
     torch.cuda.synchronize()
     assert ctx.read_status() == 0
+
+
+@pytest.mark.parametrize("R,N,K", [(60, 4096, 4096), (60, 11008, 2048), (700, 5120, 2048)])
+def test_first_call_of_a_context_is_captured(R, N, K):
+    """Nothing that a context finds out on its first call disturbs a capture; two graphs of it, replayed in turn."""
+    g = torch.Generator(device="cuda").manual_seed(R)
+    x, w = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((R, K), (N, K)))
+    ctx = make_ctx("bf16")
+    outs = [torch.zeros(R, N, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for graph, out in zip(graphs, outs):
+        with torch.cuda.graph(graph):
+            ctx.linear(jk.Linear(ctx, w), x, out)
+    for _ in range(3):
+        for graph, out in zip(graphs, outs):
+            out.zero_()
+            graph.replay()
+    other = make_ctx("bf16")
+    other.linear(jk.Linear(other, w), x, outs[2])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2])
+    assert ctx.read_status() == 0
