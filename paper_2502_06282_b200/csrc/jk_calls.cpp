@@ -54,16 +54,18 @@ void* dense(PyObject* o, const char* name, at::ScalarType type, int64_t rows, in
   }
   return t.data_ptr();
 }
-// Rows that may lie apart, [rows, n] (-1: any): the pointer and the distance (0: dense).
+// Rows that may lie apart, [rows, n] (-1: any): the pointer and the distance (0, which the library takes as dense, only for
+// a single row: the rows of an expanded array are one, and lie no distance apart).
 void* strided(const at::Tensor& t, const char* name, at::ScalarType type, int64_t rows, int64_t n, int64_t& stride) {
   if (t.scalar_type() != type || t.dim() != 2 || (rows >= 0 && t.size(0) != rows) || (n >= 0 && t.size(1) != n))
     refuse("%s: expected a %s tensor [%lld, %lld]", name, name_of(type), (long long)rows, (long long)n);
-  if (!t.is_cuda()) refuse("%s is not on a CUDA device", name);
   stride = 0;
-  if (!t.is_contiguous()) {
-    if (t.stride(1) != 1 && t.size(1) > 1) refuse("%s: expected contiguous rows", name);
-    if (t.size(0) > 1) stride = t.stride(0);
+  if (t.stride(1) != 1 && t.size(1) > 1) refuse("%s: expected contiguous rows", name);
+  if (t.size(0) > 1) {
+    stride = t.stride(0);
+    if (stride < t.size(1)) refuse("%s: its rows overlap", name);
   }
+  if (!t.is_cuda()) refuse("%s is not on a CUDA device", name);
   return t.data_ptr();
 }
 // The codes and scales of an Mx8 [rows, n] (-1: any; its arrays were checked when it was made).
@@ -193,16 +195,18 @@ PyObject* rope_qkv(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const int64_t n = B * M, width = (Hq + 2 * Hkv) * d;
     const at::Tensor& qkv = tensor(a[7], "qkv");
     const int64_t dims = qkv.dim();
-    if (qkv.scalar_type() != T || dims < 1 || qkv.size(-1) != width || qkv.numel() != n * width || !qkv.is_cuda() ||
+    if (qkv.scalar_type() != T || dims < 1 || qkv.size(-1) != width || qkv.numel() != n * width ||
         !(qkv.is_contiguous() || qkv.stride(-1) == 1))
-      refuse("qkv: expected a %s tensor [batch, n_tokens, %lld] on a CUDA device", name_of(T), (long long)width);
+      refuse("qkv: expected a %s tensor [batch, n_tokens, %lld]", name_of(T), (long long)width);
     int64_t stride = width;
     if (!qkv.is_contiguous() && n != 1) {
       const bool flat = dims == 2, deep = dims == 3 && qkv.size(0) == B && qkv.size(1) == M;
       if (!flat && !deep) refuse("qkv: expected a tensor [batch, n_tokens, %lld]", (long long)width);
       stride = deep && M > 1 ? qkv.stride(1) : qkv.stride(0);
       if (deep && B > 1 && M > 1 && qkv.stride(0) != M * stride) refuse("qkv: its rows do not lie evenly apart");
+      if (stride < width) refuse("qkv: its rows overlap");
     }
+    if (!qkv.is_cuda()) refuse("qkv is not on a CUDA device");
     int32_t sections[16];
     PyObject* seq = PySequence_Fast(a[9], "sections: expected a sequence of counts");
     if (!seq) throw refused();

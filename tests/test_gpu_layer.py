@@ -857,3 +857,28 @@ def test_first_call_of_a_context_is_captured(R, N, K):
     torch.cuda.synchronize()
     assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2])
     assert ctx.read_status() == 0
+
+
+def test_binding_refuses_expanded_rows_on_the_device():
+    """Arrays whose rows are one row in memory, as every operand; a single expanded row is an ordinary one."""
+    T = dict(dtype=torch.bfloat16, device="cuda")
+    ctx = make_ctx("bf16", Hq=4, Hkv=2)
+    x, w, out, m = torch.randn(4, 64, **T), torch.randn(96, 64, **T), torch.zeros(4, 96, **T), jk.Mx8.empty(4, 64)
+    op, one = jk.Linear(ctx, w), torch.randn(96, **T)
+    for a in ((x[:1].expand(4, 64), out), (x[0].expand(4, 64), out), (x, one.expand(4, 96)), (x, one.float().expand(4, 96)),
+              (x, out, one.expand(4, 96))):
+        with pytest.raises(ValueError, match="rows overlap"):
+            ctx.linear(op, *a)
+    with pytest.raises(ValueError, match="rows overlap"):
+        ctx.quantize_mx8(x[0].expand(4, 64), m)
+    Hq, Hkv, D, B, M = 4, 2, 64, 2, 3
+    W = (Hq + 2 * Hkv) * D
+    new = lambda: [torch.zeros(s, **T) for s in ((B, M, Hq, D), (B, Hkv, 8, D), (B, Hkv, 8, D))]
+    pos = torch.zeros(B, M, dtype=torch.int32, device="cuda")
+    for qkv in (one.repeat(6)[:W].expand(B * M, W), one.repeat(6)[:W].expand(B, M, W)):
+        with pytest.raises(ValueError, match="rows overlap"):
+            ctx.rope_qkv(B, M, qkv, pos, (D // 2,), 1e4, *new())
+    got = torch.zeros(1, 96, **T)
+    ctx.linear(op, x[0].expand(1, 64), got, residual=one.expand(1, 96))
+    ctx.linear(op, x, out, residual=one.repeat(4, 1))
+    assert torch.equal(got[0], out[0]) and ctx.read_status() == 0

@@ -152,3 +152,32 @@ def test_binding_refuses_other_arrays(lib):
     with pytest.raises(ValueError):
         ctx.rope_qkv(1, 2, bf(1, 3, 512), torch.zeros(1, 2, dtype=torch.int32), (32,), 1e4, bf(1, 2, 4, 64), bf(1, 2, 2, 64),
                      bf(1, 2, 2, 64))
+
+
+def test_binding_refuses_expanded_rows(lib):
+    """Rows that are one row in memory: the library would take the distance of 0 for dense rows and reach past that row.
+    (On host tensors, whose strides are looked at before their device.)"""
+    ctx = make_ctx()
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    x, w, out = bf(4, 64), bf(96, 64), bf(4, 96)
+    op = jk.Linear.__new__(jk.Linear)
+    op.kind, op.struct = ctx.tdtype, jk.JkLinearOp(96, 64, 0, 0, w.data_ptr())
+    op.address = C.addressof(op.struct)
+    near = bf(1000).as_strided((4, 64), (32, 1))          # rows that share elements without being one
+    for bad in (bf(1, 64).expand(4, 64), bf(64).expand(4, 64), near):
+        with pytest.raises(ValueError, match="rows overlap"):
+            ctx.linear(op, bad, out)
+    for a in ((x, bf(1, 96).expand(4, 96)), (x, torch.zeros(96).expand(4, 96))):
+        with pytest.raises(ValueError, match="device"):   # (x comes first, and is on the host)
+            ctx.linear(op, *a)
+    Hq, Hkv, D, B, M = 4, 2, 64, 2, 3
+    W = (Hq + 2 * Hkv) * D
+    rest = dict(pos=torch.zeros(B, M, dtype=torch.int32), sections=(D // 2,), rope_theta=1e4, q_out=bf(B, M, Hq, D),
+                k_out=bf(B, Hkv, 8, D), v_out=bf(B, Hkv, 8, D))
+    for qkv in (bf(W).expand(B * M, W), bf(W).expand(B, M, W), bf(B * M * W).as_strided((B, M, W), (M * 8, 8, 1))):
+        with pytest.raises(ValueError, match="rows overlap"):
+            ctx.rope_qkv(B, M, qkv, **rest)
+    with pytest.raises(ValueError, match="evenly"):
+        ctx.rope_qkv(B, M, bf(1, M, W).expand(B, M, W), **rest)
+    with pytest.raises(ValueError, match="device"):
+        ctx.rope_qkv(B, M, bf(B, M, W), **rest)
