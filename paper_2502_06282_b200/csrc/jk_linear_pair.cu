@@ -447,6 +447,7 @@ __global__ void __launch_bounds__((lp_smem<MX, OUT8, LAST>::THREADS), 1) k_linea
         }
       }
       const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * (MX ? LP_ACC2_MX : LP_N));
+      bool first = true;                   // no output of this tile has been stored yet
 #pragma unroll 1
       for (int c = 0; c < CHUNKS; ++c) {
         const int q = chunk(c), n = n0 + q * 32, most = a.n_out - n;
@@ -463,10 +464,13 @@ __global__ void __launch_bounds__((lp_smem<MX, OUT8, LAST>::THREADS), 1) k_linea
             res_ph ^= 1u << (c & 1);
           }
         } else if (out_live) {
+          // (within a tile the latest store has the other piece; chunks past the outputs store nothing, so that of the tile
+          // before may have this one)
           if (lane == 0) {
-            if (wide_out && (OUT8 || a.out_type == JK_ROWS_T)) lp_put_read<1>();
+            if (wide_out && (OUT8 || a.out_type == JK_ROWS_T) && !first) lp_put_read<1>();
             else lp_put_read<0>();
           }
+          first = false;
           __syncwarp();
           if (res_x) {
             // rows that begin anywhere: read along the rows, handed out through shared memory

@@ -882,3 +882,33 @@ def test_binding_refuses_expanded_rows_on_the_device():
     ctx.linear(op, x[0].expand(1, 64), got, residual=one.expand(1, 96))
     ctx.linear(op, x, out, residual=one.repeat(4, 1))
     assert torch.equal(got[0], out[0]) and ctx.read_status() == 0
+
+
+# More tiles than pairs of SMs, the last of the weights ending after 1 or 3 blocks of 32 outputs; few steps along k, so
+# that a tile's stores follow the last one's closely
+@pytest.mark.parametrize("kind", ["T", "mx8"])
+@pytest.mark.parametrize("out", ["T", "mx8"])
+@pytest.mark.parametrize("N,K,gated", [(1376, 128, False), (1312, 128, False), (1376, 512, False), (1184, 128, True), (1184, 384, True)])
+def test_linear_many_rows_that_end_inside_a_tile(N, K, gated, out, kind):
+    """No residual; outputs in T and in 8 bits are those in f32, rounded, over and over."""
+    R = 4096
+    g = torch.Generator(device="cuda").manual_seed(N + K)
+    ctx = make_ctx("bf16")
+    make = lambda r, s: torch.randn(r, K, generator=g, device="cuda") * s
+    pack = torch_mx8 if kind == "mx8" else (lambda x: (x.bfloat16(), x.bfloat16().double()))
+    (xd, x), (wd, w) = pack(make(R, 1.0)), pack(make(N, 0.05))
+    (ud, u) = pack(make(N, 0.05)) if gated else (None, None)
+    op = jk.Linear(ctx, wd, w_up=ud)
+    y = torch.full((R, N), float("nan"), device="cuda")
+    ctx.linear(op, xd, y)
+    z, e = x @ w.T, (K + 4) * 2.0 ** -23 * (x.abs() @ w.abs().T)
+    if gated:
+        zu, eu = x @ u.T, (K + 4) * 2.0 ** -23 * (x.abs() @ u.abs().T)
+        z, e = z * zu, e * zu.abs() + z.abs() * eu + e * eu + 2.0 ** -23 * (z * zu).abs()
+    assert bool(((y.double() - z).abs() <= e + 2.0 ** -23 * z.abs()).all())
+    want = torch_mx8(y)[0].codes if out == "mx8" else y.bfloat16()
+    for _ in range(20):
+        o = jk.Mx8.empty(R, N) if out == "mx8" else torch.zeros(R, N, dtype=torch.bfloat16, device="cuda")
+        ctx.linear(op, xd, o)
+        assert torch.equal(o.codes if out == "mx8" else o, want)
+    assert ctx.read_status() == 0
