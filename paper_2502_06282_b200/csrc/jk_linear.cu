@@ -276,6 +276,7 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int spli
         }
         lin_out<T, 4>(a, y, r0 + r, n);
       }
+      __syncwarp();                        // (lin_out lets lanes without an output go)
       asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
       return;
     }

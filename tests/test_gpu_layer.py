@@ -912,3 +912,25 @@ def test_linear_many_rows_that_end_inside_a_tile(N, K, gated, out, kind):
         ctx.linear(op, xd, o)
         assert torch.equal(o.codes if out == "mx8" else o, want)
     assert ctx.read_status() == 0
+
+
+@pytest.mark.parametrize("R,N,K,gated", [(64, 500, 2048, False), (64, 500, 2048, True), (33, 90, 1024, True), (50, 161, 4096, False),
+                                         (20, 77, 2048, False), (30, 19, 1032, True)])
+def test_linear_f32_shared_tiles_with_lanes_past_the_outputs(R, N, K, gated):
+    """Against torch's product in 64 bits; sums of 32 products, then of those sums, within the bound of K + 4 roundings."""
+    g = torch.Generator(device="cuda").manual_seed(R + N)
+    ctx = make_ctx("f32")
+    x, w, u = (torch.randn(s, generator=g, device="cuda") for s in ((R, K), (N, K), (N, K)))
+    op, guard = jk.Linear(ctx, w, w_up=u if gated else None), Guard()
+    outs = [guard.alloc((R, N), torch.float32) for _ in range(3)]
+    for o in outs:
+        ctx.linear(op, x, o)
+    guard.check()
+    assert ctx.read_status() == 0 and torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    z = x.double() @ w.double().T
+    e = (K + 4) * 2.0 ** -24 * (x.abs().double() @ w.abs().double().T)
+    if gated:
+        zu = x.double() @ u.double().T
+        eu = (K + 4) * 2.0 ** -24 * (x.abs().double() @ u.abs().double().T)
+        z, e = z * zu, e * zu.abs() + z.abs() * eu + e * eu + 2.0 ** -24 * (z * zu).abs()
+    assert bool(((outs[0].double() - z).abs() <= e + 2.0 ** -23 * (z.abs() + e)).all())

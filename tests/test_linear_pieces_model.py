@@ -43,3 +43,11 @@ def test_pieces_are_written_when_their_stores_have_been_read(gated, out8):
         for tiles in ([2, 0], [0, 2], [2, 2], [0, 1, 2], [2, 1, 2, 0], [2, 2, 2]):
             for share in range(2):
                 run(tiles, n_out, n_tile, 8, gated, share, out8)
+
+
+def test_lanes_meet_before_an_aligned_cluster_barrier():
+    """The last outputs of a shared f32 tile leave lanes at different places; the barrier wants the warp together."""
+    text = (Path(__file__).resolve().parents[1] / "paper_2502_06282_b200" / "csrc" / "jk_linear.cu").read_text()
+    before = [re.sub(r"//[^\n]*", "", part).rstrip() for part in re.split(r'asm volatile\("barrier\.cluster\.arrive', text)[:-1]]
+    assert len(before) == 2
+    assert before[1].endswith("__syncwarp();")
