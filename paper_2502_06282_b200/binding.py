@@ -505,9 +505,10 @@ class Context:
             self._check(rc, "jk_linear")
 
     def rope_qkv(self, batch, n_tokens, qkv, pos, sections, rope_theta, q_out, k_out, v_out, first_row=None):
-        """jk_rope_qkv: qkv [batch * n_tokens rows, (Hq + 2 Hkv) d], rows evenly apart; pos i32 [batch, n_tokens,
-        axes] (one axis: [batch, n_tokens] too); sections the frequencies of each axis; q_out [batch, n_tokens, Hq,
-        d]; k_out, v_out [batch, Hkv, rows, d] with the same strides and dense rows; first_row i32 [batch]."""
+        """jk_rope_qkv: qkv [batch * n_tokens rows, (Hq + 2 Hkv) d], rows evenly apart; pos i32 [batch or more, n_tokens,
+        axes] or [batch * n_tokens, axes] (one axis: without it too); sections the frequencies of each axis; q_out [batch,
+        n_tokens, Hq, d]; k_out, v_out [batch or more, Hkv, rows, d] with the same strides and dense rows; first_row i32
+        [batch or more]."""
         rc = _calls.rope_qkv(self._h.value, self.is_bf16, *self.heads, batch, n_tokens, qkv, pos, sections, rope_theta, q_out,
                              k_out, v_out, first_row)
         if rc:

@@ -206,7 +206,6 @@ PyObject* rope_qkv(PyObject*, PyObject* const* a, Py_ssize_t count) {
       if (deep && B > 1 && M > 1 && qkv.stride(0) != M * stride) refuse("qkv: its rows do not lie evenly apart");
       if (stride < width) refuse("qkv: its rows overlap");
     }
-    if (!qkv.is_cuda()) refuse("qkv is not on a CUDA device");
     int32_t sections[16];
     PyObject* seq = PySequence_Fast(a[9], "sections: expected a sequence of counts");
     if (!seq) throw refused();
@@ -218,9 +217,18 @@ PyObject* rope_qkv(PyObject*, PyObject* const* a, Py_ssize_t count) {
     Py_DECREF(seq);
     if (PyErr_Occurred()) throw refused();
     if (axes > 16) refuse("sections: too many axes");
+    // (positions made for more tokens would be read at the wrong distance from the second sequence on; more sequences, as in
+    // k_out and first_row, do no harm)
+    if (a[8] != Py_None) {
+      const at::Tensor& t = tensor(a[8], "pos");
+      const int64_t dim = t.dim();
+      const bool deep = dim == 3 && t.size(0) >= B && t.size(1) == M && t.size(2) == axes;
+      const bool flat = dim == 2 && t.size(0) == n && t.size(1) == axes;
+      const bool one = axes == 1 && ((dim == 2 && t.size(0) >= B && t.size(1) == M) || (dim == 1 && t.size(0) == n));
+      if (!deep && !flat && !one) refuse("pos: expected a tensor [batch, n_tokens, axes], here [%lld, %lld, %zd]", (long long)B, (long long)M, axes);
+    }
+    if (!qkv.is_cuda()) refuse("qkv is not on a CUDA device");
     const int32_t* pos = ints(a[8], "pos", n * axes);
-    if (pos && THPVariable_Unpack(a[8]).dim() == 3 && THPVariable_Unpack(a[8]).size(2) != axes)
-      refuse("pos: expected %zd positions for each token", axes);
     const double theta = PyFloat_AsDouble(a[10]);
     if (theta == -1. && PyErr_Occurred()) throw refused();
     const at::Tensor& q = tensor(a[11], "q_out");

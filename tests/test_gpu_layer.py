@@ -934,3 +934,25 @@ def test_linear_f32_shared_tiles_with_lanes_past_the_outputs(R, N, K, gated):
         eu = (K + 4) * 2.0 ** -24 * (x.abs().double() @ u.abs().double().T)
         z, e = z * zu, e * zu.abs() + z.abs() * eu + e * eu + 2.0 ** -24 * (z * zu).abs()
     assert bool(((outs[0].double() - z).abs() <= e + 2.0 ** -23 * (z.abs() + e)).all())
+
+
+@pytest.mark.parametrize("sections", [(32,), (8, 24)])
+def test_rope_positions_of_each_shape(sections):
+    """Positions with and without the tokens in one line agree; those of a larger tree's buffer are refused whole and taken
+    sliced."""
+    B, M, Hq, Hkv, D, A = 2, 3, 4, 2, 64, len(sections)
+    T = dict(dtype=torch.bfloat16, device="cuda")
+    ctx = make_ctx("bf16", Hq, Hkv, D)
+    qkv, large = torch.randn(B, M, (Hq + 2 * Hkv) * D, **T), torch.randint(0, 4096, (B, M + 2, A), dtype=torch.int32, device="cuda")
+    new = lambda: [torch.zeros(s, **T) for s in ((B, M, Hq, D), (B, Hkv, 8, D), (B, Hkv, 8, D))]
+    pos = large[:, :M].contiguous()
+    shapes, outs = [pos, pos.view(B * M, A)] + ([pos.view(B, M), pos.view(-1)] if A == 1 else []), []
+    for p in shapes:
+        outs.append(new())
+        ctx.rope_qkv(B, M, qkv, p, sections, 1e4, *outs[-1])
+    for o in outs[1:]:
+        assert all(torch.equal(s, t) for s, t in zip(outs[0], o))
+    for p in [large, large.view(-1, A), large[:, :M]] + ([large.view(B, M + 2)] if A == 1 else []):
+        with pytest.raises(ValueError, match="pos"):
+            ctx.rope_qkv(B, M, qkv, p, sections, 1e4, *new())
+    assert ctx.read_status() == 0

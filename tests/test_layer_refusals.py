@@ -181,3 +181,20 @@ def test_binding_refuses_expanded_rows(lib):
         ctx.rope_qkv(B, M, bf(1, M, W).expand(B, M, W), **rest)
     with pytest.raises(ValueError, match="device"):
         ctx.rope_qkv(B, M, bf(B, M, W), **rest)
+
+
+@pytest.mark.parametrize("axes,shapes,bad", [
+    (1, ((2, 3, 1), (2, 3), (6, 1), (6,), (3, 3), (5, 3, 1)), ((2, 4, 1), (2, 4), (7,), (7, 1), (3, 2), (2, 1, 3), (1, 6), (8,), (2, 2), (2, 3, 2))),
+    (2, ((2, 3, 2), (6, 2), (3, 3, 2)), ((2, 4, 2), (7, 2), (2, 6), (2, 3), (12,), (14,), (2, 3, 3), (2, 2, 3), (3, 2, 2), (1, 2, 3, 2)))])
+def test_binding_takes_positions_of_the_call_s_shape(lib, axes, shapes, bad):
+    """Positions of more tokens than the call's are refused: read on as if dense, only the first sequence's would be right.
+    Those of more sequences are read as they lie.
+    (Tensors on the host: those of a right shape are refused for their device.)"""
+    ctx = make_ctx()
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    B, M, sections = 2, 3, (32,) if axes == 1 else (8, 24)
+    for group, match in ((shapes, "device"), (bad, "pos: expected a tensor")):
+        for s in group:
+            with pytest.raises(ValueError, match=match):
+                ctx.rope_qkv(B, M, bf(B, M, 8 * 64), torch.zeros(s, dtype=torch.int32), sections, 1e4, bf(B, M, 4, 64),
+                             bf(B, 2, 8, 64), bf(B, 2, 8, 64))
