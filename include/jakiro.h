@@ -649,7 +649,8 @@ int jk_linear(jk_ctx* ctx, void* stream, const jk_linear_op* host_op, int32_t ro
  *                or a negative position sets JK_ERR_BOUNDS, and that sequence's K and V (that
  *                token) are not written.
  * n_tokens up to 2^20, not bound to max_tree; batch up to 65535, not bound to max_batch.  Outputs
- * must not overlap qkv (JK_ERR_SHAPE), nor one another.
+ * must not overlap qkv, nor one another (JK_ERR_SHAPE); K and V may be parts of one buffer whose pieces of
+ * rows x d lie between one another.
  */
 int jk_rope_qkv(jk_ctx* ctx, void* stream, int32_t batch, int32_t n_tokens, const void* qkv,
                 int64_t row_stride, const int32_t* pos, int32_t n_axes, const int32_t* host_sections,

@@ -150,6 +150,18 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) k_rope_qkv(
   }
 }
 
+// Pieces of `part` bytes lie at i inner + j outer, 0 <= i < ni, 0 <= j < no, with inner >= part and outer >= (ni - 1) inner + part
+// where there is more than one: does one of them share a byte with one of those that lie `off` further?  The distance of
+// two pieces is off - i inner - j outer with |i| < ni, |j| < no, and only the two multiples next to what is left can come near.
+static bool rope_pieces_meet(int64_t off, int64_t part, int64_t inner, int64_t ni, int64_t outer, int64_t no) {
+  for (int64_t j = no > 1 ? off / outer : 0, last = j + 1; j <= last && j < no; ++j) {
+    const int64_t r = off > j * outer ? off - j * outer : j * outer - off;
+    for (int64_t i = ni > 1 ? r / inner : 0, end = i + 1; i <= end && i < ni; ++i)
+      if ((r > i * inner ? r - i * inner : i * inner - r) < part) return true;
+  }
+  return false;
+}
+
 extern "C" int jk_rope_qkv(jk_ctx* ctx, void* stream, int32_t batch, int32_t n_tokens, const void* qkv,
                            int64_t row_stride, const int32_t* pos, int32_t n_axes, const int32_t* sections,
                            float theta, void* q_out, void* k_out, void* v_out, int64_t sb, int64_t sh, int32_t rows,
@@ -185,7 +197,12 @@ extern "C" int jk_rope_qkv(jk_ctx* ctx, void* stream, int32_t batch, int32_t n_t
   const size_t in_b = ((tokens - 1) * row_stride + width) * es, q_b = tokens * Hq * D * es;
   const size_t kv_b = ((size_t)(batch - 1) * sb + (size_t)(Hkv - 1) * sh + (size_t)rows * D) * es;
   if (jk_overlap(q_out, q_b, qkv, in_b) || jk_overlap(k_out, kv_b, qkv, in_b) || jk_overlap(v_out, kv_b, qkv, in_b) ||
-      jk_overlap(q_out, q_b, k_out, kv_b) || jk_overlap(q_out, q_b, v_out, kv_b) || k_out == v_out)
+      jk_overlap(q_out, q_b, k_out, kv_b) || jk_overlap(q_out, q_b, v_out, kv_b))
+    return JK_ERR_SHAPE;
+  // (K and V may be halves of one buffer: their pieces may lie between one another)
+  const int64_t kv_off = (int64_t)((uintptr_t)k_out > (uintptr_t)v_out ? (uintptr_t)k_out - (uintptr_t)v_out : (uintptr_t)v_out - (uintptr_t)k_out);
+  const bool by_seq = batch == 1 || sb >= (Hkv - 1) * sh + part;
+  if (by_seq ? rope_pieces_meet(kv_off, part * es, sh * es, Hkv, sb * es, batch) : rope_pieces_meet(kv_off, part * es, sb * es, batch, sh * es, Hkv))
     return JK_ERR_SHAPE;
   if (!ctx->ws) return JK_ERR_WORKSPACE;
   int32_t* status = (int32_t*)(ctx->ws + ctx->lay.status);

@@ -956,3 +956,22 @@ def test_rope_positions_of_each_shape(sections):
         with pytest.raises(ValueError, match="pos"):
             ctx.rope_qkv(B, M, qkv, p, sections, 1e4, *new())
     assert ctx.read_status() == 0
+
+
+def test_rope_k_and_v_in_one_buffer():
+    """K and V as halves of one buffer, by sequence, by head and by rows; where they would share a row the call is refused."""
+    B, M, Hq, Hkv, D, rows = 3, 5, 4, 2, 64, 8
+    T = dict(dtype=torch.bfloat16, device="cuda")
+    ctx = make_ctx("bf16", Hq, Hkv, D)
+    qkv, q = torch.randn(B, M, (Hq + 2 * Hkv) * D, **T), torch.zeros(B, M, Hq, D, **T)
+    pos, first = torch.randint(0, 99, (B, M), dtype=torch.int32, device="cuda"), torch.tensor([0, 3, 1], dtype=torch.int32, device="cuda")
+    k, v = (torch.zeros(B, Hkv, rows, D, **T) for _ in range(2))
+    ctx.rope_qkv(B, M, qkv, pos, (D // 2,), 1e4, q, k, v, first_row=first)
+    a, b, c = torch.zeros(B, 2, Hkv, rows, D, **T), torch.zeros(B, Hkv, 2, rows, D, **T), torch.zeros(B, Hkv, 2 * rows, D, **T)
+    for k2, v2 in ((a[:, 0], a[:, 1]), (b[:, :, 0], b[:, :, 1]), (c[:, :, :rows], c[:, :, rows:])):
+        ctx.rope_qkv(B, M, qkv, pos, (D // 2,), 1e4, q, k2, v2, first_row=first)
+        assert torch.equal(k, k2) and torch.equal(v, v2)
+    for k2, v2 in ((c[:, :, :rows], c[:, :, 1:rows + 1]), (c[:, :, rows - 1:-1], c[:, :, :rows]), (c, c)):
+        with pytest.raises(RuntimeError, match="jk_rope_qkv"):
+            ctx.rope_qkv(B, M, qkv, pos, (D // 2,), 1e4, q, k2, v2, first_row=first)
+    assert ctx.read_status() == 0

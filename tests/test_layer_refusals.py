@@ -1,5 +1,6 @@
 """What the calls of a target layer refuse, before anything is launched (host only: no call here reaches a device)."""
 import ctypes as C
+import random
 
 import pytest
 import torch
@@ -198,3 +199,45 @@ def test_binding_takes_positions_of_the_call_s_shape(lib, axes, shapes, bad):
             with pytest.raises(ValueError, match=match):
                 ctx.rope_qkv(B, M, bf(B, M, 8 * 64), torch.zeros(s, dtype=torch.int32), sections, 1e4, bf(B, M, 4, 64),
                              bf(B, 2, 8, 64), bf(B, 2, 8, 64))
+
+
+def rope_code(lib, ctx, a):
+    s = a["sections"]
+    return lib.jk_rope_qkv(ctx._h, None, a["batch"], a["n"], a["qkv"], a["stride"], a["pos"], len(s), (C.c_int32 * len(s))(*s),
+                           a["theta"], a["q"], a["k"], a["v"], a["sb"], a["sh"], a["rows"], a["first"])
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(v=K + 16), "SHAPE"), (dict(v=K + 128), "SHAPE"), (dict(v=K - 128), "SHAPE"), (dict(v=K + 1280), "SHAPE"),
+    (dict(v=K + 5120 - 16), "SHAPE"), (dict(v=K + 5120), "WORKSPACE"), (dict(v=K - 5120), "WORKSPACE"),
+    # heads of K and V in turn: [batch, Hkv, 2, rows, d], [batch, 2, Hkv, rows, d], [2, Hkv, batch, rows, d]
+    (dict(sh=1280, sb=2560, v=K + 1280), "WORKSPACE"), (dict(sh=1280, sb=2560, v=K + 1280 - 16), "SHAPE"),
+    (dict(sh=1280, sb=2560, v=K + 1280 + 16), "SHAPE"), (dict(sh=640, sb=2560, v=K + 2560), "WORKSPACE"),
+    (dict(sh=640, sb=2560, v=K + 1280), "SHAPE"), (dict(sb=640, sh=1280, v=K + 5120), "WORKSPACE"), (dict(sb=640, sh=1280, v=K + 2560), "SHAPE"),
+    # rows of one buffer: the first ten are K's, the next V's
+    (dict(sh=1280, sb=2560, v=K + 10 * 128), "WORKSPACE"), (dict(sh=1280, sb=2560, v=K + 9 * 128), "SHAPE"),
+    (dict(batch=1, sb=0, v=K + 640), "SHAPE"), (dict(batch=1, sb=0, v=K + 2560), "WORKSPACE")])
+def test_rope_refuses_k_and_v_that_meet(lib, change, code):
+    assert rope_code(lib, make_ctx(), {**ROPE, **change}) == E[code]
+
+
+def test_rope_k_and_v_against_every_pair_of_pieces(lib):
+    """Random layouts of 2 heads and up to 5 sequences, with both nestings: what is refused is what shares a byte."""
+    rng, ctx, seen = random.Random(5), make_ctx(), set()
+    for _ in range(4000):
+        B, rows, es, d, Hkv = rng.randint(1, 5), rng.randint(3, 6), 2, 64, 2
+        part, gap = rows * d, lambda: 8 * rng.choice([0, 0, 1, rows * d // 8, rng.randint(0, 200)])
+        if rng.random() < 0.5:
+            sh = part + gap()
+            sb = sh + part + gap()
+        else:
+            sb = part + gap()
+            sh = (B - 1) * sb + part + gap()
+        off = 16 * rng.choice([rng.randint(-60, 60), rng.randint(-800, 800), rng.choice([-1, 1]) * sb * es // 16, sh * es // 16,
+                               part * es // 16 + rng.randint(-2, 2)])
+        at = [(b * sb + h * sh) * es for b in range(B) for h in range(Hkv)]
+        meet = any(abs(off + v - k) < part * es for v in at for k in at)
+        code = rope_code(lib, ctx, {**ROPE, "batch": B, "rows": rows, "sb": sb, "sh": sh, "v": K + off})
+        assert code == E["SHAPE" if meet else "WORKSPACE"], (B, rows, sb, sh, off)
+        seen.add((meet, sb > sh))
+    assert len(seen) == 4
