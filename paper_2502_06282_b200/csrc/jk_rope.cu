@@ -185,6 +185,8 @@ extern "C" int jk_rope_qkv(jk_ctx* ctx, void* stream, int32_t batch, int32_t n_t
   if (row_stride == 0) row_stride = width;
   if (row_stride < width || row_stride > ((int64_t)1 << 31)) return JK_ERR_SHAPE;
   const int64_t part = (int64_t)rows * D;              // heads within a sequence, or sequences within a head
+  if (Hkv == 1) sh = part;                             // (the stride of a dimension of one does not count)
+  if (batch == 1) sb = Hkv * part;
   if (sh < part || sh > ((int64_t)1 << 40) || sb < 0 || sb > ((int64_t)1 << 40)) return JK_ERR_SHAPE;
   if (batch > 1 && sb < (Hkv - 1) * sh + part && (sb < part || sh < (batch - 1) * sb + part)) return JK_ERR_SHAPE;
   const int es = jk_elem_size(c.dtype);

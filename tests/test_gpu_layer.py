@@ -975,3 +975,18 @@ def test_rope_k_and_v_in_one_buffer():
         with pytest.raises(RuntimeError, match="jk_rope_qkv"):
             ctx.rope_qkv(B, M, qkv, pos, (D // 2,), 1e4, q, k2, v2, first_row=first)
     assert ctx.read_status() == 0
+
+
+def test_rope_one_head_of_k_and_v_of_any_stride():
+    """One KV head, its rows [batch, rows, 1, d] seen as [batch, 1, rows, d]: the stride of the dimension of one is d."""
+    B, M, Hq, D, rows = 2, 5, 4, 64, 8
+    T = dict(dtype=torch.bfloat16, device="cuda")
+    ctx = make_ctx("bf16", Hq, 1, D)
+    qkv, q = torch.randn(B, M, (Hq + 2) * D, **T), torch.zeros(B, M, Hq, D, **T)
+    pos = torch.randint(0, 99, (B, M), dtype=torch.int32, device="cuda")
+    a, b = ([torch.zeros(s, **T) for _ in range(2)] for s in ((B, 1, rows, D), (B, rows, 1, D)))
+    ctx.rope_qkv(B, M, qkv, pos, (D // 2,), 1e4, q, *a)
+    ctx.rope_qkv(B, M, qkv, pos, (D // 2,), 1e4, q, *(t.as_strided((B, 1, rows, D), (rows * D, D, D, 1)) for t in b))
+    for s, t in zip(a, b):
+        assert torch.equal(s[:, 0], t[:, :, 0]) and bool(s[:, :, :M].any())
+    assert ctx.read_status() == 0

@@ -241,3 +241,11 @@ def test_rope_k_and_v_against_every_pair_of_pieces(lib):
         assert code == E["SHAPE" if meet else "WORKSPACE"], (B, rows, sb, sh, off)
         seen.add((meet, sb > sh))
     assert len(seen) == 4
+
+
+@pytest.mark.parametrize("change,code", [(dict(sh=64), "WORKSPACE"), (dict(sh=0), "WORKSPACE"), (dict(sh=-4, sb=640), "WORKSPACE"),
+                                         (dict(sh=64, sb=632), "SHAPE"), (dict(batch=1, sb=-1, sh=3), "WORKSPACE"), (dict(sh=64, v=K + 128), "SHAPE")])
+def test_rope_takes_any_stride_of_a_dimension_of_one(lib, change, code):
+    ctx = jk.Context(hidden=8, n_experts=1, top_k=1, inter=8, vocab=8, n_q_heads=4, n_kv_heads=1, head_dim=64, max_batch=1,
+                     max_tree=1, max_depth=1, max_frontier=1, k_per_expert=1, dtype="bf16", allocate=False)
+    assert rope_code(lib, ctx, {**ROPE, **change}) == E[code]
