@@ -77,16 +77,16 @@ class JkLinearOp(C.Structure):
 JK_ROWS_T, JK_ROWS_F32, JK_ROWS_MX8 = 0, 1, 2
 ACTS = {"none": 0, "silu": 1, "gelu": 2}
 
-_lib = _calls = None                      # the library; its target layer's calls with the checks of their tensors
+_lib = _calls = None                      # the library; its target layer's calls with the checks of their tensors (_layer_calls)
 
 
 def lib() -> C.CDLL:
     """The loaded shared library.  Raises if it has not been built."""
-    global _lib, _calls
+    global _lib
     if _lib is None:
-        if not os.path.exists(LIB_PATH) or not os.path.exists(CALLS_PATH):
+        if not os.path.exists(LIB_PATH):
             raise RuntimeError(
-                f"{LIB_PATH} or {CALLS_PATH} is missing: build them with `python -m paper_2502_06282_b200.build` "
+                f"{LIB_PATH} is missing: build it with `python -m paper_2502_06282_b200.build` "
                 "(needs nvcc); there is no fallback implementation")
         L = C.CDLL(LIB_PATH)
         vp, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
@@ -149,10 +149,25 @@ def lib() -> C.CDLL:
                 getattr(L, name).restype = C.c_int
         L.jk_paged_scratch_ints.restype = i64
         L.jk_row_scale_bytes.restype = i64
-        from . import _calls as calls
-        calls.bind(*(C.cast(f, vp).value for f in (L.jk_add_norm, L.jk_quantize_rows, L.jk_linear, L.jk_rope_qkv)), Mx8)
-        _lib, _calls = L, calls
+        _lib = L
     return _lib
+
+
+def _layer_calls():
+    """The compiled extension through which add_norm, quantize_mx8, linear and rope_qkv are called, loaded at the first of them:
+    it is tied to one Python and one torch, which nothing else here is."""
+    global _calls
+    if _calls is None:
+        L, again = lib(), "build it with `python -m paper_2502_06282_b200.build` (needs g++)"
+        if not os.path.exists(CALLS_PATH):
+            raise RuntimeError(f"{CALLS_PATH} is missing: {again}; there is no fallback implementation")
+        try:
+            from . import _calls as calls
+        except ImportError as e:
+            raise RuntimeError(f"{CALLS_PATH} does not load ({e}): {again}") from e
+        calls.bind(*(C.cast(f, C.c_void_p).value for f in (L.jk_add_norm, L.jk_quantize_rows, L.jk_linear, L.jk_rope_qkv)), Mx8)
+        _calls = calls
+    return _calls
 
 
 class JakiroError(RuntimeError):
@@ -485,13 +500,13 @@ class Context:
 
     def add_norm(self, x, weight=None, delta=None, out_sum=None, out=None, out_mx8: "Optional[Mx8]" = None):
         """jk_add_norm: x, delta, out_sum, out [rows, n] dense, weight [n], out_mx8 an Mx8 of [rows, n]."""
-        rc = _calls.add_norm(self._h.value, self.is_bf16, x, weight, delta, out_sum, out, out_mx8)
+        rc = (_calls or _layer_calls()).add_norm(self._h.value, self.is_bf16, x, weight, delta, out_sum, out, out_mx8)
         if rc:
             self._check(rc, "jk_add_norm")
 
     def quantize_mx8(self, x, out: "Mx8"):
         """jk_quantize_rows: x [rows, n] (rows may lie apart) to an Mx8 of the same shape."""
-        rc = _calls.quantize(self._h.value, self.is_bf16, x, out)
+        rc = (_calls or _layer_calls()).quantize(self._h.value, self.is_bf16, x, out)
         if rc:
             self._check(rc, "jk_quantize_rows")
 
@@ -500,7 +515,7 @@ class Context:
         or Mx8), residual T [rows, n_out] or None; out may be the residual itself."""
         if op.kind is not self.tdtype:
             raise ValueError("the projection was made for a context of another type")
-        rc = _calls.linear(self._h.value, self.is_bf16, op.address, x, out, residual)
+        rc = (_calls or _layer_calls()).linear(self._h.value, self.is_bf16, op.address, x, out, residual)
         if rc:
             self._check(rc, "jk_linear")
 
@@ -509,7 +524,7 @@ class Context:
         axes] or [batch * n_tokens, axes] (one axis: without it too); sections the frequencies of each axis; q_out [batch,
         n_tokens, Hq, d]; k_out, v_out [batch or more, Hkv, rows, d] with the same strides and dense rows; first_row i32
         [batch or more]."""
-        rc = _calls.rope_qkv(self._h.value, self.is_bf16, *self.heads, batch, n_tokens, qkv, pos, sections, rope_theta, q_out,
+        rc = (_calls or _layer_calls()).rope_qkv(self._h.value, self.is_bf16, *self.heads, batch, n_tokens, qkv, pos, sections, rope_theta, q_out,
                              k_out, v_out, first_row)
         if rc:
             self._check(rc, "jk_rope_qkv")

@@ -10,6 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libjakiro.so")
 CALLS = os.path.join(HERE, "_calls.so")
+BUILD_DIR = os.path.join(HERE, "_build")
+CALLS_FOR = os.path.join(BUILD_DIR, "calls_built_for")     # the versions that _calls.so was built for
 SOURCES = ["jk_api.cu", "jk_expand.cu", "jk_gemm_tc.cu", "jk_attn.cu", "jk_attn_tc.cu", "jk_attn_sk.cu", "jk_attn_cl.cu",
            "jk_accept.cu", "jk_pre.cu", "jk_paged.cu", "jk_paged_attn.cu", "jk_paged_tc.cu", "jk_sample.cu",
            "jk_norm.cu", "jk_rope.cu", "jk_linear.cu", "jk_linear_tc.cu", "jk_linear_pair.cu"]
@@ -22,12 +24,30 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found")
 
 
-def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
+def _older(target: str, sources) -> bool:
+    """Is the target missing, or older than one of its sources?"""
+    return not os.path.exists(target) or any(os.path.getmtime(d) > os.path.getmtime(target) for d in sources)
+
+
+def _built_for() -> str:
+    """What _calls.so holds for: it is tied to one Python and one torch, the library to neither."""
+    import torch
+    return f"{sys.implementation.cache_tag} {torch.__version__} {int(torch._C._GLIBCXX_USE_CXX11_ABI)}\n"
+
+
+def library_needs_build() -> bool:
+    return _older(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != "jk_calls.cpp"] + [os.path.join(INCLUDE, "jakiro.h")])
+
+
+def calls_need_build() -> bool:
+    if _older(CALLS, [os.path.join(CSRC, "jk_calls.cpp"), os.path.join(INCLUDE, "jakiro.h")]) or not os.path.exists(CALLS_FOR):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, "jakiro.h")]
-    return any(os.path.getmtime(d) > t for d in deps)
+    with open(CALLS_FOR) as f:
+        return f.read() != _built_for()
+
+
+def needs_build() -> bool:
+    return library_needs_build() or calls_need_build()
 
 
 def _calls_command() -> list:
@@ -43,30 +63,38 @@ def _calls_command() -> list:
             + [f"-l{n}" for n in ("torch_python", "torch_cpu", "c10", "c10_cuda")])
 
 
+def _finish(name: str, p: subprocess.Popen, verbose: bool) -> None:
+    out, _ = p.communicate()
+    if verbose or p.returncode:
+        sys.stderr.write(out.decode())
+    if p.returncode:
+        raise RuntimeError(f"the compiler failed on {name}")
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not needs_build():
-        return LIB
-    build_dir = os.path.join(HERE, "_build")
-    os.makedirs(build_dir, exist_ok=True)
-    common = [_nvcc(), "-std=c++17", "-O3", "-lineinfo", "-gencode",
-              "arch=compute_100a,code=sm_100a", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
-    if verbose:
-        common += ["-Xptxas", "-v"]
-    objs = []
+    """Builds what is missing, older than its sources or, of _calls.so, made for another Python or torch.  The library is
+    there, and all calls but the target layer's work from Python, even where _calls.so cannot be built."""
+    library, calls = force or library_needs_build(), force or calls_need_build()
+    os.makedirs(BUILD_DIR, exist_ok=True)
+    pipes = dict(stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
     procs = []
-    for src in SOURCES:
-        obj = os.path.join(build_dir, src.replace(".cu", ".o"))
-        objs.append(obj)
-        procs.append((src, subprocess.Popen(common + ["-c", os.path.join(CSRC, src), "-o", obj],
-                                            stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
-    procs.append(("jk_calls.cpp", subprocess.Popen(_calls_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+    if library:
+        common = [_nvcc(), "-std=c++17", "-O3", "-lineinfo", "-gencode",
+                  "arch=compute_100a,code=sm_100a", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
+        if verbose:
+            common += ["-Xptxas", "-v"]
+        objs = [os.path.join(BUILD_DIR, src.replace(".cu", ".o")) for src in SOURCES]
+        procs = [(src, subprocess.Popen(common + ["-c", os.path.join(CSRC, src), "-o", obj], **pipes))
+                 for src, obj in zip(SOURCES, objs)]
+    extension = subprocess.Popen(_calls_command(), **pipes) if calls else None
     for src, p in procs:
-        out, _ = p.communicate()
-        if verbose or p.returncode:
-            sys.stderr.write(out.decode())
-        if p.returncode:
-            raise RuntimeError(f"the compiler failed on {src}")
-    subprocess.check_call([_nvcc(), "-shared", "-o", LIB] + objs + ["-cudart", "static"])
+        _finish(src, p, verbose)
+    if library:
+        subprocess.check_call([_nvcc(), "-shared", "-o", LIB] + objs + ["-cudart", "static"])
+    if calls:
+        _finish("jk_calls.cpp", extension, verbose)
+        with open(CALLS_FOR, "w") as f:
+            f.write(_built_for())
     return LIB
 
 

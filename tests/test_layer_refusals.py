@@ -1,6 +1,7 @@
 """What the calls of a target layer refuse, before anything is launched (host only: no call here reaches a device)."""
 import ctypes as C
 import random
+import sys
 
 import pytest
 import torch
@@ -249,3 +250,34 @@ def test_rope_takes_any_stride_of_a_dimension_of_one(lib, change, code):
     ctx = jk.Context(hidden=8, n_experts=1, top_k=1, inter=8, vocab=8, n_q_heads=4, n_kv_heads=1, head_dim=64, max_batch=1,
                      max_tree=1, max_depth=1, max_frontier=1, k_per_expert=1, dtype="bf16", allocate=False)
     assert rope_code(lib, ctx, {**ROPE, **change}) == E[code]
+
+
+def test_library_loads_without_the_extension(lib, monkeypatch, tmp_path):
+    """Only the target layer's four calls need it: without it, or with one that does not load, the rest is there and they
+    say what is missing."""
+    monkeypatch.setattr(jk, "_lib", None)
+    monkeypatch.setattr(jk, "_calls", None)
+    monkeypatch.setattr(jk, "CALLS_PATH", str(tmp_path / "none.so"))
+    assert jk.lib().jk_row_scale_bytes(1, 32) == 512
+    ctx, x = make_ctx(), torch.zeros(4, 64, dtype=torch.bfloat16)
+    with pytest.raises(RuntimeError, match="none.so is missing"):
+        ctx.add_norm(x, out=x)
+    monkeypatch.undo()
+    with pytest.raises(ValueError):                        # (the extension is there again, and refuses host tensors)
+        ctx.add_norm(x, out=x)
+
+
+def test_extension_that_does_not_load_is_named(lib, monkeypatch):
+    import paper_2502_06282_b200 as package
+    monkeypatch.setattr(jk, "_calls", None)
+    monkeypatch.delattr(package, "_calls", raising=False)
+    monkeypatch.setitem(sys.modules, "paper_2502_06282_b200._calls", None)
+    with pytest.raises(RuntimeError, match="_calls.so does not load"):
+        make_ctx().quantize_mx8(None, None)
+
+
+def test_extension_is_built_again_for_another_torch(lib, monkeypatch):
+    from paper_2502_06282_b200 import build
+    assert not build.needs_build()
+    monkeypatch.setattr(build, "_built_for", lambda: "another\n")
+    assert build.needs_build() and build.calls_need_build() and not build.library_needs_build()
