@@ -622,7 +622,9 @@ typedef struct {
  *                (0 = n_out), or mx8 (dense, with out_scale; n_out a multiple of 32)
  * n_in is a multiple of 8 (T) or 32 (mx8) up to 131072, n_out any number up to 2^20, rows up to
  * 2^20; rows of x are 16-byte aligned.  Products are exact and summed in f32 (f32 contexts: f32
- * multiply-adds), the epilogue is f32, y is rounded once.  out may be residual itself (same
+ * multiply-adds), the epilogue is f32, y is rounded once.  SiLU and GELU: within a few units of f32 on CUDA
+ * cores; on the tensor cores within 2^-18 of their value, which f32 outputs show (GELU of 16- and 8-bit
+ * outputs: 2^-16).  out may be residual itself (same
  * stride), or columns of one buffer of which x and residual are others; any overlap of out with an
  * input is refused (JK_ERR_SHAPE).  bf16 contexts and mx8 operands run on the tensor cores while the
  * tensor path is on (mx8: in bf16 contexts).  After JK_ERR_TIMEOUT in the status, set the workspace

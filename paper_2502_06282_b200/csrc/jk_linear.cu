@@ -306,12 +306,12 @@ __global__ void __launch_bounds__(256) k_linear_block(const lin_args a, int spli
 
 // Up to 16 rows, while a scale block's outputs need not meet: warps of outputs, of two each where there are more than the SMs
 // hold at a time (16 x 1928 x 4250 31.2 us with one, 17.8 with two, 1 x 4096 x 4096 15.0 and 12.3, 5 x 8192 x 8192 80
-// and 86, 16 x 512 x 512 2.5 and 3.0; gated, where two are four rows of weights, 5.8 and 9.1 for 16 x 512 x 1376).  Up to 32, blocks of 32 rows with up to 8 to
+// and 86, 16 x 512 x 512 2.5 and 3.0; gated, where two are four rows of weights, 5.8 and 9.1 for 16 x 1376 x 512).  Up to 32, blocks of 32 rows with up to 8 to
 // a tile.  Else blocks of 128 or of 64 rows, the latter with 1 to 8 to a tile, by what the SM with the most of them needs:
 // a step of 16 along k takes a block of 128 rows 1.63 us, one of 64 rows 1.13 us alone on its SM and 0.98 next to another.
 // Measured in f32, us, with 128 rows / 64 / 64 shared by 2: 1024 x 4096 x 4096 837 / 992 / 872, 256 x 4096 x 4096 417 / 289 /
 // 257, 313 x 9352 x 3456 gated 1803 / 1151 / 1143; the whole range against CUDA 12.9's library, which makes the products
-// alone: 16 x 512 x 1376 gated 5.8 (31), 60 x 4096 x 4096 68 (88), 1024 x 4096 x 4096 837 (626).
+// alone: 16 x 1376 x 512 gated 5.8 (31), 60 x 4096 x 4096 68 (88), 1024 x 4096 x 4096 837 (626).
 template <typename TX, typename T>
 static void launch_cc(cudaStream_t st, const lin_args& a, int sms) {
   const bool gated = a.w_up != nullptr;

@@ -23,7 +23,8 @@
 //
 // Bound by the tensor cores and the power they take: 2047 rows, 5120 x 5120 in bf16 79 us on a cool card (1360 TFLOP/s), 87 to
 // 92 back to back, where the clock falls to 1.5 GHz; 4099 rows, 14336 x 4096 gated in 8 bits 365 us (2640), 430 back to
-// back.  480 rows, 5120 x 13824 in 8 bits 40 us (1690): 40 tiles among 74 pairs, of which the hand-over takes 13.
+// back.  480 rows, 5120 x 13824 in 8 bits 40 us (1690), 42 to 48 back to back: 40 tiles among 74 pairs, of which the hand-over
+// takes 13.
 #include <type_traits>
 
 #include "jk_linear_tc.cuh"

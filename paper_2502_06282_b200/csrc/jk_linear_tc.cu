@@ -16,9 +16,9 @@
 // cluster of 2, 4 or 8 CTAs for each, whose sums pass through the cluster's shared memory.  Sums are formed in
 // the same order on every run.
 //
-// Bound by the weights' way from memory: 60 rows, 11008 x 4096 gated in bf16 33 us (5.5 TB/s), 1 row 14336 x 4096 gated in
-// 8 bits 19.4 us (6.25 TB/s); short calls by the gap between launches (1.2 us), the first boxes (1.3) and the
-// hand-over: 60 rows 4096 x 4096 9.7 us (3.5 TB/s).
+// Bound by the weights' way from memory: 60 rows, 11008 x 4096 gated in bf16 32 to 37 us (5.6 to 4.9 TB/s), 1 row 14336 x 4096
+// gated in 8 bits 19.4 to 21.3 us (6.25 to 5.7); short calls by the gap between launches (1.2 us), the first boxes (1.3) and
+// the hand-over: 60 rows 4096 x 4096 9.7 to 10.7 us (3.5 to 3.2 TB/s).
 //
 // Roles: warp 0 loads (TMA), warp 1 issues products, warps 2-17 drain accumulators and do the epilogue.  Every
 // wait is bounded: after about 2 s it records JK_ERR_TIMEOUT, the CTA lets its copies land, frees its

@@ -7,8 +7,8 @@
 // holds pieces of 8 consecutive elements; four neighbouring lanes make a scale block of 32, whose
 // largest element takes two shuffles.
 //
-// Bound by memory: 8191 rows of 8192 with sum and 8-bit rows, 472 MB in 81 us (5.8 TB/s); 240 rows of 4096 2.8 us and one row
-// 1.8 us are a launch, a chain of two loads and a reduction.
+// Bound by memory: 8191 rows of 8192 with sum and 8-bit rows, 472 MB in 75 to 83 us (6.3 to 5.7 TB/s); 240 rows of 4096 2.8 us and
+// one row 1.8 us, replayed from a graph, are a launch, a chain of two loads and a reduction.
 #include "jk_mx8.cuh"
 
 // ------------------------------------------------------------------------------------------ pieces
